@@ -265,6 +265,165 @@ int rtopk_aggregate_update_momentum(const uint32_t *idx, const float *val,
                                     float eta, float scale, float mu,
                                     float *omega, float *velocity, void *stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * Matrix parameters: what stands before and after the sparse exchange in a
+ * training step. A layer's products in 8-bit integers give its outputs and the
+ * binary32 gradient that rtopk_encode takes; the master's step below moves a
+ * matrix by its orthogonalised momentum. Matrices are row-major, `ld` is the
+ * distance of their rows in elements.
+ * ---------------------------------------------------------------------------
+ */
+#define RTOPK_F32 0
+#define RTOPK_BF16 1
+#define RTOPK_F16 2
+
+#define RTOPK_ROWS 0
+#define RTOPK_COLUMNS 1
+
+/*
+ * Quantisation to 8 bits with a scale for each row (a token, an output
+ * channel) or for each column:
+ *     scale = max |x| / 127,  q = round to nearest, ties to even (x / scale)
+ * both divisions binary32. Along RTOPK_ROWS, q is [rows][ldq] as x is, scale
+ * [rows]. Along RTOPK_COLUMNS the matrix is also turned over, q is [cols][ldq]
+ * with the rows of x along its rows, scale [cols]: the contraction of a
+ * gradient runs over the tokens, and the product below over rows.
+ * A row (column) whose scale would be below 2^-126 gets scale 0 and numbers 0;
+ * one that holds an infinity or a not-a-number gets scale NaN and numbers 0,
+ * so that everything it goes into is NaN.
+ *
+ * x      device, [rows][ldx] of `type`; any alignment of its elements' size,
+ *        16-byte aligned rows are read fastest
+ * rows   0 .. 2^22 (0: nothing to do along rows, scales 0 along columns)
+ * cols   1 .. 2^22; cols <= ldx <= 2^22
+ * q      device; what lies between the numbers and ldq is not written. Rows
+ *        that start on 16 bytes (base and ldq) let the product load them
+ *        directly
+ * workspace  device, 256-byte aligned, >= rtopk_quantize_i8_workspace_bytes
+ *        (0 along rows)
+ */
+int rtopk_quantize_i8_workspace_bytes(uint64_t rows, uint64_t cols, int along, uint64_t *bytes);
+int rtopk_quantize_i8(const void *x, int type, uint64_t rows, uint64_t cols, uint64_t ldx,
+                      int along, int8_t *q, uint64_t ldq, float *scale,
+                      void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * out[i][j] = a_scale[i] * b_scale[j] * sum_k a[i][k] * b[j][k] + bias[j].
+ * The sums are exact (any of -128 .. 127); they are rounded to binary32 once,
+ * then take the scales and the bias in binary32, and the type of `out`.
+ *
+ * a      device, [m][lda] int8; a_scale device, [m]
+ * b      device, [n][ldb] int8; b_scale device, [n]
+ * bias   device, [n] binary32, or null
+ * m, n, k  0 .. 2^22 (k = 0: out is the bias), lda, ldb <= 2^22
+ * out    device, [m][ldo] of out_type; must not overlap an input
+ * workspace  device, 256-byte aligned, >= rtopk_matmul_i8_workspace_bytes
+ */
+int rtopk_matmul_i8_workspace_bytes(uint64_t m, uint64_t n, uint64_t k, uint64_t *bytes);
+int rtopk_matmul_i8(const int8_t *a, const float *a_scale, const int8_t *b, const float *b_scale,
+                    const float *bias, uint64_t m, uint64_t n, uint64_t k,
+                    uint64_t lda, uint64_t ldb, void *out, int out_type, uint64_t ldo,
+                    void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * A layer's forward product: x quantised by row (token) as rtopk_quantize_i8
+ * does, times weights that are quantised already: out = x w^T + bias.
+ *
+ * x      device, [m][ldx] of `type`, m tokens (0 .. 2^22) of k numbers
+ * w      device, [n][ldw] int8, a row for each output channel; w_scale [n]
+ * the rest as above; both calls' sizes limit as rtopk_matmul_i8's do, k and n
+ * are at least 1
+ */
+int rtopk_linear_i8_workspace_bytes(uint64_t m, uint64_t k, uint64_t n, uint64_t *bytes);
+int rtopk_linear_i8(const void *x, int type, uint64_t m, uint64_t k, uint64_t ldx,
+                    const int8_t *w, const float *w_scale, uint64_t n, uint64_t ldw,
+                    const float *bias, void *out, int out_type, uint64_t ldo,
+                    void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * Its backward products, the gradients passed straight through the rounding:
+ *     dx = dy w        dy quantised by row, w by column
+ *     dw = dy^T x      both quantised by column (over the tokens)
+ *     db = sum of dy's rows, in binary32 or more
+ *
+ * dy, x  device, [m][lddy] and [m][ldx] of `type`
+ * w_turned, w_turned_scale  device, [k][ldw] int8 and [k]: the weights [n][k]
+ *        quantised along RTOPK_COLUMNS
+ * dx     device, [m][lddx] of `type`, or null
+ * dw     device, [n][lddw] binary32, or null (then x is not read): with
+ *        lddw = k the gradient as rtopk_encode takes it
+ * db     device, [n] binary32, or null; only with dw
+ * m = 0 writes zeros to dw and db
+ */
+int rtopk_linear_i8_backward_workspace_bytes(uint64_t m, uint64_t k, uint64_t n, uint64_t *bytes);
+int rtopk_linear_i8_backward(const void *dy, const void *x, int type,
+                             uint64_t m, uint64_t k, uint64_t n, uint64_t lddy, uint64_t ldx,
+                             const int8_t *w_turned, const float *w_turned_scale, uint64_t ldw,
+                             void *dx, uint64_t lddx, float *dw, uint64_t lddw, float *db,
+                             void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * Orthogonalises `count` matrices of equal shape: with X = G / (|G|_F + eps),
+ * turned over if G has more rows than columns, each step takes its three
+ * coefficients (a, b, c) and
+ *     A = X X^T,  X <- a X + (b A + c A A) X
+ * which moves every singular value s of X to a s + b s^3 + c s^5 and leaves
+ * the singular vectors. (3.4445, -4.7750, 2.0315) five times is in common use
+ * for updates of neural networks. Members are independent of each other, up to
+ * 16 share launches.
+ *
+ * products  RTOPK_PRODUCTS_PAIRS: numbers between the products are pairs of
+ *        halves (22 bits), each product is three half products: as exact as
+ *        binary32. RTOPK_PRODUCTS_HALVES: halves (11 bits, three more than
+ *        bfloat16 has), a third of the time
+ * x      HOST array of device pointers to [rows][ldx] of `type`
+ * out    HOST array of device pointers to [rows][ldo] of out_type; may be x
+ * rows, cols  1 .. 2^21, rows * cols < 2^32
+ * coefficients  HOST, [steps][3], 1 <= steps <= 64, read during the call. If
+ *        singular values that start in [0, 1] can pass 7.5 (or what b A + c A A
+ *        holds 60), the call returns RTOPK_EINVAL
+ * eps    >= 0. A matrix of zeros gives zeros (eps = 0 too); one that holds an
+ *        infinity or a not-a-number gives NaN everywhere
+ * workspace  device, 256-byte aligned, >= rtopk_orthogonalize_workspace_bytes
+ */
+#define RTOPK_PRODUCTS_PAIRS 0
+#define RTOPK_PRODUCTS_HALVES 1
+int rtopk_orthogonalize_workspace_bytes(uint32_t count, uint64_t rows, uint64_t cols, int products,
+                                        uint64_t *bytes);
+int rtopk_orthogonalize(uint32_t count, const void *const *x, int type,
+                        uint64_t rows, uint64_t cols, uint64_t ldx,
+                        uint32_t steps, const float *coefficients, float eps, int products,
+                        void *const *out, int out_type, uint64_t ldo,
+                        void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * The master's step for `count` matrix parameters of equal shape, each with
+ * messages of its own from n workers, indices counted along the flat matrix:
+ *     average  = (1/n) sum of the messages, as rtopk_aggregate forms it
+ *     u        = scale * average
+ *     velocity = mu * velocity + u
+ *     G        = mu * velocity + u (nesterov != 0), or velocity
+ *     omega    = (1 - eta * decay) * omega - eta * gain * orthogonalised(G)
+ * u rounded, the next two fused multiply-adds; keep = 1 - eta * decay and
+ * step = eta * gain rounded to binary32, omega = fma(-step, O, keep * omega).
+ *
+ * idx, val         HOST arrays of device pointers, each [n*k] as for
+ *                  rtopk_aggregate with d = rows * cols
+ * omega, velocity  HOST arrays of device pointers, [rows * cols] binary32,
+ *                  updated in place; no two of them may overlap
+ * the rest as for rtopk_orthogonalize
+ */
+int rtopk_aggregate_update_orthogonal_workspace_bytes(uint32_t count, uint64_t rows, uint64_t cols,
+                                                      int products, uint64_t *bytes);
+int rtopk_aggregate_update_orthogonal(uint32_t count, const uint32_t *const *idx,
+                                      const float *const *val, uint32_t n, uint64_t k,
+                                      uint64_t rows, uint64_t cols, float eta, float scale,
+                                      float mu, int nesterov, float decay, float gain,
+                                      uint32_t steps, const float *coefficients, float eps,
+                                      int products, float *const *omega, float *const *velocity,
+                                      void *workspace, uint64_t workspace_bytes, void *stream);
+
 const char *rtopk_strerror(int code);
 
 /* Library version: major * 10000 + minor * 100 + patch. */

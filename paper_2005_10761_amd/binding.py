@@ -18,6 +18,12 @@ EXPORTS = ("rtopk_encode_workspace_bytes", "rtopk_aggregate_workspace_bytes", "r
            "rtopk_encode_batch", "rtopk_encode_batch_device_step",
            "rtopk_aggregate", "rtopk_aggregate_update", "rtopk_aggregate_update_workspace_bytes",
            "rtopk_aggregate_update_momentum", "rtopk_aggregate_update_static",
+           "rtopk_quantize_i8_workspace_bytes", "rtopk_quantize_i8",
+           "rtopk_matmul_i8_workspace_bytes", "rtopk_matmul_i8",
+           "rtopk_linear_i8_workspace_bytes", "rtopk_linear_i8",
+           "rtopk_linear_i8_backward_workspace_bytes", "rtopk_linear_i8_backward",
+           "rtopk_orthogonalize_workspace_bytes", "rtopk_orthogonalize",
+           "rtopk_aggregate_update_orthogonal_workspace_bytes", "rtopk_aggregate_update_orthogonal",
            "rtopk_strerror", "rtopk_version")
 # ... and include/rtopk_diag.h
 DIAG_EXPORTS = ("rtopk_encode_stats", "rtopk_trace_next_encode", "rtopk_force_next_encode",
@@ -86,6 +92,25 @@ def load_library() -> ctypes.CDLL:
     L.rtopk_trace_next_encode.restype = ctypes.c_int
     L.rtopk_force_next_encode.argtypes = [ctypes.c_uint]
     L.rtopk_force_next_encode.restype = ctypes.c_int
+    i32, f32, pu64 = ctypes.c_int, ctypes.c_float, ctypes.POINTER(u64)
+    for name, args in {
+            "rtopk_quantize_i8_workspace_bytes": [u64, u64, i32, pu64],
+            "rtopk_quantize_i8": [vp, i32, u64, u64, u64, i32, vp, u64, vp, vp, u64, vp],
+            "rtopk_matmul_i8_workspace_bytes": [u64, u64, u64, pu64],
+            "rtopk_matmul_i8": [vp, vp, vp, vp, vp, u64, u64, u64, u64, u64, vp, i32, u64, vp, u64, vp],
+            "rtopk_linear_i8_workspace_bytes": [u64, u64, u64, pu64],
+            "rtopk_linear_i8": [vp, i32, u64, u64, u64, vp, vp, u64, u64, vp, vp, i32, u64, vp, u64, vp],
+            "rtopk_linear_i8_backward_workspace_bytes": [u64, u64, u64, pu64],
+            "rtopk_linear_i8_backward": [vp, vp, i32, u64, u64, u64, u64, u64, vp, vp, u64, vp, u64,
+                                         vp, u64, vp, vp, u64, vp],
+            "rtopk_orthogonalize_workspace_bytes": [u32, u64, u64, i32, pu64],
+            "rtopk_orthogonalize": [u32, vp, i32, u64, u64, u64, u32, vp, f32, i32, vp, i32, u64, vp,
+                                    u64, vp],
+            "rtopk_aggregate_update_orthogonal_workspace_bytes": [u32, u64, u64, i32, pu64],
+            "rtopk_aggregate_update_orthogonal": [u32, vp, vp, u32, u64, u64, u64, f32, f32, f32, i32, f32,
+                                                  f32, u32, vp, f32, i32, vp, vp, vp, u64, vp]}.items():
+        getattr(L, name).argtypes = args
+        getattr(L, name).restype = i32
     L.rtopk_strerror.argtypes = [ctypes.c_int]
     L.rtopk_strerror.restype = ctypes.c_char_p
     L.rtopk_version.argtypes = []
@@ -335,3 +360,245 @@ def encode_stats(workspace: torch.Tensor, stream=None) -> dict:
     if rc:
         raise RtopkError(rc, "rtopk_encode_stats")
     return {name: int(getattr(st, name)) for name, _ in EncodeStats._fields_}
+
+
+# ---- matrix parameters: a layer's products in 8-bit integers, orthogonalised updates ----------
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_ALONG = {"rows": 0, "columns": 1}
+_PRODUCTS = {"pairs": 0, "halves": 1}
+#: (a, b, c) of every step, in common use for updates of neural networks
+QUINTIC = (3.4445, -4.7750, 2.0315)
+
+
+def _matrix(t: torch.Tensor, name: str, types=None) -> None:
+    if not t.is_cuda or t.dim() != 2 or (types is not None and t.dtype not in types):
+        raise TypeError(f"{name} must be a matrix on the GPU" + (f" of {' or '.join(map(str, types))}" if types else ""))
+    if t.size(1) > 1 and t.stride(1) != 1 or t.size(0) > 1 and t.stride(0) < t.size(1):
+        raise TypeError(f"the elements of {name}'s rows must be neighbours, and its rows must not overlap")
+
+
+def _ld(t: torch.Tensor) -> int:
+    """Distance of a matrix's rows in elements."""
+    return t.stride(0) if t.size(0) > 1 else max(t.size(1), 1)
+
+
+def _vector(t: torch.Tensor, length: int, name: str) -> None:
+    _need(t, torch.float32, name)
+    if t.numel() != length:
+        raise ValueError(f"{name} must have {length} elements")
+
+
+def _bytes(name: str, *args) -> int:
+    out = ctypes.c_uint64(0)
+    rc = getattr(load_library(), name)(*args, ctypes.byref(out))
+    if rc:
+        raise RtopkError(rc, name)
+    return out.value
+
+
+def _workspace(workspace: Optional[torch.Tensor], need: int, device, stream):
+    """The caller's workspace, or memory of torch's allocator on the call's stream: (pointer, bytes, what holds it)."""
+    if workspace is not None:
+        return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+    if not need:
+        return None, 0, None
+    if stream is None:
+        held = torch.empty(need + 256, dtype=torch.uint8, device=device)
+    else:
+        with torch.cuda.stream(stream):
+            held = torch.empty(need + 256, dtype=torch.uint8, device=device)
+    at = held.data_ptr()
+    return at + -at % 256, need, held
+
+
+def quantize_i8_workspace_bytes(rows: int, cols: int, along: str = "rows") -> int:
+    return _bytes("rtopk_quantize_i8_workspace_bytes", rows, cols, _ALONG[along])
+
+
+def quantize_i8(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, along: str = "rows",
+                workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """rtopk_quantize_i8: ``q`` (int8) and ``scale`` of the matrix ``x``, a scale for each row, or
+    (``along="columns"``) for each column, ``q`` then holding ``x`` turned over. Give ``q`` rows that start on
+    16 bytes (a multiple of 16 between them) where the product is to read it fast. ``workspace``: None
+    takes it from torch's allocator, here and in the calls below."""
+    _matrix(x, "x", _TYPES)
+    _matrix(q, "q", (torch.int8,))
+    rows, cols = x.shape
+    if tuple(q.shape) != ((rows, cols) if along == "rows" else (cols, rows)):
+        raise ValueError("q must have the shape of x, or of x turned over along columns")
+    _vector(scale, q.size(0), "scale")
+    ws, ws_bytes, held = _workspace(workspace, 0 if along == "rows" else quantize_i8_workspace_bytes(rows, cols, along),
+                                    x.device, stream)
+    rc = load_library().rtopk_quantize_i8(_ptr(x), _TYPES[x.dtype], rows, cols, _ld(x), _ALONG[along], _ptr(q), _ld(q),
+                                          _ptr(scale), ws, ws_bytes, _stream_handle(stream))
+    if rc:
+        raise RtopkError(rc, "rtopk_quantize_i8")
+
+
+def matmul_i8_workspace_bytes(m: int, n: int, k: int) -> int:
+    return _bytes("rtopk_matmul_i8_workspace_bytes", m, n, k)
+
+
+def matmul_i8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor, out: torch.Tensor,
+              bias: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """rtopk_matmul_i8: out[i, j] = a_scale[i] b_scale[j] sum_k a[i, k] b[j, k] (+ bias[j])."""
+    _matrix(a, "a", (torch.int8,))
+    _matrix(b, "b", (torch.int8,))
+    _matrix(out, "out", _TYPES)
+    (m, k), n = a.shape, b.size(0)
+    if b.size(1) != k or tuple(out.shape) != (m, n):
+        raise ValueError("a is [m, k], b [n, k], out [m, n]")
+    _vector(a_scale, m, "a_scale")
+    _vector(b_scale, n, "b_scale")
+    if bias is not None:
+        _vector(bias, n, "bias")
+    ws, ws_bytes, held = _workspace(workspace, 0 if workspace is not None else matmul_i8_workspace_bytes(m, n, k), a.device, stream)
+    rc = load_library().rtopk_matmul_i8(_ptr(a), _ptr(a_scale), _ptr(b), _ptr(b_scale), _ptr(bias), m, n, k, _ld(a), _ld(b),
+                                        _ptr(out), _TYPES[out.dtype], _ld(out), ws, ws_bytes, _stream_handle(stream))
+    if rc:
+        raise RtopkError(rc, "rtopk_matmul_i8")
+
+
+def linear_i8_workspace_bytes(m: int, k: int, n: int) -> int:
+    return _bytes("rtopk_linear_i8_workspace_bytes", m, k, n)
+
+
+def linear_i8(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, out: torch.Tensor, bias: Optional[torch.Tensor] = None,
+              workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """rtopk_linear_i8: out = x w^T + bias, ``x`` [m, k] quantised by token on the way, ``w`` [n, k] int8 with
+    ``w_scale`` [n] as :func:`quantize_i8` leaves them."""
+    _matrix(x, "x", _TYPES)
+    _matrix(w, "w", (torch.int8,))
+    _matrix(out, "out", _TYPES)
+    (m, k), n = x.shape, w.size(0)
+    if w.size(1) != k or tuple(out.shape) != (m, n):
+        raise ValueError("x is [m, k], w [n, k], out [m, n]")
+    _vector(w_scale, n, "w_scale")
+    if bias is not None:
+        _vector(bias, n, "bias")
+    ws, ws_bytes, held = _workspace(workspace, 0 if workspace is not None else linear_i8_workspace_bytes(m, k, n), x.device, stream)
+    rc = load_library().rtopk_linear_i8(_ptr(x), _TYPES[x.dtype], m, k, _ld(x), _ptr(w), _ptr(w_scale), n, _ld(w), _ptr(bias),
+                                        _ptr(out), _TYPES[out.dtype], _ld(out), ws, ws_bytes, _stream_handle(stream))
+    if rc:
+        raise RtopkError(rc, "rtopk_linear_i8")
+
+
+def linear_i8_backward_workspace_bytes(m: int, k: int, n: int) -> int:
+    return _bytes("rtopk_linear_i8_backward_workspace_bytes", m, k, n)
+
+
+def linear_i8_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w_turned: Optional[torch.Tensor],
+                       w_turned_scale: Optional[torch.Tensor], dx: Optional[torch.Tensor], dw: Optional[torch.Tensor],
+                       db: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """rtopk_linear_i8_backward: the gradients of :func:`linear_i8`'s input, weights (binary32, [n, k]) and bias from
+    ``dy`` [m, n]. ``w_turned`` [k, n] and its scales: the weights quantised along columns. ``dx`` or ``dw`` may be
+    None, and then what only they need too."""
+    if dx is None and dw is None:
+        raise ValueError("neither dx nor dw is asked for")
+    if dx is not None and (w_turned is None or w_turned_scale is None) or dw is not None and x is None:
+        raise ValueError("dx needs w_turned and its scales, dw needs x")
+    if db is not None and dw is None:
+        raise ValueError("db comes with dw")
+    _matrix(dy, "dy", _TYPES)
+    m, n = dy.shape
+    k = (dx if dx is not None else dw).size(1)
+    if dx is not None:
+        _matrix(dx, "dx", (dy.dtype,))
+        _matrix(w_turned, "w_turned", (torch.int8,))
+        _vector(w_turned_scale, k, "w_turned_scale")
+        if tuple(dx.shape) != (m, k) or tuple(w_turned.shape) != (k, n):
+            raise ValueError("dy is [m, n], dx [m, k], w_turned [k, n]")
+    if dw is not None:
+        _matrix(x, "x", (dy.dtype,))
+        _matrix(dw, "dw", (torch.float32,))
+        if tuple(x.shape) != (m, k) or tuple(dw.shape) != (n, k):
+            raise ValueError("dy is [m, n], x [m, k], dw [n, k]")
+    if db is not None:
+        _vector(db, n, "db")
+    ws, ws_bytes, held = _workspace(workspace, 0 if workspace is not None else linear_i8_backward_workspace_bytes(m, k, n),
+                                    dy.device, stream)
+    ld = lambda t: 0 if t is None else _ld(t)   # noqa: E731
+    rc = load_library().rtopk_linear_i8_backward(
+        _ptr(dy), _ptr(x), _TYPES[dy.dtype], m, k, n, _ld(dy), ld(x), _ptr(w_turned), _ptr(w_turned_scale), ld(w_turned),
+        _ptr(dx), ld(dx), _ptr(dw), ld(dw), _ptr(db), ws, ws_bytes, _stream_handle(stream))
+    if rc:
+        raise RtopkError(rc, "rtopk_linear_i8_backward")
+
+
+def _coefficients(coefficients, steps: Optional[int]):
+    """(number of steps, their coefficients as binary32): one triple for all of 5 or ``steps``, or a triple for each."""
+    rows = [tuple(c) for c in coefficients] if not isinstance(coefficients[0], (int, float)) else \
+        [tuple(coefficients)] * (5 if steps is None else steps)
+    if not rows or any(len(c) != 3 for c in rows) or (steps is not None and len(rows) != steps):
+        raise ValueError("coefficients: three numbers, or three for each step")
+    return len(rows), (ctypes.c_float * (3 * len(rows)))(*[v for c in rows for v in c])
+
+
+def orthogonalize_workspace_bytes(count: int, rows: int, cols: int, products: str = "pairs") -> int:
+    return _bytes("rtopk_orthogonalize_workspace_bytes", count, rows, cols, _PRODUCTS[products])
+
+
+def orthogonalize(xs, outs, steps: Optional[int] = None, coefficients=QUINTIC, eps: float = 1e-7,
+                  products: Optional[str] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """rtopk_orthogonalize: Newton-Schulz orthogonalisation of every matrix of the list ``xs`` (equal shapes, types and
+    row distances) into ``outs`` (which may be ``xs``). ``products``: "pairs" (as exact as binary32) or "halves" (a
+    third of the time); None takes pairs for binary32 outputs and halves for 16-bit ones."""
+    count = len(xs)
+    if count < 1 or len(outs) != count:
+        raise ValueError("xs and outs must have the same length >= 1")
+    x, out = xs[0], outs[0]
+    for a, b in zip(xs, outs):
+        _matrix(a, "x", (x.dtype,) if x.dtype in _TYPES else _TYPES)
+        _matrix(b, "out", (out.dtype,) if out.dtype in _TYPES else _TYPES)
+        if a.shape != x.shape or b.shape != x.shape or _ld(a) != _ld(x) or _ld(b) != _ld(out):
+            raise ValueError("all matrices must have one shape, and one distance of their rows")
+    products = products or ("pairs" if out.dtype == torch.float32 else "halves")
+    rows, cols = x.shape
+    number, abc = _coefficients(coefficients, steps)
+    ws, ws_bytes, held = _workspace(workspace, 0 if workspace is not None else
+                                    orthogonalize_workspace_bytes(count, rows, cols, products), x.device, stream)
+    vp_arr = ctypes.c_void_p * count
+    rc = load_library().rtopk_orthogonalize(
+        count, vp_arr(*[_ptr(t) for t in xs]), _TYPES[x.dtype], rows, cols, _ld(x), number, abc, eps, _PRODUCTS[products],
+        vp_arr(*[_ptr(t) for t in outs]), _TYPES[out.dtype], _ld(out), ws, ws_bytes, _stream_handle(stream))
+    if rc:
+        raise RtopkError(rc, "rtopk_orthogonalize")
+
+
+def aggregate_update_orthogonal_workspace_bytes(count: int, rows: int, cols: int, products: str = "pairs") -> int:
+    return _bytes("rtopk_aggregate_update_orthogonal_workspace_bytes", count, rows, cols, _PRODUCTS[products])
+
+
+def aggregate_update_orthogonal(idx, val, n: int, k: int, eta: float, scale: float, mu: float, omega, velocity,
+                                nesterov: bool = True, decay: float = 0.0, gain: float = 1.0, steps: Optional[int] = None,
+                                coefficients=QUINTIC, eps: float = 1e-7, products: str = "pairs",
+                                workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """rtopk_aggregate_update_orthogonal: for every matrix of the list ``omega`` (with its ``velocity`` and its n
+    messages ``idx``, ``val`` back to back): velocity = mu velocity + scale average, and omega = (1 - eta decay)
+    omega - eta gain orthogonalised(mu velocity + scale average, or velocity without ``nesterov``), in place."""
+    count = len(omega)
+    if count < 1 or not (len(idx) == len(val) == len(velocity) == count):
+        raise ValueError("idx, val, omega and velocity must have the same length >= 1")
+    if omega[0].dim() != 2:
+        raise ValueError("omega must hold matrices")
+    rows, cols = omega[0].shape
+    for i, v, w, m in zip(idx, val, omega, velocity):
+        _need(i, torch.int32, "idx")
+        _need(v, torch.float32, "val")
+        _need(w, torch.float32, "omega")
+        _need(m, torch.float32, "velocity")
+        if tuple(w.shape) != (rows, cols) or m.numel() != rows * cols:
+            raise ValueError("all of omega must have one shape, and velocity as many elements")
+        if i.numel() < n * k or v.numel() < n * k:
+            raise ValueError("idx/val must hold n*k entries")
+    number, abc = _coefficients(coefficients, steps)
+    ws, ws_bytes, held = _workspace(workspace, 0 if workspace is not None else
+                                    aggregate_update_orthogonal_workspace_bytes(count, rows, cols, products), omega[0].device, stream)
+    vp_arr = ctypes.c_void_p * count
+    pointers = lambda ts: vp_arr(*[_ptr(t) for t in ts])   # noqa: E731
+    rc = load_library().rtopk_aggregate_update_orthogonal(
+        count, pointers(idx), pointers(val), n, k, rows, cols, eta, scale, mu, int(bool(nesterov)), decay, gain, number, abc, eps,
+        _PRODUCTS[products], pointers(omega), pointers(velocity), ws, ws_bytes, _stream_handle(stream))
+    if rc:
+        raise RtopkError(rc, "rtopk_aggregate_update_orthogonal")

@@ -1155,7 +1155,7 @@ extern "C" const char *rtopk_strerror(int code)
 {
     switch (code) {
     case RTOPK_OK: return "ok";
-    case RTOPK_EINVAL: return "invalid argument (null pointer, sizes outside 1 <= k <= r <= d < 2^32, n < 1, or grad overlaps residual)";
+    case RTOPK_EINVAL: return "invalid argument (null pointer, sizes outside 1 <= k <= r <= d < 2^32, n < 1, or grad overlaps residual; of a matrix call: a size, row distance, type or coefficient outside its domain)";
     case RTOPK_EWORKSPACE: return "workspace missing, not 256-byte aligned, or too small";
     case RTOPK_EHIP: return "a HIP call or kernel launch failed";
     case RTOPK_ETOOLARGE: return "sizes exceed the library's built-in scratch array (rtopk_aggregate_update_static needs 4 bytes per worker and per 2048 coordinates within RTOPK_STATIC_SCRATCH_BYTES); use the entry point that takes a workspace";
@@ -1163,7 +1163,7 @@ extern "C" const char *rtopk_strerror(int code)
     }
 }
 
-extern "C" int rtopk_version(void) { return 200; }
+extern "C" int rtopk_version(void) { return 300; }
 
 // 1 when the library was built with RTOPK_DEBUG_CHECKS, else 0
 extern "C" int rtopk_debug_checks(void)

@@ -1,0 +1,568 @@
+// Orthogonalised updates (gfx950): the polar factor of a matrix, approached by
+// Newton-Schulz products, and the master's weight step that uses it.
+//
+//   X = G / (|G|_F + eps), turned over where G has more rows than columns
+//   each step, with coefficients (a, b, c):
+//     A = X X^T,  B = b A + c A A,  X <- a X + B X
+//
+// All three products have both operands' rows along the contraction: A's rows
+// and B's are its columns too, and X is kept twice, as it is and turned over
+// (the product that makes a new X writes both). A and B are symmetric: only
+// tiles on and above the diagonal are computed, and written on both sides.
+//
+// Numbers between the products are halves (11 bits; bfloat16, in common use
+// here, has 8) or pairs of halves (22 bits), times a power of two that puts
+// what the iteration can hold into a half's range: its singular values are
+// bounded by the coefficients, which the host checks before it launches.
+// Products are summed in binary32. |G|_F is summed in binary64. Of the division by it
+// only the power of two is applied to G (that is exact); the rest, between 1 and
+// 2, goes into the first step's coefficients, so that a bfloat16 G enters the
+// products unrounded.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "../../include/rtopk.h"
+#include "rtopk_matrix.h"
+
+namespace rtopk {
+
+// powers of two that X, A and B are stored with: singular values of X up to kMostX, entries of A up to its square,
+// entries of B up to kMostB stay finite
+constexpr int kLogX = 12, kLogA = 10;
+constexpr double kMostX = 7.5, kMostB = 60.0;
+constexpr u32 kMembers = 16;            // matrices in one launch
+
+struct Members { void *p[kMembers]; };
+
+// ---- stored numbers -------------------------------------------------------
+// A row of halves, or of blocks of 128 bytes: 32 high halves, their 32 low halves.
+template <Operands kOf> struct Stored {
+    static constexpr u32 kBlock = kOf == kPairs ? 32u : 64u;      // numbers in a slice
+    static __host__ __device__ u32 row_bytes(u32 cols) { return (cols + kBlock - 1) / kBlock * kSlice; }
+    static __host__ __device__ u32 padded(u32 cols) { return (cols + kBlock - 1) / kBlock * kBlock; }
+    static __device__ __forceinline__ u32 at(u32 col) { return kOf == kPairs ? (col >> 5) * kSlice + (col & 31u) * 2u : col * 2u; }
+    // four neighbours from a multiple of four on
+    static __device__ __forceinline__ void put(unsigned char *row, u32 col, const f32x4 &v)
+    {
+        f16x4 hi;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) hi[c] = (_Float16)v[c];
+        *(f16x4 *)(row + at(col)) = hi;
+        if (kOf == kPairs) {
+            f16x4 lo;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) lo[c] = (_Float16)(v[c] - (float)hi[c]);
+            *(f16x4 *)(row + at(col) + 64) = lo;
+        }
+    }
+    static __device__ __forceinline__ void put(unsigned char *row, u32 col, float v)
+    {
+        const _Float16 hi = (_Float16)v;
+        *(_Float16 *)(row + at(col)) = hi;
+        if (kOf == kPairs) *(_Float16 *)(row + at(col) + 64) = (_Float16)(v - (float)hi);
+    }
+    static __device__ __forceinline__ f32x4 get(const unsigned char *row, u32 col)
+    {
+        const f16x4 hi = *(const f16x4 *)(row + at(col));
+        f32x4 v;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[c] = (float)hi[c];
+        if (kOf == kPairs) {
+            const f16x4 lo = *(const f16x4 *)(row + at(col) + 64);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] += (float)lo[c];
+        }
+        return v;
+    }
+};
+
+// ---- the norm ---------------------------------------------------------------
+constexpr u32 kNormThreads = 256, kNormBlocks = 64;
+
+// the sum of the workgroup's values, in thread 0
+__device__ __forceinline__ double block_sum(double v)
+{
+    __shared__ double part[kNormThreads / kWave];
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+    if (lane_id() == 0) part[threadIdx.x / kWave] = v;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        for (int w = 1; w < (int)(kNormThreads / kWave); ++w) v += part[w];
+    return v;
+}
+
+__global__ void __launch_bounds__(kNormThreads)
+k_norm(Members x, int type, u32 rows, u32 cols, u64 ld, double *__restrict__ part)
+{
+    const void *g = x.p[blockIdx.y];
+    double sum = 0.0;
+    for (u32 r = blockIdx.x; r < rows; r += gridDim.x)
+        for (u32 c = threadIdx.x; c < cols; c += kNormThreads) {
+            const double v = (double)read_as(g, (u64)r * ld + c, type);
+            sum += v * v;
+        }
+    sum = block_sum(sum);
+    if (threadIdx.x == 0) part[blockIdx.y * kNormBlocks + blockIdx.x] = sum;
+}
+
+// The momentum of the master's step, and the norm of what is to be orthogonalised:
+// u = scale * average, v <- fma(mu, v, u), g = fma(mu, v, u) or the new v itself. `average` holds the averages, and g
+// afterwards.
+__global__ void __launch_bounds__(kNormThreads)
+k_velocity(Members velocity, float *__restrict__ average, u64 d, float scale, float mu, int nesterov, double *__restrict__ part)
+{
+    float *v = (float *)velocity.p[blockIdx.y], *g = average + blockIdx.y * align_up(d, 64);
+    double sum = 0.0;
+    for (u64 i = (u64)blockIdx.x * kNormThreads + threadIdx.x; i < d; i += (u64)gridDim.x * kNormThreads) {
+        const float u = scale * g[i], now = fmaf(mu, v[i], u);
+        v[i] = now;
+        const float to = nesterov ? fmaf(mu, now, u) : now;
+        g[i] = to;
+        sum += (double)to * (double)to;
+    }
+    sum = block_sum(sum);
+    if (threadIdx.x == 0) part[blockIdx.y * kNormBlocks + blockIdx.x] = sum;
+}
+
+// ---- G into stored numbers, as it is and turned over --------------------------
+struct Start {
+    Members x;
+    int type;
+    u32 rows, cols;
+    u64 ld;
+    unsigned char *as_is, *turned;      // [rows] rows of cols, [cols] rows of rows
+    u64 as_is_stride, turned_stride;    // from matrix to matrix
+    const double *part;
+    float eps;
+    float *rho;                         // what is left of the division, for the first step
+};
+
+constexpr u32 kSide = 64;
+
+template <Operands kOf>
+__global__ void __launch_bounds__(256) k_start(Start g)
+{
+    typedef Stored<kOf> S;
+    __shared__ float tile[kSide][kSide + 1];
+    __shared__ int exponent;
+    const u32 r0 = blockIdx.y * kSide, c0 = blockIdx.x * kSide, member = blockIdx.z;
+    if (threadIdx.x < kWave) {
+        double sum = threadIdx.x < kNormBlocks ? g.part[member * kNormBlocks + threadIdx.x] : 0.0;
+#pragma unroll
+        for (int o = kWave / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+        const double norm = sqrt(sum);
+        int e = 0;
+        float rho;
+        if (norm > 0.0 && norm < __builtin_huge_val()) {
+            (void)frexp(norm, &e);
+            rho = (float)(ldexp(1.0, e) / (norm + (double)g.eps));
+        } else {
+            rho = norm == 0.0 ? 0.0f : __uint_as_float(0x7FC00000u);       // an infinity or a not-a-number: all of it is NaN
+        }
+        if (threadIdx.x == 0) {
+            exponent = e;
+            if (blockIdx.x == 0 && blockIdx.y == 0) g.rho[member] = rho;
+        }
+    }
+    __syncthreads();
+    const int e = kLogX - exponent;
+    for (u32 i = threadIdx.x; i < kSide * kSide; i += 256) {
+        const u32 r = r0 + i / kSide, c = c0 + i % kSide;
+        const float v = r < g.rows && c < g.cols ? read_as(g.x.p[member], (u64)r * g.ld + c, g.type) : 0.0f;
+        tile[i / kSide][i % kSide] = ldexpf(v, e);
+    }
+    __syncthreads();
+    const u32 row_a = S::row_bytes(g.cols), row_t = S::row_bytes(g.rows);
+    unsigned char *as_is = g.as_is + member * g.as_is_stride, *turned = g.turned + member * g.turned_stride;
+    for (u32 i = threadIdx.x; i < kSide * kSide / 4; i += 256) {
+        const u32 r = i / (kSide / 4), c = i % (kSide / 4) * 4;
+        if (r0 + r < g.rows && c0 + c < S::padded(g.cols))
+            S::put(as_is + (u64)(r0 + r) * row_a, c0 + c, f32x4{tile[r][c], tile[r][c + 1], tile[r][c + 2], tile[r][c + 3]});
+        if (c0 + r < g.cols && r0 + c < S::padded(g.rows))
+            S::put(turned + (u64)(c0 + r) * row_t, r0 + c, f32x4{tile[c][r], tile[c + 1][r], tile[c + 2][r], tile[c + 3][r]});
+    }
+}
+
+// ---- the products -------------------------------------------------------------
+enum Step { kGram, kPoly, kNext, kLast };
+
+struct Product {
+    const unsigned char *left, *right;      // rows of the result, columns of the result
+    u64 left_stride, right_stride;          // from matrix to matrix
+    u32 rows, cols, inner;                  // of the result, and numbers of the contraction
+    u32 tiles_m, tiles_n, tiles;            // tiles: of one matrix
+    const unsigned char *old;               // kPoly: A; kNext, kLast: X with the result's orientation
+    u64 old_stride;
+    unsigned char *out, *turned;            // the result, and turned over
+    u64 out_stride, turned_stride;
+    float c_old, c_sum;
+    const float *rho;                       // first step only, else null
+    // kLast
+    Members to;
+    int type;
+    u64 ldo;
+    float gain, keep;                       // to <- keep * to + gain * result, where `update`
+    int update;
+};
+
+template <Operands kOf, class T, Step kStep>
+__global__ void __launch_bounds__(T::kThreads) k_step(Product g)
+{
+    typedef Stored<kOf> S;
+    __shared__ __align__(16) unsigned char lds[T::kLds];
+    constexpr bool kSymmetric = kStep == kGram || kStep == kPoly;
+    const u32 place = xcd_place(blockIdx.x, gridDim.x), member = place / g.tiles;
+    u32 ti, tj, at = place - member * g.tiles;
+    if (kSymmetric) {                       // row ti of the triangle has tiles_n - ti tiles
+        ti = 0;
+        while (at >= g.tiles_n - ti) at -= g.tiles_n - ti++;
+        tj = ti + at;
+    } else {
+        tile_at(at, g.tiles_m, g.tiles_n, ti, tj);
+    }
+    const u32 i0 = ti * T::kRowsM, j0 = tj * T::kRowsN;
+    const u32 bytes = S::row_bytes(g.inner);
+    const TileRows a{g.left + member * g.left_stride + (u64)i0 * bytes, g.rows - i0, bytes, bytes};
+    const TileRows b{g.right + member * g.right_stride + (u64)j0 * bytes, g.cols - j0, bytes, bytes};
+    T t;
+    t.clear();
+    t.template multiply<true>(a, b, 0, bytes / kSlice, lds);
+
+    const float rho = g.rho ? g.rho[member] : 1.0f;
+    const float c_sum = kStep == kGram ? g.c_sum * rho * rho : g.c_sum * rho, c_old = g.c_old * rho;
+    const u32 row_out = S::row_bytes(g.cols), row_turned = S::row_bytes(g.rows);
+    const unsigned char *old = g.old + member * g.old_stride;
+    unsigned char *out = g.out + member * g.out_stride, *turned = g.turned + member * g.turned_stride;
+    t.each([&](u32 r, u32 c, const f32x4 &sum) {
+        const u32 row = i0 + r, col = j0 + c;
+        if (row >= g.rows || col >= S::padded(g.cols)) return;
+        f32x4 v = sum * c_sum;
+        if (kStep != kGram) v += c_old * S::get(old + (u64)row * row_out, col);
+#pragma unroll
+        for (u32 q = 0; q < 4; ++q)
+            if (col + q >= g.cols) v[q] = 0.0f;
+        if (kStep == kLast) {
+            const u32 have = col < g.cols ? g.cols - col : 0u;
+            void *to = g.to.p[member];
+            const u32 size = g.type == 0 ? 4u : 2u;
+            const u64 first = (u64)row * g.ldo + col;
+            if (g.update) {
+                float *w = (float *)to + first;
+#pragma unroll
+                for (u32 q = 0; q < 4; ++q)
+                    if (q < have) w[q] = fmaf(g.gain, v[q], g.keep * w[q]);
+            } else {
+                write_four(to, first, g.type, v, have, (((uintptr_t)to | (g.ldo * size)) & (4u * size - 1u)) == 0);
+            }
+            return;
+        }
+        S::put(out + (u64)row * row_out, col, v);
+        if (kSymmetric ? ti != tj : true)
+#pragma unroll
+            for (u32 q = 0; q < 4; ++q)
+                if (col + q < g.cols) S::put(turned + (u64)(col + q) * row_turned, row, v[q]);
+    });
+    // what pads the turned rows is zero
+    if (!kSymmetric && kStep != kLast && i0 + T::kRowsM >= g.rows) {
+        const u32 pad = S::padded(g.rows) - g.rows;
+        for (u32 i = threadIdx.x; i < T::kRowsN * pad; i += T::kThreads)
+            if (j0 + i / pad < g.cols) S::put(turned + (u64)(j0 + i / pad) * row_turned, g.rows + i % pad, 0.0f);
+    }
+}
+
+}  // namespace rtopk
+
+using namespace rtopk;
+
+namespace {
+
+constexpr u64 kMostSide = 1u << 21;      // offsets inside a tile of 256 rows fit 32 bits
+constexpr u32 kMostSteps = 64;
+constexpr u32 kUnits = 256;
+
+struct Shape {
+    u32 rows, cols;
+    u32 m() const { return std::min(rows, cols); }
+    u32 n() const { return std::max(rows, cols); }
+    bool over() const { return rows > cols; }       // X is G turned over
+};
+
+struct Parts {
+    double *norm;
+    float *rho, *average;
+    unsigned char *x[2], *xt[2], *a, *b;
+    u64 x_stride, xt_stride, a_stride;
+};
+
+template <Operands kOf>
+u64 cut(void *base, u32 members, const Shape &s, bool average, Parts &p)
+{
+    typedef Stored<kOf> S;
+    unsigned char *at = (unsigned char *)base;
+    u64 used = 0;
+    auto take = [&](u64 bytes) { unsigned char *q = at + used; used += align_up(bytes, 256); return q; };
+    p.x_stride = align_up((u64)s.m() * S::row_bytes(s.n()), 256);
+    p.xt_stride = align_up((u64)s.n() * S::row_bytes(s.m()), 256);
+    p.a_stride = align_up((u64)s.m() * S::row_bytes(s.m()), 256);
+    p.norm = (double *)take(kMembers * kNormBlocks * sizeof(double));
+    p.rho = (float *)take(kMembers * sizeof(float));
+    for (int i = 0; i < 2; ++i) {
+        p.x[i] = take(members * p.x_stride);
+        p.xt[i] = take(members * p.xt_stride);
+    }
+    p.a = take(members * p.a_stride);
+    p.b = take(members * p.a_stride);
+    p.average = average ? (float *)take(members * align_up((u64)s.rows * s.cols, 64) * sizeof(float)) : nullptr;
+    return used;
+}
+
+u64 cut(int products, void *base, u32 members, const Shape &s, bool average, Parts &p)
+{
+    return products == RTOPK_PRODUCTS_PAIRS ? cut<kPairs>(base, members, s, average, p) : cut<kHalves>(base, members, s, average, p);
+}
+
+// Whether iterates that start with singular values in [0, 1] stay where their stored forms are finite.
+bool coefficients_ok(const float *abc, u32 steps)
+{
+    double hi = 1.0;
+    for (u32 s = 0; s < steps; ++s) {
+        const double a = abc[3 * s], b = abc[3 * s + 1], c = abc[3 * s + 2];
+        if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+        // largest |a t + b t^3 + c t^5| and |b u + c u^2|, u = t^2, for t up to hi: at the ends or where the derivatives vanish
+        double x = 0.0, p = 0.0;
+        auto look = [&](double u) {
+            if (!(u > 0.0) || u > hi * hi) return;
+            x = std::max(x, std::fabs(std::sqrt(u) * (a + u * (b + u * c))));
+            p = std::max(p, std::fabs(u * (b + u * c)));
+        };
+        look(hi * hi);
+        if (c != 0.0) {
+            look(-b / (2.0 * c));
+            const double root = 9.0 * b * b - 20.0 * a * c;
+            if (root >= 0.0) {
+                look((-3.0 * b + std::sqrt(root)) / (10.0 * c));
+                look((-3.0 * b - std::sqrt(root)) / (10.0 * c));
+            }
+        } else if (b != 0.0) {
+            look(-a / (3.0 * b));
+        }
+        if (!(x <= kMostX) || !(p <= kMostB)) return false;
+        hi = x;
+    }
+    return true;
+}
+
+template <Operands kOf, class T, Step kStep>
+int launch(Product g, u32 members, hipStream_t stream)
+{
+    g.tiles_m = (g.rows + T::kRowsM - 1) / T::kRowsM;
+    g.tiles_n = (g.cols + T::kRowsN - 1) / T::kRowsN;
+    g.tiles = kStep == kGram || kStep == kPoly ? g.tiles_n * (g.tiles_n + 1) / 2 : g.tiles_m * g.tiles_n;
+    k_step<kOf, T, kStep><<<g.tiles * members, T::kThreads, 0, stream>>>(g);
+    return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_EHIP;
+}
+
+template <Operands kOf, Step kStep>
+int launch(const Product &g, u32 members, hipStream_t stream)
+{
+    auto tiles = [&](u32 t) {
+        const u64 i = (g.rows + t - 1) / t, j = (g.cols + t - 1) / t;
+        return (kStep == kGram || kStep == kPoly ? j * (j + 1) / 2 : i * j) * members;
+    };
+    if (tiles(256) >= 200) return launch<kOf, Tile<kOf, 256, 256, 2, 4>, kStep>(g, members, stream);
+    if (tiles(128) >= 64) return launch<kOf, Tile<kOf, 128, 128, 2, 2>, kStep>(g, members, stream);
+    return launch<kOf, Tile<kOf, 64, 64, 2, 2>, kStep>(g, members, stream);
+}
+
+struct Target {
+    Members to;
+    int type;
+    u64 ld;
+    float gain, keep;
+    int update;
+};
+
+// From G and the parts of its norm to the end.
+template <Operands kOf>
+int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 steps, const float *abc, float eps, const Parts &p,
+            const Target &target, hipStream_t stream)
+{
+    typedef Stored<kOf> S;
+    const u32 m = s.m(), n = s.n();
+    Start start{x, type, s.rows, s.cols, ldx, s.over() ? p.xt[0] : p.x[0], s.over() ? p.x[0] : p.xt[0],
+                s.over() ? p.xt_stride : p.x_stride, s.over() ? p.x_stride : p.xt_stride, p.norm, eps, p.rho};
+    const dim3 grid((std::max(S::padded(s.cols), s.cols) + kSide - 1) / kSide, (S::padded(s.rows) + kSide - 1) / kSide, members);
+    k_start<kOf><<<grid, 256, 0, stream>>>(start);
+    if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
+    for (u32 i = 0; i < steps; ++i) {
+        const unsigned char *xi = p.x[i & 1], *xti = p.xt[i & 1];
+        const float a = abc[3 * i], b = abc[3 * i + 1], c = abc[3 * i + 2];
+        const float *rho = i == 0 ? p.rho : nullptr;
+        Product g{};
+        g.left = g.right = xi;
+        g.left_stride = g.right_stride = p.x_stride;
+        g.rows = g.cols = m;
+        g.inner = n;
+        g.old = p.a;
+        g.out = g.turned = p.a;
+        g.old_stride = g.out_stride = g.turned_stride = p.a_stride;
+        g.c_sum = ldexpf(1.0f, kLogA - 2 * kLogX);
+        g.rho = rho;
+        if (const int rc = launch<kOf, kGram>(g, members, stream)) return rc;
+        g.left = g.right = p.a;
+        g.left_stride = g.right_stride = p.a_stride;
+        g.inner = m;
+        g.out = g.turned = p.b;
+        g.c_old = b;
+        g.c_sum = c * ldexpf(1.0f, -kLogA);
+        g.rho = nullptr;
+        if (const int rc = launch<kOf, kPoly>(g, members, stream)) return rc;
+        g.rho = rho;
+        if (i + 1 < steps) {
+            g.left = p.b;
+            g.right = xti;
+            g.right_stride = p.xt_stride;
+            g.cols = n;
+            g.old = xi;
+            g.old_stride = p.x_stride;
+            g.out = p.x[1 - (i & 1)];
+            g.turned = p.xt[1 - (i & 1)];
+            g.out_stride = p.x_stride;
+            g.turned_stride = p.xt_stride;
+            g.c_old = a;
+            g.c_sum = ldexpf(1.0f, -kLogA);
+            if (const int rc = launch<kOf, kNext>(g, members, stream)) return rc;
+            continue;
+        }
+        // the last product writes with G's orientation
+        g.left = s.over() ? xti : p.b;
+        g.right = s.over() ? p.b : xti;
+        g.left_stride = s.over() ? p.xt_stride : p.a_stride;
+        g.right_stride = s.over() ? p.a_stride : p.xt_stride;
+        g.rows = s.rows;
+        g.cols = s.cols;
+        g.old = s.over() ? xti : xi;
+        g.old_stride = s.over() ? p.xt_stride : p.x_stride;
+        g.c_old = a * ldexpf(1.0f, -kLogX);
+        g.c_sum = ldexpf(1.0f, -kLogA - kLogX);
+        g.to = target.to;
+        g.type = target.type;
+        g.ldo = target.ld;
+        g.gain = target.gain;
+        g.keep = target.keep;
+        g.update = target.update;
+        if (const int rc = launch<kOf, kLast>(g, members, stream)) return rc;
+    }
+    return RTOPK_OK;
+}
+
+int iterate(int products, const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 steps, const float *abc, float eps,
+            const Parts &p, const Target &target, hipStream_t stream)
+{
+    return products == RTOPK_PRODUCTS_PAIRS ? iterate<kPairs>(x, type, ldx, s, members, steps, abc, eps, p, target, stream)
+                                            : iterate<kHalves>(x, type, ldx, s, members, steps, abc, eps, p, target, stream);
+}
+
+bool type_ok(int type) { return type == RTOPK_F32 || type == RTOPK_BF16 || type == RTOPK_F16; }
+bool sizes_ok(uint32_t count, uint64_t rows, uint64_t cols, int products)
+{
+    return count >= 1 && rows >= 1 && cols >= 1 && rows <= kMostSide && cols <= kMostSide && rows * cols <= 0xFFFFFFFFull &&
+           (products == RTOPK_PRODUCTS_PAIRS || products == RTOPK_PRODUCTS_HALVES);
+}
+bool iteration_ok(uint32_t steps, const float *abc, float eps)
+{
+    return steps >= 1 && steps <= kMostSteps && abc && eps >= 0.0f && std::isfinite(eps) && coefficients_ok(abc, steps);
+}
+
+}  // namespace
+
+extern "C" int rtopk_orthogonalize_workspace_bytes(uint32_t count, uint64_t rows, uint64_t cols, int products, uint64_t *bytes)
+{
+    if (!bytes || !sizes_ok(count, rows, cols, products)) return RTOPK_EINVAL;
+    Parts p;
+    *bytes = cut(products, nullptr, std::min(count, kMembers), Shape{(u32)rows, (u32)cols}, false, p);
+    return RTOPK_OK;
+}
+
+extern "C" int rtopk_orthogonalize(uint32_t count, const void *const *x, int type, uint64_t rows, uint64_t cols, uint64_t ldx,
+                                   uint32_t steps, const float *coefficients, float eps, int products, void *const *out, int out_type,
+                                   uint64_t ldo, void *workspace, uint64_t workspace_bytes, void *stream_v)
+{
+    uint64_t need = 0;
+    if (!x || !out || !type_ok(type) || !type_ok(out_type) ||
+        rtopk_orthogonalize_workspace_bytes(count, rows, cols, products, &need) != RTOPK_OK)
+        return RTOPK_EINVAL;
+    if (ldx < cols || ldo < cols || !iteration_ok(steps, coefficients, eps)) return RTOPK_EINVAL;
+    for (uint32_t i = 0; i < count; ++i)
+        if (!x[i] || !out[i]) return RTOPK_EINVAL;
+    if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need) return RTOPK_EWORKSPACE;
+    hipStream_t stream = (hipStream_t)stream_v;
+    const Shape s{(u32)rows, (u32)cols};
+    Parts p;
+    cut(products, workspace, std::min(count, kMembers), s, false, p);
+    for (uint32_t first = 0; first < count; first += kMembers) {
+        const u32 members = std::min(count - first, kMembers);
+        Members from{};
+        Target to{Members{}, out_type, ldo, 0.0f, 0.0f, 0};
+        for (u32 i = 0; i < members; ++i) {
+            from.p[i] = const_cast<void *>(x[first + i]);
+            to.to.p[i] = out[first + i];
+        }
+        k_norm<<<dim3(kNormBlocks, members), kNormThreads, 0, stream>>>(from, type, s.rows, s.cols, ldx, p.norm);
+        if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
+        if (const int rc = iterate(products, from, type, ldx, s, members, steps, coefficients, eps, p, to, stream)) return rc;
+    }
+    return RTOPK_OK;
+}
+
+extern "C" int rtopk_aggregate_update_orthogonal_workspace_bytes(uint32_t count, uint64_t rows, uint64_t cols, int products,
+                                                                 uint64_t *bytes)
+{
+    if (!bytes || !sizes_ok(count, rows, cols, products)) return RTOPK_EINVAL;
+    Parts p;
+    *bytes = cut(products, nullptr, std::min(count, kMembers), Shape{(u32)rows, (u32)cols}, true, p);
+    return RTOPK_OK;
+}
+
+extern "C" int rtopk_aggregate_update_orthogonal(uint32_t count, const uint32_t *const *idx, const float *const *val, uint32_t n,
+                                                 uint64_t k, uint64_t rows, uint64_t cols, float eta, float scale, float mu,
+                                                 int nesterov, float decay, float gain, uint32_t steps, const float *coefficients,
+                                                 float eps, int products, float *const *omega, float *const *velocity,
+                                                 void *workspace, uint64_t workspace_bytes, void *stream_v)
+{
+    uint64_t need = 0;
+    if (!idx || !val || !omega || !velocity || n < 1 || k < 1 ||
+        rtopk_aggregate_update_orthogonal_workspace_bytes(count, rows, cols, products, &need) != RTOPK_OK)
+        return RTOPK_EINVAL;
+    if (!iteration_ok(steps, coefficients, eps)) return RTOPK_EINVAL;
+    const u64 d = rows * cols;
+    for (uint32_t i = 0; i < count; ++i) {
+        if (!idx[i] || !val[i] || !omega[i] || !velocity[i]) return RTOPK_EINVAL;
+        const uintptr_t w0 = (uintptr_t)omega[i], v0 = (uintptr_t)velocity[i];
+        if (w0 < v0 + d * 4 && v0 < w0 + d * 4) return RTOPK_EINVAL;
+    }
+    if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need) return RTOPK_EWORKSPACE;
+    hipStream_t stream = (hipStream_t)stream_v;
+    const Shape s{(u32)rows, (u32)cols};
+    Parts p;
+    cut(products, workspace, std::min(count, kMembers), s, true, p);
+    for (uint32_t first = 0; first < count; first += kMembers) {
+        const u32 members = std::min(count - first, kMembers);
+        Members velocities{}, steps_of{};
+        Target to{Members{}, RTOPK_F32, cols, -(eta * gain), 1.0f - eta * decay, 1};
+        for (u32 i = 0; i < members; ++i) {
+            float *average = p.average + i * align_up(d, 64);
+            if (const int rc = rtopk_aggregate(idx[first + i], val[first + i], n, k, d, average, nullptr, 0, stream_v)) return rc;
+            velocities.p[i] = velocity[first + i];
+            steps_of.p[i] = average;
+            to.to.p[i] = omega[first + i];
+        }
+        k_velocity<<<dim3(kNormBlocks, members), kNormThreads, 0, stream>>>(velocities, p.average, d, scale, mu, nesterov, p.norm);
+        if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
+        if (const int rc = iterate(products, steps_of, RTOPK_F32, cols, s, members, steps, coefficients, eps, p, to, stream)) return rc;
+    }
+    return RTOPK_OK;
+}

@@ -1,0 +1,287 @@
+"""8-bit quantisation, products and a layer's forward and backward on the GPU, against the definitions: the quantised
+numbers and scales bit for bit against binary32 arithmetic on the host, sums as whole numbers, everything after them in
+binary64 with the rounding of the steps that are left as the tolerance."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2005_10761_amd as rt
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+# relative rounding to the type, and the smallest step that it has
+ROUND = {"f32": (0.0, 0.0), "bf16": (2.0 ** -8, 1e-40), "f16": (2.0 ** -11, 2.0 ** -25)}
+
+
+def quantized(x, along):
+    """The definition, in binary32 on the host: (numbers, scales), turned over along columns."""
+    x = np.asarray(x, np.float32)
+    x = x if along == "rows" else x.T
+    with np.errstate(all="ignore"):
+        largest = np.abs(x).max(1) if x.shape[1] else np.zeros(x.shape[0], np.float32)
+        scale = (largest / np.float32(127)).astype(np.float32)
+        scale[scale < np.float32(2.0 ** -126)] = 0
+        scale[~np.isfinite(largest)] = np.nan
+        safe = np.where(scale > 0, scale, np.float32(1))[:, None]
+        q = np.where((scale > 0)[:, None], np.rint((x / safe).astype(np.float32)), 0)
+    return q.astype(np.int8), scale
+
+
+def laid(values, dtype, ld=None, offset=0):
+    """A device matrix whose rows are `ld` elements apart and which starts `offset` elements into its storage; what lies
+    between is garbage that must not matter."""
+    rows, cols = values.shape
+    ld = cols if ld is None else ld
+    store = torch.full((offset + rows * ld + 64,), 77, dtype=dtype, device=DEV)
+    view = store[offset:offset + rows * ld].view(rows, ld)[:, :cols]
+    view.copy_(torch.as_tensor(np.ascontiguousarray(values)).to(DEV).to(dtype))
+    return view
+
+
+def host(t):
+    return t.detach().float().cpu().numpy() if t.is_floating_point() else t.detach().cpu().numpy()
+
+
+def check_sums(out, kind, a, sa, b, sb, bias=None):
+    """out against sa_i sb_j sum + bias_j: the sum is exact, its binary32 form, two products and the bias round."""
+    sums = a.astype(np.int64) @ b.astype(np.int64).T if a.shape[1] < 4096 else (a.astype(np.float64) @ b.astype(np.float64).T)
+    scaled = sums.astype(np.float64) * np.outer(sa.astype(np.float64), sb.astype(np.float64))
+    want = scaled + (0.0 if bias is None else bias.astype(np.float64))
+    rel, least = ROUND[kind]
+    room = 2.0 ** -24 * (4 * np.abs(scaled) + 2 * np.abs(want))
+    room = room + rel * (np.abs(want) + room) + least + 1e-44
+    got = host(out).astype(np.float64)
+    assert got.shape == want.shape
+    if kind == "f16":                       # from half a step beyond the largest half on, an infinity
+        beyond = np.abs(want) >= 65520
+        close = np.abs(np.abs(want) - 65520) <= 2 * room
+        assert np.all((np.isinf(got) & (np.sign(got) == np.sign(want)))[beyond & ~close])
+        got, want, room = got[~beyond & ~close], want[~beyond & ~close], room[~beyond & ~close]
+    off = np.abs(got - want) > room
+    assert not off.any(), (np.argwhere(off)[:4], got[off][:4], want[off][:4], room[off][:4])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows, cols, pad, offset", [
+    (1, 1, 0, 0), (1, 1500, 0, 0), (3, 7, 1, 1), (5, 8, 0, 0), (64, 129, 3, 1), (130, 511, 1, 0), (1030, 40, 0, 0), (1100, 2052, 4, 3),
+    (7, 5000, 0, 0), (300, 64, 0, 0)])
+def test_quantized_numbers_and_scales(kind, rows, cols, pad, offset):
+    rng = np.random.default_rng(rows * 10_007 + cols)
+    x = (rng.standard_normal((rows, cols)) * np.exp(rng.standard_normal((rows, 1)))).astype(np.float32)
+    x[rng.random((rows, cols)) < 0.1] = 0
+    if rows > 4:
+        x[1] = 0                                            # a row of zeros
+        x[2] = 127.0 * np.where(rng.random(cols) < 0.5, 1, -1)
+        x[3] = np.round(x[3] * 64) / 128 + 0.0              # many halves: ties
+        x[3, 0] = 63.5
+    xd = laid(x, TYPES[kind], cols + pad, offset)
+    x = host(xd)                                            # as the type holds it
+    for along in ("rows", "columns"):
+        want_q, want_s = quantized(x, along)
+        r, c = want_q.shape
+        for ldq in (c, -(-c // 16) * 16 + 16):
+            store = torch.full((r * ldq + 16,), 99, dtype=torch.int8, device=DEV)
+            q = store[:r * ldq].view(r, ldq)[:, :c]
+            scale = torch.full((r,), -5.0, device=DEV)
+            rt.quantize_i8(xd, q, scale, along=along)
+            assert np.array_equal(host(scale).view(np.uint32), want_s.view(np.uint32)), along
+            assert np.array_equal(host(q), want_q), along
+            beyond = store[:r * ldq].view(r, ldq)[:, c:]
+            assert bool((beyond == 99).all()) and bool((store[r * ldq:] == 99).all())
+
+
+def test_quantized_special_rows():
+    cols = 300
+    x = np.ones((9, cols), np.float32)
+    x[0, 5] = np.nan
+    x[1, 299] = np.inf
+    x[2, 0] = -np.inf
+    x[3] = 0
+    x[4] = 1e-40                    # a scale that would be a subnormal: counts as zeros
+    x[5] = 127 * 2.0 ** -126        # the smallest that does not
+    x[6] = 3.4028235e38
+    x[7] = -0.0
+    xd = laid(x, torch.float32)
+    q, scale = torch.empty(9, cols, dtype=torch.int8, device=DEV), torch.empty(9, device=DEV)
+    rt.quantize_i8(xd, q, scale)
+    want_q, want_s = quantized(x, "rows")
+    assert np.array_equal(host(q), want_q)
+    assert np.array_equal(np.isnan(host(scale)), [True, True, True] + [False] * 6)
+    assert np.array_equal(host(scale)[3:], want_s[3:]) and host(scale)[4] == 0 and host(scale)[5] == np.float32(2.0 ** -126)
+    qc, sc = torch.empty(cols, 9, dtype=torch.int8, device=DEV), torch.empty(cols, device=DEV)
+    rt.quantize_i8(xd, qc, sc, along="columns")
+    want_q, want_s = quantized(x, "columns")
+    assert np.array_equal(host(qc), want_q) and np.array_equal(np.isnan(host(sc)), np.isnan(want_s))
+    # through a layer: NaN rows come out as NaN, rows without a scale as the bias
+    w = np.arange(-60, 60, dtype=np.int8)[:, None] * np.ones((1, cols), np.int8)
+    ws, bias = np.full(120, 0.5, np.float32), np.linspace(-1, 1, 120).astype(np.float32)
+    out = torch.empty(9, 120, device=DEV)
+    rt.linear_i8(xd, laid(w, torch.int8), torch.as_tensor(ws, device=DEV), out, bias=torch.as_tensor(bias, device=DEV))
+    got = host(out)
+    assert np.isnan(got[:3]).all()
+    assert np.array_equal(got[[3, 4, 7]], np.broadcast_to(bias, (3, 120)))
+    assert not np.isnan(got[3:]).any()
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("m, n, k", [
+    (1, 1, 1), (1, 10, 0), (2, 3, 15), (15, 17, 16), (16, 16, 64), (17, 100, 127), (33, 65, 128), (64, 64, 129), (100, 130, 500),
+    (129, 257, 640), (300, 70, 1500), (257, 513, 1024), (40, 48, 20_000)])
+def test_product(kind, m, n, k):
+    rng = np.random.default_rng(m * 1_000_003 + n * 1009 + k)
+    a = rng.integers(-128, 128, (m, k)).astype(np.int8)
+    b = rng.integers(-128, 128, (n, k)).astype(np.int8)
+    sa, sb = np.exp(rng.standard_normal(m)).astype(np.float32), np.exp(rng.standard_normal(n)).astype(np.float32) / 64
+    bias = rng.standard_normal(n).astype(np.float32)
+    dev = lambda v: torch.as_tensor(v, device=DEV)      # noqa: E731
+    # rows that start on 16 bytes; rows one after the other; rows that start anywhere
+    for lda, ldb, oa, ob, ldo in ((-(-k // 16) * 16 + 16, -(-k // 16) * 16, 0, 0, n), (max(k, 1), max(k, 1), 0, 0, n + 3),
+                                  (k + 3, k + 1, 1, 5, n + 1)):
+        ad, bd = laid(a, torch.int8, lda, oa), laid(b, torch.int8, max(ldb, 1), ob)
+        store = torch.full((m * ldo + 8,), 55.0, dtype=TYPES[kind], device=DEV)
+        out = store[:m * ldo].view(m, ldo)[:, :n]
+        rt.matmul_i8(ad, dev(sa), bd, dev(sb), out, bias=dev(bias))
+        check_sums(out, kind, a, sa, b, sb, bias)
+        assert bool((store[:m * ldo].view(m, ldo)[:, n:] == 55).all()) and bool((store[m * ldo:] == 55).all())
+    out = torch.empty(m, n, dtype=TYPES[kind], device=DEV)
+    rt.matmul_i8(ad, dev(sa), bd, dev(sb), out)
+    check_sums(out, kind, a, sa, b, sb)
+
+
+def test_product_of_sums_beyond_31_bits():
+    """140,000 products of -128 by -128 are 2^31 and more."""
+    k = 140_000
+    for m, n in ((3, 5), (200, 130)):
+        a, b = np.full((m, k), -128, np.int8), np.full((n, k), -128, np.int8)
+        b[1] = 127
+        one_m, one_n = np.ones(m, np.float32), np.ones(n, np.float32)
+        out = torch.empty(m, n, device=DEV)
+        rt.matmul_i8(laid(a, torch.int8), torch.as_tensor(one_m, device=DEV), laid(b, torch.int8), torch.as_tensor(one_n, device=DEV), out)
+        check_sums(out, "f32", a, one_m, b, one_n)
+
+
+def test_nothing_to_do():
+    z = lambda *s, t=torch.float32: torch.zeros(*s, dtype=t, device=DEV)     # noqa: E731
+    rt.matmul_i8(z(0, 8, t=torch.int8), z(0), z(4, 8, t=torch.int8), z(4), z(0, 4))
+    rt.linear_i8(z(0, 8), z(4, 8, t=torch.int8), z(4), z(0, 4))
+    rt.quantize_i8(z(0, 8), z(0, 8, t=torch.int8), z(0))
+    scale = torch.full((8,), 3.0, device=DEV)
+    rt.quantize_i8(z(0, 8), z(8, 0, t=torch.int8), scale, along="columns")
+    assert bool((scale == 0).all())
+    dw, db = torch.full((4, 8), 3.0, device=DEV), torch.full((4,), 3.0, device=DEV)
+    rt.linear_i8_backward(z(0, 4), z(0, 8), z(8, 4, t=torch.int8), z(8), z(0, 8), dw, db)
+    assert bool((dw == 0).all()) and bool((db == 0).all())
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("m, k, n, pad", [
+    (1, 1, 1, 0), (1, 1500, 1000, 4), (2, 130, 70, 0), (7, 515, 301, 1), (13, 2048, 160, 0), (16, 1024, 640, 16), (17, 64, 33, 0), (31, 4100, 48, 12),
+    (40, 256, 300, 0), (64, 999, 257, 1), (200, 384, 272, 0), (1, 20_000, 40, 0)])
+def test_forward(kind, m, k, n, pad):
+    rng = np.random.default_rng(m * 31 + k * 7 + n)
+    x = laid((rng.standard_normal((m, k)) * np.exp(rng.standard_normal((m, 1)))).astype(np.float32), TYPES[kind], k + pad, pad % 3)
+    w = rng.integers(-127, 128, (n, k)).astype(np.int8)
+    sw, bias = (np.exp(rng.standard_normal(n)) / 100).astype(np.float32), rng.standard_normal(n).astype(np.float32)
+    q, s = quantized(host(x), "rows")
+    dev = lambda v: torch.as_tensor(v, device=DEV)      # noqa: E731
+    for ldw, ow in ((-(-k // 16) * 16, 0), (k, 0), (k + 5, 3)):
+        for with_bias in (True, False):
+            out = torch.empty(m, n + 1, dtype=TYPES[kind], device=DEV)[:, :n]
+            rt.linear_i8(x, laid(w, torch.int8, ldw, ow), dev(sw), out, bias=dev(bias) if with_bias else None)
+            check_sums(out, kind, q, s, w, sw, bias if with_bias else None)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("m, k, n", [(1, 1, 1), (1, 70, 33), (5, 130, 64), (129, 65, 257), (300, 200, 100), (1025, 96, 40), (700, 260, 520)])
+def test_backward(kind, m, k, n):
+    rng = np.random.default_rng(m + 13 * k + 1009 * n)
+    x = laid((rng.standard_normal((m, k)) * (1 + 9 * (rng.random(k) < 0.05))).astype(np.float32), TYPES[kind], k + 8, 0)
+    dy = laid((1e-3 * rng.standard_normal((m, n)) * np.exp(rng.standard_normal((m, 1)))).astype(np.float32), TYPES[kind], n, 1)
+    w = laid((rng.standard_normal((n, k)) / np.sqrt(k)).astype(np.float32), torch.float32)
+    wq, ws = torch.empty(k, -(-n // 16) * 16, dtype=torch.int8, device=DEV)[:, :n], torch.empty(k, device=DEV)
+    rt.quantize_i8(w, wq, ws, along="columns")
+    dx = torch.empty(m, k, dtype=TYPES[kind], device=DEV)
+    dw, db = torch.empty(n, k, device=DEV), torch.empty(n, device=DEV)
+    rt.linear_i8_backward(dy, x, wq, ws, dx, dw, db)
+    xh, dyh = host(x), host(dy)
+    wt_q, wt_s = quantized(host(w), "columns")
+    check_sums(dx, kind, *quantized(dyh, "rows"), wt_q, wt_s)
+    a, sa = quantized(dyh, "columns")
+    b, sb = quantized(xh, "columns")
+    check_sums(dw, "f32", a, sa, b, sb)
+    # m additions in any order
+    room = (m + 2) * 2.0 ** -24 * np.abs(dyh).astype(np.float64).sum(0)
+    assert np.all(np.abs(host(db) - dyh.astype(np.float64).sum(0)) <= room)
+    # the formula's gradient, within half a step of what was quantised: |dw - dy^T x| <= sum |dy| sx / 2 + |x| sdy / 2 + sx sdy / 4
+    exact = dyh.astype(np.float64).T @ xh.astype(np.float64)
+    room = 0.5 * np.outer(np.abs(dyh).sum(0), sb) + 0.5 * np.outer(sa, np.abs(xh).sum(0)) + 0.25 * m * np.outer(sa, sb)
+    assert np.all(np.abs(host(dw) - exact) <= 1.001 * room + 1e-30)
+    # and against differences of the loss sum(dy * (x w^T + bias)) along one direction of the weights and the bias, which it is linear in
+    e, f = rng.standard_normal((n, k)), rng.standard_normal(n)
+    loss = lambda step: float((dyh.astype(np.float64) * (xh.astype(np.float64) @ (host(w) + step * e).T + step * f)).sum())   # noqa: E731
+    difference = (loss(0.5) - loss(-0.5))
+    along = float((host(dw).astype(np.float64) * e).sum() + (host(db).astype(np.float64) * f).sum())
+    wide = float((1.001 * room * np.abs(e)).sum() + ((m + 2) * 2.0 ** -24 * np.abs(dyh).sum(0) * np.abs(f)).sum()) + 1e-9 * abs(difference) + 1e-12
+    assert abs(along - difference) <= wide
+    # the parts alone are the same numbers
+    dx2, dw2 = torch.empty_like(dx), torch.empty_like(dw)
+    rt.linear_i8_backward(dy, None, wq, ws, dx2, None)
+    rt.linear_i8_backward(dy, x, None, None, None, dw2)
+    assert torch.equal(dx2, dx) and torch.equal(dw2, dw)
+
+
+def test_same_bits_on_another_stream_in_a_graph_and_again():
+    m, k, n = 333, 700, 260
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.randn(m, k, device=DEV, generator=g).bfloat16()
+    w = torch.randn(n, k, device=DEV, generator=g)
+    wq, ws = torch.empty(n, 704, dtype=torch.int8, device=DEV)[:, :k], torch.empty(n, device=DEV)
+    out = torch.empty(m, n, dtype=torch.bfloat16, device=DEV)
+    space = torch.empty(rt.linear_i8_workspace_bytes(m, k, n), dtype=torch.uint8, device=DEV)
+    space.fill_(0xA5)
+    rt.quantize_i8(w, wq, ws)
+    rt.linear_i8(x, wq, ws, out, workspace=space)
+    first = out.clone()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    other = torch.empty_like(out)
+    rt.linear_i8(x, wq, ws, other, stream=stream)
+    stream.synchronize()
+    assert torch.equal(other, first)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        rt.quantize_i8(w, wq, ws)
+        rt.linear_i8(x, wq, ws, out, workspace=space)
+    for step in range(3):
+        x.copy_(torch.randn(m, k, device=DEV, generator=g))
+        out.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        rt.linear_i8(x, wq, ws, other)
+        assert torch.equal(out, other), step
+
+
+def test_refusals_of_the_binding():
+    z = lambda *s, t=torch.float32: torch.zeros(*s, dtype=t, device=DEV)     # noqa: E731
+    i8 = torch.int8
+    with pytest.raises(TypeError):
+        rt.linear_i8(z(4, 8).t(), z(4, 4, t=i8), z(4), z(8, 4))             # columns in memory
+    with pytest.raises(TypeError):
+        rt.linear_i8(z(4, 8, t=torch.float64), z(4, 8, t=i8), z(4), z(4, 4))
+    with pytest.raises(ValueError):
+        rt.linear_i8(z(4, 8), z(4, 9, t=i8), z(4), z(4, 4))
+    with pytest.raises(ValueError):
+        rt.linear_i8(z(4, 8), z(5, 8, t=i8), z(4), z(4, 5))
+    with pytest.raises(ValueError):
+        rt.matmul_i8(z(4, 8, t=i8), z(4), z(5, 8, t=i8), z(5), z(4, 5), bias=z(4))
+    with pytest.raises(ValueError):
+        rt.quantize_i8(z(4, 8), z(4, 8, t=i8), z(8), along="columns")
+    with pytest.raises(KeyError):
+        rt.quantize_i8(z(4, 8), z(8, 4, t=i8), z(8), along="diagonals")
+    with pytest.raises(TypeError):
+        rt.linear_i8_backward(z(4, 8), z(4, 6), None, None, None, z(8, 6, t=torch.bfloat16))
+    with pytest.raises(rt.RtopkError) as e:
+        rt.linear_i8(z(4, 8), z(4, 8, t=i8), z(4), z(4, 4), workspace=z(16, t=torch.uint8))
+    assert e.value.code == -2
