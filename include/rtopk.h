@@ -381,8 +381,8 @@ int rtopk_linear_i8_backward(const void *dy, const void *x, int type,
  * out    HOST array of device pointers to [rows][ldo] of out_type; may be x
  * rows, cols  1 .. 2^21, rows * cols < 2^32
  * coefficients  HOST, [steps][3], 1 <= steps <= 64, read during the call. If
- *        singular values that start in [0, 1] can pass 7.5 (or what b A + c A A
- *        holds 60), the call returns RTOPK_EINVAL
+ *        singular values s that start in [0, 1] can pass 7.5 (or a + b s^2 +
+ *        c s^4 can pass 60), the call returns RTOPK_EINVAL
  * eps    >= 0. A matrix of zeros gives zeros (eps = 0 too); one that holds an
  *        infinity or a not-a-number gives NaN everywhere
  * workspace  device, 256-byte aligned, >= rtopk_orthogonalize_workspace_bytes

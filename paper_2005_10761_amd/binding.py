@@ -543,7 +543,8 @@ def orthogonalize(xs, outs, steps: Optional[int] = None, coefficients=QUINTIC, e
                   products: Optional[str] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """rtopk_orthogonalize: Newton-Schulz orthogonalisation of every matrix of the list ``xs`` (equal shapes, types and
     row distances) into ``outs`` (which may be ``xs``). ``products``: "pairs" (as exact as binary32) or "halves" (a
-    third of the time); None takes pairs for binary32 outputs and halves for 16-bit ones."""
+    third of the time); None takes halves for bfloat16 outputs, whose rounding is more than what they lose, and pairs
+    for others."""
     count = len(xs)
     if count < 1 or len(outs) != count:
         raise ValueError("xs and outs must have the same length >= 1")
@@ -553,7 +554,7 @@ def orthogonalize(xs, outs, steps: Optional[int] = None, coefficients=QUINTIC, e
         _matrix(b, "out", (out.dtype,) if out.dtype in _TYPES else _TYPES)
         if a.shape != x.shape or b.shape != x.shape or _ld(a) != _ld(x) or _ld(b) != _ld(out):
             raise ValueError("all matrices must have one shape, and one distance of their rows")
-    products = products or ("pairs" if out.dtype == torch.float32 else "halves")
+    products = products or ("halves" if out.dtype == torch.bfloat16 else "pairs")
     rows, cols = x.shape
     number, abc = _coefficients(coefficients, steps)
     ws, ws_bytes, held = _workspace(workspace, 0 if workspace is not None else

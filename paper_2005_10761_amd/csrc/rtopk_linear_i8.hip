@@ -37,28 +37,6 @@ __device__ __forceinline__ int quantized(float x, float s) { return s > 0.0f ? (
 
 __device__ __forceinline__ u32 magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
 
-// Eight neighbours from column c on, zeros beyond `cols`. `wide`: rows start on 16 bytes.
-__device__ __forceinline__ void read_eight(float (&v)[8], const void *row, u32 c, u32 cols, int type, bool wide)
-{
-    if (wide && c + 8u <= cols) {
-        if (type == 0) {
-            const f32x4 lo = *(const f32x4 *)((const float *)row + c), hi = *(const f32x4 *)((const float *)row + c + 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { v[i] = lo[i]; v[4 + i] = hi[i]; }
-        } else {
-            const i32x4 w = *(const i32x4 *)((const u16 *)row + c);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const u16 h = (u16)((u32)w[i >> 1] >> (16 * (i & 1)));
-                v[i] = type == 1 ? __uint_as_float((u32)h << 16) : (float)__builtin_bit_cast(_Float16, h);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? read_as(row, c + i, type) : 0.0f;
-    }
-}
-
 struct RowsToQuantize {
     const void *x;
     u64 ldx;            // elements
@@ -304,14 +282,12 @@ using namespace rtopk;
 
 namespace {
 
-typedef Tile<kBytes, 256, 256, 4, 2> Large;
-typedef Tile<kBytes, 128, 128, 2, 2> Middle;
-typedef Tile<kBytes, 64, 64, 2, 2> Small;
+typedef Tile<kBytes, 256, 256, 2, 4, 2, true> Large;
+typedef Tile<kBytes, 128, 128, 2, 2, 2, false> Middle;
+typedef Tile<kBytes, 64, 64, 2, 2, 2, false> Small;
 
 // A sum of so many slices of products of -128 .. 127 stays below 2^31.
 constexpr u32 kMostSlices = 1016;
-constexpr u32 kUnits = 256;
-
 enum Shape { kLarge, kMiddle, kSmall };
 struct Plan {
     Shape shape;

@@ -39,17 +39,33 @@ struct TileRows {
     u32 bytes;
 };
 
-template <Operands kOf, int kM, int kN, int kWavesM, int kWavesN>
+// A tile of kM x kN sums on kWavesM x kWavesN wavefronts, by instructions of kSide x kSide. Rates of a full chip at
+// 8192 x 8192 (8192 bytes of contraction; 10^12 operations a second, a product of pairs counted once):
+//                          bytes  halves  pairs
+//   256 x 256, 2 x 4, 16    2554    1240    479    kAhead; without it 2116 / 1090 (pairs never use it: 100 registers spilt)
+//   256 x 256, 2 x 4, 32    2359    1161    436
+//   256 x 256, 2 x 2, 16    2175    1112      -    (one wavefront a SIMD: nobody fills its waits)
+//   128 x 128, 2 x 2, 16    1953     949    464    (two workgroups a unit; alone on its unit 388)
+//   128 x 128, 2 x 2, 32    2131    1046    396
+// What bounds 256 x 256 is power: the matrix units are busy in 65% of the cycles, and the clock falls from 2.4 to 1.7 GHz.
+// kAhead: the first half of the next slice is read into registers before the second half of this one is multiplied.
+template <Operands kOf, int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kAhead>
 struct Tile {
     static constexpr int kRowsM = kM, kRowsN = kN;
     static constexpr int kWaves = kWavesM * kWavesN, kThreads = kWaves * kWave;
-    static constexpr int kStage = (kM + kN) * kSlice, kLds = 2 * kStage;
+    static constexpr int kStage = (kM + kN) * kSlice, kLds = kStages * kStage;
     static constexpr int kFragsM = kM / kWavesM / 16, kFragsN = kN / kWavesN / 16;
     static constexpr int kLoadsM = kM / 8 / kWaves, kLoadsN = kN / 8 / kWaves, kLoads = kLoadsM + kLoadsN;
     static_assert(kLoadsM * kWaves * 8 == kM && kLoadsN * kWaves * 8 == kN, "every wavefront loads whole groups of eight rows");
+    static_assert(kFragsM * kWavesM * 16 == kM && kFragsN * kWavesN * 16 == kN, "whole instructions");
+    static_assert(kStages >= 2 && (!kAhead || kStages == 2), "one slice under way at least");
     typedef typename Sums<kOf>::type Sum;
     // sum[i][j]: row 16 i + l % 16 of the wavefront's rows of A, rows 16 j + 4 (l / 16) .. + 3 of its rows of B
     Sum sum[kFragsM][kFragsN];
+    // half a slice: 64 bytes of the wavefront's rows
+    struct Half {
+        i32x4 a[kFragsM], b[kFragsN];
+    };
 
     static __device__ __forceinline__ u32 wave() { return (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)); }
     static __device__ __forceinline__ u32 row0() { return wave() / kWavesN * (kM / kWavesM); }
@@ -63,9 +79,12 @@ struct Tile {
             for (int j = 0; j < kFragsN; ++j) sum[i][j] = Sum{0, 0, 0, 0};
     }
 
-    // LDS holds a slice as rows of eight 16-byte pieces; piece c of row r lies in place c ^ (r / 2 % 8), so
-    // that sixteen rows' pieces of one c are in sixteen different groups of banks (two rows fill the 64 banks).
-    static __device__ __forceinline__ u32 place(u32 row, u32 piece) { return row * kSlice + ((piece ^ ((row >> 1) & 7u)) << 4); }
+    // LDS holds a slice as rows of eight 16-byte pieces; piece c of row r lies in place c ^ turn(r). Two rows fill the 64
+    // banks, and a 16-byte read takes sixteen lanes at a time, not in their order: 0-3, 12-15, 20-23, 24-27 (eight rows of
+    // one piece, eight others of the next) and so on. The turn puts what they read into sixteen different places: the
+    // counter of bank conflicts reads zero; with r / 2 % 8 every read took twice its cycles.
+    static __device__ __forceinline__ u32 turn(u32 row) { return (row & 2u) | ((row >> 1) & 4u); }
+    static __device__ __forceinline__ u32 place(u32 row, u32 piece) { return row * kSlice + ((piece ^ turn(row)) << 4); }
 
     // row of its operand that load q of this lane takes (the lane's piece of it: lane % 8, as placed)
     static __device__ __forceinline__ u32 row_of(int q)
@@ -76,6 +95,16 @@ struct Tile {
     static __device__ __forceinline__ u32 stage_at(int q)
     {
         return (q < kLoadsM ? 0 : kM * kSlice) + ((q < kLoadsM ? q : q - kLoadsM) * kWaves + wave()) * 8 * kSlice;
+    }
+
+    // Until at most kMore of this wavefront's loads to LDS are under way and all its reads from there are done, and until
+    // every wavefront of the workgroup has come as far. (A fence would wait for every load to LDS.)
+    template <int kMore>
+    static __device__ __forceinline__ void wait_and_meet()
+    {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kMore) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
     }
 
     // Adds the slices [from, to) of both operands. kWhole: rows start on 16 bytes (base and stride), and every slice
@@ -96,34 +125,64 @@ struct Tile {
             for (int q = 0; q < kLoads; ++q) {
                 const TileRows &t = q < kLoadsM ? a : b;
                 const u32 r = row_of(q), row = r < t.rows ? r : t.rows - 1u;
-                offset[q] = row * t.stride + (((lane & 7u) ^ ((r >> 1) & 7u)) << 4);
+                offset[q] = row * t.stride + (((lane & 7u) ^ turn(r)) << 4);
             }
             const auto ra = __builtin_amdgcn_make_buffer_rsrc((void *)a.first, 0, 0xFFFFFFFFu, 0x00020000);
             const auto rb = __builtin_amdgcn_make_buffer_rsrc((void *)b.first, 0, 0xFFFFFFFFu, 0x00020000);
-            auto load = [&](u32 slice, unsigned char *stage) {
+            auto load = [&](u32 slice) {
+                unsigned char *stage = lds + (slice - from) % kStages * kStage;
 #pragma unroll
                 for (int q = 0; q < kLoads; ++q)
                     __builtin_amdgcn_raw_ptr_buffer_load_lds(q < kLoadsM ? ra : rb,
                                                              (__attribute__((address_space(3))) void *)(stage + stage_at(q)), 16,
                                                              offset[q], slice * kSlice, 0, 0);
             };
-            load(s, lds);
-            for (; s < whole; ++s) {
-                // this wavefront's part of slice s has come; after the barrier everybody's has, and nobody reads the other stage
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                lds_barrier();
-                if (s + 1 < whole) load(s + 1, lds + ((s + 1 - from) & 1u) * kStage);
-                one_slice(lds + ((s - from) & 1u) * kStage);
+            load(s);
+            if constexpr (kAhead) {
+                if (s + 1 < whole) {
+                    load(s + 1);
+                    wait_and_meet<kLoads>();
+                } else {
+                    wait_and_meet<0>();
+                }
+                Half first, second;
+                read(first, lds, 0);
+                for (; s < whole; ++s) {
+                    read(second, lds + ((s - from) & 1u) * kStage, 1);
+                    add(first, first);
+                    mix();
+                    if (s + 1 < whole) {
+                        // this wavefront has read all of slice s, and its part of slice s + 1 has come; after the barrier
+                        // that holds for everybody: the stage of slice s may be overwritten, that of s + 1 read
+                        wait_and_meet<0>();
+                        if (s + 2 < whole) load(s + 2);
+                        read(first, lds + ((s + 1 - from) & 1u) * kStage, 0);
+                    }
+                    add(second, second);
+                    mix();
+                }
+            } else {
+#pragma unroll
+                for (int q = 1; q < kStages - 1; ++q)
+                    if (s + q < whole) load(s + q);
+                for (; s < whole; ++s) {
+                    // this wavefront's part of slice s has come (those of the kStages - 2 after it may be on their way); after
+                    // the barrier everybody's has, and nobody reads the stage of slice s - 1
+                    if (s + kStages - 2 < whole) wait_and_meet<(kStages - 2) * kLoads>();
+                    else wait_and_meet<0>();
+                    if (s + kStages - 1 < whole) load(s + kStages - 1);
+                    one_slice(lds + (s - from) % kStages * kStage);
+                }
             }
         }
         for (; s < to; ++s) {
-            unsigned char *stage = lds + ((s - from) & 1u) * kStage;
+            unsigned char *stage = lds + (s - from) % kStages * kStage;
             i32x4 piece[kLoads];
 #pragma unroll
             for (int q = 0; q < kLoads; ++q) {
                 const TileRows &t = q < kLoadsM ? a : b;
                 const u32 r = row_of(q), row = r < t.rows ? r : t.rows - 1u;
-                const u32 at = s * kSlice + (((lane_id() & 7u) ^ ((r >> 1) & 7u)) << 4);
+                const u32 at = s * kSlice + (((lane_id() & 7u) ^ turn(r)) << 4);
                 const unsigned char *p = t.first + (u64)row * t.stride + at;
                 if (at + 16u <= t.bytes) {
                     __builtin_memcpy(&piece[q], p, 16);
@@ -133,53 +192,67 @@ struct Tile {
                     piece[q] = i32x4{(int)word[0], (int)word[1], (int)word[2], (int)word[3]};
                 }
             }
+            // (everybody has read the slice that lay in this stage, two or more slices ago, before the barrier of the last one)
 #pragma unroll
             for (int q = 0; q < kLoads; ++q) *(i32x4 *)(stage + stage_at(q) + lane_id() * 16u) = piece[q];
-            lds_barrier();      // (a stage is written again two slices later: the barrier between keeps its readers apart)
+            lds_barrier();
             one_slice(stage);
         }
 #endif
     }
 
+    // half h of a slice in LDS
+    __device__ __forceinline__ void read(Half &f, const unsigned char *stage, u32 h) const
+    {
+        const u32 ra = row0() + (lane_id() & 15u), rb = col0() + (lane_id() & 15u), piece = 4 * h + (lane_id() >> 4);
+#pragma unroll
+        for (int j = 0; j < kFragsN; ++j) f.b[j] = *(const i32x4 *)(stage + kM * kSlice + place(rb + 16 * j, piece));
+#pragma unroll
+        for (int i = 0; i < kFragsM; ++i) f.a[i] = *(const i32x4 *)(stage + place(ra + 16 * i, piece));
+    }
+
     // one slice that lies in LDS, into the sums
     __device__ __forceinline__ void one_slice(const unsigned char *stage)
     {
-        const u32 lane = lane_id();
-        const u32 ra = row0() + (lane & 15u), rb = col0() + (lane & 15u);
-        i32x4 fa[2][kFragsM], fb[2][kFragsN];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int j = 0; j < kFragsN; ++j)
-                fb[h][j] = *(const i32x4 *)(stage + kM * kSlice + place(rb + 16 * j, 4 * h + (lane >> 4)));
-#pragma unroll
-            for (int i = 0; i < kFragsM; ++i) fa[h][i] = *(const i32x4 *)(stage + place(ra + 16 * i, 4 * h + (lane >> 4)));
-        }
+        Half first, second;
+        read(first, stage, 0);
+        read(second, stage, 1);
         if (kOf == kPairs) {
-            add(fa[0], fb[0]);
-            add(fa[1], fb[0]);
-            add(fa[0], fb[1]);
+            add(first, first);
+            add(second, first);
+            add(first, second);
         } else {
-            add(fa[0], fb[0]);
-            add(fa[1], fb[1]);
+            add(first, first);
+            add(second, second);
         }
     }
 
-    __device__ __forceinline__ void add(const i32x4 (&fa)[kFragsM], const i32x4 (&fb)[kFragsN])
+    __device__ __forceinline__ void add(const Half &a, const Half &b)
     {
 #pragma unroll
         for (int i = 0; i < kFragsM; ++i)
 #pragma unroll
             for (int j = 0; j < kFragsN; ++j) {
                 if constexpr (kOf == kBytes)
-                    sum[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[j], fa[i], sum[i][j], 0, 0, 0);
+                    sum[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b.b[j], a.a[i], sum[i][j], 0, 0, 0);
                 else
-                    sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, fb[j]),
-                                                                       __builtin_bit_cast(f16x8, fa[i]), sum[i][j], 0, 0, 0);
+                    sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, b.b[j]),
+                                                                       __builtin_bit_cast(f16x8, a.a[i]), sum[i][j], 0, 0, 0);
             }
     }
 
-    // act(row, col, sums): this lane's sums of rows row of A and col .. col + 3 of B, counted from the tile's first
+    // the reads of one half between the products of the other
+    __device__ __forceinline__ void mix() const
+    {
+#pragma unroll
+        for (int q = 0; q < kFragsM + kFragsN; ++q) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // a read from LDS
+            __builtin_amdgcn_sched_group_barrier(0x8, kFragsM * kFragsN / (kFragsM + kFragsN), 0);      // products
+        }
+    }
+
+    // act(row, col, sums): this lane's sums of row `row` of A and rows col .. col + 3 of B, counted from the tile's first.
+    // Every lane of the wavefront makes the same calls.
     template <class Act>
     __device__ __forceinline__ void each(Act act) const
     {
@@ -217,6 +290,28 @@ __device__ __forceinline__ float read_as(const void *p, u64 at, int type)
                        : (float)((const _Float16 *)p)[at];
 }
 
+// Eight neighbours from column c on, zeros beyond `cols`. `wide`: rows start on 16 bytes.
+__device__ __forceinline__ void read_eight(float (&v)[8], const void *row, u32 c, u32 cols, int type, bool wide)
+{
+    if (wide && c + 8u <= cols) {
+        if (type == 0) {
+            const f32x4 lo = *(const f32x4 *)((const float *)row + c), hi = *(const f32x4 *)((const float *)row + c + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[i] = lo[i]; v[4 + i] = hi[i]; }
+        } else {
+            const i32x4 w = *(const i32x4 *)((const u16 *)row + c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const u16 h = (u16)((u32)w[i >> 1] >> (16 * (i & 1)));
+                v[i] = type == 1 ? __uint_as_float((u32)h << 16) : (float)__builtin_bit_cast(_Float16, h);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? read_as(row, c + i, type) : 0.0f;
+    }
+}
+
 __device__ __forceinline__ u16 half_bits(float v, int type)
 {
     return type == 1 ? __builtin_bit_cast(u16, (__bf16)v) : __builtin_bit_cast(u16, (_Float16)v);
@@ -242,6 +337,28 @@ __device__ __forceinline__ void write_four(void *p, u64 at, int type, const f32x
     }
 }
 
-inline u32 type_bytes(int type) { return type == 0 ? 4u : 2u; }
+// What a launch of tiles costs, in microseconds, from times of full chips (256, 512, .. tiles) at 8 and 64 slices: a launch,
+// the tiles that one compute unit gets one after the other, their slices, and what comes before and after them. 64 x 64: up to
+// three tiles share a unit; 128 x 128: two.
+struct TileCost {
+    double slice64[3], slice128[2], slice192, slice256;      // one slice of one tile alone, of two (three) sharing a unit
+};
+constexpr TileCost kCostBytes{{0.29, 0.32, 0.54}, {0.62, 0.84}, 0.90, 1.60};
+constexpr TileCost kCostHalves{{0.29, 0.33, 0.54}, {0.61, 0.86}, 0.92, 1.46};
+constexpr TileCost kCostPairs{{0.30, 0.38, 0.57}, {0.70, 1.10}, 1.15, 1.97};
+constexpr u32 kUnits = 256;
+
+inline double tiles_cost(const TileCost &c, u32 edge, u64 tiles, double slices)
+{
+    const double each = (double)((tiles + kUnits - 1) / kUnits);
+    if (edge == 256) return 4.5 + each * (7.0 + slices * c.slice256);
+    if (edge == 192) return 4.5 + each * (4.6 + slices * c.slice192);
+    if (edge == 128) {
+        const double twos = (double)((u64)each / 2), one = each - 2 * twos;
+        return 4.5 + twos * (3.1 + slices * c.slice128[1]) + one * (1.5 + slices * c.slice128[0]);
+    }
+    const double threes = (double)((u64)each / 3), rest = each - 3 * threes;
+    return 4.5 + threes * (1.5 + slices * c.slice64[2]) + (rest > 0 ? 0.5 * rest + slices * c.slice64[(int)rest - 1] : 0.0);
+}
 
 }  // namespace rtopk

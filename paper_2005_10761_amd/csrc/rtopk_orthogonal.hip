@@ -3,11 +3,18 @@
 //
 //   X = G / (|G|_F + eps), turned over where G has more rows than columns
 //   each step, with coefficients (a, b, c):
-//     A = X X^T,  B = b A + c A A,  X <- a X + B X
+//     A = X X^T,  X <- (a I + b A + c A A) X
 //
-// All three products have both operands' rows along the contraction: A's rows
-// and B's are its columns too, and X is kept twice, as it is and turned over
-// (the product that makes a new X writes both). A and B are symmetric: only
+// as three products, with D = A - I in A's place:
+//     D = X X^T - I,  P = (a + b + c) I + (b + 2 c) D + c D D,  X <- P X.
+// Once the singular values are near 1, a, b A and c A A cancel (3.4, -4.8 and
+// 2.0 leave 0.7) and what A and B lost in rounding does not; D is small there,
+// and P has what is left of the cancellation, so that the result keeps its digits
+// (halves, a batch of 256 x 2304: relative error 14 10^-4 with A, B and a X + B X, see below for D and P).
+//
+// All three products have both operands' rows along the contraction: D's rows
+// and P's are its columns too, and X is kept twice, as it is and turned over
+// (the product that makes a new X writes both). D and P are symmetric: only
 // tiles on and above the diagonal are computed, and written on both sides.
 //
 // Numbers between the products are halves (11 bits; bfloat16, in common use
@@ -28,13 +35,27 @@
 
 namespace rtopk {
 
-// powers of two that X, A and B are stored with: singular values of X up to kMostX, entries of A up to its square,
-// entries of B up to kMostB stay finite
-constexpr int kLogX = 12, kLogA = 10;
-constexpr double kMostX = 7.5, kMostB = 60.0;
+// powers of two that X, D and P are stored with: singular values of X up to kMostX, entries of D up to its square,
+// entries of P up to kMostP stay finite
+constexpr int kLogX = 12, kLogD = 10;
+constexpr double kMostX = 7.5, kMostP = 60.0;
 constexpr u32 kMembers = 16;            // matrices in one launch
 
 struct Members { void *p[kMembers]; };
+
+// Four lanes with four halves each: lane i gets the i-th of all four.
+__device__ __forceinline__ uint2 turned_quad(uint2 d)
+{
+    const bool upper = (lane_id() & 2u) != 0, odd = (lane_id() & 1u) != 0;
+    // two lanes on: the lower two keep halves 0 and 1 of lanes q and q + 2, the upper two 2 and 3
+    const u32 got = (u32)__builtin_amdgcn_mov_dpp((int)(upper ? d.x : d.y), 0x4E /* quad_perm 2 3 0 1 */, 0xF, 0xF, true);
+    const u32 a = upper ? got : d.x, b = upper ? d.y : got;
+    // the neighbour: even lanes keep the low halves
+    const u32 give = odd ? (a & 0xFFFFu) | (b << 16) : (a >> 16) | (b & 0xFFFF0000u);
+    const u32 r = (u32)__builtin_amdgcn_mov_dpp((int)give, 0xB1 /* quad_perm 1 0 3 2 */, 0xF, 0xF, true);
+    return odd ? make_uint2((r & 0xFFFFu) | (a & 0xFFFF0000u), (r >> 16) | (b & 0xFFFF0000u))
+               : make_uint2((a & 0xFFFFu) | (r << 16), (b & 0xFFFFu) | (r & 0xFFFF0000u));
+}
 
 // ---- stored numbers -------------------------------------------------------
 // A row of halves, or of blocks of 128 bytes: 32 high halves, their 32 low halves.
@@ -57,11 +78,22 @@ template <Operands kOf> struct Stored {
             *(f16x4 *)(row + at(col) + 64) = lo;
         }
     }
-    static __device__ __forceinline__ void put(unsigned char *row, u32 col, float v)
+    // Every four lanes 4 q .. 4 q + 3 have a row each (neighbours, from a multiple of four on) and the same four columns:
+    // lane 4 q + i stores column i, the four rows side by side, to `column` of the matrix turned over.
+    static __device__ __forceinline__ void put_turned(unsigned char *column, u32 row, const f32x4 &v, bool there)
     {
-        const _Float16 hi = (_Float16)v;
-        *(_Float16 *)(row + at(col)) = hi;
-        if (kOf == kPairs) *(_Float16 *)(row + at(col) + 64) = (_Float16)(v - (float)hi);
+        f16x4 hi, lo;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            hi[c] = (_Float16)v[c];
+            lo[c] = (_Float16)(v[c] - (float)hi[c]);
+        }
+        const uint2 h = turned_quad(__builtin_bit_cast(uint2, hi));
+        if (there) *(uint2 *)(column + at(row & ~3u)) = h;
+        if (kOf == kPairs) {
+            const uint2 l = turned_quad(__builtin_bit_cast(uint2, lo));
+            if (there) *(uint2 *)(column + at(row & ~3u) + 64) = l;
+        }
     }
     static __device__ __forceinline__ f32x4 get(const unsigned char *row, u32 col)
     {
@@ -79,9 +111,9 @@ template <Operands kOf> struct Stored {
 };
 
 // ---- the norm ---------------------------------------------------------------
-constexpr u32 kNormThreads = 256, kNormBlocks = 64;
+constexpr u32 kNormThreads = 256, kNormBlocks = 512;     // workgroups (and parts of the sum) for one matrix, at most
 
-// the sum of the workgroup's values, in thread 0
+// the sum of the workgroup's values, in every thread
 __device__ __forceinline__ double block_sum(double v)
 {
     __shared__ double part[kNormThreads / kWave];
@@ -89,21 +121,30 @@ __device__ __forceinline__ double block_sum(double v)
     for (int o = kWave / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
     if (lane_id() == 0) part[threadIdx.x / kWave] = v;
     __syncthreads();
-    if (threadIdx.x == 0)
-        for (int w = 1; w < (int)(kNormThreads / kWave); ++w) v += part[w];
+    v = part[0];
+#pragma unroll
+    for (int w = 1; w < (int)(kNormThreads / kWave); ++w) v += part[w];
     return v;
 }
 
+// Pieces of eight neighbours of a matrix (from a multiple of eight columns on), each wavefront 64 of them at a time.
+// One read of the matrix: 10 us for four of 6000 x 1500 (14.4 TB/s, they come from the last-level cache).
 __global__ void __launch_bounds__(kNormThreads)
 k_norm(Members x, int type, u32 rows, u32 cols, u64 ld, double *__restrict__ part)
 {
     const void *g = x.p[blockIdx.y];
+    const u32 pieces = (cols + 7) / 8;
+    const u64 all = (u64)rows * pieces, step = (u64)gridDim.x * kNormThreads;
+    const u64 row_bytes = ld * (type == 0 ? 4u : 2u);
+    const bool wide = (((uintptr_t)g | row_bytes) & 15u) == 0;
     double sum = 0.0;
-    for (u32 r = blockIdx.x; r < rows; r += gridDim.x)
-        for (u32 c = threadIdx.x; c < cols; c += kNormThreads) {
-            const double v = (double)read_as(g, (u64)r * ld + c, type);
-            sum += v * v;
-        }
+    for (u64 at = (u64)blockIdx.x * kNormThreads + threadIdx.x; at < all; at += step) {
+        const u32 r = (u32)(at / pieces), c = (u32)(at - (u64)r * pieces) * 8u;
+        float v[8];
+        read_eight(v, (const unsigned char *)g + r * row_bytes, c, cols, type, wide);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += (double)v[i] * (double)v[i];
+    }
     sum = block_sum(sum);
     if (threadIdx.x == 0) part[blockIdx.y * kNormBlocks + blockIdx.x] = sum;
 }
@@ -116,13 +157,27 @@ k_velocity(Members velocity, float *__restrict__ average, u64 d, float scale, fl
 {
     float *v = (float *)velocity.p[blockIdx.y], *g = average + blockIdx.y * align_up(d, 64);
     double sum = 0.0;
-    for (u64 i = (u64)blockIdx.x * kNormThreads + threadIdx.x; i < d; i += (u64)gridDim.x * kNormThreads) {
-        const float u = scale * g[i], now = fmaf(mu, v[i], u);
-        v[i] = now;
-        const float to = nesterov ? fmaf(mu, now, u) : now;
-        g[i] = to;
+    auto step = [&](float &now, float &to) {
+        const float u = scale * to;
+        now = fmaf(mu, now, u);
+        to = nesterov ? fmaf(mu, now, u) : now;
         sum += (double)to * (double)to;
+    };
+    const u64 fours = ((uintptr_t)v & 15u) == 0 ? d / 4 : 0;
+    const u64 first = (u64)blockIdx.x * kNormThreads + threadIdx.x, stride = (u64)gridDim.x * kNormThreads;
+    for (u64 i = first; i < fours; i += stride) {
+        f32x4 now = *(const f32x4 *)(v + 4 * i), to = *(const f32x4 *)(g + 4 * i);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            float x = now[c], y = to[c];
+            step(x, y);
+            now[c] = x;
+            to[c] = y;
+        }
+        *(f32x4 *)(v + 4 * i) = now;
+        *(f32x4 *)(g + 4 * i) = to;
     }
+    for (u64 i = 4 * fours + first; i < d; i += stride) step(v[i], g[i]);
     sum = block_sum(sum);
     if (threadIdx.x == 0) part[blockIdx.y * kNormBlocks + blockIdx.x] = sum;
 }
@@ -136,6 +191,7 @@ struct Start {
     unsigned char *as_is, *turned;      // [rows] rows of cols, [cols] rows of rows
     u64 as_is_stride, turned_stride;    // from matrix to matrix
     const double *part;
+    u32 parts;
     float eps;
     float *rho;                         // what is left of the division, for the first step
 };
@@ -143,31 +199,22 @@ struct Start {
 constexpr u32 kSide = 64;
 
 template <Operands kOf>
-__global__ void __launch_bounds__(256) k_start(Start g)
+__global__ void __launch_bounds__(kNormThreads) k_start(Start g)
 {
     typedef Stored<kOf> S;
     __shared__ float tile[kSide][kSide + 1];
-    __shared__ int exponent;
     const u32 r0 = blockIdx.y * kSide, c0 = blockIdx.x * kSide, member = blockIdx.z;
-    if (threadIdx.x < kWave) {
-        double sum = threadIdx.x < kNormBlocks ? g.part[member * kNormBlocks + threadIdx.x] : 0.0;
-#pragma unroll
-        for (int o = kWave / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
-        const double norm = sqrt(sum);
-        int e = 0;
-        float rho;
-        if (norm > 0.0 && norm < __builtin_huge_val()) {
-            (void)frexp(norm, &e);
-            rho = (float)(ldexp(1.0, e) / (norm + (double)g.eps));
-        } else {
-            rho = norm == 0.0 ? 0.0f : __uint_as_float(0x7FC00000u);       // an infinity or a not-a-number: all of it is NaN
-        }
-        if (threadIdx.x == 0) {
-            exponent = e;
-            if (blockIdx.x == 0 && blockIdx.y == 0) g.rho[member] = rho;
-        }
+    double sum = 0.0;
+    for (u32 i = threadIdx.x; i < g.parts; i += kNormThreads) sum += g.part[member * kNormBlocks + i];
+    const double norm = sqrt(block_sum(sum));
+    int exponent = 0;
+    if (norm > 0.0 && norm < __builtin_huge_val()) (void)frexp(norm, &exponent);
+    if (threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) {
+        // zeros stay zeros; an infinity or a not-a-number makes all of it NaN
+        g.rho[member] = norm == 0.0 ? 0.0f
+                        : norm < __builtin_huge_val() ? (float)(ldexp(1.0, exponent) / (norm + (double)g.eps))
+                                                      : __uint_as_float(0x7FC00000u);
     }
-    __syncthreads();
     const int e = kLogX - exponent;
     for (u32 i = threadIdx.x; i < kSide * kSide; i += 256) {
         const u32 r = r0 + i / kSide, c = c0 + i % kSide;
@@ -194,11 +241,9 @@ struct Product {
     u64 left_stride, right_stride;          // from matrix to matrix
     u32 rows, cols, inner;                  // of the result, and numbers of the contraction
     u32 tiles_m, tiles_n, tiles;            // tiles: of one matrix
-    const unsigned char *old;               // kPoly: A; kNext, kLast: X with the result's orientation
-    u64 old_stride;
     unsigned char *out, *turned;            // the result, and turned over
     u64 out_stride, turned_stride;
-    float c_old, c_sum;
+    float c_sum, c_old, c_one;              // of the product, of D (kPoly) and of the identity (kPoly, and -1 in kGram)
     const float *rho;                       // first step only, else null
     // kLast
     Members to;
@@ -225,52 +270,54 @@ __global__ void __launch_bounds__(T::kThreads) k_step(Product g)
     }
     const u32 i0 = ti * T::kRowsM, j0 = tj * T::kRowsN;
     const u32 bytes = S::row_bytes(g.inner);
-    const TileRows a{g.left + member * g.left_stride + (u64)i0 * bytes, g.rows - i0, bytes, bytes};
+    const unsigned char *left = g.left + member * g.left_stride;
+    const TileRows a{left + (u64)i0 * bytes, g.rows - i0, bytes, bytes};
     const TileRows b{g.right + member * g.right_stride + (u64)j0 * bytes, g.cols - j0, bytes, bytes};
     T t;
     t.clear();
     t.template multiply<true>(a, b, 0, bytes / kSlice, lds);
 
     const float rho = g.rho ? g.rho[member] : 1.0f;
-    const float c_sum = kStep == kGram ? g.c_sum * rho * rho : g.c_sum * rho, c_old = g.c_old * rho;
+    const float c_sum = kStep == kGram ? g.c_sum * rho * rho : g.c_sum * rho;
     const u32 row_out = S::row_bytes(g.cols), row_turned = S::row_bytes(g.rows);
-    const unsigned char *old = g.old + member * g.old_stride;
     unsigned char *out = g.out + member * g.out_stride, *turned = g.turned + member * g.turned_stride;
     t.each([&](u32 r, u32 c, const f32x4 &sum) {
         const u32 row = i0 + r, col = j0 + c;
-        if (row >= g.rows || col >= S::padded(g.cols)) return;
+        const bool there = row < g.rows && col < S::padded(g.cols);
         f32x4 v = sum * c_sum;
-        if (kStep != kGram) v += c_old * S::get(old + (u64)row * row_out, col);
+        if (kStep == kPoly && there) v += g.c_old * S::get(left + (u64)row * bytes, col);      // (left is D)
 #pragma unroll
-        for (u32 q = 0; q < 4; ++q)
-            if (col + q >= g.cols) v[q] = 0.0f;
+        for (u32 q = 0; q < 4; ++q) {
+            if (kSymmetric && col + q == row) v[q] += g.c_one;
+            if (row >= g.rows || col + q >= g.cols) v[q] = 0.0f;        // what pads the rows is zero
+        }
         if (kStep == kLast) {
-            const u32 have = col < g.cols ? g.cols - col : 0u;
+            if (!there || col >= g.cols) return;
+            const u32 have = g.cols - col;
             void *to = g.to.p[member];
-            const u32 size = g.type == 0 ? 4u : 2u;
             const u64 first = (u64)row * g.ldo + col;
             if (g.update) {
                 float *w = (float *)to + first;
+                const bool wide = (((uintptr_t)to | (g.ldo * 4u)) & 15u) == 0 && have >= 4u;
+                f32x4 x;
 #pragma unroll
-                for (u32 q = 0; q < 4; ++q)
-                    if (q < have) w[q] = fmaf(g.gain, v[q], g.keep * w[q]);
+                for (u32 q = 0; q < 4; ++q) x[q] = wide || q >= have ? 0.0f : w[q];
+                if (wide) x = *(const f32x4 *)w;
+#pragma unroll
+                for (u32 q = 0; q < 4; ++q) x[q] = fmaf(g.gain, v[q], g.keep * x[q]);
+                write_four(to, first, 0, x, have, wide);
             } else {
+                const u32 size = g.type == 0 ? 4u : 2u;
                 write_four(to, first, g.type, v, have, (((uintptr_t)to | (g.ldo * size)) & (4u * size - 1u)) == 0);
             }
             return;
         }
-        S::put(out + (u64)row * row_out, col, v);
-        if (kSymmetric ? ti != tj : true)
-#pragma unroll
-            for (u32 q = 0; q < 4; ++q)
-                if (col + q < g.cols) S::put(turned + (u64)(col + q) * row_turned, row, v[q]);
+        if (there) S::put(out + (u64)row * row_out, col, v);
+        if (!kSymmetric || ti != tj) {
+            const u32 column = col + (lane_id() & 3u);
+            S::put_turned(turned + (u64)column * row_turned, row, v, column < g.cols && (row & ~3u) < S::padded(g.rows));
+        }
     });
-    // what pads the turned rows is zero
-    if (!kSymmetric && kStep != kLast && i0 + T::kRowsM >= g.rows) {
-        const u32 pad = S::padded(g.rows) - g.rows;
-        for (u32 i = threadIdx.x; i < T::kRowsN * pad; i += T::kThreads)
-            if (j0 + i / pad < g.cols) S::put(turned + (u64)(j0 + i / pad) * row_turned, g.rows + i % pad, 0.0f);
-    }
 }
 
 }  // namespace rtopk
@@ -281,8 +328,6 @@ namespace {
 
 constexpr u64 kMostSide = 1u << 21;      // offsets inside a tile of 256 rows fit 32 bits
 constexpr u32 kMostSteps = 64;
-constexpr u32 kUnits = 256;
-
 struct Shape {
     u32 rows, cols;
     u32 m() const { return std::min(rows, cols); }
@@ -293,8 +338,8 @@ struct Shape {
 struct Parts {
     double *norm;
     float *rho, *average;
-    unsigned char *x[2], *xt[2], *a, *b;
-    u64 x_stride, xt_stride, a_stride;
+    unsigned char *x[2], *xt[2], *d, *p;
+    u64 x_stride, xt_stride, d_stride;
 };
 
 template <Operands kOf>
@@ -306,15 +351,15 @@ u64 cut(void *base, u32 members, const Shape &s, bool average, Parts &p)
     auto take = [&](u64 bytes) { unsigned char *q = at + used; used += align_up(bytes, 256); return q; };
     p.x_stride = align_up((u64)s.m() * S::row_bytes(s.n()), 256);
     p.xt_stride = align_up((u64)s.n() * S::row_bytes(s.m()), 256);
-    p.a_stride = align_up((u64)s.m() * S::row_bytes(s.m()), 256);
+    p.d_stride = align_up((u64)s.m() * S::row_bytes(s.m()), 256);
     p.norm = (double *)take(kMembers * kNormBlocks * sizeof(double));
     p.rho = (float *)take(kMembers * sizeof(float));
     for (int i = 0; i < 2; ++i) {
         p.x[i] = take(members * p.x_stride);
         p.xt[i] = take(members * p.xt_stride);
     }
-    p.a = take(members * p.a_stride);
-    p.b = take(members * p.a_stride);
+    p.d = take(members * p.d_stride);
+    p.p = take(members * p.d_stride);
     p.average = average ? (float *)take(members * align_up((u64)s.rows * s.cols, 64) * sizeof(float)) : nullptr;
     return used;
 }
@@ -331,12 +376,12 @@ bool coefficients_ok(const float *abc, u32 steps)
     for (u32 s = 0; s < steps; ++s) {
         const double a = abc[3 * s], b = abc[3 * s + 1], c = abc[3 * s + 2];
         if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
-        // largest |a t + b t^3 + c t^5| and |b u + c u^2|, u = t^2, for t up to hi: at the ends or where the derivatives vanish
-        double x = 0.0, p = 0.0;
+        // largest |a t + b t^3 + c t^5| and |a + b u + c u^2|, u = t^2, for t up to hi: at the ends or where the derivatives vanish
+        double x = 0.0, p = std::fabs(a);
         auto look = [&](double u) {
             if (!(u > 0.0) || u > hi * hi) return;
             x = std::max(x, std::fabs(std::sqrt(u) * (a + u * (b + u * c))));
-            p = std::max(p, std::fabs(u * (b + u * c)));
+            p = std::max(p, std::fabs(a + u * (b + u * c)));
         };
         look(hi * hi);
         if (c != 0.0) {
@@ -349,7 +394,7 @@ bool coefficients_ok(const float *abc, u32 steps)
         } else if (b != 0.0) {
             look(-a / (3.0 * b));
         }
-        if (!(x <= kMostX) || !(p <= kMostB)) return false;
+        if (!(x <= kMostX) || !(p <= kMostP)) return false;
         hi = x;
     }
     return true;
@@ -368,13 +413,23 @@ int launch(Product g, u32 members, hipStream_t stream)
 template <Operands kOf, Step kStep>
 int launch(const Product &g, u32 members, hipStream_t stream)
 {
-    auto tiles = [&](u32 t) {
-        const u64 i = (g.rows + t - 1) / t, j = (g.cols + t - 1) / t;
-        return (kStep == kGram || kStep == kPoly ? j * (j + 1) / 2 : i * j) * members;
-    };
-    if (tiles(256) >= 200) return launch<kOf, Tile<kOf, 256, 256, 2, 4>, kStep>(g, members, stream);
-    if (tiles(128) >= 64) return launch<kOf, Tile<kOf, 128, 128, 2, 2>, kStep>(g, members, stream);
-    return launch<kOf, Tile<kOf, 64, 64, 2, 2>, kStep>(g, members, stream);
+    constexpr bool kAhead = kOf != kPairs;
+    const double slices = Stored<kOf>::row_bytes(g.inner) / kSlice;
+    u32 best = 0;
+    double least = 0.0;
+    for (const u32 edge : {64u, 128u, 192u, 256u}) {
+        const u64 i = (g.rows + edge - 1) / edge, j = (g.cols + edge - 1) / edge;
+        const u64 tiles = (kStep == kGram || kStep == kPoly ? j * (j + 1) / 2 : i * j) * members;
+        const double cost = tiles_cost(kOf == kPairs ? kCostPairs : kCostHalves, edge, tiles, slices);
+        if (!best || cost < least) {
+            best = edge;
+            least = cost;
+        }
+    }
+    if (best == 256) return launch<kOf, Tile<kOf, 256, 256, 2, 4, 2, kAhead>, kStep>(g, members, stream);
+    if (best == 192) return launch<kOf, Tile<kOf, 192, 192, 2, 4, 2, kAhead>, kStep>(g, members, stream);
+    if (best == 128) return launch<kOf, Tile<kOf, 128, 128, 2, 2, 2, false>, kStep>(g, members, stream);
+    return launch<kOf, Tile<kOf, 64, 64, 2, 2, 3, false>, kStep>(g, members, stream);
 }
 
 struct Target {
@@ -387,67 +442,62 @@ struct Target {
 
 // From G and the parts of its norm to the end.
 template <Operands kOf>
-int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 steps, const float *abc, float eps, const Parts &p,
-            const Target &target, hipStream_t stream)
+int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 norm_parts, u32 steps, const float *abc, float eps,
+            const Parts &p, const Target &target, hipStream_t stream)
 {
     typedef Stored<kOf> S;
     const u32 m = s.m(), n = s.n();
-    Start start{x, type, s.rows, s.cols, ldx, s.over() ? p.xt[0] : p.x[0], s.over() ? p.x[0] : p.xt[0],
-                s.over() ? p.xt_stride : p.x_stride, s.over() ? p.x_stride : p.xt_stride, p.norm, eps, p.rho};
-    const dim3 grid((std::max(S::padded(s.cols), s.cols) + kSide - 1) / kSide, (S::padded(s.rows) + kSide - 1) / kSide, members);
-    k_start<kOf><<<grid, 256, 0, stream>>>(start);
+    const Start start{x, type, s.rows, s.cols, ldx, s.over() ? p.xt[0] : p.x[0], s.over() ? p.x[0] : p.xt[0],
+                      s.over() ? p.xt_stride : p.x_stride, s.over() ? p.x_stride : p.xt_stride, p.norm, norm_parts, eps, p.rho};
+    const dim3 grid((S::padded(s.cols) + kSide - 1) / kSide, (S::padded(s.rows) + kSide - 1) / kSide, members);
+    k_start<kOf><<<grid, kNormThreads, 0, stream>>>(start);
     if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
     for (u32 i = 0; i < steps; ++i) {
         const unsigned char *xi = p.x[i & 1], *xti = p.xt[i & 1];
-        const float a = abc[3 * i], b = abc[3 * i + 1], c = abc[3 * i + 2];
+        const double a = abc[3 * i], b = abc[3 * i + 1], c = abc[3 * i + 2];
         const float *rho = i == 0 ? p.rho : nullptr;
         Product g{};
         g.left = g.right = xi;
         g.left_stride = g.right_stride = p.x_stride;
         g.rows = g.cols = m;
         g.inner = n;
-        g.old = p.a;
-        g.out = g.turned = p.a;
-        g.old_stride = g.out_stride = g.turned_stride = p.a_stride;
-        g.c_sum = ldexpf(1.0f, kLogA - 2 * kLogX);
+        g.out = g.turned = p.d;
+        g.out_stride = g.turned_stride = p.d_stride;
+        g.c_sum = ldexpf(1.0f, kLogD - 2 * kLogX);
+        g.c_one = -ldexpf(1.0f, kLogD);
         g.rho = rho;
         if (const int rc = launch<kOf, kGram>(g, members, stream)) return rc;
-        g.left = g.right = p.a;
-        g.left_stride = g.right_stride = p.a_stride;
+        g.left = g.right = p.d;
+        g.left_stride = g.right_stride = p.d_stride;
         g.inner = m;
-        g.out = g.turned = p.b;
-        g.c_old = b;
-        g.c_sum = c * ldexpf(1.0f, -kLogA);
+        g.out = g.turned = p.p;
+        g.c_sum = (float)(c * ldexp(1.0, -kLogD));
+        g.c_old = (float)(b + 2.0 * c);
+        g.c_one = (float)((a + b + c) * ldexp(1.0, kLogD));
         g.rho = nullptr;
         if (const int rc = launch<kOf, kPoly>(g, members, stream)) return rc;
         g.rho = rho;
         if (i + 1 < steps) {
-            g.left = p.b;
+            g.left = p.p;
             g.right = xti;
             g.right_stride = p.xt_stride;
             g.cols = n;
-            g.old = xi;
-            g.old_stride = p.x_stride;
             g.out = p.x[1 - (i & 1)];
             g.turned = p.xt[1 - (i & 1)];
             g.out_stride = p.x_stride;
             g.turned_stride = p.xt_stride;
-            g.c_old = a;
-            g.c_sum = ldexpf(1.0f, -kLogA);
+            g.c_sum = ldexpf(1.0f, -kLogD);
             if (const int rc = launch<kOf, kNext>(g, members, stream)) return rc;
             continue;
         }
         // the last product writes with G's orientation
-        g.left = s.over() ? xti : p.b;
-        g.right = s.over() ? p.b : xti;
-        g.left_stride = s.over() ? p.xt_stride : p.a_stride;
-        g.right_stride = s.over() ? p.a_stride : p.xt_stride;
+        g.left = s.over() ? xti : p.p;
+        g.right = s.over() ? p.p : xti;
+        g.left_stride = s.over() ? p.xt_stride : p.d_stride;
+        g.right_stride = s.over() ? p.d_stride : p.xt_stride;
         g.rows = s.rows;
         g.cols = s.cols;
-        g.old = s.over() ? xti : xi;
-        g.old_stride = s.over() ? p.xt_stride : p.x_stride;
-        g.c_old = a * ldexpf(1.0f, -kLogX);
-        g.c_sum = ldexpf(1.0f, -kLogA - kLogX);
+        g.c_sum = ldexpf(1.0f, -kLogD - kLogX);
         g.to = target.to;
         g.type = target.type;
         g.ldo = target.ld;
@@ -459,11 +509,19 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
     return RTOPK_OK;
 }
 
-int iterate(int products, const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 steps, const float *abc, float eps,
-            const Parts &p, const Target &target, hipStream_t stream)
+int iterate(int products, const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 norm_parts, u32 steps,
+            const float *abc, float eps, const Parts &p, const Target &target, hipStream_t stream)
 {
-    return products == RTOPK_PRODUCTS_PAIRS ? iterate<kPairs>(x, type, ldx, s, members, steps, abc, eps, p, target, stream)
-                                            : iterate<kHalves>(x, type, ldx, s, members, steps, abc, eps, p, target, stream);
+    return products == RTOPK_PRODUCTS_PAIRS
+               ? iterate<kPairs>(x, type, ldx, s, members, norm_parts, steps, abc, eps, p, target, stream)
+               : iterate<kHalves>(x, type, ldx, s, members, norm_parts, steps, abc, eps, p, target, stream);
+}
+
+// workgroups for the norm of one of so many matrices: a few elements for every thread, and not many more than fill the chip
+u32 norm_blocks(u64 d, u32 members)
+{
+    const u64 most = std::max<u64>(1, 8 * kUnits / members), enough = (d + 8 * kNormThreads - 1) / (8 * kNormThreads);
+    return (u32)std::min<u64>(std::min(most, enough), kNormBlocks);
 }
 
 bool type_ok(int type) { return type == RTOPK_F32 || type == RTOPK_BF16 || type == RTOPK_F16; }
@@ -511,9 +569,10 @@ extern "C" int rtopk_orthogonalize(uint32_t count, const void *const *x, int typ
             from.p[i] = const_cast<void *>(x[first + i]);
             to.to.p[i] = out[first + i];
         }
-        k_norm<<<dim3(kNormBlocks, members), kNormThreads, 0, stream>>>(from, type, s.rows, s.cols, ldx, p.norm);
+        const u32 parts = norm_blocks((u64)s.rows * s.cols, members);
+        k_norm<<<dim3(parts, members), kNormThreads, 0, stream>>>(from, type, s.rows, s.cols, ldx, p.norm);
         if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
-        if (const int rc = iterate(products, from, type, ldx, s, members, steps, coefficients, eps, p, to, stream)) return rc;
+        if (const int rc = iterate(products, from, type, ldx, s, members, parts, steps, coefficients, eps, p, to, stream)) return rc;
     }
     return RTOPK_OK;
 }
@@ -560,9 +619,10 @@ extern "C" int rtopk_aggregate_update_orthogonal(uint32_t count, const uint32_t 
             steps_of.p[i] = average;
             to.to.p[i] = omega[first + i];
         }
-        k_velocity<<<dim3(kNormBlocks, members), kNormThreads, 0, stream>>>(velocities, p.average, d, scale, mu, nesterov, p.norm);
+        const u32 parts = norm_blocks(d, members);
+        k_velocity<<<dim3(parts, members), kNormThreads, 0, stream>>>(velocities, p.average, d, scale, mu, nesterov, p.norm);
         if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
-        if (const int rc = iterate(products, steps_of, RTOPK_F32, cols, s, members, steps, coefficients, eps, p, to, stream)) return rc;
+        if (const int rc = iterate(products, steps_of, RTOPK_F32, cols, s, members, parts, steps, coefficients, eps, p, to, stream)) return rc;
     }
     return RTOPK_OK;
 }

@@ -99,7 +99,7 @@ def test_types_row_distances_and_members(kind, out_kind):
         xs = [laid(g, TYPES[kind], cols + pad, 1) for g in gs]
         outs = [laid(np.zeros((rows, cols), np.float32), TYPES[out_kind], cols + pad + 1, i % 2) for i in range(count)]
         rt.orthogonalize(xs, outs)
-        products = "pairs" if out_kind == "f32" else "halves"
+        products = "halves" if out_kind == "bf16" else "pairs"
         for x, out in zip(xs, outs):
             want, room = reference(host(x), products=products)
             check(out, want, room, out_kind, SHARP[products])
