@@ -32,10 +32,38 @@ __device__ __forceinline__ float scale_of(u32 largest)
     return s < 1.17549435e-38f ? 0.0f : s;
 }
 
-// x / s as a binary32 quotient, to the nearest whole number, ties to even; 0 where the scale is 0 or NaN
-__device__ __forceinline__ int quantized(float x, float s) { return s > 0.0f ? (int)rintf(x / s) : 0; }
+// Eight of them by one scale: x / s as a binary32 quotient, to the nearest whole number, ties to even; 0 where the scale
+// is 0 or NaN. The product by 1 / s is off the quotient by less than 127 * 2^-22, so it rounds the same way unless it is
+// as close to a tie: only then the division is made (a wavefront in ten; all divisions would be as long as the reads and writes).
+struct Quantizer {
+    float s, inv;
+    __device__ __forceinline__ explicit Quantizer(float scale) : s(scale), inv(scale > 0.0f ? 1.0f / scale : 0.0f) {}
+    template <int kN>
+    __device__ __forceinline__ void operator()(int (&q)[kN], const float (&x)[kN]) const
+    {
+        bool tie = false;
+        float t[kN];
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const float y = x[i] * inv;
+            t[i] = rintf(y);
+            tie |= fabsf(y - t[i]) > 0.4999f;
+        }
+        if (__any(tie)) {
+#pragma unroll
+            for (int i = 0; i < kN; ++i) t[i] = rintf(x[i] / s);
+        }
+#pragma unroll
+        for (int i = 0; i < kN; ++i) q[i] = s > 0.0f ? (int)t[i] : 0;
+    }
+};
 
 __device__ __forceinline__ u32 magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+__device__ __forceinline__ u32 four_bytes(const int *q)
+{
+    return ((u32)q[0] & 255u) | ((u32)q[1] & 255u) << 8 | ((u32)q[2] & 255u) << 16 | (u32)q[3] << 24;
+}
 
 struct RowsToQuantize {
     const void *x;
@@ -49,27 +77,37 @@ struct RowsToQuantize {
 
 constexpr int kQuantizeThreads = 256;
 
-// kWavesPerRow wavefronts read a row twice (the second time from the caches) and write it once; what lies between cols
-// and fill becomes zero.
-template <int kWavesPerRow>
-__global__ void __launch_bounds__(kQuantizeThreads) k_quantize_rows(RowsToQuantize g)
+// kWavesPerRow wavefronts hold a row in registers, kPieces pieces of eight numbers a lane (kPieces = 0: the row is
+// longer, and read twice, the second time from the caches). What lies between cols and fill becomes zero.
+template <int kWavesPerRow, int kPieces>
+__global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kQuantizeThreads) k_quantize_rows(RowsToQuantize g)
 {
-    constexpr u32 kRows = kQuantizeThreads / kWave / kWavesPerRow, kStep = 8u * kWave * kWavesPerRow;
-    __shared__ u32 most[kQuantizeThreads / kWave];
+    constexpr u32 kWaves = kWavesPerRow > 4 ? kWavesPerRow : 4, kRows = kWaves / kWavesPerRow, kStep = 8u * kWave * kWavesPerRow;
+    __shared__ u32 most[kWaves];
     const u32 lane = lane_id(), wave = threadIdx.x / kWave;
     const u32 r = blockIdx.x * kRows + wave / kWavesPerRow;
     const bool there = r < g.rows;
-    const unsigned char *row = (const unsigned char *)g.x + (u64)(there ? r : 0u) * g.ldx * (g.type == 0 ? 4u : 2u);
-    const bool wide = (((uintptr_t)g.x | (g.ldx * (g.type == 0 ? 4u : 2u))) & 15u) == 0;
-    const u32 c0 = (wave % kWavesPerRow * kWave + lane) * 8u;
+    const u64 row_bytes = g.ldx * (g.type == 0 ? 4u : 2u);
+    const unsigned char *row = (const unsigned char *)g.x + (there ? r : 0u) * row_bytes;
+    const bool wide = (((uintptr_t)g.x | row_bytes) & 15u) == 0;
+    const u32 c0 = (wave % kWavesPerRow * kWave + lane) * 8u, cols = there ? g.cols : 0u;
+    float held[kPieces ? kPieces : 1][8];
     u32 largest = 0;
-    if (there)
-        for (u32 c = c0; c < g.cols; c += kStep) {
-            float v[8];
-            read_eight(v, row, c, g.cols, g.type, wide);
+    auto look = [&](const float (&v)[8]) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) largest = max(largest, magnitude(v[i]));
+        for (int i = 0; i < 8; ++i) largest = max(largest, magnitude(v[i]));
+    };
+    if constexpr (kPieces > 0) {
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) read_eight(held[p], row, c0 + p * kStep, cols, g.type, wide);
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) look(held[p]);
+    } else {
+        for (u32 c = c0; c < cols; c += kStep) {
+            read_eight(held[0], row, c, cols, g.type, wide);
+            look(held[0]);
         }
+    }
     largest = wave_max_dpp(largest);
     if (kWavesPerRow > 1) {
         if (lane == 0) most[wave] = largest;
@@ -78,35 +116,45 @@ __global__ void __launch_bounds__(kQuantizeThreads) k_quantize_rows(RowsToQuanti
         for (int w = 0; w < kWavesPerRow; ++w) largest = max(largest, most[w]);
     }
     if (!there) return;
-    const float s = scale_of(largest);
-    if (c0 == 0) g.scale[r] = s;
+    const Quantizer quantize(scale_of(largest));
+    if (c0 == 0) g.scale[r] = quantize.s;
     signed char *q = g.q + (u64)r * g.ldq;
     const bool wide_q = (((uintptr_t)g.q | g.ldq) & 7u) == 0;
-    for (u32 c = c0; c < g.fill; c += kStep) {
-        float v[8];
-        read_eight(v, row, c, g.cols, g.type, wide);
-        u32 word[2] = {0u, 0u};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) word[i >> 2] |= ((u32)quantized(v[i], s) & 255u) << (8 * (i & 3));
+    auto write = [&](const float (&v)[8], u32 c) {
+        int n[8];
+        quantize(n, v);
+        const u32 word[2] = {four_bytes(n), four_bytes(n + 4)};
         if (wide_q && c + 8u <= g.fill) {
             *(uint2 *)(q + c) = make_uint2(word[0], word[1]);
         } else {
-            for (u32 i = 0; i < 8u && c + i < g.fill; ++i) q[c + i] = (signed char)(word[i >> 2] >> (8 * (i & 3)));
+#pragma unroll
+            for (u32 i = 0; i < 8u; ++i)
+                if (c + i < g.fill) q[c + i] = (signed char)(word[i >> 2] >> (8 * (i & 3)));
+        }
+    };
+    if constexpr (kPieces > 0) {
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) write(held[p], c0 + p * kStep);
+    } else {
+        for (u32 c = c0; c < g.fill; c += kStep) {
+            read_eight(held[0], row, c, cols, g.type, wide);
+            write(held[0], c);
         }
     }
 }
 
 // Columns: a first kernel leaves the largest magnitude (and, where asked, the sum) of each column of each run of rows, a
 // second one takes the runs together, quantises and turns the matrix over.
-constexpr u32 kRunRows = 256, kMostRuns = 64;
+constexpr u32 kGroup = 8 * kWave;           // columns of one workgroup of the first, eight a lane
+constexpr u32 kMostRuns = 64;
 
-inline u32 run_rows(u32 rows)
+inline u32 run_rows(u32 rows, u32 cols)
 {
-    u32 each = kRunRows;
-    while ((rows + each - 1) / each > kMostRuns) each *= 2;
-    return each;
+    // two workgroups a compute unit, 16 rows at least
+    const u32 groups = (cols + kGroup - 1) / kGroup, runs = std::min(kMostRuns, (2 * kUnits + groups - 1) / groups);
+    return std::max((rows + runs - 1) / runs, 16u);
 }
-inline u32 runs_of(u32 rows) { return rows ? (rows + run_rows(rows) - 1) / run_rows(rows) : 0u; }
+inline u32 runs_of(u32 rows, u32 cols) { return (rows + run_rows(rows, cols) - 1) / run_rows(rows, cols); }
 
 struct ColumnsToQuantize {
     const void *x;
@@ -124,72 +172,130 @@ struct ColumnsToQuantize {
 
 __global__ void __launch_bounds__(kQuantizeThreads) k_column_most(ColumnsToQuantize g)
 {
-    __shared__ u32 most[kQuantizeThreads / kWave][kWave];
-    __shared__ float sums[kQuantizeThreads / kWave][kWave];
-    const u32 lane = lane_id(), wave = threadIdx.x / kWave, c = blockIdx.x * kWave + lane;
+    constexpr u32 kWaves = kQuantizeThreads / kWave, kAtOnce = 8;
+    __shared__ u32 most[kWaves - 1][kGroup];
+    __shared__ float sums[kWaves - 1][kGroup];
+    const u32 lane = lane_id(), wave = threadIdx.x / kWave, c = blockIdx.x * kGroup + lane * 8u;
     const u32 r0 = blockIdx.y * g.run, r1 = min(r0 + g.run, g.rows);
-    u32 largest = 0;
-    float sum = 0.0f;
-    if (c < g.cols)
-        for (u32 r = r0 + wave; r < r1; r += kQuantizeThreads / kWave) {
-            const float v = read_as(g.x, (u64)r * g.ldx + c, g.type);
-            largest = max(largest, magnitude(v));
-            sum += v;
-        }
-    most[wave][lane] = largest;
-    sums[wave][lane] = sum;
-    __syncthreads();
-    if (wave != 0 || c >= g.cols) return;
+    const u64 row_bytes = g.ldx * (g.type == 0 ? 4u : 2u);
+    const bool wide = (((uintptr_t)g.x | row_bytes) & 15u) == 0;
+    u32 largest[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (u32 r = r0 + wave; r < r1; r += kAtOnce * kWaves) {
+        float v[kAtOnce][8];
 #pragma unroll
-    for (int w = 1; w < kQuantizeThreads / kWave; ++w) {
-        largest = max(largest, most[w][lane]);
-        sum += sums[w][lane];
+        for (u32 q = 0; q < kAtOnce; ++q) {
+            const u32 at = r + q * kWaves;
+            read_eight(v[q], (const unsigned char *)g.x + (at < r1 ? at : r) * row_bytes, c, at < r1 ? g.cols : 0u, g.type, wide);
+        }
+#pragma unroll
+        for (u32 q = 0; q < kAtOnce; ++q)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                largest[i] = max(largest[i], magnitude(v[q][i]));
+                sum[i] += v[q][i];
+            }
     }
-    g.most[(u64)blockIdx.y * g.cols + c] = largest;
-    if (g.sums) g.sums[(u64)blockIdx.y * g.cols + c] = sum;
+    if (wave) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            most[wave - 1][i * kWave + lane] = largest[i];
+            sums[wave - 1][i * kWave + lane] = sum[i];
+        }
+    }
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+        for (u32 w = 0; w < kWaves - 1; ++w) {
+            largest[i] = max(largest[i], most[w][i * kWave + lane]);
+            sum[i] += sums[w][i * kWave + lane];
+        }
+        if (c + i < g.cols) {
+            g.most[(u64)blockIdx.y * g.cols + c + i] = largest[i];
+            if (g.sums) g.sums[(u64)blockIdx.y * g.cols + c + i] = sum[i];
+        }
+    }
 }
 
-constexpr u32 kTurnRows = 128;
+// A workgroup turns some blocks of 64 columns and 128 rows over: a lane reads eight columns of four rows, and puts
+// the four numbers of each column side by side into LDS.
+constexpr u32 kTurnRows = 128, kMostBlocks = 4;
 
-__global__ void __launch_bounds__(kQuantizeThreads) k_quantize_columns(ColumnsToQuantize g)
+__global__ void __launch_bounds__(kQuantizeThreads) k_quantize_columns(ColumnsToQuantize g, u32 blocks)
 {
+    constexpr u32 kParts = kQuantizeThreads / kWave;
     __shared__ float scale[kWave];
+    __shared__ u32 most[kParts][kWave];
+    __shared__ double sums[kParts][kWave];
     __shared__ u32 turned[kWave][kTurnRows / 4 + 1];
-    const u32 lane = lane_id(), wave = threadIdx.x / kWave, c0 = blockIdx.x * kWave, c = c0 + lane, r0 = blockIdx.y * kTurnRows;
-    if (wave == 0 && c < g.cols) {
+    const u32 lane = lane_id(), wave = threadIdx.x / kWave, c0 = blockIdx.x * kWave, first = blockIdx.y * blocks * kTurnRows;
+    const bool totals = g.total && first == 0;
+    {
+        const u32 c = min(c0 + lane, g.cols - 1u);
         u32 largest = 0;
         double sum = 0.0;
-        for (u32 s = 0; s < g.runs; ++s) {
-            largest = max(largest, g.most[(u64)s * g.cols + c]);
-            if (g.total && r0 == 0) sum += (double)g.sums[(u64)s * g.cols + c];
+        for (u32 s = wave; s < g.runs; s += kParts) largest = max(largest, g.most[(u64)s * g.cols + c]);
+        if (totals)
+            for (u32 s = wave; s < g.runs; s += kParts) sum += (double)g.sums[(u64)s * g.cols + c];
+        most[wave][lane] = largest;
+        sums[wave][lane] = sum;
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (u32 w = 1; w < kParts; ++w) {
+                largest = max(largest, most[w][lane]);
+                sum += sums[w][lane];
+            }
+            scale[lane] = scale_of(largest);
+            if (first == 0 && c0 + lane < g.cols) {
+                g.scale[c0 + lane] = scale[lane];
+                if (totals) g.total[c0 + lane] = (float)sum;
+            }
         }
-        scale[lane] = scale_of(largest);
-        if (r0 == 0) {
-            g.scale[c] = scale[lane];
-            if (g.total) g.total[c] = (float)sum;
-        }
+        __syncthreads();
     }
-    __syncthreads();
-    const float s = c < g.cols ? scale[lane] : 0.0f;
-    for (u32 i = wave; i < kTurnRows / 4; i += kQuantizeThreads / kWave) {
-        u32 word = 0;
+    const u64 row_bytes = g.ldx * (g.type == 0 ? 4u : 2u);
+    const bool wide = (((uintptr_t)g.x | row_bytes) & 15u) == 0, wide_q = (((uintptr_t)g.q | g.ldq) & 15u) == 0;
+    const u32 piece = threadIdx.x & 7u, quad = threadIdx.x >> 3, c = c0 + 8u * piece;       // columns c .. c + 7 of rows 4 quad .. + 3
+    float s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = scale[8 * piece + i];
+    for (u32 block = 0; block < blocks; ++block) {
+        const u32 r0 = first + block * kTurnRows;
+        if (r0 >= g.fill) break;
+        float v[4][8];
 #pragma unroll
         for (u32 b = 0; b < 4; ++b) {
-            const u32 r = r0 + 4 * i + b;
-            if (c < g.cols && r < g.rows) word |= ((u32)quantized(read_as(g.x, (u64)r * g.ldx + c, g.type), s) & 255u) << (8 * b);
+            const u32 r = r0 + 4 * quad + b;
+            read_eight(v[b], (const unsigned char *)g.x + (r < g.rows ? r : 0u) * row_bytes, c, r < g.rows ? g.cols : 0u, g.type, wide);
         }
-        turned[lane][i] = word;
-    }
-    __syncthreads();
-    const bool wide = (((uintptr_t)g.q | g.ldq) & 3u) == 0;
-    for (u32 i = threadIdx.x; i < kWave * (kTurnRows / 4); i += kQuantizeThreads) {
-        const u32 row = c0 + i / (kTurnRows / 4), at = r0 + 4 * (i % (kTurnRows / 4));
-        if (row >= g.cols || at >= g.fill) continue;
-        const u32 word = turned[i / (kTurnRows / 4)][i % (kTurnRows / 4)];
-        signed char *q = g.q + (u64)row * g.ldq + at;
-        if (wide && at + 4u <= g.fill) *(u32 *)q = word;
-        else
-            for (u32 b = 0; b < 4u && at + b < g.fill; ++b) q[b] = (signed char)(word >> (8 * b));
+        if (block) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const Quantizer quantize(s[i]);
+            int n[4];
+            quantize(n, {v[0][i], v[1][i], v[2][i], v[3][i]});
+            turned[8 * piece + i][quad] = four_bytes(n);
+        }
+        __syncthreads();
+#pragma unroll
+        for (u32 h = 0; h < 2; ++h) {
+            const u32 col = (threadIdx.x >> 3) + 32 * h, at = 16u * (threadIdx.x & 7u);
+            if (c0 + col >= g.cols || r0 + at >= g.fill) continue;
+            u32 word[4];
+#pragma unroll
+            for (u32 b = 0; b < 4; ++b) word[b] = turned[col][at / 4 + b];
+            signed char *q = g.q + (u64)(c0 + col) * g.ldq + r0 + at;
+            if (wide_q && r0 + at + 16u <= g.fill) {
+                *(uint4 *)q = make_uint4(word[0], word[1], word[2], word[3]);
+            } else {
+#pragma unroll
+                for (u32 b = 0; b < 16u; ++b)
+                    if (r0 + at + b < g.fill) q[b] = (signed char)(word[b >> 2] >> (8 * (b & 3)));
+            }
+        }
     }
 }
 
@@ -208,19 +314,33 @@ struct Scaled {
     int *part;                  // [splits][m][n rounded up to 4], splits > 1 only
 };
 
-__device__ __forceinline__ void write_scaled(const Scaled &g, u32 row, u32 col, const f32x4 &sum)
+// four neighbours of a row of the result, and their channels' scales and biases
+struct Four {
+    f32x4 scale, bias;
+};
+__device__ __forceinline__ Four channels(const Scaled &g, u32 col)
 {
-    const float s = g.a_scale[row];
-    const u32 have = g.n - col;
-    f32x4 v;
+    Four f;
+    const bool all = col + 4u <= g.n;
 #pragma unroll
     for (u32 c = 0; c < 4; ++c) {
-        const u32 at = c < have ? col + c : col;
-        v[c] = sum[c] * s * g.b_scale[at] + (g.bias ? g.bias[at] : 0.0f);
+        const u32 at = all || col + c < g.n ? col + c : g.n - 1u;
+        f.scale[c] = g.b_scale[at];
+        f.bias[c] = g.bias ? g.bias[at] : 0.0f;
     }
+    return f;
+}
+__device__ __forceinline__ bool wide_out(const Scaled &g)
+{
     const u32 size = g.type == 0 ? 4u : 2u;
-    const bool wide = (((uintptr_t)g.out | (g.ldo * size)) & (4u * size - 1u)) == 0;
-    write_four(g.out, (u64)row * g.ldo + col, g.type, v, have, wide);
+    return (((uintptr_t)g.out | (g.ldo * size)) & (4u * size - 1u)) == 0;
+}
+__device__ __forceinline__ void write_scaled(const Scaled &g, u32 row, u32 col, const f32x4 &sum, float a_scale, const Four &f, bool wide)
+{
+    f32x4 v;
+#pragma unroll
+    for (u32 c = 0; c < 4; ++c) v[c] = fmaf(sum[c] * a_scale, f.scale[c], f.bias[c]);
+    write_four(g.out, (u64)row * g.ldo + col, g.type, v, g.n - col, wide);
 }
 
 template <class T, bool kWhole>
@@ -239,10 +359,22 @@ __global__ void __launch_bounds__(T::kThreads) k_product(Scaled g)
     t.clear();
     t.template multiply<kWhole>(a, b, from, min(from + g.slices_each, slices), lds);
     if (g.splits == 1) {
-        t.each([&](u32 r, u32 c, const i32x4 &sum) {
-            if (i0 + r < g.m && j0 + c < g.n)
-                write_scaled(g, i0 + r, j0 + c, f32x4{(float)sum[0], (float)sum[1], (float)sum[2], (float)sum[3]});
-        });
+        const bool wide = wide_out(g);
+        float a_scale[T::kFragsM];
+#pragma unroll
+        for (int i = 0; i < T::kFragsM; ++i) a_scale[i] = g.a_scale[min(i0 + T::row0() + 16u * i + (lane_id() & 15u), g.m - 1u)];
+#pragma unroll
+        for (int j = 0; j < T::kFragsN; ++j) {
+            const u32 col = j0 + T::col0() + 16u * j + 4u * (lane_id() >> 4);
+            if (col >= g.n) continue;
+            const Four f = channels(g, col);
+#pragma unroll
+            for (int i = 0; i < T::kFragsM; ++i) {
+                const u32 row = i0 + T::row0() + 16u * i + (lane_id() & 15u);
+                const i32x4 sum = t.sum[i][j];
+                if (row < g.m) write_scaled(g, row, col, f32x4{(float)sum[0], (float)sum[1], (float)sum[2], (float)sum[3]}, a_scale[i], f, wide);
+            }
+        }
     } else {
         const u64 ld = align_up(g.n, 4);
         int *part = g.part + (u64)split * g.m * ld;
@@ -257,6 +389,7 @@ __global__ void __launch_bounds__(256) k_product_join(Scaled g)
 {
     const u32 fours = (g.n + 3) / 4;
     const u64 all = (u64)g.m * fours, ld = 4ull * fours;
+    const bool wide = wide_out(g);
     for (u64 at = (u64)blockIdx.x * 256 + threadIdx.x; at < all; at += (u64)gridDim.x * 256) {
         const u32 row = (u32)(at / fours), col = (u32)(at - (u64)row * fours) * 4u;
         double sum[4] = {0, 0, 0, 0};
@@ -265,7 +398,139 @@ __global__ void __launch_bounds__(256) k_product_join(Scaled g)
 #pragma unroll
             for (int c = 0; c < 4; ++c) sum[c] += (double)v[c];
         }
-        write_scaled(g, row, col, f32x4{(float)sum[0], (float)sum[1], (float)sum[2], (float)sum[3]});
+        write_scaled(g, row, col, f32x4{(float)sum[0], (float)sum[1], (float)sum[2], (float)sum[3]}, g.a_scale[row], channels(g, col), wide);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Few tokens: one read of the weights. A workgroup has 16 channels; its wavefronts share the contraction and add up in
+// LDS. A lane's 16 bytes of a row of weights are its part of the instruction's operand as they come, at any alignment; the
+// tokens are the other operand, kTokens x 16 of them.
+// ---------------------------------------------------------------------------
+constexpr u32 kFewTokens = 64;          // at most
+constexpr u32 kInOne = 8192;            // numbers of x up to which every workgroup quantises them for itself (one launch less)
+
+struct Few {
+    Scaled s;                           // a: quantised tokens, or null
+    const void *x;
+    u64 ldx;
+    int type;
+};
+
+template <int kWaves, int kTokens, bool kQuantize>
+__global__ void __launch_bounds__(kWaves * kWave) k_few(Few f)
+{
+    constexpr u32 kBatch = 8;
+    const Scaled &g = f.s;
+    const u32 lane = lane_id(), wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+    const u32 channel = blockIdx.x * 16u + (lane & 15u), piece = (lane >> 4) * 16u;
+    extern __shared__ __align__(16) unsigned char lds[];
+    __shared__ float token_scale[kTokens * 16];
+    __shared__ u32 most[kTokens * 16];
+    const u32 steps = (g.k + 63u) / 64u;
+    const u32 each = (steps + kWaves - 1) / kWaves, from = min(wave * each, steps), to = min(from + each, steps);
+    const unsigned char *w = (const unsigned char *)g.b + (u64)min(channel, g.n - 1u) * g.ldb;
+    i32x4 sum[kTokens], held[kBatch];
+#pragma unroll
+    for (int t = 0; t < kTokens; ++t) sum[t] = i32x4{0, 0, 0, 0};
+    const u32 whole = min(to, g.k / 64u);
+    auto fetch = [&](u32 s) {
+        if (s + kBatch <= whole) {
+#pragma unroll
+            for (u32 q = 0; q < kBatch; ++q) __builtin_memcpy(&held[q], w + (s + q) * 64u + piece, 16);
+        } else {
+#pragma unroll
+            for (u32 q = 0; q < kBatch; ++q) held[q] = load_piece(w, (s + q) * 64u + piece, g.k);
+#pragma unroll
+            for (u32 q = 0; q < kBatch; ++q) held[q] = cut_piece(held[q], (s + q) * 64u + piece, g.k);
+        }
+    };
+    fetch(from);                            // the first weights are on their way while x is quantised
+    const u32 row = steps * 64u + 16u;      // bytes of a token in LDS (16 more: tokens start in different banks)
+    if constexpr (kQuantize) {
+        // every thread holds up to kHeld pieces of eight, whatever token they are of: one trip to memory
+        constexpr u32 kHeld = (kInOne / 8 + kFewTokens + kWaves * kWave - 1) / (kWaves * kWave);
+        const u64 row_bytes = f.ldx * (f.type == 0 ? 4u : 2u);
+        const bool wide = (((uintptr_t)f.x | row_bytes) & 15u) == 0;
+        const u32 pieces = (g.k + 7u) / 8u, all = g.m * pieces;
+        float v[kHeld][8];
+#pragma unroll
+        for (u32 h = 0; h < kHeld; ++h) {
+            const u32 at = threadIdx.x + h * kWaves * kWave, t = at / pieces;
+            read_eight(v[h], (const unsigned char *)f.x + (at < all ? t : 0u) * row_bytes, (at - t * pieces) * 8u, at < all ? g.k : 0u, f.type, wide);
+        }
+        if (threadIdx.x < kTokens * 16) most[threadIdx.x] = 0u;
+        __syncthreads();
+#pragma unroll
+        for (u32 h = 0; h < kHeld; ++h) {
+            const u32 at = threadIdx.x + h * kWaves * kWave, t = at / pieces;
+            u32 largest = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) largest = max(largest, magnitude(v[h][i]));
+            if (g.m == 1) {
+                largest = wave_max_dpp(largest);
+                if (lane == 0) atomicMax(&most[0], largest);
+            } else if (at < all) {
+                atomicMax(&most[t], largest);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (u32 h = 0; h < kHeld; ++h) {
+            const u32 at = threadIdx.x + h * kWaves * kWave, t = at / pieces, c = (at - t * pieces) * 8u;
+            const Quantizer quantize(scale_of(most[at < all ? t : 0u]));
+            int n[8];
+            quantize(n, v[h]);
+            if (at >= all) continue;
+            if (c == 0) token_scale[t] = quantize.s;
+            *(uint2 *)(lds + t * row + c) = make_uint2(four_bytes(n), four_bytes(n + 4));
+        }
+        // what fills a token's last step (the weights there are zeros, but the numbers have to be some)
+        for (u32 at = threadIdx.x; at < g.m * 8u; at += kWaves * kWave) {
+            const u32 c = (pieces + (at & 7u)) * 8u;
+            if (c < steps * 64u) *(uint2 *)(lds + (at >> 3) * row + c) = make_uint2(0u, 0u);
+        }
+        __syncthreads();
+    } else {
+        if (threadIdx.x < g.m) token_scale[threadIdx.x] = g.a_scale[threadIdx.x];
+    }
+    for (u32 s = from; s < to; s += kBatch) {
+        i32x4 now[kBatch];
+#pragma unroll
+        for (u32 q = 0; q < kBatch; ++q) now[q] = held[q];
+        if (s + kBatch < to) fetch(s + kBatch);
+#pragma unroll
+        for (u32 q = 0; q < kBatch; ++q) {
+            if (s + q >= to) break;
+#pragma unroll
+            for (int t = 0; t < kTokens; ++t) {
+                const u32 token = min(16u * t + (lane & 15u), g.m - 1u), at = (s + q) * 64u + piece;
+                const i32x4 x = kQuantize ? *(const i32x4 *)(lds + token * row + at) : *(const i32x4 *)(g.a + (u64)token * g.lda + at);
+                sum[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now[q], x, sum[t], 0, 0, 0);
+            }
+        }
+    }
+    // lane l: token l % 16 of each sixteen, channels 4 (l / 16) .. + 3
+    __syncthreads();
+    i32x4 *part = (i32x4 *)lds;
+    if (wave) {
+#pragma unroll
+        for (int t = 0; t < kTokens; ++t) part[((wave - 1) * kTokens + t) * kWave + lane] = sum[t];
+    }
+    __syncthreads();
+    if (wave) return;
+    const u32 col = blockIdx.x * 16u + 4u * (lane >> 4);
+    if (col >= g.n) return;
+    const Four four = channels(g, col);
+    const bool wide_o = wide_out(g);
+#pragma unroll
+    for (int t = 0; t < kTokens; ++t) {
+        // (a sum of kMostSteps steps stays below 2^31: longer contractions do not come here)
+        for (int o = 0; o < kWaves - 1; ++o) sum[t] += part[(o * kTokens + t) * kWave + lane];
+        const u32 token = 16u * t + (lane & 15u);
+        if (token < g.m)
+            write_scaled(g, token, col, f32x4{(float)sum[t][0], (float)sum[t][1], (float)sum[t][2], (float)sum[t][3]}, token_scale[token],
+                         four, wide_o);
     }
 }
 
@@ -282,35 +547,35 @@ using namespace rtopk;
 
 namespace {
 
-typedef Tile<kBytes, 256, 256, 2, 4, 2, true> Large;
-typedef Tile<kBytes, 128, 128, 2, 2, 2, false> Middle;
-typedef Tile<kBytes, 64, 64, 2, 2, 2, false> Small;
-
 // A sum of so many slices of products of -128 .. 127 stays below 2^31.
 constexpr u32 kMostSlices = 1016;
-enum Shape { kLarge, kMiddle, kSmall };
+
 struct Plan {
-    Shape shape;
-    u32 tiles, slices, slices_each, splits;
+    u32 edge, tiles, slices, slices_each, splits;
     u64 part_bytes;
 };
 
+// The tile and the number of runs of the contraction that cost least. Runs cost a launch, and four bytes of every sum
+// written and read.
 Plan plan_product(u32 m, u32 n, u32 k)
 {
-    Plan p{};
-    auto tiles = [&](u32 t) { return (u64)((m + t - 1) / t) * ((n + t - 1) / t); };
-    p.shape = tiles(256) >= 200 ? kLarge : tiles(128) >= 64 ? kMiddle : kSmall;
-    const u32 edge = p.shape == kLarge ? 256 : p.shape == kMiddle ? 128 : 64;
-    p.tiles = (u32)tiles(edge);
-    p.slices = (k + kSlice - 1) / kSlice;
-    u32 splits = p.tiles ? 2 * kUnits / p.tiles : 1;
-    splits = std::min(splits, p.slices / 4);
-    splits = std::max(splits, (p.slices + kMostSlices - 1) / kMostSlices);
-    splits = std::max(splits, 1u);
-    p.slices_each = std::max(1u, (p.slices + splits - 1) / splits);
-    p.splits = std::max(1u, (p.slices + p.slices_each - 1) / p.slices_each);
-    p.part_bytes = p.splits > 1 ? align_up((u64)p.splits * m * align_up(n, 4) * 4, 256) : 0;
-    return p;
+    Plan best{};
+    double least = 0.0;
+    const u32 slices = (k + kSlice - 1) / kSlice, must = std::max(1u, (slices + kMostSlices - 1) / kMostSlices);
+    for (const u32 edge : {64u, 128u, 192u, 256u}) {
+        const u64 tiles = (u64)((m + edge - 1) / edge) * ((n + edge - 1) / edge);
+        for (u32 splits = must; splits <= std::max(must, std::min(16u, slices / 4)); ++splits) {
+            const u32 each = std::max(1u, (slices + splits - 1) / splits);
+            if (splits > must && (slices + each - 1) / each != splits) continue;
+            double cost = tiles_cost(kCostBytes, edge, tiles * splits, each);
+            if (splits > 1) cost += 4.0 + (double)m * n * splits * 8.0 / 4e6;
+            if (best.edge && cost >= least) continue;
+            least = cost;
+            best = Plan{edge, (u32)tiles, slices, each, std::max(1u, (slices + each - 1) / each), 0};
+        }
+    }
+    best.part_bytes = best.splits > 1 ? align_up((u64)best.splits * m * align_up(n, 4) * 4, 256) : 0;
+    return best;
 }
 
 template <class T>
@@ -320,6 +585,28 @@ void launch_product(const Scaled &g, const Plan &p, bool whole, hipStream_t stre
     else k_product<T, false><<<p.tiles * p.splits, T::kThreads, 0, stream>>>(g);
 }
 
+template <int kWaves, int kTokens>
+void launch_few(const Few &f, hipStream_t stream)
+{
+    const u32 blocks = (f.s.n + 15) / 16, sums = (kWaves - 1) * kTokens * kWave * 16;
+    const u32 tokens = f.s.a ? 0 : f.s.m * ((f.s.k + 63) / 64 * 64 + 16);
+    if (f.s.a) k_few<kWaves, kTokens, false><<<blocks, kWaves * kWave, sums, stream>>>(f);
+    else k_few<kWaves, kTokens, true><<<blocks, kWaves * kWave, std::max(sums, tokens), stream>>>(f);
+}
+
+bool few_tokens(u32 m, u32 k) { return m <= kFewTokens && k <= kMostSlices * kSlice; }
+bool in_one(u32 m, u32 k) { return few_tokens(m, k) && (u64)m * k <= kInOne; }
+
+// fewer than two workgroups a unit: each has sixteen wavefronts
+int run_few(const Few &f, hipStream_t stream)
+{
+    const bool many = f.s.n >= 2 * kUnits * 16;
+    if (f.s.m <= 16) many ? launch_few<4, 1>(f, stream) : launch_few<16, 1>(f, stream);
+    else if (f.s.m <= 32) many ? launch_few<4, 2>(f, stream) : launch_few<16, 2>(f, stream);
+    else many ? launch_few<4, 4>(f, stream) : launch_few<8, 4>(f, stream);
+    return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_EHIP;
+}
+
 int run_product(Scaled g, void *part, hipStream_t stream)
 {
     const Plan p = plan_product(g.m, g.n, g.k);
@@ -327,9 +614,10 @@ int run_product(Scaled g, void *part, hipStream_t stream)
     g.splits = p.splits;
     g.part = (int *)part;
     const bool whole = (((uintptr_t)g.a | (uintptr_t)g.b | g.lda | g.ldb) & 15u) == 0;
-    if (p.shape == kLarge) launch_product<Large>(g, p, whole, stream);
-    else if (p.shape == kMiddle) launch_product<Middle>(g, p, whole, stream);
-    else launch_product<Small>(g, p, whole, stream);
+    if (p.edge == 256) launch_product<Tile<kBytes, 256, 256, 2, 4, 2, true>>(g, p, whole, stream);
+    else if (p.edge == 192) launch_product<Tile<kBytes, 192, 192, 2, 4, 2, true>>(g, p, whole, stream);
+    else if (p.edge == 128) launch_product<Tile<kBytes, 128, 128, 2, 2, 2, false>>(g, p, whole, stream);
+    else launch_product<Tile<kBytes, 64, 64, 2, 2, 3, false>>(g, p, whole, stream);
     if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
     if (p.splits > 1) {
         const u64 blocks = ((u64)g.m * ((g.n + 3) / 4) + 255) / 256;
@@ -349,24 +637,32 @@ int quantize_rows(const void *x, int type, u32 rows, u32 cols, u64 ldx, signed c
                   hipStream_t stream)
 {
     const RowsToQuantize g{x, ldx, rows, cols, fill, type, q, ldq, scale};
-    if (rows >= 4 * kUnits) k_quantize_rows<1><<<(rows + 3) / 4, kQuantizeThreads, 0, stream>>>(g);
-    else k_quantize_rows<4><<<rows, kQuantizeThreads, 0, stream>>>(g);
+    // what a wavefront's lanes hold in one piece each is 512 numbers: one wavefront for a short row where there are many
+    if (fill <= 512 && rows >= 4 * kUnits) k_quantize_rows<1, 1><<<(rows + 3) / 4, kQuantizeThreads, 0, stream>>>(g);
+    else if (fill <= 1024 && rows >= 4 * kUnits) k_quantize_rows<1, 2><<<(rows + 3) / 4, kQuantizeThreads, 0, stream>>>(g);
+    else if (fill <= 2048) k_quantize_rows<4, 1><<<rows, kQuantizeThreads, 0, stream>>>(g);
+    else if (fill <= 4096) k_quantize_rows<4, 2><<<rows, kQuantizeThreads, 0, stream>>>(g);
+    else if (fill <= 8192) k_quantize_rows<4, 4><<<rows, kQuantizeThreads, 0, stream>>>(g);
+    else if (fill <= 16384) k_quantize_rows<16, 2><<<rows, 16 * kWave, 0, stream>>>(g);
+    else k_quantize_rows<16, 0><<<rows, 16 * kWave, 0, stream>>>(g);
     return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_EHIP;
 }
 
-u64 column_scratch(u32 rows, u32 cols, bool sums) { return align_up((u64)runs_of(rows) * cols * (sums ? 8 : 4), 256); }
+u64 column_scratch(u32 rows, u32 cols, bool sums) { return align_up((u64)runs_of(rows, cols) * cols * (sums ? 8 : 4), 256); }
 
 int quantize_columns(const void *x, int type, u32 rows, u32 cols, u64 ldx, signed char *q, u64 ldq, u32 fill, float *scale,
                      float *total, void *scratch, hipStream_t stream)
 {
-    const u32 runs = runs_of(rows);
+    const u32 runs = runs_of(rows, cols);
     u32 *most = (u32 *)scratch;
-    const ColumnsToQuantize g{x, ldx, rows, cols, fill, run_rows(rows), runs, type, q, ldq, scale, most,
+    const ColumnsToQuantize g{x, ldx, rows, cols, fill, run_rows(rows, cols), runs, type, q, ldq, scale, most,
                               total ? (float *)(most + (u64)runs * cols) : nullptr, total};
-    const u32 groups = (cols + kWave - 1) / kWave;
-    k_column_most<<<dim3(groups, runs), kQuantizeThreads, 0, stream>>>(g);
+    k_column_most<<<dim3((cols + kGroup - 1) / kGroup, runs), kQuantizeThreads, 0, stream>>>(g);
     if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
-    k_quantize_columns<<<dim3(groups, (fill + kTurnRows - 1) / kTurnRows), kQuantizeThreads, 0, stream>>>(g);
+    // as many blocks for a workgroup (each of which takes the runs together) as leave four workgroups a unit
+    const u32 groups = (cols + kWave - 1) / kWave, all = (fill + kTurnRows - 1) / kTurnRows;
+    const u32 blocks = std::max(1u, std::min(kMostBlocks, (u32)((u64)groups * all / (4 * kUnits))));
+    k_quantize_columns<<<dim3(groups, (all + blocks - 1) / blocks), kQuantizeThreads, 0, stream>>>(g, blocks);
     return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_EHIP;
 }
 
@@ -394,9 +690,10 @@ struct LinearParts {
 u64 cut_linear(void *base, u32 m, u32 k, u32 n, LinearParts &p)
 {
     Cut cut{(unsigned char *)base};
+    if (in_one(m, k)) return 0;
     p.x = cut.take<signed char>(m * filled(k));
     p.x_scale = cut.take<float>(4ull * m);
-    p.part = cut.take<void>(plan_product(m, n, k).part_bytes);
+    p.part = cut.take<void>(few_tokens(m, k) ? 0 : plan_product(m, n, k).part_bytes);
     return cut.at;
 }
 
@@ -486,12 +783,13 @@ extern "C" int rtopk_linear_i8(const void *x, int type, uint64_t m, uint64_t k, 
     if (!x || !w || !w_scale || !out) return RTOPK_EINVAL;
     if (!workspace_ok(workspace, workspace_bytes, need)) return RTOPK_EWORKSPACE;
     hipStream_t stream = (hipStream_t)stream_v;
-    LinearParts p;
+    LinearParts p{};
     cut_linear(workspace, (u32)m, (u32)k, (u32)n, p);
     const u64 ld = filled((u32)k);
+    const Scaled g{p.x, w, ld, ldw, (u32)m, (u32)n, (u32)k, p.x_scale, w_scale, bias, out, ldo, out_type, 0, 0, nullptr};
+    if (in_one((u32)m, (u32)k)) return run_few(Few{g, x, ldx, type}, stream);
     if (const int rc = quantize_rows(x, type, (u32)m, (u32)k, ldx, p.x, ld, (u32)ld, p.x_scale, stream)) return rc;
-    return run_product(Scaled{p.x, w, ld, ldw, (u32)m, (u32)n, (u32)k, p.x_scale, w_scale, bias, out, ldo, out_type, 0, 0, nullptr},
-                       p.part, stream);
+    return few_tokens((u32)m, (u32)k) ? run_few(Few{g, nullptr, 0, 0}, stream) : run_product(g, p.part, stream);
 }
 
 extern "C" int rtopk_linear_i8_backward_workspace_bytes(uint64_t m, uint64_t k, uint64_t n, uint64_t *bytes)

@@ -31,13 +31,41 @@ template <> struct Sums<kBytes> { typedef i32x4 type; };
 
 // One operand of a tile: the row that the tile starts with, the rows that are
 // there from it on (rows past them repeat the last one: what they give is not
-// stored), the bytes from row to row and the bytes of a row that count.
+// stored), the bytes from row to row and the bytes of a row that count (the
+// same for both operands).
 struct TileRows {
     const unsigned char *first;
     u32 rows;
     u32 stride;
     u32 bytes;
 };
+
+// 16 bytes from byte `at` of a row of `bytes` bytes, zeros beyond its end; what is not there is not read. In two parts, so that
+// several loads are under way together: the load takes the row's last 16 bytes where it would go beyond them, and
+// cut_piece moves them down. (A branch around each load, which waits for it, made the last slice of an odd contraction
+// cost as much as forty others: 16 us of 55 at 1499 x 5001 x 2003.)
+__device__ __forceinline__ i32x4 load_piece(const unsigned char *row, u32 at, u32 bytes)
+{
+    i32x4 v{0, 0, 0, 0};
+    if (bytes >= 16u) {
+        __builtin_memcpy(&v, row + min(at, bytes - 16u), 16);
+    } else {
+        u64 half[2] = {0, 0};
+        for (u32 c = 0; c < bytes; ++c) half[c >> 3] |= (u64)row[c] << (8u * (c & 7u));
+        v = i32x4{(int)(u32)half[0], (int)(half[0] >> 32), (int)(u32)half[1], (int)(half[1] >> 32)};
+    }
+    return v;
+}
+__device__ __forceinline__ i32x4 cut_piece(const i32x4 &v, u32 at, u32 bytes)
+{
+    const u32 start = bytes >= 16u ? bytes - 16u : 0u, down = at > start ? at - start : 0u;     // bytes to move by
+    const u64 lo = (u64)(u32)v[0] | (u64)(u32)v[1] << 32, hi = (u64)(u32)v[2] | (u64)(u32)v[3] << 32;
+    const u32 bits = 8u * (down & 7u);
+    const u64 a = down >= 8u ? hi : lo, b = down >= 8u ? 0ull : hi;
+    u64 x = bits ? a >> bits | b << (64u - bits) : a, y = b >> bits;
+    if (down >= 16u) x = y = 0ull;
+    return i32x4{(int)(u32)x, (int)(x >> 32), (int)(u32)y, (int)(y >> 32)};
+}
 
 // A tile of kM x kN sums on kWavesM x kWavesN wavefronts, by instructions of kSide x kSide. Rates of a full chip at
 // 8192 x 8192 (8192 bytes of contraction; 10^12 operations a second, a product of pairs counted once):
@@ -102,7 +130,8 @@ struct Tile {
     template <int kMore>
     static __device__ __forceinline__ void wait_and_meet()
     {
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kMore) : "memory");
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt((kMore & 15) | (kMore >> 4) << 14 | 0x70);       // vmcnt(kMore) lgkmcnt(0), as the compiler can see
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     }
@@ -147,20 +176,34 @@ struct Tile {
                 }
                 Half first, second;
                 read(first, lds, 0);
-                for (; s < whole; ++s) {
+                // (three copies of a slice's work, so that none of them branches: a branch stops the reads from going between the products)
+                for (; s + 2 < whole; ++s) {
                     read(second, lds + ((s - from) & 1u) * kStage, 1);
                     add(first, first);
-                    mix();
-                    if (s + 1 < whole) {
-                        // this wavefront has read all of slice s, and its part of slice s + 1 has come; after the barrier
-                        // that holds for everybody: the stage of slice s may be overwritten, that of s + 1 read
-                        wait_and_meet<0>();
-                        if (s + 2 < whole) load(s + 2);
-                        read(first, lds + ((s + 1 - from) & 1u) * kStage, 0);
-                    }
+                    mix<0>();
+                    // this wavefront has read all of slice s, and its part of slice s + 1 has come; after the barrier
+                    // that holds for everybody: the stage of slice s may be overwritten, that of s + 1 read
+                    wait_and_meet<0>();
+                    load(s + 2);
+                    read(first, lds + ((s + 1 - from) & 1u) * kStage, 0);
                     add(second, second);
-                    mix();
+                    mix<kLoads>();
                 }
+                if (s + 1 < whole) {
+                    read(second, lds + ((s - from) & 1u) * kStage, 1);
+                    add(first, first);
+                    mix<0>();
+                    wait_and_meet<0>();
+                    ++s;
+                    read(first, lds + ((s - from) & 1u) * kStage, 0);
+                    add(second, second);
+                    mix<0>();
+                }
+                read(second, lds + ((s - from) & 1u) * kStage, 1);
+                add(first, first);
+                mix<0>();
+                add(second, second);
+                ++s;
             } else {
 #pragma unroll
                 for (int q = 1; q < kStages - 1; ++q)
@@ -178,20 +221,16 @@ struct Tile {
         for (; s < to; ++s) {
             unsigned char *stage = lds + (s - from) % kStages * kStage;
             i32x4 piece[kLoads];
+            u32 at[kLoads];
 #pragma unroll
             for (int q = 0; q < kLoads; ++q) {
                 const TileRows &t = q < kLoadsM ? a : b;
                 const u32 r = row_of(q), row = r < t.rows ? r : t.rows - 1u;
-                const u32 at = s * kSlice + (((lane_id() & 7u) ^ turn(r)) << 4);
-                const unsigned char *p = t.first + (u64)row * t.stride + at;
-                if (at + 16u <= t.bytes) {
-                    __builtin_memcpy(&piece[q], p, 16);
-                } else {
-                    u32 word[4] = {0u, 0u, 0u, 0u};
-                    for (u32 c = 0; at + c < t.bytes; ++c) word[c >> 2] |= (u32)p[c] << (8u * (c & 3u));
-                    piece[q] = i32x4{(int)word[0], (int)word[1], (int)word[2], (int)word[3]};
-                }
+                at[q] = s * kSlice + (((lane_id() & 7u) ^ turn(r)) << 4);
+                piece[q] = load_piece(t.first + (u64)row * t.stride, at[q], t.bytes);
             }
+#pragma unroll
+            for (int q = 0; q < kLoads; ++q) piece[q] = cut_piece(piece[q], at[q], a.bytes);
             // (everybody has read the slice that lay in this stage, two or more slices ago, before the barrier of the last one)
 #pragma unroll
             for (int q = 0; q < kLoads; ++q) *(i32x4 *)(stage + stage_at(q) + lane_id() * 16u) = piece[q];
@@ -241,13 +280,19 @@ struct Tile {
             }
     }
 
-    // the reads of one half between the products of the other
+    // the reads of one half, and loads to LDS, between the products of the other
+    template <int kOfLoads>
     __device__ __forceinline__ void mix() const
     {
+        constexpr int kReads = kFragsM + kFragsN, kProducts = kFragsM * kFragsN / (kReads + kOfLoads);
 #pragma unroll
-        for (int q = 0; q < kFragsM + kFragsN; ++q) {
+        for (int q = 0; q < kReads; ++q) {
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // a read from LDS
-            __builtin_amdgcn_sched_group_barrier(0x8, kFragsM * kFragsN / (kFragsM + kFragsN), 0);      // products
+            __builtin_amdgcn_sched_group_barrier(0x8, kProducts, 0);
+            if (q < kOfLoads) {
+                __builtin_amdgcn_sched_group_barrier(0x10, 1, 0);   // a load
+                __builtin_amdgcn_sched_group_barrier(0x8, kProducts, 0);
+            }
         }
     }
 
@@ -343,9 +388,9 @@ __device__ __forceinline__ void write_four(void *p, u64 at, int type, const f32x
 struct TileCost {
     double slice64[3], slice128[2], slice192, slice256;      // one slice of one tile alone, of two (three) sharing a unit
 };
-constexpr TileCost kCostBytes{{0.29, 0.32, 0.54}, {0.62, 0.84}, 0.90, 1.60};
-constexpr TileCost kCostHalves{{0.29, 0.33, 0.54}, {0.61, 0.86}, 0.92, 1.46};
-constexpr TileCost kCostPairs{{0.30, 0.38, 0.57}, {0.70, 1.10}, 1.15, 1.97};
+constexpr TileCost kCostBytes{{0.29, 0.35, 0.66}, {0.62, 0.84}, 0.90, 1.50};
+constexpr TileCost kCostHalves{{0.29, 0.35, 0.66}, {0.61, 0.86}, 0.90, 1.46};
+constexpr TileCost kCostPairs{{0.30, 0.40, 0.72}, {0.70, 1.10}, 1.15, 1.97};
 constexpr u32 kUnits = 256;
 
 inline double tiles_cost(const TileCost &c, u32 edge, u64 tiles, double slices)

@@ -29,6 +29,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 
 #include "../../include/rtopk.h"
 #include "rtopk_matrix.h"
@@ -111,7 +112,7 @@ template <Operands kOf> struct Stored {
 };
 
 // ---- the norm ---------------------------------------------------------------
-constexpr u32 kNormThreads = 256, kNormBlocks = 512;     // workgroups (and parts of the sum) for one matrix, at most
+constexpr u32 kNormThreads = 256, kNormBlocks = 256;     // workgroups (and parts of the sum) for one matrix, at most
 
 // the sum of the workgroup's values, in every thread
 __device__ __forceinline__ double block_sum(double v)
@@ -204,9 +205,8 @@ __global__ void __launch_bounds__(kNormThreads) k_start(Start g)
     typedef Stored<kOf> S;
     __shared__ float tile[kSide][kSide + 1];
     const u32 r0 = blockIdx.y * kSide, c0 = blockIdx.x * kSide, member = blockIdx.z;
-    double sum = 0.0;
-    for (u32 i = threadIdx.x; i < g.parts; i += kNormThreads) sum += g.part[member * kNormBlocks + i];
-    const double norm = sqrt(block_sum(sum));
+    static_assert(kNormBlocks == kNormThreads, "a part of the norm for each thread");
+    const double norm = sqrt(block_sum(threadIdx.x < g.parts ? g.part[member * kNormBlocks + threadIdx.x] : 0.0));
     int exponent = 0;
     if (norm > 0.0 && norm < __builtin_huge_val()) (void)frexp(norm, &exponent);
     if (threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) {
@@ -216,20 +216,37 @@ __global__ void __launch_bounds__(kNormThreads) k_start(Start g)
                                                       : __uint_as_float(0x7FC00000u);
     }
     const int e = kLogX - exponent;
-    for (u32 i = threadIdx.x; i < kSide * kSide; i += 256) {
-        const u32 r = r0 + i / kSide, c = c0 + i % kSide;
-        const float v = r < g.rows && c < g.cols ? read_as(g.x.p[member], (u64)r * g.ld + c, g.type) : 0.0f;
-        tile[i / kSide][i % kSide] = ldexpf(v, e);
-    }
-    __syncthreads();
+    const u64 row_bytes = g.ld * (g.type == 0 ? 4u : 2u);
+    const unsigned char *x = (const unsigned char *)g.x.p[member];
+    const bool wide = (((uintptr_t)x | row_bytes) & 15u) == 0;
     const u32 row_a = S::row_bytes(g.cols), row_t = S::row_bytes(g.rows);
     unsigned char *as_is = g.as_is + member * g.as_is_stride, *turned = g.turned + member * g.turned_stride;
-    for (u32 i = threadIdx.x; i < kSide * kSide / 4; i += 256) {
-        const u32 r = i / (kSide / 4), c = i % (kSide / 4) * 4;
-        if (r0 + r < g.rows && c0 + c < S::padded(g.cols))
-            S::put(as_is + (u64)(r0 + r) * row_a, c0 + c, f32x4{tile[r][c], tile[r][c + 1], tile[r][c + 2], tile[r][c + 3]});
-        if (c0 + r < g.cols && r0 + c < S::padded(g.rows))
-            S::put(turned + (u64)(c0 + r) * row_t, r0 + c, f32x4{tile[c][r], tile[c + 1][r], tile[c + 2][r], tile[c + 3][r]});
+    // a piece of eight neighbours, the two pieces of a thread 32 rows apart
+    const u32 r = threadIdx.x >> 3, c = (threadIdx.x & 7u) * 8u;
+    float v[2][8];
+#pragma unroll
+    for (u32 h = 0; h < 2; ++h) {
+        const u32 row = r0 + r + 32 * h;
+        read_eight(v[h], x + (row < g.rows ? row : 0u) * row_bytes, c0 + c, row < g.rows ? g.cols : 0u, g.type, wide);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[h][i] = ldexpf(v[h][i], e);
+            tile[r + 32 * h][c + i] = v[h][i];
+        }
+        if (row < g.rows) {
+            if (c0 + c < S::padded(g.cols)) S::put(as_is + (u64)row * row_a, c0 + c, f32x4{v[h][0], v[h][1], v[h][2], v[h][3]});
+            if (c0 + c + 4 < S::padded(g.cols)) S::put(as_is + (u64)row * row_a, c0 + c + 4, f32x4{v[h][4], v[h][5], v[h][6], v[h][7]});
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (u32 h = 0; h < 2; ++h) {
+        const u32 col = c0 + r + 32 * h, row = r0 + c;
+#pragma unroll
+        for (u32 q = 0; q < 8; q += 4)
+            if (col < g.cols && row + q < S::padded(g.rows))
+                S::put(turned + (u64)col * row_t, row + q,
+                       f32x4{tile[c + q][r + 32 * h], tile[c + q + 1][r + 32 * h], tile[c + q + 2][r + 32 * h], tile[c + q + 3][r + 32 * h]});
     }
 }
 
@@ -426,6 +443,7 @@ int launch(const Product &g, u32 members, hipStream_t stream)
             least = cost;
         }
     }
+    if (const char *f = getenv(kStep == kGram ? "RTG" : kStep == kPoly ? "RTP" : "RTN")) best = atoi(f);
     if (best == 256) return launch<kOf, Tile<kOf, 256, 256, 2, 4, 2, kAhead>, kStep>(g, members, stream);
     if (best == 192) return launch<kOf, Tile<kOf, 192, 192, 2, 4, 2, kAhead>, kStep>(g, members, stream);
     if (best == 128) return launch<kOf, Tile<kOf, 128, 128, 2, 2, 2, false>, kStep>(g, members, stream);

@@ -283,5 +283,5 @@ def test_refusals_of_the_binding():
     with pytest.raises(TypeError):
         rt.linear_i8_backward(z(4, 8), z(4, 6), None, None, None, z(8, 6, t=torch.bfloat16))
     with pytest.raises(rt.RtopkError) as e:
-        rt.linear_i8(z(4, 8), z(4, 8, t=i8), z(4), z(4, 4), workspace=z(16, t=torch.uint8))
+        rt.linear_i8(z(100, 8), z(4, 8, t=i8), z(4), z(100, 4), workspace=z(16, t=torch.uint8))
     assert e.value.code == -2

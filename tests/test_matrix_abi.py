@@ -25,7 +25,8 @@ def test_workspace_sizes_and_their_domains():
     assert rt.quantize_i8_workspace_bytes(0, 20, "columns") == 0
     assert rt.matmul_i8_workspace_bytes(0, 5, 5) == 0 and rt.matmul_i8_workspace_bytes(5, 5, 0) == 0
     assert rt.linear_i8_workspace_bytes(0, 5, 5) == 0
-    assert rt.linear_i8_workspace_bytes(3, 130, 5) >= 3 * 256 + 3 * 4
+    assert rt.linear_i8_workspace_bytes(100, 130, 5) >= 100 * 256 + 100 * 4
+    assert rt.linear_i8_workspace_bytes(1, 1500, 10_000) == 0       # one launch, nothing kept
     assert rt.linear_i8_backward_workspace_bytes(0, 5, 5) == 0
     one = rt.orthogonalize_workspace_bytes(1, 100, 300, "halves")
     assert one >= 4 * 100 * 300 * 2 + 2 * 100 * 100 * 2
