@@ -29,7 +29,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdlib>
 
 #include "../../include/rtopk.h"
 #include "rtopk_matrix.h"
@@ -251,7 +250,9 @@ __global__ void __launch_bounds__(kNormThreads) k_start(Start g)
 }
 
 // ---- the products -------------------------------------------------------------
-enum Step { kGram, kPoly, kNext, kLast };
+// kSymmetric: a product of two matrices that commute and are symmetric, or X X^T; kPart: a run of X X^T's contraction, its
+// sums in binary32 for k_join; kNext: the new X and its turned form; kLast: the result, with G's orientation.
+enum Step { kSymmetric, kPart, kNext, kLast };
 
 struct Product {
     const unsigned char *left, *right;      // rows of the result, columns of the result
@@ -260,8 +261,13 @@ struct Product {
     u32 tiles_m, tiles_n, tiles;            // tiles: of one matrix
     unsigned char *out, *turned;            // the result, and turned over
     u64 out_stride, turned_stride;
-    float c_sum, c_old, c_one;              // of the product, of D (kPoly) and of the identity (kPoly, and -1 in kGram)
+    // kSymmetric: result = c_sum rho^2 product + c_old old + c_one I; kNext, kLast: c_sum rho product
+    float c_sum, c_old, c_one;
+    const unsigned char *old;               // laid out as the result, or null
     const float *rho;                       // first step only, else null
+    // kPart
+    float *part;                            // [splits][matrices][rows][rows rounded up to 4]
+    u32 members, splits, slices_each;
     // kLast
     Members to;
     int type;
@@ -270,71 +276,151 @@ struct Product {
     int update;
 };
 
+// tile `at` of the triangle on and above the diagonal of n x n tiles: row i of them has n - i
+__device__ __forceinline__ void triangle_at(u32 at, u32 n, u32 &i, u32 &j)
+{
+    i = 0;
+    while (at >= n - i) at -= n - i++;
+    j = i + at;
+}
+
 template <Operands kOf, class T, Step kStep>
 __global__ void __launch_bounds__(T::kThreads) k_step(Product g)
 {
     typedef Stored<kOf> S;
     __shared__ __align__(16) unsigned char lds[T::kLds];
-    constexpr bool kSymmetric = kStep == kGram || kStep == kPoly;
-    const u32 place = xcd_place(blockIdx.x, gridDim.x), member = place / g.tiles;
-    u32 ti, tj, at = place - member * g.tiles;
-    if (kSymmetric) {                       // row ti of the triangle has tiles_n - ti tiles
-        ti = 0;
-        while (at >= g.tiles_n - ti) at -= g.tiles_n - ti++;
-        tj = ti + at;
-    } else {
-        tile_at(at, g.tiles_m, g.tiles_n, ti, tj);
-    }
+    constexpr bool kTriangle = kStep == kSymmetric || kStep == kPart;
+    const u32 place = xcd_place(blockIdx.x, gridDim.x), split = kStep == kPart ? place / (g.tiles * g.members) : 0u;
+    const u32 left_over = place - split * g.tiles * g.members, member = left_over / g.tiles, at = left_over - member * g.tiles;
+    u32 ti, tj;
+    if (kTriangle) triangle_at(at, g.tiles_n, ti, tj);
+    else tile_at(at, g.tiles_m, g.tiles_n, ti, tj);
     const u32 i0 = ti * T::kRowsM, j0 = tj * T::kRowsN;
-    const u32 bytes = S::row_bytes(g.inner);
-    const unsigned char *left = g.left + member * g.left_stride;
-    const TileRows a{left + (u64)i0 * bytes, g.rows - i0, bytes, bytes};
+    const u32 bytes = S::row_bytes(g.inner), slices = bytes / kSlice;
+    const TileRows a{g.left + member * g.left_stride + (u64)i0 * bytes, g.rows - i0, bytes, bytes};
     const TileRows b{g.right + member * g.right_stride + (u64)j0 * bytes, g.cols - j0, bytes, bytes};
+    const u32 row_out = S::row_bytes(g.cols), row_turned = S::row_bytes(g.rows);
+    const u32 row1 = i0 + T::row0() + (lane_id() & 15u), col1 = j0 + T::col0() + 4u * (lane_id() >> 4);
     T t;
     t.clear();
-    t.template multiply<true>(a, b, 0, bytes / kSlice, lds);
+    if (kStep == kSymmetric && g.old) {
+        // the old matrix's part goes into the sums first: its loads are under way together (after the products, between the
+        // stores, each is waited for: 95 us for 4096 x 4096, 72 without it)
+        const unsigned char *old = g.old + member * g.out_stride;
+        const float ratio = g.c_old / g.c_sum;
+#pragma unroll
+        for (int i = 0; i < T::kFragsM; ++i)
+#pragma unroll
+            for (int j = 0; j < T::kFragsN; ++j)
+                if (row1 + 16 * i < g.rows && col1 + 16 * j < S::padded(g.cols))
+                    t.sum[i][j] = ratio * S::get(old + (u64)(row1 + 16 * i) * row_out, col1 + 16 * j);
+    }
+    const u32 from = kStep == kPart ? split * g.slices_each : 0u;
+    t.template multiply<true>(a, b, from, kStep == kPart ? min(from + g.slices_each, slices) : slices, lds);
 
+    if constexpr (kStep == kPart) {
+        const u64 ld = align_up(g.rows, 4);
+        float *part = g.part + ((u64)split * g.members + member) * g.rows * ld;
+#pragma unroll
+        for (int i = 0; i < T::kFragsM; ++i)
+#pragma unroll
+            for (int j = 0; j < T::kFragsN; ++j)
+                if (row1 + 16 * i < g.rows && col1 + 16 * j < g.cols) *(f32x4 *)(part + (row1 + 16 * i) * ld + col1 + 16 * j) = t.sum[i][j];
+        return;
+    }
     const float rho = g.rho ? g.rho[member] : 1.0f;
-    const float c_sum = kStep == kGram ? g.c_sum * rho * rho : g.c_sum * rho;
-    const u32 row_out = S::row_bytes(g.cols), row_turned = S::row_bytes(g.rows);
+    const float c_sum = kTriangle ? g.c_sum * rho * rho : g.c_sum * rho;
+    if constexpr (kStep == kLast) {
+        void *to = g.to.p[member];
+        const u32 size = g.type == 0 ? 4u : 2u;
+        const bool wide = (((uintptr_t)to | (g.ldo * size)) & (4u * size - 1u)) == 0;
+#pragma unroll
+        for (int i = 0; i < T::kFragsM; ++i) {
+            const u32 row = row1 + 16 * i;
+            if (row >= g.rows) continue;
+            const u64 first = (u64)row * g.ldo;
+            f32x4 w[T::kFragsN];                // (a row of fragments' old weights at a time, for the same reason)
+            if (g.update) {
+#pragma unroll
+                for (int j = 0; j < T::kFragsN; ++j) {
+                    const u32 col = col1 + 16 * j;
+                    const float *from_w = (const float *)to + first + col;
+                    if (wide && col + 4u <= g.cols) w[j] = *(const f32x4 *)from_w;
+                    else
+#pragma unroll
+                        for (u32 q = 0; q < 4; ++q) w[j][q] = col + q < g.cols ? from_w[q] : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < T::kFragsN; ++j) {
+                const u32 col = col1 + 16 * j;
+                if (col >= g.cols) continue;
+                f32x4 v = t.sum[i][j] * c_sum;
+                if (g.update)
+#pragma unroll
+                    for (u32 q = 0; q < 4; ++q) v[q] = fmaf(g.gain, v[q], g.keep * w[j][q]);
+                write_four(to, first + col, g.type, v, g.cols - col, wide);
+            }
+        }
+        return;
+    }
     unsigned char *out = g.out + member * g.out_stride, *turned = g.turned + member * g.turned_stride;
     t.each([&](u32 r, u32 c, const f32x4 &sum) {
         const u32 row = i0 + r, col = j0 + c;
-        const bool there = row < g.rows && col < S::padded(g.cols);
         f32x4 v = sum * c_sum;
-        if (kStep == kPoly && there) v += g.c_old * S::get(left + (u64)row * bytes, col);      // (left is D)
 #pragma unroll
         for (u32 q = 0; q < 4; ++q) {
-            if (kSymmetric && col + q == row) v[q] += g.c_one;
+            if (kTriangle && col + q == row) v[q] += g.c_one;
             if (row >= g.rows || col + q >= g.cols) v[q] = 0.0f;        // what pads the rows is zero
         }
-        if (kStep == kLast) {
-            if (!there || col >= g.cols) return;
-            const u32 have = g.cols - col;
-            void *to = g.to.p[member];
-            const u64 first = (u64)row * g.ldo + col;
-            if (g.update) {
-                float *w = (float *)to + first;
-                const bool wide = (((uintptr_t)to | (g.ldo * 4u)) & 15u) == 0 && have >= 4u;
-                f32x4 x;
-#pragma unroll
-                for (u32 q = 0; q < 4; ++q) x[q] = wide || q >= have ? 0.0f : w[q];
-                if (wide) x = *(const f32x4 *)w;
-#pragma unroll
-                for (u32 q = 0; q < 4; ++q) x[q] = fmaf(g.gain, v[q], g.keep * x[q]);
-                write_four(to, first, 0, x, have, wide);
-            } else {
-                const u32 size = g.type == 0 ? 4u : 2u;
-                write_four(to, first, g.type, v, have, (((uintptr_t)to | (g.ldo * size)) & (4u * size - 1u)) == 0);
-            }
-            return;
-        }
-        if (there) S::put(out + (u64)row * row_out, col, v);
-        if (!kSymmetric || ti != tj) {
+        if (row < g.rows && col < S::padded(g.cols)) S::put(out + (u64)row * row_out, col, v);
+        if (!kTriangle || ti != tj) {
             const u32 column = col + (lane_id() & 3u);
             S::put_turned(turned + (u64)column * row_turned, row, v, column < g.cols && (row & ~3u) < S::padded(g.rows));
         }
     });
+}
+
+// The runs of X X^T together, in their order, scaled, less the identity: D, both sides of the diagonal, by blocks of 64 x 64.
+template <Operands kOf>
+__global__ void __launch_bounds__(256) k_join(Product g)
+{
+    typedef Stored<kOf> S;
+    __shared__ float tile[kSide][kSide + 1];
+    const u32 member = blockIdx.y, n = (g.rows + kSide - 1) / kSide;
+    u32 ti, tj;
+    triangle_at(blockIdx.x, n, ti, tj);
+    const u32 r = threadIdx.x >> 4, c = (threadIdx.x & 15u) * 4u;
+    const u64 ld = align_up(g.rows, 4), one = (u64)g.rows * ld;
+    const float rho = g.rho ? g.rho[member] : 1.0f, c_sum = g.c_sum * rho * rho;
+    const u32 row_out = S::row_bytes(g.rows);
+    unsigned char *out = g.out + member * g.out_stride;
+#pragma unroll
+    for (u32 h = 0; h < 4; ++h) {
+        const u32 row = ti * kSide + r + 16 * h, col = tj * kSide + c;
+        f32x4 v{0, 0, 0, 0};
+        if (row < g.rows && col < g.rows) {
+            const float *p = g.part + member * one + row * ld + col;
+#pragma unroll 4
+            for (u32 s = 0; s < g.splits; ++s) v += *(const f32x4 *)(p + s * g.members * one);
+        }
+        v *= c_sum;
+#pragma unroll
+        for (u32 q = 0; q < 4; ++q) {
+            if (col + q == row) v[q] += g.c_one;
+            if (row >= g.rows || col + q >= g.rows) v[q] = 0.0f;
+            tile[r + 16 * h][c + q] = v[q];
+        }
+        if (row < g.rows && col < S::padded(g.rows)) S::put(out + (u64)row * row_out, col, v);
+    }
+    if (ti == tj) return;
+    __syncthreads();
+#pragma unroll
+    for (u32 h = 0; h < 4; ++h) {
+        const u32 row = tj * kSide + r + 16 * h, col = ti * kSide + c;
+        if (row < g.rows)
+            S::put(out + (u64)row * row_out, col, f32x4{tile[c][r + 16 * h], tile[c + 1][r + 16 * h], tile[c + 2][r + 16 * h], tile[c + 3][r + 16 * h]});
+    }
 }
 
 }  // namespace rtopk
@@ -352,43 +438,92 @@ struct Shape {
     bool over() const { return rows > cols; }       // X is G turned over
 };
 
-struct Parts {
-    double *norm;
-    float *rho, *average;
-    unsigned char *x[2], *xt[2], *d, *p;
-    u64 x_stride, xt_stride, d_stride;
+// How X X^T is made: tiles of `edge`, the contraction in so many runs.
+struct GramPlan {
+    u32 edge, splits, slices_each;
 };
 
 template <Operands kOf>
-u64 cut(void *base, u32 members, const Shape &s, bool average, Parts &p)
+u32 best_edge(bool triangle, u32 rows, u32 cols, u32 members, double slices, double *cost)
+{
+    u32 best = 0;
+    for (const u32 edge : {64u, 128u, 192u, 256u}) {
+        const u64 i = (rows + edge - 1) / edge, j = (cols + edge - 1) / edge;
+        const double c = tiles_cost(kOf == kPairs ? kCostPairs : kCostHalves, edge, (triangle ? j * (j + 1) / 2 : i * j) * members, slices);
+        if (best && c >= *cost) continue;
+        best = edge;
+        *cost = c;
+    }
+    return best;
+}
+
+// Runs cost a launch, and their sums, four bytes each, written and read.
+template <Operands kOf>
+GramPlan plan_gram(u32 members, const Shape &s, double *cost)
+{
+    const u32 m = s.m(), slices = Stored<kOf>::row_bytes(s.n()) / kSlice;
+    GramPlan best{0, 1, slices};
+    best.edge = best_edge<kOf>(true, m, m, members, slices, cost);
+    for (u32 splits = 2; splits <= std::min(16u, slices / 4); ++splits) {
+        const u32 each = (slices + splits - 1) / splits;
+        if ((slices + each - 1) / each != splits) continue;
+        double c = 0.0;
+        const u32 edge = best_edge<kOf>(true, m, m, members * splits, each, &c);
+        c += 5.0 + 4.0 * m * m * members * (splits + 1) / 4e6;
+        if (c >= *cost) continue;
+        *cost = c;
+        best = GramPlan{edge, splits, each};
+    }
+    return best;
+}
+
+struct Parts {
+    double *norm;
+    float *rho, *average, *part;
+    unsigned char *x[2], *xt[2], *square[4];
+    u64 x_stride, xt_stride, square_stride;
+};
+
+template <Operands kOf>
+u64 cut(void *base, u32 count, const Shape &s, bool average, Parts &p)
 {
     typedef Stored<kOf> S;
+    const u32 members = std::min(count, kMembers);
     unsigned char *at = (unsigned char *)base;
     u64 used = 0;
     auto take = [&](u64 bytes) { unsigned char *q = at + used; used += align_up(bytes, 256); return q; };
     p.x_stride = align_up((u64)s.m() * S::row_bytes(s.n()), 256);
     p.xt_stride = align_up((u64)s.n() * S::row_bytes(s.m()), 256);
-    p.d_stride = align_up((u64)s.m() * S::row_bytes(s.m()), 256);
+    p.square_stride = align_up((u64)s.m() * S::row_bytes(s.m()), 256);
     p.norm = (double *)take(kMembers * kNormBlocks * sizeof(double));
     p.rho = (float *)take(kMembers * sizeof(float));
     for (int i = 0; i < 2; ++i) {
         p.x[i] = take(members * p.x_stride);
         p.xt[i] = take(members * p.xt_stride);
     }
-    p.d = take(members * p.d_stride);
-    p.p = take(members * p.d_stride);
+    for (int i = 0; i < 4; ++i) p.square[i] = take(members * p.square_stride);
+    auto sums = [&](u32 matrices) {
+        double cost;
+        const u32 splits = matrices ? plan_gram<kOf>(matrices, s, &cost).splits : 1;
+        return splits > 1 ? (u64)splits * matrices * s.m() * align_up(s.m(), 4) : 0;
+    };
+    // (the last launches may have fewer matrices, and more runs)
+    const u64 part = std::max(sums(members), sums(count > kMembers ? count % kMembers : 0));
+    p.part = (float *)take(part * sizeof(float));
     p.average = average ? (float *)take(members * align_up((u64)s.rows * s.cols, 64) * sizeof(float)) : nullptr;
     return used;
 }
 
-u64 cut(int products, void *base, u32 members, const Shape &s, bool average, Parts &p)
+u64 cut(int products, void *base, u32 count, const Shape &s, bool average, Parts &p)
 {
-    return products == RTOPK_PRODUCTS_PAIRS ? cut<kPairs>(base, members, s, average, p) : cut<kHalves>(base, members, s, average, p);
+    return products == RTOPK_PRODUCTS_PAIRS ? cut<kPairs>(base, count, s, average, p) : cut<kHalves>(base, count, s, average, p);
 }
 
-// Whether iterates that start with singular values in [0, 1] stay where their stored forms are finite.
-bool coefficients_ok(const float *abc, u32 steps)
+// Whether iterates that start with singular values in [0, 1] stay where their stored forms are finite. largest: of
+// |a + b s^2 + c s^4| in any step.
+bool coefficients_ok(const float *abc, u32 steps, double *largest)
 {
+    *largest = 0.0;
     double hi = 1.0;
     for (u32 s = 0; s < steps; ++s) {
         const double a = abc[3 * s], b = abc[3 * s + 1], c = abc[3 * s + 2];
@@ -412,6 +547,7 @@ bool coefficients_ok(const float *abc, u32 steps)
             look(-a / (3.0 * b));
         }
         if (!(x <= kMostX) || !(p <= kMostP)) return false;
+        *largest = std::max(*largest, p);
         hi = x;
     }
     return true;
@@ -420,33 +556,22 @@ bool coefficients_ok(const float *abc, u32 steps)
 template <Operands kOf, class T, Step kStep>
 int launch(Product g, u32 members, hipStream_t stream)
 {
+    constexpr bool kTriangle = kStep == kSymmetric || kStep == kPart;
     g.tiles_m = (g.rows + T::kRowsM - 1) / T::kRowsM;
     g.tiles_n = (g.cols + T::kRowsN - 1) / T::kRowsN;
-    g.tiles = kStep == kGram || kStep == kPoly ? g.tiles_n * (g.tiles_n + 1) / 2 : g.tiles_m * g.tiles_n;
-    k_step<kOf, T, kStep><<<g.tiles * members, T::kThreads, 0, stream>>>(g);
+    g.tiles = kTriangle ? g.tiles_n * (g.tiles_n + 1) / 2 : g.tiles_m * g.tiles_n;
+    g.members = members;
+    k_step<kOf, T, kStep><<<g.tiles * members * (kStep == kPart ? g.splits : 1u), T::kThreads, 0, stream>>>(g);
     return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_EHIP;
 }
 
 template <Operands kOf, Step kStep>
-int launch(const Product &g, u32 members, hipStream_t stream)
+int launch(const Product &g, u32 members, u32 edge, hipStream_t stream)
 {
     constexpr bool kAhead = kOf != kPairs;
-    const double slices = Stored<kOf>::row_bytes(g.inner) / kSlice;
-    u32 best = 0;
-    double least = 0.0;
-    for (const u32 edge : {64u, 128u, 192u, 256u}) {
-        const u64 i = (g.rows + edge - 1) / edge, j = (g.cols + edge - 1) / edge;
-        const u64 tiles = (kStep == kGram || kStep == kPoly ? j * (j + 1) / 2 : i * j) * members;
-        const double cost = tiles_cost(kOf == kPairs ? kCostPairs : kCostHalves, edge, tiles, slices);
-        if (!best || cost < least) {
-            best = edge;
-            least = cost;
-        }
-    }
-    if (const char *f = getenv(kStep == kGram ? "RTG" : kStep == kPoly ? "RTP" : "RTN")) best = atoi(f);
-    if (best == 256) return launch<kOf, Tile<kOf, 256, 256, 2, 4, 2, kAhead>, kStep>(g, members, stream);
-    if (best == 192) return launch<kOf, Tile<kOf, 192, 192, 2, 4, 2, kAhead>, kStep>(g, members, stream);
-    if (best == 128) return launch<kOf, Tile<kOf, 128, 128, 2, 2, 2, false>, kStep>(g, members, stream);
+    if (edge == 256) return launch<kOf, Tile<kOf, 256, 256, 2, 4, 2, kAhead>, kStep>(g, members, stream);
+    if (edge == 192) return launch<kOf, Tile<kOf, 192, 192, 2, 4, 2, kAhead>, kStep>(g, members, stream);
+    if (edge == 128) return launch<kOf, Tile<kOf, 128, 128, 2, 2, 2, false>, kStep>(g, members, stream);
     return launch<kOf, Tile<kOf, 64, 64, 2, 2, 3, false>, kStep>(g, members, stream);
 }
 
@@ -460,8 +585,8 @@ struct Target {
 
 // From G and the parts of its norm to the end.
 template <Operands kOf>
-int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 norm_parts, u32 steps, const float *abc, float eps,
-            const Parts &p, const Target &target, hipStream_t stream)
+int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 norm_parts, u32 steps, const float *abc,
+            double largest_p, float eps, const Parts &p, const Target &target, hipStream_t stream)
 {
     typedef Stored<kOf> S;
     const u32 m = s.m(), n = s.n();
@@ -470,51 +595,105 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
     const dim3 grid((S::padded(s.cols) + kSide - 1) / kSide, (S::padded(s.rows) + kSide - 1) / kSide, members);
     k_start<kOf><<<grid, kNormThreads, 0, stream>>>(start);
     if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
-    for (u32 i = 0; i < steps; ++i) {
-        const unsigned char *xi = p.x[i & 1], *xti = p.xt[i & 1];
-        const double a = abc[3 * i], b = abc[3 * i + 1], c = abc[3 * i + 2];
-        const float *rho = i == 0 ? p.rho : nullptr;
+    double gram_cost, square_cost, next_cost;
+    const GramPlan gram = plan_gram<kOf>(members, s, &gram_cost);
+    const double square_slices = S::row_bytes(m) / kSlice;
+    const u32 square_edge = best_edge<kOf>(true, m, m, members, square_slices, &square_cost);
+    const u32 next_edge = best_edge<kOf>(false, m, n, members, square_slices, &next_cost);
+
+    // X X^T - I (the first step's X still lacks rho)
+    auto make_gram = [&](const unsigned char *x_now, unsigned char *to, const float *rho) -> int {
         Product g{};
-        g.left = g.right = xi;
+        g.left = g.right = x_now;
         g.left_stride = g.right_stride = p.x_stride;
         g.rows = g.cols = m;
         g.inner = n;
-        g.out = g.turned = p.d;
-        g.out_stride = g.turned_stride = p.d_stride;
+        g.out = g.turned = to;
+        g.out_stride = g.turned_stride = p.square_stride;
         g.c_sum = ldexpf(1.0f, kLogD - 2 * kLogX);
         g.c_one = -ldexpf(1.0f, kLogD);
         g.rho = rho;
-        if (const int rc = launch<kOf, kGram>(g, members, stream)) return rc;
-        g.left = g.right = p.d;
-        g.left_stride = g.right_stride = p.d_stride;
-        g.inner = m;
-        g.out = g.turned = p.p;
+        if (gram.splits == 1) return launch<kOf, kSymmetric>(g, members, gram.edge, stream);
+        g.part = p.part;
+        g.splits = gram.splits;
+        g.slices_each = gram.slices_each;
+        if (const int rc = launch<kOf, kPart>(g, members, gram.edge, stream)) return rc;
+        g.members = members;
+        const u32 side = (m + kSide - 1) / kSide;
+        k_join<kOf><<<dim3(side * (side + 1) / 2, members), 256, 0, stream>>>(g);
+        return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_EHIP;
+    };
+    // to = c left right + d old + e I, of matrices that commute and are symmetric
+    auto make_square = [&](const unsigned char *left, const unsigned char *right, const unsigned char *old, unsigned char *to, double c,
+                           double d, double e) -> int {
+        Product g{};
+        g.left = left;
+        g.right = right;
+        g.left_stride = g.right_stride = p.square_stride;
+        g.rows = g.cols = g.inner = m;
+        g.out = g.turned = to;
+        g.out_stride = g.turned_stride = p.square_stride;
+        // (d old is divided by c to go into the sums: a c of zero is made so small that it adds nothing)
+        if (std::fabs(c) < ldexp(std::fabs(d), -40)) c = ldexp(std::fabs(d), -40);
         g.c_sum = (float)(c * ldexp(1.0, -kLogD));
-        g.c_old = (float)(b + 2.0 * c);
-        g.c_one = (float)((a + b + c) * ldexp(1.0, kLogD));
-        g.rho = nullptr;
-        if (const int rc = launch<kOf, kPoly>(g, members, stream)) return rc;
+        g.c_old = (float)d;
+        g.c_one = (float)(e * ldexp(1.0, kLogD));
+        g.old = d != 0.0 ? old : nullptr;
+        return launch<kOf, kSymmetric>(g, members, square_edge, stream);
+    };
+    unsigned char *const *q = p.square;
+    auto make_poly = [&](const unsigned char *d, unsigned char *to, const float *k) -> int {
+        const double a = k[0], b = k[1], c = k[2];
+        return make_square(d, d, d, to, c, b + 2.0 * c, a + b + c);
+    };
+    // Two steps at a time: from D and P of the first, X X^T of the second is P (D + I) P without X, and both polynomials
+    // go to X as one. Three more products of m x m, X X^T and P X once less: where X is long. With pairs only (the second D
+    // carries the first one's roundings, twelve times larger, to where the singular values are small), and not with
+    // coefficients that make P large.
+    const bool twos = kOf == kPairs && largest_p <= 4.0 && gram_cost + next_cost > 1.05 * 3.0 * square_cost;
+    u32 now = 0;
+    for (u32 i = 0; i < steps;) {
+        const unsigned char *x_now = p.x[now], *xt_now = p.xt[now];
+        const float *rho = i == 0 ? p.rho : nullptr;
+        if (const int rc = make_gram(x_now, q[0], rho)) return rc;
+        if (const int rc = make_poly(q[0], q[1], abc + 3 * i)) return rc;
+        unsigned char *poly = q[1];
+        u32 did = 1;
+        if (twos && i + 1 < steps) {
+            if (const int rc = make_square(q[1], q[1], nullptr, q[2], 1.0, 0.0, 0.0)) return rc;            // E = P P
+            if (const int rc = make_square(q[0], q[2], q[2], q[3], 1.0, 1.0, -1.0)) return rc;              // D E + E - I
+            if (const int rc = make_poly(q[3], q[0], abc + 3 * (i + 1))) return rc;
+            if (const int rc = make_square(q[0], q[1], nullptr, q[2], 1.0, 0.0, 0.0)) return rc;            // both polynomials
+            poly = q[2];
+            did = 2;
+        }
+        i += did;
+        Product g{};
         g.rho = rho;
-        if (i + 1 < steps) {
-            g.left = p.p;
-            g.right = xti;
+        if (i < steps) {
+            g.left = poly;
+            g.left_stride = p.square_stride;
+            g.right = xt_now;
             g.right_stride = p.xt_stride;
+            g.rows = g.inner = m;
             g.cols = n;
-            g.out = p.x[1 - (i & 1)];
-            g.turned = p.xt[1 - (i & 1)];
+            now = 1 - now;
+            g.out = p.x[now];
+            g.turned = p.xt[now];
             g.out_stride = p.x_stride;
             g.turned_stride = p.xt_stride;
             g.c_sum = ldexpf(1.0f, -kLogD);
-            if (const int rc = launch<kOf, kNext>(g, members, stream)) return rc;
+            if (const int rc = launch<kOf, kNext>(g, members, next_edge, stream)) return rc;
             continue;
         }
         // the last product writes with G's orientation
-        g.left = s.over() ? xti : p.p;
-        g.right = s.over() ? p.p : xti;
-        g.left_stride = s.over() ? p.xt_stride : p.d_stride;
-        g.right_stride = s.over() ? p.d_stride : p.xt_stride;
+        g.left = s.over() ? xt_now : poly;
+        g.right = s.over() ? poly : xt_now;
+        g.left_stride = s.over() ? p.xt_stride : p.square_stride;
+        g.right_stride = s.over() ? p.square_stride : p.xt_stride;
         g.rows = s.rows;
         g.cols = s.cols;
+        g.inner = m;
         g.c_sum = ldexpf(1.0f, -kLogD - kLogX);
         g.to = target.to;
         g.type = target.type;
@@ -522,17 +701,17 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
         g.gain = target.gain;
         g.keep = target.keep;
         g.update = target.update;
-        if (const int rc = launch<kOf, kLast>(g, members, stream)) return rc;
+        if (const int rc = launch<kOf, kLast>(g, members, next_edge, stream)) return rc;
     }
     return RTOPK_OK;
 }
 
 int iterate(int products, const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 norm_parts, u32 steps,
-            const float *abc, float eps, const Parts &p, const Target &target, hipStream_t stream)
+            const float *abc, double largest_p, float eps, const Parts &p, const Target &target, hipStream_t stream)
 {
     return products == RTOPK_PRODUCTS_PAIRS
-               ? iterate<kPairs>(x, type, ldx, s, members, norm_parts, steps, abc, eps, p, target, stream)
-               : iterate<kHalves>(x, type, ldx, s, members, norm_parts, steps, abc, eps, p, target, stream);
+               ? iterate<kPairs>(x, type, ldx, s, members, norm_parts, steps, abc, largest_p, eps, p, target, stream)
+               : iterate<kHalves>(x, type, ldx, s, members, norm_parts, steps, abc, largest_p, eps, p, target, stream);
 }
 
 // workgroups for the norm of one of so many matrices: a few elements for every thread, and not many more than fill the chip
@@ -548,9 +727,9 @@ bool sizes_ok(uint32_t count, uint64_t rows, uint64_t cols, int products)
     return count >= 1 && rows >= 1 && cols >= 1 && rows <= kMostSide && cols <= kMostSide && rows * cols <= 0xFFFFFFFFull &&
            (products == RTOPK_PRODUCTS_PAIRS || products == RTOPK_PRODUCTS_HALVES);
 }
-bool iteration_ok(uint32_t steps, const float *abc, float eps)
+bool iteration_ok(uint32_t steps, const float *abc, float eps, double *largest_p)
 {
-    return steps >= 1 && steps <= kMostSteps && abc && eps >= 0.0f && std::isfinite(eps) && coefficients_ok(abc, steps);
+    return steps >= 1 && steps <= kMostSteps && abc && eps >= 0.0f && std::isfinite(eps) && coefficients_ok(abc, steps, largest_p);
 }
 
 }  // namespace
@@ -559,7 +738,7 @@ extern "C" int rtopk_orthogonalize_workspace_bytes(uint32_t count, uint64_t rows
 {
     if (!bytes || !sizes_ok(count, rows, cols, products)) return RTOPK_EINVAL;
     Parts p;
-    *bytes = cut(products, nullptr, std::min(count, kMembers), Shape{(u32)rows, (u32)cols}, false, p);
+    *bytes = cut(products, nullptr, count, Shape{(u32)rows, (u32)cols}, false, p);
     return RTOPK_OK;
 }
 
@@ -568,17 +747,18 @@ extern "C" int rtopk_orthogonalize(uint32_t count, const void *const *x, int typ
                                    uint64_t ldo, void *workspace, uint64_t workspace_bytes, void *stream_v)
 {
     uint64_t need = 0;
+    double largest_p = 0.0;
     if (!x || !out || !type_ok(type) || !type_ok(out_type) ||
         rtopk_orthogonalize_workspace_bytes(count, rows, cols, products, &need) != RTOPK_OK)
         return RTOPK_EINVAL;
-    if (ldx < cols || ldo < cols || !iteration_ok(steps, coefficients, eps)) return RTOPK_EINVAL;
+    if (ldx < cols || ldo < cols || !iteration_ok(steps, coefficients, eps, &largest_p)) return RTOPK_EINVAL;
     for (uint32_t i = 0; i < count; ++i)
         if (!x[i] || !out[i]) return RTOPK_EINVAL;
     if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need) return RTOPK_EWORKSPACE;
     hipStream_t stream = (hipStream_t)stream_v;
     const Shape s{(u32)rows, (u32)cols};
     Parts p;
-    cut(products, workspace, std::min(count, kMembers), s, false, p);
+    cut(products, workspace, count, s, false, p);
     for (uint32_t first = 0; first < count; first += kMembers) {
         const u32 members = std::min(count - first, kMembers);
         Members from{};
@@ -590,7 +770,7 @@ extern "C" int rtopk_orthogonalize(uint32_t count, const void *const *x, int typ
         const u32 parts = norm_blocks((u64)s.rows * s.cols, members);
         k_norm<<<dim3(parts, members), kNormThreads, 0, stream>>>(from, type, s.rows, s.cols, ldx, p.norm);
         if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
-        if (const int rc = iterate(products, from, type, ldx, s, members, parts, steps, coefficients, eps, p, to, stream)) return rc;
+        if (const int rc = iterate(products, from, type, ldx, s, members, parts, steps, coefficients, largest_p, eps, p, to, stream)) return rc;
     }
     return RTOPK_OK;
 }
@@ -600,7 +780,7 @@ extern "C" int rtopk_aggregate_update_orthogonal_workspace_bytes(uint32_t count,
 {
     if (!bytes || !sizes_ok(count, rows, cols, products)) return RTOPK_EINVAL;
     Parts p;
-    *bytes = cut(products, nullptr, std::min(count, kMembers), Shape{(u32)rows, (u32)cols}, true, p);
+    *bytes = cut(products, nullptr, count, Shape{(u32)rows, (u32)cols}, true, p);
     return RTOPK_OK;
 }
 
@@ -611,10 +791,11 @@ extern "C" int rtopk_aggregate_update_orthogonal(uint32_t count, const uint32_t 
                                                  void *workspace, uint64_t workspace_bytes, void *stream_v)
 {
     uint64_t need = 0;
+    double largest_p = 0.0;
     if (!idx || !val || !omega || !velocity || n < 1 || k < 1 ||
         rtopk_aggregate_update_orthogonal_workspace_bytes(count, rows, cols, products, &need) != RTOPK_OK)
         return RTOPK_EINVAL;
-    if (!iteration_ok(steps, coefficients, eps)) return RTOPK_EINVAL;
+    if (!iteration_ok(steps, coefficients, eps, &largest_p)) return RTOPK_EINVAL;
     const u64 d = rows * cols;
     for (uint32_t i = 0; i < count; ++i) {
         if (!idx[i] || !val[i] || !omega[i] || !velocity[i]) return RTOPK_EINVAL;
@@ -625,7 +806,7 @@ extern "C" int rtopk_aggregate_update_orthogonal(uint32_t count, const uint32_t 
     hipStream_t stream = (hipStream_t)stream_v;
     const Shape s{(u32)rows, (u32)cols};
     Parts p;
-    cut(products, workspace, std::min(count, kMembers), s, true, p);
+    cut(products, workspace, count, s, true, p);
     for (uint32_t first = 0; first < count; first += kMembers) {
         const u32 members = std::min(count - first, kMembers);
         Members velocities{}, steps_of{};
@@ -640,7 +821,7 @@ extern "C" int rtopk_aggregate_update_orthogonal(uint32_t count, const uint32_t 
         const u32 parts = norm_blocks(d, members);
         k_velocity<<<dim3(parts, members), kNormThreads, 0, stream>>>(velocities, p.average, d, scale, mu, nesterov, p.norm);
         if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
-        if (const int rc = iterate(products, steps_of, RTOPK_F32, cols, s, members, parts, steps, coefficients, eps, p, to, stream)) return rc;
+        if (const int rc = iterate(products, steps_of, RTOPK_F32, cols, s, members, parts, steps, coefficients, largest_p, eps, p, to, stream)) return rc;
     }
     return RTOPK_OK;
 }

@@ -32,7 +32,7 @@ def test_workspace_sizes_and_their_domains():
     assert one >= 4 * 100 * 300 * 2 + 2 * 100 * 100 * 2
     assert rt.orthogonalize_workspace_bytes(1, 300, 100, "halves") == one
     assert rt.orthogonalize_workspace_bytes(1, 100, 300, "pairs") > one
-    assert rt.orthogonalize_workspace_bytes(16, 100, 300, "halves") == rt.orthogonalize_workspace_bytes(40, 100, 300, "halves")
+    assert rt.orthogonalize_workspace_bytes(16, 100, 300, "halves") <= rt.orthogonalize_workspace_bytes(40, 100, 300, "halves") < 17 * one
     assert rt.aggregate_update_orthogonal_workspace_bytes(1, 100, 300, "halves") >= one + 4 * 100 * 300
     for call in (lambda: rt.quantize_i8_workspace_bytes(MOST + 1, 4), lambda: rt.quantize_i8_workspace_bytes(4, 0),
                  lambda: rt.matmul_i8_workspace_bytes(4, 4, MOST + 1), lambda: rt.linear_i8_workspace_bytes(4, 0, 4),
