@@ -454,36 +454,40 @@ __global__ void __launch_bounds__(kWaves * kWave) k_few(Few f)
         const bool wide = (((uintptr_t)f.x | row_bytes) & 15u) == 0;
         const u32 pieces = (g.k + 7u) / 8u, all = g.m * pieces;
         float v[kHeld][8];
+        u32 token[kHeld], c[kHeld];
 #pragma unroll
         for (u32 h = 0; h < kHeld; ++h) {
-            const u32 at = threadIdx.x + h * kWaves * kWave, t = at / pieces;
-            read_eight(v[h], (const unsigned char *)f.x + (at < all ? t : 0u) * row_bytes, (at - t * pieces) * 8u, at < all ? g.k : 0u, f.type, wide);
+            if (h * kWaves * kWave >= all) break;               // (uniform: a short token is one round of 1500 instructions less)
+            const u32 at = threadIdx.x + h * kWaves * kWave;
+            token[h] = g.m == 1 || at >= all ? 0u : at / pieces;
+            c[h] = (at - token[h] * pieces) * 8u;
+            read_eight(v[h], (const unsigned char *)f.x + token[h] * row_bytes, c[h], at < all ? g.k : 0u, f.type, wide);
         }
         if (threadIdx.x < kTokens * 16) most[threadIdx.x] = 0u;
         __syncthreads();
 #pragma unroll
         for (u32 h = 0; h < kHeld; ++h) {
-            const u32 at = threadIdx.x + h * kWaves * kWave, t = at / pieces;
+            if (h * kWaves * kWave >= all) break;
             u32 largest = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) largest = max(largest, magnitude(v[h][i]));
             if (g.m == 1) {
                 largest = wave_max_dpp(largest);
                 if (lane == 0) atomicMax(&most[0], largest);
-            } else if (at < all) {
-                atomicMax(&most[t], largest);
+            } else {
+                atomicMax(&most[token[h]], largest);
             }
         }
         __syncthreads();
 #pragma unroll
         for (u32 h = 0; h < kHeld; ++h) {
-            const u32 at = threadIdx.x + h * kWaves * kWave, t = at / pieces, c = (at - t * pieces) * 8u;
-            const Quantizer quantize(scale_of(most[at < all ? t : 0u]));
+            if (h * kWaves * kWave >= all) break;
+            const Quantizer quantize(scale_of(most[token[h]]));
             int n[8];
             quantize(n, v[h]);
-            if (at >= all) continue;
-            if (c == 0) token_scale[t] = quantize.s;
-            *(uint2 *)(lds + t * row + c) = make_uint2(four_bytes(n), four_bytes(n + 4));
+            if (threadIdx.x + h * kWaves * kWave >= all) continue;
+            if (c[h] == 0) token_scale[token[h]] = quantize.s;
+            *(uint2 *)(lds + token[h] * row + c[h]) = make_uint2(four_bytes(n), four_bytes(n + 4));
         }
         // what fills a token's last step (the weights there are zeros, but the numbers have to be some)
         for (u32 at = threadIdx.x; at < g.m * 8u; at += kWaves * kWave) {

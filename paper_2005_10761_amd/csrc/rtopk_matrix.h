@@ -241,21 +241,23 @@ struct Tile {
     }
 
     // half h of a slice in LDS
-    __device__ __forceinline__ void read(Half &f, const unsigned char *stage, u32 h) const
+    __device__ __forceinline__ void read(Half &f, const unsigned char *stage, u32 h) const { read(f, stage, stage + kM * kSlice, h); }
+    __device__ __forceinline__ void read(Half &f, const unsigned char *stage_a, const unsigned char *stage_b, u32 h) const
     {
         const u32 ra = row0() + (lane_id() & 15u), rb = col0() + (lane_id() & 15u), piece = 4 * h + (lane_id() >> 4);
 #pragma unroll
-        for (int j = 0; j < kFragsN; ++j) f.b[j] = *(const i32x4 *)(stage + kM * kSlice + place(rb + 16 * j, piece));
+        for (int j = 0; j < kFragsN; ++j) f.b[j] = *(const i32x4 *)(stage_b + place(rb + 16 * j, piece));
 #pragma unroll
-        for (int i = 0; i < kFragsM; ++i) f.a[i] = *(const i32x4 *)(stage + place(ra + 16 * i, piece));
+        for (int i = 0; i < kFragsM; ++i) f.a[i] = *(const i32x4 *)(stage_a + place(ra + 16 * i, piece));
     }
 
     // one slice that lies in LDS, into the sums
-    __device__ __forceinline__ void one_slice(const unsigned char *stage)
+    __device__ __forceinline__ void one_slice(const unsigned char *stage) { one_slice(stage, stage + kM * kSlice); }
+    __device__ __forceinline__ void one_slice(const unsigned char *stage_a, const unsigned char *stage_b)
     {
         Half first, second;
-        read(first, stage, 0);
-        read(second, stage, 1);
+        read(first, stage_a, stage_b, 0);
+        read(second, stage_a, stage_b, 1);
         if (kOf == kPairs) {
             add(first, first);
             add(second, first);

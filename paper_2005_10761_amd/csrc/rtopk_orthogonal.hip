@@ -198,23 +198,29 @@ struct Start {
 
 constexpr u32 kSide = 64;
 
+// From the parts of a matrix's norm: the exponent that its elements are moved by, and (to *rho, where there is one) what is
+// left of the division. By all threads of a workgroup of kNormThreads.
+__device__ __forceinline__ int exponent_of(const double *part, u32 parts, float eps, float *rho)
+{
+    static_assert(kNormBlocks == kNormThreads, "a part of the norm for each thread");
+    const double norm = sqrt(block_sum(threadIdx.x < parts ? part[threadIdx.x] : 0.0));
+    int exponent = 0;
+    if (norm > 0.0 && norm < __builtin_huge_val()) (void)frexp(norm, &exponent);
+    if (threadIdx.x == 0 && rho) {
+        // zeros stay zeros; an infinity or a not-a-number makes all of it NaN
+        *rho = norm == 0.0 ? 0.0f
+               : norm < __builtin_huge_val() ? (float)(ldexp(1.0, exponent) / (norm + (double)eps)) : __uint_as_float(0x7FC00000u);
+    }
+    return kLogX - exponent;
+}
+
 template <Operands kOf>
 __global__ void __launch_bounds__(kNormThreads) k_start(Start g)
 {
     typedef Stored<kOf> S;
     __shared__ float tile[kSide][kSide + 1];
     const u32 r0 = blockIdx.y * kSide, c0 = blockIdx.x * kSide, member = blockIdx.z;
-    static_assert(kNormBlocks == kNormThreads, "a part of the norm for each thread");
-    const double norm = sqrt(block_sum(threadIdx.x < g.parts ? g.part[member * kNormBlocks + threadIdx.x] : 0.0));
-    int exponent = 0;
-    if (norm > 0.0 && norm < __builtin_huge_val()) (void)frexp(norm, &exponent);
-    if (threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) {
-        // zeros stay zeros; an infinity or a not-a-number makes all of it NaN
-        g.rho[member] = norm == 0.0 ? 0.0f
-                        : norm < __builtin_huge_val() ? (float)(ldexp(1.0, exponent) / (norm + (double)g.eps))
-                                                      : __uint_as_float(0x7FC00000u);
-    }
-    const int e = kLogX - exponent;
+    const int e = exponent_of(g.part + member * kNormBlocks, g.parts, g.eps, blockIdx.x == 0 && blockIdx.y == 0 ? g.rho + member : nullptr);
     const u64 row_bytes = g.ld * (g.type == 0 ? 4u : 2u);
     const unsigned char *x = (const unsigned char *)g.x.p[member];
     const bool wide = (((uintptr_t)x | row_bytes) & 15u) == 0;
@@ -423,6 +429,243 @@ __global__ void __launch_bounds__(256) k_join(Product g)
     }
 }
 
+// ---- matrices with a side of up to 64: one launch for a step ---------------------
+// X's long side is cut into runs of blocks of 64. A workgroup has a run: it takes the runs' parts of X X^T together (every
+// workgroup for itself, in one order: they all have the same D), makes D and P in LDS, the new X of its run block by
+// block, and that block's part of the next X X^T while it is in LDS. Only X turned over and the parts go through memory.
+// 64 x 576, four of them, five steps: 16 launches of the kernels above take 95 us (each as long as a launch).
+typedef unsigned char u8;
+
+struct Narrow {
+    Members x;                  // k_narrow_start: G
+    int type;
+    u32 rows, cols;             // of G
+    u64 ld;
+    const double *norm;
+    u32 norm_parts;
+    float eps;
+    float *rho;
+    const u8 *xt;               // [members][n] rows of m, k_narrow: read
+    u8 *xt_next;                // written
+    u64 xt_stride;
+    const float *part;          // [members][runs][64][64], read
+    float *part_next;           // written
+    u32 runs, blocks_each;
+    float c_gram, c_sum, c_old, c_one;
+    bool first, last;
+    Members to;                 // the result
+    int to_type;
+    u64 ldo;
+    float gain, keep, c_last;
+    int update;
+};
+
+template <Operands kOf> struct Block {      // 64 rows of 64 numbers in LDS, slices as Tile reads them
+    typedef Tile<kOf, 64, 64, 2, 2, 2, false> T;
+    static constexpr u32 kSlices = kSide / Stored<kOf>::kBlock, kBytes = kSlices * kSide * kSlice;
+    static __device__ __forceinline__ u8 *at(u8 *block, u32 row, u32 byte)
+    {
+        return block + (byte / kSlice) * (kSide * kSlice) + T::place(row, (byte % kSlice) >> 4) + (byte & 15u);
+    }
+    static __device__ __forceinline__ void put(u8 *block, u32 row, u32 col, const f32x4 &v)
+    {
+        f16x4 hi, lo;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            hi[c] = (_Float16)v[c];
+            lo[c] = (_Float16)(v[c] - (float)hi[c]);
+        }
+        const u32 byte = Stored<kOf>::at(col);
+        *(f16x4 *)at(block, row, byte) = hi;
+        if (kOf == kPairs) *(f16x4 *)at(block, row, byte + 64) = lo;
+    }
+    static __device__ __forceinline__ f32x4 get(u8 *block, u32 row, u32 col)
+    {
+        const u32 byte = Stored<kOf>::at(col);
+        const f16x4 hi = *(const f16x4 *)at(block, row, byte);
+        f32x4 v;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[c] = (float)hi[c];
+        if (kOf == kPairs) {
+            const f16x4 lo = *(const f16x4 *)at(block, row, byte + 64);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] += (float)lo[c];
+        }
+        return v;
+    }
+    static __device__ __forceinline__ void multiply(T &t, const u8 *a, const u8 *b)
+    {
+#pragma unroll
+        for (u32 s = 0; s < kSlices; ++s) t.one_slice(a + s * kSide * kSlice, b + s * kSide * kSlice);
+    }
+};
+
+// a block's part of X X^T, all of them of one workgroup: in binary32 to memory
+template <class T>
+__device__ __forceinline__ void write_part(const T &gram, float *to)
+{
+    gram.each([&](u32 r, u32 c, const f32x4 &sum) { *(f32x4 *)(to + r * kSide + c) = sum; });
+}
+
+template <Operands kOf>
+__global__ void __launch_bounds__(kNormThreads) k_narrow_start(Narrow g)
+{
+    typedef Stored<kOf> S;
+    typedef Block<kOf> B;
+    __shared__ float tile[kSide][kSide + 1];            // [m][n]
+    __shared__ __align__(16) u8 rows[B::kBytes];
+    const u32 member = blockIdx.y, run = blockIdx.x;
+    const bool over = g.rows > g.cols;
+    const u32 m = over ? g.cols : g.rows, n = over ? g.rows : g.cols;
+    const int e = exponent_of(g.norm + member * kNormBlocks, g.norm_parts, g.eps, run == 0 ? g.rho + member : nullptr);
+    const u64 row_bytes = g.ld * (g.type == 0 ? 4u : 2u);
+    const u8 *x = (const u8 *)g.x.p[member];
+    const bool wide = (((uintptr_t)x | row_bytes) & 15u) == 0;
+    u8 *xt = g.xt_next + member * g.xt_stride;
+    typename B::T gram;
+    gram.clear();
+    for (u32 b = 0; b < g.blocks_each; ++b) {
+        const u32 n0 = (run * g.blocks_each + b) * kSide;
+        if (n0 >= n) break;
+        // pieces of eight along G's rows
+#pragma unroll
+        for (u32 h = 0; h < 2; ++h) {
+            const u32 r = (threadIdx.x >> 3) + 32 * h, c = (threadIdx.x & 7u) * 8u;
+            const u32 row = over ? n0 + r : r, col = over ? c : n0 + c;
+            float v[8];
+            read_eight(v, x + (row < g.rows ? row : 0u) * row_bytes, col, row < g.rows ? g.cols : 0u, g.type, wide);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) (over ? tile[c + i][r] : tile[r][c + i]) = ldexpf(v[i], e);
+        }
+        __syncthreads();
+#pragma unroll
+        for (u32 h = 0; h < 4; ++h) {
+            const u32 r = (threadIdx.x >> 4) + 16 * h, c = (threadIdx.x & 15u) * 4u;
+            B::put(rows, r, c, f32x4{tile[r][c], tile[r][c + 1], tile[r][c + 2], tile[r][c + 3]});
+            if (n0 + r < n && c < S::padded(m))
+                S::put(xt + (u64)(n0 + r) * S::row_bytes(m), c, f32x4{tile[c][r], tile[c + 1][r], tile[c + 2][r], tile[c + 3][r]});
+        }
+        __syncthreads();
+        B::multiply(gram, rows, rows);
+    }
+    write_part(gram, g.part_next + ((u64)member * g.runs + run) * kSide * kSide);
+}
+
+template <Operands kOf>
+__global__ void __launch_bounds__(kNormThreads) k_narrow(Narrow g)
+{
+    typedef Stored<kOf> S;
+    typedef Block<kOf> B;
+    typedef typename B::T T;
+    __shared__ __align__(16) u8 lds[3][B::kBytes];      // D, then rows of the new X; P; X turned over
+    const u32 member = blockIdx.y, run = blockIdx.x;
+    const bool over = g.rows > g.cols;
+    const u32 m = over ? g.cols : g.rows, n = over ? g.rows : g.cols;
+    const float rho = g.first ? g.rho[member] : 1.0f;
+    const u32 row_xt = S::row_bytes(m), pieces = row_xt / 16;       // 16-byte pieces of a row of X turned over
+    const u8 *xt = g.xt + member * g.xt_stride;
+    u8 *xt_next = g.xt_next + member * g.xt_stride;
+    // a block of X turned over: rows of the long side, 16 bytes a thread and time
+    constexpr u32 kPieces = B::kBytes / 16 / kNormThreads;
+    auto load = [&](i32x4 (&v)[kPieces], u32 n0) {
+#pragma unroll
+        for (u32 q = 0; q < kPieces; ++q) {
+            const u32 at = threadIdx.x + q * kNormThreads, r = at / (B::kSlices * 8u), piece = at % (B::kSlices * 8u);
+            v[q] = i32x4{0, 0, 0, 0};
+            if (n0 + r < n && piece < pieces) v[q] = *(const i32x4 *)(xt + (u64)(n0 + r) * row_xt + piece * 16u);
+        }
+    };
+    const u32 first_block = run * g.blocks_each;
+    i32x4 held[kPieces];
+    load(held, first_block * kSide);
+    {
+        // D
+        const u32 r = threadIdx.x >> 2, c = (threadIdx.x & 3u) * 16u;
+        const float *part = g.part + (u64)member * g.runs * kSide * kSide + r * kSide + c;
+        f32x4 sum[4] = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll 4
+        for (u32 s = 0; s < g.runs; ++s)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sum[q] += *(const f32x4 *)(part + s * kSide * kSide + 4 * q);
+        const float scale = g.c_gram * rho * rho;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            f32x4 v = sum[q] * scale;
+#pragma unroll
+            for (u32 i = 0; i < 4; ++i)
+                if (c + 4 * q + i == r && r < m) v[i] -= (float)(1 << kLogD);
+            B::put(lds[0], r, c + 4 * q, v);
+        }
+    }
+    __syncthreads();
+    {
+        // P
+        T t;
+        t.clear();
+        B::multiply(t, lds[0], lds[0]);
+        t.each([&](u32 r, u32 c, const f32x4 &sum) {
+            f32x4 v = g.c_sum * sum + g.c_old * B::get(lds[0], r, c);
+#pragma unroll
+            for (u32 i = 0; i < 4; ++i)
+                if (c + i == r && r < m) v[i] += g.c_one;
+            B::put(lds[1], r, c, v);
+        });
+    }
+    T gram;
+    gram.clear();
+    for (u32 b = 0; b < g.blocks_each; ++b) {
+        const u32 n0 = (first_block + b) * kSide;
+        if (n0 >= n) break;
+#pragma unroll
+        for (u32 q = 0; q < kPieces; ++q) {
+            const u32 at = threadIdx.x + q * kNormThreads, r = at / (B::kSlices * 8u), piece = at % (B::kSlices * 8u);
+            *(i32x4 *)B::at(lds[2], r, piece * 16u) = held[q];
+        }
+        __syncthreads();                // (and P, and everybody has read D and the last block's rows)
+        if (b + 1 < g.blocks_each) load(held, n0 + kSide);
+        T t;
+        t.clear();
+        B::multiply(t, lds[1], lds[2]);
+        if (g.last) {
+            void *to = g.to.p[member];
+            const u32 size = g.to_type == 0 ? 4u : 2u;
+            const bool wide = !over && (((uintptr_t)to | (g.ldo * size)) & (4u * size - 1u)) == 0;
+            t.each([&](u32 r, u32 c, const f32x4 &sum) {
+                if (r >= m || n0 + c >= n) return;
+                f32x4 v = sum * (g.c_last * rho);
+                const u32 have = n - n0 - c;
+                const u64 at = over ? (u64)(n0 + c) * g.ldo + r : (u64)r * g.ldo + n0 + c, next = over ? g.ldo : 1u;
+                if (g.update) {
+                    const float *w = (const float *)to;
+#pragma unroll
+                    for (u32 q = 0; q < 4; ++q)
+                        if (q < have) v[q] = fmaf(g.gain, v[q], g.keep * w[at + q * next]);
+                }
+                if (!over) write_four(to, at, g.to_type, v, have, wide);
+                else
+#pragma unroll
+                    for (u32 q = 0; q < 4; ++q)
+                        if (q < have) write_as(to, at + q * next, g.to_type, v[q]);
+            });
+        } else {
+            const float c = ldexpf(rho, -kLogD);
+            t.each([&](u32 r, u32 col, const f32x4 &sum) {
+                f32x4 v = sum * c;
+#pragma unroll
+                for (u32 q = 0; q < 4; ++q)
+                    if (r >= m || n0 + col + q >= n) v[q] = 0.0f;
+                B::put(lds[0], r, col, v);
+                const u32 column = n0 + col + (lane_id() & 3u);
+                S::put_turned(xt_next + (u64)column * row_xt, r, v, column < n && (r & ~3u) < S::padded(m));
+            });
+            __syncthreads();
+            B::multiply(gram, lds[0], lds[0]);
+        }
+        __syncthreads();
+    }
+    if (!g.last) write_part(gram, g.part_next + ((u64)member * g.runs + run) * kSide * kSide);
+}
+
 }  // namespace rtopk
 
 using namespace rtopk;
@@ -477,6 +720,20 @@ GramPlan plan_gram(u32 members, const Shape &s, double *cost)
     return best;
 }
 
+// A side of up to 64: the long side's blocks of 64 in so many runs. A workgroup reads every run's part and makes its own
+// run's blocks: 0.27 us for a run and 1.2 for a block, least where the runs are the root of 4.4 times the blocks.
+struct NarrowPlan {
+    u32 runs, blocks_each;
+};
+NarrowPlan plan_narrow(const Shape &s)
+{
+    const u32 blocks = (s.n() + kSide - 1) / kSide;
+    const u32 runs = std::min(blocks, std::max(16u, (u32)std::ceil(std::sqrt(4.4 * blocks))));
+    const u32 each = (blocks + runs - 1) / runs;
+    return NarrowPlan{(blocks + each - 1) / each, each};
+}
+bool is_narrow(const Shape &s) { return s.m() <= kSide; }
+
 struct Parts {
     double *norm;
     float *rho, *average, *part;
@@ -497,6 +754,12 @@ u64 cut(void *base, u32 count, const Shape &s, bool average, Parts &p)
     p.square_stride = align_up((u64)s.m() * S::row_bytes(s.m()), 256);
     p.norm = (double *)take(kMembers * kNormBlocks * sizeof(double));
     p.rho = (float *)take(kMembers * sizeof(float));
+    if (is_narrow(s)) {
+        for (int i = 0; i < 2; ++i) p.xt[i] = take(members * p.xt_stride);
+        p.part = (float *)take(2ull * members * plan_narrow(s).runs * kSide * kSide * sizeof(float));
+        p.average = average ? (float *)take(members * align_up((u64)s.rows * s.cols, 64) * sizeof(float)) : nullptr;
+        return used;
+    }
     for (int i = 0; i < 2; ++i) {
         p.x[i] = take(members * p.x_stride);
         p.xt[i] = take(members * p.xt_stride);
@@ -583,12 +846,62 @@ struct Target {
     int update;
 };
 
+template <Operands kOf>
+int iterate_narrow(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 norm_parts, u32 steps, const float *abc, float eps,
+                   const Parts &p, const Target &target, hipStream_t stream)
+{
+    const NarrowPlan plan = plan_narrow(s);
+    const dim3 grid(plan.runs, members);
+    float *part[2] = {p.part, p.part + (u64)members * plan.runs * kSide * kSide};
+    Narrow g{};
+    g.x = x;
+    g.type = type;
+    g.rows = s.rows;
+    g.cols = s.cols;
+    g.ld = ldx;
+    g.norm = p.norm;
+    g.norm_parts = norm_parts;
+    g.eps = eps;
+    g.rho = p.rho;
+    g.xt_stride = p.xt_stride;
+    g.runs = plan.runs;
+    g.blocks_each = plan.blocks_each;
+    g.xt_next = p.xt[0];
+    g.part_next = part[0];
+    g.c_gram = ldexpf(1.0f, kLogD - 2 * kLogX);
+    g.c_last = ldexpf(1.0f, -kLogD - kLogX);
+    g.to = target.to;
+    g.to_type = target.type;
+    g.ldo = target.ld;
+    g.gain = target.gain;
+    g.keep = target.keep;
+    g.update = target.update;
+    k_narrow_start<kOf><<<grid, kNormThreads, 0, stream>>>(g);
+    if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
+    for (u32 i = 0; i < steps; ++i) {
+        const double a = abc[3 * i], b = abc[3 * i + 1], c = abc[3 * i + 2];
+        g.xt = p.xt[i & 1];
+        g.xt_next = p.xt[1 - (i & 1)];
+        g.part = part[i & 1];
+        g.part_next = part[1 - (i & 1)];
+        g.c_sum = (float)(c * ldexp(1.0, -kLogD));
+        g.c_old = (float)(b + 2.0 * c);
+        g.c_one = (float)((a + b + c) * ldexp(1.0, kLogD));
+        g.first = i == 0;
+        g.last = i + 1 == steps;
+        k_narrow<kOf><<<grid, kNormThreads, 0, stream>>>(g);
+        if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
+    }
+    return RTOPK_OK;
+}
+
 // From G and the parts of its norm to the end.
 template <Operands kOf>
 int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 norm_parts, u32 steps, const float *abc,
             double largest_p, float eps, const Parts &p, const Target &target, hipStream_t stream)
 {
     typedef Stored<kOf> S;
+    if (is_narrow(s)) return iterate_narrow<kOf>(x, type, ldx, s, members, norm_parts, steps, abc, eps, p, target, stream);
     const u32 m = s.m(), n = s.n();
     const Start start{x, type, s.rows, s.cols, ldx, s.over() ? p.xt[0] : p.x[0], s.over() ? p.x[0] : p.xt[0],
                       s.over() ? p.xt_stride : p.x_stride, s.over() ? p.x_stride : p.xt_stride, p.norm, norm_parts, eps, p.rho};
