@@ -335,12 +335,16 @@ __device__ __forceinline__ bool wide_out(const Scaled &g)
     const u32 size = g.type == 0 ? 4u : 2u;
     return (((uintptr_t)g.out | (g.ldo * size)) & (4u * size - 1u)) == 0;
 }
-__device__ __forceinline__ void write_scaled(const Scaled &g, u32 row, u32 col, const f32x4 &sum, float a_scale, const Four &f, bool wide)
+__device__ __forceinline__ f32x4 scaled(const f32x4 &sum, float a_scale, const Four &f)
 {
     f32x4 v;
 #pragma unroll
     for (u32 c = 0; c < 4; ++c) v[c] = fmaf(sum[c] * a_scale, f.scale[c], f.bias[c]);
-    write_four(g.out, (u64)row * g.ldo + col, g.type, v, g.n - col, wide);
+    return v;
+}
+__device__ __forceinline__ void write_scaled(const Scaled &g, u32 row, u32 col, const f32x4 &sum, float a_scale, const Four &f, bool wide)
+{
+    write_four(g.out, (u64)row * g.ldo + col, g.type, scaled(sum, a_scale, f), g.n - col, wide);
 }
 
 template <class T, bool kWhole>
@@ -362,17 +366,35 @@ __global__ void __launch_bounds__(T::kThreads) k_product(Scaled g)
         const bool wide = wide_out(g);
         float a_scale[T::kFragsM];
 #pragma unroll
-        for (int i = 0; i < T::kFragsM; ++i) a_scale[i] = g.a_scale[min(i0 + T::row0() + 16u * i + (lane_id() & 15u), g.m - 1u)];
+        for (int i = 0; i < T::kFragsM; ++i) a_scale[i] = g.a_scale[min(i0 + T::row_at(i), g.m - 1u)];
+        const bool eights = T::wide_at(0) && g.type != 0 && (((uintptr_t)g.out | g.ldo * 2u) & 15u) == 0;
 #pragma unroll
         for (int j = 0; j < T::kFragsN; ++j) {
-            const u32 col = j0 + T::col0() + 16u * j + 4u * (lane_id() >> 4);
+            const u32 col = j0 + T::col_at(j);
             if (col >= g.n) continue;
             const Four f = channels(g, col);
 #pragma unroll
             for (int i = 0; i < T::kFragsM; ++i) {
-                const u32 row = i0 + T::row0() + 16u * i + (lane_id() & 15u);
                 const i32x4 sum = t.sum[i][j];
-                if (row < g.m) write_scaled(g, row, col, f32x4{(float)sum[0], (float)sum[1], (float)sum[2], (float)sum[3]}, a_scale[i], f, wide);
+                const f32x4 v = scaled(f32x4{(float)sum[0], (float)sum[1], (float)sum[2], (float)sum[3]}, a_scale[i], f);
+                t.sum[i][j] = __builtin_bit_cast(i32x4, v);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < T::kFragsM; ++i) {
+            const u32 row = i0 + T::row_at(i);
+            if (row >= g.m) continue;
+#pragma unroll
+            for (int j = 0; j < T::kFragsN; j += T::step_at(j)) {
+                const u32 col = j0 + T::col_at(j), next = j0 + T::col_at(T::next_to(j));
+                const f32x4 v = __builtin_bit_cast(f32x4, t.sum[i][j]), u = __builtin_bit_cast(f32x4, t.sum[i][T::next_to(j)]);
+                const u64 first = (u64)row * g.ldo;
+                if (T::wide_at(j) && eights && col + 8u <= g.n) {
+                    write_eight(g.out, first + col, g.type, v, u);
+                } else {
+                    if (col < g.n) write_four(g.out, first + col, g.type, v, g.n - col, wide);
+                    if (T::wide_at(j) && next < g.n) write_four(g.out, first + next, g.type, u, g.n - next, wide);
+                }
             }
         }
     } else {
@@ -582,11 +604,16 @@ Plan plan_product(u32 m, u32 n, u32 k)
     return best;
 }
 
-template <class T>
+// eight columns a lane where the result has 16 bits, four where it (or a run's sums) has 32
+template <int kEdge, int kWavesM, int kWavesN, int kStages, bool kAhead>
 void launch_product(const Scaled &g, const Plan &p, bool whole, hipStream_t stream)
 {
-    if (whole) k_product<T, true><<<p.tiles * p.splits, T::kThreads, 0, stream>>>(g);
-    else k_product<T, false><<<p.tiles * p.splits, T::kThreads, 0, stream>>>(g);
+    typedef Tile<kBytes, kEdge, kEdge, kWavesM, kWavesN, kStages, kAhead, kWide> Eights;
+    typedef Tile<kBytes, kEdge, kEdge, kWavesM, kWavesN, kStages, kAhead, kRuns> Fours;
+    const u32 grid = p.tiles * p.splits;
+    if (!whole) k_product<Fours, false><<<grid, Fours::kThreads, 0, stream>>>(g);
+    else if (g.type != 0 && p.splits == 1) k_product<Eights, true><<<grid, Eights::kThreads, 0, stream>>>(g);
+    else k_product<Fours, true><<<grid, Fours::kThreads, 0, stream>>>(g);
 }
 
 template <int kWaves, int kTokens>
@@ -618,10 +645,10 @@ int run_product(Scaled g, void *part, hipStream_t stream)
     g.splits = p.splits;
     g.part = (int *)part;
     const bool whole = (((uintptr_t)g.a | (uintptr_t)g.b | g.lda | g.ldb) & 15u) == 0;
-    if (p.edge == 256) launch_product<Tile<kBytes, 256, 256, 2, 4, 2, true>>(g, p, whole, stream);
-    else if (p.edge == 192) launch_product<Tile<kBytes, 192, 192, 2, 4, 2, true>>(g, p, whole, stream);
-    else if (p.edge == 128) launch_product<Tile<kBytes, 128, 128, 2, 2, 2, false>>(g, p, whole, stream);
-    else launch_product<Tile<kBytes, 64, 64, 2, 2, 3, false>>(g, p, whole, stream);
+    if (p.edge == 256) launch_product<256, 2, 4, 2, true>(g, p, whole, stream);
+    else if (p.edge == 192) launch_product<192, 2, 4, 2, true>(g, p, whole, stream);
+    else if (p.edge == 128) launch_product<128, 2, 2, 2, false>(g, p, whole, stream);
+    else launch_product<64, 2, 2, 3, false>(g, p, whole, stream);
     if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
     if (p.splits > 1) {
         const u64 blocks = ((u64)g.m * ((g.n + 3) / 4) + 255) / 256;

@@ -77,7 +77,13 @@ __device__ __forceinline__ i32x4 cut_piece(const i32x4 &v, u32 at, u32 bytes)
 //   128 x 128, 2 x 2, 32    2131    1046    396
 // What bounds 256 x 256 is power: the matrix units are busy in 65% of the cycles, and the clock falls from 2.4 to 1.7 GHz.
 // kAhead: the first half of the next slice is read into registers before the second half of this one is multiplied.
-template <Operands kOf, int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kAhead>
+// How the rows of a wavefront's operands are dealt to its instructions, so that what a lane ends up with is stored in wide pieces:
+// kInOrder: fragment i has rows 16 i ..; kRuns: of A, a lane's rows are neighbours (eight, or four, or two of them: they
+// lie side by side in a result that is turned over); kWide: those, and of B the rows of two fragments alternate by
+// four, so that a lane has eight neighbouring columns (16 bytes of a 16-bit result; 64 bytes of a row from four lanes).
+enum Deal { kInOrder, kRuns, kWide };
+
+template <Operands kOf, int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kAhead, Deal kDeal = kInOrder>
 struct Tile {
     static constexpr int kRowsM = kM, kRowsN = kN;
     static constexpr int kWaves = kWavesM * kWavesN, kThreads = kWaves * kWave;
@@ -88,7 +94,7 @@ struct Tile {
     static_assert(kFragsM * kWavesM * 16 == kM && kFragsN * kWavesN * 16 == kN, "whole instructions");
     static_assert(kStages >= 2 && (!kAhead || kStages == 2), "one slice under way at least");
     typedef typename Sums<kOf>::type Sum;
-    // sum[i][j]: row 16 i + l % 16 of the wavefront's rows of A, rows 16 j + 4 (l / 16) .. + 3 of its rows of B
+    // sum[i][j]: row row_at(i) of A, rows col_at(j) .. + 3 of B
     Sum sum[kFragsM][kFragsN];
     // half a slice: 64 bytes of the wavefront's rows
     struct Half {
@@ -98,6 +104,27 @@ struct Tile {
     static __device__ __forceinline__ u32 wave() { return (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)); }
     static __device__ __forceinline__ u32 row0() { return wave() / kWavesN * (kM / kWavesM); }
     static __device__ __forceinline__ u32 col0() { return wave() % kWavesN * (kN / kWavesN); }
+
+    // row r of fragment i of the wavefront's rows of A, and of fragment j of its rows of B
+    static __device__ __forceinline__ u32 of_a(int i, u32 r)
+    {
+        constexpr int kEight = kFragsM / 8 * 8, kFour = kFragsM / 4 * 4, kRest = kFragsM - kFour;
+        if (kDeal == kInOrder) return 16u * i + r;
+        if (i < kEight) return 128u * (i / 8) + 8u * r + i % 8;
+        if (i < kFour) return 16u * kEight + 64u * ((i - kEight) / 4) + 4u * r + (i - kEight) % 4;
+        return 16u * kFour + kRest * r + (i - kFour);
+    }
+    static __device__ __forceinline__ u32 of_b(int j, u32 r)
+    {
+        if (kDeal == kWide && (j | 1) < kFragsN) return 32u * (j >> 1) + 8u * (r >> 2) + 4u * (j & 1) + (r & 3u);
+        return 16u * j + r;
+    }
+    static __device__ __forceinline__ u32 row_at(int i) { return row0() + of_a(i, lane_id() & 15u); }
+    static __device__ __forceinline__ u32 col_at(int j) { return col0() + of_b(j, 4u * (lane_id() >> 4)); }
+    // whether fragments j and j + 1 have eight neighbouring columns
+    static constexpr bool wide_at(int j) { return kDeal == kWide && j % 2 == 0 && j + 1 < kFragsN; }
+    static constexpr int step_at(int j) { return wide_at(j) ? 2 : 1; }
+    static constexpr int next_to(int j) { return j + 1 < kFragsN ? j + 1 : j; }
 
     __device__ __forceinline__ void clear()
     {
@@ -118,6 +145,14 @@ struct Tile {
     static __device__ __forceinline__ u32 row_of(int q)
     {
         return ((q < kLoadsM ? q : q - kLoadsM) * kWaves + wave()) * 8u + (lane_id() >> 3);
+    }
+    // the row of the operand that lies in row r of a stage
+    static __device__ __forceinline__ u32 dealt(int q, u32 r)
+    {
+        constexpr u32 kRowsA = kM / kWavesM, kRowsB = kN / kWavesN;
+        if (kDeal == kInOrder) return r;
+        if (q < kLoadsM) return r / kRowsA * kRowsA + of_a((int)(r % kRowsA / 16u), r & 15u);
+        return r / kRowsB * kRowsB + of_b((int)(r % kRowsB / 16u), r & 15u);
     }
     // where the wavefront's load q begins in a stage; lane l's 16 bytes follow at 16 l
     static __device__ __forceinline__ u32 stage_at(int q)
@@ -153,7 +188,7 @@ struct Tile {
 #pragma unroll
             for (int q = 0; q < kLoads; ++q) {
                 const TileRows &t = q < kLoadsM ? a : b;
-                const u32 r = row_of(q), row = r < t.rows ? r : t.rows - 1u;
+                const u32 r = row_of(q), row = min(dealt(q, r), t.rows - 1u);
                 offset[q] = row * t.stride + (((lane & 7u) ^ turn(r)) << 4);
             }
             const auto ra = __builtin_amdgcn_make_buffer_rsrc((void *)a.first, 0, 0xFFFFFFFFu, 0x00020000);
@@ -225,7 +260,7 @@ struct Tile {
 #pragma unroll
             for (int q = 0; q < kLoads; ++q) {
                 const TileRows &t = q < kLoadsM ? a : b;
-                const u32 r = row_of(q), row = r < t.rows ? r : t.rows - 1u;
+                const u32 r = row_of(q), row = min(dealt(q, r), t.rows - 1u);
                 at[q] = s * kSlice + (((lane_id() & 7u) ^ turn(r)) << 4);
                 piece[q] = load_piece(t.first + (u64)row * t.stride, at[q], t.bytes);
             }
@@ -303,11 +338,10 @@ struct Tile {
     template <class Act>
     __device__ __forceinline__ void each(Act act) const
     {
-        const u32 r = row0() + (lane_id() & 15u), c = col0() + 4u * (lane_id() >> 4);
 #pragma unroll
         for (int i = 0; i < kFragsM; ++i)
 #pragma unroll
-            for (int j = 0; j < kFragsN; ++j) act(r + 16u * i, c + 16u * j, sum[i][j]);
+            for (int j = 0; j < kFragsN; ++j) act(row_at(i), col_at(j), sum[i][j]);
     }
 };
 
@@ -368,6 +402,19 @@ __device__ __forceinline__ void write_as(void *p, u64 at, int type, float v)
 {
     if (type == 0) ((float *)p)[at] = v;
     else ((u16 *)p)[at] = half_bits(v, type);
+}
+
+// Eight neighbours of a 16-bit type, all there and from 16 bytes on.
+__device__ __forceinline__ void write_eight(void *p, u64 at, int type, const f32x4 &a, const f32x4 &b)
+{
+    typedef u16 u16x8 __attribute__((ext_vector_type(8)));
+    u16x8 v;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        v[c] = half_bits(a[c], type);
+        v[4 + c] = half_bits(b[c], type);
+    }
+    *(u16x8 *)((u16 *)p + at) = v;
 }
 
 // Four neighbours, of which `have` are there; `wide`: all four places start on 4 elements' bytes.

@@ -78,6 +78,22 @@ template <Operands kOf> struct Stored {
             *(f16x4 *)(row + at(col) + 64) = lo;
         }
     }
+    // kN neighbours (2, 4 or 8) from a multiple of kN on
+    template <int kN>
+    static __device__ __forceinline__ void put_run(unsigned char *row, u32 col, const float (&v)[kN])
+    {
+        typedef _Float16 Run __attribute__((ext_vector_type(kN)));
+        Run hi;
+#pragma unroll
+        for (int c = 0; c < kN; ++c) hi[c] = (_Float16)v[c];
+        *(Run *)(row + at(col)) = hi;
+        if (kOf == kPairs) {
+            Run lo;
+#pragma unroll
+            for (int c = 0; c < kN; ++c) lo[c] = (_Float16)(v[c] - (float)hi[c]);
+            *(Run *)(row + at(col) + 64) = lo;
+        }
+    }
     // Every four lanes 4 q .. 4 q + 3 have a row each (neighbours, from a multiple of four on) and the same four columns:
     // lane 4 q + i stores column i, the four rows side by side, to `column` of the matrix turned over.
     static __device__ __forceinline__ void put_turned(unsigned char *column, u32 row, const f32x4 &v, bool there)
@@ -306,7 +322,6 @@ __global__ void __launch_bounds__(T::kThreads) k_step(Product g)
     const TileRows a{g.left + member * g.left_stride + (u64)i0 * bytes, g.rows - i0, bytes, bytes};
     const TileRows b{g.right + member * g.right_stride + (u64)j0 * bytes, g.cols - j0, bytes, bytes};
     const u32 row_out = S::row_bytes(g.cols), row_turned = S::row_bytes(g.rows);
-    const u32 row1 = i0 + T::row0() + (lane_id() & 15u), col1 = j0 + T::col0() + 4u * (lane_id() >> 4);
     T t;
     t.clear();
     if (kStep == kSymmetric && g.old) {
@@ -318,8 +333,8 @@ __global__ void __launch_bounds__(T::kThreads) k_step(Product g)
         for (int i = 0; i < T::kFragsM; ++i)
 #pragma unroll
             for (int j = 0; j < T::kFragsN; ++j)
-                if (row1 + 16 * i < g.rows && col1 + 16 * j < S::padded(g.cols))
-                    t.sum[i][j] = ratio * S::get(old + (u64)(row1 + 16 * i) * row_out, col1 + 16 * j);
+                if (i0 + T::row_at(i) < g.rows && j0 + T::col_at(j) < S::padded(g.cols))
+                    t.sum[i][j] = ratio * S::get(old + (u64)(i0 + T::row_at(i)) * row_out, j0 + T::col_at(j));
     }
     const u32 from = kStep == kPart ? split * g.slices_each : 0u;
     t.template multiply<true>(a, b, from, kStep == kPart ? min(from + g.slices_each, slices) : slices, lds);
@@ -327,11 +342,9 @@ __global__ void __launch_bounds__(T::kThreads) k_step(Product g)
     if constexpr (kStep == kPart) {
         const u64 ld = align_up(g.rows, 4);
         float *part = g.part + ((u64)split * g.members + member) * g.rows * ld;
-#pragma unroll
-        for (int i = 0; i < T::kFragsM; ++i)
-#pragma unroll
-            for (int j = 0; j < T::kFragsN; ++j)
-                if (row1 + 16 * i < g.rows && col1 + 16 * j < g.cols) *(f32x4 *)(part + (row1 + 16 * i) * ld + col1 + 16 * j) = t.sum[i][j];
+        t.each([&](u32 r, u32 c, const f32x4 &sum) {
+            if (i0 + r < g.rows && j0 + c < g.cols) *(f32x4 *)(part + (i0 + r) * ld + j0 + c) = sum;
+        });
         return;
     }
     const float rho = g.rho ? g.rho[member] : 1.0f;
@@ -342,14 +355,14 @@ __global__ void __launch_bounds__(T::kThreads) k_step(Product g)
         const bool wide = (((uintptr_t)to | (g.ldo * size)) & (4u * size - 1u)) == 0;
 #pragma unroll
         for (int i = 0; i < T::kFragsM; ++i) {
-            const u32 row = row1 + 16 * i;
+            const u32 row = i0 + T::row_at(i);
             if (row >= g.rows) continue;
             const u64 first = (u64)row * g.ldo;
             f32x4 w[T::kFragsN];                // (a row of fragments' old weights at a time, for the same reason)
             if (g.update) {
 #pragma unroll
                 for (int j = 0; j < T::kFragsN; ++j) {
-                    const u32 col = col1 + 16 * j;
+                    const u32 col = j0 + T::col_at(j);
                     const float *from_w = (const float *)to + first + col;
                     if (wide && col + 4u <= g.cols) w[j] = *(const f32x4 *)from_w;
                     else
@@ -359,32 +372,80 @@ __global__ void __launch_bounds__(T::kThreads) k_step(Product g)
             }
 #pragma unroll
             for (int j = 0; j < T::kFragsN; ++j) {
-                const u32 col = col1 + 16 * j;
-                if (col >= g.cols) continue;
-                f32x4 v = t.sum[i][j] * c_sum;
+                t.sum[i][j] *= c_sum;
                 if (g.update)
 #pragma unroll
-                    for (u32 q = 0; q < 4; ++q) v[q] = fmaf(g.gain, v[q], g.keep * w[j][q]);
-                write_four(to, first + col, g.type, v, g.cols - col, wide);
+                    for (u32 q = 0; q < 4; ++q) t.sum[i][j][q] = fmaf(g.gain, t.sum[i][j][q], g.keep * w[j][q]);
+            }
+            const bool eights = g.type != 0 && (((uintptr_t)to | (g.ldo * size)) & 15u) == 0;
+#pragma unroll
+            for (int j = 0; j < T::kFragsN; j += T::step_at(j)) {
+                const u32 col = j0 + T::col_at(j), next = j0 + T::col_at(T::next_to(j));
+                if (T::wide_at(j) && eights && col + 8u <= g.cols) {
+                    write_eight(to, first + col, g.type, t.sum[i][j], t.sum[i][T::next_to(j)]);
+                } else {
+                    if (col < g.cols) write_four(to, first + col, g.type, t.sum[i][j], g.cols - col, wide);
+                    if (T::wide_at(j) && next < g.cols) write_four(to, first + next, g.type, t.sum[i][T::next_to(j)], g.cols - next, wide);
+                }
             }
         }
         return;
     }
-    unsigned char *out = g.out + member * g.out_stride, *turned = g.turned + member * g.turned_stride;
-    t.each([&](u32 r, u32 c, const f32x4 &sum) {
-        const u32 row = i0 + r, col = j0 + c;
-        f32x4 v = sum * c_sum;
 #pragma unroll
-        for (u32 q = 0; q < 4; ++q) {
-            if (kTriangle && col + q == row) v[q] += g.c_one;
-            if (row >= g.rows || col + q >= g.cols) v[q] = 0.0f;        // what pads the rows is zero
+    for (int i = 0; i < T::kFragsM; ++i)
+#pragma unroll
+        for (int j = 0; j < T::kFragsN; ++j) {
+            const u32 row = i0 + T::row_at(i), col = j0 + T::col_at(j);
+            t.sum[i][j] *= c_sum;
+#pragma unroll
+            for (u32 q = 0; q < 4; ++q) {
+                if (kTriangle && col + q == row) t.sum[i][j][q] += g.c_one;
+                if (row >= g.rows || col + q >= g.cols) t.sum[i][j][q] = 0.0f;          // what pads the rows is zero
+            }
         }
-        if (row < g.rows && col < S::padded(g.cols)) S::put(out + (u64)row * row_out, col, v);
-        if (!kTriangle || ti != tj) {
-            const u32 column = col + (lane_id() & 3u);
-            S::put_turned(turned + (u64)column * row_turned, row, v, column < g.cols && (row & ~3u) < S::padded(g.rows));
+    unsigned char *out = g.out + member * g.out_stride, *turned = g.turned + member * g.turned_stride;
+#pragma unroll
+    for (int i = 0; i < T::kFragsM; ++i) {
+        const u32 row = i0 + T::row_at(i);
+        if (row >= g.rows) continue;
+        unsigned char *to = out + (u64)row * row_out;
+#pragma unroll
+        for (int j = 0; j < T::kFragsN; j += T::step_at(j)) {
+            const u32 col = j0 + T::col_at(j);
+            if (col >= S::padded(g.cols)) continue;
+            const f32x4 &v = t.sum[i][j], &u = t.sum[i][T::next_to(j)];
+            if (T::wide_at(j)) S::template put_run<8>(to, col, {v[0], v[1], v[2], v[3], u[0], u[1], u[2], u[3]});
+            else S::put(to, col, v);
         }
-    });
+    }
+    if (kTriangle && ti == tj) return;
+#pragma unroll
+    for (int j = 0; j < T::kFragsN; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const u32 col = j0 + T::col_at(j) + e;
+            if (col >= g.cols) continue;
+            unsigned char *to = turned + (u64)col * row_turned;
+            constexpr int kEight = T::kFragsM / 8 * 8, kFour = T::kFragsM / 4 * 4;
+            static_assert(T::kFragsM % 4 == 0 || T::kFragsM % 4 == 2, "a rest of two");
+#pragma unroll
+            for (int i = 0; i + 8 <= kEight; i += 8) {
+                const u32 row = i0 + T::row_at(i);
+                if (row < S::padded(g.rows))
+                    S::template put_run<8>(to, row, {t.sum[i][j][e], t.sum[i + 1][j][e], t.sum[i + 2][j][e], t.sum[i + 3][j][e],
+                                                     t.sum[i + 4][j][e], t.sum[i + 5][j][e], t.sum[i + 6][j][e], t.sum[i + 7][j][e]});
+            }
+#pragma unroll
+            for (int i = kEight; i + 4 <= kFour; i += 4) {
+                const u32 row = i0 + T::row_at(i);
+                if (row < S::padded(g.rows))
+                    S::template put_run<4>(to, row, {t.sum[i][j][e], t.sum[i + 1][j][e], t.sum[i + 2][j][e], t.sum[i + 3][j][e]});
+            }
+            if constexpr (T::kFragsM % 4 == 2) {
+                const u32 row = i0 + T::row_at(kFour);
+                if (row < S::padded(g.rows)) S::template put_run<2>(to, row, {t.sum[kFour][j][e], t.sum[kFour + 1][j][e]});
+            }
+        }
 }
 
 // The runs of X X^T together, in their order, scaled, less the identity: D, both sides of the diagonal, by blocks of 64 x 64.
@@ -831,11 +892,13 @@ int launch(Product g, u32 members, hipStream_t stream)
 template <Operands kOf, Step kStep>
 int launch(const Product &g, u32 members, u32 edge, hipStream_t stream)
 {
+    // eight columns a lane where halves are stored; four where binary32 is (a fragment's 64 bytes of a row)
     constexpr bool kAhead = kOf != kPairs;
-    if (edge == 256) return launch<kOf, Tile<kOf, 256, 256, 2, 4, 2, kAhead>, kStep>(g, members, stream);
-    if (edge == 192) return launch<kOf, Tile<kOf, 192, 192, 2, 4, 2, kAhead>, kStep>(g, members, stream);
-    if (edge == 128) return launch<kOf, Tile<kOf, 128, 128, 2, 2, 2, false>, kStep>(g, members, stream);
-    return launch<kOf, Tile<kOf, 64, 64, 2, 2, 3, false>, kStep>(g, members, stream);
+    constexpr Deal kDeal = kStep == kPart || (kStep == kLast && kOf == kPairs) ? kRuns : kWide;
+    if (edge == 256) return launch<kOf, Tile<kOf, 256, 256, 2, 4, 2, kAhead, kDeal>, kStep>(g, members, stream);
+    if (edge == 192) return launch<kOf, Tile<kOf, 192, 192, 2, 4, 2, kAhead, kDeal>, kStep>(g, members, stream);
+    if (edge == 128) return launch<kOf, Tile<kOf, 128, 128, 2, 2, 2, false, kDeal>, kStep>(g, members, stream);
+    return launch<kOf, Tile<kOf, 64, 64, 2, 2, 3, false, kDeal>, kStep>(g, members, stream);
 }
 
 struct Target {
