@@ -65,11 +65,45 @@ __device__ __forceinline__ u32 four_bytes(const int *q)
     return ((u32)q[0] & 255u) | ((u32)q[1] & 255u) << 8 | ((u32)q[2] & 255u) << 16 | (u32)q[3] << 24;
 }
 
+// Eight neighbours of a row as they are in memory, and as numbers. The load has no branch around it (several are under
+// way together): a lane whose eight are not all there takes the row's first eight, or zeros of the library's where the row is
+// shorter, and `numbers` reads what there is of them one by one.
+static __device__ const u32 kNothing[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+
+template <int kType> struct Eight {
+    i32x4 w[kType == RTOPK_F32 ? 2 : 1];
+    static constexpr u32 kSize = kType == RTOPK_F32 ? 4u : 2u;
+    __device__ __forceinline__ void load(const unsigned char *row, u32 c, u32 cols)
+    {
+        const unsigned char *p = cols < 8u ? (const unsigned char *)kNothing : row + (c + 8u <= cols ? c : 0u) * kSize;
+        __builtin_memcpy(w, p, sizeof w);
+    }
+    __device__ __forceinline__ void numbers(float (&v)[8], const unsigned char *row, u32 c, u32 cols) const
+    {
+        const bool all = c + 8u <= cols;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float x;
+            if (kType == RTOPK_F32) {
+                x = __uint_as_float((u32)w[kType == RTOPK_F32 ? i >> 2 : 0][i & 3]);
+            } else {
+                const u16 h = (u16)((u32)w[0][i >> 1] >> (16 * (i & 1)));
+                x = kType == RTOPK_BF16 ? __uint_as_float((u32)h << 16) : (float)__builtin_bit_cast(_Float16, h);
+            }
+            v[i] = all ? x : 0.0f;
+        }
+        if (c < cols && !all) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c + i < cols) v[i] = read_as(row, c + i, kType);
+        }
+    }
+};
+
 struct RowsToQuantize {
     const void *x;
     u64 ldx;            // elements
     u32 rows, cols, fill;
-    int type;
     signed char *q;
     u64 ldq;
     float *scale;
@@ -79,7 +113,7 @@ constexpr int kQuantizeThreads = 256;
 
 // kWavesPerRow wavefronts hold a row in registers, kPieces pieces of eight numbers a lane (kPieces = 0: the row is
 // longer, and read twice, the second time from the caches). What lies between cols and fill becomes zero.
-template <int kWavesPerRow, int kPieces>
+template <int kType, int kWavesPerRow, int kPieces>
 __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kQuantizeThreads) k_quantize_rows(RowsToQuantize g)
 {
     constexpr u32 kWaves = kWavesPerRow > 4 ? kWavesPerRow : 4, kRows = kWaves / kWavesPerRow, kStep = 8u * kWave * kWavesPerRow;
@@ -87,25 +121,25 @@ __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kQua
     const u32 lane = lane_id(), wave = threadIdx.x / kWave;
     const u32 r = blockIdx.x * kRows + wave / kWavesPerRow;
     const bool there = r < g.rows;
-    const u64 row_bytes = g.ldx * (g.type == 0 ? 4u : 2u);
-    const unsigned char *row = (const unsigned char *)g.x + (there ? r : 0u) * row_bytes;
-    const bool wide = (((uintptr_t)g.x | row_bytes) & 15u) == 0;
-    const u32 c0 = (wave % kWavesPerRow * kWave + lane) * 8u, cols = there ? g.cols : 0u;
-    float held[kPieces ? kPieces : 1][8];
+    const unsigned char *row = (const unsigned char *)g.x + (there ? r : 0u) * g.ldx * Eight<kType>::kSize;
+    const u32 c0 = (wave % kWavesPerRow * kWave + lane) * 8u;
+    Eight<kType> held[kPieces ? kPieces : 1];
     u32 largest = 0;
-    auto look = [&](const float (&v)[8]) {
+    auto look = [&](const Eight<kType> &e, u32 c) {
+        float v[8];
+        e.numbers(v, row, c, g.cols);
 #pragma unroll
         for (int i = 0; i < 8; ++i) largest = max(largest, magnitude(v[i]));
     };
     if constexpr (kPieces > 0) {
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) read_eight(held[p], row, c0 + p * kStep, cols, g.type, wide);
+        for (int p = 0; p < kPieces; ++p) held[p].load(row, c0 + p * kStep, g.cols);
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) look(held[p]);
+        for (int p = 0; p < kPieces; ++p) look(held[p], c0 + p * kStep);
     } else {
-        for (u32 c = c0; c < cols; c += kStep) {
-            read_eight(held[0], row, c, cols, g.type, wide);
-            look(held[0]);
+        for (u32 c = c0; c < g.cols; c += kStep) {
+            held[0].load(row, c, g.cols);
+            look(held[0], c);
         }
     }
     largest = wave_max_dpp(largest);
@@ -120,8 +154,10 @@ __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kQua
     if (c0 == 0) g.scale[r] = quantize.s;
     signed char *q = g.q + (u64)r * g.ldq;
     const bool wide_q = (((uintptr_t)g.q | g.ldq) & 7u) == 0;
-    auto write = [&](const float (&v)[8], u32 c) {
+    auto write = [&](const Eight<kType> &e, u32 c) {
+        float v[8];
         int n[8];
+        e.numbers(v, row, c, g.cols);
         quantize(n, v);
         const u32 word[2] = {four_bytes(n), four_bytes(n + 4)};
         if (wide_q && c + 8u <= g.fill) {
@@ -137,7 +173,7 @@ __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kQua
         for (int p = 0; p < kPieces; ++p) write(held[p], c0 + p * kStep);
     } else {
         for (u32 c = c0; c < g.fill; c += kStep) {
-            read_eight(held[0], row, c, cols, g.type, wide);
+            held[0].load(row, c, g.cols);
             write(held[0], c);
         }
     }
@@ -150,8 +186,8 @@ constexpr u32 kMostRuns = 64;
 
 inline u32 run_rows(u32 rows, u32 cols)
 {
-    // two workgroups a compute unit, 16 rows at least
-    const u32 groups = (cols + kGroup - 1) / kGroup, runs = std::min(kMostRuns, (2 * kUnits + groups - 1) / groups);
+    // four workgroups a compute unit, 16 rows at least
+    const u32 groups = (cols + kGroup - 1) / kGroup, runs = std::min(kMostRuns, (4 * kUnits + groups - 1) / groups);
     return std::max((rows + runs - 1) / runs, 16u);
 }
 inline u32 runs_of(u32 rows, u32 cols) { return (rows + run_rows(rows, cols) - 1) / run_rows(rows, cols); }
@@ -161,7 +197,6 @@ struct ColumnsToQuantize {
     u64 ldx;
     u32 rows, cols, fill;       // fill: the length that a turned row gets, zeros from `rows` on
     u32 run, runs;
-    int type;
     signed char *q;             // [cols][ldq]
     u64 ldq;
     float *scale;
@@ -170,6 +205,7 @@ struct ColumnsToQuantize {
     float *total;               // [cols], or null
 };
 
+template <int kType>
 __global__ void __launch_bounds__(kQuantizeThreads) k_column_most(ColumnsToQuantize g)
 {
     constexpr u32 kWaves = kQuantizeThreads / kWave, kAtOnce = 8;
@@ -177,24 +213,24 @@ __global__ void __launch_bounds__(kQuantizeThreads) k_column_most(ColumnsToQuant
     __shared__ float sums[kWaves - 1][kGroup];
     const u32 lane = lane_id(), wave = threadIdx.x / kWave, c = blockIdx.x * kGroup + lane * 8u;
     const u32 r0 = blockIdx.y * g.run, r1 = min(r0 + g.run, g.rows);
-    const u64 row_bytes = g.ldx * (g.type == 0 ? 4u : 2u);
-    const bool wide = (((uintptr_t)g.x | row_bytes) & 15u) == 0;
+    const u64 row_bytes = g.ldx * Eight<kType>::kSize;
     u32 largest[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (u32 r = r0 + wave; r < r1; r += kAtOnce * kWaves) {
-        float v[kAtOnce][8];
+        Eight<kType> e[kAtOnce];
+#pragma unroll
+        for (u32 q = 0; q < kAtOnce; ++q) e[q].load((const unsigned char *)g.x + min(r + q * kWaves, r1 - 1u) * row_bytes, c, g.cols);
 #pragma unroll
         for (u32 q = 0; q < kAtOnce; ++q) {
-            const u32 at = r + q * kWaves;
-            read_eight(v[q], (const unsigned char *)g.x + (at < r1 ? at : r) * row_bytes, c, at < r1 ? g.cols : 0u, g.type, wide);
-        }
-#pragma unroll
-        for (u32 q = 0; q < kAtOnce; ++q)
+            if (r + q * kWaves >= r1) break;
+            float v[8];
+            e[q].numbers(v, (const unsigned char *)g.x + (r + q * kWaves) * row_bytes, c, g.cols);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                largest[i] = max(largest[i], magnitude(v[q][i]));
-                sum[i] += v[q][i];
+                largest[i] = max(largest[i], magnitude(v[i]));
+                sum[i] += v[i];
             }
+        }
     }
     if (wave) {
 #pragma unroll
@@ -220,9 +256,10 @@ __global__ void __launch_bounds__(kQuantizeThreads) k_column_most(ColumnsToQuant
 }
 
 // A workgroup turns some blocks of 64 columns and 128 rows over: a lane reads eight columns of four rows, and puts
-// the four numbers of each column side by side into LDS.
+// the four numbers of each column side by side into LDS. The next block is on its way while this one is turned.
 constexpr u32 kTurnRows = 128, kMostBlocks = 4;
 
+template <int kType>
 __global__ void __launch_bounds__(kQuantizeThreads) k_quantize_columns(ColumnsToQuantize g, u32 blocks)
 {
     constexpr u32 kParts = kQuantizeThreads / kWave;
@@ -232,13 +269,23 @@ __global__ void __launch_bounds__(kQuantizeThreads) k_quantize_columns(ColumnsTo
     __shared__ u32 turned[kWave][kTurnRows / 4 + 1];
     const u32 lane = lane_id(), wave = threadIdx.x / kWave, c0 = blockIdx.x * kWave, first = blockIdx.y * blocks * kTurnRows;
     const bool totals = g.total && first == 0;
+    const u64 row_bytes = g.ldx * Eight<kType>::kSize;
+    const bool wide_q = (((uintptr_t)g.q | g.ldq) & 15u) == 0;
+    const u32 piece = threadIdx.x & 7u, quad = threadIdx.x >> 3, c = c0 + 8u * piece;       // columns c .. c + 7 of rows 4 quad .. + 3
+    Eight<kType> e[4];
+    auto load = [&](u32 r0) {
+#pragma unroll
+        for (u32 b = 0; b < 4; ++b) e[b].load((const unsigned char *)g.x + min(r0 + 4 * quad + b, g.rows - 1u) * row_bytes, c, g.cols);
+    };
+    load(first);
     {
-        const u32 c = min(c0 + lane, g.cols - 1u);
+        const u32 at = min(c0 + lane, g.cols - 1u);
         u32 largest = 0;
         double sum = 0.0;
-        for (u32 s = wave; s < g.runs; s += kParts) largest = max(largest, g.most[(u64)s * g.cols + c]);
+#pragma unroll 8
+        for (u32 s = wave; s < g.runs; s += kParts) largest = max(largest, g.most[(u64)s * g.cols + at]);
         if (totals)
-            for (u32 s = wave; s < g.runs; s += kParts) sum += (double)g.sums[(u64)s * g.cols + c];
+            for (u32 s = wave; s < g.runs; s += kParts) sum += (double)g.sums[(u64)s * g.cols + at];
         most[wave][lane] = largest;
         sums[wave][lane] = sum;
         __syncthreads();
@@ -256,9 +303,6 @@ __global__ void __launch_bounds__(kQuantizeThreads) k_quantize_columns(ColumnsTo
         }
         __syncthreads();
     }
-    const u64 row_bytes = g.ldx * (g.type == 0 ? 4u : 2u);
-    const bool wide = (((uintptr_t)g.x | row_bytes) & 15u) == 0, wide_q = (((uintptr_t)g.q | g.ldq) & 15u) == 0;
-    const u32 piece = threadIdx.x & 7u, quad = threadIdx.x >> 3, c = c0 + 8u * piece;       // columns c .. c + 7 of rows 4 quad .. + 3
     float s[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) s[i] = scale[8 * piece + i];
@@ -269,8 +313,9 @@ __global__ void __launch_bounds__(kQuantizeThreads) k_quantize_columns(ColumnsTo
 #pragma unroll
         for (u32 b = 0; b < 4; ++b) {
             const u32 r = r0 + 4 * quad + b;
-            read_eight(v[b], (const unsigned char *)g.x + (r < g.rows ? r : 0u) * row_bytes, c, r < g.rows ? g.cols : 0u, g.type, wide);
+            e[b].numbers(v[b], (const unsigned char *)g.x + min(r, g.rows - 1u) * row_bytes, c, r < g.rows ? g.cols : 0u);
         }
+        if (block + 1 < blocks) load(r0 + kTurnRows);
         if (block) __syncthreads();
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -582,8 +627,9 @@ struct Plan {
 };
 
 // The tile and the number of runs of the contraction that cost least. Runs cost a launch, and four bytes of every sum
-// written and read.
-Plan plan_product(u32 m, u32 n, u32 k)
+// written and read. Rows that do not start on 128 bytes take two lines for every slice: a slice is 1.3 times as long
+// (1499 x 5001 x 2003, rows 5248 or 5008 bytes apart: 38 / 46 us; 2048 x 4096 x 4096, 4096 or 4160: 37 / 45).
+Plan plan_product(u32 m, u32 n, u32 k, bool on_lines)
 {
     Plan best{};
     double least = 0.0;
@@ -593,8 +639,8 @@ Plan plan_product(u32 m, u32 n, u32 k)
         for (u32 splits = must; splits <= std::max(must, std::min(16u, slices / 4)); ++splits) {
             const u32 each = std::max(1u, (slices + splits - 1) / splits);
             if (splits > must && (slices + each - 1) / each != splits) continue;
-            double cost = tiles_cost(kCostBytes, edge, tiles * splits, each);
-            if (splits > 1) cost += 4.0 + (double)m * n * splits * 8.0 / 4e6;
+            double cost = tiles_cost(kCostBytes, edge, tiles * splits, each * (on_lines ? 1.0 : 1.3));
+            if (splits > 1) cost += 3.0 + (double)m * n * splits * 8.0 / 6e6;
             if (best.edge && cost >= least) continue;
             least = cost;
             best = Plan{edge, (u32)tiles, slices, each, std::max(1u, (slices + each - 1) / each), 0};
@@ -603,6 +649,8 @@ Plan plan_product(u32 m, u32 n, u32 k)
     best.part_bytes = best.splits > 1 ? align_up((u64)best.splits * m * align_up(n, 4) * 4, 256) : 0;
     return best;
 }
+// what a product of these sizes may need for the runs' sums, however its rows lie
+u64 part_bytes(u32 m, u32 n, u32 k) { return std::max(plan_product(m, n, k, false).part_bytes, plan_product(m, n, k, true).part_bytes); }
 
 // eight columns a lane where the result has 16 bits, four where it (or a run's sums) has 32
 template <int kEdge, int kWavesM, int kWavesN, int kStages, bool kAhead>
@@ -640,7 +688,7 @@ int run_few(const Few &f, hipStream_t stream)
 
 int run_product(Scaled g, void *part, hipStream_t stream)
 {
-    const Plan p = plan_product(g.m, g.n, g.k);
+    const Plan p = plan_product(g.m, g.n, g.k, ((g.lda | g.ldb) & 127u) == 0);
     g.slices_each = p.slices_each;
     g.splits = p.splits;
     g.part = (int *)part;
@@ -664,37 +712,53 @@ constexpr u64 kMostSize = 1u << 22;
 bool size_ok(u64 v) { return v >= 1 && v <= kMostSize; }
 bool type_ok(int type) { return type == RTOPK_F32 || type == RTOPK_BF16 || type == RTOPK_F16; }
 
+template <int kType>
+void launch_rows(const RowsToQuantize &g, hipStream_t stream)
+{
+    // what a wavefront's lanes hold in one piece each is 512 numbers: one wavefront for a short row where there are many
+    const u32 rows = g.rows, fill = g.fill;
+    if (fill <= 512 && rows >= 4 * kUnits) k_quantize_rows<kType, 1, 1><<<(rows + 3) / 4, kQuantizeThreads, 0, stream>>>(g);
+    else if (fill <= 1024 && rows >= 4 * kUnits) k_quantize_rows<kType, 1, 2><<<(rows + 3) / 4, kQuantizeThreads, 0, stream>>>(g);
+    else if (fill <= 2048) k_quantize_rows<kType, 4, 1><<<rows, kQuantizeThreads, 0, stream>>>(g);
+    else if (fill <= 4096) k_quantize_rows<kType, 4, 2><<<rows, kQuantizeThreads, 0, stream>>>(g);
+    else if (fill <= 8192) k_quantize_rows<kType, 4, 4><<<rows, kQuantizeThreads, 0, stream>>>(g);
+    else if (fill <= 16384) k_quantize_rows<kType, 16, 2><<<rows, 16 * kWave, 0, stream>>>(g);
+    else k_quantize_rows<kType, 16, 0><<<rows, 16 * kWave, 0, stream>>>(g);
+}
+
 int quantize_rows(const void *x, int type, u32 rows, u32 cols, u64 ldx, signed char *q, u64 ldq, u32 fill, float *scale,
                   hipStream_t stream)
 {
-    const RowsToQuantize g{x, ldx, rows, cols, fill, type, q, ldq, scale};
-    // what a wavefront's lanes hold in one piece each is 512 numbers: one wavefront for a short row where there are many
-    if (fill <= 512 && rows >= 4 * kUnits) k_quantize_rows<1, 1><<<(rows + 3) / 4, kQuantizeThreads, 0, stream>>>(g);
-    else if (fill <= 1024 && rows >= 4 * kUnits) k_quantize_rows<1, 2><<<(rows + 3) / 4, kQuantizeThreads, 0, stream>>>(g);
-    else if (fill <= 2048) k_quantize_rows<4, 1><<<rows, kQuantizeThreads, 0, stream>>>(g);
-    else if (fill <= 4096) k_quantize_rows<4, 2><<<rows, kQuantizeThreads, 0, stream>>>(g);
-    else if (fill <= 8192) k_quantize_rows<4, 4><<<rows, kQuantizeThreads, 0, stream>>>(g);
-    else if (fill <= 16384) k_quantize_rows<16, 2><<<rows, 16 * kWave, 0, stream>>>(g);
-    else k_quantize_rows<16, 0><<<rows, 16 * kWave, 0, stream>>>(g);
+    const RowsToQuantize g{x, ldx, rows, cols, fill, q, ldq, scale};
+    if (type == RTOPK_F32) launch_rows<RTOPK_F32>(g, stream);
+    else if (type == RTOPK_BF16) launch_rows<RTOPK_BF16>(g, stream);
+    else launch_rows<RTOPK_F16>(g, stream);
     return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_EHIP;
 }
 
 u64 column_scratch(u32 rows, u32 cols, bool sums) { return align_up((u64)runs_of(rows, cols) * cols * (sums ? 8 : 4), 256); }
+
+template <int kType>
+int launch_columns(const ColumnsToQuantize &g, hipStream_t stream)
+{
+    k_column_most<kType><<<dim3((g.cols + kGroup - 1) / kGroup, g.runs), kQuantizeThreads, 0, stream>>>(g);
+    if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
+    // as many blocks for a workgroup (each of which takes the runs together) as leave four workgroups a unit
+    const u32 groups = (g.cols + kWave - 1) / kWave, all = (g.fill + kTurnRows - 1) / kTurnRows;
+    const u32 blocks = std::max(1u, std::min(kMostBlocks, (u32)((u64)groups * all / (4 * kUnits))));
+    k_quantize_columns<kType><<<dim3(groups, (all + blocks - 1) / blocks), kQuantizeThreads, 0, stream>>>(g, blocks);
+    return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_EHIP;
+}
 
 int quantize_columns(const void *x, int type, u32 rows, u32 cols, u64 ldx, signed char *q, u64 ldq, u32 fill, float *scale,
                      float *total, void *scratch, hipStream_t stream)
 {
     const u32 runs = runs_of(rows, cols);
     u32 *most = (u32 *)scratch;
-    const ColumnsToQuantize g{x, ldx, rows, cols, fill, run_rows(rows, cols), runs, type, q, ldq, scale, most,
+    const ColumnsToQuantize g{x, ldx, rows, cols, fill, run_rows(rows, cols), runs, q, ldq, scale, most,
                               total ? (float *)(most + (u64)runs * cols) : nullptr, total};
-    k_column_most<<<dim3((cols + kGroup - 1) / kGroup, runs), kQuantizeThreads, 0, stream>>>(g);
-    if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
-    // as many blocks for a workgroup (each of which takes the runs together) as leave four workgroups a unit
-    const u32 groups = (cols + kWave - 1) / kWave, all = (fill + kTurnRows - 1) / kTurnRows;
-    const u32 blocks = std::max(1u, std::min(kMostBlocks, (u32)((u64)groups * all / (4 * kUnits))));
-    k_quantize_columns<<<dim3(groups, (all + blocks - 1) / blocks), kQuantizeThreads, 0, stream>>>(g, blocks);
-    return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_EHIP;
+    return type == RTOPK_F32 ? launch_columns<RTOPK_F32>(g, stream)
+           : type == RTOPK_BF16 ? launch_columns<RTOPK_BF16>(g, stream) : launch_columns<RTOPK_F16>(g, stream);
 }
 
 bool workspace_ok(const void *p, u64 bytes, u64 need) { return need == 0 || (p && ((uintptr_t)p & 255u) == 0 && bytes >= need); }
@@ -724,7 +788,7 @@ u64 cut_linear(void *base, u32 m, u32 k, u32 n, LinearParts &p)
     if (in_one(m, k)) return 0;
     p.x = cut.take<signed char>(m * filled(k));
     p.x_scale = cut.take<float>(4ull * m);
-    p.part = cut.take<void>(few_tokens(m, k) ? 0 : plan_product(m, n, k).part_bytes);
+    p.part = cut.take<void>(few_tokens(m, k) ? 0 : part_bytes(m, n, k));
     return cut.at;
 }
 
@@ -743,7 +807,7 @@ u64 cut_backward(void *base, u32 m, u32 k, u32 n, BackwardParts &p)
     p.dy_turned_scale = cut.take<float>(4ull * n);
     p.x_turned_scale = cut.take<float>(4ull * k);
     p.scratch = cut.take<void>(std::max(column_scratch(m, n, true), column_scratch(m, k, false)));
-    p.part = cut.take<void>(std::max(plan_product(m, k, n).part_bytes, plan_product(n, k, m).part_bytes));
+    p.part = cut.take<void>(std::max(part_bytes(m, k, n), part_bytes(n, k, m)));
     return cut.at;
 }
 
@@ -777,7 +841,7 @@ extern "C" int rtopk_quantize_i8(const void *x, int type, uint64_t rows, uint64_
 extern "C" int rtopk_matmul_i8_workspace_bytes(uint64_t m, uint64_t n, uint64_t k, uint64_t *bytes)
 {
     if (!bytes || m > kMostSize || n > kMostSize || k > kMostSize) return RTOPK_EINVAL;
-    *bytes = m && n ? plan_product((u32)m, (u32)n, (u32)k).part_bytes : 0;
+    *bytes = m && n ? part_bytes((u32)m, (u32)n, (u32)k) : 0;
     return RTOPK_OK;
 }
 

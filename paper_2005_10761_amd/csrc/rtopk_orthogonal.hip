@@ -449,8 +449,10 @@ __global__ void __launch_bounds__(T::kThreads) k_step(Product g)
 }
 
 // The runs of X X^T together, in their order, scaled, less the identity: D, both sides of the diagonal, by blocks of 64 x 64.
+constexpr u32 kJoinThreads = kSide * kSide / 4;
+
 template <Operands kOf>
-__global__ void __launch_bounds__(256) k_join(Product g)
+__global__ void __launch_bounds__(kJoinThreads) k_join(Product g)
 {
     typedef Stored<kOf> S;
     __shared__ float tile[kSide][kSide + 1];
@@ -462,13 +464,12 @@ __global__ void __launch_bounds__(256) k_join(Product g)
     const float rho = g.rho ? g.rho[member] : 1.0f, c_sum = g.c_sum * rho * rho;
     const u32 row_out = S::row_bytes(g.rows);
     unsigned char *out = g.out + member * g.out_stride;
-#pragma unroll
-    for (u32 h = 0; h < 4; ++h) {
-        const u32 row = ti * kSide + r + 16 * h, col = tj * kSide + c;
+    {
+        const u32 row = ti * kSide + r, col = tj * kSide + c;
         f32x4 v{0, 0, 0, 0};
         if (row < g.rows && col < g.rows) {
             const float *p = g.part + member * one + row * ld + col;
-#pragma unroll 4
+#pragma unroll 8
             for (u32 s = 0; s < g.splits; ++s) v += *(const f32x4 *)(p + s * g.members * one);
         }
         v *= c_sum;
@@ -476,18 +477,14 @@ __global__ void __launch_bounds__(256) k_join(Product g)
         for (u32 q = 0; q < 4; ++q) {
             if (col + q == row) v[q] += g.c_one;
             if (row >= g.rows || col + q >= g.rows) v[q] = 0.0f;
-            tile[r + 16 * h][c + q] = v[q];
+            tile[r][c + q] = v[q];
         }
         if (row < g.rows && col < S::padded(g.rows)) S::put(out + (u64)row * row_out, col, v);
     }
     if (ti == tj) return;
     __syncthreads();
-#pragma unroll
-    for (u32 h = 0; h < 4; ++h) {
-        const u32 row = tj * kSide + r + 16 * h, col = ti * kSide + c;
-        if (row < g.rows)
-            S::put(out + (u64)row * row_out, col, f32x4{tile[c][r + 16 * h], tile[c + 1][r + 16 * h], tile[c + 2][r + 16 * h], tile[c + 3][r + 16 * h]});
-    }
+    const u32 row = tj * kSide + r, col = ti * kSide + c;
+    if (row < g.rows) S::put(out + (u64)row * row_out, col, f32x4{tile[c][r], tile[c + 1][r], tile[c + 2][r], tile[c + 3][r]});
 }
 
 // ---- matrices with a side of up to 64: one launch for a step ---------------------
@@ -996,7 +993,7 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
         if (const int rc = launch<kOf, kPart>(g, members, gram.edge, stream)) return rc;
         g.members = members;
         const u32 side = (m + kSide - 1) / kSide;
-        k_join<kOf><<<dim3(side * (side + 1) / 2, members), 256, 0, stream>>>(g);
+        k_join<kOf><<<dim3(side * (side + 1) / 2, members), kJoinThreads, 0, stream>>>(g);
         return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_EHIP;
     };
     // to = c left right + d old + e I, of matrices that commute and are symmetric
