@@ -382,7 +382,7 @@ int rtopk_linear_i8_backward(const void *dy, const void *x, int type,
  * rows, cols  1 .. 2^21, rows * cols < 2^32
  * coefficients  HOST, [steps][3], 1 <= steps <= 64, read during the call. If
  *        singular values s that start in [0, 1] can pass 7.5 (or a + b s^2 +
- *        c s^4 can pass 60), the call returns RTOPK_EINVAL
+ *        c s^4 can pass 30), the call returns RTOPK_EINVAL
  * eps    >= 0. A matrix of zeros gives zeros (eps = 0 too); one that holds an
  *        infinity or a not-a-number gives NaN everywhere
  * workspace  device, 256-byte aligned, >= rtopk_orthogonalize_workspace_bytes

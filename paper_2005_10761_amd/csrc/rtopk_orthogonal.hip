@@ -5,16 +5,20 @@
 //   each step, with coefficients (a, b, c):
 //     A = X X^T,  X <- (a I + b A + c A A) X
 //
-// as three products, with D = A - I in A's place:
-//     D = X X^T - I,  P = (a + b + c) I + (b + 2 c) D + c D D,  X <- P X.
-// Once the singular values are near 1, a, b A and c A A cancel (3.4, -4.8 and
-// 2.0 leave 0.7) and what A and B lost in rounding does not; D is small there,
-// and P has what is left of the cancellation, so that the result keeps its digits
-// (halves, a batch of 256 x 2304: relative error 14 10^-4 with A, B and a X + B X, see below for D and P).
+// as three products around a multiple of the identity that is near A's diagonal
+// (h; k is what the polynomial a + b h + c h^2 is there):
+//     D = X X^T - h I,  Q = (b + 2 c h) D + c D D,  X <- k X + Q X.
+// What is stored rounded, D and Q, is small where A and the polynomial are
+// mostly their diagonals: in the first steps, where A is nothing but small
+// (h = 0 would do), and in the last ones, where a, b A and c A A cancel (3.4, -4.8
+// and 2.0 leave 0.7; h = 1 would do). h is what the diagonal of A becomes if all
+// singular values are alike: 1 / m, and from step to step h (a + b h + c h^2)^2. It only
+// decides what the roundings are: halves, 256 x 2304, relative error of the result 13 10^-4 with
+// h = 0 and the polynomial itself in Q's place, 16 with h = 1, 7.5 so. With pairs, k goes into Q (k X is not read then).
 //
 // All three products have both operands' rows along the contraction: D's rows
-// and P's are its columns too, and X is kept twice, as it is and turned over
-// (the product that makes a new X writes both). D and P are symmetric: only
+// and Q's are its columns too, and X is kept twice, as it is and turned over
+// (the product that makes a new X writes both). D and Q are symmetric: only
 // tiles on and above the diagonal are computed, and written on both sides.
 //
 // Numbers between the products are halves (11 bits; bfloat16, in common use
@@ -35,10 +39,10 @@
 
 namespace rtopk {
 
-// powers of two that X, D and P are stored with: singular values of X up to kMostX, entries of D up to its square,
-// entries of P up to kMostP stay finite
+// powers of two that X, D and Q are stored with: singular values of X up to kMostX, entries of D up to its square,
+// entries of Q up to kMostP (or, less k, its double) stay finite
 constexpr int kLogX = 12, kLogD = 10;
-constexpr double kMostX = 7.5, kMostP = 60.0;
+constexpr double kMostX = 7.5, kMostP = 30.0;
 constexpr u32 kMembers = 16;            // matrices in one launch
 
 struct Members { void *p[kMembers]; };
@@ -283,7 +287,7 @@ struct Product {
     u32 tiles_m, tiles_n, tiles;            // tiles: of one matrix
     unsigned char *out, *turned;            // the result, and turned over
     u64 out_stride, turned_stride;
-    // kSymmetric: result = c_sum rho^2 product + c_old old + c_one I; kNext, kLast: c_sum rho product
+    // kSymmetric: result = c_sum rho^2 product + c_old old + c_one I; kNext, kLast: (c_sum product + c_old old) rho
     float c_sum, c_old, c_one;
     const unsigned char *old;               // laid out as the result, or null
     const float *rho;                       // first step only, else null
@@ -324,7 +328,7 @@ __global__ void __launch_bounds__(T::kThreads) k_step(Product g)
     const u32 row_out = S::row_bytes(g.cols), row_turned = S::row_bytes(g.rows);
     T t;
     t.clear();
-    if (kStep == kSymmetric && g.old) {
+    if (kStep != kPart && g.old) {
         // the old matrix's part goes into the sums first: its loads are under way together (after the products, between the
         // stores, each is waited for: 95 us for 4096 x 4096, 72 without it)
         const unsigned char *old = g.old + member * g.out_stride;
@@ -509,7 +513,7 @@ struct Narrow {
     const float *part;          // [members][runs][64][64], read
     float *part_next;           // written
     u32 runs, blocks_each;
-    float c_gram, c_sum, c_old, c_one;
+    float c_gram, shift, c_sum, c_old, c_one, c_x;      // D = c_gram X X^T - shift; Q = c_sum D D + c_old D + c_one; X <- Q X + c_x X
     bool first, last;
     Members to;                 // the result
     int to_type;
@@ -651,7 +655,7 @@ __global__ void __launch_bounds__(kNormThreads) k_narrow(Narrow g)
             f32x4 v = sum[q] * scale;
 #pragma unroll
             for (u32 i = 0; i < 4; ++i)
-                if (c + 4 * q + i == r && r < m) v[i] -= (float)(1 << kLogD);
+                if (c + 4 * q + i == r && r < m) v[i] -= g.shift;
             B::put(lds[0], r, c + 4 * q, v);
         }
     }
@@ -683,6 +687,15 @@ __global__ void __launch_bounds__(kNormThreads) k_narrow(Narrow g)
         if (b + 1 < g.blocks_each) load(held, n0 + kSide);
         T t;
         t.clear();
+        if (kOf == kHalves) {           // (the part of X itself: X turned over holds it)
+#pragma unroll
+            for (int i = 0; i < T::kFragsM; ++i)
+#pragma unroll
+                for (int j = 0; j < T::kFragsN; ++j)
+#pragma unroll
+                    for (u32 q = 0; q < 4; ++q)
+                        t.sum[i][j][q] = g.c_x * (float)*(const _Float16 *)B::at(lds[2], T::col_at(j) + q, S::at(T::row_at(i)));
+        }
         B::multiply(t, lds[1], lds[2]);
         if (g.last) {
             void *to = g.to.p[member];
@@ -906,6 +919,12 @@ struct Target {
     int update;
 };
 
+// A step's polynomial a + b x + c x^2 around h, and h for the next step.
+struct Around {
+    double c, slope, value, next;
+    Around(const float *k, double h) : c(k[2]), slope(k[1] + 2.0 * k[2] * h), value(k[0] + h * (k[1] + h * k[2])), next(h * value * value) {}
+};
+
 template <Operands kOf>
 int iterate_narrow(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 norm_parts, u32 steps, const float *abc, float eps,
                    const Parts &p, const Target &target, hipStream_t stream)
@@ -938,15 +957,19 @@ int iterate_narrow(const Members &x, int type, u64 ldx, const Shape &s, u32 memb
     g.update = target.update;
     k_narrow_start<kOf><<<grid, kNormThreads, 0, stream>>>(g);
     if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
+    double h = 1.0 / s.m();
     for (u32 i = 0; i < steps; ++i) {
-        const double a = abc[3 * i], b = abc[3 * i + 1], c = abc[3 * i + 2];
+        const Around at(abc + 3 * i, h);
         g.xt = p.xt[i & 1];
         g.xt_next = p.xt[1 - (i & 1)];
         g.part = part[i & 1];
         g.part_next = part[1 - (i & 1)];
-        g.c_sum = (float)(c * ldexp(1.0, -kLogD));
-        g.c_old = (float)(b + 2.0 * c);
-        g.c_one = (float)((a + b + c) * ldexp(1.0, kLogD));
+        g.shift = (float)(h * ldexp(1.0, kLogD));
+        g.c_sum = (float)(at.c * ldexp(1.0, -kLogD));
+        g.c_old = (float)at.slope;
+        g.c_one = kOf == kPairs ? (float)(at.value * ldexp(1.0, kLogD)) : 0.0f;
+        g.c_x = kOf == kPairs ? 0.0f : (float)(at.value * ldexp(1.0, kLogD));
+        h = at.next;
         g.first = i == 0;
         g.last = i + 1 == steps;
         k_narrow<kOf><<<grid, kNormThreads, 0, stream>>>(g);
@@ -974,8 +997,8 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
     const u32 square_edge = best_edge<kOf>(true, m, m, members, square_slices, &square_cost);
     const u32 next_edge = best_edge<kOf>(false, m, n, members, square_slices, &next_cost);
 
-    // X X^T - I (the first step's X still lacks rho)
-    auto make_gram = [&](const unsigned char *x_now, unsigned char *to, const float *rho) -> int {
+    // X X^T - h I (the first step's X still lacks rho)
+    auto make_gram = [&](const unsigned char *x_now, unsigned char *to, double h, const float *rho) -> int {
         Product g{};
         g.left = g.right = x_now;
         g.left_stride = g.right_stride = p.x_stride;
@@ -984,7 +1007,7 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
         g.out = g.turned = to;
         g.out_stride = g.turned_stride = p.square_stride;
         g.c_sum = ldexpf(1.0f, kLogD - 2 * kLogX);
-        g.c_one = -ldexpf(1.0f, kLogD);
+        g.c_one = (float)(-h * ldexp(1.0, kLogD));
         g.rho = rho;
         if (gram.splits == 1) return launch<kOf, kSymmetric>(g, members, gram.edge, stream);
         g.part = p.part;
@@ -1015,30 +1038,36 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
         return launch<kOf, kSymmetric>(g, members, square_edge, stream);
     };
     unsigned char *const *q = p.square;
-    auto make_poly = [&](const unsigned char *d, unsigned char *to, const float *k) -> int {
-        const double a = k[0], b = k[1], c = k[2];
-        return make_square(d, d, d, to, c, b + 2.0 * c, a + b + c);
+    // Q from D; with pairs the whole polynomial
+    auto make_poly = [&](const unsigned char *d, unsigned char *to, const Around &at) -> int {
+        return make_square(d, d, d, to, at.c, at.slope, kOf == kPairs ? at.value : 0.0);
     };
-    // Two steps at a time: from D and P of the first, X X^T of the second is P (D + I) P without X, and both polynomials
-    // go to X as one. Three more products of m x m, X X^T and P X once less: where X is long. With pairs only (the second D
-    // carries the first one's roundings, twelve times larger, to where the singular values are small), and not with
-    // coefficients that make P large.
+    // Two steps at a time: from D and P of the first, X X^T of the second is P (D + h I) P without X, and both polynomials
+    // go to X as one. Three more products of m x m, X X^T and P X once less: where X is long. With pairs only, and not with
+    // coefficients that make P large: the second D takes up the first one's roundings, up to P^2 times larger (1500 x 6000:
+    // relative error 2.2 10^-6, one step at a time 1.2, a plain binary32 iteration 2.1; with h = 1 it would be 24).
     const bool twos = kOf == kPairs && largest_p <= 4.0 && gram_cost + next_cost > 1.05 * 3.0 * square_cost;
     u32 now = 0;
+    double h = 1.0 / m;
     for (u32 i = 0; i < steps;) {
         const unsigned char *x_now = p.x[now], *xt_now = p.xt[now];
         const float *rho = i == 0 ? p.rho : nullptr;
-        if (const int rc = make_gram(x_now, q[0], rho)) return rc;
-        if (const int rc = make_poly(q[0], q[1], abc + 3 * i)) return rc;
+        const Around at(abc + 3 * i, h);
+        if (const int rc = make_gram(x_now, q[0], h, rho)) return rc;
+        if (const int rc = make_poly(q[0], q[1], at)) return rc;
         unsigned char *poly = q[1];
         u32 did = 1;
         if (twos && i + 1 < steps) {
+            const Around second(abc + 3 * (i + 1), at.next);
             if (const int rc = make_square(q[1], q[1], nullptr, q[2], 1.0, 0.0, 0.0)) return rc;            // E = P P
-            if (const int rc = make_square(q[0], q[2], q[2], q[3], 1.0, 1.0, -1.0)) return rc;              // D E + E - I
-            if (const int rc = make_poly(q[3], q[0], abc + 3 * (i + 1))) return rc;
+            if (const int rc = make_square(q[0], q[2], q[2], q[3], 1.0, h, -at.next)) return rc;            // D E + h E - h' I
+            if (const int rc = make_poly(q[3], q[0], second)) return rc;
             if (const int rc = make_square(q[0], q[1], nullptr, q[2], 1.0, 0.0, 0.0)) return rc;            // both polynomials
             poly = q[2];
             did = 2;
+            h = second.next;
+        } else {
+            h = at.next;
         }
         i += did;
         Product g{};
@@ -1056,6 +1085,10 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
             g.out_stride = p.x_stride;
             g.turned_stride = p.xt_stride;
             g.c_sum = ldexpf(1.0f, -kLogD);
+            if (kOf == kHalves) {
+                g.old = x_now;
+                g.c_old = (float)at.value;
+            }
             if (const int rc = launch<kOf, kNext>(g, members, next_edge, stream)) return rc;
             continue;
         }
@@ -1068,6 +1101,11 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
         g.cols = s.cols;
         g.inner = m;
         g.c_sum = ldexpf(1.0f, -kLogD - kLogX);
+        if (kOf == kHalves) {
+            g.old = s.over() ? xt_now : x_now;
+            g.out_stride = s.over() ? p.xt_stride : p.x_stride;
+            g.c_old = (float)(at.value * ldexp(1.0, -kLogX));
+        }
         g.to = target.to;
         g.type = target.type;
         g.ldo = target.ld;
