@@ -694,9 +694,9 @@ int run_product(Scaled g, void *part, hipStream_t stream)
     g.part = (int *)part;
     const bool whole = (((uintptr_t)g.a | (uintptr_t)g.b | g.lda | g.ldb) & 15u) == 0;
     if (p.edge == 256) launch_product<256, 2, 4, 2, true>(g, p, whole, stream);
-    else if (p.edge == 192) launch_product<192, 2, 4, 2, true>(g, p, whole, stream);
-    else if (p.edge == 128) launch_product<128, 2, 2, 2, false>(g, p, whole, stream);
-    else launch_product<64, 2, 2, 3, false>(g, p, whole, stream);
+    else if (p.edge == 192) launch_product<192, 2, 4, 3, true>(g, p, whole, stream);
+    else if (p.edge == 128) launch_product<128, 2, 4, 2, true>(g, p, whole, stream);
+    else launch_product<64, 2, 4, 3, true>(g, p, whole, stream);
     if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
     if (p.splits > 1) {
         const u64 blocks = ((u64)g.m * ((g.n + 3) / 4) + 255) / 256;

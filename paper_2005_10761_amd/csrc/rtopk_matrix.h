@@ -92,7 +92,7 @@ struct Tile {
     static constexpr int kLoadsM = kM / 8 / kWaves, kLoadsN = kN / 8 / kWaves, kLoads = kLoadsM + kLoadsN;
     static_assert(kLoadsM * kWaves * 8 == kM && kLoadsN * kWaves * 8 == kN, "every wavefront loads whole groups of eight rows");
     static_assert(kFragsM * kWavesM * 16 == kM && kFragsN * kWavesN * 16 == kN, "whole instructions");
-    static_assert(kStages >= 2 && (!kAhead || kStages == 2), "one slice under way at least");
+    static_assert(kStages >= 2, "one slice under way at least");
     typedef typename Sums<kOf>::type Sum;
     // sum[i][j]: row row_at(i) of A, rows col_at(j) .. + 3 of B
     Sum sum[kFragsM][kFragsN];
@@ -203,41 +203,35 @@ struct Tile {
             };
             load(s);
             if constexpr (kAhead) {
-                if (s + 1 < whole) {
-                    load(s + 1);
-                    wait_and_meet<kLoads>();
-                } else {
-                    wait_and_meet<0>();
-                }
+#pragma unroll
+                for (int q = 1; q < kStages; ++q)
+                    if (s + q < whole) load(s + q);
+                if (s + kStages <= whole) wait_and_meet<(kStages - 1) * kLoads>();
+                else wait_and_meet<0>();
                 Half first, second;
                 read(first, lds, 0);
                 // (three copies of a slice's work, so that none of them branches: a branch stops the reads from going between the products)
-                for (; s + 2 < whole; ++s) {
-                    read(second, lds + ((s - from) & 1u) * kStage, 1);
+                for (; s + kStages < whole; ++s) {
+                    read(second, lds + (s - from) % kStages * kStage, 1);
                     add(first, first);
                     mix<0>();
                     // this wavefront has read all of slice s, and its part of slice s + 1 has come; after the barrier
                     // that holds for everybody: the stage of slice s may be overwritten, that of s + 1 read
-                    wait_and_meet<0>();
-                    load(s + 2);
-                    read(first, lds + ((s + 1 - from) & 1u) * kStage, 0);
-                    add(second, second);
-                    mix<kLoads>();
+                    wait_and_meet<(kStages - 2) * kLoads>();
+                    load(s + kStages);
+                    ahead<kLoads>(first, second, lds + (s + 1 - from) % kStages * kStage);
                 }
-                if (s + 1 < whole) {
-                    read(second, lds + ((s - from) & 1u) * kStage, 1);
+                for (; s + 1 < whole; ++s) {
+                    read(second, lds + (s - from) % kStages * kStage, 1);
                     add(first, first);
                     mix<0>();
                     wait_and_meet<0>();
-                    ++s;
-                    read(first, lds + ((s - from) & 1u) * kStage, 0);
-                    add(second, second);
-                    mix<0>();
+                    ahead<0>(first, second, lds + (s + 1 - from) % kStages * kStage);
                 }
-                read(second, lds + ((s - from) & 1u) * kStage, 1);
+                read(second, lds + (s - from) % kStages * kStage, 1);
                 add(first, first);
                 mix<0>();
-                add(second, second);
+                rest(first, second);
                 ++s;
             } else {
 #pragma unroll
@@ -293,14 +287,8 @@ struct Tile {
         Half first, second;
         read(first, stage_a, stage_b, 0);
         read(second, stage_a, stage_b, 1);
-        if (kOf == kPairs) {
-            add(first, first);
-            add(second, first);
-            add(first, second);
-        } else {
-            add(first, first);
-            add(second, second);
-        }
+        add(first, first);
+        rest(first, second);
     }
 
     __device__ __forceinline__ void add(const Half &a, const Half &b)
@@ -317,11 +305,38 @@ struct Tile {
             }
     }
 
+    // what is left to do with a slice once its first half's own products are done
+    __device__ __forceinline__ void rest(const Half &first, const Half &second)
+    {
+        if (kOf == kPairs) {
+            add(second, first);
+            add(first, second);
+        } else {
+            add(second, second);
+        }
+    }
+    // that, while the next slice's first half is read
+    template <int kOfLoads>
+    __device__ __forceinline__ void ahead(Half &first, const Half &second, const unsigned char *next)
+    {
+        if constexpr (kOf == kPairs) {
+            Half after;
+            read(after, next, 0);
+            rest(first, second);
+            mix<kOfLoads>();
+            first = after;
+        } else {
+            read(first, next, 0);
+            rest(first, second);
+            mix<kOfLoads>();
+        }
+    }
+
     // the reads of one half, and loads to LDS, between the products of the other
     template <int kOfLoads>
     __device__ __forceinline__ void mix() const
     {
-        constexpr int kReads = kFragsM + kFragsN, kProducts = kFragsM * kFragsN / (kReads + kOfLoads);
+        constexpr int kReads = kFragsM + kFragsN, kPer = kFragsM * kFragsN / (kReads + kOfLoads), kProducts = kPer ? kPer : 1;
 #pragma unroll
         for (int q = 0; q < kReads; ++q) {
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // a read from LDS

@@ -510,8 +510,9 @@ struct Narrow {
     const u8 *xt;               // [members][n] rows of m, k_narrow: read
     u8 *xt_next;                // written
     u64 xt_stride;
-    const float *part;          // [members][runs][64][64], read
-    float *part_next;           // written
+    const float *part;          // [members][runs][64][64], read; or, joined, [members][64][64]
+    float *part_next;           // [members][runs][64][64], written
+    float *joined;              // [members][64][64], or null
     u32 runs, blocks_each;
     float c_gram, shift, c_sum, c_old, c_one, c_x;      // D = c_gram X X^T - shift; Q = c_sum D D + c_old D + c_one; X <- Q X + c_x X
     bool first, last;
@@ -613,6 +614,24 @@ __global__ void __launch_bounds__(kNormThreads) k_narrow_start(Narrow g)
     write_part(gram, g.part_next + ((u64)member * g.runs + run) * kSide * kSide);
 }
 
+// Many runs' parts together, by themselves (every workgroup of a step reading 27 of them took 10 us of its 25): sixteen
+// groups of sixteen threads each add up every sixteenth part of 64 sums, then the groups in order.
+__global__ void __launch_bounds__(256) k_narrow_join(Narrow g)
+{
+    __shared__ f32x4 part[16][16];
+    const u32 group = threadIdx.x >> 4, at = blockIdx.x * 16u + (threadIdx.x & 15u), member = blockIdx.y;
+    const f32x4 *p = (const f32x4 *)(g.part + (u64)member * g.runs * kSide * kSide) + at;
+    f32x4 sum{0, 0, 0, 0};
+#pragma unroll 8
+    for (u32 s = group; s < g.runs; s += 16) sum += p[s * (kSide * kSide / 4)];
+    part[group][threadIdx.x & 15u] = sum;
+    __syncthreads();
+    if (group) return;
+#pragma unroll
+    for (u32 s = 1; s < 16; ++s) sum += part[s][threadIdx.x];
+    ((f32x4 *)(g.joined + (u64)member * kSide * kSide))[at] = sum;
+}
+
 template <Operands kOf>
 __global__ void __launch_bounds__(kNormThreads) k_narrow(Narrow g)
 {
@@ -643,10 +662,11 @@ __global__ void __launch_bounds__(kNormThreads) k_narrow(Narrow g)
     {
         // D
         const u32 r = threadIdx.x >> 2, c = (threadIdx.x & 3u) * 16u;
-        const float *part = g.part + (u64)member * g.runs * kSide * kSide + r * kSide + c;
+        const u32 runs = g.joined ? 1u : g.runs;
+        const float *part = (g.joined ? g.joined : g.part) + (u64)member * runs * kSide * kSide + r * kSide + c;
         f32x4 sum[4] = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll 4
-        for (u32 s = 0; s < g.runs; ++s)
+        for (u32 s = 0; s < runs; ++s)
 #pragma unroll
             for (int q = 0; q < 4; ++q) sum[q] += *(const f32x4 *)(part + s * kSide * kSide + 4 * q);
         const float scale = g.c_gram * rho * rho;
@@ -791,23 +811,27 @@ GramPlan plan_gram(u32 members, const Shape &s, double *cost)
     return best;
 }
 
-// A side of up to 64: the long side's blocks of 64 in so many runs. A workgroup reads every run's part and makes its own
-// run's blocks: 0.27 us for a run and 1.2 for a block, least where the runs are the root of 4.4 times the blocks.
+// A side of up to 64: the long side's blocks of 64 in so many runs. Up to kFewRuns of them are added up by every workgroup of
+// the next step; beyond, a launch does it, and there are as many runs as fill the chip. us a step, five blocks / nine /
+// 79 / 157: every workgroup for itself 9 / 9 / 20 / 25, a launch 13 / 13 / 13 / 14.
+constexpr u32 kFewRuns = 16;
 struct NarrowPlan {
     u32 runs, blocks_each;
+    bool join;
 };
-NarrowPlan plan_narrow(const Shape &s)
+NarrowPlan plan_narrow(const Shape &s, u32 members)
 {
     const u32 blocks = (s.n() + kSide - 1) / kSide;
-    const u32 runs = std::min(blocks, std::max(16u, (u32)std::ceil(std::sqrt(4.4 * blocks))));
-    const u32 each = (blocks + runs - 1) / runs;
-    return NarrowPlan{(blocks + each - 1) / each, each};
+    const u32 most = std::max(kFewRuns, 2 * kUnits / members);
+    const u32 each = blocks <= 2 * kFewRuns ? (blocks + kFewRuns - 1) / kFewRuns : (blocks + most - 1) / most;
+    const u32 runs = (blocks + each - 1) / each;
+    return NarrowPlan{runs, each, runs > kFewRuns};
 }
 bool is_narrow(const Shape &s) { return s.m() <= kSide; }
 
 struct Parts {
     double *norm;
-    float *rho, *average, *part;
+    float *rho, *average, *part, *joined;
     unsigned char *x[2], *xt[2], *square[4];
     u64 x_stride, xt_stride, square_stride;
 };
@@ -827,7 +851,11 @@ u64 cut(void *base, u32 count, const Shape &s, bool average, Parts &p)
     p.rho = (float *)take(kMembers * sizeof(float));
     if (is_narrow(s)) {
         for (int i = 0; i < 2; ++i) p.xt[i] = take(members * p.xt_stride);
-        p.part = (float *)take(2ull * members * plan_narrow(s).runs * kSide * kSide * sizeof(float));
+        // (fewer matrices have more runs each, but not more in all than 2 * kUnits and what rounding up adds)
+        const u64 runs = std::max((u64)members * plan_narrow(s, members).runs,
+                                  count > kMembers && count % kMembers ? (u64)(count % kMembers) * plan_narrow(s, count % kMembers).runs : 0);
+        p.part = (float *)take(2 * runs * kSide * kSide * sizeof(float));
+        p.joined = (float *)take((u64)members * kSide * kSide * sizeof(float));
         p.average = average ? (float *)take(members * align_up((u64)s.rows * s.cols, 64) * sizeof(float)) : nullptr;
         return used;
     }
@@ -903,12 +931,11 @@ template <Operands kOf, Step kStep>
 int launch(const Product &g, u32 members, u32 edge, hipStream_t stream)
 {
     // eight columns a lane where halves are stored; four where binary32 is (a fragment's 64 bytes of a row)
-    constexpr bool kAhead = kOf != kPairs;
     constexpr Deal kDeal = kStep == kPart || (kStep == kLast && kOf == kPairs) ? kRuns : kWide;
-    if (edge == 256) return launch<kOf, Tile<kOf, 256, 256, 2, 4, 2, kAhead, kDeal>, kStep>(g, members, stream);
-    if (edge == 192) return launch<kOf, Tile<kOf, 192, 192, 2, 4, 2, kAhead, kDeal>, kStep>(g, members, stream);
-    if (edge == 128) return launch<kOf, Tile<kOf, 128, 128, 2, 2, 2, false, kDeal>, kStep>(g, members, stream);
-    return launch<kOf, Tile<kOf, 64, 64, 2, 2, 3, false, kDeal>, kStep>(g, members, stream);
+    if (edge == 256) return launch<kOf, Tile<kOf, 256, 256, 2, 4, 2, kOf != kPairs, kDeal>, kStep>(g, members, stream);
+    if (edge == 192) return launch<kOf, Tile<kOf, 192, 192, 2, 4, 3, true, kDeal>, kStep>(g, members, stream);
+    if (edge == 128) return launch<kOf, Tile<kOf, 128, 128, 2, 4, 2, true, kDeal>, kStep>(g, members, stream);
+    return launch<kOf, Tile<kOf, 64, 64, 2, 4, 3, true, kDeal>, kStep>(g, members, stream);
 }
 
 struct Target {
@@ -929,7 +956,7 @@ template <Operands kOf>
 int iterate_narrow(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 norm_parts, u32 steps, const float *abc, float eps,
                    const Parts &p, const Target &target, hipStream_t stream)
 {
-    const NarrowPlan plan = plan_narrow(s);
+    const NarrowPlan plan = plan_narrow(s, members);
     const dim3 grid(plan.runs, members);
     float *part[2] = {p.part, p.part + (u64)members * plan.runs * kSide * kSide};
     Narrow g{};
@@ -947,6 +974,7 @@ int iterate_narrow(const Members &x, int type, u64 ldx, const Shape &s, u32 memb
     g.blocks_each = plan.blocks_each;
     g.xt_next = p.xt[0];
     g.part_next = part[0];
+    g.joined = plan.join ? p.joined : nullptr;
     g.c_gram = ldexpf(1.0f, kLogD - 2 * kLogX);
     g.c_last = ldexpf(1.0f, -kLogD - kLogX);
     g.to = target.to;
@@ -972,6 +1000,10 @@ int iterate_narrow(const Members &x, int type, u64 ldx, const Shape &s, u32 memb
         h = at.next;
         g.first = i == 0;
         g.last = i + 1 == steps;
+        if (plan.join) {
+            k_narrow_join<<<dim3(kSide * kSide / 64, members), 256, 0, stream>>>(g);
+            if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
+        }
         k_narrow<kOf><<<grid, kNormThreads, 0, stream>>>(g);
         if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
     }
