@@ -175,11 +175,20 @@ struct Tile {
     // but a last one that goes beyond `bytes` goes to LDS by loads that pass the registers by, the next one under way
     // while this one is multiplied. The slice that goes beyond, and every slice of rows that start anywhere, comes through
     // registers, where what lies beyond `bytes` is not read and counts as zero.
+    // prepare(): what else the sums wait for (the sums' first values from memory), called once the first slices are on their way.
     template <bool kWhole>
     __device__ __forceinline__ void multiply(const TileRows &a, const TileRows &b, u32 from, u32 to, unsigned char *lds)
     {
+        multiply<kWhole>(a, b, from, to, lds, [] {});
+    }
+    template <bool kWhole, class Prepare>
+    __device__ __forceinline__ void multiply(const TileRows &a, const TileRows &b, u32 from, u32 to, unsigned char *lds, Prepare prepare)
+    {
 #if defined(__HIP_DEVICE_COMPILE__)      // (the host pass does not know the buffer instructions)
-        if (from >= to) return;
+        if (from >= to) {
+            prepare();
+            return;
+        }
         const u32 whole = kWhole ? (a.bytes / kSlice < to ? a.bytes / kSlice : to) : from;
         u32 s = from;
         if (kWhole && s < whole) {
@@ -206,6 +215,7 @@ struct Tile {
 #pragma unroll
                 for (int q = 1; q < kStages; ++q)
                     if (s + q < whole) load(s + q);
+                prepare();
                 if (s + kStages <= whole) wait_and_meet<(kStages - 1) * kLoads>();
                 else wait_and_meet<0>();
                 Half first, second;
@@ -237,6 +247,7 @@ struct Tile {
 #pragma unroll
                 for (int q = 1; q < kStages - 1; ++q)
                     if (s + q < whole) load(s + q);
+                prepare();
                 for (; s < whole; ++s) {
                     // this wavefront's part of slice s has come (those of the kStages - 2 after it may be on their way); after
                     // the barrier everybody's has, and nobody reads the stage of slice s - 1
@@ -247,6 +258,7 @@ struct Tile {
                 }
             }
         }
+        if (s == from) prepare();
         for (; s < to; ++s) {
             unsigned char *stage = lds + (s - from) % kStages * kStage;
             i32x4 piece[kLoads];

@@ -128,6 +128,18 @@ template <Operands kOf> struct Stored {
         }
         return v;
     }
+    // eight neighbours from a multiple of eight on
+    static __device__ __forceinline__ void get_eight(f32x4 &a, f32x4 &b, const unsigned char *row, u32 col)
+    {
+        const f16x8 hi = *(const f16x8 *)(row + at(col));
+        f16x8 lo{0, 0, 0, 0, 0, 0, 0, 0};
+        if (kOf == kPairs) lo = *(const f16x8 *)(row + at(col) + 64);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            a[c] = (float)hi[c] + (float)lo[c];
+            b[c] = (float)hi[4 + c] + (float)lo[4 + c];
+        }
+    }
 };
 
 // ---- the norm ---------------------------------------------------------------
@@ -328,20 +340,29 @@ __global__ void __launch_bounds__(T::kThreads) k_step(Product g)
     const u32 row_out = S::row_bytes(g.cols), row_turned = S::row_bytes(g.rows);
     T t;
     t.clear();
-    if (kStep != kPart && g.old) {
-        // the old matrix's part goes into the sums first: its loads are under way together (after the products, between the
-        // stores, each is waited for: 95 us for 4096 x 4096, 72 without it)
+    const u32 from = kStep == kPart ? split * g.slices_each : 0u;
+    t.template multiply<true>(a, b, from, kStep == kPart ? min(from + g.slices_each, slices) : slices, lds, [&] {
+        if (kStep == kPart || !g.old) return;
+        // the old matrix's part goes into the sums first: its loads are under way together, and with the first slices (after the
+        // products, between the stores, each would be waited for: 95 us for 4096 x 4096, 72 without it; and so they are where a
+        // branch stands around each: what lies beyond the matrix is read from its edge, and not stored)
         const unsigned char *old = g.old + member * g.out_stride;
         const float ratio = g.c_old / g.c_sum;
 #pragma unroll
+        for (int i = 0; i < T::kFragsM; ++i) {
+            const unsigned char *row = old + (u64)min(i0 + T::row_at(i), g.rows - 1u) * row_out;
+            constexpr int kPaired = T::wide_at(0) ? T::kFragsN / 2 * 2 : 0;
+#pragma unroll
+            for (int j = 0; j < kPaired; j += 2)
+                S::get_eight(t.sum[i][j], t.sum[i][T::next_to(j)], row, min(j0 + T::col_at(j), S::padded(g.cols) - 8u));
+#pragma unroll
+            for (int j = kPaired; j < T::kFragsN; ++j) t.sum[i][j] = S::get(row, min(j0 + T::col_at(j), S::padded(g.cols) - 4u));
+        }
+#pragma unroll
         for (int i = 0; i < T::kFragsM; ++i)
 #pragma unroll
-            for (int j = 0; j < T::kFragsN; ++j)
-                if (i0 + T::row_at(i) < g.rows && j0 + T::col_at(j) < S::padded(g.cols))
-                    t.sum[i][j] = ratio * S::get(old + (u64)(i0 + T::row_at(i)) * row_out, j0 + T::col_at(j));
-    }
-    const u32 from = kStep == kPart ? split * g.slices_each : 0u;
-    t.template multiply<true>(a, b, from, kStep == kPart ? min(from + g.slices_each, slices) : slices, lds);
+            for (int j = 0; j < T::kFragsN; ++j) t.sum[i][j] *= ratio;
+    });
 
     if constexpr (kStep == kPart) {
         const u64 ld = align_up(g.rows, 4);
@@ -357,29 +378,36 @@ __global__ void __launch_bounds__(T::kThreads) k_step(Product g)
         void *to = g.to.p[member];
         const u32 size = g.type == 0 ? 4u : 2u;
         const bool wide = (((uintptr_t)to | (g.ldo * size)) & (4u * size - 1u)) == 0;
+        // the old weights of a row of fragments, on their way while the row before is stored; without a branch, as above
+        f32x4 w[2][T::kFragsN];
+        const bool all_fours = wide && g.cols >= 4u;
+        auto weights = [&](f32x4 (&to_w)[T::kFragsN], int i) {
+            const float *row = (const float *)to + (u64)min(i0 + T::row_at(i), g.rows - 1u) * g.ldo;
+            if (all_fours) {
+#pragma unroll
+                for (int j = 0; j < T::kFragsN; ++j) to_w[j] = *(const f32x4 *)(row + min(j0 + T::col_at(j), (g.cols - 4u) & ~3u));
+            }
+#pragma unroll
+            for (int j = 0; j < T::kFragsN; ++j) {
+                const u32 col = j0 + T::col_at(j);
+                if (col < g.cols && (!all_fours || col + 4u > g.cols))
+#pragma unroll
+                    for (u32 q = 0; q < 4; ++q) to_w[j][q] = col + q < g.cols ? row[col + q] : 0.0f;
+            }
+        };
+        if (g.update) weights(w[0], 0);
 #pragma unroll
         for (int i = 0; i < T::kFragsM; ++i) {
             const u32 row = i0 + T::row_at(i);
+            if (g.update && i + 1 < T::kFragsM) weights(w[(i + 1) & 1], i + 1 < T::kFragsM ? i + 1 : i);
             if (row >= g.rows) continue;
             const u64 first = (u64)row * g.ldo;
-            f32x4 w[T::kFragsN];                // (a row of fragments' old weights at a time, for the same reason)
-            if (g.update) {
-#pragma unroll
-                for (int j = 0; j < T::kFragsN; ++j) {
-                    const u32 col = j0 + T::col_at(j);
-                    const float *from_w = (const float *)to + first + col;
-                    if (wide && col + 4u <= g.cols) w[j] = *(const f32x4 *)from_w;
-                    else
-#pragma unroll
-                        for (u32 q = 0; q < 4; ++q) w[j][q] = col + q < g.cols ? from_w[q] : 0.0f;
-                }
-            }
 #pragma unroll
             for (int j = 0; j < T::kFragsN; ++j) {
                 t.sum[i][j] *= c_sum;
                 if (g.update)
 #pragma unroll
-                    for (u32 q = 0; q < 4; ++q) t.sum[i][j][q] = fmaf(g.gain, t.sum[i][j][q], g.keep * w[j][q]);
+                    for (u32 q = 0; q < 4; ++q) t.sum[i][j][q] = fmaf(g.gain, t.sum[i][j][q], g.keep * w[i & 1][j][q]);
             }
             const bool eights = g.type != 0 && (((uintptr_t)to | (g.ldo * size)) & 15u) == 0;
 #pragma unroll
