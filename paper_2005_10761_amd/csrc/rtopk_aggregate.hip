@@ -37,8 +37,10 @@
 // sparse messages take one kernel instead (k_weights), whose workgroups form
 // the sums in a hash table, whatever stretch of coordinates the entries span.
 #include "rtopk_common.h"
+#include "rtopk_direction.h"
 #include "../../include/rtopk.h"
 
+#include <algorithm>
 #include <mutex>
 
 namespace rtopk {
@@ -158,6 +160,87 @@ __device__ __forceinline__ u32 lane_left(u32 v, u32 first)
     return (u32)__builtin_amdgcn_update_dpp((int)first, (int)v, 0x138 /* wave_shr:1 */, 0xF, 0xF, false);
 }
 
+// The n messages' entries in [tile_base, tile_end), added in worker order into a wavefront's tile in LDS, which holds zeros.
+// groups: workers are taken 64 at a time; with one group, lane w's pos0 is where worker w's entries begin, and where
+// the next tile's begin afterwards.
+__device__ __forceinline__ void add_messages(float *tile, const u32 *__restrict__ idx, const float *__restrict__ val, u32 n, u64 k,
+                                             u64 tile_base, u64 tile_end, u32 groups, u64 &pos0)
+{
+    const u32 lane = lane_id();
+            for (u32 w0 = 0; w0 < n; w0 += kWave) {
+                const u32 nw = n - w0 < (u32)kWave ? n - w0 : (u32)kWave;
+                u64 lo = groups == 1 ? pos0 : wave_lower_bounds(idx, w0, nw, k, tile_base, 0, k);
+                // ---- worker after worker: the next 64 pairs of its message in one
+                //      coalesced load, those below the tile's end added into the tile;
+                //      the loads of kAggAhead workers are in flight together --------
+                for (u32 g0 = 0; g0 < nw; g0 += kAggAhead) {
+                    u64 from[kAggAhead];
+                    u32 ri[kAggAhead];
+                    float rv[kAggAhead];
+    #pragma unroll
+                    for (int q = 0; q < kAggAhead; ++q) {
+                        const u32 w = g0 + q < nw ? g0 + q : nw - 1;
+                        from[q] = read_lane_u64(lo, (int)w);
+                        const u64 j = from[q] + lane;
+                        const bool in = g0 + q < nw && j < k;
+                        ri[q] = in ? idx[(u64)(w0 + w) * k + j] : 0xFFFFFFFFu;
+                        rv[q] = in ? val[(u64)(w0 + w) * k + j] : 0.0f;
+                    }
+    #pragma unroll
+                    for (int q = 0; q < kAggAhead; ++q) {
+                        if (g0 + q >= nw) break;
+                        const u32 w = g0 + q;
+                        const u32 *si = idx + (u64)(w0 + w) * k;
+                        const float *sv = val + (u64)(w0 + w) * k;
+                        u64 at = from[q];
+                        // 64 pairs into the tile; returns how many of them lay inside it
+                        auto add_slice = [&](u32 i, float v) -> u32 {
+                            const bool inside = (u64)i < tile_end;     // 0xFFFFFFFF marks "no entry"
+                            const u64 mask = __ballot(inside);         // a prefix of the lanes: sorted
+                            // repeated indices inside one message (never produced by the
+                            // encoder, but allowed) must be added in position order
+                            const bool dup = inside && lane_left(i, 0xFFFFFFFFu) == i;
+                            if (__ballot(dup) == 0ull) {
+                                if (inside) tile[i - tile_base] += v;
+                            } else {
+                                for (u64 rest = mask; rest; rest &= rest - 1) {
+                                    const int src = __ffsll((unsigned long long)rest) - 1;
+                                    if ((int)lane == src) tile[i - tile_base] += v;
+                                }
+                            }
+                            return popc_mask(mask);
+                        };
+                        u32 took = add_slice(ri[q], rv[q]);
+                        at += took;
+                        // The slice filled all 64 lanes: the message is crowded here (its
+                        // entries cluster in a few tiles). The next kAggMore slices are
+                        // fetched together and added in order up to the first that ends
+                        // inside the tile.
+                        while (took == (u32)kWave) {
+                            u32 mi[kAggMore];
+                            float mv[kAggMore];
+    #pragma unroll
+                            for (int s2 = 0; s2 < kAggMore; ++s2) {
+                                const u64 j = at + (u64)s2 * kWave + lane;
+                                mi[s2] = j < k ? si[j] : 0xFFFFFFFFu;
+                                mv[s2] = j < k ? sv[j] : 0.0f;
+                            }
+    #pragma unroll
+                            for (int s2 = 0; s2 < kAggMore; ++s2) {
+                                if (took == (u32)kWave) {
+                                    took = add_slice(mi[s2], mv[s2]);
+                                    at += took;
+                                }
+                            }
+                        }
+                        // the new position of worker w goes back into lane w
+                        if (lane == w) lo = at;
+                    }
+                }
+                if (groups == 1) pos0 = lo;
+            }
+}
+
 // What the momentum form of the kernel does with the average of a coordinate:
 // u = scale * average, v <- fma(mu, v, u), w <- fma(neg_eta, v, w) with the
 // rounded new velocity.
@@ -204,78 +287,7 @@ k_aggregate(const u32 *__restrict__ idx, const float *__restrict__ val, u32 n, u
         for (int i = lane; i < kAggTile / 4; i += kWave)
             reinterpret_cast<float4 *>(tile)[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 
-        for (u32 w0 = 0; w0 < n; w0 += kWave) {
-            const u32 nw = n - w0 < (u32)kWave ? n - w0 : (u32)kWave;
-            u64 lo = groups == 1 ? pos0 : wave_lower_bounds(idx, w0, nw, k, tile_base, 0, k);
-            // ---- worker after worker: the next 64 pairs of its message in one
-            //      coalesced load, those below the tile's end added into the tile;
-            //      the loads of kAggAhead workers are in flight together --------
-            for (u32 g0 = 0; g0 < nw; g0 += kAggAhead) {
-                u64 from[kAggAhead];
-                u32 ri[kAggAhead];
-                float rv[kAggAhead];
-#pragma unroll
-                for (int q = 0; q < kAggAhead; ++q) {
-                    const u32 w = g0 + q < nw ? g0 + q : nw - 1;
-                    from[q] = read_lane_u64(lo, (int)w);
-                    const u64 j = from[q] + lane;
-                    const bool in = g0 + q < nw && j < k;
-                    ri[q] = in ? idx[(u64)(w0 + w) * k + j] : 0xFFFFFFFFu;
-                    rv[q] = in ? val[(u64)(w0 + w) * k + j] : 0.0f;
-                }
-#pragma unroll
-                for (int q = 0; q < kAggAhead; ++q) {
-                    if (g0 + q >= nw) break;
-                    const u32 w = g0 + q;
-                    const u32 *si = idx + (u64)(w0 + w) * k;
-                    const float *sv = val + (u64)(w0 + w) * k;
-                    u64 at = from[q];
-                    // 64 pairs into the tile; returns how many of them lay inside it
-                    auto add_slice = [&](u32 i, float v) -> u32 {
-                        const bool inside = (u64)i < tile_end;     // 0xFFFFFFFF marks "no entry"
-                        const u64 mask = __ballot(inside);         // a prefix of the lanes: sorted
-                        // repeated indices inside one message (never produced by the
-                        // encoder, but allowed) must be added in position order
-                        const bool dup = inside && lane_left(i, 0xFFFFFFFFu) == i;
-                        if (__ballot(dup) == 0ull) {
-                            if (inside) tile[i - tile_base] += v;
-                        } else {
-                            for (u64 rest = mask; rest; rest &= rest - 1) {
-                                const int src = __ffsll((unsigned long long)rest) - 1;
-                                if ((int)lane == src) tile[i - tile_base] += v;
-                            }
-                        }
-                        return popc_mask(mask);
-                    };
-                    u32 took = add_slice(ri[q], rv[q]);
-                    at += took;
-                    // The slice filled all 64 lanes: the message is crowded here (its
-                    // entries cluster in a few tiles). The next kAggMore slices are
-                    // fetched together and added in order up to the first that ends
-                    // inside the tile.
-                    while (took == (u32)kWave) {
-                        u32 mi[kAggMore];
-                        float mv[kAggMore];
-#pragma unroll
-                        for (int s2 = 0; s2 < kAggMore; ++s2) {
-                            const u64 j = at + (u64)s2 * kWave + lane;
-                            mi[s2] = j < k ? si[j] : 0xFFFFFFFFu;
-                            mv[s2] = j < k ? sv[j] : 0.0f;
-                        }
-#pragma unroll
-                        for (int s2 = 0; s2 < kAggMore; ++s2) {
-                            if (took == (u32)kWave) {
-                                took = add_slice(mi[s2], mv[s2]);
-                                at += took;
-                            }
-                        }
-                    }
-                    // the new position of worker w goes back into lane w
-                    if (lane == w) lo = at;
-                }
-            }
-            if (groups == 1) pos0 = lo;
-        }
+        add_messages(tile, idx, val, n, k, tile_base, tile_end, groups, pos0);
         if (out_vec && tile_base + kAggTile <= d) {
             float4 *o4 = reinterpret_cast<float4 *>(out + tile_base);
             constexpr int kVecs = kAggTile / 4 / kWave;
@@ -328,6 +340,82 @@ k_aggregate(const u32 *__restrict__ idx, const float *__restrict__ val, u32 n, u
                 }
             }
         }
+    }
+}
+
+// The master's step for matrices, up to the direction it takes: u = scale * average, v <- fma(mu, v, u), direction =
+// fma(mu, v, u) or the new v, and a part of the direction's squared norm for each workgroup (binary64). One kernel for the
+// average, the momentum and the norm: 20 bytes per coordinate where they take 36 one by one (four matrices of
+// 6000 x 1500, five workers: 157 us one by one). blockIdx.y: the matrix.
+template <bool kNesterov>
+__global__ void __launch_bounds__(kAggThreads)
+k_direction(DirectionMembers g, u32 n, u64 k, u64 d, u64 tiles, u32 tiles_per_wave, float scale, float mu, float *__restrict__ direction,
+            u64 direction_stride, double *__restrict__ part, u32 part_stride)
+{
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    __shared__ __align__(16) float tile_s[kAggWaves][kAggTile];
+    __shared__ double sum_s[kAggWaves];
+    const u32 lane = lane_id(), wave = threadIdx.x / kWave, member = blockIdx.y;
+    const u32 *__restrict__ idx = g.idx[member];
+    const float *__restrict__ val = g.val[member];
+    float *velocity = g.velocity[member], *to = direction + member * direction_stride;
+    float *tile = tile_s[wave];
+    const u64 first_tile = ((u64)blockIdx.x * kAggWaves + wave) * tiles_per_wave;
+    const u64 last_tile = first_tile + tiles_per_wave < tiles ? first_tile + tiles_per_wave : tiles;
+    const float fn = (float)n;
+    const bool vec = ((uintptr_t)velocity & 15u) == 0;
+    const u32 groups = (n + kWave - 1) / kWave;
+    double sum = 0.0;
+    auto step = [&](float total, float &v) {
+        const float u = scale * (total / fn);
+        v = fmaf(mu, v, u);
+        const float t = kNesterov ? fmaf(mu, v, u) : v;
+        sum += (double)t * (double)t;
+        return t;
+    };
+    u64 pos0 = 0;
+    if (groups == 1 && first_tile < last_tile) pos0 = wave_lower_bounds(idx, 0, n, k, first_tile * kAggTile, 0, k);
+    for (u64 t = first_tile; t < last_tile; ++t) {
+        const u64 tile_base = t * kAggTile;
+        const u64 tile_end = tile_base + kAggTile < d ? tile_base + kAggTile : d;
+        constexpr int kVecs = kAggTile / 4 / kWave;
+        const bool whole = vec && tile_base + kAggTile <= d;
+        f32x4 v[kVecs];
+        f32x4 *v4 = (f32x4 *)(velocity + tile_base), *t4 = (f32x4 *)(to + tile_base);
+        if (whole) {
+#pragma unroll
+            for (int q = 0; q < kVecs; ++q) v[q] = __builtin_nontemporal_load(v4 + q * kWave + lane);
+        }
+        for (int i = lane; i < kAggTile / 4; i += kWave) reinterpret_cast<float4 *>(tile)[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        add_messages(tile, idx, val, n, k, tile_base, tile_end, groups, pos0);
+        if (whole) {
+#pragma unroll
+            for (int q = 0; q < kVecs; ++q) {
+                f32x4 a = reinterpret_cast<const f32x4 *>(tile)[q * kWave + lane];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    float x = v[q][c];
+                    a[c] = step(a[c], x);
+                    v[q][c] = x;
+                }
+                __builtin_nontemporal_store(v[q], v4 + q * kWave + lane);
+                t4[q * kWave + lane] = a;
+            }
+        } else {
+            for (u64 i = lane; tile_base + i < tile_end; i += kWave) {
+                float x = velocity[tile_base + i];
+                to[tile_base + i] = step(tile[i], x);
+                velocity[tile_base + i] = x;
+            }
+        }
+    }
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+    if (lane == 0) sum_s[wave] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kAggWaves; ++w) sum += sum_s[w];
+        part[(u64)member * part_stride + blockIdx.x] = sum;
     }
 }
 
@@ -1050,6 +1138,22 @@ extern "C" int rtopk_aggregate_update_momentum(const uint32_t *idx, const float 
         idx, val, n, k, d, tiles, run, omega, Momentum{scale, mu, -eta, velocity});
     if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
     return RTOPK_OK;
+}
+
+int rtopk::launch_direction(u32 members, const DirectionMembers &g, u32 n, u64 k, u64 d, float scale, float mu, bool nesterov,
+                            float *direction, u64 direction_stride, double *part, u32 part_stride, u32 *parts, hipStream_t stream)
+{
+    for (u32 i = 0; i < members; ++i)
+        if (const int rc = debug_check_messages(g.idx[i], n, k, d, stream)) return rc;
+    const u64 tiles = (d + kAggTile - 1) / kAggTile;
+    // as many wavefronts as there are parts for their sums, and no more than four of the chip's worth over all matrices
+    const u64 most = std::max<u64>(1, std::min<u64>(part_stride, 1024 / members)) * kAggWaves;
+    const u32 run = (u32)((tiles + most - 1) / most);
+    *parts = (u32)((tiles + (u64)run * kAggWaves - 1) / ((u64)run * kAggWaves));
+    const dim3 grid(*parts, members);
+    if (nesterov) k_direction<true><<<grid, kAggThreads, 0, stream>>>(g, n, k, d, tiles, run, scale, mu, direction, direction_stride, part, part_stride);
+    else k_direction<false><<<grid, kAggThreads, 0, stream>>>(g, n, k, d, tiles, run, scale, mu, direction, direction_stride, part, part_stride);
+    return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_EHIP;
 }
 
 extern "C" int rtopk_aggregate_update_workspace_bytes(uint64_t d, uint32_t n, uint64_t k,

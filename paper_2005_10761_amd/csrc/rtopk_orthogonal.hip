@@ -35,6 +35,7 @@
 #include <cmath>
 
 #include "../../include/rtopk.h"
+#include "rtopk_direction.h"
 #include "rtopk_matrix.h"
 
 namespace rtopk {
@@ -43,8 +44,6 @@ namespace rtopk {
 // entries of Q up to kMostP (or, less k, its double) stay finite
 constexpr int kLogX = 12, kLogD = 10;
 constexpr double kMostX = 7.5, kMostP = 30.0;
-constexpr u32 kMembers = 16;            // matrices in one launch
-
 struct Members { void *p[kMembers]; };
 
 // Four lanes with four halves each: lane i gets the i-th of all four.
@@ -146,16 +145,17 @@ template <Operands kOf> struct Stored {
 constexpr u32 kNormThreads = 256, kNormBlocks = 256;     // workgroups (and parts of the sum) for one matrix, at most
 
 // the sum of the workgroup's values, in every thread
+template <int kThreads>
 __device__ __forceinline__ double block_sum(double v)
 {
-    __shared__ double part[kNormThreads / kWave];
+    __shared__ double part[kThreads / kWave];
 #pragma unroll
     for (int o = kWave / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
     if (lane_id() == 0) part[threadIdx.x / kWave] = v;
     __syncthreads();
     v = part[0];
 #pragma unroll
-    for (int w = 1; w < (int)(kNormThreads / kWave); ++w) v += part[w];
+    for (int w = 1; w < kThreads / kWave; ++w) v += part[w];
     return v;
 }
 
@@ -177,40 +177,7 @@ k_norm(Members x, int type, u32 rows, u32 cols, u64 ld, double *__restrict__ par
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum += (double)v[i] * (double)v[i];
     }
-    sum = block_sum(sum);
-    if (threadIdx.x == 0) part[blockIdx.y * kNormBlocks + blockIdx.x] = sum;
-}
-
-// The momentum of the master's step, and the norm of what is to be orthogonalised:
-// u = scale * average, v <- fma(mu, v, u), g = fma(mu, v, u) or the new v itself. `average` holds the averages, and g
-// afterwards.
-__global__ void __launch_bounds__(kNormThreads)
-k_velocity(Members velocity, float *__restrict__ average, u64 d, float scale, float mu, int nesterov, double *__restrict__ part)
-{
-    float *v = (float *)velocity.p[blockIdx.y], *g = average + blockIdx.y * align_up(d, 64);
-    double sum = 0.0;
-    auto step = [&](float &now, float &to) {
-        const float u = scale * to;
-        now = fmaf(mu, now, u);
-        to = nesterov ? fmaf(mu, now, u) : now;
-        sum += (double)to * (double)to;
-    };
-    const u64 fours = ((uintptr_t)v & 15u) == 0 ? d / 4 : 0;
-    const u64 first = (u64)blockIdx.x * kNormThreads + threadIdx.x, stride = (u64)gridDim.x * kNormThreads;
-    for (u64 i = first; i < fours; i += stride) {
-        f32x4 now = *(const f32x4 *)(v + 4 * i), to = *(const f32x4 *)(g + 4 * i);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            float x = now[c], y = to[c];
-            step(x, y);
-            now[c] = x;
-            to[c] = y;
-        }
-        *(f32x4 *)(v + 4 * i) = now;
-        *(f32x4 *)(g + 4 * i) = to;
-    }
-    for (u64 i = 4 * fours + first; i < d; i += stride) step(v[i], g[i]);
-    sum = block_sum(sum);
+    sum = block_sum<kNormThreads>(sum);
     if (threadIdx.x == 0) part[blockIdx.y * kNormBlocks + blockIdx.x] = sum;
 }
 
@@ -231,11 +198,12 @@ struct Start {
 constexpr u32 kSide = 64;
 
 // From the parts of a matrix's norm: the exponent that its elements are moved by, and (to *rho, where there is one) what is
-// left of the division. By all threads of a workgroup of kNormThreads.
+// left of the division. By all kThreads threads of a workgroup.
+template <int kThreads>
 __device__ __forceinline__ int exponent_of(const double *part, u32 parts, float eps, float *rho)
 {
-    static_assert(kNormBlocks == kNormThreads, "a part of the norm for each thread");
-    const double norm = sqrt(block_sum(threadIdx.x < parts ? part[threadIdx.x] : 0.0));
+    static_assert(kNormBlocks <= kThreads, "a part of the norm for each thread");
+    const double norm = sqrt(block_sum<kThreads>(threadIdx.x < parts ? part[threadIdx.x] : 0.0));
     int exponent = 0;
     if (norm > 0.0 && norm < __builtin_huge_val()) (void)frexp(norm, &exponent);
     if (threadIdx.x == 0 && rho) {
@@ -252,7 +220,7 @@ __global__ void __launch_bounds__(kNormThreads) k_start(Start g)
     typedef Stored<kOf> S;
     __shared__ float tile[kSide][kSide + 1];
     const u32 r0 = blockIdx.y * kSide, c0 = blockIdx.x * kSide, member = blockIdx.z;
-    const int e = exponent_of(g.part + member * kNormBlocks, g.parts, g.eps, blockIdx.x == 0 && blockIdx.y == 0 ? g.rho + member : nullptr);
+    const int e = exponent_of<kNormThreads>(g.part + member * kNormBlocks, g.parts, g.eps, blockIdx.x == 0 && blockIdx.y == 0 ? g.rho + member : nullptr);
     const u64 row_bytes = g.ld * (g.type == 0 ? 4u : 2u);
     const unsigned char *x = (const unsigned char *)g.x.p[member];
     const bool wide = (((uintptr_t)x | row_bytes) & 15u) == 0;
@@ -271,19 +239,17 @@ __global__ void __launch_bounds__(kNormThreads) k_start(Start g)
             tile[r + 32 * h][c + i] = v[h][i];
         }
         if (row < g.rows) {
-            if (c0 + c < S::padded(g.cols)) S::put(as_is + (u64)row * row_a, c0 + c, f32x4{v[h][0], v[h][1], v[h][2], v[h][3]});
-            if (c0 + c + 4 < S::padded(g.cols)) S::put(as_is + (u64)row * row_a, c0 + c + 4, f32x4{v[h][4], v[h][5], v[h][6], v[h][7]});
+            if (c0 + c < S::padded(g.cols)) S::template put_run<8>(as_is + (u64)row * row_a, c0 + c, v[h]);
         }
     }
     __syncthreads();
 #pragma unroll
     for (u32 h = 0; h < 2; ++h) {
         const u32 col = c0 + r + 32 * h, row = r0 + c;
+        float u[8];
 #pragma unroll
-        for (u32 q = 0; q < 8; q += 4)
-            if (col < g.cols && row + q < S::padded(g.rows))
-                S::put(turned + (u64)col * row_t, row + q,
-                       f32x4{tile[c + q][r + 32 * h], tile[c + q + 1][r + 32 * h], tile[c + q + 2][r + 32 * h], tile[c + q + 3][r + 32 * h]});
+        for (u32 q = 0; q < 8; ++q) u[q] = tile[c + q][r + 32 * h];
+        if (col < g.cols && row < S::padded(g.rows)) S::template put_run<8>(turned + (u64)col * row_t, row, u);
     }
 }
 
@@ -525,6 +491,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(Product g)
 // block, and that block's part of the next X X^T while it is in LDS. Only X turned over and the parts go through memory.
 // 64 x 576, four of them, five steps: 16 launches of the kernels above take 95 us (each as long as a launch).
 typedef unsigned char u8;
+constexpr int kNarrowThreads = 512;
 
 struct Narrow {
     Members x;                  // k_narrow_start: G
@@ -552,7 +519,7 @@ struct Narrow {
 };
 
 template <Operands kOf> struct Block {      // 64 rows of 64 numbers in LDS, slices as Tile reads them
-    typedef Tile<kOf, 64, 64, 2, 2, 2, false> T;
+    typedef Tile<kOf, 64, 64, 2, 4, 2, false> T;
     static constexpr u32 kSlices = kSide / Stored<kOf>::kBlock, kBytes = kSlices * kSide * kSlice;
     static __device__ __forceinline__ u8 *at(u8 *block, u32 row, u32 byte)
     {
@@ -599,7 +566,7 @@ __device__ __forceinline__ void write_part(const T &gram, float *to)
 }
 
 template <Operands kOf>
-__global__ void __launch_bounds__(kNormThreads) k_narrow_start(Narrow g)
+__global__ void __launch_bounds__(kNarrowThreads) k_narrow_start(Narrow g)
 {
     typedef Stored<kOf> S;
     typedef Block<kOf> B;
@@ -608,7 +575,7 @@ __global__ void __launch_bounds__(kNormThreads) k_narrow_start(Narrow g)
     const u32 member = blockIdx.y, run = blockIdx.x;
     const bool over = g.rows > g.cols;
     const u32 m = over ? g.cols : g.rows, n = over ? g.rows : g.cols;
-    const int e = exponent_of(g.norm + member * kNormBlocks, g.norm_parts, g.eps, run == 0 ? g.rho + member : nullptr);
+    const int e = exponent_of<kNarrowThreads>(g.norm + member * kNormBlocks, g.norm_parts, g.eps, run == 0 ? g.rho + member : nullptr);
     const u64 row_bytes = g.ld * (g.type == 0 ? 4u : 2u);
     const u8 *x = (const u8 *)g.x.p[member];
     const bool wide = (((uintptr_t)x | row_bytes) & 15u) == 0;
@@ -618,10 +585,8 @@ __global__ void __launch_bounds__(kNormThreads) k_narrow_start(Narrow g)
     for (u32 b = 0; b < g.blocks_each; ++b) {
         const u32 n0 = (run * g.blocks_each + b) * kSide;
         if (n0 >= n) break;
-        // pieces of eight along G's rows
-#pragma unroll
-        for (u32 h = 0; h < 2; ++h) {
-            const u32 r = (threadIdx.x >> 3) + 32 * h, c = (threadIdx.x & 7u) * 8u;
+        {   // pieces of eight along G's rows
+            const u32 r = threadIdx.x >> 3, c = (threadIdx.x & 7u) * 8u;
             const u32 row = over ? n0 + r : r, col = over ? c : n0 + c;
             float v[8];
             read_eight(v, x + (row < g.rows ? row : 0u) * row_bytes, col, row < g.rows ? g.cols : 0u, g.type, wide);
@@ -630,8 +595,8 @@ __global__ void __launch_bounds__(kNormThreads) k_narrow_start(Narrow g)
         }
         __syncthreads();
 #pragma unroll
-        for (u32 h = 0; h < 4; ++h) {
-            const u32 r = (threadIdx.x >> 4) + 16 * h, c = (threadIdx.x & 15u) * 4u;
+        for (u32 h = 0; h < 2; ++h) {
+            const u32 r = (threadIdx.x >> 4) + 32 * h, c = (threadIdx.x & 15u) * 4u;
             B::put(rows, r, c, f32x4{tile[r][c], tile[r][c + 1], tile[r][c + 2], tile[r][c + 3]});
             if (n0 + r < n && c < S::padded(m))
                 S::put(xt + (u64)(n0 + r) * S::row_bytes(m), c, f32x4{tile[c][r], tile[c + 1][r], tile[c + 2][r], tile[c + 3][r]});
@@ -661,7 +626,7 @@ __global__ void __launch_bounds__(256) k_narrow_join(Narrow g)
 }
 
 template <Operands kOf>
-__global__ void __launch_bounds__(kNormThreads) k_narrow(Narrow g)
+__global__ void __launch_bounds__(kNarrowThreads) k_narrow(Narrow g)
 {
     typedef Stored<kOf> S;
     typedef Block<kOf> B;
@@ -675,11 +640,11 @@ __global__ void __launch_bounds__(kNormThreads) k_narrow(Narrow g)
     const u8 *xt = g.xt + member * g.xt_stride;
     u8 *xt_next = g.xt_next + member * g.xt_stride;
     // a block of X turned over: rows of the long side, 16 bytes a thread and time
-    constexpr u32 kPieces = B::kBytes / 16 / kNormThreads;
+    constexpr u32 kPieces = B::kBytes / 16 / kNarrowThreads;
     auto load = [&](i32x4 (&v)[kPieces], u32 n0) {
 #pragma unroll
         for (u32 q = 0; q < kPieces; ++q) {
-            const u32 at = threadIdx.x + q * kNormThreads, r = at / (B::kSlices * 8u), piece = at % (B::kSlices * 8u);
+            const u32 at = threadIdx.x + q * kNarrowThreads, r = at / (B::kSlices * 8u), piece = at % (B::kSlices * 8u);
             v[q] = i32x4{0, 0, 0, 0};
             if (n0 + r < n && piece < pieces) v[q] = *(const i32x4 *)(xt + (u64)(n0 + r) * row_xt + piece * 16u);
         }
@@ -689,17 +654,17 @@ __global__ void __launch_bounds__(kNormThreads) k_narrow(Narrow g)
     load(held, first_block * kSide);
     {
         // D
-        const u32 r = threadIdx.x >> 2, c = (threadIdx.x & 3u) * 16u;
+        const u32 r = threadIdx.x >> 3, c = (threadIdx.x & 7u) * 8u;
         const u32 runs = g.joined ? 1u : g.runs;
         const float *part = (g.joined ? g.joined : g.part) + (u64)member * runs * kSide * kSide + r * kSide + c;
-        f32x4 sum[4] = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}};
-#pragma unroll 4
+        f32x4 sum[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll 8
         for (u32 s = 0; s < runs; ++s)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) sum[q] += *(const f32x4 *)(part + s * kSide * kSide + 4 * q);
+            for (int q = 0; q < 2; ++q) sum[q] += *(const f32x4 *)(part + s * kSide * kSide + 4 * q);
         const float scale = g.c_gram * rho * rho;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < 2; ++q) {
             f32x4 v = sum[q] * scale;
 #pragma unroll
             for (u32 i = 0; i < 4; ++i)
@@ -728,7 +693,7 @@ __global__ void __launch_bounds__(kNormThreads) k_narrow(Narrow g)
         if (n0 >= n) break;
 #pragma unroll
         for (u32 q = 0; q < kPieces; ++q) {
-            const u32 at = threadIdx.x + q * kNormThreads, r = at / (B::kSlices * 8u), piece = at % (B::kSlices * 8u);
+            const u32 at = threadIdx.x + q * kNarrowThreads, r = at / (B::kSlices * 8u), piece = at % (B::kSlices * 8u);
             *(i32x4 *)B::at(lds[2], r, piece * 16u) = held[q];
         }
         __syncthreads();                // (and P, and everybody has read D and the last block's rows)
@@ -859,13 +824,13 @@ bool is_narrow(const Shape &s) { return s.m() <= kSide; }
 
 struct Parts {
     double *norm;
-    float *rho, *average, *part, *joined;
+    float *rho, *direction, *part, *joined;
     unsigned char *x[2], *xt[2], *square[4];
     u64 x_stride, xt_stride, square_stride;
 };
 
 template <Operands kOf>
-u64 cut(void *base, u32 count, const Shape &s, bool average, Parts &p)
+u64 cut(void *base, u32 count, const Shape &s, bool direction, Parts &p)
 {
     typedef Stored<kOf> S;
     const u32 members = std::min(count, kMembers);
@@ -884,7 +849,7 @@ u64 cut(void *base, u32 count, const Shape &s, bool average, Parts &p)
                                   count > kMembers && count % kMembers ? (u64)(count % kMembers) * plan_narrow(s, count % kMembers).runs : 0);
         p.part = (float *)take(2 * runs * kSide * kSide * sizeof(float));
         p.joined = (float *)take((u64)members * kSide * kSide * sizeof(float));
-        p.average = average ? (float *)take(members * align_up((u64)s.rows * s.cols, 64) * sizeof(float)) : nullptr;
+        p.direction = direction ? (float *)take(members * align_up((u64)s.rows * s.cols, 64) * sizeof(float)) : nullptr;
         return used;
     }
     for (int i = 0; i < 2; ++i) {
@@ -900,13 +865,13 @@ u64 cut(void *base, u32 count, const Shape &s, bool average, Parts &p)
     // (the last launches may have fewer matrices, and more runs)
     const u64 part = std::max(sums(members), sums(count > kMembers ? count % kMembers : 0));
     p.part = (float *)take(part * sizeof(float));
-    p.average = average ? (float *)take(members * align_up((u64)s.rows * s.cols, 64) * sizeof(float)) : nullptr;
+    p.direction = direction ? (float *)take(members * align_up((u64)s.rows * s.cols, 64) * sizeof(float)) : nullptr;
     return used;
 }
 
-u64 cut(int products, void *base, u32 count, const Shape &s, bool average, Parts &p)
+u64 cut(int products, void *base, u32 count, const Shape &s, bool direction, Parts &p)
 {
-    return products == RTOPK_PRODUCTS_PAIRS ? cut<kPairs>(base, count, s, average, p) : cut<kHalves>(base, count, s, average, p);
+    return products == RTOPK_PRODUCTS_PAIRS ? cut<kPairs>(base, count, s, direction, p) : cut<kHalves>(base, count, s, direction, p);
 }
 
 // Whether iterates that start with singular values in [0, 1] stay where their stored forms are finite. largest: of
@@ -1011,7 +976,7 @@ int iterate_narrow(const Members &x, int type, u64 ldx, const Shape &s, u32 memb
     g.gain = target.gain;
     g.keep = target.keep;
     g.update = target.update;
-    k_narrow_start<kOf><<<grid, kNormThreads, 0, stream>>>(g);
+    k_narrow_start<kOf><<<grid, kNarrowThreads, 0, stream>>>(g);
     if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
     double h = 1.0 / s.m();
     for (u32 i = 0; i < steps; ++i) {
@@ -1032,7 +997,7 @@ int iterate_narrow(const Members &x, int type, u64 ldx, const Shape &s, u32 memb
             k_narrow_join<<<dim3(kSide * kSide / 64, members), 256, 0, stream>>>(g);
             if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
         }
-        k_narrow<kOf><<<grid, kNormThreads, 0, stream>>>(g);
+        k_narrow<kOf><<<grid, kNarrowThreads, 0, stream>>>(g);
         if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
     }
     return RTOPK_OK;
@@ -1280,19 +1245,21 @@ extern "C" int rtopk_aggregate_update_orthogonal(uint32_t count, const uint32_t 
     cut(products, workspace, count, s, true, p);
     for (uint32_t first = 0; first < count; first += kMembers) {
         const u32 members = std::min(count - first, kMembers);
-        Members velocities{}, steps_of{};
+        Members directions{};
+        DirectionMembers from{};
         Target to{Members{}, RTOPK_F32, cols, -(eta * gain), 1.0f - eta * decay, 1};
         for (u32 i = 0; i < members; ++i) {
-            float *average = p.average + i * align_up(d, 64);
-            if (const int rc = rtopk_aggregate(idx[first + i], val[first + i], n, k, d, average, nullptr, 0, stream_v)) return rc;
-            velocities.p[i] = velocity[first + i];
-            steps_of.p[i] = average;
+            from.idx[i] = idx[first + i];
+            from.val[i] = val[first + i];
+            from.velocity[i] = velocity[first + i];
+            directions.p[i] = p.direction + i * align_up(d, 64);
             to.to.p[i] = omega[first + i];
         }
-        const u32 parts = norm_blocks(d, members);
-        k_velocity<<<dim3(parts, members), kNormThreads, 0, stream>>>(velocities, p.average, d, scale, mu, nesterov, p.norm);
-        if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
-        if (const int rc = iterate(products, steps_of, RTOPK_F32, cols, s, members, parts, steps, coefficients, largest_p, eps, p, to, stream)) return rc;
+        u32 parts = 0;
+        if (const int rc = launch_direction(members, from, n, k, d, scale, mu, nesterov != 0, p.direction, align_up(d, 64), p.norm, kNormBlocks,
+                                            &parts, stream))
+            return rc;
+        if (const int rc = iterate(products, directions, RTOPK_F32, cols, s, members, parts, steps, coefficients, largest_p, eps, p, to, stream)) return rc;
     }
     return RTOPK_OK;
 }
