@@ -372,6 +372,7 @@ def encode_stats(workspace: torch.Tensor, stream=None) -> dict:
 # ---- matrix parameters: a layer's products in 8-bit integers, orthogonalised updates ----------
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_INT8 = (torch.int8,)
 _ALONG = {"rows": 0, "columns": 1}
 _PRODUCTS = {"pairs": 0, "halves": 1}
 #: (a, b, c) of every step, in common use for updates of neural networks
@@ -425,6 +426,7 @@ def _workspace(workspace: Optional[torch.Tensor], need: int, device, stream):
     return at + -at % 256, need, held
 
 
+@functools.lru_cache(maxsize=1024)
 def quantize_i8_workspace_bytes(rows: int, cols: int, along: str = "rows") -> int:
     return _bytes("rtopk_quantize_i8_workspace_bytes", rows, cols, _ALONG[along])
 
@@ -435,20 +437,20 @@ def quantize_i8(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, along: st
     (``along="columns"``) for each column, ``q`` then holding ``x`` turned over. Give ``q`` rows that start on
     16 bytes (a multiple of 16 between them) where the product is to read it fast. ``workspace``: None
     takes it from torch's allocator, here and in the calls below."""
-    _matrix(x, "x", _TYPES)
-    _matrix(q, "q", (torch.int8,))
-    rows, cols = x.shape
-    if tuple(q.shape) != ((rows, cols) if along == "rows" else (cols, rows)):
+    ldx, ldq = _matrix(x, "x", _TYPES), _matrix(q, "q", _INT8)
+    rows, cols = x.size()
+    if q.size() != ((rows, cols) if along == "rows" else (cols, rows)):
         raise ValueError("q must have the shape of x, or of x turned over along columns")
     _vector(scale, q.size(0), "scale")
-    ws, ws_bytes, held = _workspace(workspace, 0 if along == "rows" else quantize_i8_workspace_bytes(rows, cols, along),
-                                    x.device, stream)
-    rc = load_library().rtopk_quantize_i8(_ptr(x), _TYPES[x.dtype], rows, cols, _ld(x), _ALONG[along], _ptr(q), _ld(q),
-                                          _ptr(scale), ws, ws_bytes, _stream_handle(stream))
+    need = 0 if along == "rows" or workspace is not None else quantize_i8_workspace_bytes(rows, cols, along)
+    ws, ws_bytes, held = _workspace(workspace, need, x.device, stream)
+    rc = load_library().rtopk_quantize_i8(x.data_ptr(), _TYPES[x.dtype], rows, cols, ldx, _ALONG[along], q.data_ptr(), ldq,
+                                          scale.data_ptr(), ws, ws_bytes, _stream_handle(stream))
     if rc:
         raise RtopkError(rc, "rtopk_quantize_i8")
 
 
+@functools.lru_cache(maxsize=1024)
 def matmul_i8_workspace_bytes(m: int, n: int, k: int) -> int:
     return _bytes("rtopk_matmul_i8_workspace_bytes", m, n, k)
 
@@ -456,19 +458,18 @@ def matmul_i8_workspace_bytes(m: int, n: int, k: int) -> int:
 def matmul_i8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor, out: torch.Tensor,
               bias: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """rtopk_matmul_i8: out[i, j] = a_scale[i] b_scale[j] sum_k a[i, k] b[j, k] (+ bias[j])."""
-    _matrix(a, "a", (torch.int8,))
-    _matrix(b, "b", (torch.int8,))
-    _matrix(out, "out", _TYPES)
-    (m, k), n = a.shape, b.size(0)
-    if b.size(1) != k or tuple(out.shape) != (m, n):
+    lda, ldb, ldo = _matrix(a, "a", _INT8), _matrix(b, "b", _INT8), _matrix(out, "out", _TYPES)
+    (m, k), (n, b_k) = a.size(), b.size()
+    if b_k != k or out.size() != (m, n):
         raise ValueError("a is [m, k], b [n, k], out [m, n]")
     _vector(a_scale, m, "a_scale")
     _vector(b_scale, n, "b_scale")
     if bias is not None:
         _vector(bias, n, "bias")
-    ws, ws_bytes, held = _workspace(workspace, 0 if workspace is not None else matmul_i8_workspace_bytes(m, n, k), a.device, stream)
-    rc = load_library().rtopk_matmul_i8(_ptr(a), _ptr(a_scale), _ptr(b), _ptr(b_scale), _ptr(bias), m, n, k, _ld(a), _ld(b),
-                                        _ptr(out), _TYPES[out.dtype], _ld(out), ws, ws_bytes, _stream_handle(stream))
+    need = 0 if workspace is not None else matmul_i8_workspace_bytes(m, n, k)
+    ws, ws_bytes, held = _workspace(workspace, need, a.device, stream)
+    rc = load_library().rtopk_matmul_i8(a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), _ptr(bias), m, n, k, lda, ldb,
+                                        out.data_ptr(), _TYPES[out.dtype], ldo, ws, ws_bytes, _stream_handle(stream))
     if rc:
         raise RtopkError(rc, "rtopk_matmul_i8")
 
@@ -476,9 +477,6 @@ def matmul_i8(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: 
 @functools.lru_cache(maxsize=1024)
 def linear_i8_workspace_bytes(m: int, k: int, n: int) -> int:
     return _bytes("rtopk_linear_i8_workspace_bytes", m, k, n)
-
-
-_INT8 = (torch.int8,)
 
 
 def linear_i8(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, out: torch.Tensor, bias: Optional[torch.Tensor] = None,
@@ -494,13 +492,14 @@ def linear_i8(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, out: torc
     if bias is not None:
         _vector(bias, n, "bias")
     need = 0 if workspace is not None else linear_i8_workspace_bytes(m, k, n)
-    ws, ws_bytes, held = _workspace(workspace, need, x.device, stream) if need or workspace is not None else (None, 0, None)
+    ws, ws_bytes, held = _workspace(workspace, need, x.device, stream)
     rc = load_library().rtopk_linear_i8(x.data_ptr(), _TYPES[x.dtype], m, k, ldx, w.data_ptr(), w_scale.data_ptr(), n, ldw, _ptr(bias),
                                         out.data_ptr(), _TYPES[out.dtype], ldo, ws, ws_bytes, _stream_handle(stream))
     if rc:
         raise RtopkError(rc, "rtopk_linear_i8")
 
 
+@functools.lru_cache(maxsize=1024)
 def linear_i8_backward_workspace_bytes(m: int, k: int, n: int) -> int:
     return _bytes("rtopk_linear_i8_backward_workspace_bytes", m, k, n)
 
@@ -522,7 +521,7 @@ def linear_i8_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w_turned: Op
     k = (dx if dx is not None else dw).size(1)
     if dx is not None:
         _matrix(dx, "dx", (dy.dtype,))
-        _matrix(w_turned, "w_turned", (torch.int8,))
+        _matrix(w_turned, "w_turned", _INT8)
         _vector(w_turned_scale, k, "w_turned_scale")
         if tuple(dx.shape) != (m, k) or tuple(w_turned.shape) != (k, n):
             raise ValueError("dy is [m, n], dx [m, k], w_turned [k, n]")
@@ -552,6 +551,7 @@ def _coefficients(coefficients, steps: Optional[int]):
     return len(rows), (ctypes.c_float * (3 * len(rows)))(*[v for c in rows for v in c])
 
 
+@functools.lru_cache(maxsize=1024)
 def orthogonalize_workspace_bytes(count: int, rows: int, cols: int, products: str = "pairs") -> int:
     return _bytes("rtopk_orthogonalize_workspace_bytes", count, rows, cols, _PRODUCTS[products])
 
@@ -584,6 +584,7 @@ def orthogonalize(xs, outs, steps: Optional[int] = None, coefficients=QUINTIC, e
         raise RtopkError(rc, "rtopk_orthogonalize")
 
 
+@functools.lru_cache(maxsize=1024)
 def aggregate_update_orthogonal_workspace_bytes(count: int, rows: int, cols: int, products: str = "pairs") -> int:
     return _bytes("rtopk_aggregate_update_orthogonal_workspace_bytes", count, rows, cols, _PRODUCTS[products])
 

@@ -65,41 +65,6 @@ __device__ __forceinline__ u32 four_bytes(const int *q)
     return ((u32)q[0] & 255u) | ((u32)q[1] & 255u) << 8 | ((u32)q[2] & 255u) << 16 | (u32)q[3] << 24;
 }
 
-// Eight neighbours of a row as they are in memory, and as numbers. The load has no branch around it (several are under
-// way together): a lane whose eight are not all there takes the row's first eight, or zeros of the library's where the row is
-// shorter, and `numbers` reads what there is of them one by one.
-static __device__ const u32 kNothing[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-
-template <int kType> struct Eight {
-    i32x4 w[kType == RTOPK_F32 ? 2 : 1];
-    static constexpr u32 kSize = kType == RTOPK_F32 ? 4u : 2u;
-    __device__ __forceinline__ void load(const unsigned char *row, u32 c, u32 cols)
-    {
-        const unsigned char *p = cols < 8u ? (const unsigned char *)kNothing : row + (c + 8u <= cols ? c : 0u) * kSize;
-        __builtin_memcpy(w, p, sizeof w);
-    }
-    __device__ __forceinline__ void numbers(float (&v)[8], const unsigned char *row, u32 c, u32 cols) const
-    {
-        const bool all = c + 8u <= cols;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float x;
-            if (kType == RTOPK_F32) {
-                x = __uint_as_float((u32)w[kType == RTOPK_F32 ? i >> 2 : 0][i & 3]);
-            } else {
-                const u16 h = (u16)((u32)w[0][i >> 1] >> (16 * (i & 1)));
-                x = kType == RTOPK_BF16 ? __uint_as_float((u32)h << 16) : (float)__builtin_bit_cast(_Float16, h);
-            }
-            v[i] = all ? x : 0.0f;
-        }
-        if (c < cols && !all) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (c + i < cols) v[i] = read_as(row, c + i, kType);
-        }
-    }
-};
-
 struct RowsToQuantize {
     const void *x;
     u64 ldx;            // elements
@@ -153,15 +118,14 @@ __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kQua
     const Quantizer quantize(scale_of(largest));
     if (c0 == 0) g.scale[r] = quantize.s;
     signed char *q = g.q + (u64)r * g.ldq;
-    const bool wide_q = (((uintptr_t)g.q | g.ldq) & 7u) == 0;
     auto write = [&](const Eight<kType> &e, u32 c) {
         float v[8];
         int n[8];
         e.numbers(v, row, c, g.cols);
         quantize(n, v);
         const u32 word[2] = {four_bytes(n), four_bytes(n + 4)};
-        if (wide_q && c + 8u <= g.fill) {
-            *(uint2 *)(q + c) = make_uint2(word[0], word[1]);
+        if (c + 8u <= g.fill) {
+            __builtin_memcpy(q + c, word, 8);
         } else {
 #pragma unroll
             for (u32 i = 0; i < 8u; ++i)
@@ -270,7 +234,6 @@ __global__ void __launch_bounds__(kQuantizeThreads) k_quantize_columns(ColumnsTo
     const u32 lane = lane_id(), wave = threadIdx.x / kWave, c0 = blockIdx.x * kWave, first = blockIdx.y * blocks * kTurnRows;
     const bool totals = g.total && first == 0;
     const u64 row_bytes = g.ldx * Eight<kType>::kSize;
-    const bool wide_q = (((uintptr_t)g.q | g.ldq) & 15u) == 0;
     const u32 piece = threadIdx.x & 7u, quad = threadIdx.x >> 3, c = c0 + 8u * piece;       // columns c .. c + 7 of rows 4 quad .. + 3
     Eight<kType> e[4];
     auto load = [&](u32 r0) {
@@ -333,8 +296,8 @@ __global__ void __launch_bounds__(kQuantizeThreads) k_quantize_columns(ColumnsTo
 #pragma unroll
             for (u32 b = 0; b < 4; ++b) word[b] = turned[col][at / 4 + b];
             signed char *q = g.q + (u64)(c0 + col) * g.ldq + r0 + at;
-            if (wide_q && r0 + at + 16u <= g.fill) {
-                *(uint4 *)q = make_uint4(word[0], word[1], word[2], word[3]);
+            if (r0 + at + 16u <= g.fill) {
+                __builtin_memcpy(q, word, 16);
             } else {
 #pragma unroll
                 for (u32 b = 0; b < 16u; ++b)
@@ -366,19 +329,14 @@ struct Four {
 __device__ __forceinline__ Four channels(const Scaled &g, u32 col)
 {
     Four f;
-    const bool all = col + 4u <= g.n;
+    const float *bias = g.bias ? g.bias : (const float *)kNothing;
 #pragma unroll
     for (u32 c = 0; c < 4; ++c) {
-        const u32 at = all || col + c < g.n ? col + c : g.n - 1u;
+        const u32 at = min(col + c, g.n - 1u);
         f.scale[c] = g.b_scale[at];
-        f.bias[c] = g.bias ? g.bias[at] : 0.0f;
+        f.bias[c] = bias[g.bias ? at : 0u];
     }
     return f;
-}
-__device__ __forceinline__ bool wide_out(const Scaled &g)
-{
-    const u32 size = g.type == 0 ? 4u : 2u;
-    return (((uintptr_t)g.out | (g.ldo * size)) & (4u * size - 1u)) == 0;
 }
 __device__ __forceinline__ f32x4 scaled(const f32x4 &sum, float a_scale, const Four &f)
 {
@@ -387,9 +345,9 @@ __device__ __forceinline__ f32x4 scaled(const f32x4 &sum, float a_scale, const F
     for (u32 c = 0; c < 4; ++c) v[c] = fmaf(sum[c] * a_scale, f.scale[c], f.bias[c]);
     return v;
 }
-__device__ __forceinline__ void write_scaled(const Scaled &g, u32 row, u32 col, const f32x4 &sum, float a_scale, const Four &f, bool wide)
+__device__ __forceinline__ void write_scaled(const Scaled &g, u32 row, u32 col, const f32x4 &sum, float a_scale, const Four &f)
 {
-    write_four(g.out, (u64)row * g.ldo + col, g.type, scaled(sum, a_scale, f), g.n - col, wide);
+    write_four(g.out, (u64)row * g.ldo + col, g.type, scaled(sum, a_scale, f), g.n - col);
 }
 
 template <class T, bool kWhole>
@@ -408,11 +366,9 @@ __global__ void __launch_bounds__(T::kThreads) k_product(Scaled g)
     t.clear();
     t.template multiply<kWhole>(a, b, from, min(from + g.slices_each, slices), lds);
     if (g.splits == 1) {
-        const bool wide = wide_out(g);
         float a_scale[T::kFragsM];
 #pragma unroll
         for (int i = 0; i < T::kFragsM; ++i) a_scale[i] = g.a_scale[min(i0 + T::row_at(i), g.m - 1u)];
-        const bool eights = T::wide_at(0) && g.type != 0 && (((uintptr_t)g.out | g.ldo * 2u) & 15u) == 0;
 #pragma unroll
         for (int j = 0; j < T::kFragsN; ++j) {
             const u32 col = j0 + T::col_at(j);
@@ -431,15 +387,11 @@ __global__ void __launch_bounds__(T::kThreads) k_product(Scaled g)
             if (row >= g.m) continue;
 #pragma unroll
             for (int j = 0; j < T::kFragsN; j += T::step_at(j)) {
-                const u32 col = j0 + T::col_at(j), next = j0 + T::col_at(T::next_to(j));
+                const u32 col = j0 + T::col_at(j);
                 const f32x4 v = __builtin_bit_cast(f32x4, t.sum[i][j]), u = __builtin_bit_cast(f32x4, t.sum[i][T::next_to(j)]);
-                const u64 first = (u64)row * g.ldo;
-                if (T::wide_at(j) && eights && col + 8u <= g.n) {
-                    write_eight(g.out, first + col, g.type, v, u);
-                } else {
-                    if (col < g.n) write_four(g.out, first + col, g.type, v, g.n - col, wide);
-                    if (T::wide_at(j) && next < g.n) write_four(g.out, first + next, g.type, u, g.n - next, wide);
-                }
+                if (col >= g.n) continue;
+                if (T::wide_at(j)) write_eight(g.out, (u64)row * g.ldo + col, g.type, v, u, g.n - col);
+                else write_four(g.out, (u64)row * g.ldo + col, g.type, v, g.n - col);
             }
         }
     } else {
@@ -456,7 +408,6 @@ __global__ void __launch_bounds__(256) k_product_join(Scaled g)
 {
     const u32 fours = (g.n + 3) / 4;
     const u64 all = (u64)g.m * fours, ld = 4ull * fours;
-    const bool wide = wide_out(g);
     for (u64 at = (u64)blockIdx.x * 256 + threadIdx.x; at < all; at += (u64)gridDim.x * 256) {
         const u32 row = (u32)(at / fours), col = (u32)(at - (u64)row * fours) * 4u;
         double sum[4] = {0, 0, 0, 0};
@@ -465,7 +416,7 @@ __global__ void __launch_bounds__(256) k_product_join(Scaled g)
 #pragma unroll
             for (int c = 0; c < 4; ++c) sum[c] += (double)v[c];
         }
-        write_scaled(g, row, col, f32x4{(float)sum[0], (float)sum[1], (float)sum[2], (float)sum[3]}, g.a_scale[row], channels(g, col), wide);
+        write_scaled(g, row, col, f32x4{(float)sum[0], (float)sum[1], (float)sum[2], (float)sum[3]}, g.a_scale[row], channels(g, col));
     }
 }
 
@@ -481,12 +432,13 @@ struct Few {
     Scaled s;                           // a: quantised tokens, or null
     const void *x;
     u64 ldx;
-    int type;
 };
 
-template <int kWaves, int kTokens, bool kQuantize>
+// kType: of x, or -1 where it is quantised already
+template <int kWaves, int kTokens, int kType>
 __global__ void __launch_bounds__(kWaves * kWave) k_few(Few f)
 {
+    constexpr bool kQuantize = kType >= 0;
     constexpr u32 kBatch = 8;
     const Scaled &g = f.s;
     const u32 lane = lane_id(), wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
@@ -507,9 +459,12 @@ __global__ void __launch_bounds__(kWaves * kWave) k_few(Few f)
             for (u32 q = 0; q < kBatch; ++q) __builtin_memcpy(&held[q], w + (s + q) * 64u + piece, 16);
         } else {
 #pragma unroll
-            for (u32 q = 0; q < kBatch; ++q) held[q] = load_piece(w, (s + q) * 64u + piece, g.k);
+            for (u32 q = 0; q < kBatch; ++q)            // (no more loads than steps: rows at odd places are slow to read, 16 x 123 x 1359
+                // took 13 us with eight loads for each wavefront, 7 so)
+                if (s + q < to) held[q] = load_piece(w, (s + q) * 64u + piece, g.k);
 #pragma unroll
-            for (u32 q = 0; q < kBatch; ++q) held[q] = cut_piece(held[q], (s + q) * 64u + piece, g.k);
+            for (u32 q = 0; q < kBatch; ++q)
+                if (s + q < to) held[q] = cut_piece(held[q], (s + q) * 64u + piece, g.k);
         }
     };
     fetch(from);                            // the first weights are on their way while x is quantised
@@ -517,9 +472,11 @@ __global__ void __launch_bounds__(kWaves * kWave) k_few(Few f)
     if constexpr (kQuantize) {
         // every thread holds up to kHeld pieces of eight, whatever token they are of: one trip to memory
         constexpr u32 kHeld = (kInOne / 8 + kFewTokens + kWaves * kWave - 1) / (kWaves * kWave);
-        const u64 row_bytes = f.ldx * (f.type == 0 ? 4u : 2u);
-        const bool wide = (((uintptr_t)f.x | row_bytes) & 15u) == 0;
+        typedef Eight<kQuantize ? kType : 0> E;
+        const u64 row_bytes = f.ldx * E::kSize;
+        const unsigned char *x = (const unsigned char *)f.x;
         const u32 pieces = (g.k + 7u) / 8u, all = g.m * pieces;
+        E held_x[kHeld];
         float v[kHeld][8];
         u32 token[kHeld], c[kHeld];
 #pragma unroll
@@ -528,13 +485,15 @@ __global__ void __launch_bounds__(kWaves * kWave) k_few(Few f)
             const u32 at = threadIdx.x + h * kWaves * kWave;
             token[h] = g.m == 1 || at >= all ? 0u : at / pieces;
             c[h] = (at - token[h] * pieces) * 8u;
-            read_eight(v[h], (const unsigned char *)f.x + token[h] * row_bytes, c[h], at < all ? g.k : 0u, f.type, wide);
+            if (at >= all) c[h] = pieces * 8u;              // nothing: zeros
+            held_x[h].load(x + token[h] * row_bytes, c[h], g.k);
         }
         if (threadIdx.x < kTokens * 16) most[threadIdx.x] = 0u;
         __syncthreads();
 #pragma unroll
         for (u32 h = 0; h < kHeld; ++h) {
             if (h * kWaves * kWave >= all) break;
+            held_x[h].numbers(v[h], x + token[h] * row_bytes, c[h], g.k);
             u32 largest = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) largest = max(largest, magnitude(v[h][i]));
@@ -593,7 +552,6 @@ __global__ void __launch_bounds__(kWaves * kWave) k_few(Few f)
     const u32 col = blockIdx.x * 16u + 4u * (lane >> 4);
     if (col >= g.n) return;
     const Four four = channels(g, col);
-    const bool wide_o = wide_out(g);
 #pragma unroll
     for (int t = 0; t < kTokens; ++t) {
         // (a sum of kMostSteps steps stays below 2^31: longer contractions do not come here)
@@ -601,7 +559,7 @@ __global__ void __launch_bounds__(kWaves * kWave) k_few(Few f)
         const u32 token = 16u * t + (lane & 15u);
         if (token < g.m)
             write_scaled(g, token, col, f32x4{(float)sum[t][0], (float)sum[t][1], (float)sum[t][2], (float)sum[t][3]}, token_scale[token],
-                         four, wide_o);
+                         four);
     }
 }
 
@@ -665,24 +623,27 @@ void launch_product(const Scaled &g, const Plan &p, bool whole, hipStream_t stre
 }
 
 template <int kWaves, int kTokens>
-void launch_few(const Few &f, hipStream_t stream)
+void launch_few(const Few &f, int type, hipStream_t stream)
 {
     const u32 blocks = (f.s.n + 15) / 16, sums = (kWaves - 1) * kTokens * kWave * 16;
     const u32 tokens = f.s.a ? 0 : f.s.m * ((f.s.k + 63) / 64 * 64 + 16);
-    if (f.s.a) k_few<kWaves, kTokens, false><<<blocks, kWaves * kWave, sums, stream>>>(f);
-    else k_few<kWaves, kTokens, true><<<blocks, kWaves * kWave, std::max(sums, tokens), stream>>>(f);
+    const u32 lds = std::max(sums, tokens);
+    if (f.s.a) k_few<kWaves, kTokens, -1><<<blocks, kWaves * kWave, lds, stream>>>(f);
+    else if (type == RTOPK_F32) k_few<kWaves, kTokens, RTOPK_F32><<<blocks, kWaves * kWave, lds, stream>>>(f);
+    else if (type == RTOPK_BF16) k_few<kWaves, kTokens, RTOPK_BF16><<<blocks, kWaves * kWave, lds, stream>>>(f);
+    else k_few<kWaves, kTokens, RTOPK_F16><<<blocks, kWaves * kWave, lds, stream>>>(f);
 }
 
 bool few_tokens(u32 m, u32 k) { return m <= kFewTokens && k <= kMostSlices * kSlice; }
 bool in_one(u32 m, u32 k) { return few_tokens(m, k) && (u64)m * k <= kInOne; }
 
 // fewer than two workgroups a unit: each has sixteen wavefronts
-int run_few(const Few &f, hipStream_t stream)
+int run_few(const Few &f, int type, hipStream_t stream)
 {
     const bool many = f.s.n >= 2 * kUnits * 16;
-    if (f.s.m <= 16) many ? launch_few<4, 1>(f, stream) : launch_few<16, 1>(f, stream);
-    else if (f.s.m <= 32) many ? launch_few<4, 2>(f, stream) : launch_few<16, 2>(f, stream);
-    else many ? launch_few<4, 4>(f, stream) : launch_few<8, 4>(f, stream);
+    if (f.s.m <= 16) many ? launch_few<4, 1>(f, type, stream) : launch_few<16, 1>(f, type, stream);
+    else if (f.s.m <= 32) many ? launch_few<4, 2>(f, type, stream) : launch_few<16, 2>(f, type, stream);
+    else many ? launch_few<4, 4>(f, type, stream) : launch_few<8, 4>(f, type, stream);
     return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_EHIP;
 }
 
@@ -882,9 +843,9 @@ extern "C" int rtopk_linear_i8(const void *x, int type, uint64_t m, uint64_t k, 
     cut_linear(workspace, (u32)m, (u32)k, (u32)n, p);
     const u64 ld = filled((u32)k);
     const Scaled g{p.x, w, ld, ldw, (u32)m, (u32)n, (u32)k, p.x_scale, w_scale, bias, out, ldo, out_type, 0, 0, nullptr};
-    if (in_one((u32)m, (u32)k)) return run_few(Few{g, x, ldx, type}, stream);
+    if (in_one((u32)m, (u32)k)) return run_few(Few{g, x, ldx}, type, stream);
     if (const int rc = quantize_rows(x, type, (u32)m, (u32)k, ldx, p.x, ld, (u32)ld, p.x_scale, stream)) return rc;
-    return few_tokens((u32)m, (u32)k) ? run_few(Few{g, nullptr, 0, 0}, stream) : run_product(g, p.part, stream);
+    return few_tokens((u32)m, (u32)k) ? run_few(Few{g, nullptr, 0}, type, stream) : run_product(g, p.part, stream);
 }
 
 extern "C" int rtopk_linear_i8_backward_workspace_bytes(uint64_t m, uint64_t k, uint64_t n, uint64_t *bytes)

@@ -398,27 +398,46 @@ __device__ __forceinline__ float read_as(const void *p, u64 at, int type)
                        : (float)((const _Float16 *)p)[at];
 }
 
-// Eight neighbours from column c on, zeros beyond `cols`. `wide`: rows start on 16 bytes.
-__device__ __forceinline__ void read_eight(float (&v)[8], const void *row, u32 c, u32 cols, int type, bool wide)
-{
-    if (wide && c + 8u <= cols) {
-        if (type == 0) {
-            const f32x4 lo = *(const f32x4 *)((const float *)row + c), hi = *(const f32x4 *)((const float *)row + c + 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { v[i] = lo[i]; v[4 + i] = hi[i]; }
-        } else {
-            const i32x4 w = *(const i32x4 *)((const u16 *)row + c);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const u16 h = (u16)((u32)w[i >> 1] >> (16 * (i & 1)));
-                v[i] = type == 1 ? __uint_as_float((u32)h << 16) : (float)__builtin_bit_cast(_Float16, h);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? read_as(row, c + i, type) : 0.0f;
+// Eight neighbours of a row as they are in memory, and as numbers. The load has no branch around it (several are under
+// way together): a lane whose eight are not all there takes the row's last eight, and `numbers` moves them down; where the row
+// has no eight it takes zeros of the library's, and `numbers` reads what there is one by one.
+static __device__ const u32 kNothing[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+
+template <int kType> struct Eight {
+    i32x4 w[kType == 0 ? 2 : 1];
+    static constexpr u32 kSize = kType == 0 ? 4u : 2u;
+    __device__ __forceinline__ void load(const unsigned char *row, u32 c, u32 cols)
+    {
+        const unsigned char *p = cols < 8u ? (const unsigned char *)kNothing : row + min(c, cols - 8u) * kSize;
+        __builtin_memcpy(w, p, sizeof w);
     }
-}
+    __device__ __forceinline__ void numbers(float (&v)[8], const unsigned char *row, u32 c, u32 cols) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float x;
+            if (kType == 0) {
+                x = __uint_as_float((u32)w[kType == 0 ? i >> 2 : 0][i & 3]);
+            } else {
+                const u16 h = (u16)((u32)w[0][i >> 1] >> (16 * (i & 1)));
+                x = kType == 1 ? __uint_as_float((u32)h << 16) : (float)__builtin_bit_cast(_Float16, h);
+            }
+            v[i] = c < cols ? x : 0.0f;
+        }
+        if (c + 8u <= cols) return;
+        if (cols >= 8u) {                   // a row's last piece was read from the row's last eight on: down it moves
+            const u32 down = c - (cols - 8u);
+#pragma unroll
+            for (int by = 4; by; by >>= 1)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = down & by ? (i + by < 8 ? v[i + by] : 0.0f) : v[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c + i < cols) v[i] = read_as(row, c + i, kType);
+        }
+    }
+};
 
 __device__ __forceinline__ u16 half_bits(float v, int type)
 {
@@ -431,30 +450,36 @@ __device__ __forceinline__ void write_as(void *p, u64 at, int type, float v)
     else ((u16 *)p)[at] = half_bits(v, type);
 }
 
-// Eight neighbours of a 16-bit type, all there and from 16 bytes on.
-__device__ __forceinline__ void write_eight(void *p, u64 at, int type, const f32x4 &a, const f32x4 &b)
+// Four and eight neighbours from `at` on, of which `have` are there. Wide stores at any alignment (rows of an odd
+// length start anywhere: a product of 729 x 185 x 16179 into halves 20 us, number by number 35).
+__device__ __forceinline__ void write_four(void *p, u64 at, int type, const f32x4 &v, u32 have)
 {
-    typedef u16 u16x8 __attribute__((ext_vector_type(8)));
-    u16x8 v;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        v[c] = half_bits(a[c], type);
-        v[4 + c] = half_bits(b[c], type);
-    }
-    *(u16x8 *)((u16 *)p + at) = v;
-}
-
-// Four neighbours, of which `have` are there; `wide`: all four places start on 4 elements' bytes.
-__device__ __forceinline__ void write_four(void *p, u64 at, int type, const f32x4 &v, u32 have, bool wide)
-{
-    typedef u16 u16x4 __attribute__((ext_vector_type(4)));
-    if (wide && have >= 4u) {
-        if (type == 0) *(f32x4 *)((float *)p + at) = v;
-        else *(u16x4 *)((u16 *)p + at) = u16x4{half_bits(v[0], type), half_bits(v[1], type), half_bits(v[2], type), half_bits(v[3], type)};
+    if (have >= 4u) {
+        if (type == 0) {
+            __builtin_memcpy((float *)p + at, &v, 16);
+        } else {
+            const u16 w[4] = {half_bits(v[0], type), half_bits(v[1], type), half_bits(v[2], type), half_bits(v[3], type)};
+            __builtin_memcpy((u16 *)p + at, w, 8);
+        }
     } else {
 #pragma unroll
         for (u32 c = 0; c < 4; ++c)
             if (c < have) write_as(p, at + c, type, v[c]);
+    }
+}
+__device__ __forceinline__ void write_eight(void *p, u64 at, int type, const f32x4 &a, const f32x4 &b, u32 have)
+{
+    if (type != 0 && have >= 8u) {
+        u16 w[8];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            w[c] = half_bits(a[c], type);
+            w[4 + c] = half_bits(b[c], type);
+        }
+        __builtin_memcpy((u16 *)p + at, w, 16);
+    } else {
+        write_four(p, at, type, a, have);
+        if (have > 4u) write_four(p, at + 4, type, b, have - 4u);
     }
 }
 

@@ -159,23 +159,38 @@ __device__ __forceinline__ double block_sum(double v)
     return v;
 }
 
-// Pieces of eight neighbours of a matrix (from a multiple of eight columns on), each wavefront 64 of them at a time.
-// One read of the matrix: 10 us for four of 6000 x 1500 (14.4 TB/s, they come from the last-level cache).
+// Pieces of eight neighbours of a matrix (from a multiple of eight columns on), four of a thread under way. One read: four
+// matrices of 6000 x 1500 binary32 at 4.1 TB/s with two pieces under way.
+template <int kType>
 __global__ void __launch_bounds__(kNormThreads)
-k_norm(Members x, int type, u32 rows, u32 cols, u64 ld, double *__restrict__ part)
+k_norm(Members x, u32 rows, u32 cols, u64 ld, double *__restrict__ part)
 {
-    const void *g = x.p[blockIdx.y];
+    constexpr u32 kAtOnce = 4;
+    const unsigned char *g = (const unsigned char *)x.p[blockIdx.y];
     const u32 pieces = (cols + 7) / 8;
     const u64 all = (u64)rows * pieces, step = (u64)gridDim.x * kNormThreads;
-    const u64 row_bytes = ld * (type == 0 ? 4u : 2u);
-    const bool wide = (((uintptr_t)g | row_bytes) & 15u) == 0;
+    const u64 row_bytes = ld * Eight<kType>::kSize;
     double sum = 0.0;
-    for (u64 at = (u64)blockIdx.x * kNormThreads + threadIdx.x; at < all; at += step) {
-        const u32 r = (u32)(at / pieces), c = (u32)(at - (u64)r * pieces) * 8u;
-        float v[8];
-        read_eight(v, (const unsigned char *)g + r * row_bytes, c, cols, type, wide);
+    for (u64 at = (u64)blockIdx.x * kNormThreads + threadIdx.x; at < all; at += kAtOnce * step) {
+        Eight<kType> e[kAtOnce];
+        const unsigned char *row[kAtOnce];
+        u32 c[kAtOnce];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += (double)v[i] * (double)v[i];
+        for (u32 q = 0; q < kAtOnce; ++q) {
+            const u64 here = min(at + q * step, all - 1u);
+            const u32 r = (u32)(here / pieces);
+            row[q] = g + r * row_bytes;
+            c[q] = (u32)(here - (u64)r * pieces) * 8u;
+            e[q].load(row[q], c[q], cols);
+        }
+#pragma unroll
+        for (u32 q = 0; q < kAtOnce; ++q) {
+            if (at + q * step >= all) break;
+            float v[8];
+            e[q].numbers(v, row[q], c[q], cols);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += (double)v[i] * (double)v[i];
+        }
     }
     sum = block_sum<kNormThreads>(sum);
     if (threadIdx.x == 0) part[blockIdx.y * kNormBlocks + blockIdx.x] = sum;
@@ -184,7 +199,6 @@ k_norm(Members x, int type, u32 rows, u32 cols, u64 ld, double *__restrict__ par
 // ---- G into stored numbers, as it is and turned over --------------------------
 struct Start {
     Members x;
-    int type;
     u32 rows, cols;
     u64 ld;
     unsigned char *as_is, *turned;      // [rows] rows of cols, [cols] rows of rows
@@ -214,25 +228,27 @@ __device__ __forceinline__ int exponent_of(const double *part, u32 parts, float 
     return kLogX - exponent;
 }
 
-template <Operands kOf>
+template <Operands kOf, int kType>
 __global__ void __launch_bounds__(kNormThreads) k_start(Start g)
 {
     typedef Stored<kOf> S;
     __shared__ float tile[kSide][kSide + 1];
     const u32 r0 = blockIdx.y * kSide, c0 = blockIdx.x * kSide, member = blockIdx.z;
     const int e = exponent_of<kNormThreads>(g.part + member * kNormBlocks, g.parts, g.eps, blockIdx.x == 0 && blockIdx.y == 0 ? g.rho + member : nullptr);
-    const u64 row_bytes = g.ld * (g.type == 0 ? 4u : 2u);
+    const u64 row_bytes = g.ld * Eight<kType>::kSize;
     const unsigned char *x = (const unsigned char *)g.x.p[member];
-    const bool wide = (((uintptr_t)x | row_bytes) & 15u) == 0;
     const u32 row_a = S::row_bytes(g.cols), row_t = S::row_bytes(g.rows);
     unsigned char *as_is = g.as_is + member * g.as_is_stride, *turned = g.turned + member * g.turned_stride;
     // a piece of eight neighbours, the two pieces of a thread 32 rows apart
     const u32 r = threadIdx.x >> 3, c = (threadIdx.x & 7u) * 8u;
     float v[2][8];
+    Eight<kType> held[2];
+#pragma unroll
+    for (u32 h = 0; h < 2; ++h) held[h].load(x + min(r0 + r + 32 * h, g.rows - 1u) * row_bytes, c0 + c, g.cols);
 #pragma unroll
     for (u32 h = 0; h < 2; ++h) {
         const u32 row = r0 + r + 32 * h;
-        read_eight(v[h], x + (row < g.rows ? row : 0u) * row_bytes, c0 + c, row < g.rows ? g.cols : 0u, g.type, wide);
+        held[h].numbers(v[h], x + min(row, g.rows - 1u) * row_bytes, c0 + c, row < g.rows ? g.cols : 0u);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             v[h][i] = ldexpf(v[h][i], e);
@@ -342,21 +358,18 @@ __global__ void __launch_bounds__(T::kThreads) k_step(Product g)
     const float c_sum = kTriangle ? g.c_sum * rho * rho : g.c_sum * rho;
     if constexpr (kStep == kLast) {
         void *to = g.to.p[member];
-        const u32 size = g.type == 0 ? 4u : 2u;
-        const bool wide = (((uintptr_t)to | (g.ldo * size)) & (4u * size - 1u)) == 0;
         // the old weights of a row of fragments, on their way while the row before is stored; without a branch, as above
         f32x4 w[2][T::kFragsN];
-        const bool all_fours = wide && g.cols >= 4u;
         auto weights = [&](f32x4 (&to_w)[T::kFragsN], int i) {
             const float *row = (const float *)to + (u64)min(i0 + T::row_at(i), g.rows - 1u) * g.ldo;
-            if (all_fours) {
+            if (g.cols >= 4u) {
 #pragma unroll
-                for (int j = 0; j < T::kFragsN; ++j) to_w[j] = *(const f32x4 *)(row + min(j0 + T::col_at(j), (g.cols - 4u) & ~3u));
+                for (int j = 0; j < T::kFragsN; ++j) __builtin_memcpy(&to_w[j], row + min(j0 + T::col_at(j), g.cols - 4u), 16);
             }
 #pragma unroll
             for (int j = 0; j < T::kFragsN; ++j) {
                 const u32 col = j0 + T::col_at(j);
-                if (col < g.cols && (!all_fours || col + 4u > g.cols))
+                if (col < g.cols && col + 4u > g.cols)
 #pragma unroll
                     for (u32 q = 0; q < 4; ++q) to_w[j][q] = col + q < g.cols ? row[col + q] : 0.0f;
             }
@@ -375,16 +388,12 @@ __global__ void __launch_bounds__(T::kThreads) k_step(Product g)
 #pragma unroll
                     for (u32 q = 0; q < 4; ++q) t.sum[i][j][q] = fmaf(g.gain, t.sum[i][j][q], g.keep * w[i & 1][j][q]);
             }
-            const bool eights = g.type != 0 && (((uintptr_t)to | (g.ldo * size)) & 15u) == 0;
 #pragma unroll
             for (int j = 0; j < T::kFragsN; j += T::step_at(j)) {
-                const u32 col = j0 + T::col_at(j), next = j0 + T::col_at(T::next_to(j));
-                if (T::wide_at(j) && eights && col + 8u <= g.cols) {
-                    write_eight(to, first + col, g.type, t.sum[i][j], t.sum[i][T::next_to(j)]);
-                } else {
-                    if (col < g.cols) write_four(to, first + col, g.type, t.sum[i][j], g.cols - col, wide);
-                    if (T::wide_at(j) && next < g.cols) write_four(to, first + next, g.type, t.sum[i][T::next_to(j)], g.cols - next, wide);
-                }
+                const u32 col = j0 + T::col_at(j);
+                if (col >= g.cols) continue;
+                if (T::wide_at(j)) write_eight(to, first + col, g.type, t.sum[i][j], t.sum[i][T::next_to(j)], g.cols - col);
+                else write_four(to, first + col, g.type, t.sum[i][j], g.cols - col);
             }
         }
         return;
@@ -495,7 +504,6 @@ constexpr int kNarrowThreads = 512;
 
 struct Narrow {
     Members x;                  // k_narrow_start: G
-    int type;
     u32 rows, cols;             // of G
     u64 ld;
     const double *norm;
@@ -565,7 +573,7 @@ __device__ __forceinline__ void write_part(const T &gram, float *to)
     gram.each([&](u32 r, u32 c, const f32x4 &sum) { *(f32x4 *)(to + r * kSide + c) = sum; });
 }
 
-template <Operands kOf>
+template <Operands kOf, int kType>
 __global__ void __launch_bounds__(kNarrowThreads) k_narrow_start(Narrow g)
 {
     typedef Stored<kOf> S;
@@ -576,9 +584,8 @@ __global__ void __launch_bounds__(kNarrowThreads) k_narrow_start(Narrow g)
     const bool over = g.rows > g.cols;
     const u32 m = over ? g.cols : g.rows, n = over ? g.rows : g.cols;
     const int e = exponent_of<kNarrowThreads>(g.norm + member * kNormBlocks, g.norm_parts, g.eps, run == 0 ? g.rho + member : nullptr);
-    const u64 row_bytes = g.ld * (g.type == 0 ? 4u : 2u);
+    const u64 row_bytes = g.ld * Eight<kType>::kSize;
     const u8 *x = (const u8 *)g.x.p[member];
-    const bool wide = (((uintptr_t)x | row_bytes) & 15u) == 0;
     u8 *xt = g.xt_next + member * g.xt_stride;
     typename B::T gram;
     gram.clear();
@@ -589,7 +596,9 @@ __global__ void __launch_bounds__(kNarrowThreads) k_narrow_start(Narrow g)
             const u32 r = threadIdx.x >> 3, c = (threadIdx.x & 7u) * 8u;
             const u32 row = over ? n0 + r : r, col = over ? c : n0 + c;
             float v[8];
-            read_eight(v, x + (row < g.rows ? row : 0u) * row_bytes, col, row < g.rows ? g.cols : 0u, g.type, wide);
+            Eight<kType> held;
+            held.load(x + min(row, g.rows - 1u) * row_bytes, col, g.cols);
+            held.numbers(v, x + min(row, g.rows - 1u) * row_bytes, col, row < g.rows ? g.cols : 0u);
 #pragma unroll
             for (int i = 0; i < 8; ++i) (over ? tile[c + i][r] : tile[r][c + i]) = ldexpf(v[i], e);
         }
@@ -712,8 +721,6 @@ __global__ void __launch_bounds__(kNarrowThreads) k_narrow(Narrow g)
         B::multiply(t, lds[1], lds[2]);
         if (g.last) {
             void *to = g.to.p[member];
-            const u32 size = g.to_type == 0 ? 4u : 2u;
-            const bool wide = !over && (((uintptr_t)to | (g.ldo * size)) & (4u * size - 1u)) == 0;
             t.each([&](u32 r, u32 c, const f32x4 &sum) {
                 if (r >= m || n0 + c >= n) return;
                 f32x4 v = sum * (g.c_last * rho);
@@ -725,7 +732,7 @@ __global__ void __launch_bounds__(kNarrowThreads) k_narrow(Narrow g)
                     for (u32 q = 0; q < 4; ++q)
                         if (q < have) v[q] = fmaf(g.gain, v[q], g.keep * w[at + q * next]);
                 }
-                if (!over) write_four(to, at, g.to_type, v, have, wide);
+                if (!over) write_four(to, at, g.to_type, v, have);
                 else
 #pragma unroll
                     for (u32 q = 0; q < 4; ++q)
@@ -954,7 +961,6 @@ int iterate_narrow(const Members &x, int type, u64 ldx, const Shape &s, u32 memb
     float *part[2] = {p.part, p.part + (u64)members * plan.runs * kSide * kSide};
     Narrow g{};
     g.x = x;
-    g.type = type;
     g.rows = s.rows;
     g.cols = s.cols;
     g.ld = ldx;
@@ -976,7 +982,9 @@ int iterate_narrow(const Members &x, int type, u64 ldx, const Shape &s, u32 memb
     g.gain = target.gain;
     g.keep = target.keep;
     g.update = target.update;
-    k_narrow_start<kOf><<<grid, kNarrowThreads, 0, stream>>>(g);
+    if (type == RTOPK_F32) k_narrow_start<kOf, RTOPK_F32><<<grid, kNarrowThreads, 0, stream>>>(g);
+    else if (type == RTOPK_BF16) k_narrow_start<kOf, RTOPK_BF16><<<grid, kNarrowThreads, 0, stream>>>(g);
+    else k_narrow_start<kOf, RTOPK_F16><<<grid, kNarrowThreads, 0, stream>>>(g);
     if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
     double h = 1.0 / s.m();
     for (u32 i = 0; i < steps; ++i) {
@@ -1011,10 +1019,12 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
     typedef Stored<kOf> S;
     if (is_narrow(s)) return iterate_narrow<kOf>(x, type, ldx, s, members, norm_parts, steps, abc, eps, p, target, stream);
     const u32 m = s.m(), n = s.n();
-    const Start start{x, type, s.rows, s.cols, ldx, s.over() ? p.xt[0] : p.x[0], s.over() ? p.x[0] : p.xt[0],
+    const Start start{x, s.rows, s.cols, ldx, s.over() ? p.xt[0] : p.x[0], s.over() ? p.x[0] : p.xt[0],
                       s.over() ? p.xt_stride : p.x_stride, s.over() ? p.x_stride : p.xt_stride, p.norm, norm_parts, eps, p.rho};
     const dim3 grid((S::padded(s.cols) + kSide - 1) / kSide, (S::padded(s.rows) + kSide - 1) / kSide, members);
-    k_start<kOf><<<grid, kNormThreads, 0, stream>>>(start);
+    if (type == RTOPK_F32) k_start<kOf, RTOPK_F32><<<grid, kNormThreads, 0, stream>>>(start);
+    else if (type == RTOPK_BF16) k_start<kOf, RTOPK_BF16><<<grid, kNormThreads, 0, stream>>>(start);
+    else k_start<kOf, RTOPK_F16><<<grid, kNormThreads, 0, stream>>>(start);
     if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
     double gram_cost, square_cost, next_cost;
     const GramPlan gram = plan_gram<kOf>(members, s, &gram_cost);
@@ -1204,7 +1214,10 @@ extern "C" int rtopk_orthogonalize(uint32_t count, const void *const *x, int typ
             to.to.p[i] = out[first + i];
         }
         const u32 parts = norm_blocks((u64)s.rows * s.cols, members);
-        k_norm<<<dim3(parts, members), kNormThreads, 0, stream>>>(from, type, s.rows, s.cols, ldx, p.norm);
+        const dim3 grid(parts, members);
+        if (type == RTOPK_F32) k_norm<RTOPK_F32><<<grid, kNormThreads, 0, stream>>>(from, s.rows, s.cols, ldx, p.norm);
+        else if (type == RTOPK_BF16) k_norm<RTOPK_BF16><<<grid, kNormThreads, 0, stream>>>(from, s.rows, s.cols, ldx, p.norm);
+        else k_norm<RTOPK_F16><<<grid, kNormThreads, 0, stream>>>(from, s.rows, s.cols, ldx, p.norm);
         if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
         if (const int rc = iterate(products, from, type, ldx, s, members, parts, steps, coefficients, largest_p, eps, p, to, stream)) return rc;
     }
