@@ -732,7 +732,7 @@ struct Cut {
     u64 at = 0;
     template <class P> P *take(u64 bytes)
     {
-        P *p = (P *)(base + at);
+        P *p = base ? (P *)(base + at) : nullptr;     // (without a base only the size is asked for)
         at += align_up(bytes, 256);
         return p;
     }

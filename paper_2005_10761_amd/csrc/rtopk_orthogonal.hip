@@ -843,7 +843,11 @@ u64 cut(void *base, u32 count, const Shape &s, bool direction, Parts &p)
     const u32 members = std::min(count, kMembers);
     unsigned char *at = (unsigned char *)base;
     u64 used = 0;
-    auto take = [&](u64 bytes) { unsigned char *q = at + used; used += align_up(bytes, 256); return q; };
+    auto take = [&](u64 bytes) {
+        unsigned char *q = at ? at + used : nullptr;            // (without a base only the size is asked for)
+        used += align_up(bytes, 256);
+        return q;
+    };
     p.x_stride = align_up((u64)s.m() * S::row_bytes(s.n()), 256);
     p.xt_stride = align_up((u64)s.n() * S::row_bytes(s.m()), 256);
     p.square_stride = align_up((u64)s.m() * S::row_bytes(s.m()), 256);
