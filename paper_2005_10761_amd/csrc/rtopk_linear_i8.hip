@@ -167,15 +167,22 @@ struct ColumnsToQuantize {
     u32 *most;                  // [runs][cols]
     float *sums;                // [runs][cols], or null
     float *total;               // [cols], or null
+    u32 blocks;                 // of kTurnRows rows that a workgroup of the second turns over
+};
+// one matrix, or two of one type in the same launches (blockIdx.z): a layer's backward quantises dy and x
+struct Columns {
+    ColumnsToQuantize of[2];
 };
 
 template <int kType>
-__global__ void __launch_bounds__(kQuantizeThreads) k_column_most(ColumnsToQuantize g)
+__global__ void __launch_bounds__(kQuantizeThreads) k_column_most(Columns both)
 {
+    const ColumnsToQuantize &g = both.of[blockIdx.z];
     constexpr u32 kWaves = kQuantizeThreads / kWave, kAtOnce = 8;
     __shared__ u32 most[kWaves - 1][kGroup];
     __shared__ float sums[kWaves - 1][kGroup];
     const u32 lane = lane_id(), wave = threadIdx.x / kWave, c = blockIdx.x * kGroup + lane * 8u;
+    if (blockIdx.x * kGroup >= g.cols || blockIdx.y >= g.runs) return;        // (the other matrix is larger)
     const u32 r0 = blockIdx.y * g.run, r1 = min(r0 + g.run, g.rows);
     const u64 row_bytes = g.ldx * Eight<kType>::kSize;
     u32 largest[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -224,14 +231,16 @@ __global__ void __launch_bounds__(kQuantizeThreads) k_column_most(ColumnsToQuant
 constexpr u32 kTurnRows = 128, kMostBlocks = 4;
 
 template <int kType>
-__global__ void __launch_bounds__(kQuantizeThreads) k_quantize_columns(ColumnsToQuantize g, u32 blocks)
+__global__ void __launch_bounds__(kQuantizeThreads) k_quantize_columns(Columns both)
 {
+    const ColumnsToQuantize &g = both.of[blockIdx.z];
     constexpr u32 kParts = kQuantizeThreads / kWave;
     __shared__ float scale[kWave];
     __shared__ u32 most[kParts][kWave];
     __shared__ double sums[kParts][kWave];
     __shared__ u32 turned[kWave][kTurnRows / 4 + 1];
-    const u32 lane = lane_id(), wave = threadIdx.x / kWave, c0 = blockIdx.x * kWave, first = blockIdx.y * blocks * kTurnRows;
+    const u32 lane = lane_id(), wave = threadIdx.x / kWave, c0 = blockIdx.x * kWave, blocks = g.blocks, first = blockIdx.y * blocks * kTurnRows;
+    if (c0 >= g.cols || first >= g.fill) return;
     const bool totals = g.total && first == 0;
     const u64 row_bytes = g.ldx * Eight<kType>::kSize;
     const u32 piece = threadIdx.x & 7u, quad = threadIdx.x >> 3, c = c0 + 8u * piece;       // columns c .. c + 7 of rows 4 quad .. + 3
@@ -700,26 +709,38 @@ int quantize_rows(const void *x, int type, u32 rows, u32 cols, u64 ldx, signed c
 u64 column_scratch(u32 rows, u32 cols, bool sums) { return align_up((u64)runs_of(rows, cols) * cols * (sums ? 8 : 4), 256); }
 
 template <int kType>
-int launch_columns(const ColumnsToQuantize &g, hipStream_t stream)
+int launch_columns(const Columns &c, u32 count, hipStream_t stream)
 {
-    k_column_most<kType><<<dim3((g.cols + kGroup - 1) / kGroup, g.runs), kQuantizeThreads, 0, stream>>>(g);
+    dim3 most(1, 1, count), turn(1, 1, count);
+    for (u32 i = 0; i < count; ++i) {
+        const ColumnsToQuantize &g = c.of[i];
+        most.x = std::max(most.x, (g.cols + kGroup - 1) / kGroup);
+        most.y = std::max(most.y, g.runs);
+        turn.x = std::max(turn.x, (g.cols + kWave - 1) / kWave);
+        turn.y = std::max(turn.y, ((g.fill + kTurnRows - 1) / kTurnRows + g.blocks - 1) / g.blocks);
+    }
+    k_column_most<kType><<<most, kQuantizeThreads, 0, stream>>>(c);
     if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
-    // as many blocks for a workgroup (each of which takes the runs together) as leave four workgroups a unit
-    const u32 groups = (g.cols + kWave - 1) / kWave, all = (g.fill + kTurnRows - 1) / kTurnRows;
-    const u32 blocks = std::max(1u, std::min(kMostBlocks, (u32)((u64)groups * all / (4 * kUnits))));
-    k_quantize_columns<kType><<<dim3(groups, (all + blocks - 1) / blocks), kQuantizeThreads, 0, stream>>>(g, blocks);
+    k_quantize_columns<kType><<<turn, kQuantizeThreads, 0, stream>>>(c);
     return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_EHIP;
 }
 
-int quantize_columns(const void *x, int type, u32 rows, u32 cols, u64 ldx, signed char *q, u64 ldq, u32 fill, float *scale,
-                     float *total, void *scratch, hipStream_t stream)
+ColumnsToQuantize columns_of(const void *x, u32 rows, u32 cols, u64 ldx, signed char *q, u64 ldq, u32 fill, float *scale,
+                             float *total, void *scratch)
 {
     const u32 runs = runs_of(rows, cols);
     u32 *most = (u32 *)scratch;
-    const ColumnsToQuantize g{x, ldx, rows, cols, fill, run_rows(rows, cols), runs, q, ldq, scale, most,
-                              total ? (float *)(most + (u64)runs * cols) : nullptr, total};
-    return type == RTOPK_F32 ? launch_columns<RTOPK_F32>(g, stream)
-           : type == RTOPK_BF16 ? launch_columns<RTOPK_BF16>(g, stream) : launch_columns<RTOPK_F16>(g, stream);
+    // as many blocks for a workgroup (each of which takes the runs together) as leave four workgroups a unit
+    const u32 groups = (cols + kWave - 1) / kWave, all = (fill + kTurnRows - 1) / kTurnRows;
+    const u32 blocks = std::max(1u, std::min(kMostBlocks, (u32)((u64)groups * all / (4 * kUnits))));
+    return ColumnsToQuantize{x, ldx, rows, cols, fill, run_rows(rows, cols), runs, q, ldq, scale, most,
+                             total ? (float *)(most + (u64)runs * cols) : nullptr, total, blocks};
+}
+
+int quantize_columns(const Columns &c, u32 count, int type, hipStream_t stream)
+{
+    return type == RTOPK_F32 ? launch_columns<RTOPK_F32>(c, count, stream)
+           : type == RTOPK_BF16 ? launch_columns<RTOPK_BF16>(c, count, stream) : launch_columns<RTOPK_F16>(c, count, stream);
 }
 
 bool workspace_ok(const void *p, u64 bytes, u64 need) { return need == 0 || (p && ((uintptr_t)p & 255u) == 0 && bytes >= need); }
@@ -756,7 +777,7 @@ u64 cut_linear(void *base, u32 m, u32 k, u32 n, LinearParts &p)
 struct BackwardParts {
     signed char *dy, *dy_turned, *x_turned;
     float *dy_scale, *dy_turned_scale, *x_turned_scale;
-    void *scratch, *part;
+    void *dy_scratch, *x_scratch, *part;
 };
 u64 cut_backward(void *base, u32 m, u32 k, u32 n, BackwardParts &p)
 {
@@ -767,7 +788,8 @@ u64 cut_backward(void *base, u32 m, u32 k, u32 n, BackwardParts &p)
     p.dy_scale = cut.take<float>(4ull * m);
     p.dy_turned_scale = cut.take<float>(4ull * n);
     p.x_turned_scale = cut.take<float>(4ull * k);
-    p.scratch = cut.take<void>(std::max(column_scratch(m, n, true), column_scratch(m, k, false)));
+    p.dy_scratch = cut.take<void>(column_scratch(m, n, true));
+    p.x_scratch = cut.take<void>(column_scratch(m, k, false));
     p.part = cut.take<void>(std::max(part_bytes(m, k, n), part_bytes(n, k, m)));
     return cut.at;
 }
@@ -796,7 +818,8 @@ extern "C" int rtopk_quantize_i8(const void *x, int type, uint64_t rows, uint64_
         k_zero<<<1, 256, 0, stream>>>(scale, 1, (u32)cols, cols);
         return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_EHIP;
     }
-    return quantize_columns(x, type, (u32)rows, (u32)cols, ldx, q, ldq, (u32)rows, scale, nullptr, workspace, stream);
+    const Columns c{{columns_of(x, (u32)rows, (u32)cols, ldx, q, ldq, (u32)rows, scale, nullptr, workspace), {}}};
+    return quantize_columns(c, 1, type, stream);
 }
 
 extern "C" int rtopk_matmul_i8_workspace_bytes(uint64_t m, uint64_t n, uint64_t k, uint64_t *bytes)
@@ -888,12 +911,9 @@ extern "C" int rtopk_linear_i8_backward(const void *dy, const void *x, int type,
     }
     if (!dw) return RTOPK_OK;
     const u64 ld = filled((u32)m);
-    if (const int rc = quantize_columns(dy, type, (u32)m, (u32)n, lddy, p.dy_turned, ld, (u32)ld, p.dy_turned_scale, db, p.scratch,
-                                        stream))
-        return rc;
-    if (const int rc = quantize_columns(x, type, (u32)m, (u32)k, ldx, p.x_turned, ld, (u32)ld, p.x_turned_scale, nullptr, p.scratch,
-                                        stream))
-        return rc;
+    const Columns c{{columns_of(dy, (u32)m, (u32)n, lddy, p.dy_turned, ld, (u32)ld, p.dy_turned_scale, db, p.dy_scratch),
+                     columns_of(x, (u32)m, (u32)k, ldx, p.x_turned, ld, (u32)ld, p.x_turned_scale, nullptr, p.x_scratch)}};
+    if (const int rc = quantize_columns(c, 2, type, stream)) return rc;
     return run_product(Scaled{p.dy_turned, p.x_turned, ld, ld, (u32)n, (u32)k, (u32)m, p.dy_turned_scale, p.x_turned_scale, nullptr,
                               dw, lddw, RTOPK_F32, 0, 0, nullptr},
                        p.part, stream);
