@@ -438,11 +438,11 @@ __global__ void __launch_bounds__(256) k_product_join(Scaled g)
 // ---------------------------------------------------------------------------
 // Few tokens: one read of the weights. A workgroup has 16 channels; its wavefronts share the contraction and add up in
 // LDS. A lane's 16 bytes of a row of weights are its part of the instruction's operand as they come, at any alignment; the
-// tokens are the other operand, kTokens x 16 of them. Bound by the read of the weights: 16384 x 4096 with 13 tokens 17.6 us,
+// tokens are the other operand, up to 16 of them. Bound by the read of the weights: 16384 x 4096 with 13 tokens 17.6 us,
 // 3.8 TB/s; 10000 x 1500 with one token, quantised in the same launch, 6.2 us, of which a launch of nothing is 2.
 // ---------------------------------------------------------------------------
-constexpr u32 kFewTokens = 64;          // at most
-constexpr u32 kInOne = 8192;            // numbers of x up to which every workgroup quantises them for itself (one launch less)
+constexpr u32 kFewTokens = 16;          // at most: what one instruction takes
+constexpr u32 kInOne = 8192;            // numbers of x that a workgroup can quantise for itself (one launch less)
 
 struct Few {
     Scaled s;                           // a: quantised tokens, or null
@@ -451,7 +451,7 @@ struct Few {
 };
 
 // kType: of x, or -1 where it is quantised already
-template <int kWaves, int kTokens, int kType>
+template <int kWaves, int kType>
 __global__ void __launch_bounds__(kWaves * kWave) k_few(Few f)
 {
     constexpr bool kQuantize = kType >= 0;
@@ -460,14 +460,12 @@ __global__ void __launch_bounds__(kWaves * kWave) k_few(Few f)
     const u32 lane = lane_id(), wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
     const u32 channel = blockIdx.x * 16u + (lane & 15u), piece = (lane >> 4) * 16u;
     extern __shared__ __align__(16) unsigned char lds[];
-    __shared__ float token_scale[kTokens * 16];
-    __shared__ u32 most[kTokens * 16];
+    __shared__ float token_scale[kFewTokens];
+    __shared__ u32 most[kFewTokens];
     const u32 steps = (g.k + 63u) / 64u;
     const u32 each = (steps + kWaves - 1) / kWaves, from = min(wave * each, steps), to = min(from + each, steps);
     const unsigned char *w = (const unsigned char *)g.b + (u64)min(channel, g.n - 1u) * g.ldb;
-    i32x4 sum[kTokens], held[kBatch];
-#pragma unroll
-    for (int t = 0; t < kTokens; ++t) sum[t] = i32x4{0, 0, 0, 0};
+    i32x4 sum{0, 0, 0, 0}, held[kBatch];
     const u32 whole = min(to, g.k / 64u);
     auto fetch = [&](u32 s) {
         if (s + kBatch <= whole) {
@@ -504,7 +502,7 @@ __global__ void __launch_bounds__(kWaves * kWave) k_few(Few f)
             if (at >= all) c[h] = pieces * 8u;              // nothing: zeros
             held_x[h].load(x + token[h] * row_bytes, c[h], g.k);
         }
-        if (threadIdx.x < kTokens * 16) most[threadIdx.x] = 0u;
+        if (threadIdx.x < kFewTokens) most[threadIdx.x] = 0u;
         __syncthreads();
 #pragma unroll
         for (u32 h = 0; h < kHeld; ++h) {
@@ -548,35 +546,23 @@ __global__ void __launch_bounds__(kWaves * kWave) k_few(Few f)
 #pragma unroll
         for (u32 q = 0; q < kBatch; ++q) {
             if (s + q >= to) break;
-#pragma unroll
-            for (int t = 0; t < kTokens; ++t) {
-                const u32 token = min(16u * t + (lane & 15u), g.m - 1u), at = (s + q) * 64u + piece;
-                const i32x4 x = kQuantize ? *(const i32x4 *)(lds + token * row + at) : *(const i32x4 *)(g.a + (u64)token * g.lda + at);
-                sum[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now[q], x, sum[t], 0, 0, 0);
-            }
+            const u32 token = min(lane & 15u, g.m - 1u), at = (s + q) * 64u + piece;
+            const i32x4 x = kQuantize ? *(const i32x4 *)(lds + token * row + at) : *(const i32x4 *)(g.a + (u64)token * g.lda + at);
+            sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(now[q], x, sum, 0, 0, 0);
         }
     }
-    // lane l: token l % 16 of each sixteen, channels 4 (l / 16) .. + 3
+    // lane l: token l % 16, channels 4 (l / 16) .. + 3
     __syncthreads();
     i32x4 *part = (i32x4 *)lds;
-    if (wave) {
-#pragma unroll
-        for (int t = 0; t < kTokens; ++t) part[((wave - 1) * kTokens + t) * kWave + lane] = sum[t];
-    }
+    if (wave) part[(wave - 1) * kWave + lane] = sum;
     __syncthreads();
     if (wave) return;
-    const u32 col = blockIdx.x * 16u + 4u * (lane >> 4);
-    if (col >= g.n) return;
+    const u32 col = blockIdx.x * 16u + 4u * (lane >> 4), token = lane & 15u;
+    if (col >= g.n || token >= g.m) return;
     const Four four = channels(g, col);
-#pragma unroll
-    for (int t = 0; t < kTokens; ++t) {
-        // (a sum of kMostSteps steps stays below 2^31: longer contractions do not come here)
-        for (int o = 0; o < kWaves - 1; ++o) sum[t] += part[(o * kTokens + t) * kWave + lane];
-        const u32 token = 16u * t + (lane & 15u);
-        if (token < g.m)
-            write_scaled(g, token, col, f32x4{(float)sum[t][0], (float)sum[t][1], (float)sum[t][2], (float)sum[t][3]}, token_scale[token],
-                         four);
-    }
+    // (a sum of kMostSlices slices stays below 2^31: longer contractions do not come here)
+    for (int o = 0; o < kWaves - 1; ++o) sum += part[o * kWave + lane];
+    write_scaled(g, token, col, f32x4{(float)sum[0], (float)sum[1], (float)sum[2], (float)sum[3]}, token_scale[token], four);
 }
 
 // no tokens: the weights' gradient is zero
@@ -638,28 +624,34 @@ void launch_product(const Scaled &g, const Plan &p, bool whole, hipStream_t stre
     else k_product<Fours, true><<<grid, Fours::kThreads, 0, stream>>>(g);
 }
 
-template <int kWaves, int kTokens>
+template <int kWaves>
 void launch_few(const Few &f, int type, hipStream_t stream)
 {
-    const u32 blocks = (f.s.n + 15) / 16, sums = (kWaves - 1) * kTokens * kWave * 16;
+    const u32 blocks = (f.s.n + 15) / 16, sums = (kWaves - 1) * kWave * 16;
     const u32 tokens = f.s.a ? 0 : f.s.m * ((f.s.k + 63) / 64 * 64 + 16);
     const u32 lds = std::max(sums, tokens);
-    if (f.s.a) k_few<kWaves, kTokens, -1><<<blocks, kWaves * kWave, lds, stream>>>(f);
-    else if (type == RTOPK_F32) k_few<kWaves, kTokens, RTOPK_F32><<<blocks, kWaves * kWave, lds, stream>>>(f);
-    else if (type == RTOPK_BF16) k_few<kWaves, kTokens, RTOPK_BF16><<<blocks, kWaves * kWave, lds, stream>>>(f);
-    else k_few<kWaves, kTokens, RTOPK_F16><<<blocks, kWaves * kWave, lds, stream>>>(f);
+    if (f.s.a) k_few<kWaves, -1><<<blocks, kWaves * kWave, lds, stream>>>(f);
+    else if (type == RTOPK_F32) k_few<kWaves, RTOPK_F32><<<blocks, kWaves * kWave, lds, stream>>>(f);
+    else if (type == RTOPK_BF16) k_few<kWaves, RTOPK_BF16><<<blocks, kWaves * kWave, lds, stream>>>(f);
+    else k_few<kWaves, RTOPK_F16><<<blocks, kWaves * kWave, lds, stream>>>(f);
 }
 
+// us with the weights in memory, k x n = 4096 x 16384 / 1504 x 10000 / 4096 x 4096 / 8192 x 1024: one token 15 / 7 / 8 / 8, by
+// tiles 20 / 11 / 13 / 14; sixteen 23 / 10 / 11 / 13, by tiles 20 / 10 / 13 / 16. (Two and four instructions' worth of
+// tokens were slower than tiles: 32 tokens 30 / 12 / 13 / 17, by tiles 21 / 11 / 14 / 16.)
 bool few_tokens(u32 m, u32 k) { return m <= kFewTokens && k <= kMostSlices * kSlice; }
-bool in_one(u32 m, u32 k) { return few_tokens(m, k) && (u64)m * k <= kInOne; }
+// Every workgroup of a unit quantises the tokens again: 16 x 500 by 30000 channels (eight workgroups a unit) 19 us, in a
+// launch of its own 10; but 1 x 4096 by 16384 (four) 15, and with that launch 20.
+bool in_one(u32 m, u32 k, u32 n)
+{
+    return few_tokens(m, k) && (u64)m * k <= kInOne && (u64)m * k * ((n + 16 * kUnits - 1) / (16 * kUnits)) <= 20000;
+}
 
-// fewer than two workgroups a unit: each has sixteen wavefronts
+// Up to a workgroup a unit each has sixteen wavefronts (4 x 8192 by 1024 channels 12 us, with four wavefronts 15), then four (1 x
+// 4096 by 8000 channels 9 us, with sixteen 14).
 int run_few(const Few &f, int type, hipStream_t stream)
 {
-    const bool many = f.s.n >= 2 * kUnits * 16;
-    if (f.s.m <= 16) many ? launch_few<4, 1>(f, type, stream) : launch_few<16, 1>(f, type, stream);
-    else if (f.s.m <= 32) many ? launch_few<4, 2>(f, type, stream) : launch_few<16, 2>(f, type, stream);
-    else many ? launch_few<4, 4>(f, type, stream) : launch_few<8, 4>(f, type, stream);
+    f.s.n > kUnits * 16 ? launch_few<4>(f, type, stream) : launch_few<16>(f, type, stream);
     return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_EHIP;
 }
 
@@ -774,7 +766,7 @@ struct LinearParts {
 u64 cut_linear(void *base, u32 m, u32 k, u32 n, LinearParts &p)
 {
     Cut cut{(unsigned char *)base};
-    if (in_one(m, k)) return 0;
+    if (in_one(m, k, n)) return 0;
     p.x = cut.take<signed char>(m * filled(k));
     p.x_scale = cut.take<float>(4ull * m);
     p.part = cut.take<void>(few_tokens(m, k) ? 0 : part_bytes(m, n, k));
@@ -873,7 +865,7 @@ extern "C" int rtopk_linear_i8(const void *x, int type, uint64_t m, uint64_t k, 
     cut_linear(workspace, (u32)m, (u32)k, (u32)n, p);
     const u64 ld = filled((u32)k);
     const Scaled g{p.x, w, ld, ldw, (u32)m, (u32)n, (u32)k, p.x_scale, w_scale, bias, out, ldo, out_type, 0, 0, nullptr};
-    if (in_one((u32)m, (u32)k)) return run_few(Few{g, x, ldx}, type, stream);
+    if (in_one((u32)m, (u32)k, (u32)n)) return run_few(Few{g, x, ldx}, type, stream);
     if (const int rc = quantize_rows(x, type, (u32)m, (u32)k, ldx, p.x, ld, (u32)ld, p.x_scale, stream)) return rc;
     return few_tokens((u32)m, (u32)k) ? run_few(Few{g, nullptr, 0}, type, stream) : run_product(g, p.part, stream);
 }
