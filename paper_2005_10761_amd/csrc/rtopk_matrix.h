@@ -80,7 +80,7 @@ __device__ __forceinline__ i32x4 cut_piece(const i32x4 &v, u32 at, u32 bytes)
 // 64 and 128 go to small results, on 2 x 4 wavefronts too: a slice of 64 x 64 takes 0.3 us alone on its unit, of which its
 // products are 0.08: the rest is one barrier and two trips to LDS one after the other (six stages in the place of three
 // change nothing, so it is not the loads). 192 is for pairs and for results where 256 leaves units without a tile; 160 was
-// no better than 128 or 192 on seven of eight shapes.
+// slower than the best of these on ten of eleven shapes (four squares of 1500: 1% of the call faster).
 //
 // How the rows of a wavefront's operands are dealt to its instructions, so that what a lane ends up with is stored in wide pieces:
 // kInOrder: fragment i has rows 16 i ..; kRuns: of A, a lane's rows are neighbours (eight, or four, or two of them: they
