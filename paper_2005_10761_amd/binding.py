@@ -559,9 +559,9 @@ def orthogonalize_workspace_bytes(count: int, rows: int, cols: int, products: st
 def orthogonalize(xs, outs, steps: Optional[int] = None, coefficients=QUINTIC, eps: float = 1e-7,
                   products: Optional[str] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """rtopk_orthogonalize: Newton-Schulz orthogonalisation of every matrix of the list ``xs`` (equal shapes, types and
-    row distances) into ``outs`` (which may be ``xs``). ``products``: "pairs" (as exact as binary32) or "halves" (a
-    third of the time); None takes halves for bfloat16 outputs, whose rounding is more than what they lose, and pairs
-    for others."""
+    row distances) into ``outs`` (which may be ``xs``). ``products``: "pairs" (None too: 22 bits between the
+    products, about as exact as binary32), or "halves" (11 bits, down to a third of the time), whose error grows with what the strongest directions
+    have over the others: beyond a bfloat16 result's own rounding from about 30 times in each element on."""
     count = len(xs)
     if count < 1 or len(outs) != count:
         raise ValueError("xs and outs must have the same length >= 1")
@@ -571,7 +571,7 @@ def orthogonalize(xs, outs, steps: Optional[int] = None, coefficients=QUINTIC, e
         _matrix(b, "out", (out.dtype,) if out.dtype in _TYPES else _TYPES)
         if a.shape != x.shape or b.shape != x.shape or _ld(a) != _ld(x) or _ld(b) != _ld(out):
             raise ValueError("all matrices must have one shape, and one distance of their rows")
-    products = products or ("halves" if out.dtype == torch.bfloat16 else "pairs")
+    products = products or "pairs"
     rows, cols = x.shape
     number, abc = _coefficients(coefficients, steps)
     ws, ws_bytes, held = _workspace(workspace, 0 if workspace is not None else
