@@ -391,7 +391,10 @@ int rtopk_linear_i8_backward(const void *dy, const void *x, int type,
  *        singular values s that start in [0, 1] can pass 7.5 (or a + b s^2 +
  *        c s^4 can pass 30), the call returns RTOPK_EINVAL
  * eps    >= 0. A matrix of zeros gives zeros (eps = 0 too); one that holds an
- *        infinity or a not-a-number gives NaN everywhere
+ *        infinity or a not-a-number gives NaN everywhere. |G|_F may be far below
+ *        eps: down to 2^-100 eps the result keeps its bits where a is not
+ *        much smaller than |b| and |c| (A is computed to 2^-22, or 2^-11, of
+ *        what its diagonal would be without eps)
  * workspace  device, 256-byte aligned, >= rtopk_orthogonalize_workspace_bytes
  */
 #define RTOPK_PRODUCTS_PAIRS 0

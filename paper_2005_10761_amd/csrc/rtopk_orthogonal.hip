@@ -24,15 +24,18 @@
 // Numbers between the products are halves (11 bits; bfloat16, in common use
 // here, has 8) or pairs of halves (22 bits), times a power of two that puts
 // what the iteration can hold into a half's range: its singular values are
-// bounded by the coefficients, which the host checks before it launches.
+// bounded by the coefficients, which the host checks before it launches. Where they
+// are small (the norm is below eps, or the coefficients shrink them), each
+// step's X has a power of two of its own, from a bound that follows them.
 // Products are summed in binary32. |G|_F is summed in binary64. Of the division by it
 // only the power of two is applied to G (that is exact); the rest, between 1 and
-// 2, goes into the first step's coefficients, so that a bfloat16 G enters the
-// products unrounded.
+// 2 (or less, by eps), goes into the first step's coefficients, so that a
+// bfloat16 G enters the products unrounded.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cmath>
+#include <cstring>
 
 #include "../../include/rtopk.h"
 #include "rtopk_direction.h"
@@ -44,7 +47,14 @@ namespace rtopk {
 // entries of Q up to kMostP (or, less k, its double) stay finite
 constexpr int kLogX = 12, kLogD = 10;
 constexpr double kMostX = 7.5, kMostP = 30.0;
+constexpr int kMostDown = 100;          // X is scaled by no less than 2^-100: quotients of two scales are binary32
 struct Members { void *p[kMembers]; };
+
+constexpr u32 kMostSteps = 64;
+struct Steps {
+    u32 count;
+    float abc[kMostSteps][3];
+};
 
 // Four lanes with four halves each: lane i gets the i-th of all four.
 __device__ __forceinline__ uint2 turned_quad(uint2 d)
@@ -207,24 +217,50 @@ struct Start {
     const double *part;
     u32 parts;
     float eps;
-    float *rho;                         // what is left of the division, for the first step
+    Steps steps;
+    float *scale;                       // of X before each step and after the last, see exponent_of
 };
 
 constexpr u32 kSide = 64;               // k_start's and k_join's blocks, and what a narrow matrix is at most
 
-// From the parts of a matrix's norm: the exponent that its elements are moved by, and (to *rho, where there is one) what is
-// left of the division. By all kThreads threads of a workgroup.
+__device__ __forceinline__ float read_lane(float v, u32 lane)
+{
+    return __uint_as_float((u32)__builtin_amdgcn_readlane((int)__float_as_uint(v), (int)lane));
+}
+
+// From the parts of a matrix's norm: the exponent that its elements are moved by, and (where there is a `scale`) what X is its
+// stored numbers times, but for 2^-kLogX, before step i: scale[i * kMembers]. Before the first that is what is left of the division; then
+// it is 1 unless a bound on the singular values is below a half, which then lie in a half's range as they do elsewhere
+// (without it a norm of 10^-4 eps lost 5 of the 22 bits of pairs, one of 10^-8 eps all of them).
+// By all kThreads threads of a workgroup.
 template <int kThreads>
-__device__ __forceinline__ int exponent_of(const double *part, u32 parts, float eps, float *rho)
+__device__ __forceinline__ int exponent_of(const double *part, u32 parts, float eps, const Steps &steps, float *scale)
 {
     static_assert(kNormBlocks <= kThreads, "a part of the norm for each thread");
     const double norm = sqrt(block_sum<kThreads>(threadIdx.x < parts ? part[threadIdx.x] : 0.0));
     int exponent = 0;
     if (norm > 0.0 && norm < __builtin_huge_val()) (void)frexp(norm, &exponent);
-    if (threadIdx.x == 0 && rho) {
+    if (threadIdx.x < kWave && scale) {
         // zeros stay zeros; an infinity or a not-a-number makes all of it NaN
-        *rho = norm == 0.0 ? 0.0f
-               : norm < __builtin_huge_val() ? (float)(ldexp(1.0, exponent) / (norm + (double)eps)) : __uint_as_float(0x7FC00000u);
+        const bool some = norm > 0.0 && norm < __builtin_huge_val();
+        const u32 lane = threadIdx.x;
+        if (lane == 0)
+            scale[0] = norm == 0.0 ? 0.0f : some ? (float)(ldexp(1.0, exponent) / (norm + (double)eps)) : __uint_as_float(0x7FC00000u);
+        // the singular values' bound; lane i has step i's coefficients, and its bound after it
+        float a = 0.0f, b = 0.0f, c = 0.0f, most = some ? (float)(norm / (norm + (double)eps)) : 1.0f, mine = most;
+        if (lane < steps.count) {
+            a = fabsf(steps.abc[lane][0]);
+            b = fabsf(steps.abc[lane][1]);
+            c = fabsf(steps.abc[lane][2]);
+        }
+        for (u32 i = 0; i < steps.count; ++i) {
+            const float square = most * most;
+            most = fminf(most * (read_lane(a, i) + square * (read_lane(b, i) + square * read_lane(c, i))), (float)kMostX);
+            if (lane == i) mine = most;
+        }
+        int e = 0;
+        if (mine < 0.5f) (void)frexpf(mine, &e);
+        if (lane < steps.count) scale[(lane + 1) * kMembers] = ldexpf(1.0f, max(e, -kMostDown));
     }
     return kLogX - exponent;
 }
@@ -237,7 +273,8 @@ __global__ void __launch_bounds__(kNormThreads) k_start(Start g)
     typedef Stored<kOf> S;
     __shared__ float tile[kSide][kSide + 1];
     const u32 r0 = blockIdx.y * kSide, c0 = blockIdx.x * kSide, member = blockIdx.z;
-    const int e = exponent_of<kNormThreads>(g.part + member * kNormBlocks, g.parts, g.eps, blockIdx.x == 0 && blockIdx.y == 0 ? g.rho + member : nullptr);
+    const int e = exponent_of<kNormThreads>(g.part + member * kNormBlocks, g.parts, g.eps, g.steps,
+                                            blockIdx.x == 0 && blockIdx.y == 0 ? g.scale + member : nullptr);
     const u64 row_bytes = g.ld * Eight<kType>::kSize;
     const unsigned char *x = (const unsigned char *)g.x.p[member];
     const u32 row_a = S::row_bytes(g.cols), row_t = S::row_bytes(g.rows);
@@ -284,10 +321,10 @@ struct Product {
     u32 tiles_m, tiles_n, tiles;            // tiles: of one matrix
     unsigned char *out, *turned;            // the result, and turned over
     u64 out_stride, turned_stride;
-    // kSymmetric: result = c_sum rho^2 product + c_old old + c_one I; kNext, kLast: (c_sum product + c_old old) rho
+    // kSymmetric: result = c_sum scale^2 product + c_old old + c_one I; kNext, kLast: (c_sum product + c_old old) scale / next
     float c_sum, c_old, c_one;
     const unsigned char *old;               // laid out as the result, or null
-    const float *rho;                       // first step only, else null
+    const float *scale, *next;              // of the matrices' X before and after, or null for 1
     // kPart
     float *part;                            // [splits][matrices][rows][rows rounded up to 4]
     u32 members, splits, slices_each;
@@ -327,11 +364,15 @@ __global__ void __launch_bounds__(T::kThreads) k_step(Product g)
     const TileRows a{g.left + member * g.left_stride + (u64)i0 * bytes, g.rows - i0, bytes, bytes};
     const TileRows b{g.right + member * g.right_stride + (u64)j0 * bytes, g.cols - j0, bytes, bytes};
     const u32 row_out = S::row_bytes(g.cols), row_turned = S::row_bytes(g.rows);
+    float scale = 1.0f, next = 1.0f;
     T t;
     t.clear();
     const u32 from = kStep == kPart ? split * g.slices_each : 0u;
     t.template multiply<true>(a, b, from, kStep == kPart ? min(from + g.slices_each, slices) : slices, lds, [&] {
-        if (kStep == kPart || !g.old) return;
+        if (kStep == kPart) return;
+        if (g.scale) scale = g.scale[member];           // (on its way with the first slices too)
+        if (kStep == kNext) next = g.next[member];
+        if (!g.old) return;
         // the old matrix's part goes into the sums first: its loads are under way together, and with the first slices (after the
         // products, between the stores, each would be waited for: 95 us for 4096 x 4096, 72 without it; and so they are where a
         // branch stands around each: what lies beyond the matrix is read from its edge, and not stored)
@@ -361,8 +402,7 @@ __global__ void __launch_bounds__(T::kThreads) k_step(Product g)
         });
         return;
     }
-    const float rho = g.rho ? g.rho[member] : 1.0f;
-    const float c_sum = kTriangle ? g.c_sum * rho * rho : g.c_sum * rho;
+    const float c_sum = kTriangle ? g.c_sum * scale * scale : g.c_sum * (scale / next);
     if constexpr (kStep == kLast) {
         void *to = g.to.p[member];
         // the old weights of a row of fragments, on their way while the row before is stored; without a branch, as above
@@ -476,7 +516,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(Product g)
     triangle_at(blockIdx.x, n, ti, tj);
     const u32 r = threadIdx.x >> 4, c = (threadIdx.x & 15u) * 4u;
     const u64 ld = align_up(g.rows, 4), one = (u64)g.rows * ld;
-    const float rho = g.rho ? g.rho[member] : 1.0f, c_sum = g.c_sum * rho * rho;
+    const float scale = g.scale[member], c_sum = g.c_sum * scale * scale;
     const u32 row_out = S::row_bytes(g.rows);
     unsigned char *out = g.out + member * g.out_stride;
     {
@@ -518,7 +558,7 @@ struct Narrow {
     const double *norm;
     u32 norm_parts;
     float eps;
-    float *rho;
+    float *scale;               // k_narrow_start: of all steps, written; k_narrow: of its step and the next
     const u8 *xt;               // [members][n] rows of m, k_narrow: read
     u8 *xt_next;                // written
     u64 xt_stride;
@@ -527,7 +567,7 @@ struct Narrow {
     float *joined;              // [members][64][64], or null
     u32 runs, blocks_each;
     float c_gram, shift, c_sum, c_old, c_one, c_x;      // D = c_gram X X^T - shift; Q = c_sum D D + c_old D + c_one; X <- Q X + c_x X
-    bool first, last;
+    bool last;
     Members to;                 // the result
     int to_type;
     u64 ldo;
@@ -583,7 +623,7 @@ __device__ __forceinline__ void write_part(const T &gram, float *to)
 }
 
 template <Operands kOf, int kType>
-__global__ void __launch_bounds__(kNarrowThreads) k_narrow_start(Narrow g)
+__global__ void __launch_bounds__(kNarrowThreads) k_narrow_start(Narrow g, Steps steps)
 {
     typedef Stored<kOf> S;
     typedef Block<kOf> B;
@@ -592,7 +632,8 @@ __global__ void __launch_bounds__(kNarrowThreads) k_narrow_start(Narrow g)
     const u32 member = blockIdx.y, run = blockIdx.x;
     const bool over = g.rows > g.cols;
     const u32 m = over ? g.cols : g.rows, n = over ? g.rows : g.cols;
-    const int e = exponent_of<kNarrowThreads>(g.norm + member * kNormBlocks, g.norm_parts, g.eps, run == 0 ? g.rho + member : nullptr);
+    const int e = exponent_of<kNarrowThreads>(g.norm + member * kNormBlocks, g.norm_parts, g.eps, steps,
+                                               run == 0 ? g.scale + member : nullptr);
     const u64 row_bytes = g.ld * Eight<kType>::kSize;
     const u8 *x = (const u8 *)g.x.p[member];
     u8 *xt = g.xt_next + member * g.xt_stride;
@@ -653,7 +694,6 @@ __global__ void __launch_bounds__(kNarrowThreads) k_narrow(Narrow g)
     const u32 member = blockIdx.y, run = blockIdx.x;
     const bool over = g.rows > g.cols;
     const u32 m = over ? g.cols : g.rows, n = over ? g.rows : g.cols;
-    const float rho = g.first ? g.rho[member] : 1.0f;
     const u32 row_xt = S::row_bytes(m), pieces = row_xt / 16;       // 16-byte pieces of a row of X turned over
     const u8 *xt = g.xt + member * g.xt_stride;
     u8 *xt_next = g.xt_next + member * g.xt_stride;
@@ -670,6 +710,10 @@ __global__ void __launch_bounds__(kNarrowThreads) k_narrow(Narrow g)
     const u32 first_block = run * g.blocks_each;
     i32x4 held[kPieces];
     load(held, first_block * kSide);
+    // (vector loads, on their way with the parts: scalar ones are waited for with the next kernel argument, 0.5 us a launch)
+    u32 at_scale = member;
+    asm("" : "+v"(at_scale));
+    const float x_scale = g.scale[at_scale], x_next = g.scale[kMembers + at_scale];
     {
         // D
         const u32 r = threadIdx.x >> 3, c = (threadIdx.x & 7u) * 8u;
@@ -680,7 +724,7 @@ __global__ void __launch_bounds__(kNarrowThreads) k_narrow(Narrow g)
         for (u32 s = 0; s < runs; ++s)
 #pragma unroll
             for (int q = 0; q < 2; ++q) sum[q] += *(const f32x4 *)(part + s * kSide * kSide + 4 * q);
-        const float scale = g.c_gram * rho * rho;
+        const float scale = g.c_gram * x_scale * x_scale;
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
             f32x4 v = sum[q] * scale;
@@ -732,7 +776,7 @@ __global__ void __launch_bounds__(kNarrowThreads) k_narrow(Narrow g)
             void *to = g.to.p[member];
             t.each([&](u32 r, u32 c, const f32x4 &sum) {
                 if (r >= m || n0 + c >= n) return;
-                f32x4 v = sum * (g.c_last * rho);
+                f32x4 v = sum * (g.c_last * x_scale);
                 const u32 have = n - n0 - c;
                 const u64 at = over ? (u64)(n0 + c) * g.ldo + r : (u64)r * g.ldo + n0 + c, next = over ? g.ldo : 1u;
                 if (g.update) {
@@ -748,7 +792,7 @@ __global__ void __launch_bounds__(kNarrowThreads) k_narrow(Narrow g)
                         if (q < have) write_as(to, at + q * next, g.to_type, v[q]);
             });
         } else {
-            const float c = ldexpf(rho, -kLogD);
+            const float c = ldexpf(x_scale / x_next, -kLogD);
             t.each([&](u32 r, u32 col, const f32x4 &sum) {
                 f32x4 v = sum * c;
 #pragma unroll
@@ -773,7 +817,6 @@ using namespace rtopk;
 namespace {
 
 constexpr u64 kMostSide = 1u << 21;      // offsets inside a tile of 256 rows fit 32 bits
-constexpr u32 kMostSteps = 64;
 struct Shape {
     u32 rows, cols;
     u32 m() const { return std::min(rows, cols); }
@@ -840,7 +883,7 @@ bool is_narrow(const Shape &s) { return s.m() <= kSide; }
 
 struct Parts {
     double *norm;
-    float *rho, *direction, *part, *joined;
+    float *scale, *direction, *part, *joined;
     unsigned char *x[2], *xt[2], *square[4];
     u64 x_stride, xt_stride, square_stride;
 };
@@ -861,7 +904,7 @@ u64 cut(void *base, u32 count, const Shape &s, bool direction, Parts &p)
     p.xt_stride = align_up((u64)s.n() * S::row_bytes(s.m()), 256);
     p.square_stride = align_up((u64)s.m() * S::row_bytes(s.m()), 256);
     p.norm = (double *)take(kMembers * kNormBlocks * sizeof(double));
-    p.rho = (float *)take(kMembers * sizeof(float));
+    p.scale = (float *)take((kMostSteps + 1) * kMembers * sizeof(float));
     if (is_narrow(s)) {
         for (int i = 0; i < 2; ++i) p.xt[i] = take(members * p.xt_stride);
         // (fewer matrices have more runs each, but not more in all than 2 * kUnits and what rounding up adds)
@@ -966,7 +1009,7 @@ struct Around {
 };
 
 template <Operands kOf>
-int iterate_narrow(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 norm_parts, u32 steps, const float *abc, float eps,
+int iterate_narrow(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 norm_parts, const Steps &steps, float eps,
                    const Parts &p, const Target &target, hipStream_t stream)
 {
     const NarrowPlan plan = plan_narrow(s, members);
@@ -980,7 +1023,7 @@ int iterate_narrow(const Members &x, int type, u64 ldx, const Shape &s, u32 memb
     g.norm = p.norm;
     g.norm_parts = norm_parts;
     g.eps = eps;
-    g.rho = p.rho;
+    g.scale = p.scale;
     g.xt_stride = p.xt_stride;
     g.runs = plan.runs;
     g.blocks_each = plan.blocks_each;
@@ -995,13 +1038,14 @@ int iterate_narrow(const Members &x, int type, u64 ldx, const Shape &s, u32 memb
     g.gain = target.gain;
     g.keep = target.keep;
     g.update = target.update;
-    if (type == RTOPK_F32) k_narrow_start<kOf, RTOPK_F32><<<grid, kNarrowThreads, 0, stream>>>(g);
-    else if (type == RTOPK_BF16) k_narrow_start<kOf, RTOPK_BF16><<<grid, kNarrowThreads, 0, stream>>>(g);
-    else k_narrow_start<kOf, RTOPK_F16><<<grid, kNarrowThreads, 0, stream>>>(g);
+    if (type == RTOPK_F32) k_narrow_start<kOf, RTOPK_F32><<<grid, kNarrowThreads, 0, stream>>>(g, steps);
+    else if (type == RTOPK_BF16) k_narrow_start<kOf, RTOPK_BF16><<<grid, kNarrowThreads, 0, stream>>>(g, steps);
+    else k_narrow_start<kOf, RTOPK_F16><<<grid, kNarrowThreads, 0, stream>>>(g, steps);
     if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
     double h = 1.0 / s.m();
-    for (u32 i = 0; i < steps; ++i) {
-        const Around at(abc + 3 * i, h);
+    for (u32 i = 0; i < steps.count; ++i) {
+        const Around at(steps.abc[i], h);
+        g.scale = p.scale + i * kMembers;
         g.xt = p.xt[i & 1];
         g.xt_next = p.xt[1 - (i & 1)];
         g.part = part[i & 1];
@@ -1012,8 +1056,7 @@ int iterate_narrow(const Members &x, int type, u64 ldx, const Shape &s, u32 memb
         g.c_one = kOf == kPairs ? (float)(at.value * ldexp(1.0, kLogD)) : 0.0f;
         g.c_x = kOf == kPairs ? 0.0f : (float)(at.value * ldexp(1.0, kLogD));
         h = at.next;
-        g.first = i == 0;
-        g.last = i + 1 == steps;
+        g.last = i + 1 == steps.count;
         if (plan.join) {
             k_narrow_join<<<dim3(kSide * kSide / 64, members), 256, 0, stream>>>(g);
             if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
@@ -1026,14 +1069,14 @@ int iterate_narrow(const Members &x, int type, u64 ldx, const Shape &s, u32 memb
 
 // From G and the parts of its norm to the end.
 template <Operands kOf>
-int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 norm_parts, u32 steps, const float *abc,
+int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 norm_parts, const Steps &steps,
             double largest_p, float eps, const Parts &p, const Target &target, hipStream_t stream)
 {
     typedef Stored<kOf> S;
-    if (is_narrow(s)) return iterate_narrow<kOf>(x, type, ldx, s, members, norm_parts, steps, abc, eps, p, target, stream);
+    if (is_narrow(s)) return iterate_narrow<kOf>(x, type, ldx, s, members, norm_parts, steps, eps, p, target, stream);
     const u32 m = s.m(), n = s.n();
     const Start start{x, s.rows, s.cols, ldx, s.over() ? p.xt[0] : p.x[0], s.over() ? p.x[0] : p.xt[0],
-                      s.over() ? p.xt_stride : p.x_stride, s.over() ? p.x_stride : p.xt_stride, p.norm, norm_parts, eps, p.rho};
+                      s.over() ? p.xt_stride : p.x_stride, s.over() ? p.x_stride : p.xt_stride, p.norm, norm_parts, eps, steps, p.scale};
     const dim3 grid((S::padded(s.cols) + kSide - 1) / kSide, (S::padded(s.rows) + kSide - 1) / kSide, members);
     if (type == RTOPK_F32) k_start<kOf, RTOPK_F32><<<grid, kNormThreads, 0, stream>>>(start);
     else if (type == RTOPK_BF16) k_start<kOf, RTOPK_BF16><<<grid, kNormThreads, 0, stream>>>(start);
@@ -1045,8 +1088,8 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
     const u32 square_edge = best_edge<kOf>(true, m, m, members, square_slices, &square_cost);
     const u32 next_edge = best_edge<kOf>(false, m, n, members, square_slices, &next_cost);
 
-    // X X^T - h I (the first step's X still lacks rho)
-    auto make_gram = [&](const unsigned char *x_now, unsigned char *to, double h, const float *rho) -> int {
+    // X X^T - h I
+    auto make_gram = [&](const unsigned char *x_now, unsigned char *to, double h, const float *scale) -> int {
         Product g{};
         g.left = g.right = x_now;
         g.left_stride = g.right_stride = p.x_stride;
@@ -1056,7 +1099,7 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
         g.out_stride = g.turned_stride = p.square_stride;
         g.c_sum = ldexpf(1.0f, kLogD - 2 * kLogX);
         g.c_one = (float)(-h * ldexp(1.0, kLogD));
-        g.rho = rho;
+        g.scale = scale;
         if (gram.splits == 1) return launch<kOf, kSymmetric>(g, members, gram.edge, stream);
         g.part = p.part;
         g.splits = gram.splits;
@@ -1097,16 +1140,16 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
     const bool twos = kOf == kPairs && largest_p <= 4.0 && gram_cost + next_cost > 1.05 * 3.0 * square_cost;
     u32 now = 0;
     double h = 1.0 / m;
-    for (u32 i = 0; i < steps;) {
+    for (u32 i = 0; i < steps.count;) {
         const unsigned char *x_now = p.x[now], *xt_now = p.xt[now];
-        const float *rho = i == 0 ? p.rho : nullptr;
-        const Around at(abc + 3 * i, h);
-        if (const int rc = make_gram(x_now, q[0], h, rho)) return rc;
+        const float *scale = p.scale + i * kMembers;
+        const Around at(steps.abc[i], h);
+        if (const int rc = make_gram(x_now, q[0], h, scale)) return rc;
         if (const int rc = make_poly(q[0], q[1], at)) return rc;
         unsigned char *poly = q[1];
         u32 did = 1;
-        if (twos && i + 1 < steps) {
-            const Around second(abc + 3 * (i + 1), at.next);
+        if (twos && i + 1 < steps.count) {
+            const Around second(steps.abc[i + 1], at.next);
             if (const int rc = make_square(q[1], q[1], nullptr, q[2], 1.0, 0.0, 0.0)) return rc;            // E = P P
             if (const int rc = make_square(q[0], q[2], q[2], q[3], 1.0, h, -at.next)) return rc;            // D E + h E - h' I
             if (const int rc = make_poly(q[3], q[0], second)) return rc;
@@ -1119,8 +1162,9 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
         }
         i += did;
         Product g{};
-        g.rho = rho;
-        if (i < steps) {
+        g.scale = scale;
+        if (i < steps.count) {
+            g.next = p.scale + i * kMembers;
             g.left = poly;
             g.left_stride = p.square_stride;
             g.right = xt_now;
@@ -1165,12 +1209,12 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
     return RTOPK_OK;
 }
 
-int iterate(int products, const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 norm_parts, u32 steps,
-            const float *abc, double largest_p, float eps, const Parts &p, const Target &target, hipStream_t stream)
+int iterate(int products, const Members &x, int type, u64 ldx, const Shape &s, u32 members, u32 norm_parts, const Steps &steps,
+            double largest_p, float eps, const Parts &p, const Target &target, hipStream_t stream)
 {
     return products == RTOPK_PRODUCTS_PAIRS
-               ? iterate<kPairs>(x, type, ldx, s, members, norm_parts, steps, abc, largest_p, eps, p, target, stream)
-               : iterate<kHalves>(x, type, ldx, s, members, norm_parts, steps, abc, largest_p, eps, p, target, stream);
+               ? iterate<kPairs>(x, type, ldx, s, members, norm_parts, steps, largest_p, eps, p, target, stream)
+               : iterate<kHalves>(x, type, ldx, s, members, norm_parts, steps, largest_p, eps, p, target, stream);
 }
 
 // workgroups for the norm of one of so many matrices: a few elements for every thread, and not many more than fill the chip
@@ -1185,6 +1229,12 @@ bool sizes_ok(uint32_t count, uint64_t rows, uint64_t cols, int products)
 {
     return count >= 1 && rows >= 1 && cols >= 1 && rows <= kMostSide && cols <= kMostSide && rows * cols <= 0xFFFFFFFFull &&
            (products == RTOPK_PRODUCTS_PAIRS || products == RTOPK_PRODUCTS_HALVES);
+}
+Steps steps_of(uint32_t count, const float *abc)
+{
+    Steps s{count, {}};
+    std::memcpy(s.abc, abc, count * sizeof s.abc[0]);
+    return s;
 }
 bool iteration_ok(uint32_t steps, const float *abc, float eps, double *largest_p)
 {
@@ -1216,6 +1266,7 @@ extern "C" int rtopk_orthogonalize(uint32_t count, const void *const *x, int typ
     if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need) return RTOPK_EWORKSPACE;
     hipStream_t stream = (hipStream_t)stream_v;
     const Shape s{(u32)rows, (u32)cols};
+    const Steps all = steps_of(steps, coefficients);
     Parts p;
     cut(products, workspace, count, s, false, p);
     for (uint32_t first = 0; first < count; first += kMembers) {
@@ -1232,7 +1283,7 @@ extern "C" int rtopk_orthogonalize(uint32_t count, const void *const *x, int typ
         else if (type == RTOPK_BF16) k_norm<RTOPK_BF16><<<grid, kNormThreads, 0, stream>>>(from, s.rows, s.cols, ldx, p.norm);
         else k_norm<RTOPK_F16><<<grid, kNormThreads, 0, stream>>>(from, s.rows, s.cols, ldx, p.norm);
         if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
-        if (const int rc = iterate(products, from, type, ldx, s, members, parts, steps, coefficients, largest_p, eps, p, to, stream)) return rc;
+        if (const int rc = iterate(products, from, type, ldx, s, members, parts, all, largest_p, eps, p, to, stream)) return rc;
     }
     return RTOPK_OK;
 }
@@ -1267,6 +1318,7 @@ extern "C" int rtopk_aggregate_update_orthogonal(uint32_t count, const uint32_t 
     if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need) return RTOPK_EWORKSPACE;
     hipStream_t stream = (hipStream_t)stream_v;
     const Shape s{(u32)rows, (u32)cols};
+    const Steps all = steps_of(steps, coefficients);
     Parts p;
     cut(products, workspace, count, s, true, p);
     for (uint32_t first = 0; first < count; first += kMembers) {
@@ -1285,7 +1337,7 @@ extern "C" int rtopk_aggregate_update_orthogonal(uint32_t count, const uint32_t 
         if (const int rc = launch_direction(members, from, n, k, d, scale, mu, nesterov != 0, p.direction, align_up(d, 64), p.norm, kNormBlocks,
                                             &parts, stream))
             return rc;
-        if (const int rc = iterate(products, directions, RTOPK_F32, cols, s, members, parts, steps, coefficients, largest_p, eps, p, to, stream)) return rc;
+        if (const int rc = iterate(products, directions, RTOPK_F32, cols, s, members, parts, all, largest_p, eps, p, to, stream)) return rc;
     }
     return RTOPK_OK;
 }
