@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kQua
     constexpr u32 kWaves = kWavesPerRow > 4 ? kWavesPerRow : 4, kRows = kWaves / kWavesPerRow, kStep = 8u * kWave * kWavesPerRow;
     __shared__ u32 most[kWaves];
     const u32 lane = lane_id(), wave = threadIdx.x / kWave;
-    const u32 r = blockIdx.x * kRows + wave / kWavesPerRow;
+    const u32 r = (blockIdx.y * gridDim.x + blockIdx.x) * kRows + wave / kWavesPerRow;
     const bool there = r < g.rows;
     const unsigned char *row = (const unsigned char *)g.x + (there ? r : 0u) * g.ldx * Eight<kType>::kSize;
     const u32 c0 = (wave % kWavesPerRow * kWave + lane) * 8u;
@@ -686,13 +686,15 @@ void launch_rows(const RowsToQuantize &g, hipStream_t stream)
 {
     // what a wavefront's lanes hold in one piece each is 512 numbers: one wavefront for a short row where there are many
     const u32 rows = g.rows, fill = g.fill;
-    if (fill <= 512 && rows >= 4 * kUnits) k_quantize_rows<kType, 1, 1><<<(rows + 3) / 4, kQuantizeThreads, 0, stream>>>(g);
-    else if (fill <= 1024 && rows >= 4 * kUnits) k_quantize_rows<kType, 1, 2><<<(rows + 3) / 4, kQuantizeThreads, 0, stream>>>(g);
-    else if (fill <= 2048) k_quantize_rows<kType, 4, 1><<<rows, kQuantizeThreads, 0, stream>>>(g);
-    else if (fill <= 4096) k_quantize_rows<kType, 4, 2><<<rows, kQuantizeThreads, 0, stream>>>(g);
-    else if (fill <= 8192) k_quantize_rows<kType, 4, 4><<<rows, kQuantizeThreads, 0, stream>>>(g);
-    else if (fill <= 16384) k_quantize_rows<kType, 16, 2><<<rows, 16 * kWave, 0, stream>>>(g);
-    else k_quantize_rows<kType, 16, 0><<<rows, 16 * kWave, 0, stream>>>(g);
+    // (a launch has less than 2^32 threads along x: 2^22 rows of 1024 threads go along y too)
+    const auto grid = [](u32 blocks) { return dim3(std::min(blocks, 1u << 20), (blocks + (1u << 20) - 1) >> 20); };
+    if (fill <= 512 && rows >= 4 * kUnits) k_quantize_rows<kType, 1, 1><<<grid((rows + 3) / 4), kQuantizeThreads, 0, stream>>>(g);
+    else if (fill <= 1024 && rows >= 4 * kUnits) k_quantize_rows<kType, 1, 2><<<grid((rows + 3) / 4), kQuantizeThreads, 0, stream>>>(g);
+    else if (fill <= 2048) k_quantize_rows<kType, 4, 1><<<grid(rows), kQuantizeThreads, 0, stream>>>(g);
+    else if (fill <= 4096) k_quantize_rows<kType, 4, 2><<<grid(rows), kQuantizeThreads, 0, stream>>>(g);
+    else if (fill <= 8192) k_quantize_rows<kType, 4, 4><<<grid(rows), kQuantizeThreads, 0, stream>>>(g);
+    else if (fill <= 16384) k_quantize_rows<kType, 16, 2><<<grid(rows), 16 * kWave, 0, stream>>>(g);
+    else k_quantize_rows<kType, 16, 0><<<grid(rows), 16 * kWave, 0, stream>>>(g);
 }
 
 int quantize_rows(const void *x, int type, u32 rows, u32 cols, u64 ldx, signed char *q, u64 ldq, u32 fill, float *scale,
