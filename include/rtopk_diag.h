@@ -1,9 +1,10 @@
 /*
  * rtopk_diag.h -- diagnostics of the rTop-k library: statistics of the last
  * encode, HIP-event tracing of its stages, hooks that force its exact fallback
- * paths, and a streaming calibration kernel. Tests, benchmarks and profiling
- * use these; a training loop needs none of them. The interface proper is
- * rtopk.h. Everything here is for eager use (not under stream capture).
+ * paths, a streaming calibration kernel, and what the matrix calls choose for
+ * given sizes. Tests, benchmarks and profiling use these; a training loop
+ * needs none of them. The interface proper is rtopk.h. Everything here is for
+ * eager use (not under stream capture).
  */
 #ifndef RTOPK_DIAG_H
 #define RTOPK_DIAG_H
@@ -126,6 +127,29 @@ int rtopk_force_next_encode(unsigned flags);
  * grad, residual: device, 16-byte aligned, d elements, not overlapping.
  */
 int rtopk_diag_stream_add(const float *grad, float *residual, uint64_t d, void *stream);
+
+/*
+ * What the matrix calls choose for given sizes (host arithmetic only, no GPU
+ * is looked at): so that a test knows which kernels its sizes reach.
+ *
+ * The 8-bit product of m x n sums of k: square tiles of `edge` rows, so many
+ * of them, the contraction in `runs` (more than one: joined by another
+ * launch). on_lines: the operands' rows start on 128 bytes.
+ */
+typedef struct rtopk_product_plan {
+    uint32_t edge, tiles, runs;
+} rtopk_product_plan_t;
+int rtopk_product_plan(uint64_t m, uint64_t n, uint64_t k, int on_lines, rtopk_product_plan_t *plan);
+
+/* The orthogonalisation of up to 16 matrices that share launches. */
+typedef struct rtopk_orthogonalize_plan {
+    uint32_t narrow;                                    /* a launch a step; then only the runs and whether they are joined are set */
+    uint32_t gram_edge, gram_runs, joined;              /* X X^T */
+    uint32_t square_edge, next_edge;                    /* products of m x m, and with X */
+    uint32_t two_at_a_time;
+} rtopk_orthogonalize_plan_t;
+int rtopk_orthogonalize_plan(uint32_t count, uint64_t rows, uint64_t cols, int products, uint32_t steps,
+                             const float *coefficients, rtopk_orthogonalize_plan_t *plan);
 
 /*
  * 1 when the library was built with RTOPK_DEBUG_CHECKS, else 0. In that build

@@ -16,7 +16,8 @@ from .binding import (RtopkError, aggregate, aggregate_update, aggregate_update_
                       QUINTIC, quantize_i8, quantize_i8_workspace_bytes, matmul_i8, matmul_i8_workspace_bytes,
                       linear_i8, linear_i8_workspace_bytes, linear_i8_backward, linear_i8_backward_workspace_bytes,
                       orthogonalize, orthogonalize_workspace_bytes,
-                      aggregate_update_orthogonal, aggregate_update_orthogonal_workspace_bytes)
+                      aggregate_update_orthogonal, aggregate_update_orthogonal_workspace_bytes,
+                      product_plan, orthogonalize_plan)
 
 __all__ = ["RtopkError", "aggregate", "aggregate_update", "aggregate_update_momentum", "aggregate_update_static", "STATIC_SCRATCH_BYTES", "aggregate_update_workspace_bytes", "aggregate_workspace_bytes", "encode", "encode_batch", "encode_batch_device_step", "diag_stream_add", "encode_stats",
            "encode_workspace_bytes", "library_path", "load_library", "strerror", "trace_next_encode", "version", "STAGES",
@@ -24,4 +25,4 @@ __all__ = ["RtopkError", "aggregate", "aggregate_update", "aggregate_update_mome
            "QUINTIC", "quantize_i8", "quantize_i8_workspace_bytes", "matmul_i8", "matmul_i8_workspace_bytes",
            "linear_i8", "linear_i8_workspace_bytes", "linear_i8_backward", "linear_i8_backward_workspace_bytes",
            "orthogonalize", "orthogonalize_workspace_bytes", "aggregate_update_orthogonal",
-           "aggregate_update_orthogonal_workspace_bytes"]
+           "aggregate_update_orthogonal_workspace_bytes", "product_plan", "orthogonalize_plan"]

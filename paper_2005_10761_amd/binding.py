@@ -28,7 +28,7 @@ EXPORTS = ("rtopk_encode_workspace_bytes", "rtopk_aggregate_workspace_bytes", "r
            "rtopk_strerror", "rtopk_version")
 # ... and include/rtopk_diag.h
 DIAG_EXPORTS = ("rtopk_encode_stats", "rtopk_trace_next_encode", "rtopk_force_next_encode",
-                "rtopk_diag_stream_add", "rtopk_debug_checks")
+                "rtopk_diag_stream_add", "rtopk_product_plan", "rtopk_orthogonalize_plan", "rtopk_debug_checks")
 
 
 class RtopkError(RuntimeError):
@@ -42,6 +42,15 @@ class EncodeStats(ctypes.Structure):
                 ("threshold_bits", ctypes.c_uint32), ("boundary_list_size", ctypes.c_uint32),
                 ("count_greater", ctypes.c_uint64), ("ties_taken", ctypes.c_uint64),
                 ("superset_size", ctypes.c_uint64), ("key_list_size", ctypes.c_uint64)]
+
+
+class ProductPlan(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_uint32) for name in ("edge", "tiles", "runs")]
+
+
+class OrthogonalizePlan(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_uint32) for name in ("narrow", "gram_edge", "gram_runs", "joined", "square_edge", "next_edge",
+                                                     "two_at_a_time")]
 
 
 def library_path() -> str:
@@ -109,7 +118,9 @@ def load_library() -> ctypes.CDLL:
                                     u64, vp],
             "rtopk_aggregate_update_orthogonal_workspace_bytes": [u32, u64, u64, i32, pu64],
             "rtopk_aggregate_update_orthogonal": [u32, vp, vp, u32, u64, u64, u64, f32, f32, f32, i32, f32,
-                                                  f32, u32, vp, f32, i32, vp, vp, vp, u64, vp]}.items():
+                                                  f32, u32, vp, f32, i32, vp, vp, vp, u64, vp],
+            "rtopk_product_plan": [u64, u64, u64, i32, vp],
+            "rtopk_orthogonalize_plan": [u32, u64, u64, i32, u32, vp, vp]}.items():
         getattr(L, name).argtypes = args
         getattr(L, name).restype = i32
     L.rtopk_strerror.argtypes = [ctypes.c_int]
@@ -621,3 +632,23 @@ def aggregate_update_orthogonal(idx, val, n: int, k: int, eta: float, scale: flo
         _PRODUCTS[products], pointers(omega), pointers(velocity), ws, ws_bytes, _stream_handle(stream))
     if rc:
         raise RtopkError(rc, "rtopk_aggregate_update_orthogonal")
+
+
+def product_plan(m: int, n: int, k: int, on_lines: bool = True) -> dict:
+    """rtopk_product_plan: the tiles and runs that the 8-bit product of these sizes takes."""
+    plan = ProductPlan()
+    rc = load_library().rtopk_product_plan(m, n, k, int(on_lines), ctypes.byref(plan))
+    if rc:
+        raise RtopkError(rc, "rtopk_product_plan")
+    return {name: int(getattr(plan, name)) for name, _ in plan._fields_}
+
+
+def orthogonalize_plan(count: int, rows: int, cols: int, products: str = "pairs", steps: Optional[int] = None,
+                       coefficients=QUINTIC) -> dict:
+    """rtopk_orthogonalize_plan: the tiles, runs and form of steps that the orthogonalisation of these sizes takes."""
+    number, abc = _coefficients(coefficients, steps)
+    plan = OrthogonalizePlan()
+    rc = load_library().rtopk_orthogonalize_plan(count, rows, cols, _PRODUCTS[products], number, abc, ctypes.byref(plan))
+    if rc:
+        raise RtopkError(rc, "rtopk_orthogonalize_plan")
+    return {name: int(getattr(plan, name)) for name, _ in plan._fields_}

@@ -15,6 +15,7 @@
 #include <algorithm>
 
 #include "../../include/rtopk.h"
+#include "../../include/rtopk_diag.h"
 #include "rtopk_matrix.h"
 
 namespace rtopk {
@@ -842,6 +843,14 @@ extern "C" int rtopk_matmul_i8(const int8_t *a, const float *a_scale, const int8
     if (!workspace_ok(workspace, workspace_bytes, need)) return RTOPK_EWORKSPACE;
     return run_product(Scaled{a, b, lda, ldb, (u32)m, (u32)n, (u32)k, a_scale, b_scale, bias, out, ldo, out_type, 0, 0, nullptr},
                        workspace, (hipStream_t)stream_v);
+}
+
+extern "C" int rtopk_product_plan(uint64_t m, uint64_t n, uint64_t k, int on_lines, rtopk_product_plan_t *plan)
+{
+    if (!plan || !size_ok(m) || !size_ok(n) || k > kMostSize) return RTOPK_EINVAL;
+    const Plan p = plan_product((u32)m, (u32)n, (u32)k, on_lines != 0);
+    *plan = rtopk_product_plan_t{p.edge, p.tiles, p.splits};
+    return RTOPK_OK;
 }
 
 extern "C" int rtopk_linear_i8_workspace_bytes(uint64_t m, uint64_t k, uint64_t n, uint64_t *bytes)

@@ -38,6 +38,7 @@
 #include <cstring>
 
 #include "../../include/rtopk.h"
+#include "../../include/rtopk_diag.h"
 #include "rtopk_direction.h"
 #include "rtopk_matrix.h"
 
@@ -863,6 +864,29 @@ GramPlan plan_gram(u32 members, const Shape &s, double *cost)
     return best;
 }
 
+// What a step of matrices with both sides beyond 64 is made of.
+struct StepPlan {
+    GramPlan gram;
+    u32 square_edge, next_edge;
+    // Two steps at a time: from D and P of the first, X X^T of the second is P (D + h I) P without X, and both polynomials
+    // go to X as one. Three more products of m x m, X X^T and P X once less: where X is long. With pairs only, and not with
+    // coefficients that make P large: the second D takes up the first one's roundings, up to P^2 times larger (1500 x 6000:
+    // relative error 2.2 10^-6, one step at a time 1.2, a plain binary32 iteration 2.1; with h = 1 it would be 24).
+    bool twos;
+};
+template <Operands kOf>
+StepPlan plan_step(u32 members, const Shape &s, double largest_p)
+{
+    StepPlan p{};
+    double gram_cost, square_cost, next_cost;
+    const double square_slices = Stored<kOf>::row_bytes(s.m()) / kSlice;
+    p.gram = plan_gram<kOf>(members, s, &gram_cost);
+    p.square_edge = best_edge<kOf>(true, s.m(), s.m(), members, square_slices, &square_cost);
+    p.next_edge = best_edge<kOf>(false, s.m(), s.n(), members, square_slices, &next_cost);
+    p.twos = kOf == kPairs && largest_p <= 4.0 && gram_cost + next_cost > 1.05 * 3.0 * square_cost;
+    return p;
+}
+
 // A side of up to 64: the long side's blocks of 64 in so many runs. Up to kFewRuns of them are added up by every workgroup of
 // the next step; beyond, a launch does it, and there are as many runs as fill the chip. us a call of five steps, one matrix of
 // 64 x 320 / 1024 / 2048 / 5056 / 10048: every workgroup for itself 39 / 47 / 58 / 100 / 153, a launch 48 / 49 / 49 / 54 / 57.
@@ -1082,11 +1106,8 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
     else if (type == RTOPK_BF16) k_start<kOf, RTOPK_BF16><<<grid, kNormThreads, 0, stream>>>(start);
     else k_start<kOf, RTOPK_F16><<<grid, kNormThreads, 0, stream>>>(start);
     if (hipGetLastError() != hipSuccess) return RTOPK_EHIP;
-    double gram_cost, square_cost, next_cost;
-    const GramPlan gram = plan_gram<kOf>(members, s, &gram_cost);
-    const double square_slices = S::row_bytes(m) / kSlice;
-    const u32 square_edge = best_edge<kOf>(true, m, m, members, square_slices, &square_cost);
-    const u32 next_edge = best_edge<kOf>(false, m, n, members, square_slices, &next_cost);
+    const StepPlan plan = plan_step<kOf>(members, s, largest_p);
+    const GramPlan &gram = plan.gram;
 
     // X X^T - h I
     auto make_gram = [&](const unsigned char *x_now, unsigned char *to, double h, const float *scale) -> int {
@@ -1126,18 +1147,13 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
         g.c_old = (float)d;
         g.c_one = (float)(e * ldexp(1.0, kLogD));
         g.old = d != 0.0 ? old : nullptr;
-        return launch<kOf, kSymmetric>(g, members, square_edge, stream);
+        return launch<kOf, kSymmetric>(g, members, plan.square_edge, stream);
     };
     unsigned char *const *q = p.square;
     // Q from D; with pairs the whole polynomial
     auto make_poly = [&](const unsigned char *d, unsigned char *to, const Around &at) -> int {
         return make_square(d, d, d, to, at.c, at.slope, kOf == kPairs ? at.value : 0.0);
     };
-    // Two steps at a time: from D and P of the first, X X^T of the second is P (D + h I) P without X, and both polynomials
-    // go to X as one. Three more products of m x m, X X^T and P X once less: where X is long. With pairs only, and not with
-    // coefficients that make P large: the second D takes up the first one's roundings, up to P^2 times larger (1500 x 6000:
-    // relative error 2.2 10^-6, one step at a time 1.2, a plain binary32 iteration 2.1; with h = 1 it would be 24).
-    const bool twos = kOf == kPairs && largest_p <= 4.0 && gram_cost + next_cost > 1.05 * 3.0 * square_cost;
     u32 now = 0;
     double h = 1.0 / m;
     for (u32 i = 0; i < steps.count;) {
@@ -1148,7 +1164,7 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
         if (const int rc = make_poly(q[0], q[1], at)) return rc;
         unsigned char *poly = q[1];
         u32 did = 1;
-        if (twos && i + 1 < steps.count) {
+        if (plan.twos && i + 1 < steps.count) {
             const Around second(steps.abc[i + 1], at.next);
             if (const int rc = make_square(q[1], q[1], nullptr, q[2], 1.0, 0.0, 0.0)) return rc;            // E = P P
             if (const int rc = make_square(q[0], q[2], q[2], q[3], 1.0, h, -at.next)) return rc;            // D E + h E - h' I
@@ -1181,7 +1197,7 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
                 g.old = x_now;
                 g.c_old = (float)at.value;
             }
-            if (const int rc = launch<kOf, kNext>(g, members, next_edge, stream)) return rc;
+            if (const int rc = launch<kOf, kNext>(g, members, plan.next_edge, stream)) return rc;
             continue;
         }
         // the last product writes with G's orientation
@@ -1204,7 +1220,7 @@ int iterate(const Members &x, int type, u64 ldx, const Shape &s, u32 members, u3
         g.gain = target.gain;
         g.keep = target.keep;
         g.update = target.update;
-        if (const int rc = launch<kOf, kLast>(g, members, next_edge, stream)) return rc;
+        if (const int rc = launch<kOf, kLast>(g, members, plan.next_edge, stream)) return rc;
     }
     return RTOPK_OK;
 }
@@ -1248,6 +1264,31 @@ extern "C" int rtopk_orthogonalize_workspace_bytes(uint32_t count, uint64_t rows
     if (!bytes || !sizes_ok(count, rows, cols, products)) return RTOPK_EINVAL;
     Parts p;
     *bytes = cut(products, nullptr, count, Shape{(u32)rows, (u32)cols}, false, p);
+    return RTOPK_OK;
+}
+
+extern "C" int rtopk_orthogonalize_plan(uint32_t count, uint64_t rows, uint64_t cols, int products, uint32_t steps,
+                                        const float *coefficients, rtopk_orthogonalize_plan_t *plan)
+{
+    double largest_p = 0.0;
+    if (!plan || count > kMembers || !sizes_ok(count, rows, cols, products) || !iteration_ok(steps, coefficients, 0.0f, &largest_p))
+        return RTOPK_EINVAL;
+    const Shape s{(u32)rows, (u32)cols};
+    *plan = rtopk_orthogonalize_plan_t{};
+    if (is_narrow(s)) {
+        const NarrowPlan p = plan_narrow(s, count);
+        plan->narrow = 1;
+        plan->gram_runs = p.runs;
+        plan->joined = p.join;
+        return RTOPK_OK;
+    }
+    const StepPlan p = products == RTOPK_PRODUCTS_PAIRS ? plan_step<kPairs>(count, s, largest_p) : plan_step<kHalves>(count, s, largest_p);
+    plan->gram_edge = p.gram.edge;
+    plan->gram_runs = p.gram.splits;
+    plan->joined = p.gram.splits > 1;
+    plan->square_edge = p.square_edge;
+    plan->next_edge = p.next_edge;
+    plan->two_at_a_time = p.twos;
     return RTOPK_OK;
 }
 
