@@ -582,6 +582,9 @@ namespace {
 // A sum of so many slices of products of -128 .. 127 stays below 2^31.
 constexpr u32 kMostSlices = 1016;
 
+// Tiles have 512 threads, and a launch less than 2^32 (2^22 x 2^15 of few terms would take so many tiles of 128).
+constexpr u64 kMostTiles = 1u << 23;
+
 struct Plan {
     u32 edge, tiles, slices, slices_each, splits;
     u64 part_bytes;
@@ -600,6 +603,7 @@ Plan plan_product(u32 m, u32 n, u32 k, bool on_lines)
         for (u32 splits = must; splits <= std::max(must, std::min(16u, slices / 4)); ++splits) {
             const u32 each = std::max(1u, (slices + splits - 1) / splits);
             if (splits > must && (slices + each - 1) / each != splits) continue;
+            if (tiles * splits >= kMostTiles && edge < 256) continue;
             double cost = tiles_cost(kCostBytes, edge, tiles * splits, each * (on_lines ? 1.0 : 1.3));
             if (splits > 1) cost += 3.0 + (double)m * n * splits * 8.0 / 6e6;
             if (best.edge && cost >= least) continue;

@@ -34,3 +34,12 @@ def test_refusals():
         with pytest.raises(rt.RtopkError):
             rt.orthogonalize_plan(**{**dict(count=1, rows=100, cols=200), **bad})
     assert rt.orthogonalize_plan(2, 64, 5000)["narrow"] == 1
+
+
+@pytest.mark.parametrize("m, n", [(1 << 22, 1 << 15), (1 << 15, 1 << 22), (1 << 22, 33_000), (1 << 22, 40_000), (1 << 22, 1 << 14)])
+def test_a_launch_of_tiles_has_less_than_2_to_32_threads(m, n):
+    """Results of up to 288 GB: a tile has 512 threads."""
+    for k in (1, 8, 64, 100, 129, 500):
+        for on_lines in (True, False):
+            p = rt.product_plan(m, n, k, on_lines)
+            assert p["tiles"] * p["runs"] * 512 < 1 << 32, (k, p)
