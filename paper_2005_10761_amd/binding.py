@@ -425,6 +425,8 @@ def _bytes(name: str, *args) -> int:
 def _workspace(workspace: Optional[torch.Tensor], need: int, device, stream):
     """The caller's workspace, or memory of torch's allocator on the call's stream: (pointer, bytes, what holds it)."""
     if workspace is not None:
+        if not workspace.is_cuda or not workspace.is_contiguous():
+            raise TypeError("workspace must be a contiguous tensor on the GPU")
         return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
     if not need:
         return None, 0, None
