@@ -612,6 +612,8 @@ def aggregate_update_orthogonal(idx, val, n: int, k: int, eta: float, scale: flo
     count = len(omega)
     if count < 1 or not (len(idx) == len(val) == len(velocity) == count):
         raise ValueError("idx, val, omega and velocity must have the same length >= 1")
+    if n < 1 or k < 1:
+        raise ValueError("n and k must be at least 1")
     if omega[0].dim() != 2:
         raise ValueError("omega must hold matrices")
     rows, cols = omega[0].shape
