@@ -164,81 +164,81 @@ __device__ __forceinline__ u32 lane_left(u32 v, u32 first)
 // groups: workers are taken 64 at a time; with one group, lane w's pos0 is where worker w's entries begin, and where
 // the next tile's begin afterwards.
 __device__ __forceinline__ void add_messages(float *tile, const u32 *__restrict__ idx, const float *__restrict__ val, u32 n, u64 k,
-                                             u64 tile_base, u64 tile_end, u32 groups, u64 &pos0)
+                                     u64 tile_base, u64 tile_end, u32 groups, u64 &pos0)
 {
     const u32 lane = lane_id();
-            for (u32 w0 = 0; w0 < n; w0 += kWave) {
-                const u32 nw = n - w0 < (u32)kWave ? n - w0 : (u32)kWave;
-                u64 lo = groups == 1 ? pos0 : wave_lower_bounds(idx, w0, nw, k, tile_base, 0, k);
-                // ---- worker after worker: the next 64 pairs of its message in one
-                //      coalesced load, those below the tile's end added into the tile;
-                //      the loads of kAggAhead workers are in flight together --------
-                for (u32 g0 = 0; g0 < nw; g0 += kAggAhead) {
-                    u64 from[kAggAhead];
-                    u32 ri[kAggAhead];
-                    float rv[kAggAhead];
-    #pragma unroll
-                    for (int q = 0; q < kAggAhead; ++q) {
-                        const u32 w = g0 + q < nw ? g0 + q : nw - 1;
-                        from[q] = read_lane_u64(lo, (int)w);
-                        const u64 j = from[q] + lane;
-                        const bool in = g0 + q < nw && j < k;
-                        ri[q] = in ? idx[(u64)(w0 + w) * k + j] : 0xFFFFFFFFu;
-                        rv[q] = in ? val[(u64)(w0 + w) * k + j] : 0.0f;
-                    }
-    #pragma unroll
-                    for (int q = 0; q < kAggAhead; ++q) {
-                        if (g0 + q >= nw) break;
-                        const u32 w = g0 + q;
-                        const u32 *si = idx + (u64)(w0 + w) * k;
-                        const float *sv = val + (u64)(w0 + w) * k;
-                        u64 at = from[q];
-                        // 64 pairs into the tile; returns how many of them lay inside it
-                        auto add_slice = [&](u32 i, float v) -> u32 {
-                            const bool inside = (u64)i < tile_end;     // 0xFFFFFFFF marks "no entry"
-                            const u64 mask = __ballot(inside);         // a prefix of the lanes: sorted
-                            // repeated indices inside one message (never produced by the
-                            // encoder, but allowed) must be added in position order
-                            const bool dup = inside && lane_left(i, 0xFFFFFFFFu) == i;
-                            if (__ballot(dup) == 0ull) {
-                                if (inside) tile[i - tile_base] += v;
-                            } else {
-                                for (u64 rest = mask; rest; rest &= rest - 1) {
-                                    const int src = __ffsll((unsigned long long)rest) - 1;
-                                    if ((int)lane == src) tile[i - tile_base] += v;
-                                }
-                            }
-                            return popc_mask(mask);
-                        };
-                        u32 took = add_slice(ri[q], rv[q]);
-                        at += took;
-                        // The slice filled all 64 lanes: the message is crowded here (its
-                        // entries cluster in a few tiles). The next kAggMore slices are
-                        // fetched together and added in order up to the first that ends
-                        // inside the tile.
-                        while (took == (u32)kWave) {
-                            u32 mi[kAggMore];
-                            float mv[kAggMore];
-    #pragma unroll
-                            for (int s2 = 0; s2 < kAggMore; ++s2) {
-                                const u64 j = at + (u64)s2 * kWave + lane;
-                                mi[s2] = j < k ? si[j] : 0xFFFFFFFFu;
-                                mv[s2] = j < k ? sv[j] : 0.0f;
-                            }
-    #pragma unroll
-                            for (int s2 = 0; s2 < kAggMore; ++s2) {
-                                if (took == (u32)kWave) {
-                                    took = add_slice(mi[s2], mv[s2]);
-                                    at += took;
-                                }
-                            }
+    for (u32 w0 = 0; w0 < n; w0 += kWave) {
+        const u32 nw = n - w0 < (u32)kWave ? n - w0 : (u32)kWave;
+        u64 lo = groups == 1 ? pos0 : wave_lower_bounds(idx, w0, nw, k, tile_base, 0, k);
+        // ---- worker after worker: the next 64 pairs of its message in one
+        //      coalesced load, those below the tile's end added into the tile;
+        //      the loads of kAggAhead workers are in flight together --------
+        for (u32 g0 = 0; g0 < nw; g0 += kAggAhead) {
+            u64 from[kAggAhead];
+            u32 ri[kAggAhead];
+            float rv[kAggAhead];
+#pragma unroll
+            for (int q = 0; q < kAggAhead; ++q) {
+                const u32 w = g0 + q < nw ? g0 + q : nw - 1;
+                from[q] = read_lane_u64(lo, (int)w);
+                const u64 j = from[q] + lane;
+                const bool in = g0 + q < nw && j < k;
+                ri[q] = in ? idx[(u64)(w0 + w) * k + j] : 0xFFFFFFFFu;
+                rv[q] = in ? val[(u64)(w0 + w) * k + j] : 0.0f;
+            }
+#pragma unroll
+            for (int q = 0; q < kAggAhead; ++q) {
+                if (g0 + q >= nw) break;
+                const u32 w = g0 + q;
+                const u32 *si = idx + (u64)(w0 + w) * k;
+                const float *sv = val + (u64)(w0 + w) * k;
+                u64 at = from[q];
+                // 64 pairs into the tile; returns how many of them lay inside it
+                auto add_slice = [&](u32 i, float v) -> u32 {
+                    const bool inside = (u64)i < tile_end;     // 0xFFFFFFFF marks "no entry"
+                    const u64 mask = __ballot(inside);         // a prefix of the lanes: sorted
+                    // repeated indices inside one message (never produced by the
+                    // encoder, but allowed) must be added in position order
+                    const bool dup = inside && lane_left(i, 0xFFFFFFFFu) == i;
+                    if (__ballot(dup) == 0ull) {
+                        if (inside) tile[i - tile_base] += v;
+                    } else {
+                        for (u64 rest = mask; rest; rest &= rest - 1) {
+                            const int src = __ffsll((unsigned long long)rest) - 1;
+                            if ((int)lane == src) tile[i - tile_base] += v;
                         }
-                        // the new position of worker w goes back into lane w
-                        if (lane == w) lo = at;
+                    }
+                    return popc_mask(mask);
+                };
+                u32 took = add_slice(ri[q], rv[q]);
+                at += took;
+                // The slice filled all 64 lanes: the message is crowded here (its
+                // entries cluster in a few tiles). The next kAggMore slices are
+                // fetched together and added in order up to the first that ends
+                // inside the tile.
+                while (took == (u32)kWave) {
+                    u32 mi[kAggMore];
+                    float mv[kAggMore];
+#pragma unroll
+                    for (int s2 = 0; s2 < kAggMore; ++s2) {
+                        const u64 j = at + (u64)s2 * kWave + lane;
+                        mi[s2] = j < k ? si[j] : 0xFFFFFFFFu;
+                        mv[s2] = j < k ? sv[j] : 0.0f;
+                    }
+#pragma unroll
+                    for (int s2 = 0; s2 < kAggMore; ++s2) {
+                        if (took == (u32)kWave) {
+                            took = add_slice(mi[s2], mv[s2]);
+                            at += took;
+                        }
                     }
                 }
-                if (groups == 1) pos0 = lo;
+                // the new position of worker w goes back into lane w
+                if (lane == w) lo = at;
             }
+        }
+        if (groups == 1) pos0 = lo;
+    }
 }
 
 // What the momentum form of the kernel does with the average of a coordinate:

@@ -684,7 +684,6 @@ int run_product(Scaled g, void *part, hipStream_t stream)
 constexpr u64 kMostSize = 1u << 22;
 
 bool size_ok(u64 v) { return v >= 1 && v <= kMostSize; }
-bool type_ok(int type) { return type == RTOPK_F32 || type == RTOPK_BF16 || type == RTOPK_F16; }
 
 template <int kType>
 void launch_rows(const RowsToQuantize &g, hipStream_t stream)
@@ -752,18 +751,6 @@ int quantize_columns(const Columns &c, u32 count, int type, hipStream_t stream)
 bool workspace_ok(const void *p, u64 bytes, u64 need) { return need == 0 || (p && ((uintptr_t)p & 255u) == 0 && bytes >= need); }
 
 u64 filled(u32 k) { return align_up(k, kSlice); }
-
-// How the workspaces of the two layer calls are laid out, part after part.
-struct Cut {
-    unsigned char *base;
-    u64 at = 0;
-    template <class P> P *take(u64 bytes)
-    {
-        P *p = base ? (P *)(base + at) : nullptr;     // (without a base only the size is asked for)
-        at += align_up(bytes, 256);
-        return p;
-    }
-};
 
 struct LinearParts {
     signed char *x;

@@ -488,6 +488,20 @@ __device__ __forceinline__ void write_eight(void *p, u64 at, int type, const f32
     }
 }
 
+inline bool type_ok(int type) { return type >= 0 && type <= 2; }
+
+// How a call's workspace is laid out, part after part.
+struct Cut {
+    unsigned char *base;
+    u64 at = 0;
+    template <class P> P *take(u64 bytes)
+    {
+        P *p = base ? (P *)(base + at) : nullptr;     // (without a base only the size is asked for)
+        at += align_up(bytes, 256);
+        return p;
+    }
+};
+
 // What a launch of tiles costs, in microseconds: a launch, the tiles that one compute unit gets one after the other, their
 // slices, and what comes before and after them. 64 x 64: up to three tiles share a unit; 128 x 128: two. From launches of
 // 256, 512, .. tiles at 8 and 64 slices, with the slices of smaller tiles as they are where the whole chip reads (a

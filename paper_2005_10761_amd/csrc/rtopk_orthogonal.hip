@@ -917,33 +917,27 @@ u64 cut(void *base, u32 count, const Shape &s, bool direction, Parts &p)
 {
     typedef Stored<kOf> S;
     const u32 members = std::min(count, kMembers);
-    unsigned char *at = (unsigned char *)base;
-    u64 used = 0;
-    auto take = [&](u64 bytes) {
-        unsigned char *q = at ? at + used : nullptr;            // (without a base only the size is asked for)
-        used += align_up(bytes, 256);
-        return q;
-    };
+    Cut cut{(unsigned char *)base};
     p.x_stride = align_up((u64)s.m() * S::row_bytes(s.n()), 256);
     p.xt_stride = align_up((u64)s.n() * S::row_bytes(s.m()), 256);
     p.square_stride = align_up((u64)s.m() * S::row_bytes(s.m()), 256);
-    p.norm = (double *)take(kMembers * kNormBlocks * sizeof(double));
-    p.scale = (float *)take((kMostSteps + 1) * kMembers * sizeof(float));
+    p.norm = cut.take<double>(kMembers * kNormBlocks * sizeof(double));
+    p.scale = cut.take<float>((kMostSteps + 1) * kMembers * sizeof(float));
     if (is_narrow(s)) {
-        for (int i = 0; i < 2; ++i) p.xt[i] = take(members * p.xt_stride);
+        for (int i = 0; i < 2; ++i) p.xt[i] = cut.take<unsigned char>(members * p.xt_stride);
         // (fewer matrices have more runs each, but not more in all than 2 * kUnits and what rounding up adds)
         const u64 runs = std::max((u64)members * plan_narrow(s, members).runs,
                                   count > kMembers && count % kMembers ? (u64)(count % kMembers) * plan_narrow(s, count % kMembers).runs : 0);
-        p.part = (float *)take(2 * runs * kSide * kSide * sizeof(float));
-        p.joined = (float *)take((u64)members * kSide * kSide * sizeof(float));
-        p.direction = direction ? (float *)take(members * align_up((u64)s.rows * s.cols, 64) * sizeof(float)) : nullptr;
-        return used;
+        p.part = cut.take<float>(2 * runs * kSide * kSide * sizeof(float));
+        p.joined = cut.take<float>((u64)members * kSide * kSide * sizeof(float));
+        p.direction = direction ? cut.take<float>(members * align_up((u64)s.rows * s.cols, 64) * sizeof(float)) : nullptr;
+        return cut.at;
     }
     for (int i = 0; i < 2; ++i) {
-        p.x[i] = take(members * p.x_stride);
-        p.xt[i] = take(members * p.xt_stride);
+        p.x[i] = cut.take<unsigned char>(members * p.x_stride);
+        p.xt[i] = cut.take<unsigned char>(members * p.xt_stride);
     }
-    for (int i = 0; i < 4; ++i) p.square[i] = take(members * p.square_stride);
+    for (int i = 0; i < 4; ++i) p.square[i] = cut.take<unsigned char>(members * p.square_stride);
     auto sums = [&](u32 matrices) {
         double cost;
         const u32 splits = matrices ? plan_gram<kOf>(matrices, s, &cost).splits : 1;
@@ -951,9 +945,9 @@ u64 cut(void *base, u32 count, const Shape &s, bool direction, Parts &p)
     };
     // (the last launches may have fewer matrices, and more runs)
     const u64 part = std::max(sums(members), sums(count > kMembers ? count % kMembers : 0));
-    p.part = (float *)take(part * sizeof(float));
-    p.direction = direction ? (float *)take(members * align_up((u64)s.rows * s.cols, 64) * sizeof(float)) : nullptr;
-    return used;
+    p.part = cut.take<float>(part * sizeof(float));
+    p.direction = direction ? cut.take<float>(members * align_up((u64)s.rows * s.cols, 64) * sizeof(float)) : nullptr;
+    return cut.at;
 }
 
 u64 cut(int products, void *base, u32 count, const Shape &s, bool direction, Parts &p)
@@ -1240,7 +1234,6 @@ u32 norm_blocks(u64 d, u32 members)
     return (u32)std::min<u64>(std::min(most, enough), kNormBlocks);
 }
 
-bool type_ok(int type) { return type == RTOPK_F32 || type == RTOPK_BF16 || type == RTOPK_F16; }
 bool sizes_ok(uint32_t count, uint64_t rows, uint64_t cols, int products)
 {
     return count >= 1 && rows >= 1 && cols >= 1 && rows <= kMostSide && cols <= kMostSide && rows * cols <= 0xFFFFFFFFull &&
