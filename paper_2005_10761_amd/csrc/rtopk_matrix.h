@@ -76,7 +76,9 @@ __device__ __forceinline__ i32x4 cut_piece(const i32x4 &v, u32 at, u32 bytes)
 //   256 x 256, 2 x 4, by instructions of 32 x 32                2359    1161    436
 //   256 x 256, 2 x 2                                            2175    1112      -    (one wavefront a SIMD: nobody fills its waits)
 //   128 x 128, 2 x 2                                            1953     949    464    (two workgroups a unit; alone on its unit 388)
-// What bounds 256 x 256 is power: the matrix units are busy in 65% of the cycles, and the clock falls from 2.4 to 1.7 GHz.
+// What bounds 256 x 256 with bytes is power: the matrix units are busy in 65% of the cycles, and the clock falls from 2.4 to 1.7
+// GHz; the library's product reaches 2116 under the same limit. Pairs (1437 as the halves that are multiplied) are within 4% of the
+// library's 1491 for halves. Halves alone are not (1240), so power is not all that bounds them; what else does was not found.
 // 64 and 128 go to small results, on 2 x 4 wavefronts too: a slice of 64 x 64 takes 0.3 us alone on its unit, of which its
 // products are 0.08: the rest is one barrier and two trips to LDS one after the other (six stages in the place of three
 // change nothing, so it is not the loads). 192 is for pairs and for results where 256 leaves units without a tile; 160 was

@@ -267,7 +267,8 @@ __device__ __forceinline__ int exponent_of(const double *part, u32 parts, float 
 }
 
 // Blocks of 64 x 64, turned over in LDS, so that both forms are written in rows. Bound by one read and two writes: four
-// matrices of 6000 x 1500 binary32 into pairs, 432 MB, 84 us, 5.1 TB/s.
+// matrices of 6000 x 1500 binary32 into pairs, 432 MB, 81 us, 5.3 TB/s (the turned reads from LDS conflict in a third of
+// its cycles, which the stores cover).
 template <Operands kOf, int kType>
 __global__ void __launch_bounds__(kNormThreads) k_start(Start g)
 {
@@ -346,8 +347,9 @@ __device__ __forceinline__ void triangle_at(u32 at, u32 n, u32 &i, u32 &j)
 }
 
 // One tile of one product, its polynomial's terms and both forms of the result from the registers. Bound by the matrix
-// units where matrices are large: P X of 4096 x 4096 halves 123 us, 1117 10^12 operations a second; of four 1500 x 6000 with
-// pairs 348 us, 311 counted once and 932 as the halves that are multiplied; D of 512 x 512, three of them, 8.8 us, which
+// units where matrices are large: P X of 4096 x 4096 with pairs 286 us, 481 10^12 operations a second counted once and 1443 as the
+// halves that are multiplied (the library's product of halves reaches 1491), with halves 123 us, 1117; of four 1500 x 6000 with
+// pairs 282 us, 384 and 1151; D of 512 x 512, three of them, 8.5 us, which
 // are a launch, sixteen slices' barriers and a store.
 template <Operands kOf, class T, Step kStep>
 __global__ void __launch_bounds__(T::kThreads) k_step(Product g)
@@ -504,7 +506,7 @@ __global__ void __launch_bounds__(T::kThreads) k_step(Product g)
 }
 
 // The runs of X X^T together, in their order, scaled, less the multiple of the identity: D, both sides of the diagonal, by
-// blocks of 64 x 64. Bound by the reads of the parts: four of 1500 x 1500 in three runs (the half of 108 MB) 22 us.
+// blocks of 64 x 64. Bound by the reads of the parts: four of 1500 x 1500 in three runs (the half of 108 MB) 20 us.
 constexpr u32 kJoinThreads = kSide * kSide / 4;
 
 template <Operands kOf>
