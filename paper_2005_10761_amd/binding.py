@@ -381,6 +381,8 @@ def encode_stats(workspace: torch.Tensor, stream=None) -> dict:
 
 
 # ---- matrix parameters: a layer's products in 8-bit integers, orthogonalised updates ----------
+# (As in all calls of this module outputs are written where they lie and nothing is recorded for autograd: a layer's gradients
+# come from linear_i8_backward.)
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _INT8 = (torch.int8,)
