@@ -434,6 +434,179 @@ int rtopk_aggregate_update_orthogonal(uint32_t count, const uint32_t *const *idx
                                       int products, float *const *omega, float *const *velocity,
                                       void *workspace, uint64_t workspace_bytes, void *stream);
 
+/*
+ * The same products in 4-bit floating point with a scale for each block of 32
+ * numbers of the contraction. A number is one of 0, 1/2, 1, 3/2, 2, 3, 4, 6 and
+ * their negatives (sign, two exponent bits, one mantissa bit: E2M1), two a
+ * byte, the even one in the lower half; a scale is the byte b for 2^(b - 127),
+ * 255 for NaN. A quantised matrix is q, [rows][ldq] BYTES with (k + 1) / 2 of
+ * them in a row (the last half byte of an odd k is 0), and scale, turned over:
+ * [blocks][lds] bytes, a row of the matrix's `rows` scales for each of
+ * the (k + 31) / 32 blocks.
+ *
+ * rtopk_quantize_mx4 takes for each block, with RTOPK_NEAREST, the least scale
+ * with max |x| < 7 scale, and rounds x / scale to the nearest number, ties to
+ * even: no number is off by more than half the step of numbers around it. With
+ * RTOPK_DRAWN, the least scale with max |x| <= 6 scale, and x / scale goes to
+ * one of the two numbers around it by chance: up where a 16-bit draw u has
+ * u + 1/2 < 65536 f, f being how far it is from the lower one to the upper one
+ * in magnitude. The mean is x to within 2^-17 of a step, as a gradient needs
+ * it. The least scale of all is 2^-127. A block that holds an infinity or a
+ * not-a-number gets scale NaN and numbers 0, so that everything it goes into is NaN.
+ *
+ * Draws: number c % 8 of Philox4x32-10's eight 16-bit numbers (word by word,
+ * lower half first) for counter (g_lo, what << 24 | g_hi, step_lo, step_hi),
+ * key (seed_lo, seed_hi), g = row * 4 * blocks + c / 8 by the row and column c
+ * of q, what = 2 along rows, 3 along columns. `step_device`, if not null, is a
+ * device uint64 that the step number is read from when the kernels run: a graph that is
+ * replayed advances it, and each replay draws afresh.
+ *
+ * x      device, [rows][ldx] of `type`, rows 0 .. 2^22, cols 1 .. 2^22 <= ldx <= 2^22
+ * along  RTOPK_ROWS: q [rows][ldq], scale [(cols + 31) / 32][lds]; RTOPK_COLUMNS:
+ *        turned over, q [cols][ldq] with the rows of x along its rows, scale
+ *        [(rows + 31) / 32][lds]. ldq, lds <= 2^22
+ * q, scale  device; what lies between a row's end and ldq or lds is not
+ *        written. Rows of q that start on 16 bytes (base and ldq) and rows of
+ *        scale that start on 4 let the product load them directly
+ */
+#define RTOPK_NEAREST 0
+#define RTOPK_DRAWN 1
+int rtopk_quantize_mx4(const void *x, int type, uint64_t rows, uint64_t cols, uint64_t ldx,
+                       int along, int rounding, uint64_t seed, uint64_t step, const uint64_t *step_device,
+                       uint8_t *q, uint64_t ldq, uint8_t *scale, uint64_t lds, void *stream);
+
+/*
+ * Back to numbers: out[r][c] = number * scale in the type of `out` (beyond its
+ * largest an infinity). rows, cols  0 .. 2^22: of q's matrix, as it lies
+ */
+int rtopk_dequantize_mx4(const uint8_t *q, uint64_t rows, uint64_t cols, uint64_t ldq,
+                         const uint8_t *scale, uint64_t lds,
+                         void *out, int type, uint64_t ldo, void *stream);
+
+/*
+ * out[i][j] = sum_k a[i][k] b[j][k] + bias[j], binary32 sums of exact products.
+ *
+ * a, a_scale  device, a quantised matrix of m rows of k numbers: lda bytes from
+ *        row to row, lda_scale from block to block
+ * b, b_scale  device, n rows of k numbers
+ * bias   device, [n] binary32, or null
+ * m, n, k  0 .. 2^22 (k = 0: out is the bias); all distances of operands <= 2^22
+ * out    device, [m][ldo] of out_type; must not overlap an input
+ * workspace  device, 256-byte aligned, >= rtopk_matmul_mx4_workspace_bytes
+ */
+int rtopk_matmul_mx4_workspace_bytes(uint64_t m, uint64_t n, uint64_t k, uint64_t *bytes);
+int rtopk_matmul_mx4(const uint8_t *a, const uint8_t *a_scale, const uint8_t *b, const uint8_t *b_scale,
+                     const float *bias, uint64_t m, uint64_t n, uint64_t k,
+                     uint64_t lda, uint64_t lda_scale, uint64_t ldb, uint64_t ldb_scale,
+                     void *out, int out_type, uint64_t ldo,
+                     void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * A layer's forward product: x, quantised to the nearest along rows on the way,
+ * times weights that are quantised already: out = x w^T + bias.
+ *
+ * x      device, [m][ldx] of `type`, m tokens (0 .. 2^22) of k numbers
+ * w, w_scale  device, n rows of k numbers, a row for each output channel
+ * the rest as above; k and n are at least 1
+ */
+int rtopk_linear_mx4_workspace_bytes(uint64_t m, uint64_t k, uint64_t n, uint64_t *bytes);
+int rtopk_linear_mx4(const void *x, int type, uint64_t m, uint64_t k, uint64_t ldx,
+                     const uint8_t *w, const uint8_t *w_scale, uint64_t n, uint64_t ldw, uint64_t ldw_scale,
+                     const float *bias, void *out, int out_type, uint64_t ldo,
+                     void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * Its backward products, the gradients passed straight through the rounding:
+ *     dx = dy w        dy quantised along rows, w along columns
+ *     dw = dy^T x      both quantised along columns (over the tokens)
+ *     db = sum of dy's rows, in binary32 or more
+ * x is quantised to the nearest, dy by `rounding` with seed and step as in
+ * rtopk_quantize_mx4.
+ *
+ * dy, x  device, [m][lddy] and [m][ldx] of `type`
+ * w_turned, w_turned_scale  device, k rows of n numbers: the weights [n][k]
+ *        quantised along RTOPK_COLUMNS
+ * dx     device, [m][lddx] of `type`, or null
+ * dw     device, [n][lddw] binary32, or null (then x is not read): with
+ *        lddw = k the gradient as rtopk_encode takes it
+ * db     device, [n] binary32, or null; only with dw
+ * m = 0 writes zeros to dw and db
+ */
+int rtopk_linear_mx4_backward_workspace_bytes(uint64_t m, uint64_t k, uint64_t n, uint64_t *bytes);
+int rtopk_linear_mx4_backward(const void *dy, const void *x, int type,
+                              uint64_t m, uint64_t k, uint64_t n, uint64_t lddy, uint64_t ldx,
+                              const uint8_t *w_turned, const uint8_t *w_turned_scale,
+                              uint64_t ldw, uint64_t ldw_scale,
+                              int rounding, uint64_t seed, uint64_t step, const uint64_t *step_device,
+                              void *dx, uint64_t lddx, float *dw, uint64_t lddw, float *db,
+                              void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * Layer norm over the rows of a matrix, what stands before a layer's product:
+ *     mean = sum x / cols,  rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps)
+ *     out  = (x - mean) rstd gamma + beta
+ * in binary32 (rows of more than 16384 numbers are summed in binary64).
+ *
+ * x      device, [rows][ldx] of `type`, rows 0 .. 2^22, cols 1 .. 2^22 <= ldx <= 2^22
+ * gamma, beta  device, [cols] binary32, or null: 1, 0
+ * eps    >= 0. (A row of equal numbers with eps = 0 gives NaN.)
+ * out    device, [rows][ldo] of out_type, ldo <= 2^22; may be x itself (types
+ *        of one size, ldo = ldx), else must not overlap an input
+ * mean, rstd  device, [rows] binary32 each, for the backward pass; or null
+ */
+int rtopk_layer_norm(const void *x, int type, uint64_t rows, uint64_t cols, uint64_t ldx,
+                     const float *gamma, const float *beta, float eps,
+                     void *out, int out_type, uint64_t ldo, float *mean, float *rstd, void *stream);
+
+/*
+ * Its gradients. With h = (x - mean) rstd and g = dy gamma:
+ *     dx     = rstd (g - mean(g) - h mean(g h)) + add
+ *     dgamma = sum over rows of dy h,  dbeta = sum over rows of dy
+ * The sums over rows are taken in a fixed order: the same bits every time.
+ *
+ * dy     device, [rows][lddy] of dy_type; x device, [rows][ldx] of `type`
+ * mean, rstd  device, [rows], as rtopk_layer_norm leaves them
+ * gamma  device, [cols], or null: 1
+ * add    device, [rows][ldadd] of `type`, or null: the gradient that reaches x
+ *        past the norm; only with dx
+ * dx     device, [rows][lddx] of `type`, or null; may be dy (types of one size),
+ *        x or add itself (equal distances of rows), else must not overlap an input
+ * dgamma, dbeta  device, [cols] binary32 each, or null; rows = 0 writes zeros
+ * All distances of rows are 2^22 at most.
+ * workspace  device, 256-byte aligned, >= rtopk_layer_norm_backward_workspace_bytes;
+ *        not read where both dgamma and dbeta are null
+ */
+int rtopk_layer_norm_backward_workspace_bytes(uint64_t rows, uint64_t cols, uint64_t *bytes);
+int rtopk_layer_norm_backward(const void *dy, int dy_type, const void *x, int type, uint64_t rows, uint64_t cols,
+                              uint64_t lddy, uint64_t ldx, const float *mean, const float *rstd, const float *gamma,
+                              const void *add, uint64_t ldadd, void *dx, uint64_t lddx, float *dgamma, float *dbeta,
+                              void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * Dropout, what stands behind a layer's product; the mask is drawn and never
+ * stored. With T = p * 65536 rounded to a whole number (ties to even):
+ *     out = (u >= T ? x * 65536 / (65536 - T) : 0) + residual
+ * in binary32. What is dropped counts as 0, whatever it was. The gradient of x
+ * is the same call on out's gradient, with the same p, seed and step and without residual; the
+ * residual's is out's gradient itself.
+ *
+ * Draws: element e = row * cols + col has number e % 8 of the eight 16-bit
+ * numbers of counter (g_lo, 1 << 24 | g_hi, step_lo, step_hi), g = e / 8, as
+ * above. They do not depend on how the rows lie, and differ from those of
+ * rtopk_encode and rtopk_quantize_mx4 with the same seed and step.
+ *
+ * x      device, [rows][ldx] of `type`
+ * residual  device, [rows][ldr] of out_type, or null
+ * out    device, [rows][ldo] of out_type; may be x (types of one size, ldo =
+ *        ldx) or residual (ldo = ldr) itself, else must not overlap an input
+ * rows, cols  0 .. 2^32 - 1, rows * cols <= 2^40; distances of rows below 2^32
+ * p      0 .. 1
+ * step_device  a device uint64 that the step number is read from, or null
+ */
+int rtopk_dropout(const void *x, int type, uint64_t rows, uint64_t cols, uint64_t ldx,
+                  const void *residual, uint64_t ldr, void *out, int out_type, uint64_t ldo,
+                  double p, uint64_t seed, uint64_t step, const uint64_t *step_device, void *stream);
+
 const char *rtopk_strerror(int code);
 
 /* Library version: major * 10000 + minor * 100 + patch. */

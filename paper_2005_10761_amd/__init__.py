@@ -17,6 +17,9 @@ from .binding import (RtopkError, aggregate, aggregate_update, aggregate_update_
                       linear_i8, linear_i8_workspace_bytes, linear_i8_backward, linear_i8_backward_workspace_bytes,
                       orthogonalize, orthogonalize_workspace_bytes,
                       aggregate_update_orthogonal, aggregate_update_orthogonal_workspace_bytes,
+                      quantize_mx4, dequantize_mx4, matmul_mx4, matmul_mx4_workspace_bytes, linear_mx4, linear_mx4_workspace_bytes,
+                      linear_mx4_backward, linear_mx4_backward_workspace_bytes,
+                      layer_norm, layer_norm_backward, layer_norm_backward_workspace_bytes, dropout,
                       product_plan, orthogonalize_plan)
 
 __all__ = ["RtopkError", "aggregate", "aggregate_update", "aggregate_update_momentum", "aggregate_update_static", "STATIC_SCRATCH_BYTES", "aggregate_update_workspace_bytes", "aggregate_workspace_bytes", "encode", "encode_batch", "encode_batch_device_step", "diag_stream_add", "encode_stats",
@@ -25,4 +28,7 @@ __all__ = ["RtopkError", "aggregate", "aggregate_update", "aggregate_update_mome
            "QUINTIC", "quantize_i8", "quantize_i8_workspace_bytes", "matmul_i8", "matmul_i8_workspace_bytes",
            "linear_i8", "linear_i8_workspace_bytes", "linear_i8_backward", "linear_i8_backward_workspace_bytes",
            "orthogonalize", "orthogonalize_workspace_bytes", "aggregate_update_orthogonal",
-           "aggregate_update_orthogonal_workspace_bytes", "product_plan", "orthogonalize_plan"]
+           "aggregate_update_orthogonal_workspace_bytes",
+           "quantize_mx4", "dequantize_mx4", "matmul_mx4", "matmul_mx4_workspace_bytes", "linear_mx4", "linear_mx4_workspace_bytes",
+           "linear_mx4_backward", "linear_mx4_backward_workspace_bytes", "layer_norm", "layer_norm_backward",
+           "layer_norm_backward_workspace_bytes", "dropout", "product_plan", "orthogonalize_plan"]

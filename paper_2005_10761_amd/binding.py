@@ -25,6 +25,12 @@ EXPORTS = ("rtopk_encode_workspace_bytes", "rtopk_aggregate_workspace_bytes", "r
            "rtopk_linear_i8_backward_workspace_bytes", "rtopk_linear_i8_backward",
            "rtopk_orthogonalize_workspace_bytes", "rtopk_orthogonalize",
            "rtopk_aggregate_update_orthogonal_workspace_bytes", "rtopk_aggregate_update_orthogonal",
+           "rtopk_quantize_mx4", "rtopk_dequantize_mx4",
+           "rtopk_matmul_mx4_workspace_bytes", "rtopk_matmul_mx4",
+           "rtopk_linear_mx4_workspace_bytes", "rtopk_linear_mx4",
+           "rtopk_linear_mx4_backward_workspace_bytes", "rtopk_linear_mx4_backward",
+           "rtopk_layer_norm", "rtopk_layer_norm_backward_workspace_bytes", "rtopk_layer_norm_backward",
+           "rtopk_dropout",
            "rtopk_strerror", "rtopk_version")
 # ... and include/rtopk_diag.h
 DIAG_EXPORTS = ("rtopk_encode_stats", "rtopk_trace_next_encode", "rtopk_force_next_encode",
@@ -111,6 +117,19 @@ def load_library() -> ctypes.CDLL:
             "rtopk_linear_i8_workspace_bytes": [u64, u64, u64, pu64],
             "rtopk_linear_i8": [vp, i32, u64, u64, u64, vp, vp, u64, u64, vp, vp, i32, u64, vp, u64, vp],
             "rtopk_linear_i8_backward_workspace_bytes": [u64, u64, u64, pu64],
+            "rtopk_quantize_mx4": [vp, i32, u64, u64, u64, i32, i32, u64, u64, vp, vp, u64, vp, u64, vp],
+            "rtopk_dequantize_mx4": [vp, u64, u64, u64, vp, u64, vp, i32, u64, vp],
+            "rtopk_matmul_mx4_workspace_bytes": [u64, u64, u64, pu64],
+            "rtopk_matmul_mx4": [vp] * 5 + [u64] * 7 + [vp, i32, u64, vp, u64, vp],
+            "rtopk_linear_mx4_workspace_bytes": [u64, u64, u64, pu64],
+            "rtopk_linear_mx4": [vp, i32, u64, u64, u64, vp, vp, u64, u64, u64, vp, vp, i32, u64, vp, u64, vp],
+            "rtopk_linear_mx4_backward_workspace_bytes": [u64, u64, u64, pu64],
+            "rtopk_linear_mx4_backward": [vp, vp, i32, u64, u64, u64, u64, u64, vp, vp, u64, u64, i32, u64, u64, vp,
+                                          vp, u64, vp, u64, vp, vp, u64, vp],
+            "rtopk_layer_norm": [vp, i32, u64, u64, u64, vp, vp, f32, vp, i32, u64, vp, vp, vp],
+            "rtopk_layer_norm_backward_workspace_bytes": [u64, u64, pu64],
+            "rtopk_layer_norm_backward": [vp, i32, vp, i32, u64, u64, u64, u64, vp, vp, vp, vp, u64, vp, u64, vp, vp, vp, u64, vp],
+            "rtopk_dropout": [vp, i32, u64, u64, u64, vp, u64, vp, i32, u64, ctypes.c_double, u64, u64, vp, vp],
             "rtopk_linear_i8_backward": [vp, vp, i32, u64, u64, u64, u64, u64, vp, vp, u64, vp, u64,
                                          vp, u64, vp, vp, u64, vp],
             "rtopk_orthogonalize_workspace_bytes": [u32, u64, u64, i32, pu64],
@@ -555,6 +574,248 @@ def linear_i8_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w_turned: Op
         _ptr(dx), ld(dx), _ptr(dw), ld(dw), _ptr(db), ws, ws_bytes, _stream_handle(stream))
     if rc:
         raise RtopkError(rc, "rtopk_linear_i8_backward")
+
+
+# ---- the same products in 4-bit floating point, a scale for each block of 32 numbers of the contraction ----------
+
+_FOUR_BITS = (torch.uint8,)
+_ROUNDING = {"nearest": 0, "drawn": 1}
+_64_BITS = 2**64 - 1
+
+
+def _here(t: torch.Tensor, name: str, *others: Optional[torch.Tensor]) -> None:
+    """Refuses tensors of another device than the current one, whose stream the kernels go to."""
+    here = torch.cuda.current_device()
+    if t.get_device() != here or any(o is not None and o.get_device() != here for o in others):
+        raise ValueError(f"{name} and all that goes with it must be on the current device")
+
+
+def _packed(q: torch.Tensor, scale: torch.Tensor, rows: int, k: Optional[int], name: str):
+    """Distances (rows of bytes, blocks of scales) of a quantised matrix of ``rows`` rows, of k numbers if given."""
+    ldq, lds = _matrix(q, name, _FOUR_BITS), _matrix(scale, name + "'s scales", _FOUR_BITS)
+    have = q.size(1)
+    if q.size(0) != rows or (k is not None and have != (k + 1) // 2) or scale.size() != ((have + 15) // 16, rows):
+        raise ValueError(f"{name} must hold two numbers a byte, [rows, (k + 1) // 2], its scales [(k + 31) // 32, rows]")
+    return ldq, lds
+
+
+def _drawn(seed: Optional[int], step):
+    """(rounding, seed, step, the device's step or None) of a seed that may be None and a step that may be a tensor."""
+    if seed is None:
+        return 0, 0, 0, None
+    if isinstance(step, torch.Tensor):
+        _need(step, torch.int64, "step")
+        if step.numel() != 1:
+            raise ValueError("step on the device is one int64")
+        return 1, seed & _64_BITS, 0, step.data_ptr()
+    return 1, seed & _64_BITS, step & _64_BITS, None
+
+
+def quantize_mx4(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, along: str = "rows", seed: Optional[int] = None, step=0,
+                 stream=None) -> None:
+    """rtopk_quantize_mx4: the matrix ``x`` [rows, cols] to 4-bit numbers ``q`` (uint8, two a byte) with a scale (uint8)
+    for each block of 32. Along rows ``q`` is [rows, (cols + 1) // 2] and ``scale`` [(cols + 31) // 32, rows]; along
+    columns ``x`` is turned over, ``q`` [cols, (rows + 1) // 2] and ``scale`` [(rows + 31) // 32, cols]. With a ``seed``
+    numbers go up or down by chance, so that their mean is kept; ``step`` is an int, or one int64 on the GPU that is read when
+    the kernel runs. Give ``q`` rows that start on 16 bytes and ``scale`` rows that start on 4 where the product is to
+    read them fast."""
+    ldx = _matrix(x, "x", _TYPES)
+    rows, cols = x.size()
+    ldq, lds = _packed(q, scale, *((rows, cols) if along == "rows" else (cols, rows)), "q")
+    rounding, seed, step, at = _drawn(seed, held := step)
+    _here(x, "x", q, scale, held if at else None)
+    rc = load_library().rtopk_quantize_mx4(x.data_ptr(), _TYPES[x.dtype], rows, cols, ldx, _ALONG[along], rounding, seed, step, at,
+                                           q.data_ptr(), ldq, scale.data_ptr(), lds, _stream_handle(stream))
+    if rc:
+        raise RtopkError(rc, "rtopk_quantize_mx4")
+
+
+def dequantize_mx4(q: torch.Tensor, scale: torch.Tensor, out: torch.Tensor, stream=None) -> None:
+    """rtopk_dequantize_mx4: the numbers of a matrix that :func:`quantize_mx4` left, ``out`` of ``q``'s rows."""
+    ldo = _matrix(out, "out", _TYPES)
+    rows, cols = out.size()
+    ldq, lds = _packed(q, scale, rows, cols, "q")
+    _here(out, "out", q, scale)
+    rc = load_library().rtopk_dequantize_mx4(q.data_ptr(), rows, cols, ldq, scale.data_ptr(), lds, out.data_ptr(), _TYPES[out.dtype], ldo,
+                                             _stream_handle(stream))
+    if rc:
+        raise RtopkError(rc, "rtopk_dequantize_mx4")
+
+
+@functools.lru_cache(maxsize=1024)
+def matmul_mx4_workspace_bytes(m: int, n: int, k: int) -> int:
+    return _bytes("rtopk_matmul_mx4_workspace_bytes", m, n, k)
+
+
+def matmul_mx4(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor, out: torch.Tensor,
+               bias: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """rtopk_matmul_mx4: out = a b^T (+ bias) of two quantised matrices of equal rows, out [a's rows, b's rows]."""
+    ldo = _matrix(out, "out", _TYPES)
+    m, n = out.size()
+    lda, lda_scale = _packed(a, a_scale, m, None, "a")
+    ldb, ldb_scale = _packed(b, b_scale, n, None, "b")
+    if a.size(1) != b.size(1):
+        raise ValueError("a and b must have rows of equal length")
+    k = 2 * a.size(1)                       # (the last half byte of an odd length is 0)
+    if bias is not None:
+        _vector(bias, n, "bias")
+    _here(out, "out", a, a_scale, b, b_scale, bias, workspace)
+    need = 0 if workspace is not None else matmul_mx4_workspace_bytes(m, n, k)
+    ws, ws_bytes, held = _workspace(workspace, need, out.device, stream)
+    rc = load_library().rtopk_matmul_mx4(a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), _ptr(bias), m, n, k, lda,
+                                         lda_scale, ldb, ldb_scale, out.data_ptr(), _TYPES[out.dtype], ldo, ws, ws_bytes,
+                                         _stream_handle(stream))
+    if rc:
+        raise RtopkError(rc, "rtopk_matmul_mx4")
+
+
+@functools.lru_cache(maxsize=1024)
+def linear_mx4_workspace_bytes(m: int, k: int, n: int) -> int:
+    return _bytes("rtopk_linear_mx4_workspace_bytes", m, k, n)
+
+
+def linear_mx4(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, out: torch.Tensor, bias: Optional[torch.Tensor] = None,
+               workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """rtopk_linear_mx4: out = x w^T + bias, ``x`` [m, k] quantised along rows on the way, ``w`` [n, (k + 1) // 2] with
+    ``w_scale`` [(k + 31) // 32, n] as :func:`quantize_mx4` leaves them."""
+    ldx, ldo = _matrix(x, "x", _TYPES), _matrix(out, "out", _TYPES)
+    (m, k), n = x.size(), out.size(1)
+    ldw, ldw_scale = _packed(w, w_scale, n, k, "w")
+    if out.size(0) != m:
+        raise ValueError("x is [m, k], out [m, n]")
+    if bias is not None:
+        _vector(bias, n, "bias")
+    _here(x, "x", w, w_scale, out, bias, workspace)
+    need = 0 if workspace is not None else linear_mx4_workspace_bytes(m, k, n)
+    ws, ws_bytes, held = _workspace(workspace, need, x.device, stream)
+    rc = load_library().rtopk_linear_mx4(x.data_ptr(), _TYPES[x.dtype], m, k, ldx, w.data_ptr(), w_scale.data_ptr(), n, ldw, ldw_scale,
+                                         _ptr(bias), out.data_ptr(), _TYPES[out.dtype], ldo, ws, ws_bytes, _stream_handle(stream))
+    if rc:
+        raise RtopkError(rc, "rtopk_linear_mx4")
+
+
+@functools.lru_cache(maxsize=1024)
+def linear_mx4_backward_workspace_bytes(m: int, k: int, n: int) -> int:
+    return _bytes("rtopk_linear_mx4_backward_workspace_bytes", m, k, n)
+
+
+def linear_mx4_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w_turned: Optional[torch.Tensor],
+                        w_turned_scale: Optional[torch.Tensor], dx: Optional[torch.Tensor], dw: Optional[torch.Tensor],
+                        db: Optional[torch.Tensor] = None, seed: Optional[int] = None, step=0,
+                        workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """rtopk_linear_mx4_backward: the gradients of :func:`linear_mx4`'s input, weights (binary32, [n, k]) and bias from
+    ``dy`` [m, n]. ``w_turned`` [k, (n + 1) // 2] and its scales: the weights quantised along columns. With a ``seed``
+    ``dy`` is rounded by chance, as :func:`quantize_mx4` does. ``dx`` or ``dw`` may be None, and then what only they need too."""
+    if dx is None and dw is None:
+        raise ValueError("neither dx nor dw is asked for")
+    if dx is not None and (w_turned is None or w_turned_scale is None) or dw is not None and x is None:
+        raise ValueError("dx needs w_turned and its scales, dw needs x")
+    if db is not None and dw is None:
+        raise ValueError("db comes with dw")
+    _matrix(dy, "dy", _TYPES)
+    m, n = dy.shape
+    k = (dx if dx is not None else dw).size(1)
+    ldw = ldw_scale = 0
+    if dx is not None:
+        _matrix(dx, "dx", (dy.dtype,))
+        if tuple(dx.shape) != (m, k):
+            raise ValueError("dy is [m, n], dx [m, k]")
+        ldw, ldw_scale = _packed(w_turned, w_turned_scale, k, n, "w_turned")
+    if dw is not None:
+        _matrix(x, "x", (dy.dtype,))
+        _matrix(dw, "dw", (torch.float32,))
+        if tuple(x.shape) != (m, k) or tuple(dw.shape) != (n, k):
+            raise ValueError("dy is [m, n], x [m, k], dw [n, k]")
+    if db is not None:
+        _vector(db, n, "db")
+    rounding, seed, step, at = _drawn(seed, held := step)
+    asked = (x if dw is not None else None, dw, db, workspace, held if at else None)
+    _here(dy, "dy", *asked, *((dx, w_turned, w_turned_scale) if dx is not None else ()))
+    ws, ws_bytes, room = _workspace(workspace, 0 if workspace is not None else linear_mx4_backward_workspace_bytes(m, k, n),
+                                    dy.device, stream)
+    ld = lambda t: 0 if t is None else _ld(t)   # noqa: E731
+    rc = load_library().rtopk_linear_mx4_backward(
+        _ptr(dy), _ptr(x), _TYPES[dy.dtype], m, k, n, _ld(dy), ld(x), _ptr(w_turned), _ptr(w_turned_scale), ldw, ldw_scale,
+        rounding, seed, step, at, _ptr(dx), ld(dx), _ptr(dw), ld(dw), _ptr(db), ws, ws_bytes, _stream_handle(stream))
+    if rc:
+        raise RtopkError(rc, "rtopk_linear_mx4_backward")
+
+
+# ---- what stands before and behind a layer's product: layer norm, dropout onto the residual path ------------------
+
+def layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], out: torch.Tensor,
+               mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, eps: float = 1e-5, stream=None) -> None:
+    """rtopk_layer_norm: out = (x - mean) rstd gamma + beta for each row of the matrix ``x``; ``gamma`` and ``beta``
+    binary32 of a row's length (None: 1, 0). ``mean`` and ``rstd`` (binary32, one a row) are left for
+    :func:`layer_norm_backward` where they are given. ``out`` may be ``x``."""
+    ldx, ldo = _matrix(x, "x", _TYPES), _matrix(out, "out", _TYPES)
+    rows, cols = x.size()
+    if out.size() != x.size():
+        raise ValueError("out must have the shape of x")
+    for t, length, name in ((gamma, cols, "gamma"), (beta, cols, "beta"), (mean, rows, "mean"), (rstd, rows, "rstd")):
+        if t is not None:
+            _vector(t, length, name)
+    _here(x, "x", gamma, beta, out, mean, rstd)
+    rc = load_library().rtopk_layer_norm(x.data_ptr(), _TYPES[x.dtype], rows, cols, ldx, _ptr(gamma), _ptr(beta), eps, out.data_ptr(),
+                                         _TYPES[out.dtype], ldo, _ptr(mean), _ptr(rstd), _stream_handle(stream))
+    if rc:
+        raise RtopkError(rc, "rtopk_layer_norm")
+
+
+@functools.lru_cache(maxsize=1024)
+def layer_norm_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return _bytes("rtopk_layer_norm_backward_workspace_bytes", rows, cols)
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, gamma: Optional[torch.Tensor],
+                        dx: Optional[torch.Tensor], dgamma: Optional[torch.Tensor] = None, dbeta: Optional[torch.Tensor] = None,
+                        add: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """rtopk_layer_norm_backward: the gradients of :func:`layer_norm`'s input (plus ``add``, what reaches ``x`` past the
+    norm) and of its weight and bias, binary32, from ``dy``. ``dx`` and ``add`` have the type of ``x``; any of the three
+    gradients may be None. ``dx`` may be ``dy``, ``x`` or ``add``."""
+    if dx is None and dgamma is None and dbeta is None:
+        raise ValueError("neither dx nor dgamma nor dbeta is asked for")
+    if add is not None and dx is None:
+        raise ValueError("add comes with dx")
+    lddy, ldx = _matrix(dy, "dy", _TYPES), _matrix(x, "x", _TYPES)
+    rows, cols = x.size()
+    lddx, ldadd = (0 if t is None else _matrix(t, name, (x.dtype,)) for t, name in ((dx, "dx"), (add, "add")))
+    if dy.size() != x.size() or any(t is not None and t.size() != x.size() for t in (dx, add)):
+        raise ValueError("dy, dx and add must have the shape of x")
+    for t, length, name in ((gamma, cols, "gamma"), (mean, rows, "mean"), (rstd, rows, "rstd"), (dgamma, cols, "dgamma"),
+                            (dbeta, cols, "dbeta")):
+        if t is not None:
+            _vector(t, length, name)
+    _here(x, "x", dy, mean, rstd, gamma, add, dx, dgamma, dbeta, workspace)
+    sums = dgamma is not None or dbeta is not None
+    need = layer_norm_backward_workspace_bytes(rows, cols) if sums and workspace is None else 0
+    ws, ws_bytes, held = _workspace(workspace, need, x.device, stream)
+    rc = load_library().rtopk_layer_norm_backward(
+        dy.data_ptr(), _TYPES[dy.dtype], x.data_ptr(), _TYPES[x.dtype], rows, cols, lddy, ldx, mean.data_ptr(), rstd.data_ptr(),
+        _ptr(gamma), _ptr(add), ldadd, _ptr(dx), lddx, _ptr(dgamma), _ptr(dbeta), ws, ws_bytes, _stream_handle(stream))
+    if rc:
+        raise RtopkError(rc, "rtopk_layer_norm_backward")
+
+
+def dropout(x: torch.Tensor, out: torch.Tensor, p: float, seed: int, step, residual: Optional[torch.Tensor] = None,
+            stream=None) -> None:
+    """rtopk_dropout: out = x with each element dropped with chance ``p`` (a whole number of 65536ths), the others scaled
+    by 1 / (1 - p), plus ``residual`` (of ``out``'s type). The mask belongs to ``seed``, ``step`` (an int, or one int64 on
+    the GPU that is read when the kernel runs) and the element's place: the gradient is the same call on ``out``'s.
+    ``out`` may be ``x`` or ``residual``."""
+    ldx, ldo = _matrix(x, "x", _TYPES), _matrix(out, "out", _TYPES)
+    ldr = 0 if residual is None else _matrix(residual, "residual", (out.dtype,))
+    rows, cols = x.size()
+    if out.size() != x.size() or (residual is not None and residual.size() != x.size()):
+        raise ValueError("out and residual must have the shape of x")
+    if seed is None:
+        raise TypeError("dropout needs a seed")
+    _, seed, step, at = _drawn(seed, held := step)
+    _here(x, "x", out, residual, held if at else None)
+    rc = load_library().rtopk_dropout(x.data_ptr(), _TYPES[x.dtype], rows, cols, ldx, _ptr(residual), ldr, out.data_ptr(),
+                                      _TYPES[out.dtype], ldo, p, seed, step, at, _stream_handle(stream))
+    if rc:
+        raise RtopkError(rc, "rtopk_dropout")
 
 
 def _coefficients(coefficients, steps: Optional[int]):

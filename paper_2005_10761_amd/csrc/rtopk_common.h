@@ -54,6 +54,46 @@ __device__ __forceinline__ u64 sample_key(u32 index, const PhiloxSeed &s)
 }
 
 // ---------------------------------------------------------------------------
+// What other calls draw from the same generator: eight 16-bit numbers of each counter (group_lo, what << 24 | group_hi,
+// step_lo, step_hi), word by word, lower half first. `what` keeps the calls' draws apart from each other and, being
+// above zero, from the sampling keys of the same seed and step (groups stay below 2^56).
+// ---------------------------------------------------------------------------
+enum DrawsFor : u32 { kDrawsForDropout = 1, kDrawsForRows = 2, kDrawsForColumns = 3 };
+
+struct Drawing {
+    u64 seed, step;
+    const u64 *step_device;         // if not null, the step number is read from there
+    __device__ __forceinline__ PhiloxSeed get() const
+    {
+        const u64 t = step_device ? *step_device : step;
+        return PhiloxSeed{(u32)seed, (u32)(seed >> 32), (u32)t, (u32)(t >> 32)};
+    }
+};
+
+struct EightDraws {
+    u32 word[4];
+    __device__ __forceinline__ u32 operator[](int i) const { return i & 1 ? word[i >> 1] >> 16 : word[i >> 1] & 0xFFFFu; }
+};
+
+__device__ __forceinline__ EightDraws draw_eight(u64 group, DrawsFor what, const PhiloxSeed &s)
+{
+    u32 c0 = (u32)group, c1 = (u32)(group >> 32) | (u32)what << 24, c2 = s.step_lo, c3 = s.step_hi;
+    u32 k0 = s.seed_lo, k1 = s.seed_hi;
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+        const u64 p0 = (u64)0xD2511F53u * c0, p1 = (u64)0xCD9E8D57u * c2;
+        const u32 n0 = xor3((u32)(p1 >> 32), c1, k0), n2 = xor3((u32)(p0 >> 32), c3, k1);
+        c1 = (u32)p1;
+        c3 = (u32)p0;
+        c0 = n0;
+        c2 = n2;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return EightDraws{{c0, c1, c2, c3}};
+}
+
+// ---------------------------------------------------------------------------
 // Wave-level helpers.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ u32 lane_id() { return threadIdx.x & (kWave - 1); }
@@ -108,6 +148,21 @@ __device__ __forceinline__ u32 wave_max_dpp(u32 v)
 __device__ __forceinline__ u32 wave_sum(u32 v)
 {
     return (u32)__builtin_amdgcn_readlane((int)wave_inclusive_sum(v), kWave - 1);
+}
+
+// The same for binary32, in one fixed order (a missing source lane reads as +0).
+__device__ __forceinline__ float wave_sum_f32(float v)
+{
+    auto at = [](u32 bits) { return __uint_as_float(bits); };
+    const u32 b = __float_as_uint(v);
+    float x = v + at(dpp_or_zero<0x111, 0xF, 0xF>(b));
+    x += at(dpp_or_zero<0x112, 0xF, 0xF>(b));
+    x += at(dpp_or_zero<0x113, 0xF, 0xF>(b));
+    x += at(dpp_or_zero<0x114, 0xF, 0xE>(__float_as_uint(x)));
+    x += at(dpp_or_zero<0x118, 0xF, 0xC>(__float_as_uint(x)));
+    x += at(dpp_or_zero<0x142, 0xA, 0xF>(__float_as_uint(x)));
+    x += at(dpp_or_zero<0x143, 0xC, 0xF>(__float_as_uint(x)));
+    return at((u32)__builtin_amdgcn_readlane((int)__float_as_uint(x), kWave - 1));
 }
 
 // smallest / largest value over the wavefront, in every lane (rare paths only:

@@ -1,0 +1,588 @@
+// A layer's products in 4-bit floating point with a scale for each block of 32 numbers of the contraction.
+//
+//   numbers    0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives (E2M1: sign, two exponent bits, one mantissa bit), two
+//              a byte, the even one in the lower half; a block's scale is the byte b for 2^(b - 127), 255 for NaN
+//   quantise   the least scale with max |x| < 7 scale (7 would round to 8, which there is not), x / scale to the
+//              nearest number, ties to even: no number is off by more than half a step. Drawn: the least scale with
+//              max |x| <= 6 scale, and up or down by chance, so that the mean is x / scale
+//   product    out[i][j] = sum over blocks of a_scale[i] b_scale[j] sum_32 a[i] b[j], + bias[j]
+//
+// A scale is a power of two, so all of the quantisation is exact but its one rounding; the matrix instruction takes
+// 128 numbers of a row with four scales, lane l has row l % 16 and block l / 16 of them, and its sums are binary32.
+// The scales lie turned over, [blocks][rows]: what neighbouring lanes need together is together in memory.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "../../include/rtopk.h"
+#include "../../include/rtopk_diag.h"
+#include "rtopk_matrix.h"
+
+namespace rtopk {
+
+constexpr u32 kBlock = 32;                  // numbers that share a scale
+constexpr u32 kStepBlocks = 4;              // blocks of one matrix instruction
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// ---------------------------------------------------------------------------
+// Quantisation.
+// ---------------------------------------------------------------------------
+
+// The scale's byte of a block whose largest |x| has these bits. One added to the exponent where the mantissa is 7/4 (3/2: more
+// than it) or more, by a carry; the least byte, 2^-127, for all that is smaller.
+__device__ __forceinline__ u32 scale_byte(u32 largest, bool drawn)
+{
+    if (largest >= 0x7F800000u) return 255u;
+    const u32 exponent = (largest + (drawn ? 0x3FFFFFu : 0x200000u)) >> 23;
+    return exponent > 2u ? exponent - 2u : 0u;
+}
+__device__ __forceinline__ float scale_value(u32 byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
+
+// Eight numbers by one scale, the first in the lowest bits; zeros where the scale is NaN.
+__device__ __forceinline__ u32 nearest_four_bits(const float (&x)[8], u32 byte)
+{
+    u32 word = 0;
+#if defined(__HIP_DEVICE_COMPILE__)
+    const float scale = scale_value(byte);
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, x[0], x[1], scale, 0);
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, x[2], x[3], scale, 1);
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, x[4], x[5], scale, 2);
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, x[6], x[7], scale, 3);
+#endif
+    return byte == 255u ? 0u : word;
+}
+
+// t = |x| / scale lies between two numbers, a step apart, a fraction f above the lower: up where a 16-bit draw u has
+// u + 1/2 < 65536 f (the chance is f to the nearest 2^-16). All of it is exact but, where t is far below a step, a product that may lose bits of
+// an f under 2^-17, which is never up.
+__device__ __forceinline__ u32 drawn_four_bits(float x, float inverse, u32 draw)
+{
+    const float t = fabsf(x) * inverse;
+    const float in_steps = t < 2.0f ? t + t : t < 4.0f ? t : 0.5f * t;
+    const float low = floorf(in_steps);
+    const u32 from = t < 2.0f ? 0u : t < 4.0f ? 2u : 4u;        // the places of 0, 1 (two steps of 1 below 2) and of 2 steps of 2 below 4
+    const u32 up = (float)draw + 0.5f < 65536.0f * (in_steps - low) ? 1u : 0u;
+    return (u32)low + from + up | (__float_as_uint(x) >> 31 << 3);
+}
+__device__ __forceinline__ u32 drawn_four_bits(const float (&x)[8], u32 byte, const EightDraws &u)
+{
+    const float inverse = __uint_as_float((254u - byte) << 23);     // (of NaN's byte: not used)
+    u32 word = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) word |= drawn_four_bits(x[i], inverse, u[i]) << (4 * i);
+    return byte == 255u ? 0u : word;
+}
+
+struct Packed {
+    unsigned char *q, *scale;
+    u64 ldq, lds;               // bytes from row to row of q, from block to block of scale
+};
+
+struct ToPack {
+    const void *x;
+    u64 ldx;                    // elements
+    u32 rows, cols;
+    u32 fill;                   // numbers of a row of q: zeros from cols on
+    Packed to;
+    Drawing drawing;
+};
+
+__device__ __forceinline__ u32 magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+// largest over the four lanes of a quad
+__device__ __forceinline__ u32 quad_max(u32 v)
+{
+    v = max(v, (u32)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));      // lanes 1 0 3 2
+    return max(v, (u32)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));   // lanes 2 3 0 1
+}
+
+// Bytes of four-bit numbers from `at` on of a row that has `bytes`
+__device__ __forceinline__ void write_bytes(unsigned char *row, u32 at, u32 word, u32 bytes)
+{
+    if (at + 4u <= bytes) {
+        __builtin_memcpy(row + at, &word, 4);
+    } else {
+#pragma unroll
+        for (u32 i = 0; i < 4; ++i)
+            if (at + i < bytes) row[at + i] = (unsigned char)(word >> (8 * i));
+    }
+}
+
+// groups of eight draws of a row of a contraction of so many numbers
+__device__ __forceinline__ u32 groups_of(u32 k) { return (k + kBlock - 1) / kBlock * (kBlock / 8); }
+
+// Along rows: a workgroup has kTileRows rows and 512 columns, a lane eight neighbours of a row, four lanes a block.
+constexpr int kPackThreads = 256;
+constexpr u32 kTileRows = 16, kTileColumns = 8 * kWave;
+
+template <int kType, bool kDrawn>
+__global__ void __launch_bounds__(kPackThreads) k_pack_rows(ToPack g)
+{
+    constexpr u32 kWaves = kPackThreads / kWave, kEach = kTileRows / kWaves;
+    __shared__ unsigned char scales[kTileColumns / kBlock][kTileRows];
+    const u32 lane = lane_id(), wave = threadIdx.x / kWave;
+    const u32 r0 = blockIdx.x * kTileRows + wave * kEach, c = blockIdx.y * kTileColumns + lane * 8u;
+    PhiloxSeed seed{};
+    if (kDrawn) seed = g.drawing.get();
+    const u32 blocks = (g.fill + kBlock - 1) / kBlock;
+    const u64 row_bytes = g.ldx * Eight<kType>::kSize;
+    Eight<kType> e[kEach];
+#pragma unroll
+    for (u32 q = 0; q < kEach; ++q) e[q].load((const unsigned char *)g.x + min(r0 + q, g.rows - 1u) * row_bytes, c, g.cols);
+#pragma unroll
+    for (u32 q = 0; q < kEach; ++q) {
+        const u32 r = r0 + q;
+        float v[8];
+        e[q].numbers(v, (const unsigned char *)g.x + min(r, g.rows - 1u) * row_bytes, c, g.cols);
+        u32 largest = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) largest = max(largest, magnitude(v[i]));
+        const u32 byte = scale_byte(quad_max(largest), kDrawn);
+        u32 word;
+        if (kDrawn) word = drawn_four_bits(v, byte, draw_eight((u64)r * groups_of(g.cols) + c / 8u, kDrawsForRows, seed));
+        else word = nearest_four_bits(v, byte);
+        if (r < g.rows) write_bytes(g.to.q + r * g.to.ldq, c / 2u, word, (g.fill + 1u) / 2u);
+        if ((lane & 3u) == 0) scales[lane >> 2][wave * kEach + q] = (unsigned char)byte;
+    }
+    __syncthreads();
+    const u32 row = threadIdx.x % kTileRows, block = threadIdx.x / kTileRows;
+    const u32 r = blockIdx.x * kTileRows + row, b = blockIdx.y * (kTileColumns / kBlock) + block;
+    if (r < g.rows && b < blocks) g.to.scale[b * g.to.lds + r] = scales[block][row];
+}
+
+// Along columns, and turned over: a wavefront has 32 rows and 64 columns, a lane four neighbouring rows of eight columns; a
+// workgroup has eight blocks of 32 rows, which it writes as 128 bytes of each column.
+constexpr u32 kTurnWaves = 8, kTurnThreads = kTurnWaves * kWave, kTurnRows = kTurnWaves * kBlock;
+
+struct ToTurn {
+    ToPack of;
+    float *sums;                // [groups of kTurnRows rows][cols], or null: the sums of the columns
+};
+struct Turns {
+    ToTurn of[2];
+    u32 drawn;                  // bit i: of[i] by chance
+};
+
+template <int kType, bool kDrawn>
+__device__ __forceinline__ void pack_columns(const ToTurn &t)
+{
+    const ToPack &g = t.of;
+    constexpr u32 kRow = kTurnRows / 2 + 4;                 // bytes of a column in LDS
+    __shared__ __align__(16) unsigned char turned[kWave * kRow];
+    __shared__ float sums[kTurnWaves][kWave];
+    const u32 lane = lane_id(), wave = threadIdx.x / kWave;
+    const u32 c0 = blockIdx.x * kWave, first = blockIdx.y * kTurnRows;
+    const u32 blocks = (g.fill + kBlock - 1) / kBlock;      // of a column
+    const u32 piece = lane & 7u, quad = lane >> 3, c = c0 + 8u * piece, r0 = first + wave * kBlock + 4u * quad;
+    PhiloxSeed seed{};
+    if (kDrawn) seed = g.drawing.get();
+    const u64 row_bytes = g.ldx * Eight<kType>::kSize;
+    Eight<kType> e[4];
+    float v[4][8];
+#pragma unroll
+    for (u32 b = 0; b < 4; ++b) e[b].load((const unsigned char *)g.x + min(r0 + b, g.rows - 1u) * row_bytes, c, g.cols);
+#pragma unroll
+    for (u32 b = 0; b < 4; ++b) {
+        e[b].numbers(v[b], (const unsigned char *)g.x + min(r0 + b, g.rows - 1u) * row_bytes, c, g.cols);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[b][i] = r0 + b < g.rows ? v[b][i] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        u32 largest = 0;
+        float sum = 0;
+#pragma unroll
+        for (u32 b = 0; b < 4; ++b) {
+            largest = max(largest, magnitude(v[b][i]));
+            sum += v[b][i];
+        }
+#pragma unroll
+        for (int o = 8; o < kWave; o <<= 1) {
+            largest = max(largest, (u32)__shfl_xor((int)largest, o, kWave));
+            sum += __shfl_xor(sum, o, kWave);
+        }
+        const u32 byte = scale_byte(largest, kDrawn), block = first / kBlock + wave;
+        if (quad == 0) {
+            if (c + i < g.cols && block < blocks) g.to.scale[block * g.to.lds + c + i] = (unsigned char)byte;
+            sums[wave][8 * piece + i] = sum;
+        }
+        u32 word = 0;
+        if (kDrawn) {
+            // (a group is eight rows of a column: two lanes share it)
+            const EightDraws u = draw_eight((u64)(c + i) * groups_of(g.rows) + r0 / 8u, kDrawsForColumns, seed);
+            const float inverse = __uint_as_float((254u - byte) << 23);
+#pragma unroll
+            for (u32 b = 0; b < 4; ++b) word |= drawn_four_bits(v[b][i], inverse, quad & 1u ? u[4 + b] : u[b]) << (4 * b);
+            word = byte == 255u ? 0u : word;
+        } else {
+            const float four[8] = {v[0][i], v[1][i], v[2][i], v[3][i], 0, 0, 0, 0};
+            word = nearest_four_bits(four, byte);
+        }
+        *(u16 *)(turned + (8 * piece + i) * kRow + wave * 16u + 2u * quad) = (u16)word;
+    }
+    __syncthreads();
+    if (t.sums && wave == 0 && c0 + lane < g.cols && first < g.rows) {
+        float sum = sums[0][lane];
+        for (u32 w = 1; w < kTurnWaves; ++w) sum += sums[w][lane];
+        t.sums[(u64)blockIdx.y * g.cols + c0 + lane] = sum;
+    }
+    const u32 col = threadIdx.x >> 3, at = 16u * (threadIdx.x & 7u);
+    if (c0 + col >= g.cols) return;
+    unsigned char *q = g.to.q + (u64)(c0 + col) * g.to.ldq;
+    const u32 have = (g.fill + 1u) / 2u, from = first / 2u + at;
+#pragma unroll
+    for (u32 w = 0; w < 4; ++w)
+        if (from + 4 * w < have) write_bytes(q, from + 4 * w, *(const u32 *)(turned + col * kRow + at + 4 * w), have);
+}
+
+template <int kType>
+__global__ void __launch_bounds__(kTurnThreads) k_pack_columns(Turns both)
+{
+    const ToTurn &t = both.of[blockIdx.z];
+    if (blockIdx.x * kWave >= t.of.cols || blockIdx.y * kTurnRows >= t.of.fill) return;        // (the other matrix is larger)
+    if (both.drawn >> blockIdx.z & 1u) pack_columns<kType, true>(t);
+    else pack_columns<kType, false>(t);
+}
+
+// The sums of the groups of rows together, in binary64.
+__global__ void __launch_bounds__(256) k_sum_groups(const float *part, u32 groups, u32 cols, float *out)
+{
+    constexpr u32 kWaves = 4;
+    __shared__ double sums[kWaves][kWave];
+    const u32 lane = lane_id(), wave = threadIdx.x / kWave, c = blockIdx.x * kWave + lane;
+    double sum = 0;
+#pragma unroll 8
+    for (u32 s = wave; s < groups; s += kWaves) sum += (double)part[(u64)s * cols + min(c, cols - 1u)];
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave || c >= cols) return;
+#pragma unroll
+    for (u32 w = 1; w < kWaves; ++w) sum += sums[w][lane];
+    out[c] = (float)sum;
+}
+
+// Back to numbers: eight of them a thread.
+struct ToUnpack {
+    const unsigned char *q, *scale;
+    u64 ldq, lds;
+    u32 rows, cols;
+    void *out;
+    int type;
+    u64 ldo;
+};
+
+__device__ __forceinline__ float four_bit_value(u32 n)
+{
+    // the exponent's and the mantissa's bits in binary32's place, its exponent moved up by 126: 1/2 is a subnormal there too
+    return __uint_as_float((n & 7u) << 22 | (n & 8u) << 28) * 8.50705917302346158658e37f;      // 2^126
+}
+
+__global__ void __launch_bounds__(256) k_unpack(ToUnpack g)
+{
+    const u32 each = (g.cols + 7u) / 8u;
+    const u64 all = (u64)g.rows * each;
+    for (u64 at = (u64)blockIdx.x * 256 + threadIdx.x; at < all; at += (u64)gridDim.x * 256) {
+        const u32 row = (u32)(at / each), c = (u32)(at - (u64)row * each) * 8u, have = g.cols - c;
+        const unsigned char *q = g.q + row * g.ldq + c / 2u;
+        u32 word = 0;
+        if (have >= 7u) __builtin_memcpy(&word, q, 4);
+        else
+            for (u32 i = 0; 2 * i < have; ++i) word |= (u32)q[i] << (8 * i);
+        const u32 byte = g.scale[c / kBlock * g.lds + row];
+        const float scale = byte == 255u ? __uint_as_float(0x7FC00000u) : scale_value(byte);
+        f32x4 v[2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = four_bit_value(word >> (4 * i)) * scale;
+        write_eight(g.out, row * g.ldo + c, g.type, v[0], v[1], have);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The product.
+// ---------------------------------------------------------------------------
+struct Product4 {
+    const unsigned char *a, *b, *a_scale, *b_scale;
+    u64 lda, ldb, lda_scale, ldb_scale;
+    u32 m, n, k;                // k: numbers
+    const float *bias;
+    void *out;
+    u64 ldo;
+    int type;
+};
+
+__device__ __forceinline__ f32x4 multiply_four(const i32x4 &a, const i32x4 &b, const f32x4 &sum, u32 a_scale, u32 b_scale)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    const i32x8 wide_a{a[0], a[1], a[2], a[3], 0, 0, 0, 0}, wide_b{b[0], b[1], b[2], b[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide_a, wide_b, sum, 4, 4, 0, (int)a_scale, 0, (int)b_scale);
+#else
+    return sum;
+#endif
+}
+
+// A wavefront has 16 x 16 results and reads both operands as the instruction takes them.
+__global__ void __launch_bounds__(256) k_product4(Product4 g)
+{
+    const u32 lane = lane_id(), wave = threadIdx.x / kWave, rows = (g.m + 15u) / 16u, cols = (g.n + 15u) / 16u;
+    for (u64 tile = (u64)blockIdx.x * 4u + wave; tile < (u64)rows * cols; tile += (u64)gridDim.x * 4u) {
+    const u32 i0 = (u32)(tile / cols) * 16u, j0 = (u32)(tile % cols) * 16u, part = lane >> 4;
+    const u32 i = min(i0 + (lane & 15u), g.m - 1u), j = min(j0 + (lane & 15u), g.n - 1u);
+    const u32 bytes = (g.k + 1u) / 2u, blocks = (g.k + kBlock - 1) / kBlock, steps = (blocks + kStepBlocks - 1) / kStepBlocks;
+    f32x4 sum{0, 0, 0, 0};
+    for (u32 s = 0; s < steps; ++s) {
+        const u32 block = kStepBlocks * s + part, at = block * (kBlock / 2);
+        const i32x4 a = cut_piece(load_piece(g.a + i * g.lda, at, bytes), at, bytes);
+        const i32x4 b = cut_piece(load_piece(g.b + j * g.ldb, at, bytes), at, bytes);
+        u32 sa = 0, sb = 0;
+        if (block < blocks) {
+            sa = g.a_scale[block * g.lda_scale + i];
+            sb = g.b_scale[block * g.ldb_scale + j];
+        }
+        sum = multiply_four(b, a, sum, sb, sa);
+    }
+    // lane l: row i0 + l % 16, columns j0 + 4 (l / 16) .. + 3
+    const u32 col = j0 + 4u * part;
+    if (i0 + (lane & 15u) >= g.m || col >= g.n) continue;
+    if (g.bias) {
+#pragma unroll
+        for (u32 c = 0; c < 4; ++c) sum[c] += g.bias[min(col + c, g.n - 1u)];
+    }
+    write_four(g.out, i * g.ldo + col, g.type, sum, g.n - col);
+    }
+}
+
+__global__ void __launch_bounds__(256) k_zero4(float *p, u32 rows, u32 cols, u64 ld)
+{
+    for (u64 at = (u64)blockIdx.x * 256 + threadIdx.x; at < (u64)rows * cols; at += (u64)gridDim.x * 256)
+        p[at / cols * ld + at % cols] = 0.0f;
+}
+
+}  // namespace rtopk
+
+using namespace rtopk;
+
+namespace {
+
+// Offsets inside a tile of 256 rows fit 32 bits.
+constexpr u64 kMostSize = 1u << 22;
+
+bool size_ok(u64 v) { return v >= 1 && v <= kMostSize; }
+int launched() { return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_EHIP; }
+bool workspace_ok(const void *p, u64 bytes, u64 need) { return need == 0 || (p && ((uintptr_t)p & 255u) == 0 && bytes >= need); }
+u64 bytes_of(u64 k) { return (k + 1) / 2; }
+u64 blocks_of(u64 k) { return (k + kBlock - 1) / kBlock; }
+// a quantised operand [rows][k]: the distances of its rows and of its scales' blocks
+bool packed_ok(u64 rows, u64 k, u64 ldq, u64 lds) { return ldq >= bytes_of(k) && ldq <= kMostSize && lds >= rows && lds <= kMostSize; }
+
+template <int kType>
+int pack_rows(const ToPack &g, bool drawn, hipStream_t stream)
+{
+    const dim3 grid((g.rows + kTileRows - 1) / kTileRows, (g.fill + kTileColumns - 1) / kTileColumns);
+    if (drawn) k_pack_rows<kType, true><<<grid, kPackThreads, 0, stream>>>(g);
+    else k_pack_rows<kType, false><<<grid, kPackThreads, 0, stream>>>(g);
+    return launched();
+}
+int pack_rows(const ToPack &g, int type, bool drawn, hipStream_t stream)
+{
+    return type == RTOPK_F32 ? pack_rows<RTOPK_F32>(g, drawn, stream)
+           : type == RTOPK_BF16 ? pack_rows<RTOPK_BF16>(g, drawn, stream) : pack_rows<RTOPK_F16>(g, drawn, stream);
+}
+
+u32 turn_groups(u32 rows) { return (rows + kTurnRows - 1) / kTurnRows; }
+
+int pack_columns(const Turns &t, u32 count, int type, hipStream_t stream)
+{
+    dim3 grid(1, 1, count);
+    for (u32 i = 0; i < count; ++i) {
+        grid.x = std::max(grid.x, (t.of[i].of.cols + kWave - 1) / kWave);
+        grid.y = std::max(grid.y, turn_groups(t.of[i].of.fill));
+    }
+    if (type == RTOPK_F32) k_pack_columns<RTOPK_F32><<<grid, kTurnThreads, 0, stream>>>(t);
+    else if (type == RTOPK_BF16) k_pack_columns<RTOPK_BF16><<<grid, kTurnThreads, 0, stream>>>(t);
+    else k_pack_columns<RTOPK_F16><<<grid, kTurnThreads, 0, stream>>>(t);
+    return launched();
+}
+
+int run_product4(const Product4 &g, hipStream_t stream)
+{
+    const u64 tiles = (u64)((g.m + 15u) / 16u) * ((g.n + 15u) / 16u);
+    k_product4<<<(unsigned)std::min<u64>((tiles + 3) / 4, 1u << 20), 256, 0, stream>>>(g);
+    return launched();
+}
+
+// rows of quantised numbers in a workspace: whole slices of the contraction, zeros behind the row's end
+u64 filled(u32 k) { return align_up(k, 2 * kSlice); }
+u64 scale_ld(u32 rows) { return align_up(rows, 16); }
+
+struct Operand {
+    unsigned char *q, *scale;
+    u64 ldq, lds;
+};
+Operand take_operand(Cut &cut, u32 rows, u32 k)
+{
+    Operand o;
+    o.ldq = filled(k) / 2;
+    o.lds = scale_ld(rows);
+    o.q = cut.take<unsigned char>(rows * o.ldq);
+    o.scale = cut.take<unsigned char>(filled(k) / kBlock * o.lds);
+    return o;
+}
+ToPack to_pack(const void *x, u64 ldx, u32 rows, u32 cols, u32 fill, const Operand &o, const Drawing &drawing)
+{
+    return ToPack{x, ldx, rows, cols, fill, Packed{o.q, o.scale, o.ldq, o.lds}, drawing};
+}
+
+u64 cut_linear(void *base, u32 m, u32 k, u32 n, Operand &x)
+{
+    Cut cut{(unsigned char *)base};
+    x = take_operand(cut, m, k);
+    return cut.at;
+}
+
+struct BackwardParts {
+    Operand dy, dy_turned, x_turned;
+    float *sums;
+};
+u64 cut_backward(void *base, u32 m, u32 k, u32 n, BackwardParts &p)
+{
+    Cut cut{(unsigned char *)base};
+    p.dy = take_operand(cut, m, n);
+    p.dy_turned = take_operand(cut, n, m);
+    p.x_turned = take_operand(cut, k, m);
+    p.sums = cut.take<float>(4ull * turn_groups(m) * n);
+    return cut.at;
+}
+
+}  // namespace
+
+extern "C" int rtopk_quantize_mx4(const void *x, int type, uint64_t rows, uint64_t cols, uint64_t ldx, int along, int rounding,
+                                  uint64_t seed, uint64_t step, const uint64_t *step_device, uint8_t *q, uint64_t ldq, uint8_t *scale,
+                                  uint64_t lds, void *stream_v)
+{
+    if (!type_ok(type) || rows > kMostSize || !size_ok(cols) || ldx < cols || ldx > kMostSize) return RTOPK_EINVAL;
+    if ((along != RTOPK_ROWS && along != RTOPK_COLUMNS) || (rounding != RTOPK_NEAREST && rounding != RTOPK_DRAWN)) return RTOPK_EINVAL;
+    if (along == RTOPK_ROWS ? !packed_ok(rows, cols, ldq, lds) : !packed_ok(cols, rows, ldq, lds)) return RTOPK_EINVAL;
+    if (rows == 0) return RTOPK_OK;
+    if (!x || !q || !scale) return RTOPK_EINVAL;
+    hipStream_t stream = (hipStream_t)stream_v;
+    const bool drawn = rounding == RTOPK_DRAWN;
+    const ToPack g{x, ldx, (u32)rows, (u32)cols, (u32)(along == RTOPK_ROWS ? cols : rows), Packed{q, scale, ldq, lds},
+                   Drawing{seed, step, drawn ? step_device : nullptr}};
+    if (along == RTOPK_ROWS) return pack_rows(g, type, drawn, stream);
+    return pack_columns(Turns{{ToTurn{g, nullptr}, {}}, drawn ? 1u : 0u}, 1, type, stream);
+}
+
+extern "C" int rtopk_dequantize_mx4(const uint8_t *q, uint64_t rows, uint64_t cols, uint64_t ldq, const uint8_t *scale, uint64_t lds,
+                                    void *out, int type, uint64_t ldo, void *stream_v)
+{
+    if (!type_ok(type) || rows > kMostSize || cols > kMostSize || !packed_ok(rows, cols, ldq, lds) || ldo < cols || ldo > kMostSize)
+        return RTOPK_EINVAL;
+    if (rows == 0 || cols == 0) return RTOPK_OK;
+    if (!q || !scale || !out) return RTOPK_EINVAL;
+    const ToUnpack g{q, scale, ldq, lds, (u32)rows, (u32)cols, out, type, ldo};
+    const u64 all = rows * ((cols + 7) / 8);
+    k_unpack<<<(unsigned)std::min<u64>((all + 255) / 256, 32 * kUnits), 256, 0, (hipStream_t)stream_v>>>(g);
+    return launched();
+}
+
+extern "C" int rtopk_matmul_mx4_workspace_bytes(uint64_t m, uint64_t n, uint64_t k, uint64_t *bytes)
+{
+    if (!bytes || m > kMostSize || n > kMostSize || k > kMostSize) return RTOPK_EINVAL;
+    *bytes = 0;
+    return RTOPK_OK;
+}
+
+extern "C" int rtopk_matmul_mx4(const uint8_t *a, const uint8_t *a_scale, const uint8_t *b, const uint8_t *b_scale, const float *bias,
+                                uint64_t m, uint64_t n, uint64_t k, uint64_t lda, uint64_t lda_scale, uint64_t ldb, uint64_t ldb_scale,
+                                void *out, int out_type, uint64_t ldo, void *workspace, uint64_t workspace_bytes, void *stream_v)
+{
+    uint64_t need = 0;
+    if (!type_ok(out_type) || rtopk_matmul_mx4_workspace_bytes(m, n, k, &need) != RTOPK_OK) return RTOPK_EINVAL;
+    if (!packed_ok(m, k, lda, lda_scale) || !packed_ok(n, k, ldb, ldb_scale) || ldo < n) return RTOPK_EINVAL;
+    if (m == 0 || n == 0) return RTOPK_OK;
+    if (((!a || !b || !a_scale || !b_scale) && k) || !out) return RTOPK_EINVAL;
+    if (!workspace_ok(workspace, workspace_bytes, need)) return RTOPK_EWORKSPACE;
+    return run_product4(Product4{a, b, a_scale, b_scale, lda, ldb, lda_scale, ldb_scale, (u32)m, (u32)n, (u32)k, bias, out, ldo, out_type},
+                        (hipStream_t)stream_v);
+}
+
+extern "C" int rtopk_linear_mx4_workspace_bytes(uint64_t m, uint64_t k, uint64_t n, uint64_t *bytes)
+{
+    if (!bytes || m > kMostSize || !size_ok(k) || !size_ok(n)) return RTOPK_EINVAL;
+    Operand x;
+    *bytes = m ? cut_linear(nullptr, (u32)m, (u32)k, (u32)n, x) : 0;
+    return RTOPK_OK;
+}
+
+extern "C" int rtopk_linear_mx4(const void *x, int type, uint64_t m, uint64_t k, uint64_t ldx, const uint8_t *w, const uint8_t *w_scale,
+                                uint64_t n, uint64_t ldw, uint64_t ldw_scale, const float *bias, void *out, int out_type, uint64_t ldo,
+                                void *workspace, uint64_t workspace_bytes, void *stream_v)
+{
+    uint64_t need = 0;
+    if (!type_ok(type) || !type_ok(out_type) || rtopk_linear_mx4_workspace_bytes(m, k, n, &need) != RTOPK_OK) return RTOPK_EINVAL;
+    if (ldx < k || ldx > kMostSize || !packed_ok(n, k, ldw, ldw_scale) || ldo < n) return RTOPK_EINVAL;
+    if (m == 0) return RTOPK_OK;
+    if (!x || !w || !w_scale || !out) return RTOPK_EINVAL;
+    if (!workspace_ok(workspace, workspace_bytes, need)) return RTOPK_EWORKSPACE;
+    hipStream_t stream = (hipStream_t)stream_v;
+    Operand q;
+    cut_linear(workspace, (u32)m, (u32)k, (u32)n, q);
+    if (const int rc = pack_rows(to_pack(x, ldx, (u32)m, (u32)k, (u32)filled((u32)k), q, Drawing{}), type, false, stream)) return rc;
+    return run_product4(Product4{q.q, w, q.scale, w_scale, q.ldq, ldw, q.lds, ldw_scale, (u32)m, (u32)n, (u32)k, bias, out, ldo, out_type}, stream);
+}
+
+extern "C" int rtopk_linear_mx4_backward_workspace_bytes(uint64_t m, uint64_t k, uint64_t n, uint64_t *bytes)
+{
+    if (!bytes || m > kMostSize || !size_ok(k) || !size_ok(n)) return RTOPK_EINVAL;
+    BackwardParts p;
+    *bytes = m ? cut_backward(nullptr, (u32)m, (u32)k, (u32)n, p) : 0;
+    return RTOPK_OK;
+}
+
+extern "C" int rtopk_linear_mx4_backward(const void *dy, const void *x, int type, uint64_t m, uint64_t k, uint64_t n, uint64_t lddy,
+                                         uint64_t ldx, const uint8_t *w_turned, const uint8_t *w_turned_scale, uint64_t ldw,
+                                         uint64_t ldw_scale, int rounding, uint64_t seed, uint64_t step, const uint64_t *step_device,
+                                         void *dx, uint64_t lddx, float *dw, uint64_t lddw, float *db, void *workspace,
+                                         uint64_t workspace_bytes, void *stream_v)
+{
+    uint64_t need = 0;
+    if (!type_ok(type) || rtopk_linear_mx4_backward_workspace_bytes(m, k, n, &need) != RTOPK_OK) return RTOPK_EINVAL;
+    if ((rounding != RTOPK_NEAREST && rounding != RTOPK_DRAWN) || lddy < n || lddy > kMostSize) return RTOPK_EINVAL;
+    if (dx && (!packed_ok(k, n, ldw, ldw_scale) || lddx < k)) return RTOPK_EINVAL;
+    if (dw && (ldx < k || ldx > kMostSize || lddw < k)) return RTOPK_EINVAL;
+    if ((!dx && !dw) || (db && !dw)) return RTOPK_EINVAL;
+    if (m && (!dy || (dx && (!w_turned || !w_turned_scale)) || (dw && !x))) return RTOPK_EINVAL;
+    if (!workspace_ok(workspace, workspace_bytes, need)) return RTOPK_EWORKSPACE;
+    hipStream_t stream = (hipStream_t)stream_v;
+    if (m == 0) {
+        if (!dw) return RTOPK_OK;
+        k_zero4<<<kUnits, 256, 0, stream>>>(dw, (u32)n, (u32)k, lddw);
+        if (db) k_zero4<<<1, 256, 0, stream>>>(db, 1, (u32)n, n);
+        return launched();
+    }
+    BackwardParts p;
+    cut_backward(workspace, (u32)m, (u32)k, (u32)n, p);
+    const bool drawn = rounding == RTOPK_DRAWN;
+    const Drawing drawing{seed, step, drawn ? step_device : nullptr};
+    if (dx) {
+        if (const int rc = pack_rows(to_pack(dy, lddy, (u32)m, (u32)n, (u32)filled((u32)n), p.dy, drawing), type, drawn, stream)) return rc;
+        if (const int rc = run_product4(Product4{p.dy.q, w_turned, p.dy.scale, w_turned_scale, p.dy.ldq, ldw, p.dy.lds, ldw_scale, (u32)m,
+                                                 (u32)k, (u32)n, nullptr, dx, lddx, type},
+                                        stream))
+            return rc;
+    }
+    if (!dw) return RTOPK_OK;
+    const u32 fill = (u32)filled((u32)m);
+    const Turns t{{ToTurn{to_pack(dy, lddy, (u32)m, (u32)n, fill, p.dy_turned, drawing), db ? p.sums : nullptr},
+                   ToTurn{to_pack(x, ldx, (u32)m, (u32)k, fill, p.x_turned, Drawing{}), nullptr}},
+                  drawn ? 1u : 0u};
+    if (const int rc = pack_columns(t, 2, type, stream)) return rc;
+    if (db) {
+        k_sum_groups<<<(unsigned)((n + kWave - 1) / kWave), 256, 0, stream>>>(p.sums, turn_groups((u32)m), (u32)n, db);
+        if (const int rc = launched()) return rc;
+    }
+    return run_product4(Product4{p.dy_turned.q, p.x_turned.q, p.dy_turned.scale, p.x_turned.scale, p.dy_turned.ldq, p.x_turned.ldq,
+                                 p.dy_turned.lds, p.x_turned.lds, (u32)n, (u32)k, (u32)m, nullptr, dw, lddw, RTOPK_F32},
+                        stream);
+}

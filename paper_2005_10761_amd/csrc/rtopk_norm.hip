@@ -1,0 +1,415 @@
+// Layer norm, forward and backward, over the rows of a matrix.
+//
+//   forward    mean = sum x / c, rstd = (sum (x - mean)^2 / c + eps)^-1/2,
+//              y = (x - mean) rstd gamma + beta
+//   backward   h = (x - mean) rstd, g = dy gamma:
+//              dx = rstd (g - mean(g) - h mean(g h)) (+ add)
+//              dgamma = sum over rows of dy h, dbeta = sum over rows of dy
+//
+// Everything between the loads and the stores is binary32 or more. The sums over rows are taken run by run, and the runs
+// in order: no atomics, the same bits every time. What bounds all of it is memory: x, dy, add once, dx once.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "../../include/rtopk.h"
+#include "rtopk_matrix.h"
+
+namespace rtopk {
+
+struct Norm {
+    const void *x;
+    u64 ldx;
+    u32 rows, cols;
+    const float *gamma, *beta;      // or null: 1 and 0
+    float eps;
+    void *out;
+    int out_type;
+    u64 ldo;
+    float *mean, *rstd;             // or null
+};
+
+constexpr int kNormThreads = 256;
+
+// Eight numbers of a vector of binary32 that may be missing.
+__device__ __forceinline__ void eight_or(float (&v)[8], const float *p, u32 c, u32 cols, float otherwise)
+{
+    if (p) {
+        Eight<0> e;
+        e.load((const unsigned char *)p, c, cols);
+        e.numbers(v, (const unsigned char *)p, c, cols);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = otherwise;
+    }
+}
+
+// The sum of one number of each lane of the kWavesPerRow wavefronts that share a row; `part` has a place for each wavefront.
+template <int kWavesPerRow, class T>
+__device__ __forceinline__ T sum_of_row(T v, T *part)
+{
+    T sum;
+    if constexpr (sizeof(T) == 4) {
+        sum = wave_sum_f32(v);
+    } else {
+        sum = v;
+#pragma unroll
+        for (int o = kWave / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+    }
+    if constexpr (kWavesPerRow > 1) {
+        const u32 wave = threadIdx.x / kWave, first = wave / kWavesPerRow * kWavesPerRow;
+        if (lane_id() == 0) part[wave] = sum;
+        __syncthreads();
+        sum = 0;
+#pragma unroll
+        for (u32 w = 0; w < kWavesPerRow; ++w) sum += part[first + w];
+    }
+    return sum;
+}
+
+// kWavesPerRow wavefronts hold a row in registers, kPieces pieces of eight numbers a lane; kPieces = 0: the row is longer
+// and read three times (the second and third time from the caches), with sums in binary64.
+template <int kType, int kWavesPerRow, int kPieces>
+__global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNormThreads) k_norm(Norm g)
+{
+    constexpr u32 kWaves = kWavesPerRow > 4 ? kWavesPerRow : 4, kRows = kWaves / kWavesPerRow, kStep = 8u * kWave * kWavesPerRow;
+    typedef typename std::conditional<kPieces == 0, double, float>::type Sum;
+    __shared__ Sum part[2][kWaves];
+    const u32 lane = lane_id(), wave = threadIdx.x / kWave;
+    const u64 r = ((u64)blockIdx.y * gridDim.x + blockIdx.x) * kRows + wave / kWavesPerRow;
+    const bool there = r < g.rows;
+    const unsigned char *row = (const unsigned char *)g.x + (there ? r : 0u) * g.ldx * Eight<kType>::kSize;
+    const u32 c0 = (wave % kWavesPerRow * kWave + lane) * 8u;
+    constexpr int kHeld = kPieces ? kPieces : 1;
+    Eight<kType> held[kHeld];
+    float x[kHeld][8];
+    Sum sum = 0, squares = 0;
+    if constexpr (kPieces > 0) {
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) held[p].load(row, c0 + p * kStep, g.cols);
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+            held[p].numbers(x[p], row, c0 + p * kStep, g.cols);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += x[p][i];
+        }
+    } else {
+        for (u32 c = c0; c < g.cols; c += kStep) {
+            held[0].load(row, c, g.cols);
+            held[0].numbers(x[0], row, c, g.cols);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += (Sum)x[0][i];
+        }
+    }
+    const float mean = (float)(sum_of_row<kWavesPerRow>(sum, part[0]) / (Sum)g.cols);
+    auto add_squares = [&](const float (&v)[8], u32 c) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float d = c + i < g.cols ? v[i] - mean : 0.0f;
+            squares += (Sum)d * (Sum)d;
+        }
+    };
+    if constexpr (kPieces > 0) {
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) add_squares(x[p], c0 + p * kStep);
+    } else {
+        for (u32 c = c0; c < g.cols; c += kStep) {
+            held[0].load(row, c, g.cols);
+            held[0].numbers(x[0], row, c, g.cols);
+            add_squares(x[0], c);
+        }
+    }
+    const float rstd = 1.0f / sqrtf((float)(sum_of_row<kWavesPerRow>(squares, part[1]) / (Sum)g.cols) + g.eps);
+    if (!there) return;
+    if (c0 == 0) {
+        if (g.mean) g.mean[r] = mean;
+        if (g.rstd) g.rstd[r] = rstd;
+    }
+    auto write = [&](const float (&v)[8], u32 c) {
+        if (c >= g.cols) return;
+        float gamma[8], beta[8];
+        eight_or(gamma, g.gamma, c, g.cols, 1.0f);
+        eight_or(beta, g.beta, c, g.cols, 0.0f);
+        f32x4 y[2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i >> 2][i & 3] = fmaf((v[i] - mean) * rstd, gamma[i], beta[i]);
+        write_eight(g.out, r * g.ldo + c, g.out_type, y[0], y[1], g.cols - c);
+    };
+    if constexpr (kPieces > 0) {
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) write(x[p], c0 + p * kStep);
+    } else {
+        for (u32 c = c0; c < g.cols; c += kStep) {
+            held[0].load(row, c, g.cols);
+            held[0].numbers(x[0], row, c, g.cols);
+            write(x[0], c);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Backward.
+// ---------------------------------------------------------------------------
+struct NormBack {
+    const void *dy, *x, *add;       // add: of x's type, or null
+    u64 lddy, ldx, ldadd;
+    u32 rows, cols;
+    const float *mean, *rstd, *gamma;
+    void *dx;                       // of x's type, or null
+    u64 lddx;
+    u32 runs, run;                  // the sums over rows: runs of so many rows
+    float *dgamma, *dbeta;          // or null
+    float *part;                    // [2][runs][cols]
+};
+
+// A row by one workgroup: its two means, then dx; dy and x are read twice, the second time from the caches.
+template <int kType, int kDyType>
+__global__ void __launch_bounds__(1024) k_norm_back_row(NormBack g)
+{
+    constexpr int kWaves = 16;
+    __shared__ double part[2][kWaves];
+    const u64 r = (u64)blockIdx.y * gridDim.x + blockIdx.x;
+    if (r >= g.rows) return;
+    const unsigned char *x_row = (const unsigned char *)g.x + r * g.ldx * Eight<kType>::kSize;
+    const unsigned char *dy_row = (const unsigned char *)g.dy + r * g.lddy * Eight<kDyType>::kSize;
+    const unsigned char *add_row = g.add ? (const unsigned char *)g.add + r * g.ldadd * Eight<kType>::kSize : nullptr;
+    const float mean = g.mean[r], rstd = g.rstd[r];
+    float h[8], d[8], gamma[8];
+    auto read = [&](u32 c) {
+        Eight<kType> ex;
+        Eight<kDyType> ey;
+        ex.load(x_row, c, g.cols);
+        ey.load(dy_row, c, g.cols);
+        eight_or(gamma, g.gamma, c, g.cols, 1.0f);
+        ex.numbers(h, x_row, c, g.cols);
+        ey.numbers(d, dy_row, c, g.cols);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            h[i] = (h[i] - mean) * rstd;
+            d[i] = c + i < g.cols ? d[i] * gamma[i] : 0.0f;
+        }
+    };
+    double sum = 0, inner = 0;
+    for (u32 c = threadIdx.x * 8u; c < g.cols; c += 8u * kWaves * kWave) {
+        read(c);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            sum += (double)d[i];
+            inner += c + i < g.cols ? (double)d[i] * (double)h[i] : 0.0;
+        }
+    }
+    const float m0 = (float)(sum_of_row<kWaves>(sum, part[0]) / g.cols), m1 = (float)(sum_of_row<kWaves>(inner, part[1]) / g.cols);
+    for (u32 c = threadIdx.x * 8u; c < g.cols; c += 8u * kWaves * kWave) {
+        read(c);
+        float more[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (add_row) {
+            Eight<kType> ea;
+            ea.load(add_row, c, g.cols);
+            ea.numbers(more, add_row, c, g.cols);
+        }
+        f32x4 v[2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = fmaf(rstd, fmaf(-h[i], m1, d[i] - m0), more[i]);
+        write_eight(g.dx, r * g.lddx + c, kType, v[0], v[1], g.cols - c);
+    }
+}
+
+// The sums of a run of rows, 512 columns a workgroup: a wavefront takes every fourth row.
+constexpr u32 kSumColumns = 8 * kWave;
+
+template <int kType, int kDyType>
+__global__ void __launch_bounds__(kNormThreads) k_norm_back_columns(NormBack g)
+{
+    constexpr u32 kWaves = kNormThreads / kWave, kAtOnce = 4;
+    __shared__ float part[2][kWaves - 1][kSumColumns];
+    const u32 lane = lane_id(), wave = threadIdx.x / kWave, c = blockIdx.x * kSumColumns + lane * 8u;
+    const u32 r0 = blockIdx.y * g.run, r1 = min(r0 + g.run, g.rows);
+    float dgamma[8] = {0, 0, 0, 0, 0, 0, 0, 0}, dbeta[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (u32 r = r0 + wave; r < r1; r += kAtOnce * kWaves) {
+        Eight<kType> ex[kAtOnce];
+        Eight<kDyType> ey[kAtOnce];
+        float mean[kAtOnce], rstd[kAtOnce];
+#pragma unroll
+        for (u32 q = 0; q < kAtOnce; ++q) {
+            const u64 row = min(r + q * kWaves, r1 - 1u);
+            ex[q].load((const unsigned char *)g.x + row * g.ldx * Eight<kType>::kSize, c, g.cols);
+            ey[q].load((const unsigned char *)g.dy + row * g.lddy * Eight<kDyType>::kSize, c, g.cols);
+            mean[q] = g.mean[row];
+            rstd[q] = g.rstd[row];
+        }
+#pragma unroll
+        for (u32 q = 0; q < kAtOnce; ++q) {
+            if (r + q * kWaves >= r1) break;
+            const u64 row = r + q * kWaves;
+            float x[8], d[8];
+            ex[q].numbers(x, (const unsigned char *)g.x + row * g.ldx * Eight<kType>::kSize, c, g.cols);
+            ey[q].numbers(d, (const unsigned char *)g.dy + row * g.lddy * Eight<kDyType>::kSize, c, g.cols);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                dgamma[i] = fmaf(d[i], (x[i] - mean[q]) * rstd[q], dgamma[i]);
+                dbeta[i] += d[i];
+            }
+        }
+    }
+    if (wave) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            part[0][wave - 1][i * kWave + lane] = dgamma[i];
+            part[1][wave - 1][i * kWave + lane] = dbeta[i];
+        }
+    }
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+        for (u32 w = 0; w < kWaves - 1; ++w) {
+            dgamma[i] += part[0][w][i * kWave + lane];
+            dbeta[i] += part[1][w][i * kWave + lane];
+        }
+        if (c + i < g.cols) {
+            g.part[(u64)blockIdx.y * g.cols + c + i] = dgamma[i];
+            g.part[((u64)g.runs + blockIdx.y) * g.cols + c + i] = dbeta[i];
+        }
+    }
+}
+
+// The runs together, in binary64; blockIdx.y: dgamma, dbeta.
+__global__ void __launch_bounds__(kNormThreads) k_norm_back_join(NormBack g)
+{
+    constexpr u32 kWaves = kNormThreads / kWave;
+    __shared__ double part[kWaves][kWave];
+    const u32 lane = lane_id(), wave = threadIdx.x / kWave, c = blockIdx.x * kWave + lane;
+    float *out = blockIdx.y ? g.dbeta : g.dgamma;
+    if (!out) return;
+    const float *from = g.part + (u64)blockIdx.y * g.runs * g.cols + min(c, g.cols - 1u);
+    double sum = 0;
+#pragma unroll 8
+    for (u32 s = wave; s < g.runs; s += kWaves) sum += (double)from[(u64)s * g.cols];
+    part[wave][lane] = sum;
+    __syncthreads();
+    if (wave || c >= g.cols) return;
+#pragma unroll
+    for (u32 w = 1; w < kWaves; ++w) sum += part[w][lane];
+    out[c] = (float)sum;
+}
+
+__global__ void __launch_bounds__(256) k_norm_zero(float *p, u32 count)
+{
+    for (u64 at = (u64)blockIdx.x * 256 + threadIdx.x; at < count; at += (u64)gridDim.x * 256) p[at] = 0.0f;
+}
+
+}  // namespace rtopk
+
+using namespace rtopk;
+
+namespace {
+
+constexpr u64 kMostSize = 1u << 22;
+
+bool size_ok(u64 v) { return v >= 1 && v <= kMostSize; }
+int launched() { return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_EHIP; }
+
+// (a launch has less than 2^32 threads along x)
+dim3 row_grid(u32 blocks) { return dim3(std::min(blocks, 1u << 20), (blocks + (1u << 20) - 1) >> 20); }
+
+template <int kType>
+int launch_norm(const Norm &g, hipStream_t stream)
+{
+    const u32 rows = g.rows, cols = g.cols;
+    if (cols <= 512 && rows >= 4 * kUnits) k_norm<kType, 1, 1><<<row_grid((rows + 3) / 4), kNormThreads, 0, stream>>>(g);
+    else if (cols <= 1024 && rows >= 4 * kUnits) k_norm<kType, 1, 2><<<row_grid((rows + 3) / 4), kNormThreads, 0, stream>>>(g);
+    else if (cols <= 2048) k_norm<kType, 4, 1><<<row_grid(rows), kNormThreads, 0, stream>>>(g);
+    else if (cols <= 4096) k_norm<kType, 4, 2><<<row_grid(rows), kNormThreads, 0, stream>>>(g);
+    else if (cols <= 8192) k_norm<kType, 4, 4><<<row_grid(rows), kNormThreads, 0, stream>>>(g);
+    else if (cols <= 16384) k_norm<kType, 16, 2><<<row_grid(rows), 16 * kWave, 0, stream>>>(g);
+    else k_norm<kType, 16, 0><<<row_grid(rows), 16 * kWave, 0, stream>>>(g);
+    return launched();
+}
+
+constexpr u32 kMostRuns = 128;
+
+// two workgroups a compute unit, 16 rows at least
+u32 run_rows(u32 rows, u32 cols)
+{
+    const u32 groups = (cols + kSumColumns - 1) / kSumColumns, runs = std::min(kMostRuns, (2 * kUnits + groups - 1) / groups);
+    return std::max((rows + runs - 1) / runs, 16u);
+}
+
+template <int kType, int kDyType>
+int launch_back(const NormBack &g, hipStream_t stream)
+{
+    if (g.dgamma || g.dbeta) {
+        k_norm_back_columns<kType, kDyType><<<dim3((g.cols + kSumColumns - 1) / kSumColumns, g.runs), kNormThreads, 0, stream>>>(g);
+        if (const int rc = launched()) return rc;
+        k_norm_back_join<<<dim3((g.cols + kWave - 1) / kWave, 2), kNormThreads, 0, stream>>>(g);
+        if (const int rc = launched()) return rc;
+    }
+    if (g.dx) k_norm_back_row<kType, kDyType><<<row_grid(g.rows), 1024, 0, stream>>>(g);     // (last: dx may be x or dy)
+    return launched();
+}
+
+template <int kType>
+int launch_back(const NormBack &g, int dy_type, hipStream_t stream)
+{
+    return dy_type == RTOPK_F32 ? launch_back<kType, RTOPK_F32>(g, stream)
+           : dy_type == RTOPK_BF16 ? launch_back<kType, RTOPK_BF16>(g, stream) : launch_back<kType, RTOPK_F16>(g, stream);
+}
+
+}  // namespace
+
+extern "C" int rtopk_layer_norm(const void *x, int type, uint64_t rows, uint64_t cols, uint64_t ldx, const float *gamma,
+                                const float *beta, float eps, void *out, int out_type, uint64_t ldo, float *mean, float *rstd,
+                                void *stream_v)
+{
+    if (!type_ok(type) || !type_ok(out_type) || rows > kMostSize || !size_ok(cols)) return RTOPK_EINVAL;
+    if (ldx < cols || ldx > kMostSize || ldo < cols || ldo > kMostSize || !(eps >= 0.0f) || std::isinf(eps)) return RTOPK_EINVAL;
+    if (rows == 0) return RTOPK_OK;
+    if (!x || !out || (x == out && (ldx != ldo || (type == RTOPK_F32) != (out_type == RTOPK_F32)))) return RTOPK_EINVAL;
+    const Norm g{x, ldx, (u32)rows, (u32)cols, gamma, beta, eps, out, out_type, ldo, mean, rstd};
+    hipStream_t stream = (hipStream_t)stream_v;
+    return type == RTOPK_F32 ? launch_norm<RTOPK_F32>(g, stream)
+           : type == RTOPK_BF16 ? launch_norm<RTOPK_BF16>(g, stream) : launch_norm<RTOPK_F16>(g, stream);
+}
+
+extern "C" int rtopk_layer_norm_backward_workspace_bytes(uint64_t rows, uint64_t cols, uint64_t *bytes)
+{
+    if (!bytes || rows > kMostSize || !size_ok(cols)) return RTOPK_EINVAL;
+    const u32 run = run_rows((u32)rows, (u32)cols);
+    *bytes = rows ? align_up(8ull * ((rows + run - 1) / run) * cols, 256) : 0;
+    return RTOPK_OK;
+}
+
+extern "C" int rtopk_layer_norm_backward(const void *dy, int dy_type, const void *x, int type, uint64_t rows, uint64_t cols,
+                                         uint64_t lddy, uint64_t ldx, const float *mean, const float *rstd, const float *gamma,
+                                         const void *add, uint64_t ldadd, void *dx, uint64_t lddx, float *dgamma, float *dbeta,
+                                         void *workspace, uint64_t workspace_bytes, void *stream_v)
+{
+    uint64_t need = 0;
+    if (!type_ok(type) || !type_ok(dy_type) || rtopk_layer_norm_backward_workspace_bytes(rows, cols, &need) != RTOPK_OK) return RTOPK_EINVAL;
+    if (lddy < cols || lddy > kMostSize || ldx < cols || ldx > kMostSize) return RTOPK_EINVAL;
+    if ((!dx && !dgamma && !dbeta) || (add && !dx) || (dx && (lddx < cols || lddx > kMostSize))) return RTOPK_EINVAL;
+    if (add && (ldadd < cols || ldadd > kMostSize)) return RTOPK_EINVAL;
+    if (rows && (!dy || !x || !mean || !rstd)) return RTOPK_EINVAL;
+    // dx may be dy, x or add itself, element for element
+    if (dx && rows && ((dx == dy && (lddx != lddy || (type == RTOPK_F32) != (dy_type == RTOPK_F32))) || (dx == x && lddx != ldx) ||
+                       (dx == add && lddx != ldadd)))
+        return RTOPK_EINVAL;
+    const bool sums = dgamma || dbeta;
+    if (sums && need && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need)) return RTOPK_EWORKSPACE;
+    hipStream_t stream = (hipStream_t)stream_v;
+    if (rows == 0) {
+        for (float *p : {dgamma, dbeta}) {
+            if (!p) continue;
+            k_norm_zero<<<(unsigned)((cols + 255) / 256), 256, 0, stream>>>(p, (u32)cols);
+            if (const int rc = launched()) return rc;
+        }
+        return RTOPK_OK;
+    }
+    const u32 run = run_rows((u32)rows, (u32)cols);
+    const NormBack g{dy, x, add, lddy, ldx, ldadd, (u32)rows, (u32)cols, mean, rstd, gamma, dx, lddx, (u32)((rows + run - 1) / run), run,
+                     dgamma, dbeta, (float *)workspace};
+    return type == RTOPK_F32 ? launch_back<RTOPK_F32>(g, dy_type, stream)
+           : type == RTOPK_BF16 ? launch_back<RTOPK_BF16>(g, dy_type, stream) : launch_back<RTOPK_F16>(g, dy_type, stream);
+}
