@@ -21,9 +21,6 @@
 namespace rtopk {
 
 constexpr u32 kBlock = 32;                  // numbers that share a scale
-constexpr u32 kStepBlocks = 4;              // blocks of one matrix instruction
-
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 // ---------------------------------------------------------------------------
 // Quantisation.
@@ -309,46 +306,81 @@ struct Product4 {
     void *out;
     u64 ldo;
     int type;
+    u32 slices_each, splits;    // the contraction in runs of so many slices
+    float *part;                // [splits][m][n rounded up to 4], splits > 1 only
 };
 
-__device__ __forceinline__ f32x4 multiply_four(const i32x4 &a, const i32x4 &b, const f32x4 &sum, u32 a_scale, u32 b_scale)
+// The biases of neighbouring columns, zeros where there are none.
+__device__ __forceinline__ f32x4 four_biases(const Product4 &g, u32 col)
 {
-#if defined(__HIP_DEVICE_COMPILE__)
-    const i32x8 wide_a{a[0], a[1], a[2], a[3], 0, 0, 0, 0}, wide_b{b[0], b[1], b[2], b[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide_a, wide_b, sum, 4, 4, 0, (int)a_scale, 0, (int)b_scale);
-#else
-    return sum;
-#endif
-}
-
-// A wavefront has 16 x 16 results and reads both operands as the instruction takes them.
-__global__ void __launch_bounds__(256) k_product4(Product4 g)
-{
-    const u32 lane = lane_id(), wave = threadIdx.x / kWave, rows = (g.m + 15u) / 16u, cols = (g.n + 15u) / 16u;
-    for (u64 tile = (u64)blockIdx.x * 4u + wave; tile < (u64)rows * cols; tile += (u64)gridDim.x * 4u) {
-    const u32 i0 = (u32)(tile / cols) * 16u, j0 = (u32)(tile % cols) * 16u, part = lane >> 4;
-    const u32 i = min(i0 + (lane & 15u), g.m - 1u), j = min(j0 + (lane & 15u), g.n - 1u);
-    const u32 bytes = (g.k + 1u) / 2u, blocks = (g.k + kBlock - 1) / kBlock, steps = (blocks + kStepBlocks - 1) / kStepBlocks;
-    f32x4 sum{0, 0, 0, 0};
-    for (u32 s = 0; s < steps; ++s) {
-        const u32 block = kStepBlocks * s + part, at = block * (kBlock / 2);
-        const i32x4 a = cut_piece(load_piece(g.a + i * g.lda, at, bytes), at, bytes);
-        const i32x4 b = cut_piece(load_piece(g.b + j * g.ldb, at, bytes), at, bytes);
-        u32 sa = 0, sb = 0;
-        if (block < blocks) {
-            sa = g.a_scale[block * g.lda_scale + i];
-            sb = g.b_scale[block * g.ldb_scale + j];
-        }
-        sum = multiply_four(b, a, sum, sb, sa);
-    }
-    // lane l: row i0 + l % 16, columns j0 + 4 (l / 16) .. + 3
-    const u32 col = j0 + 4u * part;
-    if (i0 + (lane & 15u) >= g.m || col >= g.n) continue;
+    f32x4 v{0, 0, 0, 0};
     if (g.bias) {
 #pragma unroll
-        for (u32 c = 0; c < 4; ++c) sum[c] += g.bias[min(col + c, g.n - 1u)];
+        for (u32 c = 0; c < 4; ++c) v[c] = g.bias[min(col + c, g.n - 1u)];
     }
-    write_four(g.out, i * g.ldo + col, g.type, sum, g.n - col);
+    return v;
+}
+
+// A tile, or a run of its contraction; the bias is added to the sums in registers, and the result written once.
+template <class T, bool kWhole>
+__global__ void __launch_bounds__(T::kThreads) k_product4(Product4 g)
+{
+    __shared__ __align__(16) unsigned char lds[T::kLds];
+    const u32 rows = (g.m + T::kRowsM - 1) / T::kRowsM, cols = (g.n + T::kRowsN - 1) / T::kRowsN;
+    const u32 place = xcd_place(blockIdx.x, gridDim.x), split = place / (rows * cols);
+    u32 ti, tj;
+    tile_at(place - split * rows * cols, rows, cols, ti, tj);
+    const u32 i0 = ti * T::kRowsM, j0 = tj * T::kRowsN, bytes = (g.k + 1u) / 2u;
+    const TileRows a{g.a + i0 * g.lda, g.m - i0, (u32)g.lda, bytes, g.a_scale + i0, (u32)g.lda_scale};
+    const TileRows b{g.b + j0 * g.ldb, g.n - j0, (u32)g.ldb, bytes, g.b_scale + j0, (u32)g.ldb_scale};
+    const u32 slices = (bytes + kSlice - 1) / kSlice, from = split * g.slices_each;
+    T t;
+    t.clear();
+    t.template multiply<kWhole>(a, b, from, min(from + g.slices_each, slices), lds);
+    const u64 ld = align_up(g.n, 4);
+    float *part = g.part + (u64)split * g.m * ld;
+    // a lane's columns: 4 x size neighbours for each group of fragments
+#pragma unroll
+    for (int group = 0; group < T::GroupsN::kCount; ++group) {
+        const int first = T::GroupsN::start(group), size = T::GroupsN::size(first);
+        const u32 col = j0 + T::col0() + 16u * first + 4u * size * (lane_id() >> 4);
+        f32x4 bias[4];          // `size` of them
+#pragma unroll
+        for (int w = 0; w < size; ++w) bias[w] = g.splits == 1 ? four_biases(g, col + 4 * w) : f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < T::kFragsM; ++i) {
+            const u32 row = i0 + T::row_at(i);
+            f32x4 v[4];
+#pragma unroll
+            for (int e = 0; e < 4 * size; ++e) v[e / 4][e % 4] = t.sum[i][first + e % size][e / size] + bias[e / 4][e % 4];
+            if (row >= g.m) continue;
+#pragma unroll
+            for (int w = 0; w < size; w += 2) {
+                const u32 c = col + 4u * w;
+                if (c >= g.n) continue;
+                if (g.splits > 1) {
+                    *(f32x4 *)(part + row * ld + c) = v[w];
+                    if (w + 1 < size && c + 4u < g.n) *(f32x4 *)(part + row * ld + c + 4) = v[w + 1 < size ? w + 1 : w];
+                } else if (w + 1 < size) {
+                    write_eight(g.out, row * g.ldo + c, g.type, v[w], v[w + 1 < size ? w + 1 : w], g.n - c);
+                } else {
+                    write_four(g.out, row * g.ldo + c, g.type, v[w], g.n - c);
+                }
+            }
+        }
+    }
+}
+
+// The sums of the runs together, in order, and the bias.
+__global__ void __launch_bounds__(256) k_product4_join(Product4 g)
+{
+    const u32 fours = (g.n + 3) / 4;
+    const u64 all = (u64)g.m * fours, ld = 4ull * fours;
+    for (u64 at = (u64)blockIdx.x * 256 + threadIdx.x; at < all; at += (u64)gridDim.x * 256) {
+        const u32 row = (u32)(at / fours), col = (u32)(at - (u64)row * fours) * 4u;
+        f32x4 sum = four_biases(g, col);
+        for (u32 s = 0; s < g.splits; ++s) sum += *(const f32x4 *)(g.part + ((u64)s * g.m + row) * ld + col);
+        write_four(g.out, row * g.ldo + col, g.type, sum, g.n - col);
     }
 }
 
@@ -404,11 +436,67 @@ int pack_columns(const Turns &t, u32 count, int type, hipStream_t stream)
     return launched();
 }
 
-int run_product4(const Product4 &g, hipStream_t stream)
+// Tiles have 512 threads, and a launch less than 2^32.
+constexpr u64 kMostTiles = 1u << 23;
+
+struct Plan {
+    u32 edge, tiles, slices_each, splits;
+    u64 part_bytes;
+};
+
+// The tile and the number of runs of the contraction that cost least; a slice's 128 bytes of a row cost what 128 bytes of 8-bit
+// integers do. Runs cost a launch, and four bytes of every sum written and read.
+Plan plan_product(u32 m, u32 n, u32 k, bool on_lines)
 {
-    const u64 tiles = (u64)((g.m + 15u) / 16u) * ((g.n + 15u) / 16u);
-    k_product4<<<(unsigned)std::min<u64>((tiles + 3) / 4, 1u << 20), 256, 0, stream>>>(g);
-    return launched();
+    Plan best{};
+    double least = 0.0;
+    const u32 slices = ((k + 1) / 2 + kSlice - 1) / kSlice;
+    for (const u32 edge : {64u, 128u, 192u, 256u}) {
+        const u64 tiles = (u64)((m + edge - 1) / edge) * ((n + edge - 1) / edge);
+        for (u32 splits = 1; splits <= std::max(1u, std::min(16u, slices / 4)); ++splits) {
+            const u32 each = std::max(1u, (slices + splits - 1) / splits);
+            if (splits > 1 && (slices + each - 1) / each != splits) continue;
+            if (tiles * splits >= kMostTiles && edge < 256) continue;
+            double cost = tiles_cost(kCostBytes, edge, tiles * splits, each * (on_lines ? 1.0 : 1.3));
+            if (splits > 1) cost += 3.0 + (double)m * n * splits * 8.0 / 6e6;
+            if (best.edge && cost >= least) continue;
+            least = cost;
+            best = Plan{edge, (u32)tiles, each, std::max(1u, (slices + each - 1) / each), 0};
+        }
+    }
+    best.part_bytes = best.splits > 1 ? align_up((u64)best.splits * m * align_up(n, 4) * 4, 256) : 0;
+    return best;
+}
+// what a product of these sizes may need for the runs' sums, however its rows lie
+u64 part_bytes(u32 m, u32 n, u32 k) { return std::max(plan_product(m, n, k, false).part_bytes, plan_product(m, n, k, true).part_bytes); }
+
+template <int kEdge, int kStages>
+void launch_product4(const Product4 &g, const Plan &p, bool whole, hipStream_t stream)
+{
+    typedef Tile<kFours, kEdge, kEdge, 2, 4, kStages, true, kByScale> T;
+    if (whole) k_product4<T, true><<<p.tiles * p.splits, T::kThreads, 0, stream>>>(g);
+    else k_product4<T, false><<<p.tiles * p.splits, T::kThreads, 0, stream>>>(g);
+}
+
+int run_product4(Product4 g, void *part, hipStream_t stream)
+{
+    const Plan p = plan_product(g.m, g.n, g.k, ((g.lda | g.ldb) & 127u) == 0);
+    g.slices_each = p.slices_each;
+    g.splits = p.splits;
+    g.part = (float *)part;
+    const bool whole = (((uintptr_t)g.a | (uintptr_t)g.b | g.lda | g.ldb) & 15u) == 0 &&
+                       (((uintptr_t)g.a_scale | (uintptr_t)g.b_scale | g.lda_scale | g.ldb_scale) & 3u) == 0;
+    if (p.edge == 256) launch_product4<256, 2>(g, p, whole, stream);
+    else if (p.edge == 192) launch_product4<192, 2>(g, p, whole, stream);
+    else if (p.edge == 128) launch_product4<128, 2>(g, p, whole, stream);
+    else launch_product4<64, 3>(g, p, whole, stream);
+    if (const int rc = launched()) return rc;
+    if (p.splits > 1) {
+        const u64 blocks = ((u64)g.m * ((g.n + 3) / 4) + 255) / 256;
+        k_product4_join<<<(unsigned)std::min<u64>(blocks, 16 * kUnits), 256, 0, stream>>>(g);
+        return launched();
+    }
+    return RTOPK_OK;
 }
 
 // rows of quantised numbers in a workspace: whole slices of the contraction, zeros behind the row's end
@@ -433,16 +521,22 @@ ToPack to_pack(const void *x, u64 ldx, u32 rows, u32 cols, u32 fill, const Opera
     return ToPack{x, ldx, rows, cols, fill, Packed{o.q, o.scale, o.ldq, o.lds}, drawing};
 }
 
-u64 cut_linear(void *base, u32 m, u32 k, u32 n, Operand &x)
+struct LinearParts {
+    Operand x;
+    void *part;
+};
+u64 cut_linear(void *base, u32 m, u32 k, u32 n, LinearParts &p)
 {
     Cut cut{(unsigned char *)base};
-    x = take_operand(cut, m, k);
+    p.x = take_operand(cut, m, k);
+    p.part = cut.take<void>(part_bytes(m, n, k));
     return cut.at;
 }
 
 struct BackwardParts {
     Operand dy, dy_turned, x_turned;
     float *sums;
+    void *part;
 };
 u64 cut_backward(void *base, u32 m, u32 k, u32 n, BackwardParts &p)
 {
@@ -451,6 +545,7 @@ u64 cut_backward(void *base, u32 m, u32 k, u32 n, BackwardParts &p)
     p.dy_turned = take_operand(cut, n, m);
     p.x_turned = take_operand(cut, k, m);
     p.sums = cut.take<float>(4ull * turn_groups(m) * n);
+    p.part = cut.take<void>(std::max(part_bytes(m, k, n), part_bytes(n, k, m)));
     return cut.at;
 }
 
@@ -489,7 +584,7 @@ extern "C" int rtopk_dequantize_mx4(const uint8_t *q, uint64_t rows, uint64_t co
 extern "C" int rtopk_matmul_mx4_workspace_bytes(uint64_t m, uint64_t n, uint64_t k, uint64_t *bytes)
 {
     if (!bytes || m > kMostSize || n > kMostSize || k > kMostSize) return RTOPK_EINVAL;
-    *bytes = 0;
+    *bytes = m && n ? part_bytes((u32)m, (u32)n, (u32)k) : 0;
     return RTOPK_OK;
 }
 
@@ -503,15 +598,16 @@ extern "C" int rtopk_matmul_mx4(const uint8_t *a, const uint8_t *a_scale, const 
     if (m == 0 || n == 0) return RTOPK_OK;
     if (((!a || !b || !a_scale || !b_scale) && k) || !out) return RTOPK_EINVAL;
     if (!workspace_ok(workspace, workspace_bytes, need)) return RTOPK_EWORKSPACE;
-    return run_product4(Product4{a, b, a_scale, b_scale, lda, ldb, lda_scale, ldb_scale, (u32)m, (u32)n, (u32)k, bias, out, ldo, out_type},
-                        (hipStream_t)stream_v);
+    return run_product4(Product4{a, b, a_scale, b_scale, lda, ldb, lda_scale, ldb_scale, (u32)m, (u32)n, (u32)k, bias, out, ldo, out_type,
+                                 0, 0, nullptr},
+                        workspace, (hipStream_t)stream_v);
 }
 
 extern "C" int rtopk_linear_mx4_workspace_bytes(uint64_t m, uint64_t k, uint64_t n, uint64_t *bytes)
 {
     if (!bytes || m > kMostSize || !size_ok(k) || !size_ok(n)) return RTOPK_EINVAL;
-    Operand x;
-    *bytes = m ? cut_linear(nullptr, (u32)m, (u32)k, (u32)n, x) : 0;
+    LinearParts p;
+    *bytes = m ? cut_linear(nullptr, (u32)m, (u32)k, (u32)n, p) : 0;
     return RTOPK_OK;
 }
 
@@ -526,10 +622,12 @@ extern "C" int rtopk_linear_mx4(const void *x, int type, uint64_t m, uint64_t k,
     if (!x || !w || !w_scale || !out) return RTOPK_EINVAL;
     if (!workspace_ok(workspace, workspace_bytes, need)) return RTOPK_EWORKSPACE;
     hipStream_t stream = (hipStream_t)stream_v;
-    Operand q;
-    cut_linear(workspace, (u32)m, (u32)k, (u32)n, q);
-    if (const int rc = pack_rows(to_pack(x, ldx, (u32)m, (u32)k, (u32)filled((u32)k), q, Drawing{}), type, false, stream)) return rc;
-    return run_product4(Product4{q.q, w, q.scale, w_scale, q.ldq, ldw, q.lds, ldw_scale, (u32)m, (u32)n, (u32)k, bias, out, ldo, out_type}, stream);
+    LinearParts p;
+    cut_linear(workspace, (u32)m, (u32)k, (u32)n, p);
+    if (const int rc = pack_rows(to_pack(x, ldx, (u32)m, (u32)k, (u32)filled((u32)k), p.x, Drawing{}), type, false, stream)) return rc;
+    return run_product4(Product4{p.x.q, w, p.x.scale, w_scale, p.x.ldq, ldw, p.x.lds, ldw_scale, (u32)m, (u32)n, (u32)k, bias, out, ldo,
+                                 out_type, 0, 0, nullptr},
+                        p.part, stream);
 }
 
 extern "C" int rtopk_linear_mx4_backward_workspace_bytes(uint64_t m, uint64_t k, uint64_t n, uint64_t *bytes)
@@ -568,8 +666,8 @@ extern "C" int rtopk_linear_mx4_backward(const void *dy, const void *x, int type
     if (dx) {
         if (const int rc = pack_rows(to_pack(dy, lddy, (u32)m, (u32)n, (u32)filled((u32)n), p.dy, drawing), type, drawn, stream)) return rc;
         if (const int rc = run_product4(Product4{p.dy.q, w_turned, p.dy.scale, w_turned_scale, p.dy.ldq, ldw, p.dy.lds, ldw_scale, (u32)m,
-                                                 (u32)k, (u32)n, nullptr, dx, lddx, type},
-                                        stream))
+                                                 (u32)k, (u32)n, nullptr, dx, lddx, type, 0, 0, nullptr},
+                                        p.part, stream))
             return rc;
     }
     if (!dw) return RTOPK_OK;
@@ -583,6 +681,7 @@ extern "C" int rtopk_linear_mx4_backward(const void *dy, const void *x, int type
         if (const int rc = launched()) return rc;
     }
     return run_product4(Product4{p.dy_turned.q, p.x_turned.q, p.dy_turned.scale, p.x_turned.scale, p.dy_turned.ldq, p.x_turned.ldq,
-                                 p.dy_turned.lds, p.x_turned.lds, (u32)n, (u32)k, (u32)m, nullptr, dw, lddw, RTOPK_F32},
-                        stream);
+                                 p.dy_turned.lds, p.x_turned.lds, (u32)n, (u32)k, (u32)m, nullptr, dw, lddw, RTOPK_F32, 0, 0,
+                                 nullptr},
+                        p.part, stream);
 }
