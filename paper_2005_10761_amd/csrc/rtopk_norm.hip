@@ -163,7 +163,137 @@ struct NormBack {
     float *part;                    // [2][runs][cols]
 };
 
-// A row by one workgroup: its two means, then dx; dy and x are read twice, the second time from the caches.
+// Rows by workgroups that keep going: kWavesPerRow wavefronts hold a row in registers, kPieces pieces of eight numbers a
+// lane, the next row's x and dy on their way while this one's means are taken and its dx is written; a lane's share of
+// dgamma and dbeta stays in registers over all of its rows (kSums). One read of everything, one write.
+template <int kType, int kDyType, int kWavesPerRow, int kPieces, bool kSums>
+__global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNormThreads) k_norm_back(NormBack g)
+{
+    constexpr u32 kWaves = kWavesPerRow > 4 ? kWavesPerRow : 4, kRows = kWaves / kWavesPerRow, kStep = 8u * kWave * kWavesPerRow;
+    __shared__ float means[2][2][kWaves];
+    const u32 lane = lane_id(), wave = threadIdx.x / kWave, c0 = (wave % kWavesPerRow * kWave + lane) * 8u;
+    const u32 step = gridDim.x * kRows;
+    const float per_row = 1.0f / (float)g.cols;
+    float gamma[kPieces][8], dgamma[kPieces][8], dbeta[kPieces][8];
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+        eight_or(gamma[p], g.gamma, c0 + p * kStep, g.cols, 1.0f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dgamma[p][i] = dbeta[p][i] = 0.0f;
+    }
+    Eight<kType> next_x[kPieces];
+    Eight<kDyType> next_dy[kPieces];
+    float next_mean, next_rstd;
+    auto fetch = [&](u32 r) {
+        const u64 row = min(r, g.rows - 1u);
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+            next_x[p].load((const unsigned char *)g.x + row * g.ldx * Eight<kType>::kSize, c0 + p * kStep, g.cols);
+            next_dy[p].load((const unsigned char *)g.dy + row * g.lddy * Eight<kDyType>::kSize, c0 + p * kStep, g.cols);
+        }
+        next_mean = g.mean[row];
+        next_rstd = g.rstd[row];
+    };
+    u32 r = blockIdx.x * kRows + wave / kWavesPerRow, turn = 0;
+    fetch(r);
+    for (; r < g.rows; r += step, turn ^= 1u) {
+        const unsigned char *x_row = (const unsigned char *)g.x + r * g.ldx * Eight<kType>::kSize;
+        const unsigned char *dy_row = (const unsigned char *)g.dy + r * g.lddy * Eight<kDyType>::kSize;
+        const unsigned char *add_row = (const unsigned char *)g.add + r * g.ldadd * Eight<kType>::kSize;
+        const float mean = next_mean, rstd = next_rstd;
+        Eight<kType> held_add[kPieces];
+        float h[kPieces][8], d[kPieces][8], sum = 0, inner = 0;
+        if (g.add) {
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) held_add[p].load(add_row, c0 + p * kStep, g.cols);
+        }
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+            const u32 c = c0 + p * kStep;
+            next_x[p].numbers(h[p], x_row, c, g.cols);
+            next_dy[p].numbers(d[p], dy_row, c, g.cols);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                h[p][i] = c + i < g.cols ? (h[p][i] - mean) * rstd : 0.0f;      // (d is zero there)
+                if (kSums) {
+                    dgamma[p][i] = fmaf(d[p][i], h[p][i], dgamma[p][i]);
+                    dbeta[p][i] += d[p][i];
+                }
+                d[p][i] *= gamma[p][i];
+                sum += d[p][i];
+                inner = fmaf(d[p][i], h[p][i], inner);
+            }
+        }
+        if (r + step < g.rows) fetch(r + step);
+        sum = wave_sum_f32(sum);
+        inner = wave_sum_f32(inner);
+        if constexpr (kWavesPerRow > 1) {
+            // (two places in turn: a wavefront that is a row ahead has passed this row's barrier)
+            if (lane == 0) {
+                means[turn][0][wave] = sum;
+                means[turn][1][wave] = inner;
+            }
+            lds_barrier();
+            sum = inner = 0;
+#pragma unroll
+            for (u32 w = 0; w < kWavesPerRow; ++w) {
+                sum += means[turn][0][w];
+                inner += means[turn][1][w];
+            }
+        }
+        const float m0 = sum * per_row, m1 = inner * per_row;
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+            const u32 c = c0 + p * kStep;
+            if (c >= g.cols) continue;
+            float more[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (g.add) held_add[p].numbers(more, add_row, c, g.cols);
+            f32x4 v[2];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = fmaf(rstd, fmaf(-h[p][i], m1, d[p][i] - m0), more[i]);
+            write_eight(g.dx, r * g.lddx + c, kType, v[0], v[1], g.cols - c);
+        }
+    }
+    if constexpr (kSums) {
+        float *out = g.part + (u64)blockIdx.x * g.cols;
+        const u64 beta = (u64)g.runs * g.cols;
+        if constexpr (kRows > 1) {
+            // the rows' wavefronts together
+            __shared__ float joined[2][kRows - 1][kPieces * 8 * kWave];
+            if (wave) {
+#pragma unroll
+                for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        joined[0][wave - 1][(8 * p + i) * kWave + lane] = dgamma[p][i];
+                        joined[1][wave - 1][(8 * p + i) * kWave + lane] = dbeta[p][i];
+                    }
+            }
+            __syncthreads();
+            if (wave) return;
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (u32 w = 0; w < kRows - 1; ++w) {
+                        dgamma[p][i] += joined[0][w][(8 * p + i) * kWave + lane];
+                        dbeta[p][i] += joined[1][w][(8 * p + i) * kWave + lane];
+                    }
+        }
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+            const u32 c = c0 + p * kStep;
+            if (c >= g.cols) continue;
+            write_eight(out, c, RTOPK_F32, f32x4{dgamma[p][0], dgamma[p][1], dgamma[p][2], dgamma[p][3]},
+                        f32x4{dgamma[p][4], dgamma[p][5], dgamma[p][6], dgamma[p][7]}, g.cols - c);
+            write_eight(out + beta, c, RTOPK_F32, f32x4{dbeta[p][0], dbeta[p][1], dbeta[p][2], dbeta[p][3]},
+                        f32x4{dbeta[p][4], dbeta[p][5], dbeta[p][6], dbeta[p][7]}, g.cols - c);
+        }
+    }
+}
+
+// A longer row by one workgroup: its two means, then dx; dy and x are read twice, the second time from the caches.
 template <int kType, int kDyType>
 __global__ void __launch_bounds__(1024) k_norm_back_row(NormBack g)
 {
@@ -328,23 +458,55 @@ int launch_norm(const Norm &g, hipStream_t stream)
     return launched();
 }
 
-constexpr u32 kMostRuns = 128;
+// Rows that registers hold: workgroups that keep going, two a compute unit (one of sixteen wavefronts).
+constexpr u32 kHeldColumns = 16384;
+u32 rows_at_once(u32 cols) { return cols <= 1024 ? 4 : 1; }
+u32 held_groups(u32 rows, u32 cols) { return std::min((rows + rows_at_once(cols) - 1) / rows_at_once(cols), (cols <= 8192 ? 2 : 1) * kUnits); }
 
-// two workgroups a compute unit, 16 rows at least
+// Sums alone, or of longer rows: runs of rows, two workgroups a compute unit, 16 rows at least.
+constexpr u32 kMostRuns = 128;
 u32 run_rows(u32 rows, u32 cols)
 {
     const u32 groups = (cols + kSumColumns - 1) / kSumColumns, runs = std::min(kMostRuns, (2 * kUnits + groups - 1) / groups);
     return std::max((rows + runs - 1) / runs, 16u);
 }
+u32 run_count(u32 rows, u32 cols) { return (rows + run_rows(rows, cols) - 1) / run_rows(rows, cols); }
+
+template <int kType, int kDyType, bool kSums>
+int launch_held(const NormBack &g, hipStream_t stream)
+{
+    const u32 cols = g.cols, grid = held_groups(g.rows, g.cols);
+    if (cols <= 512) k_norm_back<kType, kDyType, 1, 1, kSums><<<grid, kNormThreads, 0, stream>>>(g);
+    else if (cols <= 1024) k_norm_back<kType, kDyType, 1, 2, kSums><<<grid, kNormThreads, 0, stream>>>(g);
+    else if (cols <= 2048) k_norm_back<kType, kDyType, 4, 1, kSums><<<grid, kNormThreads, 0, stream>>>(g);
+    else if (cols <= 4096) k_norm_back<kType, kDyType, 4, 2, kSums><<<grid, kNormThreads, 0, stream>>>(g);
+    else if (cols <= 8192) k_norm_back<kType, kDyType, 8, 2, kSums><<<grid, 8 * kWave, 0, stream>>>(g);
+    else k_norm_back<kType, kDyType, 16, 2, kSums><<<grid, 16 * kWave, 0, stream>>>(g);
+    return launched();
+}
+
+int join_sums(const NormBack &g, hipStream_t stream)
+{
+    k_norm_back_join<<<dim3((g.cols + kWave - 1) / kWave, 2), kNormThreads, 0, stream>>>(g);
+    return launched();
+}
 
 template <int kType, int kDyType>
-int launch_back(const NormBack &g, hipStream_t stream)
+int launch_back(NormBack g, hipStream_t stream)
 {
-    if (g.dgamma || g.dbeta) {
+    const bool sums = g.dgamma || g.dbeta;
+    if (g.dx && g.cols <= kHeldColumns) {
+        g.runs = held_groups(g.rows, g.cols);
+        if (!sums) return launch_held<kType, kDyType, false>(g, stream);
+        if (const int rc = launch_held<kType, kDyType, true>(g, stream)) return rc;
+        return join_sums(g, stream);
+    }
+    if (sums) {
+        g.run = run_rows(g.rows, g.cols);
+        g.runs = run_count(g.rows, g.cols);
         k_norm_back_columns<kType, kDyType><<<dim3((g.cols + kSumColumns - 1) / kSumColumns, g.runs), kNormThreads, 0, stream>>>(g);
         if (const int rc = launched()) return rc;
-        k_norm_back_join<<<dim3((g.cols + kWave - 1) / kWave, 2), kNormThreads, 0, stream>>>(g);
-        if (const int rc = launched()) return rc;
+        if (const int rc = join_sums(g, stream)) return rc;
     }
     if (g.dx) k_norm_back_row<kType, kDyType><<<row_grid(g.rows), 1024, 0, stream>>>(g);     // (last: dx may be x or dy)
     return launched();
@@ -376,8 +538,11 @@ extern "C" int rtopk_layer_norm(const void *x, int type, uint64_t rows, uint64_t
 extern "C" int rtopk_layer_norm_backward_workspace_bytes(uint64_t rows, uint64_t cols, uint64_t *bytes)
 {
     if (!bytes || rows > kMostSize || !size_ok(cols)) return RTOPK_EINVAL;
-    const u32 run = run_rows((u32)rows, (u32)cols);
-    *bytes = rows ? align_up(8ull * ((rows + run - 1) / run) * cols, 256) : 0;
+    *bytes = 0;
+    if (rows) {
+        const u32 runs = run_count((u32)rows, (u32)cols), held = cols <= kHeldColumns ? held_groups((u32)rows, (u32)cols) : 0;
+        *bytes = align_up(8ull * std::max(runs, held) * cols, 256);
+    }
     return RTOPK_OK;
 }
 
@@ -407,8 +572,7 @@ extern "C" int rtopk_layer_norm_backward(const void *dy, int dy_type, const void
         }
         return RTOPK_OK;
     }
-    const u32 run = run_rows((u32)rows, (u32)cols);
-    const NormBack g{dy, x, add, lddy, ldx, ldadd, (u32)rows, (u32)cols, mean, rstd, gamma, dx, lddx, (u32)((rows + run - 1) / run), run,
+    const NormBack g{dy, x, add, lddy, ldx, ldadd, (u32)rows, (u32)cols, mean, rstd, gamma, dx, lddx, 0, 0,
                      dgamma, dbeta, (float *)workspace};
     return type == RTOPK_F32 ? launch_back<RTOPK_F32>(g, dy_type, stream)
            : type == RTOPK_BF16 ? launch_back<RTOPK_BF16>(g, dy_type, stream) : launch_back<RTOPK_F16>(g, dy_type, stream);
