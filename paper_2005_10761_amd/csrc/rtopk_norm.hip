@@ -60,7 +60,7 @@ __device__ __forceinline__ T sum_of_row(T v, T *part)
     if constexpr (kWavesPerRow > 1) {
         const u32 wave = threadIdx.x / kWave, first = wave / kWavesPerRow * kWavesPerRow;
         if (lane_id() == 0) part[wave] = sum;
-        __syncthreads();
+        lds_barrier();
         sum = 0;
 #pragma unroll
         for (u32 w = 0; w < kWavesPerRow; ++w) sum += part[first + w];
@@ -68,84 +68,110 @@ __device__ __forceinline__ T sum_of_row(T v, T *part)
     return sum;
 }
 
-// kWavesPerRow wavefronts hold a row in registers, kPieces pieces of eight numbers a lane; kPieces = 0: the row is longer
-// and read three times (the second and third time from the caches), with sums in binary64.
+// Rows by workgroups that keep going: kWavesPerRow wavefronts hold a row in registers, kPieces pieces of eight numbers a
+// lane, and gamma and beta for all of their rows; the next row is on its way while this one's mean and variance are taken.
 template <int kType, int kWavesPerRow, int kPieces>
 __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNormThreads) k_norm(Norm g)
 {
     constexpr u32 kWaves = kWavesPerRow > 4 ? kWavesPerRow : 4, kRows = kWaves / kWavesPerRow, kStep = 8u * kWave * kWavesPerRow;
-    typedef typename std::conditional<kPieces == 0, double, float>::type Sum;
-    __shared__ Sum part[2][kWaves];
-    const u32 lane = lane_id(), wave = threadIdx.x / kWave;
-    const u64 r = ((u64)blockIdx.y * gridDim.x + blockIdx.x) * kRows + wave / kWavesPerRow;
-    const bool there = r < g.rows;
-    const unsigned char *row = (const unsigned char *)g.x + (there ? r : 0u) * g.ldx * Eight<kType>::kSize;
-    const u32 c0 = (wave % kWavesPerRow * kWave + lane) * 8u;
-    constexpr int kHeld = kPieces ? kPieces : 1;
-    Eight<kType> held[kHeld];
-    float x[kHeld][8];
-    Sum sum = 0, squares = 0;
-    if constexpr (kPieces > 0) {
+    __shared__ float part[4][kWaves];
+    const u32 lane = lane_id(), wave = threadIdx.x / kWave, c0 = (wave % kWavesPerRow * kWave + lane) * 8u, step = gridDim.x * kRows;
+    const float cols = (float)g.cols;
+    Eight<kType> next[kPieces];
+    auto fetch = [&](u32 r) {
+        const unsigned char *row = (const unsigned char *)g.x + min(r, g.rows - 1u) * g.ldx * Eight<kType>::kSize;
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) held[p].load(row, c0 + p * kStep, g.cols);
+        for (int p = 0; p < kPieces; ++p) next[p].load(row, c0 + p * kStep, g.cols);
+    };
+    u32 r = blockIdx.x * kRows + wave / kWavesPerRow, turn = 0;
+    fetch(r);
+    float gamma[kPieces][8], beta[kPieces][8];
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+        eight_or(gamma[p], g.gamma, c0 + p * kStep, g.cols, 1.0f);
+        eight_or(beta[p], g.beta, c0 + p * kStep, g.cols, 0.0f);
+    }
+    for (; r < g.rows; r += step, turn ^= 2u) {
+        const unsigned char *row = (const unsigned char *)g.x + r * g.ldx * Eight<kType>::kSize;
+        float x[kPieces][8], sum = 0, squares = 0;
 #pragma unroll
         for (int p = 0; p < kPieces; ++p) {
-            held[p].numbers(x[p], row, c0 + p * kStep, g.cols);
+            next[p].numbers(x[p], row, c0 + p * kStep, g.cols);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum += x[p][i];
         }
-    } else {
-        for (u32 c = c0; c < g.cols; c += kStep) {
-            held[0].load(row, c, g.cols);
-            held[0].numbers(x[0], row, c, g.cols);
+        if (r + step < g.rows) fetch(r + step);
+        const float mean = sum_of_row<kWavesPerRow>(sum, part[turn]) / cols;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum += (Sum)x[0][i];
+        for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[p][i] = c0 + p * kStep + i < g.cols ? x[p][i] - mean : 0.0f;
+                squares = fmaf(x[p][i], x[p][i], squares);
+            }
+        // (places in turn: a wavefront that is a row ahead has passed both of this row's barriers)
+        const float rstd = 1.0f / sqrtf(sum_of_row<kWavesPerRow>(squares, part[turn + 1]) / cols + g.eps);
+        if (c0 == 0) {
+            if (g.mean) g.mean[r] = mean;
+            if (g.rstd) g.rstd[r] = rstd;
+        }
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+            const u32 c = c0 + p * kStep;
+            if (c >= g.cols) continue;
+            f32x4 y[2];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i >> 2][i & 3] = fmaf(x[p][i] * rstd, gamma[p][i], beta[p][i]);
+            write_eight(g.out, r * g.ldo + c, g.out_type, y[0], y[1], g.cols - c);
         }
     }
-    const float mean = (float)(sum_of_row<kWavesPerRow>(sum, part[0]) / (Sum)g.cols);
-    auto add_squares = [&](const float (&v)[8], u32 c) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float d = c + i < g.cols ? v[i] - mean : 0.0f;
-            squares += (Sum)d * (Sum)d;
+}
+
+// A longer row by one workgroup: it is read three times (the second and third time from the caches), with sums in binary64.
+template <int kType>
+__global__ void __launch_bounds__(1024) k_norm_row(Norm g)
+{
+    constexpr int kWaves = 16;
+    __shared__ double part[2][kWaves];
+    const u64 r = (u64)blockIdx.y * gridDim.x + blockIdx.x;
+    if (r >= g.rows) return;
+    const unsigned char *row = (const unsigned char *)g.x + r * g.ldx * Eight<kType>::kSize;
+    auto each = [&](auto act) {
+        for (u32 c = threadIdx.x * 8u; c < g.cols; c += 8u * kWaves * kWave) {
+            Eight<kType> e;
+            float x[8];
+            e.load(row, c, g.cols);
+            e.numbers(x, row, c, g.cols);
+            act(x, c);
         }
     };
-    if constexpr (kPieces > 0) {
+    double sum = 0, squares = 0;
+    each([&](const float (&x)[8], u32) {
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) add_squares(x[p], c0 + p * kStep);
-    } else {
-        for (u32 c = c0; c < g.cols; c += kStep) {
-            held[0].load(row, c, g.cols);
-            held[0].numbers(x[0], row, c, g.cols);
-            add_squares(x[0], c);
+        for (int i = 0; i < 8; ++i) sum += (double)x[i];
+    });
+    const float mean = (float)(sum_of_row<kWaves>(sum, part[0]) / g.cols);
+    each([&](const float (&x)[8], u32 c) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const double d = c + i < g.cols ? x[i] - mean : 0.0f;
+            squares += d * d;
         }
-    }
-    const float rstd = 1.0f / sqrtf((float)(sum_of_row<kWavesPerRow>(squares, part[1]) / (Sum)g.cols) + g.eps);
-    if (!there) return;
-    if (c0 == 0) {
+    });
+    const float rstd = 1.0f / sqrtf((float)(sum_of_row<kWaves>(squares, part[1]) / g.cols) + g.eps);
+    if (threadIdx.x == 0) {
         if (g.mean) g.mean[r] = mean;
         if (g.rstd) g.rstd[r] = rstd;
     }
-    auto write = [&](const float (&v)[8], u32 c) {
-        if (c >= g.cols) return;
+    each([&](const float (&x)[8], u32 c) {
         float gamma[8], beta[8];
         eight_or(gamma, g.gamma, c, g.cols, 1.0f);
         eight_or(beta, g.beta, c, g.cols, 0.0f);
         f32x4 y[2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i >> 2][i & 3] = fmaf((v[i] - mean) * rstd, gamma[i], beta[i]);
+        for (int i = 0; i < 8; ++i) y[i >> 2][i & 3] = fmaf((x[i] - mean) * rstd, gamma[i], beta[i]);
         write_eight(g.out, r * g.ldo + c, g.out_type, y[0], y[1], g.cols - c);
-    };
-    if constexpr (kPieces > 0) {
-#pragma unroll
-        for (int p = 0; p < kPieces; ++p) write(x[p], c0 + p * kStep);
-    } else {
-        for (u32 c = c0; c < g.cols; c += kStep) {
-            held[0].load(row, c, g.cols);
-            held[0].numbers(x[0], row, c, g.cols);
-            write(x[0], c);
-        }
-    }
+    });
 }
 
 // ---------------------------------------------------------------------------
@@ -405,23 +431,28 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_back_columns(NormBack g)
     }
 }
 
-// The runs together, in binary64; blockIdx.y: dgamma, dbeta.
-__global__ void __launch_bounds__(kNormThreads) k_norm_back_join(NormBack g)
+// The runs together, in binary64, 16 columns a workgroup; blockIdx.y: dgamma, dbeta.
+constexpr u32 kJoinColumns = 16, kJoinThreads = 1024;
+
+__global__ void __launch_bounds__(kJoinThreads) k_norm_back_join(NormBack g)
 {
-    constexpr u32 kWaves = kNormThreads / kWave;
-    __shared__ double part[kWaves][kWave];
-    const u32 lane = lane_id(), wave = threadIdx.x / kWave, c = blockIdx.x * kWave + lane;
+    constexpr u32 kWaves = kJoinThreads / kWave, kAtOnce = kJoinThreads / kJoinColumns;
+    __shared__ double part[kWaves][kJoinColumns];
+    const u32 c = blockIdx.x * kJoinColumns + threadIdx.x % kJoinColumns;
     float *out = blockIdx.y ? g.dbeta : g.dgamma;
     if (!out) return;
     const float *from = g.part + (u64)blockIdx.y * g.runs * g.cols + min(c, g.cols - 1u);
     double sum = 0;
 #pragma unroll 8
-    for (u32 s = wave; s < g.runs; s += kWaves) sum += (double)from[(u64)s * g.cols];
-    part[wave][lane] = sum;
-    __syncthreads();
-    if (wave || c >= g.cols) return;
+    for (u32 s = threadIdx.x / kJoinColumns; s < g.runs; s += kAtOnce) sum += (double)from[(u64)s * g.cols];
 #pragma unroll
-    for (u32 w = 1; w < kWaves; ++w) sum += part[w][lane];
+    for (int o = kJoinColumns; o < kWave; o <<= 1) sum += __shfl_xor(sum, o, kWave);
+    if (lane_id() < kJoinColumns) part[threadIdx.x / kWave][lane_id()] = sum;
+    __syncthreads();
+    if (threadIdx.x >= kJoinColumns || c >= g.cols) return;
+    sum = 0;
+#pragma unroll
+    for (u32 w = 0; w < kWaves; ++w) sum += part[w][threadIdx.x];
     out[c] = (float)sum;
 }
 
@@ -444,24 +475,27 @@ int launched() { return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_EHIP;
 // (a launch has less than 2^32 threads along x)
 dim3 row_grid(u32 blocks) { return dim3(std::min(blocks, 1u << 20), (blocks + (1u << 20) - 1) >> 20); }
 
-template <int kType>
-int launch_norm(const Norm &g, hipStream_t stream)
-{
-    const u32 rows = g.rows, cols = g.cols;
-    if (cols <= 512 && rows >= 4 * kUnits) k_norm<kType, 1, 1><<<row_grid((rows + 3) / 4), kNormThreads, 0, stream>>>(g);
-    else if (cols <= 1024 && rows >= 4 * kUnits) k_norm<kType, 1, 2><<<row_grid((rows + 3) / 4), kNormThreads, 0, stream>>>(g);
-    else if (cols <= 2048) k_norm<kType, 4, 1><<<row_grid(rows), kNormThreads, 0, stream>>>(g);
-    else if (cols <= 4096) k_norm<kType, 4, 2><<<row_grid(rows), kNormThreads, 0, stream>>>(g);
-    else if (cols <= 8192) k_norm<kType, 4, 4><<<row_grid(rows), kNormThreads, 0, stream>>>(g);
-    else if (cols <= 16384) k_norm<kType, 16, 2><<<row_grid(rows), 16 * kWave, 0, stream>>>(g);
-    else k_norm<kType, 16, 0><<<row_grid(rows), 16 * kWave, 0, stream>>>(g);
-    return launched();
-}
-
 // Rows that registers hold: workgroups that keep going, two a compute unit (one of sixteen wavefronts).
 constexpr u32 kHeldColumns = 16384;
 u32 rows_at_once(u32 cols) { return cols <= 1024 ? 4 : 1; }
-u32 held_groups(u32 rows, u32 cols) { return std::min((rows + rows_at_once(cols) - 1) / rows_at_once(cols), (cols <= 8192 ? 2 : 1) * kUnits); }
+u32 held_groups(u32 rows, u32 cols, u32 each)
+{
+    return std::min((rows + rows_at_once(cols) - 1) / rows_at_once(cols), (cols <= 4096 ? each : cols <= 8192 ? (each + 1) / 2 : 1) * kUnits);
+}
+
+template <int kType>
+int launch_norm(const Norm &g, hipStream_t stream)
+{
+    const u32 cols = g.cols, grid = held_groups(g.rows, g.cols, 4);
+    if (cols <= 512) k_norm<kType, 1, 1><<<grid, kNormThreads, 0, stream>>>(g);
+    else if (cols <= 1024) k_norm<kType, 1, 2><<<grid, kNormThreads, 0, stream>>>(g);
+    else if (cols <= 2048) k_norm<kType, 4, 1><<<grid, kNormThreads, 0, stream>>>(g);
+    else if (cols <= 4096) k_norm<kType, 4, 2><<<grid, kNormThreads, 0, stream>>>(g);
+    else if (cols <= 8192) k_norm<kType, 8, 2><<<grid, 8 * kWave, 0, stream>>>(g);
+    else if (cols <= kHeldColumns) k_norm<kType, 16, 2><<<grid, 16 * kWave, 0, stream>>>(g);
+    else k_norm_row<kType><<<row_grid(g.rows), 1024, 0, stream>>>(g);
+    return launched();
+}
 
 // Sums alone, or of longer rows: runs of rows, two workgroups a compute unit, 16 rows at least.
 constexpr u32 kMostRuns = 128;
@@ -475,7 +509,7 @@ u32 run_count(u32 rows, u32 cols) { return (rows + run_rows(rows, cols) - 1) / r
 template <int kType, int kDyType, bool kSums>
 int launch_held(const NormBack &g, hipStream_t stream)
 {
-    const u32 cols = g.cols, grid = held_groups(g.rows, g.cols);
+    const u32 cols = g.cols, grid = held_groups(g.rows, g.cols, 2);
     if (cols <= 512) k_norm_back<kType, kDyType, 1, 1, kSums><<<grid, kNormThreads, 0, stream>>>(g);
     else if (cols <= 1024) k_norm_back<kType, kDyType, 1, 2, kSums><<<grid, kNormThreads, 0, stream>>>(g);
     else if (cols <= 2048) k_norm_back<kType, kDyType, 4, 1, kSums><<<grid, kNormThreads, 0, stream>>>(g);
@@ -487,7 +521,7 @@ int launch_held(const NormBack &g, hipStream_t stream)
 
 int join_sums(const NormBack &g, hipStream_t stream)
 {
-    k_norm_back_join<<<dim3((g.cols + kWave - 1) / kWave, 2), kNormThreads, 0, stream>>>(g);
+    k_norm_back_join<<<dim3((g.cols + kJoinColumns - 1) / kJoinColumns, 2), kJoinThreads, 0, stream>>>(g);
     return launched();
 }
 
@@ -496,7 +530,7 @@ int launch_back(NormBack g, hipStream_t stream)
 {
     const bool sums = g.dgamma || g.dbeta;
     if (g.dx && g.cols <= kHeldColumns) {
-        g.runs = held_groups(g.rows, g.cols);
+        g.runs = held_groups(g.rows, g.cols, 2);
         if (!sums) return launch_held<kType, kDyType, false>(g, stream);
         if (const int rc = launch_held<kType, kDyType, true>(g, stream)) return rc;
         return join_sums(g, stream);
@@ -540,7 +574,7 @@ extern "C" int rtopk_layer_norm_backward_workspace_bytes(uint64_t rows, uint64_t
     if (!bytes || rows > kMostSize || !size_ok(cols)) return RTOPK_EINVAL;
     *bytes = 0;
     if (rows) {
-        const u32 runs = run_count((u32)rows, (u32)cols), held = cols <= kHeldColumns ? held_groups((u32)rows, (u32)cols) : 0;
+        const u32 runs = run_count((u32)rows, (u32)cols), held = cols <= kHeldColumns ? held_groups((u32)rows, (u32)cols, 2) : 0;
         *bytes = align_up(8ull * std::max(runs, held) * cols, 256);
     }
     return RTOPK_OK;
