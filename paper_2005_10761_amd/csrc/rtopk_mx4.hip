@@ -384,6 +384,140 @@ __global__ void __launch_bounds__(256) k_product4_join(Product4 g)
     }
 }
 
+// ---------------------------------------------------------------------------
+// Few tokens: one read of the weights. A workgroup has 16 channels; its wavefronts share the contraction and add up in LDS,
+// in order. A lane's 16 bytes of a row of weights are a block, as the instruction takes them, at any alignment; the tokens are
+// the other operand, up to 16 of them. Neighbouring workgroups are on one XCD: they share the lines that the scales lie in.
+// ---------------------------------------------------------------------------
+constexpr u32 kFewTokens = 16;              // at most: what one instruction takes
+constexpr u32 kStepBytes = 64, kStepBlocks = 4;     // of a row, in one instruction
+constexpr u32 kInOne = 8192;                // numbers of x that a workgroup can quantise for itself (one launch less)
+
+struct Few4 {
+    Product4 p;                             // a: quantised tokens, or null
+    const void *x;
+    u64 ldx;
+};
+
+__device__ __forceinline__ f32x4 multiply_step(const i32x4 &a, const i32x4 &b, const f32x4 &sum, u32 a_scale, u32 b_scale)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(i32x8{a[0], a[1], a[2], a[3], 0, 0, 0, 0}, i32x8{b[0], b[1], b[2], b[3], 0, 0, 0, 0},
+                                                            sum, 4, 4, 0, (int)a_scale, 0, (int)b_scale);
+#else
+    return sum;
+#endif
+}
+
+// bytes of a token in LDS: its numbers, its scales, and 16 more (tokens start in different banks)
+__host__ __device__ constexpr u32 token_bytes(u32 steps) { return (u32)align_up(steps * (kStepBytes + kStepBlocks), 16) + 16u; }
+
+// kType: of x, or -1 where it is quantised already
+template <int kWaves, int kType>
+__global__ void __launch_bounds__(kWaves * kWave) k_few4(Few4 f)
+{
+    constexpr bool kQuantize = kType >= 0;
+    constexpr u32 kBatch = 8, kThreads = kWaves * kWave;
+    const Product4 &g = f.p;
+    const u32 lane = lane_id(), wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+    const u32 group = xcd_place(blockIdx.x, gridDim.x), quarter = lane >> 4, channel = min(group * 16u + (lane & 15u), g.n - 1u);
+    extern __shared__ __align__(16) unsigned char lds[];
+    const u32 bytes = (g.k + 1u) / 2u, blocks = (g.k + kBlock - 1) / kBlock, steps = (blocks + kStepBlocks - 1) / kStepBlocks;
+    const u32 each = (steps + kWaves - 1) / kWaves, from = min(wave * each, steps), to = min(from + each, steps);
+    const unsigned char *w = g.b + channel * g.ldb, *w_scale = g.b_scale + channel;
+    f32x4 sum{0, 0, 0, 0};
+    i32x4 held[kBatch];
+    u32 held_scale[kBatch];
+    const u32 whole = min(to, bytes / kStepBytes);
+    auto fetch = [&](u32 s) {
+        if (s + kBatch <= whole) {
+#pragma unroll
+            for (u32 q = 0; q < kBatch; ++q) __builtin_memcpy(&held[q], w + (s + q) * kStepBytes + quarter * 16u, 16);
+        } else {
+#pragma unroll
+            for (u32 q = 0; q < kBatch; ++q)
+                if (s + q < to) held[q] = load_piece(w, (s + q) * kStepBytes + quarter * 16u, bytes);
+#pragma unroll
+            for (u32 q = 0; q < kBatch; ++q)
+                if (s + q < to) held[q] = cut_piece(held[q], (s + q) * kStepBytes + quarter * 16u, bytes);
+        }
+        // (behind the last block: its scale again, with numbers 0)
+#pragma unroll
+        for (u32 q = 0; q < kBatch; ++q)
+            if (s + q < to) held_scale[q] = w_scale[min((s + q) * kStepBlocks + quarter, blocks - 1u) * g.ldb_scale];
+    };
+    fetch(from);                            // the first weights are on their way while x is quantised
+    const u32 row = token_bytes(steps), scales = steps * kStepBytes;
+    if constexpr (kQuantize) {
+        // every thread holds up to kHeld pieces of eight, whatever token they are of: one trip to memory. Four threads have a block
+        constexpr u32 kHeld = (kInOne / 8 + kFewTokens * 4 * kStepBlocks + kThreads - 1) / kThreads;
+        typedef Eight<kQuantize ? kType : 0> E;
+        const u64 row_bytes = f.ldx * E::kSize;
+        const unsigned char *x = (const unsigned char *)f.x;
+        const u32 pieces = steps * kStepBlocks * 4u, all = g.m * pieces;
+        E held_x[kHeld];
+        u32 token[kHeld], c[kHeld];
+#pragma unroll
+        for (u32 h = 0; h < kHeld; ++h) {
+            if (h * kThreads >= all) break;                 // (uniform)
+            const u32 at = threadIdx.x + h * kThreads;
+            token[h] = g.m == 1 || at >= all ? 0u : at / pieces;
+            c[h] = at >= all ? pieces * 8u : (at - token[h] * pieces) * 8u;     // (beyond: zeros)
+            held_x[h].load(x + token[h] * row_bytes, c[h], g.k);
+        }
+#pragma unroll
+        for (u32 h = 0; h < kHeld; ++h) {
+            if (h * kThreads >= all) break;
+            float v[8];
+            held_x[h].numbers(v, x + token[h] * row_bytes, c[h], g.k);
+            u32 largest = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) largest = max(largest, magnitude(v[i]));
+            const u32 byte = scale_byte(quad_max(largest), false), word = nearest_four_bits(v, byte);
+            if (threadIdx.x + h * kThreads >= all) continue;
+            *(u32 *)(lds + token[h] * row + c[h] / 2u) = word;
+            if ((lane & 3u) == 0) lds[token[h] * row + scales + c[h] / kBlock] = (unsigned char)byte;
+        }
+        __syncthreads();
+    }
+    const u32 token = min(lane & 15u, g.m - 1u);
+    for (u32 s = from; s < to; s += kBatch) {
+        i32x4 now[kBatch];
+        u32 now_scale[kBatch];
+#pragma unroll
+        for (u32 q = 0; q < kBatch; ++q) {
+            now[q] = held[q];
+            now_scale[q] = held_scale[q];
+        }
+        if (s + kBatch < to) fetch(s + kBatch);
+#pragma unroll
+        for (u32 q = 0; q < kBatch; ++q) {
+            if (s + q >= to) break;
+            const u32 block = (s + q) * kStepBlocks + quarter;
+            i32x4 x;
+            u32 x_scale;
+            if constexpr (kQuantize) {
+                x = *(const i32x4 *)(lds + token * row + block * 16u);
+                x_scale = lds[token * row + scales + block];
+            } else {
+                x = *(const i32x4 *)(g.a + token * g.lda + block * 16u);
+                x_scale = g.a_scale[block * g.lda_scale + token];
+            }
+            sum = multiply_step(now[q], x, sum, now_scale[q], x_scale);
+        }
+    }
+    // lane l: token l % 16, channels 4 (l / 16) .. + 3
+    __syncthreads();
+    f32x4 *part = (f32x4 *)lds;
+    if (wave) part[(wave - 1) * kWave + lane] = sum;
+    __syncthreads();
+    if (wave) return;
+    const u32 col = group * 16u + 4u * quarter;
+    if (col >= g.n || (lane & 15u) >= g.m) return;
+    for (int o = 0; o < kWaves - 1; ++o) sum += part[o * kWave + lane];
+    write_four(g.out, token * g.ldo + col, g.type, sum + four_biases(g, col), g.n - col);
+}
+
 __global__ void __launch_bounds__(256) k_zero4(float *p, u32 rows, u32 cols, u64 ld)
 {
     for (u64 at = (u64)blockIdx.x * 256 + threadIdx.x; at < (u64)rows * cols; at += (u64)gridDim.x * 256)
@@ -499,6 +633,28 @@ int run_product4(Product4 g, void *part, hipStream_t stream)
     return RTOPK_OK;
 }
 
+template <int kWaves>
+int launch_few4(const Few4 &f, int type, hipStream_t stream)
+{
+    const u32 blocks = (f.p.n + 15) / 16, sums = (kWaves - 1) * kWave * 16;
+    const u32 tokens = f.p.a ? 0 : f.p.m * token_bytes((f.p.k + 4 * kBlock - 1) / (4 * kBlock));
+    const u32 lds = std::max(sums, tokens);
+    if (f.p.a) k_few4<kWaves, -1><<<blocks, kWaves * kWave, lds, stream>>>(f);
+    else if (type == RTOPK_F32) k_few4<kWaves, RTOPK_F32><<<blocks, kWaves * kWave, lds, stream>>>(f);
+    else if (type == RTOPK_BF16) k_few4<kWaves, RTOPK_BF16><<<blocks, kWaves * kWave, lds, stream>>>(f);
+    else k_few4<kWaves, RTOPK_F16><<<blocks, kWaves * kWave, lds, stream>>>(f);
+    return launched();
+}
+
+bool few_tokens(u32 m) { return m <= kFewTokens; }
+// Every workgroup of a unit quantises the tokens again.
+bool in_one(u32 m, u32 k, u32 n) { return few_tokens(m) && (u64)m * k <= kInOne && (u64)m * k * ((n + 16 * kUnits - 1) / (16 * kUnits)) <= 20000; }
+
+int run_few4(const Few4 &f, int type, hipStream_t stream)
+{
+    return f.p.n > kUnits * 16 ? launch_few4<4>(f, type, stream) : launch_few4<16>(f, type, stream);
+}
+
 // rows of quantised numbers in a workspace: whole slices of the contraction, zeros behind the row's end
 u64 filled(u32 k) { return align_up(k, 2 * kSlice); }
 u64 scale_ld(u32 rows) { return align_up(rows, 16); }
@@ -528,8 +684,9 @@ struct LinearParts {
 u64 cut_linear(void *base, u32 m, u32 k, u32 n, LinearParts &p)
 {
     Cut cut{(unsigned char *)base};
+    if (in_one(m, k, n)) return 0;
     p.x = take_operand(cut, m, k);
-    p.part = cut.take<void>(part_bytes(m, n, k));
+    p.part = cut.take<void>(few_tokens(m) ? 0 : part_bytes(m, n, k));
     return cut.at;
 }
 
@@ -622,12 +779,12 @@ extern "C" int rtopk_linear_mx4(const void *x, int type, uint64_t m, uint64_t k,
     if (!x || !w || !w_scale || !out) return RTOPK_EINVAL;
     if (!workspace_ok(workspace, workspace_bytes, need)) return RTOPK_EWORKSPACE;
     hipStream_t stream = (hipStream_t)stream_v;
-    LinearParts p;
+    LinearParts p{};
     cut_linear(workspace, (u32)m, (u32)k, (u32)n, p);
+    const Product4 g{p.x.q, w, p.x.scale, w_scale, p.x.ldq, ldw, p.x.lds, ldw_scale, (u32)m, (u32)n, (u32)k, bias, out, ldo, out_type, 0, 0, nullptr};
+    if (in_one((u32)m, (u32)k, (u32)n)) return run_few4(Few4{g, x, ldx}, type, stream);
     if (const int rc = pack_rows(to_pack(x, ldx, (u32)m, (u32)k, (u32)filled((u32)k), p.x, Drawing{}), type, false, stream)) return rc;
-    return run_product4(Product4{p.x.q, w, p.x.scale, w_scale, p.x.ldq, ldw, p.x.lds, ldw_scale, (u32)m, (u32)n, (u32)k, bias, out, ldo,
-                                 out_type, 0, 0, nullptr},
-                        p.part, stream);
+    return few_tokens((u32)m) ? run_few4(Few4{g, nullptr, 0}, type, stream) : run_product4(g, p.part, stream);
 }
 
 extern "C" int rtopk_linear_mx4_backward_workspace_bytes(uint64_t m, uint64_t k, uint64_t n, uint64_t *bytes)
