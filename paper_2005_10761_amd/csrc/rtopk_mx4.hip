@@ -51,16 +51,17 @@ __device__ __forceinline__ u32 nearest_four_bits(const float (&x)[8], u32 byte)
 }
 
 // t = |x| / scale lies between two numbers, a step apart, a fraction f above the lower: up where a 16-bit draw u has
-// u + 1/2 < 65536 f (the chance is f to the nearest 2^-16). All of it is exact but, where t is far below a step, a product that may lose bits of
-// an f under 2^-17, which is never up.
+// u + 1/2 < 65536 f, which is (whole numbers) u < W, W = 65536 f - 1/2 rounded up; so the place among steps is (W + 65535 - u) >> 16, with the
+// lower number's place in W's upper bits. Exact: t / step has 24 bits, and 1/2 is subtracted in one rounding that
+// loses none of them that count. (Where t is far below a step, t may have lost bits of an f under 2^-17, which is never up.)
 __device__ __forceinline__ u32 drawn_four_bits(float x, float inverse, u32 draw)
 {
     const float t = fabsf(x) * inverse;
-    const float in_steps = t < 2.0f ? t + t : t < 4.0f ? t : 0.5f * t;
-    const float low = floorf(in_steps);
-    const u32 from = t < 2.0f ? 0u : t < 4.0f ? 2u : 4u;        // the places of 0, 1 (two steps of 1 below 2) and of 2 steps of 2 below 4
-    const u32 up = (float)draw + 0.5f < 65536.0f * (in_steps - low) ? 1u : 0u;
-    return (u32)low + from + up | (__float_as_uint(x) >> 31 << 3);
+    const bool two = t >= 2.0f, four = t >= 4.0f;
+    const float steps = four ? 32768.0f : two ? 65536.0f : 131072.0f;          // 65536 / step
+    const u32 from = four ? 0x4FFFFu : two ? 0x2FFFFu : 0xFFFFu;               // 65535, and the place of 0, of 2 below 2, of 4 below 4
+    const u32 w = (u32)ceilf(fmaf(t, steps, -0.5f));
+    return (w + from - draw) >> 16 | (__float_as_uint(x) >> 28 & 8u);
 }
 __device__ __forceinline__ u32 drawn_four_bits(const float (&x)[8], u32 byte, const EightDraws &u)
 {
@@ -109,46 +110,65 @@ __device__ __forceinline__ void write_bytes(unsigned char *row, u32 at, u32 word
 // groups of eight draws of a row of a contraction of so many numbers
 __device__ __forceinline__ u32 groups_of(u32 k) { return (k + kBlock - 1) / kBlock * (kBlock / 8); }
 
-// Along rows: a workgroup has kTileRows rows and 512 columns, a lane eight neighbours of a row, four lanes a block.
+// Along rows: a workgroup has kTileRows rows and 512 columns, a lane eight neighbours of a row, four lanes a block. The scales
+// lie the other way: they are put together in LDS, kTileRows bytes of each block, and workgroups of neighbouring rows are on
+// one XCD, so that its L2 has whole lines of them.
 constexpr int kPackThreads = 256;
-constexpr u32 kTileRows = 16, kTileColumns = 8 * kWave;
+constexpr u32 kTileColumns = 8 * kWave, kTileBlocks = kTileColumns / kBlock;
 
-template <int kType, bool kDrawn>
+template <int kType, bool kDrawn, u32 kTileRows>
 __global__ void __launch_bounds__(kPackThreads) k_pack_rows(ToPack g)
 {
-    constexpr u32 kWaves = kPackThreads / kWave, kEach = kTileRows / kWaves;
-    __shared__ unsigned char scales[kTileColumns / kBlock][kTileRows];
-    const u32 lane = lane_id(), wave = threadIdx.x / kWave;
-    const u32 r0 = blockIdx.x * kTileRows + wave * kEach, c = blockIdx.y * kTileColumns + lane * 8u;
+#ifndef PB
+#define PB 4
+#endif
+    constexpr u32 kWaves = kPackThreads / kWave, kEach = kTileRows / kWaves, kAtOnce = kEach < PB ? kEach : PB;
+    __shared__ __align__(16) unsigned char scales[kTileBlocks][kTileRows];
+    const u32 lane = lane_id(), wave = threadIdx.x / kWave, tiles = (g.rows + kTileRows - 1) / kTileRows;
+    const u32 place = xcd_place(blockIdx.x, gridDim.x), tile = place % tiles, strip = place / tiles;
+    const u32 r0 = tile * kTileRows + wave * kEach, c = strip * kTileColumns + lane * 8u;
     PhiloxSeed seed{};
     if (kDrawn) seed = g.drawing.get();
-    const u32 blocks = (g.fill + kBlock - 1) / kBlock;
+    const u32 blocks = (g.fill + kBlock - 1) / kBlock, have = (g.fill + 1u) / 2u;
     const u64 row_bytes = g.ldx * Eight<kType>::kSize;
-    Eight<kType> e[kEach];
+    Eight<kType> next[kAtOnce];
+    auto fetch = [&](u32 r) {
 #pragma unroll
-    for (u32 q = 0; q < kEach; ++q) e[q].load((const unsigned char *)g.x + min(r0 + q, g.rows - 1u) * row_bytes, c, g.cols);
+        for (u32 q = 0; q < kAtOnce; ++q) next[q].load((const unsigned char *)g.x + min(r + q, g.rows - 1u) * row_bytes, c, g.cols);
+    };
+    fetch(r0);
+    for (u32 done = 0; done < kEach && r0 + done < g.rows; done += kAtOnce) {
+        Eight<kType> e[kAtOnce];
 #pragma unroll
-    for (u32 q = 0; q < kEach; ++q) {
-        const u32 r = r0 + q;
-        float v[8];
-        e[q].numbers(v, (const unsigned char *)g.x + min(r, g.rows - 1u) * row_bytes, c, g.cols);
-        u32 largest = 0;
+        for (u32 q = 0; q < kAtOnce; ++q) e[q] = next[q];
+        if (done + kAtOnce < kEach) fetch(r0 + done + kAtOnce);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) largest = max(largest, magnitude(v[i]));
-        const u32 byte = scale_byte(quad_max(largest), kDrawn);
-        u32 word;
-        if (kDrawn) word = drawn_four_bits(v, byte, draw_eight((u64)r * groups_of(g.cols) + c / 8u, kDrawsForRows, seed));
-        else word = nearest_four_bits(v, byte);
-        if (r < g.rows) write_bytes(g.to.q + r * g.to.ldq, c / 2u, word, (g.fill + 1u) / 2u);
-        if ((lane & 3u) == 0) scales[lane >> 2][wave * kEach + q] = (unsigned char)byte;
+        for (u32 q = 0; q < kAtOnce; ++q) {
+            const u32 r = r0 + done + q;
+            float v[8];
+            e[q].numbers(v, (const unsigned char *)g.x + min(r, g.rows - 1u) * row_bytes, c, g.cols);
+            u32 largest = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) largest = max(largest, magnitude(v[i]));
+            const u32 byte = scale_byte(quad_max(largest), kDrawn);
+            u32 word;
+            if (kDrawn) word = drawn_four_bits(v, byte, draw_eight((u64)r * groups_of(g.cols) + c / 8u, kDrawsForRows, seed));
+            else word = nearest_four_bits(v, byte);
+            if (r < g.rows) write_bytes(g.to.q + r * g.to.ldq, c / 2u, word, have);
+            if ((lane & 3u) == 0) scales[lane >> 2][wave * kEach + done + q] = (unsigned char)byte;
+        }
     }
     __syncthreads();
-    const u32 row = threadIdx.x % kTileRows, block = threadIdx.x / kTileRows;
-    const u32 r = blockIdx.x * kTileRows + row, b = blockIdx.y * (kTileColumns / kBlock) + block;
-    if (r < g.rows && b < blocks) g.to.scale[b * g.to.lds + r] = scales[block][row];
+    constexpr u32 kPerThread = kTileBlocks * kTileRows / kPackThreads;          // 1 or 4 neighbours
+    const u32 row = threadIdx.x * kPerThread % kTileRows, block = threadIdx.x * kPerThread / kTileRows;
+    const u32 r = tile * kTileRows + row, b = strip * kTileBlocks + block;
+    if (b >= blocks) return;
+    unsigned char *to = g.to.scale + b * g.to.lds + r;
+    if constexpr (kPerThread == 4) write_bytes(to, 0, *(const u32 *)&scales[block][row], r < g.rows ? g.rows - r : 0u);
+    else if (r < g.rows) *to = scales[block][row];
 }
 
-// Along columns, and turned over: a wavefront has 32 rows and 64 columns, a lane four neighbouring rows of eight columns; a
+// Along columns, and turned over: a wavefront has 32 rows and 64 columns, a lane eight neighbouring rows of four columns; a
 // workgroup has eight blocks of 32 rows, which it writes as 128 bytes of each column.
 constexpr u32 kTurnWaves = 8, kTurnThreads = kTurnWaves * kWave, kTurnRows = kTurnWaves * kBlock;
 
@@ -161,76 +181,118 @@ struct Turns {
     u32 drawn;                  // bit i: of[i] by chance
 };
 
+// Four neighbours of a row, as Eight does it.
+template <int kType> struct Quad {
+    u32 w[kType == 0 ? 4 : 2];
+    static constexpr u32 kSize = kType == 0 ? 4u : 2u;
+    __device__ __forceinline__ void load(const unsigned char *row, u32 c, u32 cols)
+    {
+        const unsigned char *p = cols < 4u ? (const unsigned char *)kNothing : row + min(c, cols - 4u) * kSize;
+        __builtin_memcpy(w, p, sizeof w);
+    }
+    __device__ __forceinline__ void numbers(float (&v)[4], const unsigned char *row, u32 c, u32 cols) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float x;
+            if (kType == 0) {
+                x = __uint_as_float(w[kType == 0 ? i : 0]);
+            } else {
+                const u16 h = (u16)(w[i >> 1] >> (16 * (i & 1)));
+                x = kType == 1 ? __uint_as_float((u32)h << 16) : (float)__builtin_bit_cast(_Float16, h);
+            }
+            v[i] = c < cols ? x : 0.0f;
+        }
+        if (c + 4u <= cols) return;
+        if (cols >= 4u) {
+            const u32 down = c - (cols - 4u);
+#pragma unroll
+            for (int by = 2; by; by >>= 1)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = down & by ? (i + by < 4 ? v[i + by] : 0.0f) : v[i];
+            if (down > 3u) v[0] = v[1] = v[2] = v[3] = 0.0f;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (c + i < cols) v[i] = read_as(row, c + i, kType);
+        }
+    }
+};
+
+// largest over the lanes l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ u32 max_of_four_rows(u32 v)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = max((u32)a[0], (u32)a[1]);
+    const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max((u32)b[0], (u32)b[1]);
+#endif
+    return v;
+}
+
 template <int kType, bool kDrawn>
 __device__ __forceinline__ void pack_columns(const ToTurn &t)
 {
     const ToPack &g = t.of;
     constexpr u32 kRow = kTurnRows / 2 + 4;                 // bytes of a column in LDS
     __shared__ __align__(16) unsigned char turned[kWave * kRow];
-    __shared__ float sums[kTurnWaves][kWave];
+    __shared__ float sums[4 * kTurnWaves][kWave];
     const u32 lane = lane_id(), wave = threadIdx.x / kWave;
     const u32 c0 = blockIdx.x * kWave, first = blockIdx.y * kTurnRows;
-    const u32 blocks = (g.fill + kBlock - 1) / kBlock;      // of a column
-    const u32 piece = lane & 7u, quad = lane >> 3, c = c0 + 8u * piece, r0 = first + wave * kBlock + 4u * quad;
+    const u32 blocks = (g.fill + kBlock - 1) / kBlock, block = first / kBlock + wave;     // of a column
+    const u32 c_in = 4u * (lane & 15u), part = lane >> 4, c = c0 + c_in, r0 = first + wave * kBlock + 8u * part;
     PhiloxSeed seed{};
     if (kDrawn) seed = g.drawing.get();
-    const u64 row_bytes = g.ldx * Eight<kType>::kSize;
-    Eight<kType> e[4];
-    float v[4][8];
+    const u64 row_bytes = g.ldx * Quad<kType>::kSize;
+    Quad<kType> e[8];
+    float v[8][4];
 #pragma unroll
-    for (u32 b = 0; b < 4; ++b) e[b].load((const unsigned char *)g.x + min(r0 + b, g.rows - 1u) * row_bytes, c, g.cols);
+    for (u32 b = 0; b < 8; ++b) e[b].load((const unsigned char *)g.x + min(r0 + b, g.rows - 1u) * row_bytes, c, g.cols);
 #pragma unroll
-    for (u32 b = 0; b < 4; ++b) {
-        e[b].numbers(v[b], (const unsigned char *)g.x + min(r0 + b, g.rows - 1u) * row_bytes, c, g.cols);
+    for (u32 b = 0; b < 8; ++b)
+        e[b].numbers(v[b], (const unsigned char *)g.x + min(r0 + b, g.rows - 1u) * row_bytes, c, r0 + b < g.rows ? g.cols : 0u);
+    u32 bytes = 0;
+    f32x4 sum;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[b][i] = r0 + b < g.rows ? v[b][i] : 0.0f;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
         u32 largest = 0;
-        float sum = 0;
+        sum[i] = 0;
 #pragma unroll
-        for (u32 b = 0; b < 4; ++b) {
+        for (u32 b = 0; b < 8; ++b) {
             largest = max(largest, magnitude(v[b][i]));
-            sum += v[b][i];
+            sum[i] += v[b][i];
         }
-#pragma unroll
-        for (int o = 8; o < kWave; o <<= 1) {
-            largest = max(largest, (u32)__shfl_xor((int)largest, o, kWave));
-            sum += __shfl_xor(sum, o, kWave);
-        }
-        const u32 byte = scale_byte(largest, kDrawn), block = first / kBlock + wave;
-        if (quad == 0) {
-            if (c + i < g.cols && block < blocks) g.to.scale[block * g.to.lds + c + i] = (unsigned char)byte;
-            sums[wave][8 * piece + i] = sum;
-        }
-        u32 word = 0;
-        if (kDrawn) {
-            // (a group is eight rows of a column: two lanes share it)
-            const EightDraws u = draw_eight((u64)(c + i) * groups_of(g.rows) + r0 / 8u, kDrawsForColumns, seed);
-            const float inverse = __uint_as_float((254u - byte) << 23);
-#pragma unroll
-            for (u32 b = 0; b < 4; ++b) word |= drawn_four_bits(v[b][i], inverse, quad & 1u ? u[4 + b] : u[b]) << (4 * b);
-            word = byte == 255u ? 0u : word;
-        } else {
-            const float four[8] = {v[0][i], v[1][i], v[2][i], v[3][i], 0, 0, 0, 0};
-            word = nearest_four_bits(four, byte);
-        }
-        *(u16 *)(turned + (8 * piece + i) * kRow + wave * 16u + 2u * quad) = (u16)word;
+        const u32 byte = scale_byte(max_of_four_rows(largest), kDrawn);
+        bytes |= byte << (8 * i);
+        const float eight[8] = {v[0][i], v[1][i], v[2][i], v[3][i], v[4][i], v[5][i], v[6][i], v[7][i]};
+        u32 word;
+        if (kDrawn) word = drawn_four_bits(eight, byte, draw_eight((u64)(c + i) * groups_of(g.rows) + r0 / 8u, kDrawsForColumns, seed));
+        else word = nearest_four_bits(eight, byte);
+        *(u32 *)(turned + (c_in + i) * kRow + wave * 16u + 4u * part) = word;
     }
+    if (part == 0 && c < g.cols && block < blocks) write_bytes(g.to.scale + block * g.to.lds + c, 0, bytes, g.cols - c);
+    if (t.sums) *(f32x4 *)&sums[4 * wave + part][c_in] = sum;
     __syncthreads();
     if (t.sums && wave == 0 && c0 + lane < g.cols && first < g.rows) {
-        float sum = sums[0][lane];
-        for (u32 w = 1; w < kTurnWaves; ++w) sum += sums[w][lane];
-        t.sums[(u64)blockIdx.y * g.cols + c0 + lane] = sum;
+        float all = sums[0][lane];
+        for (u32 w = 1; w < 4 * kTurnWaves; ++w) all += sums[w][lane];
+        t.sums[(u64)blockIdx.y * g.cols + c0 + lane] = all;
     }
     const u32 col = threadIdx.x >> 3, at = 16u * (threadIdx.x & 7u);
     if (c0 + col >= g.cols) return;
     unsigned char *q = g.to.q + (u64)(c0 + col) * g.to.ldq;
     const u32 have = (g.fill + 1u) / 2u, from = first / 2u + at;
+    u32 word[4];
 #pragma unroll
-    for (u32 w = 0; w < 4; ++w)
-        if (from + 4 * w < have) write_bytes(q, from + 4 * w, *(const u32 *)(turned + col * kRow + at + 4 * w), have);
+    for (u32 w = 0; w < 4; ++w) word[w] = *(const u32 *)(turned + col * kRow + at + 4 * w);
+    if (from + 16u <= have) {
+        __builtin_memcpy(q + from, word, 16);
+    } else {
+#pragma unroll
+        for (u32 w = 0; w < 4; ++w)
+            if (from + 4 * w < have) write_bytes(q, from + 4 * w, word[w], have);
+    }
 }
 
 template <int kType>
@@ -417,7 +479,7 @@ template <int kWaves, int kType>
 __global__ void __launch_bounds__(kWaves * kWave) k_few4(Few4 f)
 {
     constexpr bool kQuantize = kType >= 0;
-    constexpr u32 kBatch = 8, kThreads = kWaves * kWave;
+    constexpr u32 kBatch = 4, kThreads = kWaves * kWave;
     const Product4 &g = f.p;
     const u32 lane = lane_id(), wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
     const u32 group = xcd_place(blockIdx.x, gridDim.x), quarter = lane >> 4, channel = min(group * 16u + (lane & 15u), g.n - 1u);
@@ -446,7 +508,6 @@ __global__ void __launch_bounds__(kWaves * kWave) k_few4(Few4 f)
         for (u32 q = 0; q < kBatch; ++q)
             if (s + q < to) held_scale[q] = w_scale[min((s + q) * kStepBlocks + quarter, blocks - 1u) * g.ldb_scale];
     };
-    fetch(from);                            // the first weights are on their way while x is quantised
     const u32 row = token_bytes(steps), scales = steps * kStepBytes;
     if constexpr (kQuantize) {
         // every thread holds up to kHeld pieces of eight, whatever token they are of: one trip to memory. Four threads have a block
@@ -465,6 +526,7 @@ __global__ void __launch_bounds__(kWaves * kWave) k_few4(Few4 f)
             c[h] = at >= all ? pieces * 8u : (at - token[h] * pieces) * 8u;     // (beyond: zeros)
             held_x[h].load(x + token[h] * row_bytes, c[h], g.k);
         }
+        fetch(from);        // (the first weights are on their way while x is quantised; behind x, for loads come back in order)
 #pragma unroll
         for (u32 h = 0; h < kHeld; ++h) {
             if (h * kThreads >= all) break;
@@ -478,7 +540,9 @@ __global__ void __launch_bounds__(kWaves * kWave) k_few4(Few4 f)
             *(u32 *)(lds + token[h] * row + c[h] / 2u) = word;
             if ((lane & 3u) == 0) lds[token[h] * row + scales + c[h] / kBlock] = (unsigned char)byte;
         }
-        __syncthreads();
+        lds_barrier();
+    } else {
+        fetch(from);
     }
     const u32 token = min(lane & 15u, g.m - 1u);
     for (u32 s = from; s < to; s += kBatch) {
@@ -541,12 +605,20 @@ u64 blocks_of(u64 k) { return (k + kBlock - 1) / kBlock; }
 // a quantised operand [rows][k]: the distances of its rows and of its scales' blocks
 bool packed_ok(u64 rows, u64 k, u64 ldq, u64 lds) { return ldq >= bytes_of(k) && ldq <= kMostSize && lds >= rows && lds <= kMostSize; }
 
+template <int kType, u32 kTileRows>
+void launch_pack_rows(const ToPack &g, u32 strips, bool drawn, hipStream_t stream)
+{
+    const u32 grid = (g.rows + kTileRows - 1) / kTileRows * strips;
+    if (drawn) k_pack_rows<kType, true, kTileRows><<<grid, kPackThreads, 0, stream>>>(g);
+    else k_pack_rows<kType, false, kTileRows><<<grid, kPackThreads, 0, stream>>>(g);
+}
 template <int kType>
 int pack_rows(const ToPack &g, bool drawn, hipStream_t stream)
 {
-    const dim3 grid((g.rows + kTileRows - 1) / kTileRows, (g.fill + kTileColumns - 1) / kTileColumns);
-    if (drawn) k_pack_rows<kType, true><<<grid, kPackThreads, 0, stream>>>(g);
-    else k_pack_rows<kType, false><<<grid, kPackThreads, 0, stream>>>(g);
+    // 64 rows where that leaves two workgroups a unit
+    const u32 strips = (g.fill + kTileColumns - 1) / kTileColumns;
+    if ((u64)((g.rows + 63u) / 64u) * strips >= 2 * kUnits) launch_pack_rows<kType, 64>(g, strips, drawn, stream);
+    else launch_pack_rows<kType, 16>(g, strips, drawn, stream);
     return launched();
 }
 int pack_rows(const ToPack &g, int type, bool drawn, hipStream_t stream)
@@ -652,7 +724,7 @@ bool in_one(u32 m, u32 k, u32 n) { return few_tokens(m) && (u64)m * k <= kInOne 
 
 int run_few4(const Few4 &f, int type, hipStream_t stream)
 {
-    return f.p.n > kUnits * 16 ? launch_few4<4>(f, type, stream) : launch_few4<16>(f, type, stream);
+    return f.p.n > kUnits * 16 ? launch_few4<4>(f, type, stream) : f.p.n > kUnits * 8 ? launch_few4<8>(f, type, stream) : launch_few4<16>(f, type, stream);
 }
 
 // rows of quantised numbers in a workspace: whole slices of the contraction, zeros behind the row's end
