@@ -1,18 +1,14 @@
-// The matrix core that the 8-bit and 4-bit products and the orthogonalisation
-// share (gfx950): C = A B^T for two operands whose rows run along the
-// contraction.
+// The matrix core that the 8-bit products and the orthogonalisation share
+// (gfx950): C = A B^T for two operands whose rows run along the contraction.
 //
 // Both operands are rows of bytes to the loader: 16 bytes a lane and operand
-// are 16 8-bit integers (v_mfma_i32_16x16x64_i8), 8 halves
-// (v_mfma_f32_16x16x32_f16) or 32 4-bit numbers, a block with a scale of its
-// own (v_mfma_scale_f32_16x16x128_f8f6f4), and the instructions hold them in the
-// same lanes: lane l has row l % 16, bytes 16 * (l / 16) on. A slice of the
+// are 16 8-bit integers (v_mfma_i32_16x16x64_i8) or 8 halves
+// (v_mfma_f32_16x16x32_f16), and the two instructions hold them in the same
+// lanes: lane l has row l % 16, bytes 16 * (l / 16) on. A slice of the
 // contraction is 128 bytes of every row: two instructions deep for one 8-bit
 // or half operand; or, where a number is the sum of two halves, 64 bytes of 32
 // high halves and 64 bytes of their 32 low halves.
 #pragma once
-
-#include <utility>
 
 #include "rtopk_common.h"
 
@@ -22,15 +18,13 @@ constexpr int kSlice = 128;          // bytes of a row in one slice of the contr
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 // What the bytes are. kPairs: each number is a high and a low half, and the
 // product takes high * high, high * low and low * high (what is left out is
-// 2^-22 of the product). kFours: 16 bytes are a block of 32 4-bit numbers, with
-// a byte of scale for each block of each row.
-enum Operands { kBytes, kHalves, kPairs, kFours };
+// 2^-22 of the product).
+enum Operands { kBytes, kHalves, kPairs };
 
 template <Operands kOf> struct Sums { typedef f32x4 type; };
 template <> struct Sums<kBytes> { typedef i32x4 type; };
@@ -38,17 +32,13 @@ template <> struct Sums<kBytes> { typedef i32x4 type; };
 // One operand of a tile: the row that the tile starts with, the rows that are
 // there from it on (rows past them repeat the last one: what they give is not
 // stored), the bytes from row to row and the bytes of a row that count (the
-// same for both operands). Of kFours, the scales of the contraction's first
-// block from the tile's first row on, and the bytes from block to block.
+// same for both operands).
 struct TileRows {
     const unsigned char *first;
     u32 rows;
     u32 stride;
     u32 bytes;
-    const unsigned char *scale = nullptr;
-    u32 scale_stride = 0;
 };
-constexpr u32 kSliceBlocks = kSlice / 16;       // of kFours
 
 // 16 bytes from byte `at` of a row of `bytes` bytes, zeros beyond its end; what is not there is not read. In two parts, so that
 // several loads are under way together: the load takes the row's last 16 bytes where it would go beyond them, and
@@ -98,46 +88,24 @@ __device__ __forceinline__ i32x4 cut_piece(const i32x4 &v, u32 at, u32 bytes)
 // kInOrder: fragment i has rows 16 i ..; kRuns: of A, a lane's rows are neighbours (eight, or four, or two of them: they
 // lie side by side in a result that is turned over); kWide: those, and of B the rows of two fragments alternate by
 // four, so that a lane has eight neighbouring columns (16 bytes of a 16-bit result; 64 bytes of a row from four lanes).
-// kByScale, for kFours: a lane's rows are neighbours in groups of four (of two and one, what is left), of both operands: their
-// scales, bytes that lie side by side, are one word, of which each instruction takes its byte; and a lane has 4 x 4
-// neighbouring columns of the result.
-enum Deal { kInOrder, kRuns, kWide, kByScale };
-
-// The groups of a wavefront's fragments of one operand under kByScale: fours, then a two, then a one.
-template <int kFrags> struct Groups {
-    static constexpr int kFours = kFrags / 4 * 4, kCount = kFrags / 4 + kFrags % 4 / 2 + kFrags % 2;
-    // first fragment, number of fragments and place of the group that fragment i is in
-    static constexpr int first(int i) { return i < kFours ? i / 4 * 4 : kFrags % 4 >= 2 && i < kFours + 2 ? kFours : kFrags - 1; }
-    static constexpr int size(int i) { return i < kFours ? 4 : kFrags % 4 >= 2 && i < kFours + 2 ? 2 : 1; }
-    static constexpr int place(int i) { return i < kFours ? i / 4 : kFours / 4 + (kFrags % 4 >= 2 && i >= kFours + 2 ? 1 : 0); }
-    // first fragment of group g
-    static constexpr int start(int g) { return 4 * g < kFours ? 4 * g : g == kFours / 4 ? kFours : kFrags - 1; }
-    static __device__ __forceinline__ u32 row(int i, u32 r) { return 16u * first(i) + size(i) * r + (i - first(i)); }
-};
+enum Deal { kInOrder, kRuns, kWide };
 
 template <Operands kOf, int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kAhead, Deal kDeal = kInOrder>
 struct Tile {
     static constexpr int kRowsM = kM, kRowsN = kN;
     static constexpr int kWaves = kWavesM * kWavesN, kThreads = kWaves * kWave;
-    // scales of a slice: [8 blocks][kM] of A, [8][kN] of B, in whole loads of 256 bytes for every wavefront
-    static constexpr bool kScaled = kOf == kFours;
-    static constexpr int kScales = kSliceBlocks * (kM + kN), kScaleLoads = kScaled ? (kScales + kWaves * 256 - 1) / (kWaves * 256) : 0;
-    static constexpr int kData = (kM + kN) * kSlice, kStage = kData + kScaleLoads * kWaves * 256, kLds = kStages * kStage;
+    static constexpr int kStage = (kM + kN) * kSlice, kLds = kStages * kStage;
     static constexpr int kFragsM = kM / kWavesM / 16, kFragsN = kN / kWavesN / 16;
-    static constexpr int kLoadsM = kM / 8 / kWaves, kLoadsN = kN / 8 / kWaves, kLoads = kLoadsM + kLoadsN, kAllLoads = kLoads + kScaleLoads;
-    typedef Groups<kFragsM> GroupsM;
-    typedef Groups<kFragsN> GroupsN;
-    static_assert(kScaled == (kDeal == kByScale), "scales are read by groups of neighbours");
+    static constexpr int kLoadsM = kM / 8 / kWaves, kLoadsN = kN / 8 / kWaves, kLoads = kLoadsM + kLoadsN;
     static_assert(kLoadsM * kWaves * 8 == kM && kLoadsN * kWaves * 8 == kN, "every wavefront loads whole groups of eight rows");
     static_assert(kFragsM * kWavesM * 16 == kM && kFragsN * kWavesN * 16 == kN, "whole instructions");
     static_assert(kStages >= 2, "one slice under way at least");
     typedef typename Sums<kOf>::type Sum;
     // sum[i][j]: row row_at(i) of A, rows col_at(j) .. + 3 of B
     Sum sum[kFragsM][kFragsN];
-    // half a slice: 64 bytes of the wavefront's rows; of kFours, for each group of fragments their scales, a byte each
+    // half a slice: 64 bytes of the wavefront's rows
     struct Half {
         i32x4 a[kFragsM], b[kFragsN];
-        u32 a_scale[kScaled ? GroupsM::kCount : 1], b_scale[kScaled ? GroupsN::kCount : 1];
     };
 
     static __device__ __forceinline__ u32 wave() { return (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)); }
@@ -147,7 +115,6 @@ struct Tile {
     // row r of fragment i of the wavefront's rows of A, and of fragment j of its rows of B
     static __device__ __forceinline__ u32 of_a(int i, u32 r)
     {
-        if (kDeal == kByScale) return GroupsM::row(i, r);
         constexpr int kEight = kFragsM / 8 * 8, kFour = kFragsM / 4 * 4, kRest = kFragsM - kFour;
         if (kDeal == kInOrder) return 16u * i + r;
         if (i < kEight) return 128u * (i / 8) + 8u * r + i % 8;
@@ -156,7 +123,6 @@ struct Tile {
     }
     static __device__ __forceinline__ u32 of_b(int j, u32 r)
     {
-        if (kDeal == kByScale) return GroupsN::row(j, r);
         if (kDeal == kWide && (j | 1) < kFragsN) return 32u * (j >> 1) + 8u * (r >> 2) + 4u * (j & 1) + (r & 3u);
         return 16u * j + r;
     }
@@ -201,21 +167,6 @@ struct Tile {
         return (q < kLoadsM ? 0 : kM * kSlice) + ((q < kLoadsM ? q : q - kLoadsM) * kWaves + wave()) * 8 * kSlice;
     }
 
-    // Of kFours: where the wavefront's load q of scales begins among a stage's scales (lane l's four follow at 4 l), and
-    // what they are: of which operand, which block of the slice, which row.
-    static __device__ __forceinline__ u32 scales_at(int q) { return (u32)((q * kWaves + wave()) * 256u); }
-    static __device__ __forceinline__ bool scales_of_a(int q) { return scales_at(q) < kSliceBlocks * kM; }
-    struct ScalePlace {
-        u32 block, row;
-    };
-    static __device__ __forceinline__ ScalePlace scale_place(int q)
-    {
-        const u32 at = scales_at(q) + 4u * lane_id();
-        if (at < kSliceBlocks * kM) return {at / kM, at % kM};
-        if (at < kScales) return {(at - kSliceBlocks * kM) / kN, (at - kSliceBlocks * kM) % kN};
-        return {0u, 0u};                                // (what fills the last loads)
-    }
-
     // Until at most kMore of this wavefront's loads to LDS are under way and all its reads from there are done, and until
     // every wavefront of the workgroup has come as far. (A fence would wait for every load to LDS.)
     template <int kMore>
@@ -245,10 +196,7 @@ struct Tile {
             prepare();
             return;
         }
-        u32 full = a.bytes / kSlice;
-        // scales are loaded by fours, beyond a last row that is not there; behind the last block nothing may be read
-        if (kScaled && full * kSlice == a.bytes && ((a.rows | b.rows) & 3u)) --full;
-        const u32 whole = kWhole ? (full < to ? full : to) : from;
+        const u32 whole = kWhole ? (a.bytes / kSlice < to ? a.bytes / kSlice : to) : from;
         u32 s = from;
         if (kWhole && s < whole) {
             const u32 lane = lane_id();
@@ -261,15 +209,6 @@ struct Tile {
             }
             const auto ra = __builtin_amdgcn_make_buffer_rsrc((void *)a.first, 0, 0xFFFFFFFFu, 0x00020000);
             const auto rb = __builtin_amdgcn_make_buffer_rsrc((void *)b.first, 0, 0xFFFFFFFFu, 0x00020000);
-            u32 scale_offset[kScaled ? kScaleLoads : 1];
-            if constexpr (kScaled) {
-#pragma unroll
-                for (int q = 0; q < kScaleLoads; ++q) {
-                    const TileRows &t = scales_of_a(q) ? a : b;
-                    const ScalePlace at = scale_place(q);
-                    scale_offset[q] = at.block * t.scale_stride + min(at.row, (t.rows - 1u) & ~3u);
-                }
-            }
             auto load = [&](u32 slice) {
                 unsigned char *stage = lds + (slice - from) % kStages * kStage;
 #pragma unroll
@@ -277,16 +216,6 @@ struct Tile {
                     __builtin_amdgcn_raw_ptr_buffer_load_lds(q < kLoadsM ? ra : rb,
                                                              (__attribute__((address_space(3))) void *)(stage + stage_at(q)), 16,
                                                              offset[q], slice * kSlice, 0, 0);
-                if constexpr (kScaled) {
-#pragma unroll
-                    for (int q = 0; q < kScaleLoads; ++q) {
-                        const TileRows &t = scales_of_a(q) ? a : b;
-                        const auto r = __builtin_amdgcn_make_buffer_rsrc((void *)(t.scale + (u64)(slice * kSliceBlocks) * t.scale_stride), 0,
-                                                                         0xFFFFFFFFu, 0x00020000);
-                        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(stage + kData + scales_at(q)), 4,
-                                                                 scale_offset[q], 0, 0, 0);
-                    }
-                }
             };
             load(s);
             if constexpr (kAhead) {
@@ -294,7 +223,7 @@ struct Tile {
                 for (int q = 1; q < kStages; ++q)
                     if (s + q < whole) load(s + q);
                 prepare();
-                if (s + kStages <= whole) wait_and_meet<(kStages - 1) * kAllLoads>();
+                if (s + kStages <= whole) wait_and_meet<(kStages - 1) * kLoads>();
                 else wait_and_meet<0>();
                 Half first, second;
                 read(first, lds, 0);
@@ -305,9 +234,9 @@ struct Tile {
                     mix<0>();
                     // this wavefront has read all of slice s, and its part of slice s + 1 has come; after the barrier
                     // that holds for everybody: the stage of slice s may be overwritten, that of s + 1 read
-                    wait_and_meet<(kStages - 2) * kAllLoads>();
+                    wait_and_meet<(kStages - 2) * kLoads>();
                     load(s + kStages);
-                    ahead<kAllLoads>(first, second, lds + (s + 1 - from) % kStages * kStage);
+                    ahead<kLoads>(first, second, lds + (s + 1 - from) % kStages * kStage);
                 }
                 for (; s + 1 < whole; ++s) {
                     read(second, lds + (s - from) % kStages * kStage, 1);
@@ -329,7 +258,7 @@ struct Tile {
                 for (; s < whole; ++s) {
                     // this wavefront's part of slice s has come (those of the kStages - 2 after it may be on their way); after
                     // the barrier everybody's has, and nobody reads the stage of slice s - 1
-                    if (s + kStages - 2 < whole) wait_and_meet<(kStages - 2) * kAllLoads>();
+                    if (s + kStages - 2 < whole) wait_and_meet<(kStages - 2) * kLoads>();
                     else wait_and_meet<0>();
                     if (s + kStages - 1 < whole) load(s + kStages - 1);
                     one_slice(lds + (s - from) % kStages * kStage);
@@ -348,30 +277,11 @@ struct Tile {
                 at[q] = s * kSlice + (((lane_id() & 7u) ^ turn(r)) << 4);
                 piece[q] = load_piece(t.first + (u64)row * t.stride, at[q], t.bytes);
             }
-            u32 scales[kScaled ? kScaleLoads : 1];
-            if constexpr (kScaled) {
-                const u32 blocks = (a.bytes + 15u) / 16u;
-#pragma unroll
-                for (int q = 0; q < kScaleLoads; ++q) {
-                    const TileRows &t = scales_of_a(q) ? a : b;
-                    const ScalePlace place = scale_place(q);
-                    const u32 block = s * kSliceBlocks + place.block;
-                    scales[q] = 0;
-#pragma unroll
-                    for (u32 c = 0; c < 4; ++c)
-                        if (block < blocks && place.row + c < t.rows)
-                            scales[q] |= (u32)t.scale[(u64)block * t.scale_stride + place.row + c] << (8 * c);
-                }
-            }
 #pragma unroll
             for (int q = 0; q < kLoads; ++q) piece[q] = cut_piece(piece[q], at[q], a.bytes);
             // (everybody has read the slice that lay in this stage, two or more slices ago, before the barrier of the last one)
 #pragma unroll
             for (int q = 0; q < kLoads; ++q) *(i32x4 *)(stage + stage_at(q) + lane_id() * 16u) = piece[q];
-            if constexpr (kScaled) {
-#pragma unroll
-                for (int q = 0; q < kScaleLoads; ++q) *(u32 *)(stage + kData + scales_at(q) + lane_id() * 4u) = scales[q];
-            }
             lds_barrier();
             one_slice(stage);
         }
@@ -387,22 +297,6 @@ struct Tile {
         for (int j = 0; j < kFragsN; ++j) f.b[j] = *(const i32x4 *)(stage_b + place(rb + 16 * j, piece));
 #pragma unroll
         for (int i = 0; i < kFragsM; ++i) f.a[i] = *(const i32x4 *)(stage_a + place(ra + 16 * i, piece));
-        if constexpr (kScaled) {
-            const unsigned char *scales = stage_b + kN * kSlice;
-#pragma unroll
-            for (int g = 0; g < GroupsN::kCount; ++g)
-                f.b_scale[g] = read_scales<GroupsN>(scales + kSliceBlocks * kM + piece * kN + col0(), g);
-#pragma unroll
-            for (int g = 0; g < GroupsM::kCount; ++g) f.a_scale[g] = read_scales<GroupsM>(scales + piece * kM + row0(), g);
-        }
-    }
-    // this lane's scales of a group of fragments, from the wavefront's first row of the block on
-    template <class G>
-    static __device__ __forceinline__ u32 read_scales(const unsigned char *p, int g)
-    {
-        const int i = G::start(g);
-        p += 16 * i + G::size(i) * (lane_id() & 15u);
-        return G::size(i) == 4 ? *(const u32 *)p : G::size(i) == 2 ? *(const u16 *)p : *p;
     }
 
     // one slice that lies in LDS, into the sums
@@ -416,36 +310,15 @@ struct Tile {
         rest(first, second);
     }
 
-    // (the instruction takes which byte of the scales' words it is as a constant)
-    template <int kI, int kJ>
-    __device__ __forceinline__ void add_scaled(const Half &a, const Half &b)
-    {
-#if defined(__HIP_DEVICE_COMPILE__)
-        const i32x4 x = b.b[kJ], y = a.a[kI];
-        sum[kI][kJ] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-            i32x8{x[0], x[1], x[2], x[3], 0, 0, 0, 0}, i32x8{y[0], y[1], y[2], y[3], 0, 0, 0, 0}, sum[kI][kJ], 4, 4, kJ - GroupsN::first(kJ),
-            (int)b.b_scale[GroupsN::place(kJ)], kI - GroupsM::first(kI), (int)a.a_scale[GroupsM::place(kI)]);
-#endif
-    }
-    template <int... kAt>
-    __device__ __forceinline__ void add_all(const Half &a, const Half &b, std::integer_sequence<int, kAt...>)
-    {
-        (add_scaled<kAt / kFragsN, kAt % kFragsN>(a, b), ...);
-    }
-
     __device__ __forceinline__ void add(const Half &a, const Half &b)
     {
-        if constexpr (kScaled) {
-            add_all(a, b, std::make_integer_sequence<int, kFragsM * kFragsN>());
-            return;
-        }
 #pragma unroll
         for (int i = 0; i < kFragsM; ++i)
 #pragma unroll
             for (int j = 0; j < kFragsN; ++j) {
                 if constexpr (kOf == kBytes)
                     sum[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b.b[j], a.a[i], sum[i][j], 0, 0, 0);
-                else if constexpr (!kScaled)
+                else
                     sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, b.b[j]),
                                                                        __builtin_bit_cast(f16x8, a.a[i]), sum[i][j], 0, 0, 0);
             }
@@ -482,7 +355,7 @@ struct Tile {
     template <int kOfLoads>
     __device__ __forceinline__ void mix() const
     {
-        constexpr int kReads = kFragsM + kFragsN + (kScaled ? GroupsM::kCount + GroupsN::kCount : 0), kPer = kFragsM * kFragsN / (kReads + kOfLoads), kProducts = kPer ? kPer : 1;
+        constexpr int kReads = kFragsM + kFragsN, kPer = kFragsM * kFragsN / (kReads + kOfLoads), kProducts = kPer ? kPer : 1;
 #pragma unroll
         for (int q = 0; q < kReads; ++q) {
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // a read from LDS
@@ -536,14 +409,17 @@ __device__ __forceinline__ float read_as(const void *p, u64 at, int type)
 // way together): a lane whose eight are not all there takes the row's last eight, and `numbers` moves them down; where the row
 // has no eight it takes zeros of the library's, and `numbers` reads what there is one by one.
 static __device__ const u32 kNothing[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+// (said to be global memory: of a pointer that may be either of the two the compiler does not know it, and its flat loads
+// are waited for all together)
+typedef const __attribute__((address_space(1))) unsigned char *GlobalBytes;
 
 template <int kType> struct Eight {
     i32x4 w[kType == 0 ? 2 : 1];
     static constexpr u32 kSize = kType == 0 ? 4u : 2u;
     __device__ __forceinline__ void load(const unsigned char *row, u32 c, u32 cols)
     {
-        const unsigned char *p = cols < 8u ? (const unsigned char *)kNothing : row + min(c, cols - 8u) * kSize;
-        __builtin_memcpy(w, p, sizeof w);
+        const GlobalBytes p = cols < 8u ? (GlobalBytes)kNothing : (GlobalBytes)(row + min(c, cols - 8u) * kSize);
+        __builtin_memcpy(w, (const void *)p, sizeof w);
     }
     __device__ __forceinline__ void numbers(float (&v)[8], const unsigned char *row, u32 c, u32 cols) const
     {

@@ -16,11 +16,9 @@
 
 #include "../../include/rtopk.h"
 #include "../../include/rtopk_diag.h"
-#include "rtopk_matrix.h"
+#include "rtopk_tile4.h"
 
 namespace rtopk {
-
-constexpr u32 kBlock = 32;                  // numbers that share a scale
 
 // ---------------------------------------------------------------------------
 // Quantisation.
@@ -187,8 +185,8 @@ template <int kType> struct Quad {
     static constexpr u32 kSize = kType == 0 ? 4u : 2u;
     __device__ __forceinline__ void load(const unsigned char *row, u32 c, u32 cols)
     {
-        const unsigned char *p = cols < 4u ? (const unsigned char *)kNothing : row + min(c, cols - 4u) * kSize;
-        __builtin_memcpy(w, p, sizeof w);
+        const GlobalBytes p = cols < 4u ? (GlobalBytes)kNothing : (GlobalBytes)(row + min(c, cols - 4u) * kSize);
+        __builtin_memcpy(w, (const void *)p, sizeof w);
     }
     __device__ __forceinline__ void numbers(float (&v)[4], const unsigned char *row, u32 c, u32 cols) const
     {
@@ -383,6 +381,80 @@ __device__ __forceinline__ f32x4 four_biases(const Product4 &g, u32 col)
     return v;
 }
 
+// Lanes l of the upper half of the wavefront give x and take y of the lanes l - 32; of the odd rows of 16 lanes, and the even ones.
+__device__ __forceinline__ void exchange_halves(u32 &x, u32 &y)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    const auto r = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+    x = r[0];
+    y = r[1];
+#endif
+}
+__device__ __forceinline__ void exchange_rows(u32 &x, u32 &y)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    const auto r = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+    x = r[0];
+    y = r[1];
+#endif
+}
+__device__ __forceinline__ void exchange_halves(f32x4 &x, f32x4 &y)
+{
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        u32 a = __float_as_uint(x[c]), b = __float_as_uint(y[c]);
+        exchange_halves(a, b);
+        x[c] = __uint_as_float(a);
+        y[c] = __uint_as_float(b);
+    }
+}
+__device__ __forceinline__ void exchange_rows(f32x4 &x, f32x4 &y)
+{
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        u32 a = __float_as_uint(x[c]), b = __float_as_uint(y[c]);
+        exchange_rows(a, b);
+        x[c] = __uint_as_float(a);
+        y[c] = __uint_as_float(b);
+    }
+}
+
+// The results of a row that lanes l % 16 have together (l / 16 = quarter q: columns 4 size q .. of the 16 size from `col` on), at
+// out + at. They change hands among the four lanes, so that each store is of 64 neighbouring bytes of the row; cols: of the
+// result, 0 where the row is not there.
+__device__ __forceinline__ void write_group(void *out, u64 at, int type, f32x4 (&v)[4], int size, u32 col, u32 cols)
+{
+    const u32 q = lane_id() >> 4, crossed = 2u * (q & 1u) + (q >> 1);
+    auto four = [&](u32 c, const f32x4 &x) {
+        if (c < cols) write_four(out, at + c, type, x, cols - c);
+    };
+    auto eight = [&](u32 c, const f32x4 &x, const f32x4 &y) {
+        if (c < cols) write_eight(out, at + c, type, x, y, cols - c);
+    };
+    if (size == 1) {
+        four(col + 4u * q, v[0]);
+    } else if (type == RTOPK_F32) {
+        exchange_halves(v[0], v[size / 2]);
+        if (size == 2) {
+            four(col + 4u * crossed, v[0]);
+            four(col + 16u + 4u * crossed, v[1]);
+        } else {
+            exchange_halves(v[1], v[3]);
+            exchange_rows(v[0], v[1]);
+            exchange_rows(v[2], v[3]);
+#pragma unroll
+            for (u32 w = 0; w < 4; ++w) four(col + 16u * w + 4u * q, v[w]);
+        }
+    } else if (size == 2) {
+        eight(col + 8u * q, v[0], v[1]);
+    } else {
+        exchange_halves(v[0], v[2]);
+        exchange_halves(v[1], v[3]);
+        eight(col + 8u * crossed, v[0], v[1]);
+        eight(col + 32u + 8u * crossed, v[2], v[3]);
+    }
+}
+
 // A tile, or a run of its contraction; the bias is added to the sums in registers, and the result written once.
 template <class T, bool kWhole>
 __global__ void __launch_bounds__(T::kThreads) k_product4(Product4 g)
@@ -393,42 +465,32 @@ __global__ void __launch_bounds__(T::kThreads) k_product4(Product4 g)
     u32 ti, tj;
     tile_at(place - split * rows * cols, rows, cols, ti, tj);
     const u32 i0 = ti * T::kRowsM, j0 = tj * T::kRowsN, bytes = (g.k + 1u) / 2u;
-    const TileRows a{g.a + i0 * g.lda, g.m - i0, (u32)g.lda, bytes, g.a_scale + i0, (u32)g.lda_scale};
-    const TileRows b{g.b + j0 * g.ldb, g.n - j0, (u32)g.ldb, bytes, g.b_scale + j0, (u32)g.ldb_scale};
-    const u32 slices = (bytes + kSlice - 1) / kSlice, from = split * g.slices_each;
+    const TileRows4 a{g.a + i0 * g.lda, g.m - i0, (u32)g.lda, g.a_scale + i0, (u32)g.lda_scale};
+    const TileRows4 b{g.b + j0 * g.ldb, g.n - j0, (u32)g.ldb, g.b_scale + j0, (u32)g.ldb_scale};
+    // (runs are counted in slices, of which a unit is a whole or a half)
+    constexpr u32 kPerSlice = kSlice / T::kRow;
+    const u32 units = (bytes + T::kRow - 1) / T::kRow, from = split * g.slices_each * kPerSlice;
     T t;
     t.clear();
-    t.template multiply<kWhole>(a, b, from, min(from + g.slices_each, slices), lds);
-    const u64 ld = align_up(g.n, 4);
-    float *part = g.part + (u64)split * g.m * ld;
-    // a lane's columns: 4 x size neighbours for each group of fragments
+    t.template multiply<kWhole>(a, b, bytes, from, min(from + g.slices_each * kPerSlice, units), lds);
+    const bool last = g.splits == 1;
+    const u64 ld = last ? g.ldo : align_up(g.n, 4);
+    void *out = last ? g.out : (void *)(g.part + (u64)split * g.m * ld);
+    const int type = last ? g.type : RTOPK_F32;
 #pragma unroll
     for (int group = 0; group < T::GroupsN::kCount; ++group) {
         const int first = T::GroupsN::start(group), size = T::GroupsN::size(first);
-        const u32 col = j0 + T::col0() + 16u * first + 4u * size * (lane_id() >> 4);
+        const u32 col = j0 + T::result_column(group), group_col = j0 + T::col0() + 16u * first;
         f32x4 bias[4];          // `size` of them
 #pragma unroll
-        for (int w = 0; w < size; ++w) bias[w] = g.splits == 1 ? four_biases(g, col + 4 * w) : f32x4{0, 0, 0, 0};
+        for (int w = 0; w < size; ++w) bias[w] = last ? four_biases(g, col + 4 * w) : f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < T::kFragsM; ++i) {
             const u32 row = i0 + T::row_at(i);
-            f32x4 v[4];
+            f32x4 v[4];         // 4 x size neighbours
 #pragma unroll
             for (int e = 0; e < 4 * size; ++e) v[e / 4][e % 4] = t.sum[i][first + e % size][e / size] + bias[e / 4][e % 4];
-            if (row >= g.m) continue;
-#pragma unroll
-            for (int w = 0; w < size; w += 2) {
-                const u32 c = col + 4u * w;
-                if (c >= g.n) continue;
-                if (g.splits > 1) {
-                    *(f32x4 *)(part + row * ld + c) = v[w];
-                    if (w + 1 < size && c + 4u < g.n) *(f32x4 *)(part + row * ld + c + 4) = v[w + 1 < size ? w + 1 : w];
-                } else if (w + 1 < size) {
-                    write_eight(g.out, row * g.ldo + c, g.type, v[w], v[w + 1 < size ? w + 1 : w], g.n - c);
-                } else {
-                    write_four(g.out, row * g.ldo + c, g.type, v[w], g.n - c);
-                }
-            }
+            write_group(out, row * ld, type, v, size, group_col, row < g.m ? g.n : 0u);
         }
     }
 }
@@ -452,7 +514,6 @@ __global__ void __launch_bounds__(256) k_product4_join(Product4 g)
 // the other operand, up to 16 of them. Neighbouring workgroups are on one XCD: they share the lines that the scales lie in.
 // ---------------------------------------------------------------------------
 constexpr u32 kFewTokens = 16;              // at most: what one instruction takes
-constexpr u32 kStepBytes = 64, kStepBlocks = 4;     // of a row, in one instruction
 constexpr u32 kInOne = 8192;                // numbers of x that a workgroup can quantise for itself (one launch less)
 
 struct Few4 {
@@ -650,8 +711,22 @@ struct Plan {
     u64 part_bytes;
 };
 
-// The tile and the number of runs of the contraction that cost least; a slice's 128 bytes of a row cost what 128 bytes of 8-bit
-// integers do. Runs cost a launch, and four bytes of every sum written and read.
+// What a launch of tiles costs, in microseconds: a launch, and for the tiles that one compute unit gets one after the other what
+// comes before and after their slices, and the slices (128 bytes of every row). Two tiles of 64 or 128 share a unit. From 300
+// launches over eighteen shapes of 64 to 16384 rows and columns and contractions of 256 to 20000: the tile and runs that this picks took at
+// most 1.02 times the best ones' time.
+double launch_cost(u32 edge, u64 tiles, double slices)
+{
+    const double each = (double)((tiles + kUnits - 1) / kUnits);
+    if (edge == 256) return 3.8 + each * (6.9 + slices * 1.63);
+    if (edge == 192) return 3.8 + each * (5.3 + slices * 0.97);
+    const double twos = (double)((u64)each / 2), one = each - 2 * twos;
+    if (edge == 128) return 3.8 + twos * (3.85 + slices * 0.94) + one * (1.93 + slices * 0.63);
+    return 3.8 + twos * (1.47 + slices * 0.48) + one * (0.74 + slices * 0.31);
+}
+
+// The tile and the number of runs of the contraction that cost least. Runs cost a launch, and four bytes of every sum written and read. Rows
+// that do not start on 128 bytes take two lines for every slice.
 Plan plan_product(u32 m, u32 n, u32 k, bool on_lines)
 {
     Plan best{};
@@ -663,8 +738,8 @@ Plan plan_product(u32 m, u32 n, u32 k, bool on_lines)
             const u32 each = std::max(1u, (slices + splits - 1) / splits);
             if (splits > 1 && (slices + each - 1) / each != splits) continue;
             if (tiles * splits >= kMostTiles && edge < 256) continue;
-            double cost = tiles_cost(kCostBytes, edge, tiles * splits, each * (on_lines ? 1.0 : 1.3));
-            if (splits > 1) cost += 3.0 + (double)m * n * splits * 8.0 / 6e6;
+            double cost = launch_cost(edge, tiles * splits, each * (on_lines ? 1.0 : 1.11));
+            if (splits > 1) cost += 2.2 + (double)m * n * splits * 8.0 / 5.5e6;
             if (best.edge && cost >= least) continue;
             least = cost;
             best = Plan{edge, (u32)tiles, each, std::max(1u, (slices + each - 1) / each), 0};
@@ -676,10 +751,10 @@ Plan plan_product(u32 m, u32 n, u32 k, bool on_lines)
 // what a product of these sizes may need for the runs' sums, however its rows lie
 u64 part_bytes(u32 m, u32 n, u32 k) { return std::max(plan_product(m, n, k, false).part_bytes, plan_product(m, n, k, true).part_bytes); }
 
-template <int kEdge, int kStages>
+template <int kEdge, int kSteps, int kStages>
 void launch_product4(const Product4 &g, const Plan &p, bool whole, hipStream_t stream)
 {
-    typedef Tile<kFours, kEdge, kEdge, 2, 4, kStages, true, kByScale> T;
+    typedef Tile4<kEdge, kEdge, 2, 4, kSteps, kStages> T;
     if (whole) k_product4<T, true><<<p.tiles * p.splits, T::kThreads, 0, stream>>>(g);
     else k_product4<T, false><<<p.tiles * p.splits, T::kThreads, 0, stream>>>(g);
 }
@@ -692,10 +767,10 @@ int run_product4(Product4 g, void *part, hipStream_t stream)
     g.part = (float *)part;
     const bool whole = (((uintptr_t)g.a | (uintptr_t)g.b | g.lda | g.ldb) & 15u) == 0 &&
                        (((uintptr_t)g.a_scale | (uintptr_t)g.b_scale | g.lda_scale | g.ldb_scale) & 3u) == 0;
-    if (p.edge == 256) launch_product4<256, 2>(g, p, whole, stream);
-    else if (p.edge == 192) launch_product4<192, 2>(g, p, whole, stream);
-    else if (p.edge == 128) launch_product4<128, 2>(g, p, whole, stream);
-    else launch_product4<64, 3>(g, p, whole, stream);
+    if (p.edge == 256) launch_product4<256, 2, 2>(g, p, whole, stream);
+    else if (p.edge == 192) launch_product4<192, 2, 2>(g, p, whole, stream);
+    else if (p.edge == 128) launch_product4<128, 2, 2>(g, p, whole, stream);
+    else launch_product4<64, 2, 4>(g, p, whole, stream);
     if (const int rc = launched()) return rc;
     if (p.splits > 1) {
         const u64 blocks = ((u64)g.m * ((g.n + 3) / 4) + 255) / 256;
