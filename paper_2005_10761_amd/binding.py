@@ -583,11 +583,17 @@ _ROUNDING = {"nearest": 0, "drawn": 1}
 _64_BITS = 2**64 - 1
 
 
-def _here(t: torch.Tensor, name: str, *others: Optional[torch.Tensor]) -> None:
-    """Refuses tensors of another device than the current one, whose stream the kernels go to."""
-    here = torch.cuda.current_device()
-    if t.get_device() != here or any(o is not None and o.get_device() != here for o in others):
-        raise ValueError(f"{name} and all that goes with it must be on the current device")
+# the current device's number without the checks around it, where torch has it
+_CURRENT_DEVICE = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _stream_of(stream, name: str, *tensors: Optional[torch.Tensor]) -> Optional[int]:
+    """The handle of the stream that a call's kernels go to; refuses tensors of another device than the current one."""
+    here = _CURRENT_DEVICE()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"{name} and all that goes with it must be on the current device")
+    return _stream_handle(stream) if stream is not None or _RAW_STREAM is None else _RAW_STREAM(here) or None
 
 
 def _packed(q: torch.Tensor, scale: torch.Tensor, rows: int, k: Optional[int], name: str):
@@ -623,9 +629,9 @@ def quantize_mx4(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, along: s
     rows, cols = x.size()
     ldq, lds = _packed(q, scale, *((rows, cols) if along == "rows" else (cols, rows)), "q")
     rounding, seed, step, at = _drawn(seed, held := step)
-    _here(x, "x", q, scale, held if at else None)
+    handle = _stream_of(stream, "x", x, q, scale, held if at else None)
     rc = load_library().rtopk_quantize_mx4(x.data_ptr(), _TYPES[x.dtype], rows, cols, ldx, _ALONG[along], rounding, seed, step, at,
-                                           q.data_ptr(), ldq, scale.data_ptr(), lds, _stream_handle(stream))
+                                           q.data_ptr(), ldq, scale.data_ptr(), lds, handle)
     if rc:
         raise RtopkError(rc, "rtopk_quantize_mx4")
 
@@ -635,9 +641,9 @@ def dequantize_mx4(q: torch.Tensor, scale: torch.Tensor, out: torch.Tensor, stre
     ldo = _matrix(out, "out", _TYPES)
     rows, cols = out.size()
     ldq, lds = _packed(q, scale, rows, cols, "q")
-    _here(out, "out", q, scale)
+    handle = _stream_of(stream, "out", out, q, scale)
     rc = load_library().rtopk_dequantize_mx4(q.data_ptr(), rows, cols, ldq, scale.data_ptr(), lds, out.data_ptr(), _TYPES[out.dtype], ldo,
-                                             _stream_handle(stream))
+                                             handle)
     if rc:
         raise RtopkError(rc, "rtopk_dequantize_mx4")
 
@@ -659,12 +665,12 @@ def matmul_mx4(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale:
     k = 2 * a.size(1)                       # (the last half byte of an odd length is 0)
     if bias is not None:
         _vector(bias, n, "bias")
-    _here(out, "out", a, a_scale, b, b_scale, bias, workspace)
+    handle = _stream_of(stream, "out", out, a, a_scale, b, b_scale, bias, workspace)
     need = 0 if workspace is not None else matmul_mx4_workspace_bytes(m, n, k)
     ws, ws_bytes, held = _workspace(workspace, need, out.device, stream)
     rc = load_library().rtopk_matmul_mx4(a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), _ptr(bias), m, n, k, lda,
                                          lda_scale, ldb, ldb_scale, out.data_ptr(), _TYPES[out.dtype], ldo, ws, ws_bytes,
-                                         _stream_handle(stream))
+                                         handle)
     if rc:
         raise RtopkError(rc, "rtopk_matmul_mx4")
 
@@ -685,11 +691,11 @@ def linear_mx4(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, out: tor
         raise ValueError("x is [m, k], out [m, n]")
     if bias is not None:
         _vector(bias, n, "bias")
-    _here(x, "x", w, w_scale, out, bias, workspace)
+    handle = _stream_of(stream, "x", x, w, w_scale, out, bias, workspace)
     need = 0 if workspace is not None else linear_mx4_workspace_bytes(m, k, n)
     ws, ws_bytes, held = _workspace(workspace, need, x.device, stream)
     rc = load_library().rtopk_linear_mx4(x.data_ptr(), _TYPES[x.dtype], m, k, ldx, w.data_ptr(), w_scale.data_ptr(), n, ldw, ldw_scale,
-                                         _ptr(bias), out.data_ptr(), _TYPES[out.dtype], ldo, ws, ws_bytes, _stream_handle(stream))
+                                         _ptr(bias), out.data_ptr(), _TYPES[out.dtype], ldo, ws, ws_bytes, handle)
     if rc:
         raise RtopkError(rc, "rtopk_linear_mx4")
 
@@ -730,13 +736,13 @@ def linear_mx4_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w_turned: O
         _vector(db, n, "db")
     rounding, seed, step, at = _drawn(seed, held := step)
     asked = (x if dw is not None else None, dw, db, workspace, held if at else None)
-    _here(dy, "dy", *asked, *((dx, w_turned, w_turned_scale) if dx is not None else ()))
+    handle = _stream_of(stream, "dy", dy, *asked, *((dx, w_turned, w_turned_scale) if dx is not None else ()))
     ws, ws_bytes, room = _workspace(workspace, 0 if workspace is not None else linear_mx4_backward_workspace_bytes(m, k, n),
                                     dy.device, stream)
     ld = lambda t: 0 if t is None else _ld(t)   # noqa: E731
     rc = load_library().rtopk_linear_mx4_backward(
         _ptr(dy), _ptr(x), _TYPES[dy.dtype], m, k, n, _ld(dy), ld(x), _ptr(w_turned), _ptr(w_turned_scale), ldw, ldw_scale,
-        rounding, seed, step, at, _ptr(dx), ld(dx), _ptr(dw), ld(dw), _ptr(db), ws, ws_bytes, _stream_handle(stream))
+        rounding, seed, step, at, _ptr(dx), ld(dx), _ptr(dw), ld(dw), _ptr(db), ws, ws_bytes, handle)
     if rc:
         raise RtopkError(rc, "rtopk_linear_mx4_backward")
 
@@ -755,9 +761,9 @@ def layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[to
     for t, length, name in ((gamma, cols, "gamma"), (beta, cols, "beta"), (mean, rows, "mean"), (rstd, rows, "rstd")):
         if t is not None:
             _vector(t, length, name)
-    _here(x, "x", gamma, beta, out, mean, rstd)
+    handle = _stream_of(stream, "x", x, gamma, beta, out, mean, rstd)
     rc = load_library().rtopk_layer_norm(x.data_ptr(), _TYPES[x.dtype], rows, cols, ldx, _ptr(gamma), _ptr(beta), eps, out.data_ptr(),
-                                         _TYPES[out.dtype], ldo, _ptr(mean), _ptr(rstd), _stream_handle(stream))
+                                         _TYPES[out.dtype], ldo, _ptr(mean), _ptr(rstd), handle)
     if rc:
         raise RtopkError(rc, "rtopk_layer_norm")
 
@@ -786,13 +792,13 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
                             (dbeta, cols, "dbeta")):
         if t is not None:
             _vector(t, length, name)
-    _here(x, "x", dy, mean, rstd, gamma, add, dx, dgamma, dbeta, workspace)
+    handle = _stream_of(stream, "x", x, dy, mean, rstd, gamma, add, dx, dgamma, dbeta, workspace)
     sums = dgamma is not None or dbeta is not None
     need = layer_norm_backward_workspace_bytes(rows, cols) if sums and workspace is None else 0
     ws, ws_bytes, held = _workspace(workspace, need, x.device, stream)
     rc = load_library().rtopk_layer_norm_backward(
         dy.data_ptr(), _TYPES[dy.dtype], x.data_ptr(), _TYPES[x.dtype], rows, cols, lddy, ldx, mean.data_ptr(), rstd.data_ptr(),
-        _ptr(gamma), _ptr(add), ldadd, _ptr(dx), lddx, _ptr(dgamma), _ptr(dbeta), ws, ws_bytes, _stream_handle(stream))
+        _ptr(gamma), _ptr(add), ldadd, _ptr(dx), lddx, _ptr(dgamma), _ptr(dbeta), ws, ws_bytes, handle)
     if rc:
         raise RtopkError(rc, "rtopk_layer_norm_backward")
 
@@ -811,9 +817,9 @@ def dropout(x: torch.Tensor, out: torch.Tensor, p: float, seed: int, step, resid
     if seed is None:
         raise TypeError("dropout needs a seed")
     _, seed, step, at = _drawn(seed, held := step)
-    _here(x, "x", out, residual, held if at else None)
+    handle = _stream_of(stream, "x", x, out, residual, held if at else None)
     rc = load_library().rtopk_dropout(x.data_ptr(), _TYPES[x.dtype], rows, cols, ldx, _ptr(residual), ldr, out.data_ptr(),
-                                      _TYPES[out.dtype], ldo, p, seed, step, at, _stream_handle(stream))
+                                      _TYPES[out.dtype], ldo, p, seed, step, at, handle)
     if rc:
         raise RtopkError(rc, "rtopk_dropout")
 

@@ -142,6 +142,24 @@ def test_blocks_without_numbers_and_at_the_ends_of_the_range():
     assert np.array_equal(got[3], bias.astype(np.float64)) and np.array_equal(got[7], bias.astype(np.float64))
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_every_16_bit_number(kind):
+    """All of them but infinities and not-a-numbers, each by itself in a block with 1.5 2^e, and in blocks that a subnormal leads."""
+    every = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(TYPES[kind])
+    every = every[torch.isfinite(every)]
+    for lead in (1.5, 6.0, 2.0 ** -10, 2.0 ** -24):
+        few = every[every.abs().double() <= lead]
+        x = few[torch.randperm(len(few), generator=torch.Generator().manual_seed(1))]
+        x = torch.nn.functional.pad(x, (0, -len(x) % 31)).view(-1, 31)
+        x = torch.cat([torch.full((len(x), 1), lead, dtype=TYPES[kind]), x], 1).to(DEV)
+        for along, given in (("rows", x), ("columns", x.T.contiguous())):
+            for seed in (None, 1, 2):
+                want_q, want_s = fb.quantized(host(given), along, seed, 5)
+                q, s, _ = room_for(*want_q.shape)
+                rt.quantize_mx4(given, q, s, along=along, seed=seed, step=5)
+                assert np.array_equal(host(s), want_s) and np.array_equal(host(q), fb.packed(want_q)), (lead, along, seed)
+
+
 def test_drawn_rounding_keeps_the_mean():
     x = torch.linspace(-6, 6, 64, device=DEV).repeat(64, 1)
     q, s, _ = room_for(64, 64)
