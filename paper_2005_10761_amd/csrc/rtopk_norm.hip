@@ -184,21 +184,98 @@ struct NormBack {
     const float *mean, *rstd, *gamma;
     void *dx;                       // of x's type, or null
     u64 lddx;
+    u32 groups;                     // workgroups that share the rows
     u32 runs, run;                  // the sums over rows: runs of so many rows
     float *dgamma, *dbeta;          // or null
     float *part;                    // [2][runs][cols]
 };
 
+// All of the sums of 32 columns by one workgroup of kThreads: four lanes have eight columns each, and every kThreads / 4th row. For
+// small matrices: neither runs of rows to be joined nor a launch for them.
+constexpr u32 kDirectColumns = 32, kDirectLanes = kDirectColumns / 8;
+
+template <int kType, int kDyType, u32 kThreads>
+__device__ __forceinline__ void sum_columns(const NormBack &g, u32 strip)
+{
+    constexpr u32 kWaves = kThreads / kWave, kLanes = kThreads / kDirectLanes, kAtOnce = 4;
+    __shared__ __align__(16) float part[2][kWaves][kDirectColumns];
+    const u32 lane = lane_id(), wave = threadIdx.x / kWave, c = strip * kDirectColumns + 8u * (threadIdx.x % kDirectLanes);
+    float dgamma[8] = {0, 0, 0, 0, 0, 0, 0, 0}, dbeta[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (u32 r = threadIdx.x / kDirectLanes; r < g.rows; r += kAtOnce * kLanes) {
+        Eight<kType> ex[kAtOnce];
+        Eight<kDyType> ey[kAtOnce];
+        float mean[kAtOnce], rstd[kAtOnce];
+#pragma unroll
+        for (u32 q = 0; q < kAtOnce; ++q) {
+            const u64 row = min(r + q * kLanes, g.rows - 1u);
+            ex[q].load((const unsigned char *)g.x + row * g.ldx * Eight<kType>::kSize, c, g.cols);
+            ey[q].load((const unsigned char *)g.dy + row * g.lddy * Eight<kDyType>::kSize, c, g.cols);
+            mean[q] = g.mean[row];
+            rstd[q] = g.rstd[row];
+        }
+#pragma unroll
+        for (u32 q = 0; q < kAtOnce; ++q) {
+            const u64 row = r + q * kLanes;
+            if (row >= g.rows) break;
+            float x[8], d[8];
+            ex[q].numbers(x, (const unsigned char *)g.x + row * g.ldx * Eight<kType>::kSize, c, g.cols);
+            ey[q].numbers(d, (const unsigned char *)g.dy + row * g.lddy * Eight<kDyType>::kSize, c, g.cols);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                dgamma[i] = fmaf(d[i], (x[i] - mean[q]) * rstd[q], dgamma[i]);
+                dbeta[i] += d[i];
+            }
+        }
+    }
+#pragma unroll
+    for (int o = kDirectLanes; o < kWave; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            dgamma[i] += __shfl_xor(dgamma[i], o, kWave);
+            dbeta[i] += __shfl_xor(dbeta[i], o, kWave);
+        }
+    if (lane < kDirectLanes) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            part[0][wave][8 * lane + i] = dgamma[i];
+            part[1][wave][8 * lane + i] = dbeta[i];
+        }
+    }
+    __syncthreads();
+    const u32 which = threadIdx.x / kDirectColumns, col = threadIdx.x % kDirectColumns, at = strip * kDirectColumns + col;
+    float *out = which ? g.dbeta : g.dgamma;
+    if (which > 1 || at >= g.cols || !out) return;
+    float sum = 0;
+#pragma unroll
+    for (u32 w = 0; w < kWaves; ++w) sum += part[which][w][col];
+    out[at] = sum;
+}
+
+template <int kType, int kDyType>
+__global__ void __launch_bounds__(kNormThreads) k_norm_back_sums(NormBack g)
+{
+    sum_columns<kType, kDyType, kNormThreads>(g, blockIdx.x);
+}
+
 // Rows by workgroups that keep going: kWavesPerRow wavefronts hold a row in registers, kPieces pieces of eight numbers a
-// lane, the next row's x and dy on their way while this one's means are taken and its dx is written; a lane's share of
-// dgamma and dbeta stays in registers over all of its rows (kSums). One read of everything, one write.
-template <int kType, int kDyType, int kWavesPerRow, int kPieces, bool kSums>
+// lane, the next row's x and dy on their way while this one's means are taken and its dx is written. One read of everything,
+// one write: a lane's share of dgamma and dbeta stays in registers over all of its rows (kHeld), and the workgroups' are joined afterwards.
+// kBeside: other workgroups of the launch, from g.groups on, take the sums by themselves.
+enum SumsBy { kNone, kHeld, kBeside };
+
+template <int kType, int kDyType, int kWavesPerRow, int kPieces, SumsBy kSums>
 __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNormThreads) k_norm_back(NormBack g)
 {
+    if constexpr (kSums == kBeside) {
+        if (blockIdx.x >= g.groups) {
+            sum_columns<kType, kDyType, (kWavesPerRow > 4 ? kWavesPerRow * kWave : kNormThreads)>(g, blockIdx.x - g.groups);
+            return;
+        }
+    }
     constexpr u32 kWaves = kWavesPerRow > 4 ? kWavesPerRow : 4, kRows = kWaves / kWavesPerRow, kStep = 8u * kWave * kWavesPerRow;
     __shared__ float means[2][2][kWaves];
     const u32 lane = lane_id(), wave = threadIdx.x / kWave, c0 = (wave % kWavesPerRow * kWave + lane) * 8u;
-    const u32 step = gridDim.x * kRows;
+    const u32 step = g.groups * kRows;
     const float per_row = 1.0f / (float)g.cols;
     float gamma[kPieces][8], dgamma[kPieces][8], dbeta[kPieces][8];
 #pragma unroll
@@ -241,7 +318,7 @@ __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNor
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 h[p][i] = c + i < g.cols ? (h[p][i] - mean) * rstd : 0.0f;      // (d is zero there)
-                if (kSums) {
+                if (kSums == kHeld) {
                     dgamma[p][i] = fmaf(d[p][i], h[p][i], dgamma[p][i]);
                     dbeta[p][i] += d[p][i];
                 }
@@ -280,7 +357,7 @@ __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNor
             write_eight(g.dx, r * g.lddx + c, kType, v[0], v[1], g.cols - c);
         }
     }
-    if constexpr (kSums) {
+    if constexpr (kSums == kHeld) {
         float *out = g.part + (u64)blockIdx.x * g.cols;
         const u64 beta = (u64)g.runs * g.cols;
         if constexpr (kRows > 1) {
@@ -506,10 +583,13 @@ u32 run_rows(u32 rows, u32 cols)
 }
 u32 run_count(u32 rows, u32 cols) { return (rows + run_rows(rows, cols) - 1) / run_rows(rows, cols); }
 
-template <int kType, int kDyType, bool kSums>
+// Small matrices: their sums cost less than a launch that joins them (the second read comes from the caches).
+bool small(u64 rows, u64 cols) { return rows <= 2048 && rows * cols <= 1u << 21; }
+
+template <int kType, int kDyType, SumsBy kSums>
 int launch_held(const NormBack &g, hipStream_t stream)
 {
-    const u32 cols = g.cols, grid = held_groups(g.rows, g.cols, 2);
+    const u32 cols = g.cols, grid = g.groups + (kSums == kBeside ? (cols + kDirectColumns - 1) / kDirectColumns : 0u);
     if (cols <= 512) k_norm_back<kType, kDyType, 1, 1, kSums><<<grid, kNormThreads, 0, stream>>>(g);
     else if (cols <= 1024) k_norm_back<kType, kDyType, 1, 2, kSums><<<grid, kNormThreads, 0, stream>>>(g);
     else if (cols <= 2048) k_norm_back<kType, kDyType, 4, 1, kSums><<<grid, kNormThreads, 0, stream>>>(g);
@@ -528,21 +608,28 @@ int join_sums(const NormBack &g, hipStream_t stream)
 template <int kType, int kDyType>
 int launch_back(NormBack g, hipStream_t stream)
 {
-    const bool sums = g.dgamma || g.dbeta;
-    if (g.dx && g.cols <= kHeldColumns) {
-        g.runs = held_groups(g.rows, g.cols, 2);
-        if (!sums) return launch_held<kType, kDyType, false>(g, stream);
-        if (const int rc = launch_held<kType, kDyType, true>(g, stream)) return rc;
+    const bool held = g.dx && g.cols <= kHeldColumns, direct = small(g.rows, g.cols);
+    bool sums = g.dgamma || g.dbeta;
+    g.groups = held_groups(g.rows, g.cols, 2);
+    if (held && sums && direct && g.dx != g.x && g.dx != g.dy) return launch_held<kType, kDyType, kBeside>(g, stream);
+    if (held && sums && !direct) {
+        g.runs = g.groups;
+        if (const int rc = launch_held<kType, kDyType, kHeld>(g, stream)) return rc;
         return join_sums(g, stream);
     }
-    if (sums) {
+    // the sums first: dx may be x or dy
+    if (sums && direct) {
+        k_norm_back_sums<kType, kDyType><<<(g.cols + kDirectColumns - 1) / kDirectColumns, kNormThreads, 0, stream>>>(g);
+        if (const int rc = launched()) return rc;
+    } else if (sums) {
         g.run = run_rows(g.rows, g.cols);
         g.runs = run_count(g.rows, g.cols);
         k_norm_back_columns<kType, kDyType><<<dim3((g.cols + kSumColumns - 1) / kSumColumns, g.runs), kNormThreads, 0, stream>>>(g);
         if (const int rc = launched()) return rc;
         if (const int rc = join_sums(g, stream)) return rc;
     }
-    if (g.dx) k_norm_back_row<kType, kDyType><<<row_grid(g.rows), 1024, 0, stream>>>(g);     // (last: dx may be x or dy)
+    if (held) return launch_held<kType, kDyType, kNone>(g, stream);
+    if (g.dx) k_norm_back_row<kType, kDyType><<<row_grid(g.rows), 1024, 0, stream>>>(g);
     return launched();
 }
 
@@ -573,7 +660,7 @@ extern "C" int rtopk_layer_norm_backward_workspace_bytes(uint64_t rows, uint64_t
 {
     if (!bytes || rows > kMostSize || !size_ok(cols)) return RTOPK_EINVAL;
     *bytes = 0;
-    if (rows) {
+    if (!small(rows, cols)) {
         const u32 runs = run_count((u32)rows, (u32)cols), held = cols <= kHeldColumns ? held_groups((u32)rows, (u32)cols, 2) : 0;
         *bytes = align_up(8ull * std::max(runs, held) * cols, 256);
     }
@@ -606,7 +693,7 @@ extern "C" int rtopk_layer_norm_backward(const void *dy, int dy_type, const void
         }
         return RTOPK_OK;
     }
-    const NormBack g{dy, x, add, lddy, ldx, ldadd, (u32)rows, (u32)cols, mean, rstd, gamma, dx, lddx, 0, 0,
+    const NormBack g{dy, x, add, lddy, ldx, ldadd, (u32)rows, (u32)cols, mean, rstd, gamma, dx, lddx, 0, 0, 0,
                      dgamma, dbeta, (float *)workspace};
     return type == RTOPK_F32 ? launch_back<RTOPK_F32>(g, dy_type, stream)
            : type == RTOPK_BF16 ? launch_back<RTOPK_BF16>(g, dy_type, stream) : launch_back<RTOPK_F16>(g, dy_type, stream);

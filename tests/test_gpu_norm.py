@@ -59,7 +59,8 @@ def backward(dy, x, mean, rstd, gamma, add):
 
 SIZES = [(1, 1, 0, 0), (3, 2, 1, 1), (1, 1500, 0, 0), (5, 7, 0, 0), (4, 8, 3, 1), (1030, 40, 0, 0), (1100, 513, 2, 1), (1200, 1024, 0, 0),
          (33, 1025, 0, 0), (700, 1500, 0, 0), (9, 2047, 1, 0), (17, 4096, 8, 0), (6, 4099, 0, 0), (40, 8192, 0, 0), (5, 8200, 0, 0),
-         (3, 16384, 0, 0), (4, 16385, 1, 1), (2, 50_001, 0, 0), (300, 96, 4, 2), (2500, 3, 0, 0), (5000, 260, 0, 0)]
+         (3, 16384, 0, 0), (4, 16385, 1, 1), (2, 50_001, 0, 0), (300, 96, 4, 2), (2500, 3, 0, 0), (5000, 260, 0, 0), (2048, 1024, 0, 0),
+         (2049, 700, 1, 0), (1300, 2000, 0, 0), (600, 4000, 0, 0), (300, 8000, 0, 0), (150, 16_000, 0, 0), (130, 17_000, 0, 0)]
 
 
 def rows_of(rng, rows, cols):
@@ -117,7 +118,7 @@ def test_forward_and_backward(kind, out_kind, rows, cols, pad, offset):
     assert torch.equal(again[0], dgamma) and torch.equal(again[1], dbeta)
 
 
-@pytest.mark.parametrize("rows, cols", [(7, 5), (50, 1500), (1500, 200), (4, 20_000)])
+@pytest.mark.parametrize("rows, cols", [(7, 5), (50, 1500), (1500, 200), (4, 20_000), (3000, 1000), (2500, 3000), (130, 17_000)])
 def test_in_place(rows, cols):
     rng = np.random.default_rng(rows)
     x = torch.as_tensor(rows_of(rng, rows, cols), device=DEV).to(torch.bfloat16)

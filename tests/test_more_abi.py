@@ -29,7 +29,8 @@ def test_workspace_sizes_and_their_domains():
     assert rt.linear_mx4_workspace_bytes(300, 130, 5) >= 300 * 65 + 300 * 5
     assert rt.linear_mx4_backward_workspace_bytes(0, 5, 5) == 0
     assert rt.linear_mx4_backward_workspace_bytes(100, 64, 96) >= (100 * 96 + 96 * 100 + 64 * 100) // 2
-    assert rt.layer_norm_backward_workspace_bytes(0, 5) == 0 and rt.layer_norm_backward_workspace_bytes(1, 5) >= 40
+    assert rt.layer_norm_backward_workspace_bytes(0, 5) == 0 and rt.layer_norm_backward_workspace_bytes(2048, 1024) == 0
+    assert rt.layer_norm_backward_workspace_bytes(3000, 5) >= 40
     for call in (lambda: rt.matmul_mx4_workspace_bytes(4, 4, MOST + 1), lambda: rt.matmul_mx4_workspace_bytes(MOST + 1, 4, 4),
                  lambda: rt.linear_mx4_workspace_bytes(4, 0, 4), lambda: rt.linear_mx4_workspace_bytes(4, 4, 0),
                  lambda: rt.linear_mx4_backward_workspace_bytes(4, 4, MOST + 1), lambda: rt.layer_norm_backward_workspace_bytes(4, 0),
@@ -96,7 +97,8 @@ def test_norm_refusals():
                 dict(cols=0), dict(rows=MOST + 1), dict(dx=FAKE, dy=FAKE2, lddx=41), dict(dx=FAKE, x=FAKE2), dict(dx=FAKE, add=FAKE, x=FAKE2,
                                                                                                                   dy=FAKE2, ldadd=44)):
         assert bw(**bad) == -1, bad
-    assert bw(ws=None) == -2 and bw(bytes=8) == -2 and bw(ws=ctypes.c_void_p(0x1010)) == -2
+    large = dict(rows=4000)
+    assert bw(**large, ws=None) == -2 and bw(**large, bytes=8) == -2 and bw(**large, ws=ctypes.c_void_p(0x1010)) == -2
 
 
 def test_dropout_refusals():
