@@ -583,29 +583,47 @@ _ROUNDING = {"nearest": 0, "drawn": 1}
 _64_BITS = 2**64 - 1
 
 
-# the current device's number without the checks around it, where torch has it
-_CURRENT_DEVICE = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+# the current device's number without the checks around it, where torch has it (without a GPU, one that no tensor is on)
+_CURRENT_DEVICE = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device) if torch.cuda.device_count() else lambda: -2
+_F32 = torch.float32
 
 
-def _stream_of(stream, name: str, *tensors: Optional[torch.Tensor]) -> Optional[int]:
-    """The handle of the stream that a call's kernels go to; refuses tensors of another device than the current one."""
-    here = _CURRENT_DEVICE()
-    for t in tensors:
-        if t is not None and t.get_device() != here:
-            raise ValueError(f"{name} and all that goes with it must be on the current device")
+def _rows(t: torch.Tensor, name: str, types, here: int) -> int:
+    """:func:`_matrix` of a matrix that also has to be on the device ``here``, the current one, whose stream the kernels go to."""
+    (rows, cols), (ld, one) = (t.shape, t.stride()) if t.dim() == 2 else ((0, 0), (0, 0))
+    if t.get_device() != here or t.dtype not in types or t.dim() != 2 or rows < 2 or cols < 2 or one != 1 or ld < cols:
+        ld = _matrix(t, name, types)            # (what is rare: refused there, or a row or column)
+        _at(t, name, here)
+    return ld
+
+
+def _floats(t: torch.Tensor, length: int, name: str, here: int) -> None:
+    """:func:`_vector` of a vector on the device ``here``."""
+    if t.get_device() != here or t.dtype is not _F32 or t.numel() != length or not t.is_contiguous():
+        _vector(t, length, name)
+        _at(t, name, here)
+
+
+def _at(t: Optional[torch.Tensor], name: str, here: int) -> None:
+    if t is not None and t.get_device() != here:
+        raise ValueError(f"{name} must be on the current device, as all that goes with it")
+
+
+def _stream_on(stream, here: int) -> Optional[int]:
+    """:func:`_stream_handle`, with the current device known."""
     return _stream_handle(stream) if stream is not None or _RAW_STREAM is None else _RAW_STREAM(here) or None
 
 
-def _packed(q: torch.Tensor, scale: torch.Tensor, rows: int, k: Optional[int], name: str):
+def _packed(q: torch.Tensor, scale: torch.Tensor, rows: int, k: Optional[int], name: str, here: int):
     """Distances (rows of bytes, blocks of scales) of a quantised matrix of ``rows`` rows, of k numbers if given."""
-    ldq, lds = _matrix(q, name, _FOUR_BITS), _matrix(scale, name + "'s scales", _FOUR_BITS)
+    ldq, lds = _rows(q, name, _FOUR_BITS, here), _rows(scale, name, _FOUR_BITS, here)
     have = q.size(1)
     if q.size(0) != rows or (k is not None and have != (k + 1) // 2) or scale.size() != ((have + 15) // 16, rows):
         raise ValueError(f"{name} must hold two numbers a byte, [rows, (k + 1) // 2], its scales [(k + 31) // 32, rows]")
     return ldq, lds
 
 
-def _drawn(seed: Optional[int], step):
+def _drawn(seed: Optional[int], step, here: int):
     """(rounding, seed, step, the device's step or None) of a seed that may be None and a step that may be a tensor."""
     if seed is None:
         return 0, 0, 0, None
@@ -613,6 +631,7 @@ def _drawn(seed: Optional[int], step):
         _need(step, torch.int64, "step")
         if step.numel() != 1:
             raise ValueError("step on the device is one int64")
+        _at(step, "step", here)
         return 1, seed & _64_BITS, 0, step.data_ptr()
     return 1, seed & _64_BITS, step & _64_BITS, None
 
@@ -625,25 +644,25 @@ def quantize_mx4(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, along: s
     numbers go up or down by chance, so that their mean is kept; ``step`` is an int, or one int64 on the GPU that is read when
     the kernel runs. Give ``q`` rows that start on 16 bytes and ``scale`` rows that start on 4 where the product is to
     read them fast."""
-    ldx = _matrix(x, "x", _TYPES)
-    rows, cols = x.size()
-    ldq, lds = _packed(q, scale, *((rows, cols) if along == "rows" else (cols, rows)), "q")
-    rounding, seed, step, at = _drawn(seed, held := step)
-    handle = _stream_of(stream, "x", x, q, scale, held if at else None)
+    here = _CURRENT_DEVICE()
+    ldx = _rows(x, "x", _TYPES, here)
+    rows, cols = x.shape
+    ldq, lds = _packed(q, scale, *((rows, cols) if along == "rows" else (cols, rows)), "q", here)
+    rounding, seed, step, at = _drawn(seed, step, here)
     rc = load_library().rtopk_quantize_mx4(x.data_ptr(), _TYPES[x.dtype], rows, cols, ldx, _ALONG[along], rounding, seed, step, at,
-                                           q.data_ptr(), ldq, scale.data_ptr(), lds, handle)
+                                           q.data_ptr(), ldq, scale.data_ptr(), lds, _stream_on(stream, here))
     if rc:
         raise RtopkError(rc, "rtopk_quantize_mx4")
 
 
 def dequantize_mx4(q: torch.Tensor, scale: torch.Tensor, out: torch.Tensor, stream=None) -> None:
     """rtopk_dequantize_mx4: the numbers of a matrix that :func:`quantize_mx4` left, ``out`` of ``q``'s rows."""
-    ldo = _matrix(out, "out", _TYPES)
-    rows, cols = out.size()
-    ldq, lds = _packed(q, scale, rows, cols, "q")
-    handle = _stream_of(stream, "out", out, q, scale)
+    here = _CURRENT_DEVICE()
+    ldo = _rows(out, "out", _TYPES, here)
+    rows, cols = out.shape
+    ldq, lds = _packed(q, scale, rows, cols, "q", here)
     rc = load_library().rtopk_dequantize_mx4(q.data_ptr(), rows, cols, ldq, scale.data_ptr(), lds, out.data_ptr(), _TYPES[out.dtype], ldo,
-                                             handle)
+                                             _stream_on(stream, here))
     if rc:
         raise RtopkError(rc, "rtopk_dequantize_mx4")
 
@@ -656,21 +675,22 @@ def matmul_mx4_workspace_bytes(m: int, n: int, k: int) -> int:
 def matmul_mx4(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor, out: torch.Tensor,
                bias: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """rtopk_matmul_mx4: out = a b^T (+ bias) of two quantised matrices of equal rows, out [a's rows, b's rows]."""
-    ldo = _matrix(out, "out", _TYPES)
-    m, n = out.size()
-    lda, lda_scale = _packed(a, a_scale, m, None, "a")
-    ldb, ldb_scale = _packed(b, b_scale, n, None, "b")
+    here = _CURRENT_DEVICE()
+    ldo = _rows(out, "out", _TYPES, here)
+    m, n = out.shape
+    lda, lda_scale = _packed(a, a_scale, m, None, "a", here)
+    ldb, ldb_scale = _packed(b, b_scale, n, None, "b", here)
     if a.size(1) != b.size(1):
         raise ValueError("a and b must have rows of equal length")
     k = 2 * a.size(1)                       # (the last half byte of an odd length is 0)
     if bias is not None:
-        _vector(bias, n, "bias")
-    handle = _stream_of(stream, "out", out, a, a_scale, b, b_scale, bias, workspace)
+        _floats(bias, n, "bias", here)
+    _at(workspace, "workspace", here)
     need = 0 if workspace is not None else matmul_mx4_workspace_bytes(m, n, k)
     ws, ws_bytes, held = _workspace(workspace, need, out.device, stream)
     rc = load_library().rtopk_matmul_mx4(a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), _ptr(bias), m, n, k, lda,
                                          lda_scale, ldb, ldb_scale, out.data_ptr(), _TYPES[out.dtype], ldo, ws, ws_bytes,
-                                         handle)
+                                         _stream_on(stream, here))
     if rc:
         raise RtopkError(rc, "rtopk_matmul_mx4")
 
@@ -684,18 +704,19 @@ def linear_mx4(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, out: tor
                workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """rtopk_linear_mx4: out = x w^T + bias, ``x`` [m, k] quantised along rows on the way, ``w`` [n, (k + 1) // 2] with
     ``w_scale`` [(k + 31) // 32, n] as :func:`quantize_mx4` leaves them."""
-    ldx, ldo = _matrix(x, "x", _TYPES), _matrix(out, "out", _TYPES)
-    (m, k), n = x.size(), out.size(1)
-    ldw, ldw_scale = _packed(w, w_scale, n, k, "w")
+    here = _CURRENT_DEVICE()
+    ldx, ldo = _rows(x, "x", _TYPES, here), _rows(out, "out", _TYPES, here)
+    (m, k), n = x.shape, out.size(1)
+    ldw, ldw_scale = _packed(w, w_scale, n, k, "w", here)
     if out.size(0) != m:
         raise ValueError("x is [m, k], out [m, n]")
     if bias is not None:
-        _vector(bias, n, "bias")
-    handle = _stream_of(stream, "x", x, w, w_scale, out, bias, workspace)
+        _floats(bias, n, "bias", here)
+    _at(workspace, "workspace", here)
     need = 0 if workspace is not None else linear_mx4_workspace_bytes(m, k, n)
     ws, ws_bytes, held = _workspace(workspace, need, x.device, stream)
     rc = load_library().rtopk_linear_mx4(x.data_ptr(), _TYPES[x.dtype], m, k, ldx, w.data_ptr(), w_scale.data_ptr(), n, ldw, ldw_scale,
-                                         _ptr(bias), out.data_ptr(), _TYPES[out.dtype], ldo, ws, ws_bytes, handle)
+                                         _ptr(bias), out.data_ptr(), _TYPES[out.dtype], ldo, ws, ws_bytes, _stream_on(stream, here))
     if rc:
         raise RtopkError(rc, "rtopk_linear_mx4")
 
@@ -718,31 +739,29 @@ def linear_mx4_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w_turned: O
         raise ValueError("dx needs w_turned and its scales, dw needs x")
     if db is not None and dw is None:
         raise ValueError("db comes with dw")
-    _matrix(dy, "dy", _TYPES)
+    here = _CURRENT_DEVICE()
+    lddy = _rows(dy, "dy", _TYPES, here)
     m, n = dy.shape
-    k = (dx if dx is not None else dw).size(1)
-    ldw = ldw_scale = 0
+    k = (dx if dx is not None else dw).size(-1)
+    ldw = ldw_scale = lddx = lddw = ldx = 0
     if dx is not None:
-        _matrix(dx, "dx", (dy.dtype,))
-        if tuple(dx.shape) != (m, k):
+        lddx = _rows(dx, "dx", (dy.dtype,), here)
+        if dx.shape != (m, k):
             raise ValueError("dy is [m, n], dx [m, k]")
-        ldw, ldw_scale = _packed(w_turned, w_turned_scale, k, n, "w_turned")
+        ldw, ldw_scale = _packed(w_turned, w_turned_scale, k, n, "w_turned", here)
     if dw is not None:
-        _matrix(x, "x", (dy.dtype,))
-        _matrix(dw, "dw", (torch.float32,))
-        if tuple(x.shape) != (m, k) or tuple(dw.shape) != (n, k):
+        ldx, lddw = _rows(x, "x", (dy.dtype,), here), _rows(dw, "dw", (_F32,), here)
+        if x.shape != (m, k) or dw.shape != (n, k):
             raise ValueError("dy is [m, n], x [m, k], dw [n, k]")
     if db is not None:
-        _vector(db, n, "db")
-    rounding, seed, step, at = _drawn(seed, held := step)
-    asked = (x if dw is not None else None, dw, db, workspace, held if at else None)
-    handle = _stream_of(stream, "dy", dy, *asked, *((dx, w_turned, w_turned_scale) if dx is not None else ()))
+        _floats(db, n, "db", here)
+    _at(workspace, "workspace", here)
+    rounding, seed, step, at = _drawn(seed, step, here)
     ws, ws_bytes, room = _workspace(workspace, 0 if workspace is not None else linear_mx4_backward_workspace_bytes(m, k, n),
                                     dy.device, stream)
-    ld = lambda t: 0 if t is None else _ld(t)   # noqa: E731
     rc = load_library().rtopk_linear_mx4_backward(
-        _ptr(dy), _ptr(x), _TYPES[dy.dtype], m, k, n, _ld(dy), ld(x), _ptr(w_turned), _ptr(w_turned_scale), ldw, ldw_scale,
-        rounding, seed, step, at, _ptr(dx), ld(dx), _ptr(dw), ld(dw), _ptr(db), ws, ws_bytes, handle)
+        _ptr(dy), _ptr(x), _TYPES[dy.dtype], m, k, n, lddy, ldx, _ptr(w_turned), _ptr(w_turned_scale), ldw, ldw_scale,
+        rounding, seed, step, at, _ptr(dx), lddx, _ptr(dw), lddw, _ptr(db), ws, ws_bytes, _stream_on(stream, here))
     if rc:
         raise RtopkError(rc, "rtopk_linear_mx4_backward")
 
@@ -754,16 +773,21 @@ def layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[to
     """rtopk_layer_norm: out = (x - mean) rstd gamma + beta for each row of the matrix ``x``; ``gamma`` and ``beta``
     binary32 of a row's length (None: 1, 0). ``mean`` and ``rstd`` (binary32, one a row) are left for
     :func:`layer_norm_backward` where they are given. ``out`` may be ``x``."""
-    ldx, ldo = _matrix(x, "x", _TYPES), _matrix(out, "out", _TYPES)
-    rows, cols = x.size()
-    if out.size() != x.size():
+    here = _CURRENT_DEVICE()
+    ldx, ldo = _rows(x, "x", _TYPES, here), _rows(out, "out", _TYPES, here)
+    rows, cols = x.shape
+    if out.shape != x.shape:
         raise ValueError("out must have the shape of x")
-    for t, length, name in ((gamma, cols, "gamma"), (beta, cols, "beta"), (mean, rows, "mean"), (rstd, rows, "rstd")):
-        if t is not None:
-            _vector(t, length, name)
-    handle = _stream_of(stream, "x", x, gamma, beta, out, mean, rstd)
+    if gamma is not None:
+        _floats(gamma, cols, "gamma", here)
+    if beta is not None:
+        _floats(beta, cols, "beta", here)
+    if mean is not None:
+        _floats(mean, rows, "mean", here)
+    if rstd is not None:
+        _floats(rstd, rows, "rstd", here)
     rc = load_library().rtopk_layer_norm(x.data_ptr(), _TYPES[x.dtype], rows, cols, ldx, _ptr(gamma), _ptr(beta), eps, out.data_ptr(),
-                                         _TYPES[out.dtype], ldo, _ptr(mean), _ptr(rstd), handle)
+                                         _TYPES[out.dtype], ldo, _ptr(mean), _ptr(rstd), _stream_on(stream, here))
     if rc:
         raise RtopkError(rc, "rtopk_layer_norm")
 
@@ -783,22 +807,30 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
         raise ValueError("neither dx nor dgamma nor dbeta is asked for")
     if add is not None and dx is None:
         raise ValueError("add comes with dx")
-    lddy, ldx = _matrix(dy, "dy", _TYPES), _matrix(x, "x", _TYPES)
-    rows, cols = x.size()
-    lddx, ldadd = (0 if t is None else _matrix(t, name, (x.dtype,)) for t, name in ((dx, "dx"), (add, "add")))
-    if dy.size() != x.size() or any(t is not None and t.size() != x.size() for t in (dx, add)):
+    here = _CURRENT_DEVICE()
+    lddy, ldx, lddx, ldadd = _rows(dy, "dy", _TYPES, here), _rows(x, "x", _TYPES, here), 0, 0
+    shape = rows, cols = x.shape
+    if dx is not None:
+        lddx = _rows(dx, "dx", (x.dtype,), here)
+    if add is not None:
+        ldadd = _rows(add, "add", (x.dtype,), here)
+    if dy.shape != shape or dx is not None and dx.shape != shape or add is not None and add.shape != shape:
         raise ValueError("dy, dx and add must have the shape of x")
-    for t, length, name in ((gamma, cols, "gamma"), (mean, rows, "mean"), (rstd, rows, "rstd"), (dgamma, cols, "dgamma"),
-                            (dbeta, cols, "dbeta")):
-        if t is not None:
-            _vector(t, length, name)
-    handle = _stream_of(stream, "x", x, dy, mean, rstd, gamma, add, dx, dgamma, dbeta, workspace)
+    _floats(mean, rows, "mean", here)
+    _floats(rstd, rows, "rstd", here)
+    if gamma is not None:
+        _floats(gamma, cols, "gamma", here)
+    if dgamma is not None:
+        _floats(dgamma, cols, "dgamma", here)
+    if dbeta is not None:
+        _floats(dbeta, cols, "dbeta", here)
+    _at(workspace, "workspace", here)
     sums = dgamma is not None or dbeta is not None
     need = layer_norm_backward_workspace_bytes(rows, cols) if sums and workspace is None else 0
     ws, ws_bytes, held = _workspace(workspace, need, x.device, stream)
     rc = load_library().rtopk_layer_norm_backward(
         dy.data_ptr(), _TYPES[dy.dtype], x.data_ptr(), _TYPES[x.dtype], rows, cols, lddy, ldx, mean.data_ptr(), rstd.data_ptr(),
-        _ptr(gamma), _ptr(add), ldadd, _ptr(dx), lddx, _ptr(dgamma), _ptr(dbeta), ws, ws_bytes, handle)
+        _ptr(gamma), _ptr(add), ldadd, _ptr(dx), lddx, _ptr(dgamma), _ptr(dbeta), ws, ws_bytes, _stream_on(stream, here))
     if rc:
         raise RtopkError(rc, "rtopk_layer_norm_backward")
 
@@ -809,17 +841,17 @@ def dropout(x: torch.Tensor, out: torch.Tensor, p: float, seed: int, step, resid
     by 1 / (1 - p), plus ``residual`` (of ``out``'s type). The mask belongs to ``seed``, ``step`` (an int, or one int64 on
     the GPU that is read when the kernel runs) and the element's place: the gradient is the same call on ``out``'s.
     ``out`` may be ``x`` or ``residual``."""
-    ldx, ldo = _matrix(x, "x", _TYPES), _matrix(out, "out", _TYPES)
-    ldr = 0 if residual is None else _matrix(residual, "residual", (out.dtype,))
-    rows, cols = x.size()
-    if out.size() != x.size() or (residual is not None and residual.size() != x.size()):
+    here = _CURRENT_DEVICE()
+    ldx, ldo = _rows(x, "x", _TYPES, here), _rows(out, "out", _TYPES, here)
+    ldr = 0 if residual is None else _rows(residual, "residual", (out.dtype,), here)
+    shape = rows, cols = x.shape
+    if out.shape != shape or residual is not None and residual.shape != shape:
         raise ValueError("out and residual must have the shape of x")
     if seed is None:
         raise TypeError("dropout needs a seed")
-    _, seed, step, at = _drawn(seed, held := step)
-    handle = _stream_of(stream, "x", x, out, residual, held if at else None)
+    _, seed, step, at = _drawn(seed, step, here)
     rc = load_library().rtopk_dropout(x.data_ptr(), _TYPES[x.dtype], rows, cols, ldx, _ptr(residual), ldr, out.data_ptr(),
-                                      _TYPES[out.dtype], ldo, p, seed, step, at, handle)
+                                      _TYPES[out.dtype], ldo, p, seed, step, at, _stream_on(stream, here))
     if rc:
         raise RtopkError(rc, "rtopk_dropout")
 
