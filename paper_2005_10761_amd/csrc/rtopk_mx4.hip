@@ -140,16 +140,19 @@ __device__ __forceinline__ u32 groups_of(u32 k) { return (k + kBlock - 1) / kBlo
 constexpr int kPackThreads = 256;
 constexpr u32 kTileColumns = 8 * kWave, kTileBlocks = kTileColumns / kBlock;
 
-template <int kType, bool kDrawn, u32 kTileRows>
-__global__ void __launch_bounds__(kPackThreads) k_pack_rows(ToPack g)
+// tiles of a matrix
+template <u32 kTileRows> __host__ __device__ inline u32 row_tiles(const ToPack &g)
 {
-#ifndef PB
-#define PB 4
-#endif
-    constexpr u32 kWaves = kPackThreads / kWave, kEach = kTileRows / kWaves, kAtOnce = kEach < PB ? kEach : PB;
+    return (g.rows + kTileRows - 1) / kTileRows * ((g.fill + kTileColumns - 1) / kTileColumns);
+}
+
+template <int kType, bool kDrawn, u32 kTileRows, u32 kThreads>
+__device__ __forceinline__ void pack_rows(const ToPack &g, u32 id)
+{
+    constexpr u32 kWaves = kThreads / kWave, kEach = kTileRows / kWaves, kAtOnce = kEach < 4 ? kEach : 4;
     __shared__ __align__(16) unsigned char scales[kTileBlocks][kTileRows];
     const u32 lane = lane_id(), wave = threadIdx.x / kWave, tiles = (g.rows + kTileRows - 1) / kTileRows;
-    const u32 place = xcd_place(blockIdx.x, gridDim.x), tile = place % tiles, strip = place / tiles;
+    const u32 place = xcd_place(id, row_tiles<kTileRows>(g)), tile = place % tiles, strip = place / tiles;
     const u32 r0 = tile * kTileRows + wave * kEach, c = strip * kTileColumns + lane * 8u;
     PhiloxSeed seed{};
     if (kDrawn) seed = g.drawing.get();
@@ -183,13 +186,22 @@ __global__ void __launch_bounds__(kPackThreads) k_pack_rows(ToPack g)
         }
     }
     __syncthreads();
-    constexpr u32 kPerThread = kTileBlocks * kTileRows / kPackThreads;          // 1 or 4 neighbours
+    constexpr u32 kPerThread = kTileBlocks * kTileRows / kThreads;          // 1, 2 or 4 neighbours
     const u32 row = threadIdx.x * kPerThread % kTileRows, block = threadIdx.x * kPerThread / kTileRows;
     const u32 r = tile * kTileRows + row, b = strip * kTileBlocks + block;
-    if (b >= blocks) return;
+    if (b >= blocks || r >= g.rows) return;
     unsigned char *to = g.to.scale + b * g.to.lds + r;
-    if constexpr (kPerThread == 4) write_bytes(to, 0, *(const u32 *)&scales[block][row], r < g.rows ? g.rows - r : 0u);
-    else if (r < g.rows) *to = scales[block][row];
+    if (r + kPerThread <= g.rows) {
+        __builtin_memcpy(to, &scales[block][row], kPerThread);
+    } else {
+        for (u32 i = 0; r + i < g.rows; ++i) to[i] = scales[block][row + i];
+    }
+}
+
+template <int kType, bool kDrawn, u32 kTileRows>
+__global__ void __launch_bounds__(kPackThreads) k_pack_rows(ToPack g)
+{
+    pack_rows<kType, kDrawn, kTileRows, kPackThreads>(g, blockIdx.x);
 }
 
 // Along columns, and turned over: a wavefront has 32 rows and 64 columns, a lane eight neighbouring rows of four columns; a
@@ -319,29 +331,44 @@ __device__ __forceinline__ void pack_columns(const ToTurn &t)
     }
 }
 
+// One matrix along columns, or two, and (blockIdx.z = 2) one along rows: all that a layer's backward quantises, in one launch.
+constexpr u32 kBesideRows = 64;
+
 template <int kType>
-__global__ void __launch_bounds__(kTurnThreads) k_pack_columns(Turns both)
+__global__ void __launch_bounds__(kTurnThreads) k_pack_columns(Turns both, ToPack rows)
 {
+    if (blockIdx.z == 2) {
+        const u32 id = blockIdx.y * gridDim.x + blockIdx.x;
+        if (id >= row_tiles<kBesideRows>(rows)) return;
+        if (both.drawn & 1u) pack_rows<kType, true, kBesideRows, kTurnThreads>(rows, id);
+        else pack_rows<kType, false, kBesideRows, kTurnThreads>(rows, id);
+        return;
+    }
     const ToTurn &t = both.of[blockIdx.z];
-    if (blockIdx.x * kWave >= t.of.cols || blockIdx.y * kTurnRows >= t.of.fill) return;        // (the other matrix is larger)
+    if (blockIdx.x * kWave >= t.of.cols || blockIdx.y * kTurnRows >= t.of.fill) return;        // (another matrix is larger)
     if (both.drawn >> blockIdx.z & 1u) pack_columns<kType, true>(t);
     else pack_columns<kType, false>(t);
 }
 
-// The sums of the groups of rows together, in binary64.
-__global__ void __launch_bounds__(256) k_sum_groups(const float *part, u32 groups, u32 cols, float *out)
+// The sums of the groups of rows together, in binary64, 16 columns a workgroup.
+constexpr u32 kJoinColumns = 16, kJoinThreads = 512;
+
+__global__ void __launch_bounds__(kJoinThreads) k_sum_groups(const float *part, u32 groups, u32 cols, float *out)
 {
-    constexpr u32 kWaves = 4;
-    __shared__ double sums[kWaves][kWave];
-    const u32 lane = lane_id(), wave = threadIdx.x / kWave, c = blockIdx.x * kWave + lane;
+    constexpr u32 kWaves = kJoinThreads / kWave, kAtOnce = kJoinThreads / kJoinColumns;
+    __shared__ double sums[kWaves][kJoinColumns];
+    const u32 c = blockIdx.x * kJoinColumns + threadIdx.x % kJoinColumns;
     double sum = 0;
-#pragma unroll 8
-    for (u32 s = wave; s < groups; s += kWaves) sum += (double)part[(u64)s * cols + min(c, cols - 1u)];
-    sums[wave][lane] = sum;
-    __syncthreads();
-    if (wave || c >= cols) return;
+#pragma unroll 4
+    for (u32 s = threadIdx.x / kJoinColumns; s < groups; s += kAtOnce) sum += (double)part[(u64)s * cols + min(c, cols - 1u)];
 #pragma unroll
-    for (u32 w = 1; w < kWaves; ++w) sum += sums[w][lane];
+    for (int o = kJoinColumns; o < kWave; o <<= 1) sum += __shfl_xor(sum, o, kWave);
+    if (lane_id() < kJoinColumns) sums[threadIdx.x / kWave][lane_id()] = sum;
+    __syncthreads();
+    if (threadIdx.x >= kJoinColumns || c >= cols) return;
+    sum = 0;
+#pragma unroll
+    for (u32 w = 0; w < kWaves; ++w) sum += sums[w][threadIdx.x];
     out[c] = (float)sum;
 }
 
@@ -693,39 +720,40 @@ u64 blocks_of(u64 k) { return (k + kBlock - 1) / kBlock; }
 bool packed_ok(u64 rows, u64 k, u64 ldq, u64 lds) { return ldq >= bytes_of(k) && ldq <= kMostSize && lds >= rows && lds <= kMostSize; }
 
 template <int kType, u32 kTileRows>
-void launch_pack_rows(const ToPack &g, u32 strips, bool drawn, hipStream_t stream)
+void launch_pack_rows(const ToPack &g, bool drawn, hipStream_t stream)
 {
-    const u32 grid = (g.rows + kTileRows - 1) / kTileRows * strips;
-    if (drawn) k_pack_rows<kType, true, kTileRows><<<grid, kPackThreads, 0, stream>>>(g);
-    else k_pack_rows<kType, false, kTileRows><<<grid, kPackThreads, 0, stream>>>(g);
+    if (drawn) k_pack_rows<kType, true, kTileRows><<<row_tiles<kTileRows>(g), kPackThreads, 0, stream>>>(g);
+    else k_pack_rows<kType, false, kTileRows><<<row_tiles<kTileRows>(g), kPackThreads, 0, stream>>>(g);
 }
 template <int kType>
-int pack_rows(const ToPack &g, bool drawn, hipStream_t stream)
+int run_pack_rows(const ToPack &g, bool drawn, hipStream_t stream)
 {
     // 64 rows where that leaves two workgroups a unit
-    const u32 strips = (g.fill + kTileColumns - 1) / kTileColumns;
-    if ((u64)((g.rows + 63u) / 64u) * strips >= 2 * kUnits) launch_pack_rows<kType, 64>(g, strips, drawn, stream);
-    else launch_pack_rows<kType, 16>(g, strips, drawn, stream);
+    if (row_tiles<64>(g) >= 2 * kUnits) launch_pack_rows<kType, 64>(g, drawn, stream);
+    else launch_pack_rows<kType, 16>(g, drawn, stream);
     return launched();
 }
-int pack_rows(const ToPack &g, int type, bool drawn, hipStream_t stream)
+int run_pack_rows(const ToPack &g, int type, bool drawn, hipStream_t stream)
 {
-    return type == RTOPK_F32 ? pack_rows<RTOPK_F32>(g, drawn, stream)
-           : type == RTOPK_BF16 ? pack_rows<RTOPK_BF16>(g, drawn, stream) : pack_rows<RTOPK_F16>(g, drawn, stream);
+    return type == RTOPK_F32 ? run_pack_rows<RTOPK_F32>(g, drawn, stream)
+           : type == RTOPK_BF16 ? run_pack_rows<RTOPK_BF16>(g, drawn, stream) : run_pack_rows<RTOPK_F16>(g, drawn, stream);
 }
 
 u32 turn_groups(u32 rows) { return (rows + kTurnRows - 1) / kTurnRows; }
 
-int pack_columns(const Turns &t, u32 count, int type, hipStream_t stream)
+// `count` matrices along columns, and `rows`, if not null, along rows.
+int run_pack_columns(const Turns &t, u32 count, const ToPack *rows, int type, hipStream_t stream)
 {
-    dim3 grid(1, 1, count);
+    dim3 grid(1, 1, rows ? 3 : count);
     for (u32 i = 0; i < count; ++i) {
         grid.x = std::max(grid.x, (t.of[i].of.cols + kWave - 1) / kWave);
         grid.y = std::max(grid.y, turn_groups(t.of[i].of.fill));
     }
-    if (type == RTOPK_F32) k_pack_columns<RTOPK_F32><<<grid, kTurnThreads, 0, stream>>>(t);
-    else if (type == RTOPK_BF16) k_pack_columns<RTOPK_BF16><<<grid, kTurnThreads, 0, stream>>>(t);
-    else k_pack_columns<RTOPK_F16><<<grid, kTurnThreads, 0, stream>>>(t);
+    if (rows) grid.y = std::max(grid.y, (row_tiles<kBesideRows>(*rows) + grid.x - 1) / grid.x);
+    const ToPack other = rows ? *rows : ToPack{};
+    if (type == RTOPK_F32) k_pack_columns<RTOPK_F32><<<grid, kTurnThreads, 0, stream>>>(t, other);
+    else if (type == RTOPK_BF16) k_pack_columns<RTOPK_BF16><<<grid, kTurnThreads, 0, stream>>>(t, other);
+    else k_pack_columns<RTOPK_F16><<<grid, kTurnThreads, 0, stream>>>(t, other);
     return launched();
 }
 
@@ -894,8 +922,8 @@ extern "C" int rtopk_quantize_mx4(const void *x, int type, uint64_t rows, uint64
     const bool drawn = rounding == RTOPK_DRAWN;
     const ToPack g{x, ldx, (u32)rows, (u32)cols, (u32)(along == RTOPK_ROWS ? cols : rows), Packed{q, scale, ldq, lds},
                    Drawing{seed, step, drawn ? step_device : nullptr}};
-    if (along == RTOPK_ROWS) return pack_rows(g, type, drawn, stream);
-    return pack_columns(Turns{{ToTurn{g, nullptr}, {}}, drawn ? 1u : 0u}, 1, type, stream);
+    if (along == RTOPK_ROWS) return run_pack_rows(g, type, drawn, stream);
+    return run_pack_columns(Turns{{ToTurn{g, nullptr}, {}}, drawn ? 1u : 0u}, 1, nullptr, type, stream);
 }
 
 extern "C" int rtopk_dequantize_mx4(const uint8_t *q, uint64_t rows, uint64_t cols, uint64_t ldq, const uint8_t *scale, uint64_t lds,
@@ -956,7 +984,7 @@ extern "C" int rtopk_linear_mx4(const void *x, int type, uint64_t m, uint64_t k,
     cut_linear(workspace, (u32)m, (u32)k, (u32)n, p);
     const Product4 g{p.x.q, w, p.x.scale, w_scale, p.x.ldq, ldw, p.x.lds, ldw_scale, (u32)m, (u32)n, (u32)k, bias, out, ldo, out_type, 0, 0, nullptr};
     if (in_one((u32)m, (u32)k, (u32)n)) return run_few4(Few4{g, x, ldx}, type, stream);
-    if (const int rc = pack_rows(to_pack(x, ldx, (u32)m, (u32)k, (u32)filled((u32)k), p.x, Drawing{}), type, false, stream)) return rc;
+    if (const int rc = run_pack_rows(to_pack(x, ldx, (u32)m, (u32)k, (u32)filled((u32)k), p.x, Drawing{}), type, false, stream)) return rc;
     return few_tokens((u32)m) ? run_few4(Few4{g, nullptr, 0}, type, stream) : run_product4(g, p.part, stream);
 }
 
@@ -993,23 +1021,27 @@ extern "C" int rtopk_linear_mx4_backward(const void *dy, const void *x, int type
     cut_backward(workspace, (u32)m, (u32)k, (u32)n, p);
     const bool drawn = rounding == RTOPK_DRAWN;
     const Drawing drawing{seed, step, drawn ? step_device : nullptr};
+    const ToPack rows = to_pack(dy, lddy, (u32)m, (u32)n, (u32)filled((u32)n), p.dy, drawing);
+    if (dw) {
+        const u32 fill = (u32)filled((u32)m);
+        const Turns t{{ToTurn{to_pack(dy, lddy, (u32)m, (u32)n, fill, p.dy_turned, drawing), db ? p.sums : nullptr},
+                       ToTurn{to_pack(x, ldx, (u32)m, (u32)k, fill, p.x_turned, Drawing{}), nullptr}},
+                      drawn ? 1u : 0u};
+        if (const int rc = run_pack_columns(t, 2, dx ? &rows : nullptr, type, stream)) return rc;
+        if (db) {
+            k_sum_groups<<<(unsigned)((n + kJoinColumns - 1) / kJoinColumns), kJoinThreads, 0, stream>>>(p.sums, turn_groups((u32)m), (u32)n, db);
+            if (const int rc = launched()) return rc;
+        }
+    } else if (const int rc = run_pack_rows(rows, type, drawn, stream)) {
+        return rc;
+    }
     if (dx) {
-        if (const int rc = pack_rows(to_pack(dy, lddy, (u32)m, (u32)n, (u32)filled((u32)n), p.dy, drawing), type, drawn, stream)) return rc;
         if (const int rc = run_product4(Product4{p.dy.q, w_turned, p.dy.scale, w_turned_scale, p.dy.ldq, ldw, p.dy.lds, ldw_scale, (u32)m,
                                                  (u32)k, (u32)n, nullptr, dx, lddx, type, 0, 0, nullptr},
                                         p.part, stream))
             return rc;
     }
     if (!dw) return RTOPK_OK;
-    const u32 fill = (u32)filled((u32)m);
-    const Turns t{{ToTurn{to_pack(dy, lddy, (u32)m, (u32)n, fill, p.dy_turned, drawing), db ? p.sums : nullptr},
-                   ToTurn{to_pack(x, ldx, (u32)m, (u32)k, fill, p.x_turned, Drawing{}), nullptr}},
-                  drawn ? 1u : 0u};
-    if (const int rc = pack_columns(t, 2, type, stream)) return rc;
-    if (db) {
-        k_sum_groups<<<(unsigned)((n + kWave - 1) / kWave), 256, 0, stream>>>(p.sums, turn_groups((u32)m), (u32)n, db);
-        if (const int rc = launched()) return rc;
-    }
     return run_product4(Product4{p.dy_turned.q, p.x_turned.q, p.dy_turned.scale, p.x_turned.scale, p.dy_turned.ldq, p.x_turned.ldq,
                                  p.dy_turned.lds, p.x_turned.lds, (u32)n, (u32)k, (u32)m, nullptr, dw, lddw, RTOPK_F32, 0, 0,
                                  nullptr},
