@@ -141,6 +141,9 @@ typedef struct rtopk_product_plan {
 } rtopk_product_plan_t;
 int rtopk_product_plan(uint64_t m, uint64_t n, uint64_t k, int on_lines, rtopk_product_plan_t *plan);
 
+/* The same of the 4-bit product; k in numbers. */
+int rtopk_product_mx4_plan(uint64_t m, uint64_t n, uint64_t k, int on_lines, rtopk_product_plan_t *plan);
+
 /* The orthogonalisation of up to 16 matrices that share launches. */
 typedef struct rtopk_orthogonalize_plan {
     uint32_t narrow;                                    /* a launch a step; then only the runs and whether they are joined are set */

@@ -20,7 +20,7 @@ from .binding import (RtopkError, aggregate, aggregate_update, aggregate_update_
                       quantize_mx4, dequantize_mx4, matmul_mx4, matmul_mx4_workspace_bytes, linear_mx4, linear_mx4_workspace_bytes,
                       linear_mx4_backward, linear_mx4_backward_workspace_bytes,
                       layer_norm, layer_norm_backward, layer_norm_backward_workspace_bytes, dropout,
-                      product_plan, orthogonalize_plan)
+                      product_plan, product_mx4_plan, orthogonalize_plan)
 
 __all__ = ["RtopkError", "aggregate", "aggregate_update", "aggregate_update_momentum", "aggregate_update_static", "STATIC_SCRATCH_BYTES", "aggregate_update_workspace_bytes", "aggregate_workspace_bytes", "encode", "encode_batch", "encode_batch_device_step", "diag_stream_add", "encode_stats",
            "encode_workspace_bytes", "library_path", "load_library", "strerror", "trace_next_encode", "version", "STAGES",
@@ -31,4 +31,5 @@ __all__ = ["RtopkError", "aggregate", "aggregate_update", "aggregate_update_mome
            "aggregate_update_orthogonal_workspace_bytes",
            "quantize_mx4", "dequantize_mx4", "matmul_mx4", "matmul_mx4_workspace_bytes", "linear_mx4", "linear_mx4_workspace_bytes",
            "linear_mx4_backward", "linear_mx4_backward_workspace_bytes", "layer_norm", "layer_norm_backward",
-           "layer_norm_backward_workspace_bytes", "dropout", "product_plan", "orthogonalize_plan"]
+           "layer_norm_backward_workspace_bytes", "dropout", "product_plan", "product_mx4_plan",
+           "orthogonalize_plan"]

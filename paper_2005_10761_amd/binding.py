@@ -34,7 +34,7 @@ EXPORTS = ("rtopk_encode_workspace_bytes", "rtopk_aggregate_workspace_bytes", "r
            "rtopk_strerror", "rtopk_version")
 # ... and include/rtopk_diag.h
 DIAG_EXPORTS = ("rtopk_encode_stats", "rtopk_trace_next_encode", "rtopk_force_next_encode",
-                "rtopk_diag_stream_add", "rtopk_product_plan", "rtopk_orthogonalize_plan", "rtopk_debug_checks")
+                "rtopk_diag_stream_add", "rtopk_product_plan", "rtopk_product_mx4_plan", "rtopk_orthogonalize_plan", "rtopk_debug_checks")
 
 
 class RtopkError(RuntimeError):
@@ -139,6 +139,7 @@ def load_library() -> ctypes.CDLL:
             "rtopk_aggregate_update_orthogonal": [u32, vp, vp, u32, u64, u64, u64, f32, f32, f32, i32, f32,
                                                   f32, u32, vp, f32, i32, vp, vp, vp, u64, vp],
             "rtopk_product_plan": [u64, u64, u64, i32, vp],
+            "rtopk_product_mx4_plan": [u64, u64, u64, i32, vp],
             "rtopk_orthogonalize_plan": [u32, u64, u64, i32, u32, vp, vp]}.items():
         getattr(L, name).argtypes = args
         getattr(L, name).restype = i32
@@ -945,6 +946,15 @@ def product_plan(m: int, n: int, k: int, on_lines: bool = True) -> dict:
     rc = load_library().rtopk_product_plan(m, n, k, int(on_lines), ctypes.byref(plan))
     if rc:
         raise RtopkError(rc, "rtopk_product_plan")
+    return {name: int(getattr(plan, name)) for name, _ in plan._fields_}
+
+
+def product_mx4_plan(m: int, n: int, k: int, on_lines: bool = True) -> dict:
+    """rtopk_product_mx4_plan: the tiles and runs that the 4-bit product of these sizes takes."""
+    plan = ProductPlan()
+    rc = load_library().rtopk_product_mx4_plan(m, n, k, int(on_lines), ctypes.byref(plan))
+    if rc:
+        raise RtopkError(rc, "rtopk_product_mx4_plan")
     return {name: int(getattr(plan, name)) for name, _ in plan._fields_}
 
 

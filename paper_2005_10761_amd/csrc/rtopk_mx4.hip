@@ -961,6 +961,14 @@ extern "C" int rtopk_matmul_mx4(const uint8_t *a, const uint8_t *a_scale, const 
                         workspace, (hipStream_t)stream_v);
 }
 
+extern "C" int rtopk_product_mx4_plan(uint64_t m, uint64_t n, uint64_t k, int on_lines, rtopk_product_plan_t *plan)
+{
+    if (!plan || !size_ok(m) || !size_ok(n) || k > kMostSize) return RTOPK_EINVAL;
+    const Plan p = plan_product((u32)m, (u32)n, (u32)k, on_lines != 0);
+    *plan = rtopk_product_plan_t{p.edge, p.tiles, p.splits};
+    return RTOPK_OK;
+}
+
 extern "C" int rtopk_linear_mx4_workspace_bytes(uint64_t m, uint64_t k, uint64_t n, uint64_t *bytes)
 {
     if (!bytes || m > kMostSize || !size_ok(k) || !size_ok(n)) return RTOPK_EINVAL;

@@ -260,8 +260,8 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_back_sums(NormBack g)
 // Rows by workgroups that keep going: kWavesPerRow wavefronts hold a row in registers, kPieces pieces of eight numbers a
 // lane, the next row's x and dy on their way while this one's means are taken and its dx is written. One read of everything,
 // one write: a lane's share of dgamma and dbeta stays in registers over all of its rows (kHeld), and the workgroups' are joined afterwards.
-// kBeside: other workgroups of the launch, from g.groups on, take the sums by themselves.
-enum SumsBy { kNone, kHeld, kBeside };
+// kBeside: other workgroups of the launch, from g.groups on, take the sums by themselves (or there are none).
+enum SumsBy { kHeld, kBeside };
 
 template <int kType, int kDyType, int kWavesPerRow, int kPieces, SumsBy kSums>
 __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNormThreads) k_norm_back(NormBack g)
@@ -587,9 +587,9 @@ u32 run_count(u32 rows, u32 cols) { return (rows + run_rows(rows, cols) - 1) / r
 bool small(u64 rows, u64 cols) { return rows <= 2048 && rows * cols <= 1u << 21; }
 
 template <int kType, int kDyType, SumsBy kSums>
-int launch_held(const NormBack &g, hipStream_t stream)
+int launch_held(const NormBack &g, u32 beside, hipStream_t stream)
 {
-    const u32 cols = g.cols, grid = g.groups + (kSums == kBeside ? (cols + kDirectColumns - 1) / kDirectColumns : 0u);
+    const u32 cols = g.cols, grid = g.groups + beside;
     if (cols <= 512) k_norm_back<kType, kDyType, 1, 1, kSums><<<grid, kNormThreads, 0, stream>>>(g);
     else if (cols <= 1024) k_norm_back<kType, kDyType, 1, 2, kSums><<<grid, kNormThreads, 0, stream>>>(g);
     else if (cols <= 2048) k_norm_back<kType, kDyType, 4, 1, kSums><<<grid, kNormThreads, 0, stream>>>(g);
@@ -610,16 +610,17 @@ int launch_back(NormBack g, hipStream_t stream)
 {
     const bool held = g.dx && g.cols <= kHeldColumns, direct = small(g.rows, g.cols);
     bool sums = g.dgamma || g.dbeta;
+    const u32 strips = (g.cols + kDirectColumns - 1) / kDirectColumns;
     g.groups = held_groups(g.rows, g.cols, 2);
-    if (held && sums && direct && g.dx != g.x && g.dx != g.dy) return launch_held<kType, kDyType, kBeside>(g, stream);
+    if (held && sums && direct && g.dx != g.x && g.dx != g.dy) return launch_held<kType, kDyType, kBeside>(g, strips, stream);
     if (held && sums && !direct) {
         g.runs = g.groups;
-        if (const int rc = launch_held<kType, kDyType, kHeld>(g, stream)) return rc;
+        if (const int rc = launch_held<kType, kDyType, kHeld>(g, 0, stream)) return rc;
         return join_sums(g, stream);
     }
     // the sums first: dx may be x or dy
     if (sums && direct) {
-        k_norm_back_sums<kType, kDyType><<<(g.cols + kDirectColumns - 1) / kDirectColumns, kNormThreads, 0, stream>>>(g);
+        k_norm_back_sums<kType, kDyType><<<strips, kNormThreads, 0, stream>>>(g);
         if (const int rc = launched()) return rc;
     } else if (sums) {
         g.run = run_rows(g.rows, g.cols);
@@ -628,7 +629,7 @@ int launch_back(NormBack g, hipStream_t stream)
         if (const int rc = launched()) return rc;
         if (const int rc = join_sums(g, stream)) return rc;
     }
-    if (held) return launch_held<kType, kDyType, kNone>(g, stream);
+    if (held) return launch_held<kType, kDyType, kBeside>(g, 0, stream);
     if (g.dx) k_norm_back_row<kType, kDyType><<<row_grid(g.rows), 1024, 0, stream>>>(g);
     return launched();
 }
