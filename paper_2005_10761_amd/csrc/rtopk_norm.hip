@@ -187,7 +187,7 @@ struct NormBack {
     u32 groups;                     // workgroups that share the rows
     u32 runs, run;                  // the sums over rows: runs of so many rows
     float *dgamma, *dbeta;          // or null
-    float *part;                    // [2][runs][cols]
+    float *part;                    // [2][runs][cols], or null
 };
 
 // All of the sums of 32 columns by one workgroup of kThreads: four lanes have eight columns each, and every kThreads / 4th row. For
@@ -259,18 +259,14 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_back_sums(NormBack g)
 
 // Rows by workgroups that keep going: kWavesPerRow wavefronts hold a row in registers, kPieces pieces of eight numbers a
 // lane, the next row's x and dy on their way while this one's means are taken and its dx is written. One read of everything,
-// one write: a lane's share of dgamma and dbeta stays in registers over all of its rows (kHeld), and the workgroups' are joined afterwards.
-// kBeside: other workgroups of the launch, from g.groups on, take the sums by themselves (or there are none).
-enum SumsBy { kHeld, kBeside };
-
-template <int kType, int kDyType, int kWavesPerRow, int kPieces, SumsBy kSums>
+// one write: a lane's share of dgamma and dbeta stays in registers over all of its rows, and goes to g.part, if that is there, to be
+// joined with the other workgroups'. Workgroups of the launch from g.groups on, if there are any, take the sums by themselves.
+template <int kType, int kDyType, int kWavesPerRow, int kPieces>
 __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNormThreads) k_norm_back(NormBack g)
 {
-    if constexpr (kSums == kBeside) {
-        if (blockIdx.x >= g.groups) {
-            sum_columns<kType, kDyType, (kWavesPerRow > 4 ? kWavesPerRow * kWave : kNormThreads)>(g, blockIdx.x - g.groups);
-            return;
-        }
+    if (blockIdx.x >= g.groups) {
+        sum_columns<kType, kDyType, (kWavesPerRow > 4 ? kWavesPerRow * kWave : kNormThreads)>(g, blockIdx.x - g.groups);
+        return;
     }
     constexpr u32 kWaves = kWavesPerRow > 4 ? kWavesPerRow : 4, kRows = kWaves / kWavesPerRow, kStep = 8u * kWave * kWavesPerRow;
     __shared__ float means[2][2][kWaves];
@@ -318,10 +314,8 @@ __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNor
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 h[p][i] = c + i < g.cols ? (h[p][i] - mean) * rstd : 0.0f;      // (d is zero there)
-                if (kSums == kHeld) {
-                    dgamma[p][i] = fmaf(d[p][i], h[p][i], dgamma[p][i]);
-                    dbeta[p][i] += d[p][i];
-                }
+                dgamma[p][i] = fmaf(d[p][i], h[p][i], dgamma[p][i]);
+                dbeta[p][i] += d[p][i];
                 d[p][i] *= gamma[p][i];
                 sum += d[p][i];
                 inner = fmaf(d[p][i], h[p][i], inner);
@@ -357,7 +351,7 @@ __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNor
             write_eight(g.dx, r * g.lddx + c, kType, v[0], v[1], g.cols - c);
         }
     }
-    if constexpr (kSums == kHeld) {
+    if (g.part) {
         float *out = g.part + (u64)blockIdx.x * g.cols;
         const u64 beta = (u64)g.runs * g.cols;
         if constexpr (kRows > 1) {
@@ -564,8 +558,7 @@ template <int kType>
 int launch_norm(const Norm &g, hipStream_t stream)
 {
     const u32 cols = g.cols, grid = held_groups(g.rows, g.cols, 4);
-    if (cols <= 512) k_norm<kType, 1, 1><<<grid, kNormThreads, 0, stream>>>(g);
-    else if (cols <= 1024) k_norm<kType, 1, 2><<<grid, kNormThreads, 0, stream>>>(g);
+    if (cols <= 1024) k_norm<kType, 1, 2><<<grid, kNormThreads, 0, stream>>>(g);
     else if (cols <= 2048) k_norm<kType, 4, 1><<<grid, kNormThreads, 0, stream>>>(g);
     else if (cols <= 4096) k_norm<kType, 4, 2><<<grid, kNormThreads, 0, stream>>>(g);
     else if (cols <= 8192) k_norm<kType, 8, 2><<<grid, 8 * kWave, 0, stream>>>(g);
@@ -586,16 +579,15 @@ u32 run_count(u32 rows, u32 cols) { return (rows + run_rows(rows, cols) - 1) / r
 // Small matrices: their sums cost less than a launch that joins them (the second read comes from the caches).
 bool small(u64 rows, u64 cols) { return rows <= 2048 && rows * cols <= 1u << 21; }
 
-template <int kType, int kDyType, SumsBy kSums>
+template <int kType, int kDyType>
 int launch_held(const NormBack &g, u32 beside, hipStream_t stream)
 {
     const u32 cols = g.cols, grid = g.groups + beside;
-    if (cols <= 512) k_norm_back<kType, kDyType, 1, 1, kSums><<<grid, kNormThreads, 0, stream>>>(g);
-    else if (cols <= 1024) k_norm_back<kType, kDyType, 1, 2, kSums><<<grid, kNormThreads, 0, stream>>>(g);
-    else if (cols <= 2048) k_norm_back<kType, kDyType, 4, 1, kSums><<<grid, kNormThreads, 0, stream>>>(g);
-    else if (cols <= 4096) k_norm_back<kType, kDyType, 4, 2, kSums><<<grid, kNormThreads, 0, stream>>>(g);
-    else if (cols <= 8192) k_norm_back<kType, kDyType, 8, 2, kSums><<<grid, 8 * kWave, 0, stream>>>(g);
-    else k_norm_back<kType, kDyType, 16, 2, kSums><<<grid, 16 * kWave, 0, stream>>>(g);
+    if (cols <= 1024) k_norm_back<kType, kDyType, 1, 2><<<grid, kNormThreads, 0, stream>>>(g);
+    else if (cols <= 2048) k_norm_back<kType, kDyType, 4, 1><<<grid, kNormThreads, 0, stream>>>(g);
+    else if (cols <= 4096) k_norm_back<kType, kDyType, 4, 2><<<grid, kNormThreads, 0, stream>>>(g);
+    else if (cols <= 8192) k_norm_back<kType, kDyType, 8, 2><<<grid, 8 * kWave, 0, stream>>>(g);
+    else k_norm_back<kType, kDyType, 16, 2><<<grid, 16 * kWave, 0, stream>>>(g);
     return launched();
 }
 
@@ -609,13 +601,16 @@ template <int kType, int kDyType>
 int launch_back(NormBack g, hipStream_t stream)
 {
     const bool held = g.dx && g.cols <= kHeldColumns, direct = small(g.rows, g.cols);
-    bool sums = g.dgamma || g.dbeta;
+    const bool sums = g.dgamma || g.dbeta;
     const u32 strips = (g.cols + kDirectColumns - 1) / kDirectColumns;
     g.groups = held_groups(g.rows, g.cols, 2);
-    if (held && sums && direct && g.dx != g.x && g.dx != g.dy) return launch_held<kType, kDyType, kBeside>(g, strips, stream);
+    float *const room = g.part;
+    g.part = nullptr;
+    if (held && sums && direct && g.dx != g.x && g.dx != g.dy) return launch_held<kType, kDyType>(g, strips, stream);
     if (held && sums && !direct) {
         g.runs = g.groups;
-        if (const int rc = launch_held<kType, kDyType, kHeld>(g, 0, stream)) return rc;
+        g.part = room;
+        if (const int rc = launch_held<kType, kDyType>(g, 0, stream)) return rc;
         return join_sums(g, stream);
     }
     // the sums first: dx may be x or dy
@@ -625,11 +620,13 @@ int launch_back(NormBack g, hipStream_t stream)
     } else if (sums) {
         g.run = run_rows(g.rows, g.cols);
         g.runs = run_count(g.rows, g.cols);
+        g.part = room;
         k_norm_back_columns<kType, kDyType><<<dim3((g.cols + kSumColumns - 1) / kSumColumns, g.runs), kNormThreads, 0, stream>>>(g);
         if (const int rc = launched()) return rc;
         if (const int rc = join_sums(g, stream)) return rc;
     }
-    if (held) return launch_held<kType, kDyType, kBeside>(g, 0, stream);
+    g.part = nullptr;
+    if (held) return launch_held<kType, kDyType>(g, 0, stream);
     if (g.dx) k_norm_back_row<kType, kDyType><<<row_grid(g.rows), 1024, 0, stream>>>(g);
     return launched();
 }
