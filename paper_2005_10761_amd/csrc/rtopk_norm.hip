@@ -177,8 +177,46 @@ __global__ void __launch_bounds__(1024) k_norm_row(Norm g)
 // ---------------------------------------------------------------------------
 // Backward.
 // ---------------------------------------------------------------------------
+
+// Eight neighbours of a type that is known when the kernel runs only (the same for all lanes).
+struct EightOf {
+    i32x4 w[2];
+    __device__ __forceinline__ void load(const unsigned char *row, u32 c, u32 cols, int type)
+    {
+        if (type == RTOPK_F32) {
+            Eight<RTOPK_F32> e;
+            e.load(row, c, cols);
+            w[0] = e.w[0];
+            w[1] = e.w[1];
+        } else {
+            Eight<RTOPK_BF16> e;
+            e.load(row, c, cols);
+            w[0] = e.w[0];
+        }
+    }
+    __device__ __forceinline__ void numbers(float (&v)[8], const unsigned char *row, u32 c, u32 cols, int type) const
+    {
+        if (type == RTOPK_F32) {
+            Eight<RTOPK_F32> e;
+            e.w[0] = w[0];
+            e.w[1] = w[1];
+            e.numbers(v, row, c, cols);
+        } else if (type == RTOPK_BF16) {
+            Eight<RTOPK_BF16> e;
+            e.w[0] = w[0];
+            e.numbers(v, row, c, cols);
+        } else {
+            Eight<RTOPK_F16> e;
+            e.w[0] = w[0];
+            e.numbers(v, row, c, cols);
+        }
+    }
+};
+__device__ __forceinline__ u32 size_of(int type) { return type == RTOPK_F32 ? 4u : 2u; }
+
 struct NormBack {
     const void *dy, *x, *add;       // add: of x's type, or null
+    int dy_type;
     u64 lddy, ldx, ldadd;
     u32 rows, cols;
     const float *mean, *rstd, *gamma;
@@ -194,7 +232,7 @@ struct NormBack {
 // small matrices: neither runs of rows to be joined nor a launch for them.
 constexpr u32 kDirectColumns = 32, kDirectLanes = kDirectColumns / 8;
 
-template <int kType, int kDyType, u32 kThreads>
+template <int kType, u32 kThreads>
 __device__ __forceinline__ void sum_columns(const NormBack &g, u32 strip)
 {
     constexpr u32 kWaves = kThreads / kWave, kLanes = kThreads / kDirectLanes, kAtOnce = 4;
@@ -203,13 +241,13 @@ __device__ __forceinline__ void sum_columns(const NormBack &g, u32 strip)
     float dgamma[8] = {0, 0, 0, 0, 0, 0, 0, 0}, dbeta[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (u32 r = threadIdx.x / kDirectLanes; r < g.rows; r += kAtOnce * kLanes) {
         Eight<kType> ex[kAtOnce];
-        Eight<kDyType> ey[kAtOnce];
+        EightOf ey[kAtOnce];
         float mean[kAtOnce], rstd[kAtOnce];
 #pragma unroll
         for (u32 q = 0; q < kAtOnce; ++q) {
             const u64 row = min(r + q * kLanes, g.rows - 1u);
             ex[q].load((const unsigned char *)g.x + row * g.ldx * Eight<kType>::kSize, c, g.cols);
-            ey[q].load((const unsigned char *)g.dy + row * g.lddy * Eight<kDyType>::kSize, c, g.cols);
+            ey[q].load((const unsigned char *)g.dy + row * g.lddy * size_of(g.dy_type), c, g.cols, g.dy_type);
             mean[q] = g.mean[row];
             rstd[q] = g.rstd[row];
         }
@@ -219,7 +257,7 @@ __device__ __forceinline__ void sum_columns(const NormBack &g, u32 strip)
             if (row >= g.rows) break;
             float x[8], d[8];
             ex[q].numbers(x, (const unsigned char *)g.x + row * g.ldx * Eight<kType>::kSize, c, g.cols);
-            ey[q].numbers(d, (const unsigned char *)g.dy + row * g.lddy * Eight<kDyType>::kSize, c, g.cols);
+            ey[q].numbers(d, (const unsigned char *)g.dy + row * g.lddy * size_of(g.dy_type), c, g.cols, g.dy_type);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 dgamma[i] = fmaf(d[i], (x[i] - mean[q]) * rstd[q], dgamma[i]);
@@ -251,21 +289,21 @@ __device__ __forceinline__ void sum_columns(const NormBack &g, u32 strip)
     out[at] = sum;
 }
 
-template <int kType, int kDyType>
+template <int kType>
 __global__ void __launch_bounds__(kNormThreads) k_norm_back_sums(NormBack g)
 {
-    sum_columns<kType, kDyType, kNormThreads>(g, blockIdx.x);
+    sum_columns<kType, kNormThreads>(g, blockIdx.x);
 }
 
 // Rows by workgroups that keep going: kWavesPerRow wavefronts hold a row in registers, kPieces pieces of eight numbers a
 // lane, the next row's x and dy on their way while this one's means are taken and its dx is written. One read of everything,
 // one write: a lane's share of dgamma and dbeta stays in registers over all of its rows, and goes to g.part, if that is there, to be
 // joined with the other workgroups'. Workgroups of the launch from g.groups on, if there are any, take the sums by themselves.
-template <int kType, int kDyType, int kWavesPerRow, int kPieces>
+template <int kType, int kWavesPerRow, int kPieces>
 __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNormThreads) k_norm_back(NormBack g)
 {
     if (blockIdx.x >= g.groups) {
-        sum_columns<kType, kDyType, (kWavesPerRow > 4 ? kWavesPerRow * kWave : kNormThreads)>(g, blockIdx.x - g.groups);
+        sum_columns<kType, (kWavesPerRow > 4 ? kWavesPerRow * kWave : kNormThreads)>(g, blockIdx.x - g.groups);
         return;
     }
     constexpr u32 kWaves = kWavesPerRow > 4 ? kWavesPerRow : 4, kRows = kWaves / kWavesPerRow, kStep = 8u * kWave * kWavesPerRow;
@@ -281,14 +319,14 @@ __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNor
         for (int i = 0; i < 8; ++i) dgamma[p][i] = dbeta[p][i] = 0.0f;
     }
     Eight<kType> next_x[kPieces];
-    Eight<kDyType> next_dy[kPieces];
+    EightOf next_dy[kPieces];
     float next_mean, next_rstd;
     auto fetch = [&](u32 r) {
         const u64 row = min(r, g.rows - 1u);
 #pragma unroll
         for (int p = 0; p < kPieces; ++p) {
             next_x[p].load((const unsigned char *)g.x + row * g.ldx * Eight<kType>::kSize, c0 + p * kStep, g.cols);
-            next_dy[p].load((const unsigned char *)g.dy + row * g.lddy * Eight<kDyType>::kSize, c0 + p * kStep, g.cols);
+            next_dy[p].load((const unsigned char *)g.dy + row * g.lddy * size_of(g.dy_type), c0 + p * kStep, g.cols, g.dy_type);
         }
         next_mean = g.mean[row];
         next_rstd = g.rstd[row];
@@ -297,7 +335,7 @@ __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNor
     fetch(r);
     for (; r < g.rows; r += step, turn ^= 1u) {
         const unsigned char *x_row = (const unsigned char *)g.x + r * g.ldx * Eight<kType>::kSize;
-        const unsigned char *dy_row = (const unsigned char *)g.dy + r * g.lddy * Eight<kDyType>::kSize;
+        const unsigned char *dy_row = (const unsigned char *)g.dy + r * g.lddy * size_of(g.dy_type);
         const unsigned char *add_row = (const unsigned char *)g.add + r * g.ldadd * Eight<kType>::kSize;
         const float mean = next_mean, rstd = next_rstd;
         Eight<kType> held_add[kPieces];
@@ -310,7 +348,7 @@ __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNor
         for (int p = 0; p < kPieces; ++p) {
             const u32 c = c0 + p * kStep;
             next_x[p].numbers(h[p], x_row, c, g.cols);
-            next_dy[p].numbers(d[p], dy_row, c, g.cols);
+            next_dy[p].numbers(d[p], dy_row, c, g.cols, g.dy_type);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 h[p][i] = c + i < g.cols ? (h[p][i] - mean) * rstd : 0.0f;      // (d is zero there)
@@ -391,7 +429,7 @@ __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNor
 }
 
 // A longer row by one workgroup: its two means, then dx; dy and x are read twice, the second time from the caches.
-template <int kType, int kDyType>
+template <int kType>
 __global__ void __launch_bounds__(1024) k_norm_back_row(NormBack g)
 {
     constexpr int kWaves = 16;
@@ -399,18 +437,18 @@ __global__ void __launch_bounds__(1024) k_norm_back_row(NormBack g)
     const u64 r = (u64)blockIdx.y * gridDim.x + blockIdx.x;
     if (r >= g.rows) return;
     const unsigned char *x_row = (const unsigned char *)g.x + r * g.ldx * Eight<kType>::kSize;
-    const unsigned char *dy_row = (const unsigned char *)g.dy + r * g.lddy * Eight<kDyType>::kSize;
+    const unsigned char *dy_row = (const unsigned char *)g.dy + r * g.lddy * size_of(g.dy_type);
     const unsigned char *add_row = g.add ? (const unsigned char *)g.add + r * g.ldadd * Eight<kType>::kSize : nullptr;
     const float mean = g.mean[r], rstd = g.rstd[r];
     float h[8], d[8], gamma[8];
     auto read = [&](u32 c) {
         Eight<kType> ex;
-        Eight<kDyType> ey;
+        EightOf ey;
         ex.load(x_row, c, g.cols);
-        ey.load(dy_row, c, g.cols);
+        ey.load(dy_row, c, g.cols, g.dy_type);
         eight_or(gamma, g.gamma, c, g.cols, 1.0f);
         ex.numbers(h, x_row, c, g.cols);
-        ey.numbers(d, dy_row, c, g.cols);
+        ey.numbers(d, dy_row, c, g.cols, g.dy_type);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             h[i] = (h[i] - mean) * rstd;
@@ -445,7 +483,7 @@ __global__ void __launch_bounds__(1024) k_norm_back_row(NormBack g)
 // The sums of a run of rows, 512 columns a workgroup: a wavefront takes every fourth row.
 constexpr u32 kSumColumns = 8 * kWave;
 
-template <int kType, int kDyType>
+template <int kType>
 __global__ void __launch_bounds__(kNormThreads) k_norm_back_columns(NormBack g)
 {
     constexpr u32 kWaves = kNormThreads / kWave, kAtOnce = 4;
@@ -455,13 +493,13 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_back_columns(NormBack g)
     float dgamma[8] = {0, 0, 0, 0, 0, 0, 0, 0}, dbeta[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (u32 r = r0 + wave; r < r1; r += kAtOnce * kWaves) {
         Eight<kType> ex[kAtOnce];
-        Eight<kDyType> ey[kAtOnce];
+        EightOf ey[kAtOnce];
         float mean[kAtOnce], rstd[kAtOnce];
 #pragma unroll
         for (u32 q = 0; q < kAtOnce; ++q) {
             const u64 row = min(r + q * kWaves, r1 - 1u);
             ex[q].load((const unsigned char *)g.x + row * g.ldx * Eight<kType>::kSize, c, g.cols);
-            ey[q].load((const unsigned char *)g.dy + row * g.lddy * Eight<kDyType>::kSize, c, g.cols);
+            ey[q].load((const unsigned char *)g.dy + row * g.lddy * size_of(g.dy_type), c, g.cols, g.dy_type);
             mean[q] = g.mean[row];
             rstd[q] = g.rstd[row];
         }
@@ -471,7 +509,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_back_columns(NormBack g)
             const u64 row = r + q * kWaves;
             float x[8], d[8];
             ex[q].numbers(x, (const unsigned char *)g.x + row * g.ldx * Eight<kType>::kSize, c, g.cols);
-            ey[q].numbers(d, (const unsigned char *)g.dy + row * g.lddy * Eight<kDyType>::kSize, c, g.cols);
+            ey[q].numbers(d, (const unsigned char *)g.dy + row * g.lddy * size_of(g.dy_type), c, g.cols, g.dy_type);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 dgamma[i] = fmaf(d[i], (x[i] - mean[q]) * rstd[q], dgamma[i]);
@@ -579,15 +617,15 @@ u32 run_count(u32 rows, u32 cols) { return (rows + run_rows(rows, cols) - 1) / r
 // Small matrices: their sums cost less than a launch that joins them (the second read comes from the caches).
 bool small(u64 rows, u64 cols) { return rows <= 2048 && rows * cols <= 1u << 21; }
 
-template <int kType, int kDyType>
+template <int kType>
 int launch_held(const NormBack &g, u32 beside, hipStream_t stream)
 {
     const u32 cols = g.cols, grid = g.groups + beside;
-    if (cols <= 1024) k_norm_back<kType, kDyType, 1, 2><<<grid, kNormThreads, 0, stream>>>(g);
-    else if (cols <= 2048) k_norm_back<kType, kDyType, 4, 1><<<grid, kNormThreads, 0, stream>>>(g);
-    else if (cols <= 4096) k_norm_back<kType, kDyType, 4, 2><<<grid, kNormThreads, 0, stream>>>(g);
-    else if (cols <= 8192) k_norm_back<kType, kDyType, 8, 2><<<grid, 8 * kWave, 0, stream>>>(g);
-    else k_norm_back<kType, kDyType, 16, 2><<<grid, 16 * kWave, 0, stream>>>(g);
+    if (cols <= 1024) k_norm_back<kType, 1, 2><<<grid, kNormThreads, 0, stream>>>(g);
+    else if (cols <= 2048) k_norm_back<kType, 4, 1><<<grid, kNormThreads, 0, stream>>>(g);
+    else if (cols <= 4096) k_norm_back<kType, 4, 2><<<grid, kNormThreads, 0, stream>>>(g);
+    else if (cols <= 8192) k_norm_back<kType, 8, 2><<<grid, 8 * kWave, 0, stream>>>(g);
+    else k_norm_back<kType, 16, 2><<<grid, 16 * kWave, 0, stream>>>(g);
     return launched();
 }
 
@@ -597,7 +635,7 @@ int join_sums(const NormBack &g, hipStream_t stream)
     return launched();
 }
 
-template <int kType, int kDyType>
+template <int kType>
 int launch_back(NormBack g, hipStream_t stream)
 {
     const bool held = g.dx && g.cols <= kHeldColumns, direct = small(g.rows, g.cols);
@@ -606,36 +644,29 @@ int launch_back(NormBack g, hipStream_t stream)
     g.groups = held_groups(g.rows, g.cols, 2);
     float *const room = g.part;
     g.part = nullptr;
-    if (held && sums && direct && g.dx != g.x && g.dx != g.dy) return launch_held<kType, kDyType>(g, strips, stream);
+    if (held && sums && direct && g.dx != g.x && g.dx != g.dy) return launch_held<kType>(g, strips, stream);
     if (held && sums && !direct) {
         g.runs = g.groups;
         g.part = room;
-        if (const int rc = launch_held<kType, kDyType>(g, 0, stream)) return rc;
+        if (const int rc = launch_held<kType>(g, 0, stream)) return rc;
         return join_sums(g, stream);
     }
     // the sums first: dx may be x or dy
     if (sums && direct) {
-        k_norm_back_sums<kType, kDyType><<<strips, kNormThreads, 0, stream>>>(g);
+        k_norm_back_sums<kType><<<strips, kNormThreads, 0, stream>>>(g);
         if (const int rc = launched()) return rc;
     } else if (sums) {
         g.run = run_rows(g.rows, g.cols);
         g.runs = run_count(g.rows, g.cols);
         g.part = room;
-        k_norm_back_columns<kType, kDyType><<<dim3((g.cols + kSumColumns - 1) / kSumColumns, g.runs), kNormThreads, 0, stream>>>(g);
+        k_norm_back_columns<kType><<<dim3((g.cols + kSumColumns - 1) / kSumColumns, g.runs), kNormThreads, 0, stream>>>(g);
         if (const int rc = launched()) return rc;
         if (const int rc = join_sums(g, stream)) return rc;
     }
     g.part = nullptr;
-    if (held) return launch_held<kType, kDyType>(g, 0, stream);
-    if (g.dx) k_norm_back_row<kType, kDyType><<<row_grid(g.rows), 1024, 0, stream>>>(g);
+    if (held) return launch_held<kType>(g, 0, stream);
+    if (g.dx) k_norm_back_row<kType><<<row_grid(g.rows), 1024, 0, stream>>>(g);
     return launched();
-}
-
-template <int kType>
-int launch_back(const NormBack &g, int dy_type, hipStream_t stream)
-{
-    return dy_type == RTOPK_F32 ? launch_back<kType, RTOPK_F32>(g, stream)
-           : dy_type == RTOPK_BF16 ? launch_back<kType, RTOPK_BF16>(g, stream) : launch_back<kType, RTOPK_F16>(g, stream);
 }
 
 }  // namespace
@@ -691,8 +722,8 @@ extern "C" int rtopk_layer_norm_backward(const void *dy, int dy_type, const void
         }
         return RTOPK_OK;
     }
-    const NormBack g{dy, x, add, lddy, ldx, ldadd, (u32)rows, (u32)cols, mean, rstd, gamma, dx, lddx, 0, 0, 0,
+    const NormBack g{dy, x, add, dy_type, lddy, ldx, ldadd, (u32)rows, (u32)cols, mean, rstd, gamma, dx, lddx, 0, 0, 0,
                      dgamma, dbeta, (float *)workspace};
-    return type == RTOPK_F32 ? launch_back<RTOPK_F32>(g, dy_type, stream)
-           : type == RTOPK_BF16 ? launch_back<RTOPK_BF16>(g, dy_type, stream) : launch_back<RTOPK_F16>(g, dy_type, stream);
+    return type == RTOPK_F32 ? launch_back<RTOPK_F32>(g, stream)
+           : type == RTOPK_BF16 ? launch_back<RTOPK_BF16>(g, stream) : launch_back<RTOPK_F16>(g, stream);
 }
