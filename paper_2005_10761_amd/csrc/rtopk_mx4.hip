@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_sum_groups(const float *part, 
     out[c] = (float)sum;
 }
 
-// Back to numbers: eight of them a thread.
+// Back to numbers: a thread has the neighbours that make 16 bytes of the result, four or eight.
 struct ToUnpack {
     const unsigned char *q, *scale;
     u64 ldq, lds;
@@ -388,23 +388,27 @@ __device__ __forceinline__ float four_bit_value(u32 n)
     return __uint_as_float((n & 7u) << 22 | (n & 8u) << 28) * 8.50705917302346158658e37f;      // 2^126
 }
 
+// kShort: places fit 32 bits (a division of 64 bits is as long as all else)
+template <u32 kEach, bool kShort>
 __global__ void __launch_bounds__(256) k_unpack(ToUnpack g)
 {
-    const u32 each = (g.cols + 7u) / 8u;
+    typedef typename std::conditional<kShort, u32, u64>::type Place;
+    const u32 each = (g.cols + kEach - 1) / kEach;
     const u64 all = (u64)g.rows * each;
     for (u64 at = (u64)blockIdx.x * 256 + threadIdx.x; at < all; at += (u64)gridDim.x * 256) {
-        const u32 row = (u32)(at / each), c = (u32)(at - (u64)row * each) * 8u, have = g.cols - c;
+        const u32 row = (u32)((Place)at / each), c = (u32)(at - (u64)row * each) * kEach, have = g.cols - c;
         const unsigned char *q = g.q + row * g.ldq + c / 2u;
         u32 word = 0;
-        if (have >= 7u) __builtin_memcpy(&word, q, 4);
+        if (have + 1u >= kEach) __builtin_memcpy(&word, q, kEach / 2);
         else
             for (u32 i = 0; 2 * i < have; ++i) word |= (u32)q[i] << (8 * i);
         const u32 byte = g.scale[c / kBlock * g.lds + row];
         const float scale = byte == 255u ? __uint_as_float(0x7FC00000u) : scale_value(byte);
         f32x4 v[2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = four_bit_value(word >> (4 * i)) * scale;
-        write_eight(g.out, row * g.ldo + c, g.type, v[0], v[1], have);
+        for (int i = 0; i < (int)kEach; ++i) v[i >> 2][i & 3] = four_bit_value(word >> (4 * i)) * scale;
+        if (kEach == 4) write_four(g.out, row * g.ldo + c, g.type, v[0], have);
+        else write_eight(g.out, row * g.ldo + c, g.type, v[0], v[1], have);
     }
 }
 
@@ -934,8 +938,13 @@ extern "C" int rtopk_dequantize_mx4(const uint8_t *q, uint64_t rows, uint64_t co
     if (rows == 0 || cols == 0) return RTOPK_OK;
     if (!q || !scale || !out) return RTOPK_EINVAL;
     const ToUnpack g{q, scale, ldq, lds, (u32)rows, (u32)cols, out, type, ldo};
-    const u64 all = rows * ((cols + 7) / 8);
-    k_unpack<<<(unsigned)std::min<u64>((all + 255) / 256, 32 * kUnits), 256, 0, (hipStream_t)stream_v>>>(g);
+    hipStream_t stream = (hipStream_t)stream_v;
+    const bool fours = type == RTOPK_F32;
+    const u64 all = rows * (fours ? (cols + 3) / 4 : (cols + 7) / 8);
+    const u32 grid = (u32)std::min<u64>((all + 255) / 256, 32 * kUnits);
+    const bool fits = all + 256ull * grid < 1ull << 32;
+    if (fours) fits ? k_unpack<4, true><<<grid, 256, 0, stream>>>(g) : k_unpack<4, false><<<grid, 256, 0, stream>>>(g);
+    else fits ? k_unpack<8, true><<<grid, 256, 0, stream>>>(g) : k_unpack<8, false><<<grid, 256, 0, stream>>>(g);
     return launched();
 }
 
