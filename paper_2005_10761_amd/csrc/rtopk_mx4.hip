@@ -150,7 +150,7 @@ template <int kType, bool kDrawn, u32 kTileRows, u32 kThreads>
 __device__ __forceinline__ void pack_rows(const ToPack &g, u32 id)
 {
     constexpr u32 kWaves = kThreads / kWave, kEach = kTileRows / kWaves, kAtOnce = kEach < 4 ? kEach : 4;
-    __shared__ __align__(16) unsigned char scales[kTileBlocks][kTileRows];
+    __shared__ __align__(16) unsigned char scales[kTileBlocks][kTileRows + 4];      // (blocks start in different banks)
     const u32 lane = lane_id(), wave = threadIdx.x / kWave, tiles = (g.rows + kTileRows - 1) / kTileRows;
     const u32 place = xcd_place(id, row_tiles<kTileRows>(g)), tile = place % tiles, strip = place / tiles;
     const u32 r0 = tile * kTileRows + wave * kEach, c = strip * kTileColumns + lane * 8u;

@@ -113,17 +113,33 @@ struct Tile4 {
     // where the wavefront's load q begins in a stage; lane l's 16 bytes follow at 16 l
     static __device__ __forceinline__ u32 stage_at(int q) { return (u32)(q * kWaves + wave()) * 1024u; }
 
+    // A block's scales of kRows rows lie in LDS turned by so many: the four blocks that a step reads at the same rows, 64 bytes of each,
+    // fill the 64 banks (as they come, the reads of a 256-row tile meet four in a bank: a tenth of the cycles in which LDS works).
+    template <int kRows> static __device__ __forceinline__ u32 turned_by(u32 block)
+    {
+        return kRows == 256 ? 64u * (block & 3u) : kRows == 128 ? 64u * (block >> 1 & 1u) : 0u;
+    }
+    template <int kRows> static __device__ __forceinline__ u32 turned(u32 block, u32 row)
+    {
+        const u32 at = row + turned_by<kRows>(block);
+        return at < kRows ? at : at - kRows;
+    }
     // Where the wavefront's load q of scales begins among a stage's scales (lane l's four follow at 4 l), and what they are.
     static __device__ __forceinline__ u32 scales_at(int q) { return (u32)(q * kWaves + wave()) * 256u; }
     static __device__ __forceinline__ bool scales_of_a(int q) { return scales_at(q) < kBlocks * kM; }
     struct ScalePlace {
         u32 block, row;
     };
+    template <int kRows> static __device__ __forceinline__ ScalePlace unturned(u32 at)
+    {
+        const u32 block = at / kRows, row = at % kRows, by = turned_by<kRows>(block);
+        return {block, row >= by ? row - by : row + kRows - by};
+    }
     static __device__ __forceinline__ ScalePlace scale_place(int q)
     {
         const u32 at = scales_at(q) + 4u * lane_id();
-        if (at < kBlocks * kM) return {at / kM, at % kM};
-        if (at < kScales) return {(at - kBlocks * kM) / kN, (at - kBlocks * kM) % kN};
+        if (at < kBlocks * kM) return unturned<kM>(at);
+        if (at < kScales) return unturned<kN>(at - kBlocks * kM);
         return {0u, 0u};                                // (what fills the last loads)
     }
 
@@ -290,20 +306,20 @@ struct Tile4 {
         const u32 ra = row0() + (lane_id() & 15u), rb = kM + col0() + (lane_id() & 15u), piece = 4 * h + (lane_id() >> 4);
         const unsigned char *scales = stage + kData;
 #pragma unroll
-        for (int g = 0; g < GroupsN::kCount; ++g) f.b_scale[g] = read_scales<GroupsN>(scales + kBlocks * kM + piece * kN + col0(), g);
+        for (int g = 0; g < GroupsN::kCount; ++g) f.b_scale[g] = read_scales<GroupsN, kN>(scales + kBlocks * kM, piece, col0(), g);
 #pragma unroll
-        for (int g = 0; g < GroupsM::kCount; ++g) f.a_scale[g] = read_scales<GroupsM>(scales + piece * kM + row0(), g);
+        for (int g = 0; g < GroupsM::kCount; ++g) f.a_scale[g] = read_scales<GroupsM, kM>(scales, piece, row0(), g);
 #pragma unroll
         for (int j = 0; j < kFragsN; ++j) f.b[j] = *(const i32x4 *)(stage + place(rb + 16 * j, piece));
 #pragma unroll
         for (int i = 0; i < kFragsM; ++i) f.a[i] = *(const i32x4 *)(stage + place(ra + 16 * i, piece));
     }
-    // this lane's scales of a group of fragments, from the wavefront's first row of the block on
-    template <class G>
-    static __device__ __forceinline__ u32 read_scales(const unsigned char *p, int g)
+    // this lane's scales of a group of fragments, the wavefront's rows being `first` on (sizes divide what rows are turned by)
+    template <class G, int kRows>
+    static __device__ __forceinline__ u32 read_scales(const unsigned char *p, u32 block, u32 first, int g)
     {
         const int i = G::start(g);
-        p += 16 * i + G::size(i) * (lane_id() & 15u);
+        p += block * kRows + turned<kRows>(block, first + 16 * i + G::size(i) * (lane_id() & 15u));
         return G::size(i) == 4 ? *(const u32 *)p : G::size(i) == 2 ? *(const u16 *)p : *p;
     }
 
