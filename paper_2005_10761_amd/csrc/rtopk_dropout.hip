@@ -4,8 +4,8 @@
 //
 // u is a 16-bit draw of its own for each element: number e % 8 of the generator's group e / 8, e = row * cols + col. So the
 // mask depends on the element's place alone, not on strides or launches, the gradient is the same call on dy, and
-// what is kept is scaled by its true chance. One call of the generator for eight elements: 20 products of 16 cycles, 0.35 ns of a
-// compute unit for an element, under what 16-bit elements take to be read and written.
+// what is kept is scaled by its true chance. One call of the generator for eight elements, 20 products of 16 cycles, stays under what 16-bit
+// elements take to be read and written: bound by memory, 16384 x 4096 bfloat16 with a residual 77 us, 5.2 TB/s, without 48, 5.6 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -69,7 +69,8 @@ __device__ __forceinline__ T sum_of_row(T v, T *part)
 }
 
 // Rows by workgroups that keep going: kWavesPerRow wavefronts hold a row in registers, kPieces pieces of eight numbers a
-// lane, and gamma and beta for all of their rows; the next row is on its way while this one's mean and variance are taken.
+// lane, and gamma and beta for all of their rows; the next row is on its way while this one's mean and variance are taken. Bound by its read
+// and write: 16384 x 4096 bfloat16 48 to 53 us, 5.1 to 5.6 TB/s (a workgroup a row, which reads gamma and beta with each, 65); one row of 1500 2.9.
 template <int kType, int kWavesPerRow, int kPieces>
 __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNormThreads) k_norm(Norm g)
 {
@@ -298,7 +299,8 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_back_sums(NormBack g)
 // Rows by workgroups that keep going: kWavesPerRow wavefronts hold a row in registers, kPieces pieces of eight numbers a
 // lane, the next row's x and dy on their way while this one's means are taken and its dx is written. One read of everything,
 // one write: a lane's share of dgamma and dbeta stays in registers over all of its rows, and goes to g.part, if that is there, to be
-// joined with the other workgroups'. Workgroups of the launch from g.groups on, if there are any, take the sums by themselves.
+// joined with the other workgroups'. Workgroups of the launch from g.groups on, if there are any, take the sums by themselves. Bound by
+// memory: 16384 x 4096 bfloat16 with `add` 103 us, 5.2 TB/s (dx and the sums by a kernel each 240); 700 x 1500 9.6 us, sums beside.
 template <int kType, int kWavesPerRow, int kPieces>
 __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNormThreads) k_norm_back(NormBack g)
 {
@@ -540,7 +542,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_back_columns(NormBack g)
     }
 }
 
-// The runs together, in binary64, 16 columns a workgroup; blockIdx.y: dgamma, dbeta.
+// The runs together, in binary64, 16 columns a workgroup; blockIdx.y: dgamma, dbeta. 512 runs of 4096 columns 7 us, mostly from the caches.
 constexpr u32 kJoinColumns = 16, kJoinThreads = 1024;
 
 __global__ void __launch_bounds__(kJoinThreads) k_norm_back_join(NormBack g)

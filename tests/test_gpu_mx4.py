@@ -147,7 +147,7 @@ def test_every_16_bit_number(kind):
     """All of them but infinities and not-a-numbers, each by itself in a block with 1.5 2^e, and in blocks that a subnormal leads."""
     every = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(TYPES[kind])
     every = every[torch.isfinite(every)]
-    for lead in (1.5, 6.0, 2.0 ** -10, 2.0 ** -24):
+    for lead in (1.5, 6.0, 2.0 ** -10, 2.0 ** -24) + ((1.5 * 2.0 ** -124, 2.0 ** -126, 2.0 ** -130) if kind == "bf16" else ()):
         few = every[every.abs().double() <= lead]
         x = few[torch.randperm(len(few), generator=torch.Generator().manual_seed(1))]
         x = torch.nn.functional.pad(x, (0, -len(x) % 31)).view(-1, 31)
@@ -193,6 +193,17 @@ def test_products(kind, m, n, k):
         rt.matmul_mx4(ad, asd, bqd, bsd, out, bias=bd)
         check(out, kind, a, b, bias)
         assert bool((store[:, 0] == 7).all()) and bool((store[:, 1 + n:] == 7).all())
+
+
+def test_products_of_no_numbers():
+    q, s = torch.empty(4, 0, dtype=torch.uint8, device=DEV), torch.empty(0, 4, dtype=torch.uint8, device=DEV)
+    p, t = torch.empty(6, 0, dtype=torch.uint8, device=DEV), torch.empty(0, 6, dtype=torch.uint8, device=DEV)
+    bias, out = torch.randn(6, device=DEV), torch.empty(4, 6, device=DEV)
+    rt.matmul_mx4(q, s, p, t, out, bias=bias)
+    assert torch.equal(out, bias.expand(4, 6))
+    rt.matmul_mx4(q, s, p, t, out)
+    assert not out.any()
+    rt.dequantize_mx4(q, s, torch.empty(4, 0, device=DEV))
 
 
 def test_product_without_terms_is_the_bias():
