@@ -584,9 +584,15 @@ _ROUNDING = {"nearest": 0, "drawn": 1}
 _64_BITS = 2**64 - 1
 
 
-# the current device's number without the checks around it, where torch has it (without a GPU, one that no tensor is on)
-_CURRENT_DEVICE = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device) if torch.cuda.device_count() else lambda: -2
+# the current device's number without the checks around it, where torch has it
+_CURRENT_DEVICE = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _F32 = torch.float32
+
+
+def _device_with(t: torch.Tensor) -> int:
+    """The current device's number, asked for where ``t`` is on a GPU, so that there is one in use already: importing this
+    asks for none. Else a number that no tensor's device has."""
+    return _CURRENT_DEVICE() if t.is_cuda else -2
 
 
 def _rows(t: torch.Tensor, name: str, types, here: int) -> int:
@@ -645,7 +651,7 @@ def quantize_mx4(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, along: s
     numbers go up or down by chance, so that their mean is kept; ``step`` is an int, or one int64 on the GPU that is read when
     the kernel runs. Give ``q`` rows that start on 16 bytes and ``scale`` rows that start on 4 where the product is to
     read them fast."""
-    here = _CURRENT_DEVICE()
+    here = _device_with(x)
     ldx = _rows(x, "x", _TYPES, here)
     rows, cols = x.shape
     ldq, lds = _packed(q, scale, *((rows, cols) if along == "rows" else (cols, rows)), "q", here)
@@ -658,7 +664,7 @@ def quantize_mx4(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, along: s
 
 def dequantize_mx4(q: torch.Tensor, scale: torch.Tensor, out: torch.Tensor, stream=None) -> None:
     """rtopk_dequantize_mx4: the numbers of a matrix that :func:`quantize_mx4` left, ``out`` of ``q``'s rows."""
-    here = _CURRENT_DEVICE()
+    here = _device_with(out)
     ldo = _rows(out, "out", _TYPES, here)
     rows, cols = out.shape
     ldq, lds = _packed(q, scale, rows, cols, "q", here)
@@ -676,7 +682,7 @@ def matmul_mx4_workspace_bytes(m: int, n: int, k: int) -> int:
 def matmul_mx4(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor, out: torch.Tensor,
                bias: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """rtopk_matmul_mx4: out = a b^T (+ bias) of two quantised matrices of equal rows, out [a's rows, b's rows]."""
-    here = _CURRENT_DEVICE()
+    here = _device_with(out)
     ldo = _rows(out, "out", _TYPES, here)
     m, n = out.shape
     lda, lda_scale = _packed(a, a_scale, m, None, "a", here)
@@ -705,7 +711,7 @@ def linear_mx4(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, out: tor
                workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """rtopk_linear_mx4: out = x w^T + bias, ``x`` [m, k] quantised along rows on the way, ``w`` [n, (k + 1) // 2] with
     ``w_scale`` [(k + 31) // 32, n] as :func:`quantize_mx4` leaves them."""
-    here = _CURRENT_DEVICE()
+    here = _device_with(x)
     ldx, ldo = _rows(x, "x", _TYPES, here), _rows(out, "out", _TYPES, here)
     (m, k), n = x.shape, out.size(1)
     ldw, ldw_scale = _packed(w, w_scale, n, k, "w", here)
@@ -740,7 +746,7 @@ def linear_mx4_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w_turned: O
         raise ValueError("dx needs w_turned and its scales, dw needs x")
     if db is not None and dw is None:
         raise ValueError("db comes with dw")
-    here = _CURRENT_DEVICE()
+    here = _device_with(dy)
     lddy = _rows(dy, "dy", _TYPES, here)
     m, n = dy.shape
     k = (dx if dx is not None else dw).size(-1)
@@ -774,7 +780,7 @@ def layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[to
     """rtopk_layer_norm: out = (x - mean) rstd gamma + beta for each row of the matrix ``x``; ``gamma`` and ``beta``
     binary32 of a row's length (None: 1, 0). ``mean`` and ``rstd`` (binary32, one a row) are left for
     :func:`layer_norm_backward` where they are given. ``out`` may be ``x``."""
-    here = _CURRENT_DEVICE()
+    here = _device_with(x)
     ldx, ldo = _rows(x, "x", _TYPES, here), _rows(out, "out", _TYPES, here)
     rows, cols = x.shape
     if out.shape != x.shape:
@@ -808,7 +814,7 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, r
         raise ValueError("neither dx nor dgamma nor dbeta is asked for")
     if add is not None and dx is None:
         raise ValueError("add comes with dx")
-    here = _CURRENT_DEVICE()
+    here = _device_with(x)
     lddy, ldx, lddx, ldadd = _rows(dy, "dy", _TYPES, here), _rows(x, "x", _TYPES, here), 0, 0
     shape = rows, cols = x.shape
     if dx is not None:
@@ -842,7 +848,7 @@ def dropout(x: torch.Tensor, out: torch.Tensor, p: float, seed: int, step, resid
     by 1 / (1 - p), plus ``residual`` (of ``out``'s type). The mask belongs to ``seed``, ``step`` (an int, or one int64 on
     the GPU that is read when the kernel runs) and the element's place: the gradient is the same call on ``out``'s.
     ``out`` may be ``x`` or ``residual``."""
-    here = _CURRENT_DEVICE()
+    here = _device_with(x)
     ldx, ldo = _rows(x, "x", _TYPES, here), _rows(out, "out", _TYPES, here)
     ldr = 0 if residual is None else _rows(residual, "residual", (out.dtype,), here)
     shape = rows, cols = x.shape
