@@ -545,11 +545,12 @@ int rtopk_linear_mx4_backward(const void *dy, const void *x, int type,
  * Layer norm over the rows of a matrix, what stands before a layer's product:
  *     mean = sum x / cols,  rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps)
  *     out  = (x - mean) rstd gamma + beta
- * in binary32 (rows of more than 16384 numbers are summed in binary64).
+ * in binary32 (rows of more than 16384 numbers are summed in binary64), off by
+ * roundings of x - mean, however far the mean is from zero.
  *
  * x      device, [rows][ldx] of `type`, rows 0 .. 2^22, cols 1 .. 2^22 <= ldx <= 2^22
  * gamma, beta  device, [cols] binary32, or null: 1, 0
- * eps    >= 0. (A row of equal numbers with eps = 0 gives NaN.)
+ * eps    >= 0. (A row of equal numbers gives beta; with eps = 0 it gives NaN.)
  * out    device, [rows][ldo] of out_type, ldo <= 2^22; may be x itself (types
  *        of one size, ldo = ldx), else must not overlap an input
  * mean, rstd  device, [rows] binary32 each, for the backward pass; or null
