@@ -753,6 +753,8 @@ int run_pack_rows(const ToPack &g, int type, bool drawn, hipStream_t stream)
 
 u32 turn_groups(u32 rows) { return (rows + kTurnRows - 1) / kTurnRows; }
 
+constexpr u32 kMostAlongY = (1u << 16) - 1;
+
 // `count` matrices along columns, and `rows`, if not null, along rows.
 int run_pack_columns(const Turns &t, u32 count, const ToPack *rows, int type, hipStream_t stream)
 {
@@ -761,7 +763,12 @@ int run_pack_columns(const Turns &t, u32 count, const ToPack *rows, int type, hi
         grid.x = std::max(grid.x, (t.of[i].of.cols + kWave - 1) / kWave);
         grid.y = std::max(grid.y, turn_groups(t.of[i].of.fill));
     }
-    if (rows) grid.y = std::max(grid.y, (row_tiles<kBesideRows>(*rows) + grid.x - 1) / grid.x);
+    if (rows) {
+        // (a launch has less than 2^16 workgroups along y: 2^22 rows of few numbers take two along x)
+        const u32 tiles = row_tiles<kBesideRows>(*rows);
+        grid.x = std::max(grid.x, (tiles + kMostAlongY - 1) / kMostAlongY);
+        grid.y = std::max(grid.y, (tiles + grid.x - 1) / grid.x);
+    }
     const ToPack other = rows ? *rows : ToPack{};
     if (type == RTOPK_F32) k_pack_columns<RTOPK_F32><<<grid, kTurnThreads, 0, stream>>>(t, other);
     else if (type == RTOPK_BF16) k_pack_columns<RTOPK_BF16><<<grid, kTurnThreads, 0, stream>>>(t, other);
