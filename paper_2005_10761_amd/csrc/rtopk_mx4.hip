@@ -531,12 +531,10 @@ __global__ void __launch_bounds__(T::kThreads) k_product4(Product4 g)
     const u32 i0 = ti * T::kRowsM, j0 = tj * T::kRowsN, bytes = (g.k + 1u) / 2u;
     const TileRows4 a{g.a + i0 * g.lda, g.m - i0, (u32)g.lda, g.a_scale + i0, (u32)g.lda_scale};
     const TileRows4 b{g.b + j0 * g.ldb, g.n - j0, (u32)g.ldb, g.b_scale + j0, (u32)g.ldb_scale};
-    // (runs are counted in slices, of which a unit is a whole or a half)
-    constexpr u32 kPerSlice = kSlice / T::kRow;
-    const u32 units = (bytes + T::kRow - 1) / T::kRow, from = split * g.slices_each * kPerSlice;
+    const u32 slices = (bytes + kSlice - 1) / kSlice, from = split * g.slices_each;
     T t;
     t.clear();
-    t.template multiply<kWhole>(a, b, bytes, from, min(from + g.slices_each * kPerSlice, units), lds);
+    t.template multiply<kWhole>(a, b, bytes, from, min(from + g.slices_each, slices), lds);
     const bool last = g.splits == 1;
     const u64 ld = last ? g.ldo : align_up(g.n, 4);
     void *out = last ? g.out : (void *)(g.part + (u64)split * g.m * ld);
@@ -824,10 +822,10 @@ Plan plan_product(u32 m, u32 n, u32 k, bool on_lines)
 // what a product of these sizes may need for the runs' sums, however its rows lie
 u64 part_bytes(u32 m, u32 n, u32 k) { return std::max(plan_product(m, n, k, false).part_bytes, plan_product(m, n, k, true).part_bytes); }
 
-template <int kEdge, int kSteps, int kStages>
+template <int kEdge, int kStages>
 void launch_product4(const Product4 &g, const Plan &p, bool whole, hipStream_t stream)
 {
-    typedef Tile4<kEdge, kEdge, 2, 4, kSteps, kStages> T;
+    typedef Tile4<kEdge, kEdge, 2, 4, kStages> T;
     if (whole) k_product4<T, true><<<p.tiles * p.splits, T::kThreads, 0, stream>>>(g);
     else k_product4<T, false><<<p.tiles * p.splits, T::kThreads, 0, stream>>>(g);
 }
@@ -840,10 +838,10 @@ int run_product4(Product4 g, void *part, hipStream_t stream)
     g.part = (float *)part;
     const bool whole = (((uintptr_t)g.a | (uintptr_t)g.b | g.lda | g.ldb) & 15u) == 0 &&
                        (((uintptr_t)g.a_scale | (uintptr_t)g.b_scale | g.lda_scale | g.ldb_scale) & 3u) == 0;
-    if (p.edge == 256) launch_product4<256, 2, 2>(g, p, whole, stream);
-    else if (p.edge == 192) launch_product4<192, 2, 2>(g, p, whole, stream);
-    else if (p.edge == 128) launch_product4<128, 2, 2>(g, p, whole, stream);
-    else launch_product4<64, 2, 4>(g, p, whole, stream);
+    if (p.edge == 256) launch_product4<256, 2>(g, p, whole, stream);
+    else if (p.edge == 192) launch_product4<192, 2>(g, p, whole, stream);
+    else if (p.edge == 128) launch_product4<128, 2>(g, p, whole, stream);
+    else launch_product4<64, 4>(g, p, whole, stream);
     if (const int rc = launched()) return rc;
     if (p.splits > 1) {
         const u64 blocks = ((u64)g.m * ((g.n + 3) / 4) + 255) / 256;

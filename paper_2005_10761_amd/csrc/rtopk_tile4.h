@@ -41,11 +41,12 @@ template <int kFrags> struct Groups {
     static __device__ __forceinline__ u32 row(int i, u32 r) { return 16u * first(i) + size(i) * r + (i - first(i)); }
 };
 
-// A tile of kM x kN sums on kWavesM x kWavesN wavefronts. The contraction goes in units of kSteps instructions; kStages units
-// lie in LDS, and the fragments of the next step are read into registers while this one's are multiplied.
-template <int kM, int kN, int kWavesM, int kWavesN, int kSteps, int kStages>
+// A tile of kM x kN sums on kWavesM x kWavesN wavefronts. The contraction goes in units of two instructions, a slice of 128 bytes of
+// every row; kStages units lie in LDS, and the fragments of the next step are read into registers while this one's are multiplied.
+// (Units of one instruction, four in LDS: 2048 x 16384 x 4096 82 us, these 76.)
+template <int kM, int kN, int kWavesM, int kWavesN, int kStages>
 struct Tile4 {
-    static constexpr int kRowsM = kM, kRowsN = kN;
+    static constexpr int kRowsM = kM, kRowsN = kN, kSteps = 2;
     static constexpr int kWaves = kWavesM * kWavesN, kThreads = kWaves * kWave;
     static constexpr int kRow = kSteps * kStepBytes, kPieces = kRow / 16;        // bytes of a row in a unit, in pieces of 16
     static constexpr int kBlocks = kSteps * kStepBlocks;
@@ -61,7 +62,7 @@ struct Tile4 {
     static_assert(kLoads * kWaves * kTogether == kM + kN && kM % kTogether == 0, "every wavefront loads whole groups of rows of one operand");
     static_assert(kFragsM * kWavesM * 16 == kM && kFragsN * kWavesN * 16 == kN, "whole instructions");
     static_assert(kBlocks * kM % 256 == 0, "a load of scales is of one operand");
-    static_assert(kSteps == 1 || kSteps == 2, "two layouts of a row in LDS");
+    static_assert(kRow == kSlice, "a unit is a slice");
     static_assert(kStages >= 2 && kStages % 2 == 0 && kLds <= 160 * 1024, "stages");
 
     // sum[i][j]: row row_at(i) of A, rows of B by result_column()
@@ -93,9 +94,8 @@ struct Tile4 {
 
     // LDS holds a unit as rows of pieces of 16 bytes; piece c of row r lies in place c ^ turn(r). A 16-byte read takes sixteen
     // lanes at a time, not in their order: 0-3, 12-15, 20-23, 24-27 (eight rows of one piece, eight others of the next) and so
-    // on. The turn puts what they read into sixteen different places of the 64 banks, which four rows of four pieces or two
-    // of eight fill.
-    static __device__ __forceinline__ u32 turn(u32 row) { return kSteps == 1 ? 3u * (row >> 3 & 1u) : (row & 2u) | ((row >> 1) & 4u); }
+    // on. The turn puts what they read into sixteen different places of the 64 banks, which two rows of eight pieces fill.
+    static __device__ __forceinline__ u32 turn(u32 row) { return (row & 2u) | ((row >> 1) & 4u); }
     static __device__ __forceinline__ u32 place(u32 row, u32 piece) { return row * kRow + ((piece ^ turn(row)) << 4); }
 
     // A unit's rows lie in LDS as the fragments take them: of A, then of B. Load q of this lane: its row there, and of its operand.
@@ -214,52 +214,28 @@ struct Tile4 {
             else wait_and_meet<0>();
             Step even, odd;
             read(even, stage(u), 0);
-            // From a unit whose first step's fragments are in `now`, to the next one's in `now` (two steps) or `after` (one).
-            // A barrier says that everybody has read all of this unit, and that the next one has come; then this one's stage is
-            // loaded again. (Copies of a unit's work, so that none of them branches: a branch stops the reads from going
-            // between the products.)
-            auto pass = [&](Step &now, Step &after, bool more, u32 under_way) __attribute__((always_inline)) {
-                if constexpr (kSteps == 2) {
-                    read(after, stage(u), 1);
-                    add(now);
-                    mix<0>();
-                }
+            // From a unit whose first step's fragments are in `even` to the next one's. A barrier says that everybody has read all of
+            // this unit, and that the next one has come; then this one's stage is loaded again. (Copies of a unit's work, so that
+            // none of them branches: a branch stops the reads from going between the products.)
+            auto pass = [&](bool more, u32 under_way) __attribute__((always_inline)) {
+                read(odd, stage(u), 1);
+                add(even);
+                mix<0>();
                 if (more) wait_and_meet<(kStages - 2) * kAllLoads>();
                 else wait_and_meet_for(under_way);
                 if (more) load(u + kStages);
-                if constexpr (kSteps == 2) {
-                    read(now, stage(u + 1), 0);
-                    add(after);
-                } else {
-                    read(after, stage(u + 1), 0);
-                    add(now);
-                }
+                read(even, stage(u + 1), 0);
+                add(odd);
                 if (more) mix<kAllLoads>();
                 else mix<0>();
                 ++u;
             };
-            if constexpr (kSteps == 2) {
-                while (u + kStages < whole) pass(even, odd, true, 0);
-                while (u + 1 < whole) pass(even, odd, false, whole - u - 2);
-                read(odd, stage(u), 1);
-                add(even);
-                mix<0>();
-                add(odd);
-            } else {
-                while (u + kStages + 1 < whole) {
-                    pass(even, odd, true, 0);
-                    pass(odd, even, true, 0);
-                }
-                if (u + kStages < whole) {
-                    pass(even, odd, true, 0);
-                    even = odd;
-                }
-                while (u + 1 < whole) {
-                    pass(even, odd, false, whole - u - 2);
-                    even = odd;
-                }
-                add(even);
-            }
+            while (u + kStages < whole) pass(true, 0);
+            while (u + 1 < whole) pass(false, whole - u - 2);
+            read(odd, stage(u), 1);
+            add(even);
+            mix<0>();
+            add(odd);
             ++u;
         }
         const u32 blocks = (bytes + kBlockBytes - 1) / kBlockBytes;
