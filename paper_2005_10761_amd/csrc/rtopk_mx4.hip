@@ -136,8 +136,8 @@ __device__ __forceinline__ u32 groups_of(u32 k) { return (k + kBlock - 1) / kBlo
 
 // Along rows: a workgroup has kTileRows rows and 512 columns, a lane eight neighbours of a row, four lanes a block. The scales
 // lie the other way: they are put together in LDS, kTileRows bytes of each block, and workgroups of neighbouring rows are on
-// one XCD, so that its L2 has whole lines of them. Bound by its one read and one write: 16384 x 4096 binary32 52 us, 5.8 TB/s; 8192 x 4096
-// bfloat16 17.4 us, 4.9 TB/s (16 rows a workgroup 18.1; eight rows of a wavefront under way instead of four 19.3).
+// one XCD, so that its L2 has whole lines of them. Bound by its one read and one write: 16384 x 4096 binary32 53 us, 5.7 TB/s; 8192 x 4096
+// bfloat16 16 us, 5.2 TB/s.
 constexpr int kPackThreads = 256;
 constexpr u32 kTileColumns = 8 * kWave, kTileBlocks = kTileColumns / kBlock;
 
@@ -729,18 +729,21 @@ u64 blocks_of(u64 k) { return (k + kBlock - 1) / kBlock; }
 // a quantised operand [rows][k]: the distances of its rows and of its scales' blocks
 bool packed_ok(u64 rows, u64 k, u64 ldq, u64 lds) { return ldq >= bytes_of(k) && ldq <= kMostSize && lds >= rows && lds <= kMostSize; }
 
-template <int kType, u32 kTileRows>
-void launch_pack_rows(const ToPack &g, bool drawn, hipStream_t stream)
-{
-    if (drawn) k_pack_rows<kType, true, kTileRows><<<row_tiles<kTileRows>(g), kPackThreads, 0, stream>>>(g);
-    else k_pack_rows<kType, false, kTileRows><<<row_tiles<kTileRows>(g), kPackThreads, 0, stream>>>(g);
-}
+// 64 rows a workgroup where binary32 is rounded to the nearest, a row is longer than there are rows, and two workgroups a unit are
+// left; 16 elsewhere. us with 16 and with 64, of matrices that come from memory: binary32 4096 x 16384 66.0 / 61.4, 2048 x 16384 33.1 / 30.6,
+// 4096 x 8192 32.2 / 30.6; but 4096 x 4096 14.8 / 15.9, 16384 x 4096 53.2 / 57.7, drawn 4096 x 16384 66.5 / 68.6, 4096 x 8192 34.5 / 37.5;
+// bfloat16 4096 x 16384 35.0 / 36.0, 2048 x 16384 18.6 / 17.7, 8192 x 4096 16.2 / 16.7, drawn 21.9 / 23.7.
 template <int kType>
 int run_pack_rows(const ToPack &g, bool drawn, hipStream_t stream)
 {
-    // 64 rows where that leaves two workgroups a unit
-    if (row_tiles<64>(g) >= 2 * kUnits) launch_pack_rows<kType, 64>(g, drawn, stream);
-    else launch_pack_rows<kType, 16>(g, drawn, stream);
+    if constexpr (kType == RTOPK_F32) {
+        if (!drawn && g.cols > g.rows && row_tiles<64>(g) >= 2 * kUnits) {
+            k_pack_rows<kType, false, 64><<<row_tiles<64>(g), kPackThreads, 0, stream>>>(g);
+            return launched();
+        }
+    }
+    if (drawn) k_pack_rows<kType, true, 16><<<row_tiles<16>(g), kPackThreads, 0, stream>>>(g);
+    else k_pack_rows<kType, false, 16><<<row_tiles<16>(g), kPackThreads, 0, stream>>>(g);
     return launched();
 }
 int run_pack_rows(const ToPack &g, int type, bool drawn, hipStream_t stream)
