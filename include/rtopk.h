@@ -459,7 +459,9 @@ int rtopk_aggregate_update_orthogonal(uint32_t count, const uint32_t *const *idx
  * key (seed_lo, seed_hi), g = row * 4 * blocks + c / 8 by the row and column c
  * of q, what = 2 along rows, 3 along columns. `step_device`, if not null, is a
  * device uint64 that the step number is read from when the kernels run: a graph that is
- * replayed advances it, and each replay draws afresh.
+ * replayed advances it, and each replay draws afresh. A draw belongs to seed,
+ * step and place alone: matrices that are to be drawn independently, as those
+ * of two layers in one step, need seeds of their own.
  *
  * x      device, [rows][ldx] of `type`, rows 0 .. 2^22, cols 1 .. 2^22 <= ldx <= 2^22
  * along  RTOPK_ROWS: q [rows][ldq], scale [(cols + 31) / 32][lds]; RTOPK_COLUMNS:
@@ -521,7 +523,7 @@ int rtopk_linear_mx4(const void *x, int type, uint64_t m, uint64_t k, uint64_t l
  *     dw = dy^T x      both quantised along columns (over the tokens)
  *     db = sum of dy's rows, in binary32 or more
  * x is quantised to the nearest, dy by `rounding` with seed and step as in
- * rtopk_quantize_mx4.
+ * rtopk_quantize_mx4: a seed of its own for each layer.
  *
  * dy, x  device, [m][lddy] and [m][ldx] of `type`
  * w_turned, w_turned_scale  device, k rows of n numbers: the weights [n][k]
@@ -594,7 +596,9 @@ int rtopk_layer_norm_backward(const void *dy, int dy_type, const void *x, int ty
  * Draws: element e = row * cols + col has number e % 8 of the eight 16-bit
  * numbers of counter (g_lo, 1 << 24 | g_hi, step_lo, step_hi), g = e / 8, as
  * above. They do not depend on how the rows lie, and differ from those of
- * rtopk_encode and rtopk_quantize_mx4 with the same seed and step.
+ * rtopk_encode and rtopk_quantize_mx4 with the same seed and step. Two calls
+ * with the same seed and step have the same mask, as forward and backward need
+ * it; each place of a network needs a seed of its own.
  *
  * x      device, [rows][ldx] of `type`
  * residual  device, [rows][ldr] of out_type, or null

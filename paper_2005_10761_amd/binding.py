@@ -649,7 +649,7 @@ def quantize_mx4(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, along: s
     for each block of 32. Along rows ``q`` is [rows, (cols + 1) // 2] and ``scale`` [(cols + 31) // 32, rows]; along
     columns ``x`` is turned over, ``q`` [cols, (rows + 1) // 2] and ``scale`` [(rows + 31) // 32, cols]. With a ``seed``
     numbers go up or down by chance, so that their mean is kept; ``step`` is an int, or one int64 on the GPU that is read when
-    the kernel runs. Give ``q`` rows that start on 16 bytes and ``scale`` rows that start on 4 where the product is to
+    the kernel runs. Draws belong to seed, step and place: matrices of one step need seeds of their own. Give ``q`` rows that start on 16 bytes and ``scale`` rows that start on 4 where the product is to
     read them fast."""
     here = _device_with(x)
     ldx = _rows(x, "x", _TYPES, here)
@@ -739,7 +739,8 @@ def linear_mx4_backward(dy: torch.Tensor, x: Optional[torch.Tensor], w_turned: O
                         workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """rtopk_linear_mx4_backward: the gradients of :func:`linear_mx4`'s input, weights (binary32, [n, k]) and bias from
     ``dy`` [m, n]. ``w_turned`` [k, (n + 1) // 2] and its scales: the weights quantised along columns. With a ``seed``
-    ``dy`` is rounded by chance, as :func:`quantize_mx4` does. ``dx`` or ``dw`` may be None, and then what only they need too."""
+    ``dy`` is rounded by chance, as :func:`quantize_mx4` does; each layer needs a seed of its own, or its draws are another
+    layer's. ``dx`` or ``dw`` may be None, and then what only they need too."""
     if dx is None and dw is None:
         raise ValueError("neither dx nor dw is asked for")
     if dx is not None and (w_turned is None or w_turned_scale is None) or dw is not None and x is None:
@@ -846,7 +847,8 @@ def dropout(x: torch.Tensor, out: torch.Tensor, p: float, seed: int, step, resid
             stream=None) -> None:
     """rtopk_dropout: out = x with each element dropped with chance ``p`` (a whole number of 65536ths), the others scaled
     by 1 / (1 - p), plus ``residual`` (of ``out``'s type). The mask belongs to ``seed``, ``step`` (an int, or one int64 on
-    the GPU that is read when the kernel runs) and the element's place: the gradient is the same call on ``out``'s.
+    the GPU that is read when the kernel runs) and the element's place: the gradient is the same call on ``out``'s, and
+    each place of a network needs a seed of its own, or its mask is another's.
     ``out`` may be ``x`` or ``residual``."""
     here = _device_with(x)
     ldx, ldo = _rows(x, "x", _TYPES, here), _rows(out, "out", _TYPES, here)
