@@ -2,9 +2,10 @@
 //
 //   forward    mean = sum x / c, rstd = (sum (x - mean)^2 / c + eps)^-1/2,
 //              y = (x - mean) rstd gamma + beta
-//              A sum's roundings are off by parts of x, not of what varies around the mean: with m the mean that it gives and
-//              d = x - m, what is left is e = sum d / c, so that mean = m + e, sum (x - mean)^2 = sum d^2 - e sum d and
-//              x - mean = d - e, off by parts of d. Where all numbers are equal, d is e, and y beta.
+//              A sum's roundings are off by parts of x, not of what varies around the mean. Where the mean is larger than that:
+//              with m the mean that the sum gives and d = x - m, what is left is e = sum d / c, and mean = m + e,
+//              x - mean = d - e, off by parts of d. (Where all numbers are equal, d is e, and y beta. Where the mean is smaller,
+//              e would only add the roundings of d, which lean one way.)
 //   backward   h = (x - mean) rstd, g = dy gamma:
 //              dx = rstd (g - mean(g) - h mean(g h)) (+ add)
 //              dgamma = sum over rows of dy h, dbeta = sum over rows of dy
@@ -48,54 +49,40 @@ __device__ __forceinline__ void eight_or(float (&v)[8], const float *p, u32 c, u
     }
 }
 
-// The sums of kCount numbers of each lane of the kWavesPerRow wavefronts that share a row; `part` has a place for each of a
-// workgroup's wavefronts.
-template <int kWavesPerRow, class T, int kCount, int kWaves>
-__device__ __forceinline__ void sums_of_row(T (&v)[kCount], T (&part)[kCount][kWaves])
+// The sum of one number of each lane of the kWavesPerRow wavefronts that share a row; `part` has a place for each wavefront.
+template <int kWavesPerRow, class T>
+__device__ __forceinline__ T sum_of_row(T v, T *part)
 {
+    T sum;
+    if constexpr (sizeof(T) == 4) {
+        sum = wave_sum_f32(v);
+    } else {
+        sum = v;
 #pragma unroll
-    for (int n = 0; n < kCount; ++n) {
-        if constexpr (sizeof(T) == 4) {
-            v[n] = wave_sum_f32(v[n]);
-        } else {
-#pragma unroll
-            for (int o = kWave / 2; o > 0; o >>= 1) v[n] += __shfl_xor(v[n], o, kWave);
-        }
+        for (int o = kWave / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
     }
     if constexpr (kWavesPerRow > 1) {
         const u32 wave = threadIdx.x / kWave, first = wave / kWavesPerRow * kWavesPerRow;
-        if (lane_id() == 0) {
-#pragma unroll
-            for (int n = 0; n < kCount; ++n) part[n][wave] = v[n];
-        }
+        if (lane_id() == 0) part[wave] = sum;
         lds_barrier();
+        sum = 0;
 #pragma unroll
-        for (int n = 0; n < kCount; ++n) {
-            v[n] = 0;
-#pragma unroll
-            for (u32 w = 0; w < kWavesPerRow; ++w) v[n] += part[n][first + w];
-        }
+        for (u32 w = 0; w < kWavesPerRow; ++w) sum += part[first + w];
     }
-}
-
-// The sum of squares around the mean, of sum d, sum d^2 and e = sum d / c: not below zero, where the two are equal but for a
-// rounding; beyond binary32's largest as sum d^2 is. (What is not a number stays that.)
-template <class T> __device__ __forceinline__ T squares_around(T sum, T squares, T e)
-{
-    const T around = fma(-sum, e, squares);
-    return isinf(squares) ? squares : around < 0 ? (T)0 : around;
+    return sum;
 }
 
 // Rows by workgroups that keep going: kWavesPerRow wavefronts hold a row in registers, kPieces pieces of eight numbers a
 // lane, and gamma and beta for all of their rows; the next row is on its way while this one's mean and variance are taken. Bound by its read
-// and write: 16384 x 4096 bfloat16 48 to 53 us, 5.1 to 5.6 TB/s (a workgroup a row, which reads gamma and beta with each, 65); one row of 1500 2.9.
+// and write: 16384 x 4096 bfloat16 48 to 53 us, 5.1 to 5.6 TB/s (a workgroup a row, which reads gamma and beta with each, 65); one row of 1500 2.9. Rows whose mean is larger than their
+// standard deviation take two sums more: 53, 3.1.
 template <int kType, int kWavesPerRow, int kPieces>
 __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNormThreads) k_norm(Norm g)
 {
     constexpr u32 kWaves = kWavesPerRow > 4 ? kWavesPerRow : 4, kRows = kWaves / kWavesPerRow, kStep = 8u * kWave * kWavesPerRow;
-    __shared__ float first_part[2][1][kWaves], part[2][2][kWaves];
+    __shared__ float part[8][kWaves];
     const u32 lane = lane_id(), wave = threadIdx.x / kWave, c0 = (wave % kWavesPerRow * kWave + lane) * 8u, step = gridDim.x * kRows;
-    const float cols = (float)g.cols, per_row = 1.0f / cols;
+    const float cols = (float)g.cols;
     Eight<kType> next[kPieces];
     auto fetch = [&](u32 r) {
         const unsigned char *row = (const unsigned char *)g.x + min(r, g.rows - 1u) * g.ldx * Eight<kType>::kSize;
@@ -110,39 +97,46 @@ __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNor
         eight_or(gamma[p], g.gamma, c0 + p * kStep, g.cols, 1.0f);
         eight_or(beta[p], g.beta, c0 + p * kStep, g.cols, 0.0f);
     }
-    for (; r < g.rows; r += step, turn ^= 1u) {
+    for (; r < g.rows; r += step, turn ^= 4u) {
         const unsigned char *row = (const unsigned char *)g.x + r * g.ldx * Eight<kType>::kSize;
-        float x[kPieces][8], first[1] = {0}, sums[2] = {0, 0};
+        float x[kPieces][8], sum = 0, squares = 0;
 #pragma unroll
         for (int p = 0; p < kPieces; ++p) {
             next[p].numbers(x[p], row, c0 + p * kStep, g.cols);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) first[0] += x[p][i];
+            for (int i = 0; i < 8; ++i) sum += x[p][i];
         }
         if (r + step < g.rows) fetch(r + step);
-        // (places in turn: a wavefront that is a row ahead has passed both of this row's barriers)
-        sums_of_row<kWavesPerRow>(first, first_part[turn]);
-        const float m = first[0] * per_row;
+        // around `by`, and the squares of that
+        auto around = [&](float by) {
+            squares = 0;
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
-            const u32 c = c0 + p * kStep;
-            if (c >= g.cols) continue;
+            for (int p = 0; p < kPieces; ++p)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[p][i] -= m;
-            if (c + 8 > g.cols) {
+                for (int i = 0; i < 8; ++i) {
+                    x[p][i] = c0 + p * kStep + i < g.cols ? x[p][i] - by : 0.0f;
+                    squares = fmaf(x[p][i], x[p][i], squares);
+                }
+        };
+        // (places in turn: a wavefront that is a row ahead has passed all of this row's barriers)
+        float mean = sum_of_row<kWavesPerRow>(sum, part[turn]) / cols;
+        around(mean);
+        squares = sum_of_row<kWavesPerRow>(squares, part[turn + 1]);
+        // (the same in all of a row's wavefronts; what is beyond binary32's range counts as a larger mean)
+        if (__builtin_amdgcn_readfirstlane(!(mean * mean * cols < squares))) {
+            sum = 0;
 #pragma unroll
-                for (int i = 1; i < 8; ++i) x[p][i] = c + i < g.cols ? x[p][i] : 0.0f;
-            }
+            for (int p = 0; p < kPieces; ++p)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                sums[0] += x[p][i];
-                sums[1] = fmaf(x[p][i], x[p][i], sums[1]);
-            }
+                for (int i = 0; i < 8; ++i) sum += x[p][i];
+            const float e = sum_of_row<kWavesPerRow>(sum, part[turn + 2]) / cols;
+            around(e);
+            squares = sum_of_row<kWavesPerRow>(squares, part[turn + 3]);
+            mean += e;
         }
-        sums_of_row<kWavesPerRow>(sums, part[turn]);
-        const float e = sums[0] / cols, rstd = 1.0f / sqrtf(fmaf(squares_around(sums[0], sums[1], e), per_row, g.eps));
+        const float rstd = 1.0f / sqrtf(squares / cols + g.eps);
         if (c0 == 0) {
-            if (g.mean) g.mean[r] = m + e;
+            if (g.mean) g.mean[r] = mean;
             if (g.rstd) g.rstd[r] = rstd;
         }
 #pragma unroll
@@ -151,18 +145,19 @@ __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNor
             if (c >= g.cols) continue;
             f32x4 y[2];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i >> 2][i & 3] = fmaf((x[p][i] - e) * rstd, gamma[p][i], beta[p][i]);
+            for (int i = 0; i < 8; ++i) y[i >> 2][i & 3] = fmaf(x[p][i] * rstd, gamma[p][i], beta[p][i]);
             write_eight(g.out, r * g.ldo + c, g.out_type, y[0], y[1], g.cols - c);
         }
     }
 }
 
-// A longer row by one workgroup: it is read three times (the second and third time from the caches), with sums in binary64.
+// A longer row by one workgroup: it is read three times (the second and third time from the caches), with sums in binary64; e is what
+// m loses of the mean as binary32. 2000 x 20,000 binary32 95 us, 3.4 TB/s, 256 x 262,144 bfloat16 105, 2.6.
 template <int kType>
 __global__ void __launch_bounds__(1024) k_norm_row(Norm g)
 {
     constexpr int kWaves = 16;
-    __shared__ double first_part[1][kWaves], part[2][kWaves];
+    __shared__ double part[2][kWaves];
     const u64 r = (u64)blockIdx.y * gridDim.x + blockIdx.x;
     if (r >= g.rows) return;
     const unsigned char *row = (const unsigned char *)g.x + r * g.ldx * Eight<kType>::kSize;
@@ -175,28 +170,24 @@ __global__ void __launch_bounds__(1024) k_norm_row(Norm g)
             act(x, c);
         }
     };
-    double first[1] = {0}, sums[2] = {0, 0};
+    double sum = 0, squares = 0;
     each([&](const float (&x)[8], u32) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) first[0] += (double)x[i];
+        for (int i = 0; i < 8; ++i) sum += (double)x[i];
     });
-    sums_of_row<kWaves>(first, first_part);
-    const float m = (float)(first[0] / g.cols);
+    const double mean = sum_of_row<kWaves>(sum, part[0]) / g.cols;
+    const float m = (float)mean, e = (float)(mean - m);
     each([&](const float (&x)[8], u32 c) {
-        float left = 0;                 // (eight differences: off by parts of them, as e is)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float d = c + i < g.cols ? x[i] - m : 0.0f;
-            left += d;
-            sums[1] += (double)d * d;
+            const double d = c + i < g.cols ? x[i] - m : 0.0f;
+            squares += d * d;
         }
-        sums[0] += (double)left;
     });
-    sums_of_row<kWaves>(sums, part);
-    const float e = (float)(sums[0] / g.cols);
-    const float rstd = 1.0f / sqrtf((float)(squares_around(sums[0], sums[1], sums[0] / g.cols) / g.cols) + g.eps);
+    const double var = sum_of_row<kWaves>(squares, part[1]) / g.cols - (mean - m) * (mean - m);
+    const float rstd = 1.0f / sqrtf((float)(var < 0 ? 0.0 : var) + g.eps);
     if (threadIdx.x == 0) {
-        if (g.mean) g.mean[r] = m + e;
+        if (g.mean) g.mean[r] = m;
         if (g.rstd) g.rstd[r] = rstd;
     }
     each([&](const float (&x)[8], u32 c) {
@@ -492,17 +483,16 @@ __global__ void __launch_bounds__(1024) k_norm_back_row(NormBack g)
             d[i] = c + i < g.cols ? d[i] * gamma[i] : 0.0f;
         }
     };
-    double sums[2] = {0, 0};
+    double sum = 0, inner = 0;
     for (u32 c = threadIdx.x * 8u; c < g.cols; c += 8u * kWaves * kWave) {
         read(c);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            sums[0] += (double)d[i];
-            sums[1] += c + i < g.cols ? (double)d[i] * (double)h[i] : 0.0;
+            sum += (double)d[i];
+            inner += c + i < g.cols ? (double)d[i] * (double)h[i] : 0.0;
         }
     }
-    sums_of_row<kWaves>(sums, part);
-    const float m0 = (float)(sums[0] / g.cols), m1 = (float)(sums[1] / g.cols);
+    const float m0 = (float)(sum_of_row<kWaves>(sum, part[0]) / g.cols), m1 = (float)(sum_of_row<kWaves>(inner, part[1]) / g.cols);
     for (u32 c = threadIdx.x * 8u; c < g.cols; c += 8u * kWaves * kWave) {
         read(c);
         float more[8] = {0, 0, 0, 0, 0, 0, 0, 0};
