@@ -568,7 +568,8 @@ int rtopk_layer_norm(const void *x, int type, uint64_t rows, uint64_t cols, uint
  * The sums over rows are taken in a fixed order: the same bits every time.
  *
  * dy     device, [rows][lddy] of dy_type; x device, [rows][ldx] of `type`
- * mean, rstd  device, [rows], as rtopk_layer_norm leaves them
+ * mean, rstd  device, [rows], as rtopk_layer_norm leaves them (h is off by what
+ *        the mean loses as binary32)
  * gamma  device, [cols], or null: 1
  * add    device, [rows][ldadd] of `type`, or null: the gradient that reaches x
  *        past the norm; only with dx

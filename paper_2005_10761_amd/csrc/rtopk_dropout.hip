@@ -5,7 +5,7 @@
 // u is a 16-bit draw of its own for each element: number e % 8 of the generator's group e / 8, e = row * cols + col. So the
 // mask depends on the element's place alone, not on strides or launches, the gradient is the same call on dy, and
 // what is kept is scaled by its true chance. One call of the generator for eight elements, 20 products of 16 cycles, stays under what 16-bit
-// elements take to be read and written: bound by memory, 16384 x 4096 bfloat16 with a residual 77 us, 5.2 TB/s, without 48, 5.6 TB/s.
+// elements take to be read and written: bound by memory, 16384 x 4096 bfloat16 with a residual 79 us, 5.1 TB/s, without 48, 5.6 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -29,7 +29,7 @@ struct Dropout {
 constexpr int kDropoutThreads = 256;
 
 // kWhole: a group of eight lies in one row, as neighbours (the matrices are one piece, then rows = 1; or cols % 8 = 0). Otherwise
-// element by element.
+// element by element: 16384 x 4095 bfloat16 with rows 4100 apart 288 us with a residual, 189 without, of one piece 76 and 44.
 template <int kType, bool kWhole>
 __global__ void __launch_bounds__(kDropoutThreads) k_dropout(Dropout g)
 {

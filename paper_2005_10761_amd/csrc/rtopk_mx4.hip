@@ -66,7 +66,7 @@ __device__ __forceinline__ u32 drawn_four_bits(float x, float inverse, u32 draw)
 // The conversion instruction goes up where 2^32 f + seed >= 2^32, for the first number of a pair with the seed as it is, for the second with the
 // seed turned left by one. The rule above is 2^32 f >= 65536 u + 32769 where 2^32 f is a whole number: seed = (65535 - u) 65536 +
 // 32767. Numbers of up to 11 bits, as halves and bfloat16 have, make f a whole number of 2^-32 wherever up is possible;
-// of binary32 the rule is computed (8192 x 4096 bfloat16 by rows 27 us so, 33 computed).
+// of binary32 the rule is computed (8192 x 4096 bfloat16 by 64 rows a workgroup 27 us so, 33 computed).
 template <int kType>
 __device__ __forceinline__ u32 drawn_four_bits(const float (&x)[8], u32 byte, const EightDraws &u)
 {
@@ -206,8 +206,8 @@ __global__ void __launch_bounds__(kPackThreads) k_pack_rows(ToPack g)
 }
 
 // Along columns, and turned over: a wavefront has 32 rows and 64 columns, a lane eight neighbouring rows of four columns; a
-// workgroup has eight blocks of 32 rows, which it writes as 128 bytes of each column. Bound by memory (4096 x 4096 binary32 15.7 us, 4.9
-// TB/s), drawn by the generator (8192 x 4096 bfloat16 26 us; to the nearest 20). Four rows of eight columns a lane, with shuffles, took 35.
+// workgroup has eight blocks of 32 rows, which it writes as 128 bytes of each column. Bound by memory (4096 x 4096 binary32 14.2 us, 5.4
+// TB/s), drawn by vector instructions, the generator's products a third of their cycles (8192 x 4096 bfloat16 24 us; to the nearest 17). Four rows of eight columns a lane, with shuffles, took 35.
 constexpr u32 kTurnWaves = 8, kTurnThreads = kTurnWaves * kWave, kTurnRows = kTurnWaves * kBlock;
 
 struct ToTurn {
@@ -516,8 +516,8 @@ __device__ __forceinline__ void write_group(void *out, u64 at, int type, f32x4 (
     }
 }
 
-// A tile, or a run of its contraction; the bias is added to the sums in registers, and the result written once. 8192 x 8192 x 8192 260 us,
-// 4220 10^12 operations a second; 2048 x 16384 x 4096 77 us, 3550. What bounds it: the matrix units are busy in 40 to 52% of the cycles at 2.0 to 2.2
+// A tile, or a run of its contraction; the bias is added to the sums in registers, and the result written once. 8192 x 8192 x 8192 266 us,
+// 4140 10^12 operations a second; 2048 x 16384 x 4096 78 us, 3520. What bounds it: the matrix units are busy in 49% and 38% of the cycles at 1.8 and 2.2
 // GHz; fed from registers, with the barriers and stores but without loads and reads from LDS, these take 194 and 57, and where all numbers are equal
 // 203 and 61 (power).
 template <class T, bool kWhole>
@@ -574,7 +574,7 @@ __global__ void __launch_bounds__(256) k_product4_join(Product4 g)
 // Few tokens: one read of the weights. A workgroup has 16 channels; its wavefronts share the contraction and add up in LDS,
 // in order. A lane's 16 bytes of a row of weights are a block, as the instruction takes them, at any alignment; the tokens are
 // the other operand, up to 16 of them. Neighbouring workgroups are on one XCD: they share the lines that the scales lie in. Bound by the read of the
-// weights and a launch: 16384 x 4096 with one token 10.4 us, 3.4 TB/s, with sixteen (quantised by a launch before) 15; 10000 x 1500 with one 4.6.
+// weights and a launch: 16384 x 4096 with one token 10 us, 3.5 TB/s, with sixteen (quantised by a launch before) 16; 10000 x 1500 with one 4.7.
 // ---------------------------------------------------------------------------
 constexpr u32 kFewTokens = 16;              // at most: what one instruction takes
 constexpr u32 kInOne = 8192;                // numbers of x that a workgroup can quantise for itself (one launch less)
@@ -788,7 +788,7 @@ struct Plan {
 // What a launch of tiles costs, in microseconds: a launch, and for the tiles that one compute unit gets one after the other what
 // comes before and after their slices, and the slices (128 bytes of every row). Two tiles of 64 or 128 share a unit. From 300
 // launches over eighteen shapes of 64 to 16384 rows and columns and contractions of 256 to 20000: the tile and runs that this picks took at
-// most 1.02 times the best ones' time.
+// most 1.02 times the best ones' time there, on the shapes that the figures were fitted to.
 double launch_cost(u32 edge, u64 tiles, double slices)
 {
     const double each = (double)((tiles + kUnits - 1) / kUnits);

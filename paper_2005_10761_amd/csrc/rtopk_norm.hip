@@ -326,7 +326,9 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_back_sums(NormBack g)
 // lane, the next row's x and dy on their way while this one's means are taken and its dx is written. One read of everything,
 // one write: a lane's share of dgamma and dbeta stays in registers over all of its rows, and goes to g.part, if that is there, to be
 // joined with the other workgroups'. Workgroups of the launch from g.groups on, if there are any, take the sums by themselves. Bound by
-// memory: 16384 x 4096 bfloat16 with `add` 103 us, 5.2 TB/s (dx and the sums by a kernel each 240); 700 x 1500 9.6 us, sums beside.
+// memory to 8192 columns: 16384 x 4096 bfloat16 with `add` 104 us, 5.2 TB/s (dx and the sums by a kernel each 240), 8192 x 8192 109, 4.9; 700 x 1500
+// 9.6 us, sums beside. Sixteen wavefronts a row (8193 to 16384 columns) have 128 registers a lane and spill: 264 bytes a lane of binary32, 184 of the
+// other types, read back with each row; 4096 x 12,000 bfloat16 201 us, 2.0 TB/s, 4096 x 16,384 228, 2.4.
 template <int kType, int kWavesPerRow, int kPieces>
 __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNormThreads) k_norm_back(NormBack g)
 {
@@ -456,7 +458,8 @@ __global__ void __launch_bounds__(kWavesPerRow > 4 ? kWavesPerRow * kWave : kNor
     }
 }
 
-// A longer row by one workgroup: its two means, then dx; dy and x are read twice, the second time from the caches.
+// A longer row by one workgroup: its two means, then dx; dy and x are read twice, the second time from the caches. With the sums over rows by
+// runs before it, 2000 x 20,000 bfloat16 with `add` 113 us (76 without the sums), 2.8 TB/s.
 template <int kType>
 __global__ void __launch_bounds__(1024) k_norm_back_row(NormBack g)
 {
