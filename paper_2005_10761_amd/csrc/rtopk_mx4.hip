@@ -202,7 +202,8 @@ __device__ __forceinline__ void pack_rows(const ToPack &g, u32 id)
 template <int kType, bool kDrawn, u32 kTileRows>
 __global__ void __launch_bounds__(kPackThreads) k_pack_rows(ToPack g)
 {
-    pack_rows<kType, kDrawn, kTileRows, kPackThreads>(g, blockIdx.x);
+    const u32 id = blockIdx.y * gridDim.x + blockIdx.x;
+    if (id < row_tiles<kTileRows>(g)) pack_rows<kType, kDrawn, kTileRows, kPackThreads>(g, id);
 }
 
 // Along columns, and turned over: a wavefront has 32 rows and 64 columns, a lane eight neighbouring rows of four columns; a
@@ -729,6 +730,9 @@ u64 blocks_of(u64 k) { return (k + kBlock - 1) / kBlock; }
 // a quantised operand [rows][k]: the distances of its rows and of its scales' blocks
 bool packed_ok(u64 rows, u64 k, u64 ldq, u64 lds) { return ldq >= bytes_of(k) && ldq <= kMostSize && lds >= rows && lds <= kMostSize; }
 
+// (a launch has less than 2^32 threads along x)
+dim3 row_grid(u32 tiles) { return dim3(std::min(tiles, 1u << 20), (tiles + (1u << 20) - 1) >> 20); }
+
 // 64 rows a workgroup where binary32 is rounded to the nearest, a row is longer than there are rows, and two workgroups a unit are
 // left; 16 elsewhere. us with 16 and with 64, of matrices that come from memory: binary32 4096 x 16384 66.0 / 61.4, 2048 x 16384 33.1 / 30.6,
 // 4096 x 8192 32.2 / 30.6; but 4096 x 4096 14.8 / 15.9, 16384 x 4096 53.2 / 57.7, drawn 4096 x 16384 66.5 / 68.6, 4096 x 8192 34.5 / 37.5;
@@ -738,12 +742,12 @@ int run_pack_rows(const ToPack &g, bool drawn, hipStream_t stream)
 {
     if constexpr (kType == RTOPK_F32) {
         if (!drawn && g.cols > g.rows && row_tiles<64>(g) >= 2 * kUnits) {
-            k_pack_rows<kType, false, 64><<<row_tiles<64>(g), kPackThreads, 0, stream>>>(g);
+            k_pack_rows<kType, false, 64><<<row_grid(row_tiles<64>(g)), kPackThreads, 0, stream>>>(g);
             return launched();
         }
     }
-    if (drawn) k_pack_rows<kType, true, 16><<<row_tiles<16>(g), kPackThreads, 0, stream>>>(g);
-    else k_pack_rows<kType, false, 16><<<row_tiles<16>(g), kPackThreads, 0, stream>>>(g);
+    if (drawn) k_pack_rows<kType, true, 16><<<row_grid(row_tiles<16>(g)), kPackThreads, 0, stream>>>(g);
+    else k_pack_rows<kType, false, 16><<<row_grid(row_tiles<16>(g)), kPackThreads, 0, stream>>>(g);
     return launched();
 }
 int run_pack_rows(const ToPack &g, int type, bool drawn, hipStream_t stream)
